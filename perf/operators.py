@@ -3,9 +3,11 @@
 Two operators, each with its gradient.  Both start from activations x (T x d) and a head weight W (V x d) and never
 return the logits z = x W^T + b:
 
-  xent     loss_t = logsumexp_v z_tv - z_t,target(t); rows whose target is ignore_index or outside the vocabulary give 0
+  xent     loss_t = logsumexp_v z_tv - z_t,target(t); rows whose target is ignore_index or outside the vocabulary are left
+           out: their loss, logsumexp and gradient are 0
   distill  loss_t = tau^2 * sum_j p_tj (log p_tj - log q_t,index(t,j)), p = softmax over the teacher's listed logits / tau,
-           q = softmax over the whole vocabulary of z / tau; entries whose index is outside the vocabulary are left out
+           q = softmax over the whole vocabulary of z / tau; entries whose index is outside the vocabulary are left out, and so are
+           rows with no entry
 
 A case has "op", "pass" ("fwd": loss and logsumexp; "train": those and dx, dW and, with a bias, db for given dloss),
 "dtype", the sizes T, d, V, whether there is a bias, and for distill K (listed teacher logits per token) and tau.
@@ -155,9 +157,10 @@ def run(s):
         p = t_exp / t_sum
         log_ratio = torch.where(valid, t - t_top - t_sum.log() - (z.gather(1, at) - lse[:, None]), torch.zeros_like(t))
         loss = tau * tau * (p * log_ratio).sum(1)
+    live = valid.any(1, keepdim=True)
+    lse = torch.where(live[:, 0], lse, torch.zeros_like(lse))
     if s["pass"] == "fwd":
         return {"loss": loss, "lse": lse}
-    live = valid.any(1, keepdim=True)
     dz = torch.where(live, e / total, torch.zeros_like(e[:, :1]))
     del z, e
     dz.scatter_add_(1, at, -p)
@@ -209,6 +212,7 @@ def exact(case, seed):
             full = torch.isfinite(listed_logits).any(1)
             teacher[full] = torch.softmax(listed_logits[full], dim=1)
             loss[rows] = tau * tau * (torch.special.xlogy(teacher, teacher) - teacher * logq).sum(1)
+        lse[rows] *= teacher.sum(1) > 0.5
         if case["pass"] == "train":
             dz = (logq.exp() * teacher.sum(1, keepdim=True) - teacher) * (tau * g[rows])[:, None]
             dx[rows] = dz @ w
