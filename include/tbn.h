@@ -136,6 +136,60 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
                  int64_t N, int32_t k, int alpha_mode, float *dW, float *dA, float *dalpha,
                  void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Losses of a head over a large vocabulary, with their gradients.  The training-side module above ends at B_hat and
+ * starts at G = dL/dB_hat; these calls are what lies between the two when the tiled layer is the last one (they take any
+ * weight: B_hat, or a full-precision matrix).  The paper trains with ordinary losses and does not define them.  With
+ *
+ *     z[t][v] = sum_i x[t][i] * w[v][i] + bias[v]           v < vocab
+ *
+ * the logits z are never written to memory as a whole: the forward keeps a maximum and a sum per token and 128 classes,
+ * the backward recomputes z and holds its gradient for one piece of the vocabulary at a time.
+ *
+ * tbn_linear_xent_fwd: softmax cross entropy.
+ *     lse[t] = log sum_v exp(z[t][v]),   loss[t] = lse[t] - z[t][targets[t]]
+ *   A token whose target is ignore_index, negative or >= vocab is left out: its loss and lse are 0, its gradient is 0, and
+ *   nothing in its row of x (infinities and NaN included) reaches any result.
+ * tbn_linear_distill_fwd: distillation from a teacher's top logits.  top_index, top_logit: T x K, the classes the teacher
+ *   lists for a token and its logits there (TBN_F32 or TBN_BF16), in any order.  With
+ *     p[t][j] = softmax_j(top_logit[t][j] / tau),   q[t][v] = softmax_v(z[t][v] / tau),   lse[t] = log sum_v exp(z[t][v] / tau)
+ *     loss[t] = tau^2 * sum_j p[t][j] * (log p[t][j] - log q[t][top_index[t][j]])
+ *   Entries whose index is negative or >= vocab, and entries whose logit is -infinity, are left out of p; a token with no
+ *   entry left is left out as above.  A class listed twice counts with both its probabilities.  1 <= K <= 1024, 0 < tau.
+ * Classes with a bias of -infinity (a masked vocabulary) have probability 0 and gradient 0.  A token whose kept logits
+ * hold a NaN or +infinity, or all of whose classes are masked, has a NaN or infinite loss; no other token is affected
+ * (in the backward its dloss of 0 does not help: 0 times NaN is NaN, in its row of dx and in dw).
+ *
+ * x: T x in_f, w: vocab x in_f, both of `dtype` (TBN_BF16 or TBN_F32).  bias: vocab floats or NULL.  targets: T int64.
+ * loss, lse: T floats.  Products are accumulated in fp32; fp32 operands are contracted as two fp16 halves of 11 bits each
+ * under a common power of two (about 22 bits of every element, ending at 2^-38 of the tensor's largest magnitude).
+ *
+ * tbn_linear_xent_bwd, tbn_linear_distill_bwd: lse as the forward wrote it, dloss: T floats (dL/dloss[t]: 1/T for a mean).
+ *     dz[t][v] = dloss[t] * tau * (q[t][v] - sum_{j: top_index[t][j] = v} p[t][j])       (cross entropy: one entry, p = 1, tau = 1)
+ *     dx[t][i] = sum_v dz[t][v] w[v][i],   dw[v][i] = sum_t dz[t][v] x[t][i],   dbias[v] = sum_t dz[t][v]
+ *   dx: T x in_f of `dtype`, or NULL.  dw: vocab x in_f of dw_dtype (TBN_F32: what tbn_tile_bwd takes as G; TBN_BF16), or
+ *   NULL.  dbias: vocab floats or NULL.  All are overwritten.  With bf16 operands dz is rounded to bf16 for the two products
+ *   (dbias is summed before that rounding); sums are fp32.
+ * workspace: tbn_linear_xent_workspace_bytes(..., backward) / tbn_linear_distill_workspace_bytes(..., backward) bytes, with
+ *   backward = 0 or 1 for the call it is meant for.  T == 0: the forward is a no-op, the backward writes zeros to dw and dbias.
+ * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1024: TBN_ERR_UNSUPPORTED.
+ */
+size_t tbn_linear_xent_workspace_bytes(int64_t T, int32_t in_f, int32_t vocab, int dtype, int backward);
+int tbn_linear_xent_fwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                        const int64_t *targets, int64_t ignore_index, float *loss, float *lse,
+                        void *workspace, size_t workspace_bytes, void *stream);
+int tbn_linear_xent_bwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                        const int64_t *targets, int64_t ignore_index, const float *lse, const float *dloss, void *dx,
+                        void *dw, int dw_dtype, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+size_t tbn_linear_distill_workspace_bytes(int64_t T, int32_t in_f, int32_t vocab, int dtype, int32_t K, int backward);
+int tbn_linear_distill_fwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                           const int64_t *top_index, const void *top_logit, int top_dtype, int32_t K, float tau, float *loss,
+                           float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int tbn_linear_distill_bwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                           const int64_t *top_index, const void *top_logit, int top_dtype, int32_t K, float tau, const float *lse,
+                           const float *dloss, void *dx, void *dw, int dw_dtype, float *dbias,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
 /* Pack an existing real-valued tile (Sec. 5.1: tiles are stored one bit per element):
  * src[i] > 0 -> bit 1, else 0.  src: q fp32 values.  tile_bits: tbn_tile_words(q) words. */
 int tbn_pack_tile(const float *src, int64_t q, uint32_t *tile_bits, void *stream);

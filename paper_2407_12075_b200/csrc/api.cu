@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "head_loss.cuh"
 
 namespace tbn {
 
@@ -124,6 +125,44 @@ MlpFork *mlp_fork(cudaStream_t s)
         f.state = ok ? 1 : -1;
     }
     return f.state == 1 ? &f : nullptr;
+}
+
+// ---- losses of a large-vocabulary head: validation shared by the entry points --------------------------------------
+constexpr int64_t kHeadMost = 0x7fffffffLL - 1024;     // tile and row indices are 32-bit
+
+bool head_sizes_ok(int64_t T, int32_t in_f, int32_t vocab)
+{
+    return T >= 0 && in_f > 0 && vocab > 0 && T <= kHeadMost && in_f <= kHeadMost && vocab <= kHeadMost;
+}
+
+int head_call(head::HeadCall &c, bool backward, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (c.T < 0 || c.d <= 0 || c.V <= 0 || !valid_dtype(c.dtype)) return TBN_ERR_INVALID_ARG;
+    if (c.K > 0 && (!valid_dtype(c.top_dtype) || !(c.tau > 0.0f) || !(c.tau < 3.0e38f) || !(1.0f / c.tau < 3.0e38f))) return TBN_ERR_INVALID_ARG;
+    if (backward && c.dw && !valid_dtype(c.dw_dtype)) return TBN_ERR_INVALID_ARG;
+    if (!head_sizes_ok(c.T, c.d, c.V) || c.K > head::kMaxListed) return TBN_ERR_UNSUPPORTED;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (!aligned16(c.x) || !aligned16(c.w) || !aligned16(c.dx) || !aligned16(c.dw) || !aligned16(workspace)) return TBN_ERR_INVALID_ARG;
+    const void *four[] = {c.bias, c.loss_out, c.lse_out, c.lse, c.dloss, c.db, c.top_dtype == TBN_F32 ? c.top_logit : nullptr};
+    for (const void *q : four)
+        if (reinterpret_cast<uintptr_t>(q) & 3u) return TBN_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(c.targets) & 7u) || (reinterpret_cast<uintptr_t>(c.top_index) & 7u) || (reinterpret_cast<uintptr_t>(c.top_logit) & 1u))
+        return TBN_ERR_INVALID_ARG;
+    if (c.T == 0) {                                    // data pointers may be null; the sums over no tokens are zero
+        if (!backward) return TBN_OK;
+        const size_t dw_bytes = (size_t)c.V * c.d * dtype_bytes(c.dw_dtype);
+        if (c.dw && cudaMemsetAsync(c.dw, 0, dw_bytes, s) != cudaSuccess) return TBN_ERR_CUDA;
+        if (c.db && cudaMemsetAsync(c.db, 0, (size_t)c.V * 4, s) != cudaSuccess) return TBN_ERR_CUDA;
+        return TBN_OK;
+    }
+    if (!c.x || !c.w) return TBN_ERR_INVALID_ARG;
+    if (c.K > 0 ? (!c.top_index || !c.top_logit) : !c.targets) return TBN_ERR_INVALID_ARG;
+    if (backward ? (!c.lse || !c.dloss) : (!c.loss_out || !c.lse_out)) return TBN_ERR_INVALID_ARG;
+    if (backward && !c.dx && !c.dw && !c.db) return TBN_OK;
+    if (!workspace || workspace_bytes < head::workspace_bytes(c.T, c.d, c.V, c.dtype, c.K, backward)) return TBN_ERR_WORKSPACE;
+    c.status = device_status_ptr();
+    if (!c.status) return TBN_ERR_CUDA;
+    return backward ? head::backward(c, workspace, s) : head::forward(c, workspace, s);
 }
 
 // Validation shared by the fully-connected and convolution entry points.
@@ -804,6 +843,64 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
     if (!workspace || !aligned16(workspace) || workspace_bytes < tile_bwd_workspace_bytes(N, k)) return TBN_ERR_WORKSPACE;
     return launch_tile_bwd(G, tile_bits, alpha, W, A, N, k, alpha_mode == TBN_ALPHA_PER_TILE, dW, dA, dalpha, workspace,
                            static_cast<cudaStream_t>(stream)) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
+}
+
+// ---- losses of a large-vocabulary head ------------------------------------------------------------------------------
+size_t tbn_linear_xent_workspace_bytes(int64_t T, int32_t in_f, int32_t vocab, int dtype, int backward)
+{
+    if (!head_sizes_ok(T, in_f, vocab) || T == 0 || !valid_dtype(dtype)) return 0;
+    return head::workspace_bytes(T, in_f, vocab, dtype, 0, backward != 0);
+}
+
+size_t tbn_linear_distill_workspace_bytes(int64_t T, int32_t in_f, int32_t vocab, int dtype, int32_t K, int backward)
+{
+    if (!head_sizes_ok(T, in_f, vocab) || T == 0 || !valid_dtype(dtype) || K <= 0 || K > head::kMaxListed) return 0;
+    return head::workspace_bytes(T, in_f, vocab, dtype, K, backward != 0);
+}
+
+int tbn_linear_xent_fwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                        const int64_t *targets, int64_t ignore_index, float *loss, float *lse,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    head::HeadCall c = {};
+    c.x = x; c.w = w; c.dtype = dtype; c.T = T; c.d = in_f; c.V = vocab; c.bias = bias;
+    c.targets = targets; c.ignore_index = ignore_index; c.tau = 1.0f; c.loss_out = loss; c.lse_out = lse;
+    return head_call(c, false, workspace, workspace_bytes, stream);
+}
+
+int tbn_linear_xent_bwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                        const int64_t *targets, int64_t ignore_index, const float *lse, const float *dloss, void *dx,
+                        void *dw, int dw_dtype, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    head::HeadCall c = {};
+    c.x = x; c.w = w; c.dtype = dtype; c.T = T; c.d = in_f; c.V = vocab; c.bias = bias;
+    c.targets = targets; c.ignore_index = ignore_index; c.tau = 1.0f; c.lse = lse; c.dloss = dloss;
+    c.dx = dx; c.dx_dtype = dtype; c.dw = dw; c.dw_dtype = dw_dtype; c.db = dbias;
+    return head_call(c, true, workspace, workspace_bytes, stream);
+}
+
+int tbn_linear_distill_fwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                           const int64_t *top_index, const void *top_logit, int top_dtype, int32_t K, float tau, float *loss,
+                           float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (K <= 0) return TBN_ERR_INVALID_ARG;
+    head::HeadCall c = {};
+    c.x = x; c.w = w; c.dtype = dtype; c.T = T; c.d = in_f; c.V = vocab; c.bias = bias;
+    c.top_index = top_index; c.top_logit = top_logit; c.top_dtype = top_dtype; c.K = K; c.tau = tau; c.loss_out = loss; c.lse_out = lse;
+    return head_call(c, false, workspace, workspace_bytes, stream);
+}
+
+int tbn_linear_distill_bwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,
+                           const int64_t *top_index, const void *top_logit, int top_dtype, int32_t K, float tau, const float *lse,
+                           const float *dloss, void *dx, void *dw, int dw_dtype, float *dbias,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (K <= 0) return TBN_ERR_INVALID_ARG;
+    head::HeadCall c = {};
+    c.x = x; c.w = w; c.dtype = dtype; c.T = T; c.d = in_f; c.V = vocab; c.bias = bias;
+    c.top_index = top_index; c.top_logit = top_logit; c.top_dtype = top_dtype; c.K = K; c.tau = tau; c.lse = lse; c.dloss = dloss;
+    c.dx = dx; c.dx_dtype = dtype; c.dw = dw; c.dw_dtype = dw_dtype; c.db = dbias;
+    return head_call(c, true, workspace, workspace_bytes, stream);
 }
 
 int tbn_linear_compact_fwd(const void *z, int64_t T, int32_t rz, int32_t kz, const float *alpha_z, int alpha_mode_z, int act_z,

@@ -1,0 +1,111 @@
+// Internal interface between the two translation units of the head losses: head_loss.cu (labels, packing, reductions,
+// orchestration) and tc_head.cu (the tcgen05 contractions).
+#pragma once
+
+#include "common.cuh"
+
+namespace tbn {
+namespace head {
+
+constexpr int kTile = 256;                 // tokens x classes of one output tile (two CTAs, 128 rows each)
+constexpr int kStatCols = 128;             // classes behind one (maximum, sum, dot) triple
+constexpr int kMaxSplits = 16;
+
+__host__ __device__ inline int64_t round_up64(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
+
+// What the epilogues need to know about one kept token row.
+struct __align__(16) RowInfo {
+    float lse2;                            // log2 of the row's sum of exponentials (backward)
+    float g;                               // dloss * tau (* the fp16 scale of the gradient): backward
+    int32_t label;                         // cross entropy: the target class
+    int32_t row;                           // the row's index in the caller's tensors
+};
+
+// Powers of two that bring the fp32 operands into the range of fp16 (all 1 for bf16 operands), and their inverses.
+struct Scales { float x, w, g, inv_x, inv_w, inv_g; };
+
+// A bf16 (one plane) or fp32 (two fp16 planes: high part, remainder) operand as the contractions read it.
+struct Operand {
+    const void *data;
+    int64_t rows, plane_rows;              // rows that exist, rows between two planes
+    int32_t cols, ld;                      // columns that exist, row pitch in elements (a multiple of 8)
+};
+
+struct LogitsArgs {                        // logits of all kept tokens against classes [v0, v0 + width)
+    Operand x, w;
+    int planes;
+    const int32_t *n_live;
+    const RowInfo *rows;
+    const Scales *scales;                  // null: all 1
+    const float *bias;                     // V or null
+    float scale2;                          // log2(e) / tau
+    int64_t T, Tpad;
+    int32_t V, v0, width;
+    const int32_t *list_idx;               // distillation: [T][K] ascending, INT32_MAX behind the last entry; else null
+    const float *list_p;
+    int32_t K;
+    // forward: [stat column][Tpad]
+    float *part_max, *part_sum, *part_dot;
+    // backward
+    void *dz;                              // [planes][Tpad][ldz]
+    int32_t ldz;
+    float *col_part;                       // [Tpad / 32][ldz] or null
+    int *status;
+};
+int launch_head_stats(const LogitsArgs &a, cudaStream_t s);
+int launch_head_dz(const LogitsArgs &a, cudaStream_t s);
+
+struct GradArgs {                          // dX (+)= dz W, dW = dz^T X for one piece of the vocabulary
+    Operand x, w;
+    int planes;
+    const int32_t *n_live;
+    const RowInfo *rows;
+    const Scales *scales;
+    const void *dz;
+    int64_t T, Tpad;
+    int32_t d, V, v0, width, ldz;
+    bool want_dx, want_dw;
+    // dX: into `dx` by row when no slots are used, else fp32 partial sums [split][Tpad][d], added to when `dx_add`
+    void *dx;
+    int dx_bf16;
+    float *dx_slots;
+    int32_t dx_splits;
+    int dx_add, dx_last;                   // dx_last: this piece is the last one (without splits it finishes dx)
+    // dW: rows v0 .. of `dw`, or fp32 partial sums [split][round_up(width, 256)][d]
+    void *dw;
+    int dw_bf16;
+    float *dw_slots;
+    int32_t dw_splits;
+    int *status;
+};
+int launch_head_grads(const GradArgs &a, cudaStream_t s);
+
+
+// One call of either loss, as the C entry points hand it over.
+struct HeadCall {
+    const void *x, *w;
+    int dtype;                             // of x and w
+    int64_t T;
+    int32_t d, V;
+    const float *bias;
+    const int64_t *targets;                // cross entropy
+    int64_t ignore_index;
+    const int64_t *top_index;              // distillation: K > 0
+    const void *top_logit;
+    int top_dtype;
+    int32_t K;
+    float tau;
+    float *loss_out, *lse_out;             // forward
+    const float *lse, *dloss;              // backward
+    void *dx, *dw;
+    int dx_dtype, dw_dtype;
+    float *db;
+    int *status;
+};
+constexpr int32_t kMaxListed = 1024;
+size_t workspace_bytes(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward);
+int forward(const HeadCall &c, void *workspace, cudaStream_t s);
+int backward(const HeadCall &c, void *workspace, cudaStream_t s);
+
+}  // namespace head
+}  // namespace tbn

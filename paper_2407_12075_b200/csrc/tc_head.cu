@@ -1,0 +1,703 @@
+// The contractions behind the head losses, on tcgen05 with CTA pairs.
+//
+//   logits   Z[t][v]  = sum_i X[t][i] W[v][i]          consumed on chip: by running maxima and sums (forward), or by the
+//                                                      softmax gradient dz, which is written piece by piece (backward)
+//   dX[t][i] (+)= sum_v dz[t][v] W[v][i]               dz K-major, W with its output index contiguous
+//   dW[v][i]  = sum_t dz[t][v] X[t][i]                 both operands with their output index contiguous
+//
+// Every operand stays in the row-major form it has in memory: "K-major" and "MN-major" are the two operand forms of
+// tcgen05.mma, chosen by descriptor bits, so no product needs a transposed copy.
+//
+// A pair of CTAs (cta_group::2) computes a 256 x 256 tile: each CTA stages 128 rows of A and 128 of B per 64-element
+// step, so a byte staged feeds twice the multiplications of a 128 x 256 tile on one CTA (per 64-element step and SM:
+// 32 KB instead of 48 KB for the same 4.2 MFLOP), which is what keeps shared memory and L2 below the tensor pipe.
+// Warp roles per CTA: 0 = TMA producer, 1 = MMA issuer (the first CTA of the pair only), 2-9 = epilogue, two warps per
+// tensor-memory quadrant, 128 columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
+// main loop of the next.
+//
+// fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products hi*hi, hi*lo
+// and lo*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.
+//
+// Same conventions as the other tcgen05 kernels: every wait is bounded, a wait that gives up records the status and the
+// kernel winds down and returns.
+#include <cuda_fp16.h>
+
+#include <climits>
+
+#include "head_loss.cuh"
+#include "tc_common.cuh"
+
+namespace tbn {
+namespace head {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr uint32_t kSideBytes = 128 * 128;             // one operand, one plane, one CTA: 128 rows x 64 elements
+constexpr uint32_t kStageBudget = 6 * 2 * kSideBytes;  // 192 KB of stages
+constexpr uint32_t kTmemCols = 512;
+constexpr int kGroupM = 32;                            // token tiles that share a sweep over the classes
+
+enum { kStats = 0, kDz = 1, kGrads = 2 };
+
+struct Control {
+    uint64_t full[6], empty[6], d_full[2], d_empty[2];
+    uint32_t tmem_base;
+    int abort_flag;
+    alignas(16) float bias[kEpiWarps][kStatCols];
+};
+
+// Two jobs at most: (0) dX and (1) dW.  The logits kernels use job 0 alone.
+struct Maps { CUtensorMap a[2], b[2]; };
+
+struct LogitsParams {
+    const int32_t *n_live;
+    const RowInfo *rows;
+    const Scales *scales;
+    const float *bias;
+    float scale2;
+    int64_t Tpad;
+    int32_t V, v0, width;
+    const int32_t *list_idx;
+    const float *list_p;
+    int32_t K;
+    float *part_max, *part_sum, *part_dot;
+    void *dz;
+    int32_t ldz;
+    float *col_part;
+};
+struct GradParams {
+    const int32_t *n_live;
+    const RowInfo *rows;
+    const Scales *scales;
+    int64_t Tpad;
+    int32_t d, v0, width;
+    int32_t want_dx, want_dw;
+    void *dx;
+    float *dx_slots;
+    int32_t dx_splits, dx_bf16, dx_add, dx_last;
+    void *dw;
+    float *dw_slots;
+    int32_t dw_splits, dw_bf16;
+};
+struct KernelParams { LogitsParams l; GradParams g; int *status; };
+
+// ---- PTX forms of the CTA pair ------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+// The copy lands in this CTA; its bytes are counted on the barrier of the pair's first CTA.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
+                                         uint32_t leader) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 ad, bd;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 ad, {%1, %3};\n\t"
+        "mov.b64 bd, {%2, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], ad, bd, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// Arrives on the barrier at this offset in both CTAs once the MMAs issued so far have completed.
+__device__ __forceinline__ void commit_pair(uint32_t bar, uint32_t leader) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t.reg .b16 mask;\n\t"
+        "mov.b16 mask, 3;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], mask;\n\t}"
+        ::"r"(bar), "r"(leader) : "memory");
+}
+__device__ __forceinline__ float exp2_approx(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// ---- tile enumeration (the same arithmetic in every role) ----------------------------------------------
+struct Tile {
+    int job, split;
+    int32_t m0, n0;                        // first row of the pair's tile on either side
+    int32_t kb0, kb1;                      // 64-element steps
+};
+
+struct Schedule {
+    int32_t total;
+    // logits
+    int32_t mt, nt, kb;
+    // gradients: tiles of job 0 come first when its contraction is the longer one
+    int32_t first_job, count_first, nt_d, kb_job[2], splits[2], mt_job[2];
+
+    template <int MODE>
+    __device__ __forceinline__ void init(const KernelParams &p, int32_t n_live, int32_t k_logits) {
+        if (MODE != kGrads) {
+            mt = (n_live + kTile - 1) / kTile;
+            nt = (p.l.width + kTile - 1) / kTile;
+            kb = k_logits;
+            total = mt * nt;
+        } else {
+            nt_d = (p.g.d + kTile - 1) / kTile;
+            mt_job[0] = p.g.want_dx ? (n_live + kTile - 1) / kTile : 0;
+            mt_job[1] = p.g.want_dw ? (p.g.width + kTile - 1) / kTile : 0;
+            kb_job[0] = (p.g.width + 63) / 64;
+            kb_job[1] = (n_live + 63) / 64;
+            splits[0] = p.g.dx_splits;
+            splits[1] = p.g.dw_splits;
+            first_job = kb_job[1] / splits[1] > kb_job[0] / splits[0] ? 1 : 0;
+            count_first = mt_job[first_job] * nt_d * splits[first_job];
+            total = count_first + mt_job[first_job ^ 1] * nt_d * splits[first_job ^ 1];
+        }
+    }
+    template <int MODE>
+    __device__ __forceinline__ Tile get(int32_t i) const {
+        Tile t;
+        if (MODE != kGrads) {
+            const int32_t per_group = kGroupM * nt, g = i / per_group, rem = i - g * per_group;
+            const int32_t gm = min(kGroupM, mt - g * kGroupM), n = rem / gm;
+            t.job = 0; t.split = 0;
+            t.m0 = (g * kGroupM + (rem - n * gm)) * kTile;
+            t.n0 = n * kTile;
+            t.kb0 = 0; t.kb1 = kb;
+        } else {
+            t.job = first_job;
+            if (i >= count_first) { t.job ^= 1; i -= count_first; }
+            const int32_t row = i / nt_d;
+            t.n0 = (i - row * nt_d) * kTile;
+            t.split = row / mt_job[t.job];
+            t.m0 = (row - t.split * mt_job[t.job]) * kTile;
+            t.kb0 = (int32_t)((int64_t)t.split * kb_job[t.job] / splits[t.job]);
+            t.kb1 = (int32_t)((int64_t)(t.split + 1) * kb_job[t.job] / splits[t.job]);
+        }
+        return t;
+    }
+};
+
+// The sparse side of a row: the target class with probability 1, or the teacher's ascending list.
+struct Listed {
+    const int32_t *idx;
+    const float *p;
+    int32_t pos, count, next;
+
+    __device__ __forceinline__ void begin(const LogitsParams &l, const RowInfo &r, bool live, int32_t first) {
+        if (l.list_idx == nullptr) {
+            idx = nullptr;
+            next = live && r.label >= first ? r.label : INT_MAX;
+            return;
+        }
+        idx = l.list_idx + (int64_t)r.row * l.K;
+        p = l.list_p + (int64_t)r.row * l.K;
+        count = live ? l.K : 0;
+        int32_t lo = 0, hi = count;                    // first entry >= first
+        while (lo < hi) {
+            const int32_t mid = (lo + hi) >> 1;
+            if (__ldg(idx + mid) < first) lo = mid + 1; else hi = mid;
+        }
+        pos = lo;
+        next = pos < count ? __ldg(idx + pos) : INT_MAX;
+    }
+    __device__ __forceinline__ float weight() const { return idx ? __ldg(p + pos) : 1.0f; }
+    __device__ __forceinline__ void step() {
+        if (!idx) { next = INT_MAX; return; }
+        ++pos;
+        next = pos < count ? __ldg(idx + pos) : INT_MAX;
+    }
+};
+
+// 32 x 32 values, lane = row: returns in lane c the sum over the rows of column c (v is overwritten).
+__device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) {
+        const bool upper = (lane & s) != 0;
+#pragma unroll
+        for (int i = 0; i < s; ++i) {
+            const float send = upper ? v[i] : v[i + s], keep = upper ? v[i + s] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, s);
+        }
+    }
+    return v[0];
+}
+
+template <int PL>
+__device__ __forceinline__ void store_dz(const KernelParams &p, int64_t row, int32_t col, const float (&v)[32]) {
+    uint32_t pk[16];
+    if (PL == 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        uint16_t *dst = static_cast<uint16_t *>(p.l.dz) + row * p.l.ldz + col;
+        st_global_v8(dst, pk);
+        st_global_v8(dst + 16, pk + 8);
+    } else {
+        uint32_t lo[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+            const float2 back = __half22float2(h);
+            const __half2 r = __floats2half2_rn(v[2 * i] - back.x, v[2 * i + 1] - back.y);
+            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+            lo[i] = *reinterpret_cast<const uint32_t *>(&r);
+        }
+        uint16_t *dst = static_cast<uint16_t *>(p.l.dz) + row * p.l.ldz + col;
+        st_global_v8(dst, pk);
+        st_global_v8(dst + 16, pk + 8);
+        dst += p.l.Tpad * p.l.ldz;
+        st_global_v8(dst, lo);
+        st_global_v8(dst + 16, lo + 8);
+    }
+}
+
+// ---- the kernel ------------------------------------------------------------------------------------------
+template <int MODE, int PL, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelParams p, const int32_t k_logits)
+{
+    constexpr uint32_t kStage = 2 * PL * kSideBytes;
+    constexpr int kStages = kStageBudget / kStage;
+    constexpr uint32_t kFmt = PL == 1 ? 1u : 0u;       // bf16, or fp16 planes
+    // instruction descriptor: D fp32, M = 256, N = 256; bits 15 / 16 select the MN-major form of A / B
+    constexpr uint32_t kIdesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    // 128-byte swizzle, 8-row groups 1024 bytes apart, descriptor version 1
+    constexpr uint32_t kDescHi = 64u | (1u << 14) | (2u << 29);
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+    const uint32_t stage0 = raw + pad;
+    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget);
+    volatile int *abort_flag = &ctl->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int detail = (int)(blockIdx.x & 0xffff);
+
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
+        ctl->abort_flag = 0;
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    pdl_wait();
+
+    const int32_t n_live = *(MODE == kGrads ? p.g.n_live : p.l.n_live);
+    Schedule sched = {};
+    sched.init<MODE>(p, n_live, k_logits);
+    const int32_t first = blockIdx.x >> 1, stride = gridDim.x >> 1;
+    bool ok = true;
+
+    if (warp == 0) {
+        // ---------------- TMA producer ----------------
+        Pipe px;
+        for (int32_t i = first; i < sched.total && ok; i += stride) {
+            const Tile t = sched.get<MODE>(i);
+            const int32_t a0 = t.m0 + (int32_t)rank * 128, b0 = t.n0 + (int32_t)rank * 128;
+            const CUtensorMap *ma = &maps.a[t.job], *mb = &maps.b[t.job];
+            for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
+                ok = wait_bar(smem_u32(&ctl->empty[px.stage]), px.phase ^ 1u, abort_flag, p.status, (40 << 24) | (px.stage << 16) | detail);
+                if (!ok) break;
+                if (lane == 0) {
+                    const uint32_t own = smem_u32(&ctl->full[px.stage]), bar = map_to_rank(own, 0);
+                    if (rank == 0) mbar_arrive_expect_tx(own, 2 * kStage);
+                    const uint32_t sa = stage0 + px.stage * kStage, sb = sa + PL * kSideBytes;
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl) {
+                        const uint32_t da = sa + pl * kSideBytes, db = sb + pl * kSideBytes;
+                        if (MODE != kGrads) {
+                            tma_load_pair(da, ma, kb * 64, a0, pl, bar);
+                            tma_load_pair(db, mb, kb * 64, p.l.v0 + b0, pl, bar);
+                        } else {
+                            if (t.job == 0) {                              // dz: tokens x classes, contraction over classes
+                                tma_load_pair(da, ma, kb * 64, a0, pl, bar);
+                            } else {                                       // dz: contraction over tokens
+                                tma_load_pair(da, ma, a0, kb * 64, pl, bar);
+                                tma_load_pair(da + kSideBytes / 2, ma, a0 + 64, kb * 64, pl, bar);
+                            }
+                            const int32_t krow = (t.job == 0 ? p.g.v0 : 0) + kb * 64;
+                            tma_load_pair(db, mb, b0, krow, pl, bar);
+                            tma_load_pair(db + kSideBytes / 2, mb, b0 + 64, krow, pl, bar);
+                        }
+                    }
+                }
+                __syncwarp();
+                px.advance(kStages);
+            }
+        }
+        if (!ok) {                                     // let copies in flight land before the shared memory goes away
+            const uint64_t t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < 20000000ull) {}
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA issuer: the whole warp runs the loop, one elected lane issues ----------------
+        if (rank == 0) {
+            const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0);
+            const uint32_t leader = elect_one();
+            Pipe px, pd;
+            for (int32_t i = first; i < sched.total && ok; i += stride) {
+                const Tile t = sched.get<MODE>(i);
+                ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d_addr = tmem_u + pd.stage * kTile;
+                const bool a_mn = MODE == kGrads && t.job == 1, b_mn = MODE == kGrads;
+                const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                // low descriptor word: start address in 16-byte units, leading offset (between 64-element panels of the
+                // MN-major form: 8192 bytes).  A step of 16 along K: 32 bytes inside the swizzled row, or two 8-row groups.
+                const uint32_t a_hi = (a_mn ? 512u : 1u) << 16, b_hi = (b_mn ? 512u : 1u) << 16;
+                const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
+                for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
+                    ok = wait_bar(smem_u32(&ctl->full[px.stage]), px.phase, abort_flag, p.status, (42 << 24) | (px.stage << 16) | detail);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = stage0 + px.stage * kStage, sb = sa + PL * kSideBytes;
+                    const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
+                    constexpr uint32_t kPlane = kSideBytes >> 4;
+#pragma unroll
+                    for (int term = 0; term < (PL == 1 ? 1 : 3); ++term) {       // hi*hi, lo*hi, hi*lo
+                        const uint32_t at = a_lo + (term == 1 ? kPlane : 0u), bt = b_lo + (term == 2 ? kPlane : 0u);
+#pragma unroll
+                        for (int st = 0; st < 4; ++st)
+                            mma_pair(d_addr, at + st * a_step, bt + st * b_step, kDescHi, idesc,
+                                     term > 0 || st > 0 ? 1u : (uint32_t)(kb > t.kb0), leader);
+                    }
+                    commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
+                    px.advance(kStages);
+                }
+                if (!ok) break;
+                commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
+                pd.advance(2);
+            }
+            if (!ok) {                                 // no MMA may still read shared or tensor memory when they go away
+                const uint64_t t0 = global_timer_ns();
+                while (global_timer_ns() - t0 < 20000000ull) {}
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- epilogue: thread = row, 128 columns in chunks of 32 ----------------
+        const int ew = warp - 2, qd = warp & 3, half = ew >> 2;
+        const uint32_t t_lane = tmem_base + ((uint32_t)(qd * 32) << 16) + (uint32_t)half * 128;
+        Pipe pd;
+        float sc = 1.0f, inv_g = 1.0f;
+        if (MODE != kGrads) {
+            sc = p.l.scale2;
+            if (p.l.scales) sc *= p.l.scales->inv_x * p.l.scales->inv_w;
+        } else if (p.g.scales) {
+            inv_g = p.g.scales->inv_g;
+        }
+        for (int32_t i = first; i < sched.total; i += stride) {
+            const Tile t = sched.get<MODE>(i);
+            const int32_t row = t.m0 + (int32_t)rank * 128 + qd * 32 + lane;
+            const int32_t col0 = t.n0 + half * 128;
+            const bool live = row < n_live;
+            RowInfo info = {0.0f, 0.0f, -1, 0};
+            Listed list;
+            const float *bias_s = ctl->bias[ew];
+            if (MODE != kGrads) {
+                if (live) info = p.l.rows[row];
+                list.begin(p.l, info, live, p.l.v0 + col0);
+                if (BIAS) {                            // classes past the end get -infinity
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int32_t c = col0 + j * 32 + lane;
+                        ctl->bias[ew][j * 32 + lane] = c < p.l.width ? __ldg(p.l.bias + p.l.v0 + c) * p.l.scale2 : -INFINITY;
+                    }
+                    __syncwarp();
+                }
+            } else if (t.job == 0 && live) {
+                info.row = p.g.rows[row].row;
+            }
+            ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t t_acc = t_lane + pd.stage * kTile;
+
+            if (MODE == kStats) {
+                float m = -INFINITY, l = 0.0f, dot = 0.0f;
+#pragma unroll 1
+                for (int ch = 0; ch < 4; ++ch) {
+                    const int32_t c0 = col0 + ch * 32;
+                    uint32_t r[32];
+                    tmem_ld_32x32(t_acc + ch * 32, r);
+                    tc_wait_ld();
+                    float v[32];
+                    if (BIAS) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(r[j]), sc, bias_s[ch * 32 + j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+                        if (c0 + 32 > p.l.width) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
+                        }
+                    }
+                    const float vs = BIAS ? 1.0f : sc;
+                    while (list.next < p.l.v0 + c0 + 32) {
+                        const int rel = list.next - (p.l.v0 + c0);
+                        float z = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z = rel == j ? v[j] : z;
+                        const float w = list.weight();
+                        if (w != 0.0f) dot = fmaf(w, z * vs, dot);     // 0 times a class at -infinity is 0
+                        list.step();
+                    }
+                    __syncwarp();
+                    float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                    for (int j = 4; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], v[j]);
+                    const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * vs);
+                    const float ref = m_new == -INFINITY ? 0.0f : m_new;
+                    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s4[j & 3] += exp2_approx(fmaf(v[j], vs, -ref));
+                    l = l * exp2_approx(m - ref) + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+                    m = m_new;
+                }
+                if (live) {
+                    const int64_t at = (int64_t)((p.l.v0 + col0) / kStatCols) * p.l.Tpad + row;
+                    p.l.part_max[at] = m;
+                    p.l.part_sum[at] = l;
+                    p.l.part_dot[at] = dot;
+                }
+            } else if (MODE == kDz) {
+                const bool all_live = __all_sync(0xffffffffu, live);
+#pragma unroll 1
+                for (int ch = 0; ch < 4; ++ch) {
+                    const int32_t c0 = col0 + ch * 32;
+                    uint32_t r[32];
+                    tmem_ld_32x32(t_acc + ch * 32, r);
+                    tc_wait_ld();
+                    float v[32];
+                    if (BIAS) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(r[j]), sc, bias_s[ch * 32 + j]) - info.lse2;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(r[j]), sc, -info.lse2);
+                        if (c0 + 32 > p.l.width) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
+                    while (list.next < p.l.v0 + c0 + 32) {
+                        const int rel = list.next - (p.l.v0 + c0);
+                        const float sub = info.g * list.weight();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
+                        list.step();
+                    }
+                    __syncwarp();
+                    if (!all_live) {                   // rows behind the last kept token: exact zeros, whatever was staged
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = live ? v[j] : 0.0f;
+                    }
+                    store_dz<PL>(p, row, c0, v);
+                    if (p.l.col_part) {
+                        const float s = column_sums(v, lane);
+                        p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
+                    }
+                }
+            } else {
+                const GradParams &g = p.g;
+                const bool empty = t.kb0 >= t.kb1;     // nothing was contracted: the accumulator holds no result
+                const bool is_dx = t.job == 0;
+                const float scale = g.scales ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : 1.0f;
+                const bool in = is_dx ? live : row < g.width;
+                const int splits = is_dx ? g.dx_splits : g.dw_splits;
+                const int64_t slot_rows = is_dx ? g.Tpad : round_up64(g.width, kTile);
+                float *slot = is_dx ? g.dx_slots : g.dw_slots;
+                if (slot) slot += ((int64_t)t.split * slot_rows + row) * g.d;
+                const bool to_slot = slot != nullptr && (splits > 1 || !(is_dx && g.dx_last));
+                const bool add = is_dx && g.dx_add;
+                const int out_bf16 = to_slot ? 0 : (is_dx ? g.dx_bf16 : g.dw_bf16);
+                const int64_t out_row = is_dx ? info.row : (int64_t)g.v0 + row;
+                void *out = to_slot ? static_cast<void *>(slot)
+                                    : out_bf16 ? static_cast<void *>(static_cast<__nv_bfloat16 *>(is_dx ? g.dx : g.dw) + out_row * g.d)
+                                               : static_cast<void *>(static_cast<float *>(is_dx ? g.dx : g.dw) + out_row * g.d);
+                const float *prev = add ? (slot ? slot : static_cast<const float *>(out)) : nullptr;
+                const bool vec = g.d % 8 == 0;
+#pragma unroll 1
+                for (int ch = 0; ch < 4; ++ch) {
+                    const int32_t c0 = col0 + ch * 32;
+                    if (c0 >= g.d) break;
+                    uint32_t r[32];
+                    tmem_ld_32x32(t_acc + ch * 32, r);
+                    tc_wait_ld();
+                    if (in) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int32_t c = c0 + q * 8;
+                            if (c >= g.d) break;
+                            float v[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[q * 8 + j]) * scale;
+                            if (vec) {
+                                if (prev) {
+                                    const float4 u0 = *reinterpret_cast<const float4 *>(prev + c), u1 = *reinterpret_cast<const float4 *>(prev + c + 4);
+                                    v[0] += u0.x; v[1] += u0.y; v[2] += u0.z; v[3] += u0.w;
+                                    v[4] += u1.x; v[5] += u1.y; v[6] += u1.z; v[7] += u1.w;
+                                }
+                                if (out_bf16) {
+                                    uint32_t pk[4];
+#pragma unroll
+                                    for (int j = 0; j < 4; ++j) {
+                                        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+                                        pk[j] = *reinterpret_cast<const uint32_t *>(&h);
+                                    }
+                                    *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + c) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                                } else {
+                                    float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(out) + c);
+                                    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+                                    dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+                                }
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    if (c + j >= g.d) break;
+                                    const float w = prev ? v[j] + prev[c + j] : v[j];
+                                    if (out_bf16) static_cast<__nv_bfloat16 *>(out)[c + j] = __float2bfloat16_rn(w);
+                                    else static_cast<float *>(out)[c + j] = w;
+                                }
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
+            pd.advance(2);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+    }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------
+int sm_count()
+{
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return n;
+}
+
+// 64 x box_rows boxes of an operand's planes; what lies outside is read as zero.
+bool make_map(CUtensorMap *map, const void *data, int32_t cols, int64_t rows, int planes, int32_t ld, int64_t plane_rows, int box_rows)
+{
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)plane_rows * ld * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(data), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int MODE, int PL, bool BIAS>
+int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_logits, cudaStream_t s)
+{
+    const int pairs = sm_count() / 2;
+    if (pairs <= 0) return TBN_ERR_CUDA;
+    if (tiles <= 0) return TBN_OK;
+    const size_t smem = kStageBudget + sizeof(Control) + 1024;
+    auto kern = head_kernel<MODE, PL, BIAS>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return TBN_ERR_CUDA;
+    const unsigned grid = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
+    return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, maps, p, k_logits) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
+}
+
+LogitsParams logits_params(const LogitsArgs &a)
+{
+    LogitsParams l = {};
+    l.n_live = a.n_live; l.rows = a.rows; l.scales = a.scales; l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad;
+    l.V = a.V; l.v0 = a.v0; l.width = a.width; l.list_idx = a.list_idx; l.list_p = a.list_p; l.K = a.K;
+    l.part_max = a.part_max; l.part_sum = a.part_sum; l.part_dot = a.part_dot;
+    l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
+    return l;
+}
+
+template <int MODE>
+int launch_logits(const LogitsArgs &a, cudaStream_t s)
+{
+    Maps maps = {};
+    if (!make_map(&maps.a[0], a.x.data, a.x.cols, a.x.rows, a.planes, a.x.ld, a.x.plane_rows, 128) ||
+        !make_map(&maps.b[0], a.w.data, a.w.cols, a.w.rows, a.planes, a.w.ld, a.w.plane_rows, 128))
+        return TBN_ERR_CUDA;
+    KernelParams p = {};
+    p.l = logits_params(a);
+    p.status = a.status;
+    const int64_t tiles = (a.T + kTile - 1) / kTile * ((a.width + kTile - 1) / kTile);
+    if (tiles > INT_MAX) return TBN_ERR_UNSUPPORTED;
+    const int32_t kb = (a.x.cols + 63) / 64;
+    if (a.planes == 1) return a.bias ? launch<MODE, 1, true>(maps, p, tiles, kb, s) : launch<MODE, 1, false>(maps, p, tiles, kb, s);
+    return a.bias ? launch<MODE, 2, true>(maps, p, tiles, kb, s) : launch<MODE, 2, false>(maps, p, tiles, kb, s);
+}
+
+}  // namespace
+
+int launch_head_stats(const LogitsArgs &a, cudaStream_t s) { return launch_logits<kStats>(a, s); }
+int launch_head_dz(const LogitsArgs &a, cudaStream_t s) { return launch_logits<kDz>(a, s); }
+
+int launch_head_grads(const GradArgs &a, cudaStream_t s)
+{
+    Maps maps = {};
+    // dz rows are written for whole 256-token tiles; the tokens behind the last kept one are zeros
+    if (!make_map(&maps.a[0], a.dz, a.ldz, a.Tpad, a.planes, a.ldz, a.Tpad, 128) ||
+        !make_map(&maps.b[0], a.w.data, a.w.cols, a.w.rows, a.planes, a.w.ld, a.w.plane_rows, 64) ||
+        !make_map(&maps.a[1], a.dz, a.ldz, a.Tpad, a.planes, a.ldz, a.Tpad, 64) ||
+        !make_map(&maps.b[1], a.x.data, a.x.cols, a.x.rows, a.planes, a.x.ld, a.x.plane_rows, 64))
+        return TBN_ERR_CUDA;
+    KernelParams p = {};
+    GradParams &g = p.g;
+    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width;
+    g.want_dx = a.want_dx; g.want_dw = a.want_dw;
+    g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
+    g.dw = a.dw; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;
+    p.status = a.status;
+    const int64_t nt = (a.d + kTile - 1) / kTile;
+    const int64_t tiles = (a.want_dx ? (a.T + kTile - 1) / kTile * nt * a.dx_splits : 0) +
+                          (a.want_dw ? (a.width + kTile - 1) / kTile * nt * a.dw_splits : 0);
+    if (tiles > INT_MAX) return TBN_ERR_UNSUPPORTED;
+    return a.planes == 1 ? launch<kGrads, 1, false>(maps, p, tiles, 0, s) : launch<kGrads, 2, false>(maps, p, tiles, 0, s);
+}
+
+}  // namespace head
+}  // namespace tbn
