@@ -15,8 +15,12 @@
 // tensor-memory quadrant, 128 columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
 // main loop of the next.
 //
-// fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products hi*hi, hi*lo
-// and lo*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.
+// fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products lo*hi, hi*lo and
+// hi*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.  The tensor core cuts its running sum off toward
+// zero at every 16-element step, an error that grows with the length of the chain (measured, dot products of 1024: 2.6e-6
+// of the result's scale as one chain of 192 steps, 7e-7 for the bf16 form's 64), so with fp32 operands the chain ends
+// after every 64 elements: the small products first, then the four hi*hi steps, and the epilogue warps add the 64-element
+// sums in registers, rounding to nearest.  They keep up: 128 additions per thread against 12 steps of 256 x 256 x 16.
 //
 // Same conventions as the other tcgen05 kernels: every wait is bounded, a wait that gives up records the status and the
 // kernel winds down and returns.
@@ -362,10 +366,10 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             Pipe px, pd;
             for (int32_t i = first; i < sched.total && ok; i += stride) {
                 const Tile t = sched.get<MODE>(i);
-                ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t d_addr = tmem_u + pd.stage * kTile;
+                if (PL == 1) {
+                    ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
+                    if (!ok) break;
+                }
                 const bool a_mn = MODE == kGrads && t.job == 1, b_mn = MODE == kGrads;
                 const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 // low descriptor word: start address in 16-byte units, leading offset (between 64-element panels of the
@@ -374,25 +378,34 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
                 for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
                     ok = wait_bar(smem_u32(&ctl->full[px.stage]), px.phase, abort_flag, p.status, (42 << 24) | (px.stage << 16) | detail);
+                    if (PL == 2 && ok)
+                        ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint32_t d_addr = tmem_u + pd.stage * kTile;
                     const uint32_t sa = stage0 + px.stage * kStage, sb = sa + PL * kSideBytes;
                     const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
                     constexpr uint32_t kPlane = kSideBytes >> 4;
 #pragma unroll
-                    for (int term = 0; term < (PL == 1 ? 1 : 3); ++term) {       // hi*hi, lo*hi, hi*lo
-                        const uint32_t at = a_lo + (term == 1 ? kPlane : 0u), bt = b_lo + (term == 2 ? kPlane : 0u);
+                    for (int term = 0; term < (PL == 1 ? 1 : 3); ++term) {       // two planes: lo*hi, hi*lo, hi*hi
+                        const uint32_t at = a_lo + (PL == 2 && term == 0 ? kPlane : 0u), bt = b_lo + (PL == 2 && term == 1 ? kPlane : 0u);
 #pragma unroll
                         for (int st = 0; st < 4; ++st)
                             mma_pair(d_addr, at + st * a_step, bt + st * b_step, kDescHi, idesc,
-                                     term > 0 || st > 0 ? 1u : (uint32_t)(kb > t.kb0), leader);
+                                     term > 0 || st > 0 ? 1u : (uint32_t)(PL == 1 && kb > t.kb0), leader);
                     }
                     commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
                     px.advance(kStages);
+                    if (PL == 2) {
+                        commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
+                        pd.advance(2);
+                    }
                 }
                 if (!ok) break;
-                commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
-                pd.advance(2);
+                if (PL == 1) {
+                    commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
+                    pd.advance(2);
+                }
             }
             if (!ok) {                                 // no MMA may still read shared or tensor memory when they go away
                 const uint64_t t0 = global_timer_ns();
@@ -434,26 +447,60 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             } else if (t.job == 0 && live) {
                 info.row = p.g.rows[row].row;
             }
-            ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t t_acc = t_lane + pd.stage * kTile;
-
-            if (MODE == kStats) {
-                float m = -INFINITY, l = 0.0f, dot = 0.0f;
-#pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
-                    const int32_t c0 = col0 + ch * 32;
+            float acc[PL == 2 ? 128 : 1];
+            uint32_t t_acc = 0;
+            if (PL == 1) {
+                ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
+                if (!ok) break;
+                tc_fence_after();
+                t_acc = t_lane + pd.stage * kTile;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 128; ++j) acc[PL == 2 ? j : 0] = 0.0f;
+                for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
+                    ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int ch = 0; ch < 8; ++ch) {
+                        uint32_t r[16];
+                        tmem_ld_32x16(t_lane + pd.stage * kTile + ch * 16, r);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[PL == 2 ? ch * 16 + j : 0] += __uint_as_float(r[j]);
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
+                    pd.advance(2);
+                }
+                if (!ok) break;
+            }
+            // 32 columns of the accumulated tile
+            auto load_chunk = [&](int ch, float (&out)[32]) {
+                if (PL == 1) {
                     uint32_t r[32];
                     tmem_ld_32x32(t_acc + ch * 32, r);
                     tc_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) out[j] = __uint_as_float(r[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) out[j] = acc[PL == 2 ? ch * 32 + j : 0];
+                }
+            };
+
+            if (MODE == kStats) {
+                float m = -INFINITY, l = 0.0f, dot = 0.0f;
+#pragma unroll (PL == 2 ? 4 : 1)
+                for (int ch = 0; ch < 4; ++ch) {
+                    const int32_t c0 = col0 + ch * 32;
                     float v[32];
+                    load_chunk(ch, v);
                     if (BIAS) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(r[j]), sc, bias_s[ch * 32 + j]);
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]);
                     } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
                         if (c0 + 32 > p.l.width) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
@@ -489,19 +536,17 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 }
             } else if (MODE == kDz) {
                 const bool all_live = __all_sync(0xffffffffu, live);
-#pragma unroll 1
+#pragma unroll (PL == 2 ? 4 : 1)
                 for (int ch = 0; ch < 4; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
-                    uint32_t r[32];
-                    tmem_ld_32x32(t_acc + ch * 32, r);
-                    tc_wait_ld();
                     float v[32];
+                    load_chunk(ch, v);
                     if (BIAS) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(r[j]), sc, bias_s[ch * 32 + j]) - info.lse2;
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]) - info.lse2;
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(__uint_as_float(r[j]), sc, -info.lse2);
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
                         if (c0 + 32 > p.l.width) {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
@@ -546,13 +591,12 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                                                : static_cast<void *>(static_cast<float *>(is_dx ? g.dx : g.dw) + out_row * g.d);
                 const float *prev = add ? (slot ? slot : static_cast<const float *>(out)) : nullptr;
                 const bool vec = g.d % 8 == 0;
-#pragma unroll 1
+#pragma unroll (PL == 2 ? 4 : 1)
                 for (int ch = 0; ch < 4; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
                     if (c0 >= g.d) break;
-                    uint32_t r[32];
-                    tmem_ld_32x32(t_acc + ch * 32, r);
-                    tc_wait_ld();
+                    float r[32];
+                    load_chunk(ch, r);
                     if (in) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
@@ -560,7 +604,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                             if (c >= g.d) break;
                             float v[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[q * 8 + j]) * scale;
+                            for (int j = 0; j < 8; ++j) v[j] = empty ? 0.0f : r[q * 8 + j] * scale;
                             if (vec) {
                                 if (prev) {
                                     const float4 u0 = *reinterpret_cast<const float4 *>(prev + c), u1 = *reinterpret_cast<const float4 *>(prev + c + 4);
@@ -594,10 +638,13 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     __syncwarp();
                 }
             }
-            tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
-            pd.advance(2);
+            if (PL == 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
+                pd.advance(2);
+            }
         }
     }
 
