@@ -531,32 +531,45 @@ def tbn_linear_distill_workspace_bytes(T, in_f, vocab, dtype, K, backward) -> in
     return int(lib().tbn_linear_distill_workspace_bytes(T, in_f, vocab, dtype, K, int(bool(backward))))
 
 
-def _head_check(x, weight, bias, rows, floats, grid=()):
-    """Shapes, types and devices of a head-loss call; the library sees pointers only."""
+def _head_check(x, weight, bias, labels, floats=(), top_logit=None):
+    """Shapes, types and devices of a head-loss call; the library sees pointers only.  Returns (T, in_f, vocab, dtype)."""
     if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1]:
         raise TbnError(-2, f"head loss: x {tuple(x.shape)} and weight {tuple(weight.shape)}")
-    T, V = x.shape[0], weight.shape[0]
+    T, V, device = x.shape[0], weight.shape[0], x.device
     if weight.dtype != x.dtype:
         raise TypeError(f"x is {x.dtype}, weight is {weight.dtype}")
+    if labels.dtype != torch.int64 or labels.dim() != (1 if top_logit is None else 2) or labels.shape[0] != T:
+        raise TbnError(-2, f"head loss: {'targets' if top_logit is None else 'top_index'} must be int64, one row per token")
+    if top_logit is not None and top_logit.shape != labels.shape:
+        raise TbnError(-2, "head loss: top_logit must have the shape of top_index")
     if bias is not None and (bias.shape != (V,) or bias.dtype != torch.float32):
         raise TbnError(-2, f"head loss: bias must be float32 of shape ({V},)")
-    for name, t in rows:
-        if t.shape[0] != T or t.dtype != torch.int64 or t.dim() != (2 if grid else 1):
-            raise TbnError(-2, f"head loss: {name} must be int64 with {T} rows")
-    for name, t in grid:
-        if t.shape != rows[0][1].shape:
-            raise TbnError(-2, f"head loss: {name} must have the shape of {rows[0][0]}")
-    for name, t in floats:
+    for t in floats:
         if t.shape != (T,) or t.dtype != torch.float32:
-            raise TbnError(-2, f"head loss: {name} must be float32 of shape ({T},)")
-    for t in [weight, bias] + [t for _, t in rows] + [t for _, t in floats] + [t for _, t in grid]:
-        if t is not None and t.device != x.device:
-            raise ValueError(f"head loss: tensors on {x.device} and {t.device}")
+            raise TbnError(-2, f"head loss: lse and dloss must be float32 of shape ({T},)")
+    if not x.is_cuda:
+        raise ValueError("head loss: the tensors must be on a CUDA device")
+    for t in (weight, labels, bias, top_logit, *floats):
+        if t is not None and t.device != device:
+            raise ValueError(f"head loss: tensors on {device} and {t.device}")
+    return T, x.shape[1], V, _dtype_code(x)
+
+
+def _head_call(name, device, need, workspace, *args):
+    """Runs the entry point on the tensors' device and that device's current stream."""
+    ws = workspace if workspace is not None else _ws(need, device)
+    fn, stream = getattr(lib(), name), torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, _ptr(ws), ws.numel() * ws.element_size(), stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _ptr(ws), ws.numel() * ws.element_size(), stream)
+    _check(status, name)
 
 
 def _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype):
-    dx = torch.empty_like(x) if need_dx else None
     wd = _dtype_code(weight) if dw_dtype is None else dw_dtype
+    dx = torch.empty_like(x) if need_dx else None
     dw = torch.empty(weight.shape, dtype=_torch_dtype(wd), device=x.device) if need_dw else None
     db = torch.empty(weight.shape[0], dtype=torch.float32, device=x.device) if need_dbias else None
     return dx, dw, wd, db
@@ -565,14 +578,11 @@ def _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype):
 def tbn_linear_xent_fwd(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, bias: torch.Tensor | None = None,
                         ignore_index: int = -100, workspace: torch.Tensor | None = None):
     """Softmax cross entropy of the head x @ weight.T + bias without storing its logits.  Returns (loss [T], lse [T])."""
-    _head_check(x, weight, bias, [("targets", targets)], [])
-    (T, d), V, dt = x.shape, weight.shape[0], _dtype_code(x)
-    with torch.cuda.device(x.device):
-        loss = torch.empty(T, dtype=torch.float32, device=x.device)
-        lse = torch.empty(T, dtype=torch.float32, device=x.device)
-        ws = workspace if workspace is not None else _ws(tbn_linear_xent_workspace_bytes(T, d, V, dt, False), x.device)
-        _check(lib().tbn_linear_xent_fwd(_ptr(x), _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(targets), ignore_index, _ptr(loss),
-                                         _ptr(lse), _ptr(ws), ws.numel(), _stream()), "tbn_linear_xent_fwd")
+    T, d, V, dt = _head_check(x, weight, bias, targets)
+    loss = torch.empty(T, dtype=torch.float32, device=x.device)
+    lse = torch.empty(T, dtype=torch.float32, device=x.device)
+    _head_call("tbn_linear_xent_fwd", x.device, tbn_linear_xent_workspace_bytes(T, d, V, dt, False), workspace, _ptr(x), _ptr(weight), dt,
+               T, d, V, _ptr(bias), _ptr(targets), ignore_index, _ptr(loss), _ptr(lse))
     return loss, lse
 
 
@@ -581,29 +591,23 @@ def tbn_linear_xent_bwd(x: torch.Tensor, weight: torch.Tensor, targets: torch.Te
                         need_dbias: bool = False, dw_dtype: int | None = None, workspace: torch.Tensor | None = None):
     """Gradient of tbn_linear_xent_fwd for dloss = dL/dloss [T].  Returns (dx, dw, dbias), None for what is not asked for.
     dw_dtype: F32 gives the G that tbn_tile_bwd takes; by default dw has the weight's type."""
-    _head_check(x, weight, bias, [("targets", targets)], [("lse", lse), ("dloss", dloss)])
-    (T, d), V, dt = x.shape, weight.shape[0], _dtype_code(x)
-    with torch.cuda.device(x.device):
-        dx, dw, wd, db = _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype)
-        ws = workspace if workspace is not None else _ws(tbn_linear_xent_workspace_bytes(T, d, V, dt, True), x.device)
-        _check(lib().tbn_linear_xent_bwd(_ptr(x), _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(targets), ignore_index, _ptr(lse),
-                                         _ptr(dloss), _ptr(dx), _ptr(dw), wd, _ptr(db), _ptr(ws), ws.numel(), _stream()),
-               "tbn_linear_xent_bwd")
+    T, d, V, dt = _head_check(x, weight, bias, targets, (lse, dloss))
+    dx, dw, wd, db = _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype)
+    _head_call("tbn_linear_xent_bwd", x.device, tbn_linear_xent_workspace_bytes(T, d, V, dt, True), workspace, _ptr(x), _ptr(weight), dt,
+               T, d, V, _ptr(bias), _ptr(targets), ignore_index, _ptr(lse), _ptr(dloss), _ptr(dx), _ptr(dw), wd, _ptr(db))
     return dx, dw, db
 
 
 def tbn_linear_distill_fwd(x: torch.Tensor, weight: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor,
                            temperature: float = 1.0, bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Distillation of the head x @ weight.T + bias from a teacher's top logits (both T x K).  Returns (loss [T], lse [T])."""
-    _head_check(x, weight, bias, [("top_index", top_index)], [], [("top_logit", top_logit)])
-    (T, d), V, dt, K = x.shape, weight.shape[0], _dtype_code(x), top_index.shape[1]
-    with torch.cuda.device(x.device):
-        loss = torch.empty(T, dtype=torch.float32, device=x.device)
-        lse = torch.empty(T, dtype=torch.float32, device=x.device)
-        ws = workspace if workspace is not None else _ws(tbn_linear_distill_workspace_bytes(T, d, V, dt, K, False), x.device)
-        _check(lib().tbn_linear_distill_fwd(_ptr(x), _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit),
-                                            _dtype_code(top_logit), K, temperature, _ptr(loss), _ptr(lse), _ptr(ws), ws.numel(),
-                                            _stream()), "tbn_linear_distill_fwd")
+    T, d, V, dt = _head_check(x, weight, bias, top_index, (), top_logit)
+    K = top_index.shape[1]
+    loss = torch.empty(T, dtype=torch.float32, device=x.device)
+    lse = torch.empty(T, dtype=torch.float32, device=x.device)
+    _head_call("tbn_linear_distill_fwd", x.device, tbn_linear_distill_workspace_bytes(T, d, V, dt, K, False), workspace, _ptr(x),
+               _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit), _dtype_code(top_logit), K, temperature, _ptr(loss),
+               _ptr(lse))
     return loss, lse
 
 
@@ -612,12 +616,10 @@ def tbn_linear_distill_bwd(x: torch.Tensor, weight: torch.Tensor, top_index: tor
                            need_dw: bool = True, need_dbias: bool = False, dw_dtype: int | None = None,
                            workspace: torch.Tensor | None = None):
     """Gradient of tbn_linear_distill_fwd with respect to the student, as tbn_linear_xent_bwd.  Returns (dx, dw, dbias)."""
-    _head_check(x, weight, bias, [("top_index", top_index)], [("lse", lse), ("dloss", dloss)], [("top_logit", top_logit)])
-    (T, d), V, dt, K = x.shape, weight.shape[0], _dtype_code(x), top_index.shape[1]
-    with torch.cuda.device(x.device):
-        dx, dw, wd, db = _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype)
-        ws = workspace if workspace is not None else _ws(tbn_linear_distill_workspace_bytes(T, d, V, dt, K, True), x.device)
-        _check(lib().tbn_linear_distill_bwd(_ptr(x), _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit),
-                                            _dtype_code(top_logit), K, temperature, _ptr(lse), _ptr(dloss), _ptr(dx), _ptr(dw), wd,
-                                            _ptr(db), _ptr(ws), ws.numel(), _stream()), "tbn_linear_distill_bwd")
+    T, d, V, dt = _head_check(x, weight, bias, top_index, (lse, dloss), top_logit)
+    K = top_index.shape[1]
+    dx, dw, wd, db = _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype)
+    _head_call("tbn_linear_distill_bwd", x.device, tbn_linear_distill_workspace_bytes(T, d, V, dt, K, True), workspace, _ptr(x),
+               _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit), _dtype_code(top_logit), K, temperature, _ptr(lse),
+               _ptr(dloss), _ptr(dx), _ptr(dw), wd, _ptr(db))
     return dx, dw, db

@@ -26,19 +26,6 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;      // bound on one piece of dz (a piece has at least 1024 classes)
 
-// ---- which tokens take part -------------------------------------------------------------------------
-struct Labels {
-    const int64_t *target;                 // cross entropy
-    int64_t ignore_index;
-    int32_t V;
-    const uint8_t *flags;                  // distillation: written by teacher_kernel
-    __device__ __forceinline__ bool live(int64_t t) const {
-        if (flags) return flags[t] != 0;
-        const int64_t c = target[t];
-        return c != ignore_index && c >= 0 && c < V;
-    }
-};
-
 // ---- the teacher's entries ---------------------------------------------------------------------------
 // One warp per token: p = softmax(logit / tau) over the entries whose index is a class and whose logit is above
 // -infinity, sum p log p, and the entries sorted by class (by position among equals), which is the order in which the
@@ -132,23 +119,23 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
 }
 
 // ---- fp32 operands: largest magnitudes ------------------------------------------------------------------
-// max_bits[0..2]: bit patterns of max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows (a maximum does
-// not depend on the order in which it is taken).
-__device__ __forceinline__ void fold_max(unsigned int *slot, float v) {
-    v = warp_max(v);
+// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows.
+constexpr int kMaxBlocks = 592;
+
+__device__ __forceinline__ float block_max(float v) {
     __shared__ float part[8];
+    v = warp_max(v);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        v = threadIdx.x < (blockDim.x >> 5) ? part[threadIdx.x] : 0.0f;
-        v = warp_max(v);
-        if (threadIdx.x == 0 && v > 0.0f) atomicMax(slot, __float_as_uint(v));
-    }
+    return warp_max(part[threadIdx.x & 7]);
+}
+__device__ __forceinline__ float max4(float m, float4 v) {
+    return fmaxf(fmaxf(m, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
 }
 __global__ void __launch_bounds__(256)
 abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d, const float *__restrict__ w, int64_t w_count,
-               const float *__restrict__ dloss, float tau, unsigned int *__restrict__ max_bits)
+               const float *__restrict__ dloss, float tau, float *__restrict__ max_part)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -156,11 +143,13 @@ abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d,
     float mw = 0.0f, mx = 0.0f, mg = 0.0f;
     const int64_t w4 = w_count >> 2;
     const float4 *wv = reinterpret_cast<const float4 *>(w);
-    for (int64_t i = tid; i < w4; i += threads) {
-        const float4 v = __ldg(wv + i);
-        mw = fmaxf(mw, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+    int64_t i = tid;
+    for (; i + 3 * threads < w4; i += 4 * threads) {
+        const float4 v0 = __ldg(wv + i), v1 = __ldg(wv + i + threads), v2 = __ldg(wv + i + 2 * threads), v3 = __ldg(wv + i + 3 * threads);
+        mw = max4(max4(max4(max4(mw, v0), v1), v2), v3);
     }
-    for (int64_t i = (w4 << 2) + tid; i < w_count; i += threads) mw = fmaxf(mw, fabsf(w[i]));
+    for (; i < w4; i += threads) mw = max4(mw, __ldg(wv + i));
+    for (i = (w4 << 2) + tid; i < w_count; i += threads) mw = fmaxf(mw, fabsf(w[i]));
     const int lane = threadIdx.x & 31;
     for (int64_t t = tid >> 5; t < T; t += threads >> 5) {
         if (!labels.live(t)) continue;
@@ -168,16 +157,20 @@ abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d,
         if (dloss && lane == 0) mg = fmaxf(mg, fabsf(dloss[t] * tau));
     }
     __syncwarp();
-    fold_max(max_bits + 0, mx);
-    fold_max(max_bits + 1, mw);
-    fold_max(max_bits + 2, mg);
+    mx = block_max(mx);
+    mw = block_max(mw);
+    mg = block_max(mg);
+    if (threadIdx.x == 0) {
+        max_part[blockIdx.x] = mx;
+        max_part[kMaxBlocks + blockIdx.x] = mw;
+        max_part[2 * kMaxBlocks + blockIdx.x] = mg;
+    }
 }
 // The power of two that takes the largest magnitude to [2^14, 2^15): the high part of every element then keeps 11 bits
-// and the remainder another 11, down to 2^-38 of the largest one, below which fp16 ends.  Non-finite or zero: 1.
-__device__ __forceinline__ float scale_of(unsigned int bits) {
-    const float m = __uint_as_float(bits);
+// and the remainder another 11, down to 2^-39 of the largest one, below which fp16 ends.  Infinite or zero: 1.
+__device__ __forceinline__ float scale_of(float m) {
     if (!(m > 0.0f) || !(m < INFINITY)) return 1.0f;
-    int e = (int)(bits >> 23) - 127;                   // subnormal maxima: -127, clamped below
+    int e = (int)(__float_as_uint(m) >> 23) - 127;     // subnormal maxima: -127, clamped below
     e = e > 60 ? 60 : e < -60 ? -60 : e;
     return __uint_as_float((unsigned int)(127 + 14 - e) << 23);
 }
@@ -186,56 +179,21 @@ __device__ __forceinline__ void split16(float v, __half &hi, __half &lo) {
     lo = __float2half_rn(v - __half2float(hi));
 }
 
-// ---- weights in the form the contractions read: padded rows, fp32 as two fp16 planes --------------------------
-// Needed for fp32 weights and for rows that are not a multiple of 16 bytes; other weights are read in place.
-template <typename TW>
-__global__ void __launch_bounds__(256)
-pack_weight_kernel(const TW *__restrict__ w, int64_t V, int32_t d, int32_t ld, const unsigned int *__restrict__ max_bits,
-                   uint16_t *__restrict__ out)
-{
-    pdl_launch_dependents();
-    pdl_wait();
-    const float sc = sizeof(TW) == 4 ? scale_of(max_bits[1]) : 1.0f;
-    const int64_t groups = V * (ld >> 3), plane = V * ld;
-    const bool vec = sizeof(TW) == 4 && d % 4 == 0;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / (ld >> 3);
-        const int32_t c = (int32_t)(i - r * (ld >> 3)) * 8;
-        alignas(16) uint16_t hi[8], lo[8];
-        float v[8];
-        if (vec && c + 8 <= d) {
-            const float4 a = __ldg(reinterpret_cast<const float4 *>(w + r * d + c)), b = __ldg(reinterpret_cast<const float4 *>(w + r * d + c + 4));
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = c + j < d ? load_as_float(w, r * d + c + j) : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (sizeof(TW) == 4) {
-                __half h, l;
-                split16(v[j] * sc, h, l);
-                hi[j] = __half_as_ushort(h); lo[j] = __half_as_ushort(l);
-            } else {
-                hi[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
-            }
-        }
-        *reinterpret_cast<uint4 *>(out + r * ld + c) = *reinterpret_cast<const uint4 *>(hi);
-        if (sizeof(TW) == 4) *reinterpret_cast<uint4 *>(out + plane + r * ld + c) = *reinterpret_cast<const uint4 *>(lo);
-    }
-}
-
-// ---- kept tokens to the front ---------------------------------------------------------------------------------
-// Block b owns rows [b * per_block, ...).  It counts the kept rows before its own (re-reading the labels: at most a few
-// hundred blocks, so a few megabytes of L2 reads for tens of thousands of tokens, and no second launch or hand-over
-// between blocks), then packs its rows in order.  The last block zeroes the rows up to the next multiple of 64, which the
-// weight gradient contracts over.
+// ---- operands in the form the contractions read ---------------------------------------------------------------
+// Rows padded to 16 bytes, fp32 as two fp16 planes.  Activations are always packed: the kept tokens come to the front.
+// Block b < row_blocks owns rows [b * per_block, ...).  It counts the kept rows before its own (re-reading the labels: at
+// most a few hundred blocks, so a few megabytes of L2 reads for tens of thousands of tokens, and no second launch or
+// hand-over between blocks), then packs its rows in order.  The last row block zeroes the rows up to the next multiple of
+// 64, which the weight gradient contracts over.  The blocks behind pack the weights, where they cannot be read in place
+// (fp32, or rows that are not a multiple of 16 bytes).
 struct PackArgs {
     Labels labels;
     int64_t T, Tpad, per_block;
-    int32_t d, ld;
-    const unsigned int *max_bits;          // fp32 only
-    uint16_t *xc;
+    int32_t V, d, ld;
+    unsigned int row_blocks;
+    const float *max_part;                 // fp32 only
+    int32_t max_blocks;
+    uint16_t *xc, *wc;
     RowInfo *rows;
     int32_t *n_live;
     Scales *scales;                        // fp32 only: written here for the kernels that follow
@@ -245,16 +203,67 @@ struct PackArgs {
     void *dx;                              // backward: rows zeroed for the tokens left out (or null)
     int dx_bytes;
 };
-template <typename TX>
+
+// eight elements of a row from column c, zeros from column d on
+template <typename TS>
+__device__ __forceinline__ void pack8(const TS *__restrict__ src, int32_t c, int32_t d, float scale, uint16_t *hi_dst, uint16_t *lo_dst) {
+    alignas(16) uint16_t hi[8], lo[8];
+    if (sizeof(TS) == 2 && d % 8 == 0 && c + 8 <= d) {
+        *reinterpret_cast<uint4 *>(hi) = __ldg(reinterpret_cast<const uint4 *>(src + c));
+    } else {
+        float v[8];
+        if (sizeof(TS) == 4 && d % 4 == 0 && c + 8 <= d) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(src + c)), b = __ldg(reinterpret_cast<const float4 *>(src + c) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = c + j < d ? load_as_float(src, c + j) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (sizeof(TS) == 4) {
+                __half h, l;
+                split16(v[j] * scale, h, l);
+                hi[j] = __half_as_ushort(h); lo[j] = __half_as_ushort(l);
+            } else {
+                hi[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+            }
+        }
+    }
+    *reinterpret_cast<uint4 *>(hi_dst) = *reinterpret_cast<const uint4 *>(hi);
+    if (sizeof(TS) == 4) *reinterpret_cast<uint4 *>(lo_dst) = *reinterpret_cast<const uint4 *>(lo);
+}
+
+template <typename TS>
 __global__ void __launch_bounds__(256)
-pack_rows_kernel(const TX *__restrict__ x, PackArgs a)
+pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a)
 {
     __shared__ int warp_count[8];
     __shared__ int32_t slot[256];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t r0 = min(a.T, (int64_t)blockIdx.x * a.per_block), r1 = min(a.T, r0 + a.per_block);
+    float m[3] = {0.0f, 0.0f, 0.0f};
+    if (sizeof(TS) == 4) {
+        for (int k = 0; k < 3; ++k) {
+            for (int i = threadIdx.x; i < a.max_blocks; i += 256) m[k] = fmaxf(m[k], a.max_part[k * kMaxBlocks + i]);
+            m[k] = block_max(m[k]);
+        }
+    }
+    const float sx = scale_of(m[0]), sw = scale_of(m[1]), sg = scale_of(m[2]);
+    if (blockIdx.x >= a.row_blocks) {                  // weights
+        const int64_t vecs = a.ld >> 3, groups = a.V * vecs, plane = (int64_t)a.V * a.ld;
+        const int64_t stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
+        for (int64_t i = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x; i < groups; i += stride) {
+            const int64_t r = i / vecs;
+            const int32_t c = (int32_t)(i - r * vecs) * 8;
+            uint16_t *dst = a.wc + r * a.ld + c;
+            pack8(w + r * a.d, c, a.d, sw, dst, dst + plane);
+        }
+        return;
+    }
+    if (sizeof(TS) == 4 && blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{sx, sw, sg, 1.0f / sx, 1.0f / sw, 1.0f / sg};
+    const int64_t r0 = (int64_t)blockIdx.x * a.per_block, r1 = min(a.T, r0 + a.per_block);       // r0 < T for every row block
     int mine = 0;
     for (int64_t t = threadIdx.x; t < r0; t += 256) mine += a.labels.live(t) ? 1 : 0;
     mine = __reduce_add_sync(0xffffffffu, mine);
@@ -263,17 +272,7 @@ pack_rows_kernel(const TX *__restrict__ x, PackArgs a)
     int64_t base = 0;
     for (int i = 0; i < 8; ++i) base += warp_count[i];
 
-    float sx = 1.0f, sg = 1.0f;
-    if (sizeof(TX) == 4) {
-        sx = scale_of(a.max_bits[0]);
-        if (a.dloss) sg = scale_of(a.max_bits[2]);
-        if (blockIdx.x == 0 && threadIdx.x == 0) {
-            const float sw = scale_of(a.max_bits[1]);
-            *a.scales = Scales{sx, sw, sg, 1.0f / sx, 1.0f / sw, 1.0f / sg};
-        }
-    }
     const int64_t plane = a.Tpad * a.ld;
-    const bool vec = a.d % 8 == 0;
     for (int64_t b0 = r0; b0 < r1; b0 += 256) {
         const int64_t t = b0 + threadIdx.x;
         const bool live = t < r1 && a.labels.live(t);
@@ -288,7 +287,7 @@ pack_rows_kernel(const TX *__restrict__ x, PackArgs a)
             RowInfo info;
             info.lse2 = a.lse ? a.lse[t] * kLog2e : 0.0f;
             info.g = a.dloss ? a.dloss[t] * a.tau * sg : 0.0f;
-            info.label = a.labels.target ? (int32_t)a.labels.target[t] : -1;
+            info.label = a.labels.flags ? -1 : (int32_t)a.labels.target[t];
             info.row = (int32_t)t;
             a.rows[at] = info;
         } else if (t < r1 && a.loss_out) {
@@ -305,42 +304,22 @@ pack_rows_kernel(const TX *__restrict__ x, PackArgs a)
                 if (a.dx) {
                     uint8_t *row = static_cast<uint8_t *>(a.dx) + from * a.d * a.dx_bytes;
                     const int64_t bytes = (int64_t)a.d * a.dx_bytes;
-                    if (vec) for (int64_t c = lane * 16; c < bytes; c += 512) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0u, 0u, 0u, 0u);
+                    if (a.d % 8 == 0) for (int64_t c = lane * 16; c < bytes; c += 512) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0u, 0u, 0u, 0u);
                     else for (int64_t c = lane * 2; c < bytes; c += 64) *reinterpret_cast<uint16_t *>(row + c) = 0;
                 }
                 continue;
             }
-            const TX *src = x + from * a.d;
             uint16_t *dst = a.xc + (int64_t)to * a.ld;
-            for (int32_t c = lane * 8; c < a.ld; c += 256) {
-                alignas(16) uint16_t hi[8], lo[8];
-                if (sizeof(TX) == 2 && vec) {
-                    *reinterpret_cast<uint4 *>(hi) = __ldg(reinterpret_cast<const uint4 *>(src + c));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float v = c + j < a.d ? load_as_float(src, c + j) : 0.0f;
-                        if (sizeof(TX) == 4) {
-                            __half h, l;
-                            split16(v * sx, h, l);
-                            hi[j] = __half_as_ushort(h); lo[j] = __half_as_ushort(l);
-                        } else {
-                            hi[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-                        }
-                    }
-                }
-                *reinterpret_cast<uint4 *>(dst + c) = *reinterpret_cast<const uint4 *>(hi);
-                if (sizeof(TX) == 4) *reinterpret_cast<uint4 *>(dst + plane + c) = *reinterpret_cast<const uint4 *>(lo);
-            }
+            for (int32_t c = lane * 8; c < a.ld; c += 256) pack8(x + from * a.d, c, a.d, sx, dst + c, dst + plane + c);
         }
     }
-    if (blockIdx.x == gridDim.x - 1) {
+    if (blockIdx.x == a.row_blocks - 1) {
         if (threadIdx.x == 0) *a.n_live = (int32_t)base;
         const int64_t end = (base + 63) / 64 * 64, vecs = (end - base) * (a.ld >> 3);
         for (int64_t i = threadIdx.x; i < vecs; i += 256) {
             uint4 *p = reinterpret_cast<uint4 *>(a.xc + base * a.ld) + i;
             *p = make_uint4(0u, 0u, 0u, 0u);
-            if (sizeof(TX) == 4) *(p + (plane >> 3)) = make_uint4(0u, 0u, 0u, 0u);
+            if (sizeof(TS) == 4) *(p + (plane >> 3)) = make_uint4(0u, 0u, 0u, 0u);
         }
     }
 }
@@ -351,8 +330,8 @@ pack_rows_kernel(const TX *__restrict__ x, PackArgs a)
 template <int RB>
 __global__ void __launch_bounds__(256)
 combine_kernel(const float *__restrict__ part_max, const float *__restrict__ part_sum, const float *__restrict__ part_dot, int32_t parts,
-               int64_t Tpad, const int32_t *__restrict__ n_live, const RowInfo *__restrict__ rows, const float2 *__restrict__ teacher,
-               float tau, float *__restrict__ loss, float *__restrict__ lse)
+               int64_t Tpad, const int32_t *__restrict__ n_live, const RowInfo *__restrict__ rows, Labels labels, int32_t n_rows,
+               const float2 *__restrict__ teacher, float tau, float *__restrict__ loss, float *__restrict__ lse)
 {
     constexpr int kParts = 256 / RB;
     __shared__ float sm[256], ss[256], sd[256];
@@ -360,7 +339,11 @@ combine_kernel(const float *__restrict__ part_max, const float *__restrict__ par
     pdl_launch_dependents();
     pdl_wait();
     const int64_t row = (int64_t)blockIdx.x * RB + r;
-    const bool live = row < *n_live;
+    bool live = row < (n_live ? *n_live : n_rows);
+    if (live && !rows && !labels.live(row)) {          // rows in their own order: the ones left out are still among them
+        live = false;
+        if (g == 0) { loss[row] = 0.0f; lse[row] = 0.0f; }
+    }
     float m = -INFINITY, s = 0.0f, dot = 0.0f;
     if (live) {
 #pragma unroll 4
@@ -384,7 +367,7 @@ combine_kernel(const float *__restrict__ part_max, const float *__restrict__ par
             m = mn;
         }
         const float lse2 = m + log2f(s);               // all classes at -infinity: -infinity + log2(0)
-        const int32_t t = rows[row].row;
+        const int64_t t = rows ? (int64_t)rows[row].row : row;
         lse[t] = lse2 * kLn2;
         if (teacher) {
             const float2 e = teacher[t];               // sum p log p, sum p
@@ -395,45 +378,81 @@ combine_kernel(const float *__restrict__ part_max, const float *__restrict__ par
     }
 }
 
-// ---- backward: sums over partial results ------------------------------------------------------------------------
-// db[v0 + c] = sum over the 32-row groups of the kept tokens
-__global__ void __launch_bounds__(256)
-bias_grad_kernel(const float *__restrict__ part, int32_t ld, const int32_t *__restrict__ n_live, const Scales *__restrict__ scales,
-                 int32_t width, float *__restrict__ db)
-{
-    __shared__ float sum[8][33];
-    const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
-    pdl_launch_dependents();
-    pdl_wait();
-    const int32_t groups = (*n_live + 31) / 32;
-    const int32_t c = blockIdx.x * 32 + lane;
-    float s = 0.0f;
-#pragma unroll 4
-    for (int32_t i = g; i < groups; i += 8) s += part[(int64_t)i * ld + c];
-    sum[g][lane] = s;
-    __syncthreads();
-    if (g == 0 && c < width) {
-        for (int i = 1; i < 8; ++i) s += sum[i][lane];
-        db[c] = scales ? s * scales->inv_g : s;
-    }
-}
-
-// out[row(i)][:] = sum of the splits' partial rows i (rows == nullptr: row(i) = i, `count` rows)
-template <typename TO>
-__global__ void __launch_bounds__(256)
-join_splits_kernel(const float *__restrict__ slots, int32_t splits, int64_t slot_rows, int32_t d, const int32_t *__restrict__ n_live,
-                   const RowInfo *__restrict__ rows, int64_t count, TO *__restrict__ out)
-{
-    pdl_launch_dependents();
-    pdl_wait();
-    const int64_t n = rows ? *n_live : count;
+// ---- backward: sums over partial results, one launch per piece where there are any -----------------------------------
+struct FinishArgs {
+    const int32_t *n_live;
+    const RowInfo *rows;
+    const Scales *scales;
+    // db[v0 + c] = sum over the 32-row groups of the kept tokens (bias_blocks blocks of 32 classes)
+    const float *col_part;
+    int32_t ldz, width;
+    float *db;
+    unsigned int bias_blocks, dw_blocks, dx_blocks;
+    // rows of dw and dx: the sums of their splits
+    const float *dw_slots, *dx_slots;
+    int32_t dw_splits, dx_splits, d, dw_bf16, dx_bf16;
+    int64_t dw_slot_rows, dx_slot_rows;
+    void *dw, *dx;                         // dw: the piece's first row
+};
+__device__ __forceinline__ void join_splits(const float *slots, int32_t splits, int64_t slot_rows, int32_t d, int64_t n, const RowInfo *rows,
+                                            void *out, int bf16, int64_t first, int64_t stride) {
     const int64_t total = n * d, split_stride = slot_rows * d;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    if (d % 4 == 0) {
+        for (int64_t i = first * 4; i < total; i += stride * 4) {
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int k = 0; k < splits; ++k) {
+                const float4 v = *reinterpret_cast<const float4 *>(slots + k * split_stride + i);
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            const int64_t r = i / d, at = (rows ? (int64_t)rows[r].row : r) * d + (i - r * d);
+            if (bf16) {
+                const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
+                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(out) + at) =
+                    make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+            } else {
+                *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = s;
+            }
+        }
+        return;
+    }
+    for (int64_t i = first; i < total; i += stride) {
         float s = 0.0f;
         for (int k = 0; k < splits; ++k) s += slots[k * split_stride + i];
-        const int64_t r = i / d;
-        store_from_float(out, (rows ? (int64_t)rows[r].row : r) * d + (i - r * d), s);
+        const int64_t r = i / d, at = (rows ? (int64_t)rows[r].row : r) * d + (i - r * d);
+        if (bf16) static_cast<__nv_bfloat16 *>(out)[at] = __float2bfloat16_rn(s);
+        else static_cast<float *>(out)[at] = s;
     }
+}
+__global__ void __launch_bounds__(256)
+finish_kernel(const FinishArgs a)
+{
+    __shared__ float sum[8][33];
+    pdl_launch_dependents();
+    pdl_wait();
+    unsigned int b = blockIdx.x;
+    if (b < a.bias_blocks) {
+        const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+        const int32_t groups = (*a.n_live + 31) / 32, c = b * 32 + lane;
+        float s = 0.0f;
+#pragma unroll 4
+        for (int32_t i = g; i < groups; i += 8) s += a.col_part[(int64_t)i * a.ldz + c];
+        sum[g][lane] = s;
+        __syncthreads();
+        if (g == 0 && c < a.width) {
+            for (int i = 1; i < 8; ++i) s += sum[i][lane];
+            a.db[c] = a.scales ? s * a.scales->inv_g : s;
+        }
+        return;
+    }
+    b -= a.bias_blocks;
+    if (b < a.dw_blocks) {
+        join_splits(a.dw_slots, a.dw_splits, a.dw_slot_rows, a.d, a.width, nullptr, a.dw, a.dw_bf16, (int64_t)b * 256 + threadIdx.x,
+                    (int64_t)a.dw_blocks * 256);
+        return;
+    }
+    b -= a.dw_blocks;
+    join_splits(a.dx_slots, a.dx_splits, a.dx_slot_rows, a.d, *a.n_live, a.rows, a.dx, a.dx_bf16, (int64_t)b * 256 + threadIdx.x,
+                (int64_t)a.dx_blocks * 256);
 }
 
 // ---- workspace ----------------------------------------------------------------------------------------------------
@@ -441,35 +460,56 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
     int planes, pack_w;
-    int32_t ld, parts, width, pieces, dx_splits, dw_splits;
+    int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
+    bool direct;
     int64_t Tpad;
     bool dx_slots, dw_slots;
     size_t o_live, o_scales, o_max, o_rows, o_x, o_w, o_idx, o_p, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
 };
+
+// Classes per tile of a logits launch with `mt` token tiles: the width whose whole rounds over the SM pairs cost least, a
+// tile counted as its classes plus 32 for its hand-over; 256 unless the launch is short, since narrow tiles read more of x
+// per product.  (T = 1, V = 65536: 7 rounds of 128 take 24 us, 4 rounds of 256 27 us.)
+int32_t classes_per_tile(int64_t mt, int64_t V, int32_t least)
+{
+    const int64_t pairs = sm_count() > 1 ? sm_count() / 2 : 74;
+    int32_t best = kTile;
+    if (mt * ((V + kTile - 1) / kTile) >= 8 * pairs) return best;
+    int64_t cost = INT64_MAX;
+    for (int32_t bn = kTile; bn >= least; bn >>= 1) {
+        const int64_t c = (mt * ((V + bn - 1) / bn) + pairs - 1) / pairs * (bn + 32);
+        if (c < cost) { cost = c; best = bn; }
+    }
+    return best;
+}
 
 // Tile counts follow from the sizes alone; how many tokens are kept is known on the device only.
 Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward, bool dx_bf16)
 {
     Plan p = {};
     p.planes = dtype == TBN_F32 ? 2 : 1;
-    p.ld = (d + 7) / 8 * 8;
+    p.ld = (d + 63) / 64 * 64;                         // packed rows are whole 64-column panels
     p.pack_w = dtype == TBN_F32 || d % 8 != 0;
     p.Tpad = round_up64(T, kTile);
     const int64_t Vpad = round_up64(V, kTile);
-    p.parts = (int32_t)(Vpad / kStatCols);
+    // One tile of tokens in bf16: the forward reads x in place and leaves the dropped rows' results out at the end; with
+    // more tokens, dropping them first pays for its launch.
+    p.direct = !backward && T <= kTile && !p.pack_w;
     size_t o = 0;
     auto take = [&o](size_t bytes) { const size_t at = o; o += pad256(bytes); return at; };
     p.o_live = take(4);
     p.o_scales = take(sizeof(Scales));
-    p.o_max = take(12);
-    p.o_rows = take((size_t)p.Tpad * sizeof(RowInfo));
-    p.o_x = take((size_t)p.planes * p.Tpad * p.ld * 2);
+    p.o_max = take(3 * kMaxBlocks * 4);
+    p.o_rows = take(p.direct ? 0 : (size_t)p.Tpad * sizeof(RowInfo));
+    p.o_x = take(p.direct ? 0 : (size_t)p.planes * p.Tpad * p.ld * 2);
     p.o_w = take(p.pack_w ? (size_t)p.planes * V * p.ld * 2 : 0);
     p.o_idx = take((size_t)T * K * 4);
     p.o_p = take((size_t)T * K * 4);
     p.o_flags = take(K > 0 ? (size_t)T : 0);
     p.o_teacher = take(K > 0 ? (size_t)T * 8 : 0);
     if (!backward) {
+        p.bn = classes_per_tile(p.Tpad / kTile, V, 64);
+        p.parts = (int32_t)((V + p.bn - 1) / p.bn * 2);
         p.o_part = take((size_t)3 * p.parts * p.Tpad * 4);
     } else {
         int64_t width = (int64_t)(kPieceBytes / ((size_t)2 * p.planes * p.Tpad)) / kTile * kTile;
@@ -478,13 +518,14 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.pieces = (int32_t)((Vpad + width - 1) / width);
         p.width = (int32_t)round_up64((Vpad + p.pieces - 1) / p.pieces, kTile);
         p.pieces = (int32_t)((Vpad + p.width - 1) / p.width);
-        // a contraction is split when its few tiles would outlast the rest of the launch: no item longer than half of
-        // an SM pair's even share of the work, or 8 steps
+        p.bn = classes_per_tile(p.Tpad / kTile, V < p.width ? V : p.width, 128);
+        // A contraction is split when its few tiles would outlast the rest of the launch: no item longer than an SM pair's
+        // even share of the work (or 8 steps, 3 of the three-product form, below which a tile's own cost shows).
         const int64_t nt = (d + kTile - 1) / kTile, mt = p.Tpad / kTile, vt = p.width / kTile;
         const int64_t kx = p.width / 64, kw = (T + 63) / 64;
         const int64_t work = mt * nt * kx + vt * nt * kw;
-        int64_t most = work / (2 * 74);
-        if (most < 8) most = 8;
+        const int64_t pairs = sm_count() > 1 ? sm_count() / 2 : 74, least = p.planes == 1 ? 8 : 3;
+        const int64_t most = work / pairs > least ? work / pairs : least;
         auto splits = [most](int64_t k) { const int64_t s = (k + most - 1) / most; return (int32_t)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s); };
         p.dx_splits = splits(kx);
         p.dw_splits = splits(kw);
@@ -510,7 +551,7 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
 {
     int32_t *n_live = reinterpret_cast<int32_t *>(ws + p.o_live);
     Scales *scales = reinterpret_cast<Scales *>(ws + p.o_scales);
-    unsigned int *max_bits = reinterpret_cast<unsigned int *>(ws + p.o_max);
+    float *max_part = reinterpret_cast<float *>(ws + p.o_max);
     RowInfo *rows = reinterpret_cast<RowInfo *>(ws + p.o_rows);
     const bool f32 = c.dtype == TBN_F32;
     Labels labels = {c.targets, c.ignore_index, c.V, nullptr};
@@ -536,42 +577,41 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         out->list_p = prob;
         out->K = c.K;
     }
-    if (f32) {
-        if (cudaMemsetAsync(max_bits, 0, 12, s) != cudaSuccess) return TBN_ERR_CUDA;
-        const int64_t count = (int64_t)c.V * c.d;
-        abs_max_kernel<<<blocks_for(count > c.T * c.d ? count : c.T * c.d, 4096, 1184), 256, 0, s>>>(
-            static_cast<const float *>(c.x), labels, c.T, c.d, static_cast<const float *>(c.w), count, backward ? c.dloss : nullptr, c.tau, max_bits);
-        if (cudaGetLastError() != cudaSuccess) return TBN_ERR_CUDA;
-    }
-    if (p.pack_w) {
-        const unsigned grid = blocks_for((int64_t)c.V * (p.ld / 8), 256, 2368);
-        uint16_t *wp = reinterpret_cast<uint16_t *>(ws + p.o_w);
-        const cudaError_t e = f32
-            ? launch_pdl(pack_weight_kernel<float>, dim3(grid), dim3(256), 0, s, static_cast<const float *>(c.w), (int64_t)c.V, c.d, p.ld, max_bits, wp)
-            : launch_pdl(pack_weight_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, s, static_cast<const __nv_bfloat16 *>(c.w), (int64_t)c.V, c.d,
-                         p.ld, max_bits, wp);
-        if (e != cudaSuccess) return TBN_ERR_CUDA;
+    out->labels = labels;
+    const int32_t w_ld = p.pack_w ? p.ld : c.d;
+    out->w = Operand{p.pack_w ? static_cast<const void *>(ws + p.o_w) : c.w, c.V, c.V, w_ld, w_ld};
+    out->planes = p.planes; out->bn = p.bn;
+    out->bias = c.bias; out->scale2 = kLog2e / c.tau; out->T = c.T; out->Tpad = p.Tpad; out->V = c.V;
+    out->status = c.status;
+    if (p.direct) {
+        out->x = Operand{c.x, c.T, c.T, c.d, c.d};
+        return TBN_OK;
     }
     PackArgs a = {};
-    a.labels = labels; a.T = c.T; a.Tpad = p.Tpad; a.d = c.d; a.ld = p.ld;
+    if (f32) {
+        const int64_t count = (int64_t)c.V * c.d;
+        a.max_blocks = (int32_t)blocks_for(count > c.T * c.d ? count : c.T * c.d, 4096, kMaxBlocks);
+        if (launch_pdl(abs_max_kernel, dim3((unsigned)a.max_blocks), dim3(256), 0, s, static_cast<const float *>(c.x), labels, c.T, c.d,
+                       static_cast<const float *>(c.w), count, backward ? c.dloss : nullptr, c.tau, max_part) != cudaSuccess)
+            return TBN_ERR_CUDA;
+    }
+    a.labels = labels; a.T = c.T; a.Tpad = p.Tpad; a.V = c.V; a.d = c.d; a.ld = p.ld;
     a.per_block = (c.T + 591) / 592 < 8 ? 8 : (c.T + 591) / 592;
-    const unsigned blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);      // the last block has rows of its own
-    a.max_bits = max_bits; a.xc = reinterpret_cast<uint16_t *>(ws + p.o_x); a.rows = rows; a.n_live = n_live; a.scales = scales; a.tau = c.tau;
+    a.row_blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);              // the last one has rows of its own
+    a.max_part = max_part; a.xc = reinterpret_cast<uint16_t *>(ws + p.o_x); a.wc = reinterpret_cast<uint16_t *>(ws + p.o_w);
+    a.rows = rows; a.n_live = n_live; a.scales = scales; a.tau = c.tau;
     if (backward) {
         a.lse = c.lse; a.dloss = c.dloss; a.dx = c.dx; a.dx_bytes = c.dx_dtype == TBN_F32 ? 4 : 2;
     } else {
         a.loss_out = c.loss_out; a.lse_out = c.lse_out;
     }
-    const cudaError_t e = f32 ? launch_pdl(pack_rows_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x), a)
-                              : launch_pdl(pack_rows_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, static_cast<const __nv_bfloat16 *>(c.x), a);
+    const unsigned blocks = a.row_blocks + (p.pack_w ? blocks_for((int64_t)c.V * (p.ld / 8), 256, 2368) : 0u);
+    const cudaError_t e = f32 ? launch_pdl(pack_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x), static_cast<const float *>(c.w), a)
+                              : launch_pdl(pack_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, static_cast<const __nv_bfloat16 *>(c.x),
+                                           static_cast<const __nv_bfloat16 *>(c.w), a);
     if (e != cudaSuccess) return TBN_ERR_CUDA;
-
     out->x = Operand{ws + p.o_x, p.Tpad, p.Tpad, p.ld, p.ld};
-    out->w = Operand{p.pack_w ? static_cast<const void *>(ws + p.o_w) : c.w, c.V, c.V, p.ld, p.ld};
-    out->planes = p.planes;
     out->n_live = n_live; out->rows = rows; out->scales = f32 ? scales : nullptr;
-    out->bias = c.bias; out->scale2 = kLog2e / c.tau; out->T = c.T; out->Tpad = p.Tpad; out->V = c.V;
-    out->status = c.status;
     return TBN_OK;
 }
 
@@ -600,7 +640,7 @@ int forward(const HeadCall &c, void *workspace, cudaStream_t s)
     const int rb = c.T >= 4096 ? 32 : c.T >= 256 ? 8 : 1;
     const dim3 grid((unsigned)((c.T + rb - 1) / rb));
     auto kern = rb == 32 ? combine_kernel<32> : rb == 8 ? combine_kernel<8> : combine_kernel<1>;
-    return launch_pdl(kern, grid, dim3(256), 0, s, a.part_max, a.part_sum, a.part_dot, p.parts, p.Tpad, a.n_live, a.rows, teacher, c.tau,
+    return launch_pdl(kern, grid, dim3(256), 0, s, a.part_max, a.part_sum, a.part_dot, p.parts, p.Tpad, a.n_live, a.rows, a.labels, (int32_t)c.T, teacher, c.tau,
                       c.loss_out, c.lse_out) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 
@@ -629,36 +669,31 @@ int backward(const HeadCall &c, void *workspace, cudaStream_t s)
         a.width = c.V - a.v0 < p.width ? c.V - a.v0 : p.width;
         rc = launch_head_dz(a, s);
         if (rc != TBN_OK) return rc;
-        if (c.db && launch_pdl(bias_grad_kernel, dim3((unsigned)((a.width + 31) / 32)), dim3(256), 0, s, static_cast<const float *>(a.col_part), a.ldz,
-                               a.n_live, a.scales, a.width, c.db + a.v0) != cudaSuccess)
-            return TBN_ERR_CUDA;
-        if (!g.want_dx && !g.want_dw) continue;
-        g.v0 = a.v0; g.width = a.width;
-        g.dx_add = piece > 0;
-        g.dx_last = piece == p.pieces - 1;
-        rc = launch_head_grads(g, s);
-        if (rc != TBN_OK) return rc;
-        if (g.want_dw && p.dw_splits > 1) {
-            const int64_t rows = a.width;
-            const unsigned grid = blocks_for(rows * c.d, 1024, 1184);
-            const int64_t slot_rows = round_up64(a.width, kTile);
-            const RowInfo *none = nullptr;
-            const cudaError_t e = g.dw_bf16
-                ? launch_pdl(join_splits_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, s, static_cast<const float *>(g.dw_slots), p.dw_splits, slot_rows,
-                             c.d, a.n_live, none, rows, static_cast<__nv_bfloat16 *>(c.dw) + (int64_t)a.v0 * c.d)
-                : launch_pdl(join_splits_kernel<float>, dim3(grid), dim3(256), 0, s, static_cast<const float *>(g.dw_slots), p.dw_splits, slot_rows, c.d,
-                             a.n_live, none, rows, static_cast<float *>(c.dw) + (int64_t)a.v0 * c.d);
-            if (e != cudaSuccess) return TBN_ERR_CUDA;
+        const bool grads = g.want_dx || g.want_dw, last = piece == p.pieces - 1;
+        if (grads) {
+            g.v0 = a.v0; g.width = a.width;
+            g.dx_add = piece > 0;
+            g.dx_last = last;
+            rc = launch_head_grads(g, s);
+            if (rc != TBN_OK) return rc;
         }
-    }
-    if (g.want_dx && p.dx_splits > 1) {
-        const unsigned grid = blocks_for(c.T * c.d, 1024, 1184);
-        const cudaError_t e = dx_bf16
-            ? launch_pdl(join_splits_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, s, static_cast<const float *>(g.dx_slots), p.dx_splits, p.Tpad, c.d,
-                         a.n_live, a.rows, (int64_t)0, static_cast<__nv_bfloat16 *>(c.dx))
-            : launch_pdl(join_splits_kernel<float>, dim3(grid), dim3(256), 0, s, static_cast<const float *>(g.dx_slots), p.dx_splits, p.Tpad, c.d, a.n_live,
-                         a.rows, (int64_t)0, static_cast<float *>(c.dx));
-        if (e != cudaSuccess) return TBN_ERR_CUDA;
+        FinishArgs f = {};
+        f.n_live = a.n_live; f.rows = a.rows; f.scales = a.scales; f.d = c.d; f.width = a.width;
+        if (c.db) {
+            f.col_part = a.col_part; f.ldz = a.ldz; f.db = c.db + a.v0;
+            f.bias_blocks = (unsigned)((a.width + 31) / 32);
+        }
+        if (g.want_dw && p.dw_splits > 1) {
+            f.dw_blocks = blocks_for((int64_t)a.width * c.d, 1024, 1184);
+            f.dw_slots = g.dw_slots; f.dw_splits = p.dw_splits; f.dw_slot_rows = round_up64(a.width, kTile); f.dw_bf16 = g.dw_bf16;
+            f.dw = static_cast<char *>(c.dw) + (int64_t)a.v0 * c.d * (g.dw_bf16 ? 2 : 4);
+        }
+        if (g.want_dx && p.dx_splits > 1 && last) {
+            f.dx_blocks = blocks_for(c.T * c.d, 1024, 1184);
+            f.dx_slots = g.dx_slots; f.dx_splits = p.dx_splits; f.dx_slot_rows = p.Tpad; f.dx_bf16 = dx_bf16; f.dx = c.dx;
+        }
+        const unsigned blocks = f.bias_blocks + f.dw_blocks + f.dx_blocks;
+        if (blocks && launch_pdl(finish_kernel, dim3(blocks), dim3(256), 0, s, f) != cudaSuccess) return TBN_ERR_CUDA;
     }
     return TBN_OK;
 }

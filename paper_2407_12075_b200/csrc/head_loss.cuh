@@ -8,7 +8,6 @@ namespace tbn {
 namespace head {
 
 constexpr int kTile = 256;                 // tokens x classes of one output tile (two CTAs, 128 rows each)
-constexpr int kStatCols = 128;             // classes behind one (maximum, sum, dot) triple
 constexpr int kMaxSplits = 16;
 
 __host__ __device__ inline int64_t round_up64(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
@@ -31,11 +30,28 @@ struct Operand {
     int32_t cols, ld;                      // columns that exist, row pitch in elements (a multiple of 8)
 };
 
+// Which tokens take part.
+struct Labels {
+    const int64_t *target;                 // cross entropy
+    int64_t ignore_index;
+    int32_t V;
+    const uint8_t *flags;                  // distillation: written by teacher_kernel
+    __device__ __forceinline__ bool live(int64_t t) const {
+        if (flags) return flags[t] != 0;
+        const int64_t c = target[t];
+        return c != ignore_index && c >= 0 && c < V;
+    }
+};
+
+int sm_count();
+
 struct LogitsArgs {                        // logits of all kept tokens against classes [v0, v0 + width)
     Operand x, w;
     int planes;
-    const int32_t *n_live;
-    const RowInfo *rows;
+    const int32_t *n_live;                 // null: the T rows in their own order (forward)
+    const RowInfo *rows;                   // null with n_live
+    Labels labels;                         // used without rows
+    int32_t bn;                            // classes of a tile: 64 (forward only), 128 or 256
     const Scales *scales;                  // null: all 1
     const float *bias;                     // V or null
     float scale2;                          // log2(e) / tau
@@ -44,10 +60,10 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const int32_t *list_idx;               // distillation: [T][K] ascending, INT32_MAX behind the last entry; else null
     const float *list_p;
     int32_t K;
-    // forward: [stat column][Tpad]
+    // forward: a (maximum, sum, dot) triple for every bn / 2 classes and token: [triple][Tpad]
     float *part_max, *part_sum, *part_dot;
     // backward
-    void *dz;                              // [planes][Tpad][ldz]
+    void *dz;                              // [planes][ldz / 64][Tpad][64], see tc_head.cu
     int32_t ldz;
     float *col_part;                       // [Tpad / 32][ldz] or null
     int *status;

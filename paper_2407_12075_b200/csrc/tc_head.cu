@@ -15,6 +15,11 @@
 // tensor-memory quadrant, 128 columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
 // main loop of the next.
 //
+// dz lives in blocks that are images of the shared-memory tiles: panels of 64 classes, in a panel one 128-byte line per
+// token, the 16-byte pieces of a line permuted by the low three bits of the token as the 128-byte swizzle of tcgen05 wants
+// them.  The same 8 KB of 64 tokens x 64 classes is a K-major tile for dX and an MN-major tile for dW, a warp writes its 32
+// tokens of a panel as one contiguous 4 KB bulk copy, and every tile is one or two contiguous reads.
+//
 // fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products lo*hi, hi*lo and
 // hi*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.  The tensor core cuts its running sum off toward
 // zero at every 16-element step, an error that grows with the length of the chain (measured, dot products of 1024: 2.6e-6
@@ -26,6 +31,7 @@
 // kernel winds down and returns.
 #include <cuda_fp16.h>
 
+#include <atomic>
 #include <climits>
 
 #include "head_loss.cuh"
@@ -42,24 +48,29 @@ constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr uint32_t kSideBytes = 128 * 128;             // one operand, one plane, one CTA: 128 rows x 64 elements
 constexpr uint32_t kStageBudget = 6 * 2 * kSideBytes;  // 192 KB of stages
+constexpr uint32_t kExchange = 4096;                   // per epilogue warp: 32 lines of 128 bytes
+constexpr int kMaxStages = 16;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kGroupM = 32;                            // token tiles that share a sweep over the classes
 
 enum { kStats = 0, kDz = 1, kGrads = 2 };
 
 struct Control {
-    uint64_t full[6], empty[6], d_full[2], d_empty[2];
+    uint64_t full[kMaxStages], empty[kMaxStages], d_full[2], d_empty[2];
     uint32_t tmem_base;
     int abort_flag;
-    alignas(16) float bias[kEpiWarps][kStatCols];
 };
 
 // Two jobs at most: (0) dX and (1) dW.  The logits kernels use job 0 alone.
 struct Maps { CUtensorMap a[2], b[2]; };
 
 struct LogitsParams {
-    const int32_t *n_live;
+    const int32_t *n_live;                 // null: all Tpad-padded rows below n_rows, in their own order (forward)
     const RowInfo *rows;
+    Labels labels;                         // without rows
+    int32_t n_rows;
+    int32_t bn;                            // classes of a tile: 64, 128 or 256
+    int32_t a_rows, stages;                // token rows of a CTA's tile that are loaded; pipeline stages
     const Scales *scales;
     const float *bias;
     float scale2;
@@ -78,8 +89,8 @@ struct GradParams {
     const RowInfo *rows;
     const Scales *scales;
     int64_t Tpad;
-    int32_t d, v0, width;
-    int32_t want_dx, want_dw;
+    int32_t d, v0, width, ldz;
+    int32_t want_dx, want_dw, w_panels;    // w_panels: w can be read as panels of 64 columns
     void *dx;
     float *dx_slots;
     int32_t dx_splits, dx_bf16, dx_add, dx_last;
@@ -107,6 +118,11 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *m
     asm volatile(
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
         ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2, int32_t c3, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
                                          uint32_t leader) {
@@ -137,25 +153,33 @@ __device__ __forceinline__ float exp2_approx(float v) {
 // ---- tile enumeration (the same arithmetic in every role) ----------------------------------------------
 struct Tile {
     int job, split;
-    int32_t m0, n0;                        // first row of the pair's tile on either side
+    int32_t m0, n0, bn;                    // first row of the pair's tile on either side, and its columns
     int32_t kb0, kb1;                      // 64-element steps
 };
 
+// Which tiles a CTA pair works on, in order.  The logits tiles are alike and dealt out in turn.  The gradient launch has
+// two kinds: the longer ones are dealt out first, in turn; the pairs that got one fewer then take short ones alone for as
+// many rounds as fit into a long one, and the rest is dealt out in turn again, beginning with those pairs.
 struct Schedule {
-    int32_t total;
+    int32_t n_long, n_short, stride, me, shift, early, rounds, mine;
     // logits
     int32_t mt, nt, kb;
-    // gradients: tiles of job 0 come first when its contraction is the longer one
-    int32_t first_job, count_first, nt_d, kb_job[2], splits[2], mt_job[2];
+    // gradients
+    int32_t long_job, nt_d, kb_job[2], splits[2], mt_job[2];
 
     template <int MODE>
     __device__ __forceinline__ void init(const KernelParams &p, int32_t n_live, int32_t k_logits) {
+        stride = gridDim.x >> 1;
+        me = blockIdx.x >> 1;
+        n_short = 0; shift = 0; early = stride; rounds = 0;
         if (MODE != kGrads) {
             mt = (n_live + kTile - 1) / kTile;
-            nt = (p.l.width + kTile - 1) / kTile;
+            nt = (p.l.width + p.l.bn - 1) / p.l.bn;
             kb = k_logits;
-            total = mt * nt;
+            n_long = mt * nt;
+            bn_logits = p.l.bn;
         } else {
+            d_cols = p.g.d;
             nt_d = (p.g.d + kTile - 1) / kTile;
             mt_job[0] = p.g.want_dx ? (n_live + kTile - 1) / kTile : 0;
             mt_job[1] = p.g.want_dw ? (p.g.width + kTile - 1) / kTile : 0;
@@ -163,33 +187,54 @@ struct Schedule {
             kb_job[1] = (n_live + 63) / 64;
             splits[0] = p.g.dx_splits;
             splits[1] = p.g.dw_splits;
-            first_job = kb_job[1] / splits[1] > kb_job[0] / splits[0] ? 1 : 0;
-            count_first = mt_job[first_job] * nt_d * splits[first_job];
-            total = count_first + mt_job[first_job ^ 1] * nt_d * splits[first_job ^ 1];
+            const int32_t l0 = kb_job[0] / splits[0], l1 = kb_job[1] / splits[1];
+            long_job = l1 > l0 ? 1 : 0;
+            n_long = mt_job[long_job] * nt_d * splits[long_job];
+            n_short = mt_job[long_job ^ 1] * nt_d * splits[long_job ^ 1];
+            shift = n_long % stride;
+            if (shift) {
+                early = stride - shift;
+                rounds = max(l0, l1) / max(1, min(l0, l1));
+            }
         }
+        mine = me < n_long ? (n_long - me + stride - 1) / stride : 0;
     }
+    // The pair's step-th tile; false behind the last one.
     template <int MODE>
-    __device__ __forceinline__ Tile get(int32_t i) const {
-        Tile t;
+    __device__ __forceinline__ bool get(int32_t step, Tile &t) const {
         if (MODE != kGrads) {
+            if (step >= mine) return false;
+            const int32_t i = me + step * stride;
             const int32_t per_group = kGroupM * nt, g = i / per_group, rem = i - g * per_group;
             const int32_t gm = min(kGroupM, mt - g * kGroupM), n = rem / gm;
             t.job = 0; t.split = 0;
             t.m0 = (g * kGroupM + (rem - n * gm)) * kTile;
-            t.n0 = n * kTile;
+            t.n0 = n * bn_logits;
+            t.bn = bn_logits;
             t.kb0 = 0; t.kb1 = kb;
-        } else {
-            t.job = first_job;
-            if (i >= count_first) { t.job ^= 1; i -= count_first; }
-            const int32_t row = i / nt_d;
-            t.n0 = (i - row * nt_d) * kTile;
-            t.split = row / mt_job[t.job];
-            t.m0 = (row - t.split * mt_job[t.job]) * kTile;
-            t.kb0 = (int32_t)((int64_t)t.split * kb_job[t.job] / splits[t.job]);
-            t.kb1 = (int32_t)((int64_t)(t.split + 1) * kb_job[t.job] / splits[t.job]);
+            return true;
         }
-        return t;
+        int32_t i;
+        if (step < mine) {
+            t.job = long_job;
+            i = me + step * stride;
+        } else {
+            t.job = long_job ^ 1;
+            const int32_t q = step - mine, pos = me >= shift ? me - shift : me - shift + stride;
+            if (pos >= early) i = rounds * early + q * stride + pos;
+            else i = q < rounds ? q * early + pos : rounds * early + (q - rounds) * stride + pos;
+            if (i >= n_short) return false;
+        }
+        const int32_t row = i / nt_d;
+        t.n0 = (i - row * nt_d) * kTile;
+        t.bn = d_cols - t.n0 > 128 ? 256 : d_cols - t.n0 > 64 ? 128 : 64;
+        t.split = row / mt_job[t.job];
+        t.m0 = (row - t.split * mt_job[t.job]) * kTile;
+        t.kb0 = (int32_t)((int64_t)t.split * kb_job[t.job] / splits[t.job]);
+        t.kb1 = (int32_t)((int64_t)(t.split + 1) * kb_job[t.job] / splits[t.job]);
+        return true;
     }
+    int32_t bn_logits, d_cols;
 };
 
 // The sparse side of a row: the target class with probability 1, or the teacher's ascending list.
@@ -237,34 +282,102 @@ __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
     return v[0];
 }
 
-template <int PL>
-__device__ __forceinline__ void store_dz(const KernelParams &p, int64_t row, int32_t col, const float (&v)[32]) {
-    uint32_t pk[16];
-    if (PL == 1) {
+// 32 columns of a row's bias times log2(e) / tau, -infinity behind the last class
+__device__ __forceinline__ void load_bias(const LogitsParams &l, int32_t c0, bool vec, float (&b)[32]) {
+    const float *src = l.bias + l.v0 + c0;
+    if (vec && c0 + 32 <= l.width) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+        for (int q = 0; q < 8; ++q) {
+            const float4 u = __ldg(reinterpret_cast<const float4 *>(src) + q);
+            b[4 * q] = u.x * l.scale2; b[4 * q + 1] = u.y * l.scale2; b[4 * q + 2] = u.z * l.scale2; b[4 * q + 3] = u.w * l.scale2;
         }
-        uint16_t *dst = static_cast<uint16_t *>(p.l.dz) + row * p.l.ldz + col;
-        st_global_v8(dst, pk);
-        st_global_v8(dst + 16, pk + 8);
     } else {
-        uint32_t lo[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-            const float2 back = __half22float2(h);
-            const __half2 r = __floats2half2_rn(v[2 * i] - back.x, v[2 * i + 1] - back.y);
-            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-            lo[i] = *reinterpret_cast<const uint32_t *>(&r);
+        for (int j = 0; j < 32; ++j) b[j] = c0 + j < l.width ? __ldg(src + j) * l.scale2 : -INFINITY;
+    }
+}
+
+// One line of a dz panel: this lane's 32 values as the pieces [4 * upper, 4 * upper + 4) of its 128 bytes
+__device__ __forceinline__ void put_pieces(uint32_t line, int lane, int upper, const uint32_t (&pk)[16]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        sts_v4(line + (uint32_t)(((upper * 4 + q) ^ (lane & 7)) << 4), pk[4 * q], pk[4 * q + 1], pk[4 * q + 2], pk[4 * q + 3]);
+}
+__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(dst), "r"(src), "r"(bytes)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t lds_b32(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// The 32 x 32 fp32 values of a warp's exchange lines, stored row by row.
+struct RowsOut {
+    void *out;
+    const float *prev;                     // added first, or null
+    int32_t row, prev_row;                 // this lane's row in out and prev
+    int32_t rows_in, d;
+};
+// FORM 0: fp32 in 16-byte pieces, 8 lanes a row.  1: bf16 in 16-byte pieces, 4 lanes a row.  2: element by element, a row at a time.
+template <int FORM>
+__device__ __forceinline__ void write_rows(const RowsOut &o, uint32_t exchange, int lane, int32_t c0, bool out_bf16)
+{
+    constexpr int kLanes = FORM == 0 ? 8 : FORM == 1 ? 4 : 32, kWide = 32 / kLanes, kSteps = kLanes;
+    const int sub = lane % kLanes;
+    const int32_t c = c0 + sub * kWide;
+    const bool col_in = c < o.d;
+#pragma unroll
+    for (int h = 0; h < kSteps; h += 4) {              // four rows per lane in flight
+        float x[4][kWide];
+        int32_t to[4];
+        bool in[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int r = (h + k) * (32 / kLanes) + lane / kLanes;
+            const uint32_t src = exchange + (uint32_t)r * 128;
+            to[k] = __shfl_sync(0xffffffffu, o.row, r);
+            const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
+            in[k] = col_in && r < o.rows_in;
+            if (FORM == 2) {
+                x[k][0] = __uint_as_float(lds_b32(src + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+                if (o.prev && in[k]) x[k][0] += o.prev[(int64_t)from * o.d + c];
+            } else {
+#pragma unroll
+                for (int q = 0; q < kWide / 4; ++q) {
+                    const uint4 u = lds_v4(src + (uint32_t)(((sub * (kWide / 4) + q) ^ (r & 7)) << 4));
+                    x[k][4 * q] = __uint_as_float(u.x); x[k][4 * q + 1] = __uint_as_float(u.y);
+                    x[k][4 * q + 2] = __uint_as_float(u.z); x[k][4 * q + 3] = __uint_as_float(u.w);
+                    if (o.prev && in[k]) {
+                        const float4 w = *reinterpret_cast<const float4 *>(o.prev + (int64_t)from * o.d + c + 4 * q);
+                        x[k][4 * q] += w.x; x[k][4 * q + 1] += w.y; x[k][4 * q + 2] += w.z; x[k][4 * q + 3] += w.w;
+                    }
+                }
+            }
         }
-        uint16_t *dst = static_cast<uint16_t *>(p.l.dz) + row * p.l.ldz + col;
-        st_global_v8(dst, pk);
-        st_global_v8(dst + 16, pk + 8);
-        dst += p.l.Tpad * p.l.ldz;
-        st_global_v8(dst, lo);
-        st_global_v8(dst + 16, lo + 8);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (!in[k]) continue;
+            const int64_t at = (int64_t)to[k] * o.d + c;
+            if (FORM == 0) {
+                *reinterpret_cast<float4 *>(static_cast<float *>(o.out) + at) = make_float4(x[k][0], x[k][1], x[k][2], x[k][3]);
+            } else if (FORM == 1) {
+                uint32_t pk[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(x[k][(2 * j) % kWide], x[k][(2 * j + 1) % kWide]);
+                    pk[j] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(o.out) + at) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            } else if (out_bf16) {
+                static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x[k][0]);
+            } else {
+                static_cast<float *>(o.out)[at] = x[k][0];
+            }
+        }
     }
 }
 
@@ -274,10 +387,10 @@ __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
 head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelParams p, const int32_t k_logits)
 {
     constexpr uint32_t kStage = 2 * PL * kSideBytes;
-    constexpr int kStages = kStageBudget / kStage;
+    constexpr int kFewStages = kStageBudget / kStage;
     constexpr uint32_t kFmt = PL == 1 ? 1u : 0u;       // bf16, or fp16 planes
-    // instruction descriptor: D fp32, M = 256, N = 256; bits 15 / 16 select the MN-major form of A / B
-    constexpr uint32_t kIdesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+    // instruction descriptor: D fp32, M = 256, N added per tile; bits 15 / 16 select the MN-major form of A / B
+    constexpr uint32_t kIdesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 4) << 24);
     // 128-byte swizzle, 8-row groups 1024 bytes apart, descriptor version 1
     constexpr uint32_t kDescHi = 64u | (1u << 14) | (2u << 29);
 
@@ -285,7 +398,8 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
     const uint32_t stage0 = raw + pad;
-    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget);
+    constexpr uint32_t kExchangeBytes = MODE == kStats ? 0u : kEpiWarps * kExchange;
+    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget + kExchangeBytes);
     volatile int *abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -293,7 +407,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
         ctl->abort_flag = 0;
         fence_barrier_init();
@@ -311,47 +425,61 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     const uint32_t tmem_base = ctl->tmem_base;
     pdl_wait();
 
-    const int32_t n_live = *(MODE == kGrads ? p.g.n_live : p.l.n_live);
+    const int32_t n_live = MODE == kGrads ? *p.g.n_live : p.l.n_live ? *p.l.n_live : p.l.n_rows;
     Schedule sched = {};
     sched.init<MODE>(p, n_live, k_logits);
-    const int32_t first = blockIdx.x >> 1, stride = gridDim.x >> 1;
+    Tile t;
     bool ok = true;
+    // A logits stage holds the rows that exist: with few tokens most of it is classes, and more stages fit.  (The MMAs read
+    // 128 token rows all the same; what lies behind the loaded ones belongs to later parts of the pipeline and only
+    // reaches the accumulator rows of tokens that do not exist.)
+    const uint32_t a_bytes = MODE == kGrads ? kSideBytes : (uint32_t)p.l.a_rows * 128;
+    const uint32_t b_bytes = MODE == kGrads ? kSideBytes : (uint32_t)p.l.bn * 64;
+    const uint32_t stage_bytes = PL * (a_bytes + b_bytes);
+    const uint32_t n_stages = MODE == kGrads ? kFewStages : (uint32_t)p.l.stages;
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         Pipe px;
-        for (int32_t i = first; i < sched.total && ok; i += stride) {
-            const Tile t = sched.get<MODE>(i);
-            const int32_t a0 = t.m0 + (int32_t)rank * 128, b0 = t.n0 + (int32_t)rank * 128;
+        for (int32_t step = 0; ok && sched.get<MODE>(step, t); ++step) {
+            const int32_t a0 = t.m0 + (int32_t)rank * 128, b0 = t.n0 + (int32_t)rank * (t.bn / 2);
             const CUtensorMap *ma = &maps.a[t.job], *mb = &maps.b[t.job];
             for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
                 ok = wait_bar(smem_u32(&ctl->empty[px.stage]), px.phase ^ 1u, abort_flag, p.status, (40 << 24) | (px.stage << 16) | detail);
                 if (!ok) break;
                 if (lane == 0) {
                     const uint32_t own = smem_u32(&ctl->full[px.stage]), bar = map_to_rank(own, 0);
-                    if (rank == 0) mbar_arrive_expect_tx(own, 2 * kStage);
-                    const uint32_t sa = stage0 + px.stage * kStage, sb = sa + PL * kSideBytes;
+                    const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
+                    if (MODE != kGrads) {
+                        // with at most 128 tokens the second CTA's half of the tile stays as it is: its rows reach no result
+                        const bool load_a = rank == 0 || p.l.a_rows == 128;
+                        if (rank == 0) mbar_arrive_expect_tx(own, PL * ((p.l.a_rows == 128 ? 2 : 1) * a_bytes + 2 * b_bytes));
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) {
-                        const uint32_t da = sa + pl * kSideBytes, db = sb + pl * kSideBytes;
-                        if (MODE != kGrads) {
-                            tma_load_pair(da, ma, kb * 64, a0, pl, bar);
-                            tma_load_pair(db, mb, kb * 64, p.l.v0 + b0, pl, bar);
-                        } else {
-                            if (t.job == 0) {                              // dz: tokens x classes, contraction over classes
-                                tma_load_pair(da, ma, kb * 64, a0, pl, bar);
-                            } else {                                       // dz: contraction over tokens
-                                tma_load_pair(da, ma, a0, kb * 64, pl, bar);
-                                tma_load_pair(da + kSideBytes / 2, ma, a0 + 64, kb * 64, pl, bar);
-                            }
+                        for (int pl = 0; pl < PL; ++pl) {
+                            if (load_a) tma_load_pair(sa + pl * a_bytes, ma, kb * 64, a0, pl, bar);
+                            tma_load_pair(sb + pl * b_bytes, mb, kb * 64, p.l.v0 + b0, pl, bar);
+                        }
+                    } else {
+                        // dX: dz as 128 tokens x 64 classes.  dW: as two panels of 64 tokens x 64 classes.  Two copies per
+                        // stage and plane: with four the producer needs 640 cycles for what the MMAs do in 512.
+                        if (rank == 0) mbar_arrive_expect_tx(own, 2 * kStage);
+#pragma unroll
+                        for (int pl = 0; pl < PL; ++pl) {
+                            const uint32_t da = sa + pl * kSideBytes, db = sb + pl * kSideBytes;
+                            if (t.job == 0) tma_load_pair(da, ma, 0, a0, kb, pl, bar);
+                            else tma_load_pair(da, ma, 0, kb * 64, a0 / 64, pl, bar);
                             const int32_t krow = (t.job == 0 ? p.g.v0 : 0) + kb * 64;
-                            tma_load_pair(db, mb, b0, krow, pl, bar);
-                            tma_load_pair(db + kSideBytes / 2, mb, b0 + 64, krow, pl, bar);
+                            if (t.job == 1 || p.g.w_panels) {
+                                tma_load_pair(db, mb, b0 & 63, krow, b0 >> 6, pl, bar);
+                            } else {                   // rows that are not whole panels
+                                tma_load_pair(db, mb, b0, krow, pl, bar);
+                                tma_load_pair(db + kSideBytes / 2, mb, b0 + 64, krow, pl, bar);
+                            }
                         }
                     }
                 }
                 __syncwarp();
-                px.advance(kStages);
+                px.advance(n_stages);
             }
         }
         if (!ok) {                                     // let copies in flight land before the shared memory goes away
@@ -364,14 +492,13 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0);
             const uint32_t leader = elect_one();
             Pipe px, pd;
-            for (int32_t i = first; i < sched.total && ok; i += stride) {
-                const Tile t = sched.get<MODE>(i);
+            for (int32_t step = 0; ok && sched.get<MODE>(step, t); ++step) {
                 if (PL == 1) {
                     ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
                     if (!ok) break;
                 }
                 const bool a_mn = MODE == kGrads && t.job == 1, b_mn = MODE == kGrads;
-                const uint32_t idesc = kIdesc | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
+                const uint32_t idesc = kIdesc | ((uint32_t)(t.bn >> 3) << 17) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u);
                 // low descriptor word: start address in 16-byte units, leading offset (between 64-element panels of the
                 // MN-major form: 8192 bytes).  A step of 16 along K: 32 bytes inside the swizzled row, or two 8-row groups.
                 const uint32_t a_hi = (a_mn ? 512u : 1u) << 16, b_hi = (b_mn ? 512u : 1u) << 16;
@@ -383,19 +510,18 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d_addr = tmem_u + pd.stage * kTile;
-                    const uint32_t sa = stage0 + px.stage * kStage, sb = sa + PL * kSideBytes;
+                    const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
                     const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
-                    constexpr uint32_t kPlane = kSideBytes >> 4;
 #pragma unroll
                     for (int term = 0; term < (PL == 1 ? 1 : 3); ++term) {       // two planes: lo*hi, hi*lo, hi*hi
-                        const uint32_t at = a_lo + (PL == 2 && term == 0 ? kPlane : 0u), bt = b_lo + (PL == 2 && term == 1 ? kPlane : 0u);
+                        const uint32_t at = a_lo + (PL == 2 && term == 0 ? a_bytes >> 4 : 0u), bt = b_lo + (PL == 2 && term == 1 ? b_bytes >> 4 : 0u);
 #pragma unroll
                         for (int st = 0; st < 4; ++st)
                             mma_pair(d_addr, at + st * a_step, bt + st * b_step, kDescHi, idesc,
                                      term > 0 || st > 0 ? 1u : (uint32_t)(PL == 1 && kb > t.kb0), leader);
                     }
                     commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
-                    px.advance(kStages);
+                    px.advance(n_stages);
                     if (PL == 2) {
                         commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
                         pd.advance(2);
@@ -414,9 +540,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
         }
         __syncwarp();
     } else {
-        // ---------------- epilogue: thread = row, 128 columns in chunks of 32 ----------------
+        // ---------------- epilogue: thread = row, half of the tile's columns in chunks of 32 ----------------
         const int ew = warp - 2, qd = warp & 3, half = ew >> 2;
-        const uint32_t t_lane = tmem_base + ((uint32_t)(qd * 32) << 16) + (uint32_t)half * 128;
+        const uint32_t t_lane = tmem_base + ((uint32_t)(qd * 32) << 16);
+        const uint32_t exchange = stage0 + kStageBudget + (uint32_t)ew * kExchange;
+        const uint32_t line = exchange + (uint32_t)lane * 128;
         Pipe pd;
         float sc = 1.0f, inv_g = 1.0f;
         if (MODE != kGrads) {
@@ -425,35 +553,30 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
         } else if (p.g.scales) {
             inv_g = p.g.scales->inv_g;
         }
-        for (int32_t i = first; i < sched.total; i += stride) {
-            const Tile t = sched.get<MODE>(i);
-            const int32_t row = t.m0 + (int32_t)rank * 128 + qd * 32 + lane;
-            const int32_t col0 = t.n0 + half * 128;
+        const bool bias_vec = BIAS && (reinterpret_cast<uintptr_t>(p.l.bias) & 15) == 0;
+        for (int32_t step = 0; sched.get<MODE>(step, t); ++step) {
+            const int32_t row0 = t.m0 + (int32_t)rank * 128 + qd * 32, row = row0 + lane;
+            const int32_t hc = t.bn >> 1, col0 = t.n0 + half * hc;
             const bool live = row < n_live;
             RowInfo info = {0.0f, 0.0f, -1, 0};
             Listed list;
-            const float *bias_s = ctl->bias[ew];
             if (MODE != kGrads) {
-                if (live) info = p.l.rows[row];
-                list.begin(p.l, info, live, p.l.v0 + col0);
-                if (BIAS) {                            // classes past the end get -infinity
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int32_t c = col0 + j * 32 + lane;
-                        ctl->bias[ew][j * 32 + lane] = c < p.l.width ? __ldg(p.l.bias + p.l.v0 + c) * p.l.scale2 : -INFINITY;
-                    }
-                    __syncwarp();
+                if (live) {
+                    if (p.l.rows) info = p.l.rows[row];
+                    else { info.row = row; if (!p.l.labels.flags && p.l.labels.live(row)) info.label = (int32_t)p.l.labels.target[row]; }
                 }
+                list.begin(p.l, info, live, p.l.v0 + col0);
             } else if (t.job == 0 && live) {
                 info.row = p.g.rows[row].row;
             }
+            // the tile's sums: left in tensor memory, or (two planes) added up from its 64-element chains in registers
             float acc[PL == 2 ? 128 : 1];
             uint32_t t_acc = 0;
             if (PL == 1) {
                 ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                 if (!ok) break;
                 tc_fence_after();
-                t_acc = t_lane + pd.stage * kTile;
+                t_acc = t_lane + pd.stage * kTile + (uint32_t)(half * hc);
             } else {
 #pragma unroll
                 for (int j = 0; j < 128; ++j) acc[PL == 2 ? j : 0] = 0.0f;
@@ -463,11 +586,13 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     tc_fence_after();
 #pragma unroll
                     for (int ch = 0; ch < 8; ++ch) {
-                        uint32_t r[16];
-                        tmem_ld_32x16(t_lane + pd.stage * kTile + ch * 16, r);
-                        tc_wait_ld();
+                        if (ch * 16 < hc) {
+                            uint32_t r[16];
+                            tmem_ld_32x16(t_lane + pd.stage * kTile + (uint32_t)(half * hc + ch * 16), r);
+                            tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) acc[PL == 2 ? ch * 16 + j : 0] += __uint_as_float(r[j]);
+                            for (int j = 0; j < 16; ++j) acc[PL == 2 ? ch * 16 + j : 0] += __uint_as_float(r[j]);
+                        }
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -476,8 +601,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 }
                 if (!ok) break;
             }
-            // 32 columns of the accumulated tile
-            auto load_chunk = [&](int ch, float (&out)[32]) {
+            auto load_chunk = [&](int ch, float (&out)[32]) {      // 32 columns of the tile
                 if (PL == 1) {
                     uint32_t r[32];
                     tmem_ld_32x32(t_acc + ch * 32, r);
@@ -494,17 +618,17 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 float m = -INFINITY, l = 0.0f, dot = 0.0f;
 #pragma unroll (PL == 2 ? 4 : 1)
                 for (int ch = 0; ch < 4; ++ch) {
+                    if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32;
-                    float v[32];
+                    float b[32], v[32];
+                    if (BIAS) load_bias(p.l, c0, bias_vec, b);
                     load_chunk(ch, v);
                     if (BIAS) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]);
-                    } else {
-                        if (c0 + 32 > p.l.width) {
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]);
+                    } else if (c0 + 32 > p.l.width) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
-                        }
+                        for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
                     }
                     const float vs = BIAS ? 1.0f : sc;
                     while (list.next < p.l.v0 + c0 + 32) {
@@ -529,112 +653,134 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     m = m_new;
                 }
                 if (live) {
-                    const int64_t at = (int64_t)((p.l.v0 + col0) / kStatCols) * p.l.Tpad + row;
+                    const int64_t at = (int64_t)((p.l.v0 + col0) / hc) * p.l.Tpad + row;
                     p.l.part_max[at] = m;
                     p.l.part_sum[at] = l;
                     p.l.part_dot[at] = dot;
                 }
             } else if (MODE == kDz) {
                 const bool all_live = __all_sync(0xffffffffu, live);
-#pragma unroll (PL == 2 ? 4 : 1)
-                for (int ch = 0; ch < 4; ++ch) {
-                    const int32_t c0 = col0 + ch * 32;
-                    float v[32];
-                    load_chunk(ch, v);
-                    if (BIAS) {
+                const int32_t panels = p.l.ldz / 64;
+                uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
+#pragma unroll (PL == 2 ? 2 : 1)
+                for (int pn = 0; pn < 2; ++pn) {                       // a panel of 64 classes: two chunks
+                    if (pn * 64 >= hc) continue;
+#pragma unroll (PL == 2 ? 2 : 1)
+                    for (int u = 0; u < 2; ++u) {
+                        const int ch = pn * 2 + u;
+                        const int32_t c0 = col0 + ch * 32;
+                        float b[32], v[32];
+                        if (BIAS) load_bias(p.l, c0, bias_vec, b);
+                        load_chunk(ch, v);
+                        if (BIAS) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]) - info.lse2;
-                    } else {
+                            for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]) - info.lse2;
+                        } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
-                        if (c0 + 32 > p.l.width) {
+                            for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
+                            if (c0 + 32 > p.l.width) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
+                                for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
+                        while (list.next < p.l.v0 + c0 + 32) {
+                            const int rel = list.next - (p.l.v0 + c0);
+                            const float sub = info.g * list.weight();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
+                            list.step();
+                        }
+                        __syncwarp();
+                        if (!all_live) {               // rows behind the last kept token: exact zeros, whatever was staged
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = live ? v[j] : 0.0f;
+                        }
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (PL == 1) {
+                                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                                pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+                            } else {
+                                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+                                const float2 back = __half22float2(h);
+                                pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+                                acc[PL == 2 ? ch * 32 + 2 * i : 0] = v[2 * i] - back.x;          // the low plane follows below
+                                acc[PL == 2 ? ch * 32 + 2 * i + 1 : 0] = v[2 * i + 1] - back.y;
+                            }
+                        }
+                        if (u == 0) {                  // the previous panel has left the exchange lines
+                            if (lane == 0) bulk_wait_read();
+                            __syncwarp();
+                        }
+                        put_pieces(line, lane, u, pk);
+                        if (p.l.col_part) {
+                            const float s = column_sums(v, lane);
+                            p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
                         }
                     }
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
-                    while (list.next < p.l.v0 + c0 + 32) {
-                        const int rel = list.next - (p.l.v0 + c0);
-                        const float sub = info.g * list.weight();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
-                        list.step();
-                    }
+                    fence_proxy_async();
                     __syncwarp();
-                    if (!all_live) {                   // rows behind the last kept token: exact zeros, whatever was staged
+                    const int32_t panel = (col0 >> 6) + pn;
+                    if (lane == 0) bulk_store(dz + ((int64_t)panel * p.l.Tpad + row0) * 64, exchange, kExchange);
+                    if (PL == 2) {
+                        if (lane == 0) bulk_wait_read();
+                        __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = live ? v[j] : 0.0f;
-                    }
-                    store_dz<PL>(p, row, c0, v);
-                    if (p.l.col_part) {
-                        const float s = column_sums(v, lane);
-                        p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
+                        for (int u = 0; u < 2; ++u) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int at = PL == 2 ? (pn * 2 + u) * 32 + 2 * i : 0;
+                                const __half2 h = __floats2half2_rn(acc[at], acc[PL == 2 ? at + 1 : 0]);
+                                pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+                            }
+                            put_pieces(line, lane, u, pk);
+                        }
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) bulk_store(dz + ((int64_t)(panels + panel) * p.l.Tpad + row0) * 64, exchange, kExchange);
                     }
                 }
             } else {
+                // The 32 x 32 values go through the warp's exchange lines so that the stores cover whole rows: a lane's own
+                // row at a time is 32 lines per store instruction, and the load / store unit takes one line per cycle.
                 const GradParams &g = p.g;
                 const bool empty = t.kb0 >= t.kb1;     // nothing was contracted: the accumulator holds no result
                 const bool is_dx = t.job == 0;
                 const float scale = g.scales ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : 1.0f;
-                const bool in = is_dx ? live : row < g.width;
+                const int32_t rows_in = (is_dx ? n_live : g.width) - row0;             // rows of this warp that exist
                 const int splits = is_dx ? g.dx_splits : g.dw_splits;
-                const int64_t slot_rows = is_dx ? g.Tpad : round_up64(g.width, kTile);
                 float *slot = is_dx ? g.dx_slots : g.dw_slots;
-                if (slot) slot += ((int64_t)t.split * slot_rows + row) * g.d;
+                if (slot) slot += ((int64_t)t.split * (is_dx ? g.Tpad : round_up64(g.width, kTile)) + row0) * g.d;
                 const bool to_slot = slot != nullptr && (splits > 1 || !(is_dx && g.dx_last));
-                const bool add = is_dx && g.dx_add;
-                const int out_bf16 = to_slot ? 0 : (is_dx ? g.dx_bf16 : g.dw_bf16);
-                const int64_t out_row = is_dx ? info.row : (int64_t)g.v0 + row;
-                void *out = to_slot ? static_cast<void *>(slot)
-                                    : out_bf16 ? static_cast<void *>(static_cast<__nv_bfloat16 *>(is_dx ? g.dx : g.dw) + out_row * g.d)
-                                               : static_cast<void *>(static_cast<float *>(is_dx ? g.dx : g.dw) + out_row * g.d);
-                const float *prev = add ? (slot ? slot : static_cast<const float *>(out)) : nullptr;
-                const bool vec = g.d % 8 == 0;
+                RowsOut o;
+                o.out = to_slot ? static_cast<void *>(slot) : is_dx ? g.dx : g.dw;
+                o.row = to_slot ? lane : is_dx ? info.row : g.v0 + row0 + lane;
+                o.prev = !(is_dx && g.dx_add) ? nullptr : slot ? slot : static_cast<const float *>(g.dx);
+                o.prev_row = slot ? lane : info.row;
+                o.rows_in = rows_in; o.d = g.d;
+                const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16), vec = g.d % 8 == 0;
 #pragma unroll (PL == 2 ? 4 : 1)
                 for (int ch = 0; ch < 4; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
-                    if (c0 >= g.d) break;
-                    float r[32];
-                    load_chunk(ch, r);
-                    if (in) {
+                    if (ch * 32 >= hc || c0 >= g.d) continue;
+                    float v[32];
+                    load_chunk(ch, v);
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const int32_t c = c0 + q * 8;
-                            if (c >= g.d) break;
-                            float v[8];
+                    for (int q = 0; q < 8; ++q) {
+                        float e[4];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) v[j] = empty ? 0.0f : r[q * 8 + j] * scale;
-                            if (vec) {
-                                if (prev) {
-                                    const float4 u0 = *reinterpret_cast<const float4 *>(prev + c), u1 = *reinterpret_cast<const float4 *>(prev + c + 4);
-                                    v[0] += u0.x; v[1] += u0.y; v[2] += u0.z; v[3] += u0.w;
-                                    v[4] += u1.x; v[5] += u1.y; v[6] += u1.z; v[7] += u1.w;
-                                }
-                                if (out_bf16) {
-                                    uint32_t pk[4];
-#pragma unroll
-                                    for (int j = 0; j < 4; ++j) {
-                                        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-                                        pk[j] = *reinterpret_cast<const uint32_t *>(&h);
-                                    }
-                                    *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + c) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                                } else {
-                                    float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(out) + c);
-                                    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
-                                    dst[1] = make_float4(v[4], v[5], v[6], v[7]);
-                                }
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    if (c + j >= g.d) break;
-                                    const float w = prev ? v[j] + prev[c + j] : v[j];
-                                    if (out_bf16) static_cast<__nv_bfloat16 *>(out)[c + j] = __float2bfloat16_rn(w);
-                                    else static_cast<float *>(out)[c + j] = w;
-                                }
-                            }
-                        }
+                        for (int j = 0; j < 4; ++j) e[j] = empty ? 0.0f : v[4 * q + j] * scale;
+                        sts_v4(line + (uint32_t)((q ^ (lane & 7)) << 4), __float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]),
+                               __float_as_uint(e[3]));
                     }
+                    __syncwarp();
+                    if (!vec) write_rows<2>(o, exchange, lane, c0, out_bf16);
+                    else if (out_bf16) write_rows<1>(o, exchange, lane, c0, true);
+                    else write_rows<0>(o, exchange, lane, c0, false);
                     __syncwarp();
                 }
             }
@@ -646,6 +792,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 pd.advance(2);
             }
         }
+        if (MODE == kDz && lane == 0) bulk_wait_all();
     }
 
     tc_fence_before();
@@ -658,15 +805,8 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 }
 
 // ---- host side -----------------------------------------------------------------------------------------
-int sm_count()
-{
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return n;
-}
-
 // 64 x box_rows boxes of an operand's planes; what lies outside is read as zero.
-bool make_map(CUtensorMap *map, const void *data, int32_t cols, int64_t rows, int planes, int32_t ld, int64_t plane_rows, int box_rows)
+bool make_map(CUtensorMap *map, const void *data, int32_t cols, int64_t rows, int64_t planes, int32_t ld, int64_t plane_rows, int box_rows)
 {
     EncodeTiledFn encode = encode_tiled_fn();
     if (!encode) return false;
@@ -678,40 +818,62 @@ bool make_map(CUtensorMap *map, const void *data, int32_t cols, int64_t rows, in
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Panels of 64 columns, `box_panels` of them (64 x box_rows each) per copy.  The rows are whole panels (ld % 64 == 0).
+bool make_panel_map(CUtensorMap *map, const void *data, int64_t rows, int64_t row_bytes, int64_t panels, int64_t panel_bytes, int64_t planes,
+                    int64_t plane_bytes, int box_rows, int box_panels, CUtensorMapSwizzle swizzle)
+{
+    EncodeTiledFn encode = encode_tiled_fn();
+    if (!encode) return false;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)panels, (cuuint64_t)planes};
+    const cuuint64_t strides[3] = {(cuuint64_t)row_bytes, (cuuint64_t)panel_bytes, (cuuint64_t)plane_bytes};
+    const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_panels, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(data), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int MODE, int PL, bool BIAS>
 int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_logits, cudaStream_t s)
 {
     const int pairs = sm_count() / 2;
     if (pairs <= 0) return TBN_ERR_CUDA;
     if (tiles <= 0) return TBN_OK;
-    const size_t smem = kStageBudget + sizeof(Control) + 1024;
+    constexpr size_t smem = kStageBudget + (MODE == kStats ? 0 : kEpiWarps * kExchange) + sizeof(Control) + 1024;
+    static_assert(smem <= 227 * 1024, "shared memory");
     auto kern = head_kernel<MODE, PL, BIAS>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return TBN_ERR_CUDA;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return TBN_ERR_CUDA;
+    static std::atomic<bool> ready[64];                // the attribute is per device; setting it twice is harmless
+    if (!ready[dev].load(std::memory_order_acquire)) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return TBN_ERR_CUDA;
+        ready[dev].store(true, std::memory_order_release);
+    }
     const unsigned grid = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
     return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, maps, p, k_logits) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
-}
-
-LogitsParams logits_params(const LogitsArgs &a)
-{
-    LogitsParams l = {};
-    l.n_live = a.n_live; l.rows = a.rows; l.scales = a.scales; l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad;
-    l.V = a.V; l.v0 = a.v0; l.width = a.width; l.list_idx = a.list_idx; l.list_p = a.list_p; l.K = a.K;
-    l.part_max = a.part_max; l.part_sum = a.part_sum; l.part_dot = a.part_dot;
-    l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
-    return l;
 }
 
 template <int MODE>
 int launch_logits(const LogitsArgs &a, cudaStream_t s)
 {
     Maps maps = {};
-    if (!make_map(&maps.a[0], a.x.data, a.x.cols, a.x.rows, a.planes, a.x.ld, a.x.plane_rows, 128) ||
-        !make_map(&maps.b[0], a.w.data, a.w.cols, a.w.rows, a.planes, a.w.ld, a.w.plane_rows, 128))
+    const int64_t rows = a.T < 128 ? (a.T + 7) / 8 * 8 : 128;
+    if (!make_map(&maps.a[0], a.x.data, a.x.cols, a.x.rows, a.planes, a.x.ld, a.x.plane_rows, (int)rows) ||
+        !make_map(&maps.b[0], a.w.data, a.w.cols, a.w.rows, a.planes, a.w.ld, a.w.plane_rows, a.bn / 2))
         return TBN_ERR_CUDA;
     KernelParams p = {};
-    p.l = logits_params(a);
+    LogitsParams &l = p.l;
+    l.n_live = a.n_live; l.rows = a.rows; l.labels = a.labels; l.n_rows = (int32_t)a.T; l.bn = a.bn;
+    // the second CTA's rows: none for T <= 128
+    l.a_rows = (int32_t)rows;
+    const int64_t stage = (int64_t)a.planes * (rows * 128 + a.bn * 64), fit = (kStageBudget - kSideBytes + rows * 128) / stage;
+    l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
+    l.scales = a.scales;
+    l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width;
+    l.list_idx = a.list_idx; l.list_p = a.list_p; l.K = a.K;
+    l.part_max = a.part_max; l.part_sum = a.part_sum; l.part_dot = a.part_dot;
+    l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
     p.status = a.status;
-    const int64_t tiles = (a.T + kTile - 1) / kTile * ((a.width + kTile - 1) / kTile);
+    const int64_t tiles = (a.T + kTile - 1) / kTile * ((a.width + a.bn - 1) / a.bn);
     if (tiles > INT_MAX) return TBN_ERR_UNSUPPORTED;
     const int32_t kb = (a.x.cols + 63) / 64;
     if (a.planes == 1) return a.bias ? launch<MODE, 1, true>(maps, p, tiles, kb, s) : launch<MODE, 1, false>(maps, p, tiles, kb, s);
@@ -720,22 +882,41 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
 
 }  // namespace
 
+// Streaming multiprocessors of the current device, 0 on error.
+int sm_count()
+{
+    static std::atomic<int> cache[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    int n = cache[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        cache[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
 int launch_head_stats(const LogitsArgs &a, cudaStream_t s) { return launch_logits<kStats>(a, s); }
 int launch_head_dz(const LogitsArgs &a, cudaStream_t s) { return launch_logits<kDz>(a, s); }
 
 int launch_head_grads(const GradArgs &a, cudaStream_t s)
 {
     Maps maps = {};
-    // dz rows are written for whole 256-token tiles; the tokens behind the last kept one are zeros
-    if (!make_map(&maps.a[0], a.dz, a.ldz, a.Tpad, a.planes, a.ldz, a.Tpad, 128) ||
-        !make_map(&maps.b[0], a.w.data, a.w.cols, a.w.rows, a.planes, a.w.ld, a.w.plane_rows, 64) ||
-        !make_map(&maps.a[1], a.dz, a.ldz, a.Tpad, a.planes, a.ldz, a.Tpad, 64) ||
-        !make_map(&maps.b[1], a.x.data, a.x.cols, a.x.rows, a.planes, a.x.ld, a.x.plane_rows, 64))
+    // dz lines are written for whole 256-token tiles; the tokens behind the last kept one are zeros
+    const int64_t dz_panels = a.ldz / 64, dz_panel = a.Tpad * 128;
+    const bool w_panels = a.w.ld % 64 == 0;
+    auto by_panels = [&a](CUtensorMap *m, const Operand &o) {
+        return make_panel_map(m, o.data, o.rows, (int64_t)o.ld * 2, o.ld / 64, 128, a.planes, o.plane_rows * o.ld * 2, 64, 2, CU_TENSOR_MAP_SWIZZLE_128B);
+    };
+    if (!make_panel_map(&maps.a[0], a.dz, a.Tpad, 128, dz_panels, dz_panel, a.planes, dz_panels * dz_panel, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !make_panel_map(&maps.a[1], a.dz, a.Tpad, 128, dz_panels, dz_panel, a.planes, dz_panels * dz_panel, 64, 2, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !(w_panels ? by_panels(&maps.b[0], a.w) : make_map(&maps.b[0], a.w.data, a.w.cols, a.w.rows, a.planes, a.w.ld, a.w.plane_rows, 64)) ||
+        !by_panels(&maps.b[1], a.x))
         return TBN_ERR_CUDA;
     KernelParams p = {};
     GradParams &g = p.g;
-    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width;
-    g.want_dx = a.want_dx; g.want_dw = a.want_dw;
+    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.ldz = a.ldz;
+    g.want_dx = a.want_dx; g.want_dw = a.want_dw; g.w_panels = w_panels;
     g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
     g.dw = a.dw; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;
     p.status = a.status;
