@@ -11,14 +11,14 @@
 // A pair of CTAs (cta_group::2) computes a 256 x 256 tile: each CTA stages 128 rows of A and 128 of B per 64-element
 // step, so a byte staged feeds twice the multiplications of a 128 x 256 tile on one CTA (per 64-element step and SM:
 // 32 KB instead of 48 KB for the same 4.2 MFLOP), which is what keeps shared memory and L2 below the tensor pipe.
-// Warp roles per CTA: 0 = TMA producer, 1 = MMA issuer (the first CTA of the pair only), 2-9 = epilogue, two warps per
-// tensor-memory quadrant, 128 columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
+// Warp roles per CTA: 0 = TMA producer of A, 1 = MMA issuer (the first CTA of the pair only), 2-9 = epilogue, two warps per
+// tensor-memory quadrant, 128 columns each, 10 = TMA producer of B.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
 // main loop of the next.
 //
 // dz lives in blocks that are images of the shared-memory tiles: panels of 64 classes, in a panel one 128-byte line per
 // token, the 16-byte pieces of a line permuted by the low three bits of the token as the 128-byte swizzle of tcgen05 wants
-// them.  The same 8 KB of 64 tokens x 64 classes is a K-major tile for dX and an MN-major tile for dW, a warp writes its 32
-// tokens of a panel as one contiguous 4 KB bulk copy, and every tile is one or two contiguous reads.
+// them.  The same 8 KB of 64 tokens x 64 classes is a K-major tile for dX and an MN-major tile for dW, and every tile is one
+// or two contiguous reads.
 //
 // fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products lo*hi, hi*lo and
 // hi*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.  The tensor core cuts its running sum off toward
@@ -45,7 +45,7 @@ namespace {
 using namespace tc;
 
 constexpr int kEpiWarps = 8;
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kThreads = 96 + 32 * kEpiWarps;
 constexpr uint32_t kSideBytes = 128 * 128;             // one operand, one plane, one CTA: 128 rows x 64 elements
 constexpr uint32_t kStageBudget = 6 * 2 * kSideBytes;  // 192 KB of stages
 constexpr uint32_t kExchange = 4096;                   // per epilogue warp: 32 lines of 128 bytes
@@ -113,16 +113,30 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
-// The copy lands in this CTA; its bytes are counted on the barrier of the pair's first CTA.
-__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar) {
+// The copy lands in this CTA; its bytes are counted on the barrier of the pair's first CTA.  Run by the whole converged warp,
+// performed by the elected lane, like the MMAs: in a branch taken by one lane every operand is a per-thread value that has to
+// be moved to the uniform registers first, which made the producer the slowest part of the pipeline.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2, uint32_t bar,
+                                              uint32_t leader) {
     asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2, int32_t c3, uint32_t bar) {
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2, int32_t c3,
+                                              uint32_t bar, uint32_t leader) {
     asm volatile(
-        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %7, 0;\n\t"
+        "@q cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];\n\t}"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void expect_tx_elect(uint32_t bar, uint32_t bytes, uint32_t leader) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(leader) : "memory");
 }
 __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
                                          uint32_t leader) {
@@ -297,24 +311,28 @@ __device__ __forceinline__ void load_bias(const LogitsParams &l, int32_t c0, boo
     }
 }
 
-// One line of a dz panel: this lane's 32 values as the pieces [4 * upper, 4 * upper + 4) of its 128 bytes
-__device__ __forceinline__ void put_pieces(uint32_t line, int lane, int upper, const uint32_t (&pk)[16]) {
+// A lane's 32 values as the pieces [4 * upper, 4 * upper + 4) of its line of a dz panel: two whole 32-byte sectors, whose
+// 16-byte halves trade places in odd lanes.  Straight from registers: through shared memory and a bulk copy the lines would
+// be written in one go, but the main loop's copies and MMAs use all of shared memory's bandwidth (tiles of d = 1024 took
+// 9.5 K cycles that way, against 8.2 K of MMAs).
+__device__ __forceinline__ void store_line(uint16_t *line, int lane, int upper, const uint32_t (&pk)[16]) {
+    const bool odd = (lane & 1) != 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        sts_v4(line + (uint32_t)(((upper * 4 + q) ^ (lane & 7)) << 4), pk[4 * q], pk[4 * q + 1], pk[4 * q + 2], pk[4 * q + 3]);
-}
-__device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t bytes) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\tcp.async.bulk.commit_group;" ::"l"(dst), "r"(src), "r"(bytes)
-                 : "memory");
+    for (int h = 0; h < 2; ++h) {
+        uint32_t v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = odd ? pk[8 * h + 4 + j] : pk[8 * h + j];
+            v[4 + j] = odd ? pk[8 * h + j] : pk[8 * h + 4 + j];
+        }
+        st_global_v8(line + (((upper * 4 + 2 * h) ^ (lane & 6)) << 3), v);
+    }
 }
 __device__ __forceinline__ uint32_t lds_b32(uint32_t addr) {
     uint32_t v;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr));
     return v;
 }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
 // The 32 x 32 fp32 values of a warp's exchange lines, stored row by row.
 struct RowsOut {
     void *out;
@@ -398,7 +416,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
     const uint32_t stage0 = raw + pad;
-    constexpr uint32_t kExchangeBytes = MODE == kStats ? 0u : kEpiWarps * kExchange;
+    constexpr uint32_t kExchangeBytes = MODE == kGrads ? kEpiWarps * kExchange : 0u;
     Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget + kExchangeBytes);
     volatile int *abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -438,47 +456,47 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     const uint32_t stage_bytes = PL * (a_bytes + b_bytes);
     const uint32_t n_stages = MODE == kGrads ? kFewStages : (uint32_t)p.l.stages;
 
-    if (warp == 0) {
-        // ---------------- TMA producer ----------------
+    if (warp == 0 || warp == 10) {
+        // ---------------- TMA producers: warp 0 brings A, warp 10 brings B ----------------
+        const bool is_a = warp == 0;
+        const uint32_t leader = elect_one();
+        const uint32_t full0 = __shfl_sync(0xffffffffu, smem_u32(&ctl->full[0]), 0), bar0 = map_to_rank(full0, 0);
+        const uint32_t sm0 = __shfl_sync(0xffffffffu, stage0, 0);
         Pipe px;
         for (int32_t step = 0; ok && sched.get<MODE>(step, t); ++step) {
-            const int32_t a0 = t.m0 + (int32_t)rank * 128, b0 = t.n0 + (int32_t)rank * (t.bn / 2);
-            const CUtensorMap *ma = &maps.a[t.job], *mb = &maps.b[t.job];
+            const int32_t r0 = is_a ? t.m0 + (int32_t)rank * 128 : t.n0 + (int32_t)rank * (t.bn / 2);
+            const int job = __shfl_sync(0xffffffffu, t.job, 0);
+            const CUtensorMap *map = is_a ? &maps.a[job] : &maps.b[job];
             for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
                 ok = wait_bar(smem_u32(&ctl->empty[px.stage]), px.phase ^ 1u, abort_flag, p.status, (40 << 24) | (px.stage << 16) | detail);
                 if (!ok) break;
-                if (lane == 0) {
-                    const uint32_t own = smem_u32(&ctl->full[px.stage]), bar = map_to_rank(own, 0);
-                    const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
-                    if (MODE != kGrads) {
-                        // with at most 128 tokens the second CTA's half of the tile stays as it is: its rows reach no result
-                        const bool load_a = rank == 0 || p.l.a_rows == 128;
-                        if (rank == 0) mbar_arrive_expect_tx(own, PL * ((p.l.a_rows == 128 ? 2 : 1) * a_bytes + 2 * b_bytes));
+                const uint32_t bar = bar0 + px.stage * 8, sa = sm0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
+                if (MODE != kGrads) {
+                    // with at most 128 tokens the second CTA's half of the tile stays as it is: its rows reach no result
+                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((p.l.a_rows == 128 ? 2 : 1) * a_bytes + 2 * b_bytes), leader);
 #pragma unroll
-                        for (int pl = 0; pl < PL; ++pl) {
-                            if (load_a) tma_load_pair(sa + pl * a_bytes, ma, kb * 64, a0, pl, bar);
-                            tma_load_pair(sb + pl * b_bytes, mb, kb * 64, p.l.v0 + b0, pl, bar);
-                        }
-                    } else {
-                        // dX: dz as 128 tokens x 64 classes.  dW: as two panels of 64 tokens x 64 classes.  Two copies per
-                        // stage and plane: with four the producer needs 640 cycles for what the MMAs do in 512.
-                        if (rank == 0) mbar_arrive_expect_tx(own, 2 * kStage);
+                    for (int pl = 0; pl < PL; ++pl) {
+                        if (!is_a) tma_load_pair(sb + pl * b_bytes, map, kb * 64, p.l.v0 + r0, pl, bar, leader);
+                        else if (rank == 0 || p.l.a_rows == 128) tma_load_pair(sa + pl * a_bytes, map, kb * 64, r0, pl, bar, leader);
+                    }
+                } else {
+                    // dX: dz as 128 tokens x 64 classes, dW: as two panels of 64 tokens x 64 classes
+                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, 2 * kStage, leader);
 #pragma unroll
-                        for (int pl = 0; pl < PL; ++pl) {
-                            const uint32_t da = sa + pl * kSideBytes, db = sb + pl * kSideBytes;
-                            if (t.job == 0) tma_load_pair(da, ma, 0, a0, kb, pl, bar);
-                            else tma_load_pair(da, ma, 0, kb * 64, a0 / 64, pl, bar);
-                            const int32_t krow = (t.job == 0 ? p.g.v0 : 0) + kb * 64;
-                            if (t.job == 1 || p.g.w_panels) {
-                                tma_load_pair(db, mb, b0 & 63, krow, b0 >> 6, pl, bar);
-                            } else {                   // rows that are not whole panels
-                                tma_load_pair(db, mb, b0, krow, pl, bar);
-                                tma_load_pair(db + kSideBytes / 2, mb, b0 + 64, krow, pl, bar);
-                            }
+                    for (int pl = 0; pl < PL; ++pl) {
+                        const uint32_t dst = (is_a ? sa : sb) + pl * kSideBytes;
+                        const int32_t krow = (job == 0 ? p.g.v0 : 0) + kb * 64;
+                        if (is_a) {
+                            if (job == 0) tma_load_pair(dst, map, 0, r0, kb, pl, bar, leader);
+                            else tma_load_pair(dst, map, 0, kb * 64, r0 / 64, pl, bar, leader);
+                        } else if (job == 1 || p.g.w_panels) {
+                            tma_load_pair(dst, map, r0 & 63, krow, r0 >> 6, pl, bar, leader);
+                        } else {                       // rows that are not whole panels
+                            tma_load_pair(dst, map, r0, krow, pl, bar, leader);
+                            tma_load_pair(dst + kSideBytes / 2, map, r0 + 64, krow, pl, bar, leader);
                         }
                     }
                 }
-                __syncwarp();
                 px.advance(n_stages);
             }
         }
@@ -662,86 +680,58 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const bool all_live = __all_sync(0xffffffffu, live);
                 const int32_t panels = p.l.ldz / 64;
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
-#pragma unroll (PL == 2 ? 2 : 1)
-                for (int pn = 0; pn < 2; ++pn) {                       // a panel of 64 classes: two chunks
-                    if (pn * 64 >= hc) continue;
-#pragma unroll (PL == 2 ? 2 : 1)
-                    for (int u = 0; u < 2; ++u) {
-                        const int ch = pn * 2 + u;
-                        const int32_t c0 = col0 + ch * 32;
-                        float b[32], v[32];
-                        if (BIAS) load_bias(p.l, c0, bias_vec, b);
-                        load_chunk(ch, v);
-                        if (BIAS) {
+#pragma unroll (PL == 2 ? 4 : 1)
+                for (int ch = 0; ch < 4; ++ch) {
+                    if (ch * 32 >= hc) continue;
+                    const int32_t c0 = col0 + ch * 32;
+                    float b[32], v[32];
+                    if (BIAS) load_bias(p.l, c0, bias_vec, b);
+                    load_chunk(ch, v);
+                    if (BIAS) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]) - info.lse2;
-                        } else {
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]) - info.lse2;
+                    } else {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
-                            if (c0 + 32 > p.l.width) {
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
+                        if (c0 + 32 > p.l.width) {
 #pragma unroll
-                                for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
-                            }
-                        }
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
-                        while (list.next < p.l.v0 + c0 + 32) {
-                            const int rel = list.next - (p.l.v0 + c0);
-                            const float sub = info.g * list.weight();
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
-                            list.step();
-                        }
-                        __syncwarp();
-                        if (!all_live) {               // rows behind the last kept token: exact zeros, whatever was staged
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = live ? v[j] : 0.0f;
-                        }
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (PL == 1) {
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                                pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-                            } else {
-                                const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-                                const float2 back = __half22float2(h);
-                                pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-                                acc[PL == 2 ? ch * 32 + 2 * i : 0] = v[2 * i] - back.x;          // the low plane follows below
-                                acc[PL == 2 ? ch * 32 + 2 * i + 1 : 0] = v[2 * i + 1] - back.y;
-                            }
-                        }
-                        if (u == 0) {                  // the previous panel has left the exchange lines
-                            if (lane == 0) bulk_wait_read();
-                            __syncwarp();
-                        }
-                        put_pieces(line, lane, u, pk);
-                        if (p.l.col_part) {
-                            const float s = column_sums(v, lane);
-                            p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
+                            for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
                         }
                     }
-                    fence_proxy_async();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
+                    while (list.next < p.l.v0 + c0 + 32) {
+                        const int rel = list.next - (p.l.v0 + c0);
+                        const float sub = info.g * list.weight();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
+                        list.step();
+                    }
                     __syncwarp();
-                    const int32_t panel = (col0 >> 6) + pn;
-                    if (lane == 0) bulk_store(dz + ((int64_t)panel * p.l.Tpad + row0) * 64, exchange, kExchange);
-                    if (PL == 2) {
-                        if (lane == 0) bulk_wait_read();
-                        __syncwarp();
+                    if (!all_live) {                   // rows behind the last kept token: exact zeros, whatever was staged
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            uint32_t pk[16];
+                        for (int j = 0; j < 32; ++j) v[j] = live ? v[j] : 0.0f;
+                    }
+                    uint16_t *dst = dz + ((int64_t)(c0 >> 6) * p.l.Tpad + row) * 64;
+                    uint32_t pk[16], lo[PL == 2 ? 16 : 1];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int at = PL == 2 ? (pn * 2 + u) * 32 + 2 * i : 0;
-                                const __half2 h = __floats2half2_rn(acc[at], acc[PL == 2 ? at + 1 : 0]);
-                                pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-                            }
-                            put_pieces(line, lane, u, pk);
+                    for (int i = 0; i < 16; ++i) {
+                        if (PL == 1) {
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+                        } else {
+                            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+                            const float2 back = __half22float2(h);
+                            const __half2 r = __floats2half2_rn(v[2 * i] - back.x, v[2 * i + 1] - back.y);
+                            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
+                            lo[PL == 2 ? i : 0] = *reinterpret_cast<const uint32_t *>(&r);
                         }
-                        fence_proxy_async();
-                        __syncwarp();
-                        if (lane == 0) bulk_store(dz + ((int64_t)(panels + panel) * p.l.Tpad + row0) * 64, exchange, kExchange);
+                    }
+                    store_line(dst, lane, (c0 >> 5) & 1, pk);
+                    if constexpr (PL == 2) store_line(dst + (int64_t)panels * p.l.Tpad * 64, lane, (c0 >> 5) & 1, lo);
+                    if (p.l.col_part) {
+                        const float s = column_sums(v, lane);
+                        p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
                     }
                 }
             } else {
@@ -792,7 +782,6 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 pd.advance(2);
             }
         }
-        if (MODE == kDz && lane == 0) bulk_wait_all();
     }
 
     tc_fence_before();
@@ -838,7 +827,7 @@ int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_log
     const int pairs = sm_count() / 2;
     if (pairs <= 0) return TBN_ERR_CUDA;
     if (tiles <= 0) return TBN_OK;
-    constexpr size_t smem = kStageBudget + (MODE == kStats ? 0 : kEpiWarps * kExchange) + sizeof(Control) + 1024;
+    constexpr size_t smem = kStageBudget + (MODE == kGrads ? kEpiWarps * kExchange : 0) + sizeof(Control) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory");
     auto kern = head_kernel<MODE, PL, BIAS>;
     int dev = 0;
