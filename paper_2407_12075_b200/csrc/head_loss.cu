@@ -46,8 +46,8 @@ __device__ __forceinline__ float warp_max(float v) {
 template <typename TL>
 __global__ void __launch_bounds__(32 * kTeacherWarps)
 teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, int64_t T, int32_t K, int32_t Kp, int32_t V,
-               float inv_tau, int32_t *__restrict__ list_idx, float *__restrict__ list_p, uint8_t *__restrict__ flags,
-               float2 *__restrict__ stats)
+               float inv_tau, int32_t bucket, int32_t *__restrict__ list_idx, float *__restrict__ list_p, uint16_t *__restrict__ list_start,
+               uint8_t *__restrict__ flags, float2 *__restrict__ stats)
 {
     extern __shared__ uint8_t teacher_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -111,6 +111,15 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
         const uint64_t k = key[j];
         list_idx[t * K + j] = (int32_t)(k >> 32);
         list_p[t * K + j] = prob[(uint32_t)k];
+    }
+    for (int32_t b = lane; b <= kBuckets; b += 32) {   // where each bucket of classes begins
+        const uint64_t first = (uint64_t)b * (uint64_t)bucket << 32;
+        int32_t lo = 0, hi = K;
+        while (lo < hi) {
+            const int32_t mid = (lo + hi) >> 1;
+            if (key[mid] < first) lo = mid + 1; else hi = mid;
+        }
+        list_start[t * (kBuckets + 1) + b] = (uint16_t)lo;
     }
     if (lane == 0) {
         flags[t] = any ? 1 : 0;
@@ -325,8 +334,8 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
 }
 
 // ---- forward: join the pieces of a row ------------------------------------------------------------------------
-// RB rows x (256 / RB) threads: every thread merges every (256 / RB)-th triple, then the threads of a row are merged in a
-// fixed order.
+// RB rows x (256 / RB) threads: every thread merges every (256 / RB)-th triple, then the threads of a row are merged
+// pairwise, in a fixed order.
 template <int RB>
 __global__ void __launch_bounds__(256)
 combine_kernel(const float *__restrict__ part_max, const float *__restrict__ part_sum, const float *__restrict__ part_dot, int32_t parts,
@@ -357,15 +366,20 @@ combine_kernel(const float *__restrict__ part_max, const float *__restrict__ par
         }
     }
     sm[threadIdx.x] = m; ss[threadIdx.x] = s; sd[threadIdx.x] = dot;
-    __syncthreads();
-    if (g == 0 && live) {
-        for (int i = 1; i < kParts; ++i) {
-            const float pm = sm[i * RB + r], ps = ss[i * RB + r];
-            dot += sd[i * RB + r];
+#pragma unroll
+    for (int h = kParts / 2; h > 0; h >>= 1) {
+        __syncthreads();
+        if (g < h) {
+            const int other = threadIdx.x + h * RB;
+            const float pm = sm[other], ps = ss[other];
+            dot += sd[other];
             const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.0f : mn;
             s = s * exp2f(m - ref) + ps * exp2f(pm - ref);
             m = mn;
+            sm[threadIdx.x] = m; ss[threadIdx.x] = s; sd[threadIdx.x] = dot;
         }
+    }
+    if (g == 0 && live) {
         const float lse2 = m + log2f(s);               // all classes at -infinity: -infinity + log2(0)
         const int64_t t = rows ? (int64_t)rows[row].row : row;
         lse[t] = lse2 * kLn2;
@@ -460,27 +474,44 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
     int planes, pack_w;
+    int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
     bool direct;
     int64_t Tpad;
     bool dx_slots, dw_slots;
-    size_t o_live, o_scales, o_max, o_rows, o_x, o_w, o_idx, o_p, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
+    size_t o_live, o_scales, o_max, o_rows, o_x, o_w, o_idx, o_p, o_start, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
 };
 
-// Classes per tile of a logits launch with `mt` token tiles: the width whose whole rounds over the SM pairs cost least, a
-// tile counted as its classes plus 32 for its hand-over; 256 unless the launch is short, since narrow tiles read more of x
-// per product.  (T = 1, V = 65536: 7 rounds of 128 take 24 us, 4 rounds of 256 27 us.)
-int32_t classes_per_tile(int64_t mt, int64_t V, int32_t least)
+// Classes per tile of a logits launch: the width whose whole rounds over the SM pairs cost least.  A round costs what it
+// stages per 64-element step (the token rows that exist and the classes) plus about 64 rows' worth for its hand-over.  256
+// when there are many rounds, where narrow tiles would only read x more often.
+int32_t classes_per_tile(int64_t T, int64_t V, int32_t most, int32_t least, int32_t step)
 {
-    const int64_t pairs = sm_count() > 1 ? sm_count() / 2 : 74;
-    int32_t best = kTile;
-    if (mt * ((V + kTile - 1) / kTile) >= 8 * pairs) return best;
+    const int64_t pairs = sm_count() > 1 ? sm_count() / 2 : 74, mt = (T + kTile - 1) / kTile;
+    int32_t best = most;
+    if (mt * ((V + most - 1) / most) >= 8 * pairs) return best;
     int64_t cost = INT64_MAX;
-    for (int32_t bn = kTile; bn >= least; bn >>= 1) {
-        const int64_t c = (mt * ((V + bn - 1) / bn) + pairs - 1) / pairs * (bn + 32);
+    for (int32_t bn = most; bn >= least; bn -= step) {
+        const int64_t c = (mt * ((V + bn - 1) / bn) + pairs - 1) / pairs * ((T < kTile ? T : kTile) + bn + 64);
         if (c < cost) { cost = c; best = bn; }
     }
     return best;
+}
+
+// Time of a gradient launch in units of one 64-element step, for n0 tiles of k0 steps and n1 tiles of k1 steps over the SM
+// pairs, longest first (the order of the kernel); `own`: what a tile costs beside its steps.
+int64_t grads_makespan(int64_t n0, int64_t k0, int64_t n1, int64_t k1, int64_t own, int64_t pairs)
+{
+    if (n0 > 0 && (n1 == 0 || k0 >= k1)) { const int64_t n = n0, k = k0; n0 = n1; k0 = k1; n1 = n; k1 = k; }      // 1: the longer
+    const int64_t l = k1 + own, sh = k0 + own, a = n1 / pairs, r = n1 % pairs;
+    int64_t t = (a + (r ? 1 : 0)) * l;
+    for (;; ++t) {
+        const int64_t late = r ? (t - (a + 1) * l) / sh : 0, early = (t - a * l) / sh;
+        const int64_t room = r * late + (pairs - r) * early;
+        if (room >= n0) return t;
+        const int64_t missing = (n0 - room) / pairs * sh;             // at least this much longer
+        if (missing > sh) t += missing - sh;
+    }
 }
 
 // Tile counts follow from the sizes alone; how many tokens are kept is known on the device only.
@@ -488,6 +519,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
 {
     Plan p = {};
     p.planes = dtype == TBN_F32 ? 2 : 1;
+    p.cols = dtype == TBN_F32 ? 128 : 256;
     p.ld = (d + 63) / 64 * 64;                         // packed rows are whole 64-column panels
     p.pack_w = dtype == TBN_F32 || d % 8 != 0;
     p.Tpad = round_up64(T, kTile);
@@ -505,10 +537,11 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     p.o_w = take(p.pack_w ? (size_t)p.planes * V * p.ld * 2 : 0);
     p.o_idx = take((size_t)T * K * 4);
     p.o_p = take((size_t)T * K * 4);
+    p.o_start = take(K > 0 ? (size_t)T * (kBuckets + 1) * 2 : 0);
     p.o_flags = take(K > 0 ? (size_t)T : 0);
     p.o_teacher = take(K > 0 ? (size_t)T * 8 : 0);
     if (!backward) {
-        p.bn = classes_per_tile(p.Tpad / kTile, V, 64);
+        p.bn = classes_per_tile(T, V, p.cols, 64, 32);
         p.parts = (int32_t)((V + p.bn - 1) / p.bn * 2);
         p.o_part = take((size_t)3 * p.parts * p.Tpad * 4);
     } else {
@@ -518,17 +551,24 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.pieces = (int32_t)((Vpad + width - 1) / width);
         p.width = (int32_t)round_up64((Vpad + p.pieces - 1) / p.pieces, kTile);
         p.pieces = (int32_t)((Vpad + p.width - 1) / p.width);
-        p.bn = classes_per_tile(p.Tpad / kTile, V < p.width ? V : p.width, 128);
-        // A contraction is split when its few tiles would outlast the rest of the launch: no item longer than an SM pair's
-        // even share of the work (or 8 steps, 3 of the three-product form, below which a tile's own cost shows).
-        const int64_t nt = (d + kTile - 1) / kTile, mt = p.Tpad / kTile, vt = p.width / kTile;
-        const int64_t kx = p.width / 64, kw = (T + 63) / 64;
-        const int64_t work = mt * nt * kx + vt * nt * kw;
-        const int64_t pairs = sm_count() > 1 ? sm_count() / 2 : 74, least = p.planes == 1 ? 8 : 3;
-        const int64_t most = work / pairs > least ? work / pairs : least;
-        auto splits = [most](int64_t k) { const int64_t s = (k + most - 1) / most; return (int32_t)(s < 1 ? 1 : s > kMaxSplits ? kMaxSplits : s); };
-        p.dx_splits = splits(kx);
-        p.dw_splits = splits(kw);
+        p.bn = classes_per_tile(T, V < p.width ? V : p.width, p.cols, 128, 128);
+        // A contraction is split when its few tiles would outlast the rest of the launch.  A split adds its share of the
+        // fp32 partial sums, written here and read by the pass that joins them: 8 bytes per element and split at a few
+        // TB/s, about 1 step per 2 M elements.  A tile costs about 6 steps beside its products, 2 of the three-product form.
+        const int64_t nt = (d + p.cols - 1) / p.cols, mt = p.Tpad / kTile, vt = (V < p.width ? round_up64(V, kTile) : p.width) / kTile;
+        const int64_t kx = p.width / 64, kw = (T + 63) / 64, pairs = sm_count() > 1 ? sm_count() / 2 : 74, own = p.planes == 1 ? 6 : 2;
+        int64_t best = INT64_MAX;
+        p.dx_splits = p.dw_splits = 1;
+        for (int32_t i = 1; i <= kMaxSplits && (i == 1 || 2 * i <= kx); ++i) {
+            for (int32_t j = 1; j <= kMaxSplits && (j == 1 || 2 * j <= kw); ++j) {
+                if (j > 1 && vt * nt * j > 4 * pairs) break;
+                const int64_t join = (i > 1 ? i * p.Tpad * d : 0) + (j > 1 ? j * vt * kTile * d : 0);
+                const int64_t c = grads_makespan(mt * nt * i, (kx + i - 1) / i, vt * nt * j, (kw + j - 1) / j, own, pairs) + (join >> 21) +
+                                  (join > 0 ? own : 0);
+                if (c < best) { best = c; p.dx_splits = i; p.dw_splits = j; }
+            }
+            if (mt * nt * i > 4 * pairs) break;
+        }
         p.dx_slots = p.dx_splits > 1 || (p.pieces > 1 && dx_bf16);
         p.dw_slots = p.dw_splits > 1;
         p.o_dz = take((size_t)p.planes * p.Tpad * p.width * 2);
@@ -565,17 +605,21 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         float *prob = reinterpret_cast<float *>(ws + p.o_p);
         uint8_t *flags = reinterpret_cast<uint8_t *>(ws + p.o_flags);
         float2 *stats = reinterpret_cast<float2 *>(ws + p.o_teacher);
+        uint16_t *start = reinterpret_cast<uint16_t *>(ws + p.o_start);
+        const int32_t bucket = (int32_t)(((int64_t)c.V + kBuckets - 1) / kBuckets);
         const cudaError_t e = c.top_dtype == TBN_F32
             ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
-                         c.T, c.K, Kp, c.V, 1.0f / c.tau, idx, prob, flags, stats)
+                         c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, idx, prob, start, flags, stats)
             : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index,
-                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, idx, prob, flags, stats);
+                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, idx, prob, start, flags, stats);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
         out->list_idx = idx;
         out->list_p = prob;
+        out->list_start = start;
         out->K = c.K;
+        out->bucket = bucket;
     }
     out->labels = labels;
     const int32_t w_ld = p.pack_w ? p.ld : c.d;

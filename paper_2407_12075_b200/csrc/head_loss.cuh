@@ -9,6 +9,7 @@ namespace head {
 
 constexpr int kTile = 256;                 // tokens x classes of one output tile (two CTAs, 128 rows each)
 constexpr int kMaxSplits = 16;
+constexpr int kBuckets = 64;                // of the vocabulary, into which a teacher's sorted list is divided
 
 __host__ __device__ inline int64_t round_up64(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
@@ -51,7 +52,7 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const int32_t *n_live;                 // null: the T rows in their own order (forward)
     const RowInfo *rows;                   // null with n_live
     Labels labels;                         // used without rows
-    int32_t bn;                            // classes of a tile: 64 (forward only), 128 or 256
+    int32_t bn;                            // classes of a tile: a multiple of 32 up to 256 (backward: 128 or 256)
     const Scales *scales;                  // null: all 1
     const float *bias;                     // V or null
     float scale2;                          // log2(e) / tau
@@ -59,7 +60,8 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     int32_t V, v0, width;
     const int32_t *list_idx;               // distillation: [T][K] ascending, INT32_MAX behind the last entry; else null
     const float *list_p;
-    int32_t K;
+    const uint16_t *list_start;            // [T][kBuckets + 1]
+    int32_t K, bucket;                     // classes per bucket
     // forward: a (maximum, sum, dot) triple for every bn / 2 classes and token: [triple][Tpad]
     float *part_max, *part_sum, *part_dot;
     // backward

@@ -11,8 +11,8 @@
 // A pair of CTAs (cta_group::2) computes a 256 x 256 tile: each CTA stages 128 rows of A and 128 of B per 64-element
 // step, so a byte staged feeds twice the multiplications of a 128 x 256 tile on one CTA (per 64-element step and SM:
 // 32 KB instead of 48 KB for the same 4.2 MFLOP), which is what keeps shared memory and L2 below the tensor pipe.
-// Warp roles per CTA: 0 = TMA producer of A, 1 = MMA issuer (the first CTA of the pair only), 2-9 = epilogue, two warps per
-// tensor-memory quadrant, 128 columns each, 10 = TMA producer of B.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
+// Warp roles per CTA: 0 = TMA producer of A, 1 = MMA issuer (the first CTA of the pair only), 2 = TMA producer of B, 3 idle,
+// 4-11 = epilogue, two warps per tensor-memory quadrant, 128 columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
 // main loop of the next.
 //
 // dz lives in blocks that are images of the shared-memory tiles: panels of 64 classes, in a panel one 128-byte line per
@@ -25,7 +25,8 @@
 // zero at every 16-element step, an error that grows with the length of the chain (measured, dot products of 1024: 2.6e-6
 // of the result's scale as one chain of 192 steps, 7e-7 for the bf16 form's 64), so with fp32 operands the chain ends
 // after every 64 elements: the small products first, then the four hi*hi steps, and the epilogue warps add the 64-element
-// sums in registers, rounding to nearest.  They keep up: 128 additions per thread against 12 steps of 256 x 256 x 16.
+// sums in registers, rounding to nearest.  For that the tiles are 256 x 128 (64 running sums per thread) on four accumulators:
+// with 256 x 256 and two, the hand-overs of a chain (commit, wait, read, release) outlast its MMAs.
 //
 // Same conventions as the other tcgen05 kernels: every wait is bounded, a wait that gives up records the status and the
 // kernel winds down and returns.
@@ -45,18 +46,22 @@ namespace {
 using namespace tc;
 
 constexpr int kEpiWarps = 8;
-constexpr int kThreads = 96 + 32 * kEpiWarps;
+constexpr int kThreads = 128 + 32 * kEpiWarps;
+constexpr int kMaxStages = 24;
 constexpr uint32_t kSideBytes = 128 * 128;             // one operand, one plane, one CTA: 128 rows x 64 elements
 constexpr uint32_t kStageBudget = 6 * 2 * kSideBytes;  // 192 KB of stages
 constexpr uint32_t kExchange = 4096;                   // per epilogue warp: 32 lines of 128 bytes
-constexpr int kMaxStages = 16;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kGroupM = 32;                            // token tiles that share a sweep over the classes
 
 enum { kStats = 0, kDz = 1, kGrads = 2 };
 
+// columns of a tile at most, and accumulators in the 512 columns of tensor memory
+template <int PL> constexpr int kCols = PL == 1 ? 256 : 128;
+template <int PL> constexpr int kAccs = 512 / kCols<PL>;
+
 struct Control {
-    uint64_t full[kMaxStages], empty[kMaxStages], d_full[2], d_empty[2];
+    uint64_t full[kMaxStages], empty[kMaxStages], d_full[4], d_empty[4];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -69,7 +74,7 @@ struct LogitsParams {
     const RowInfo *rows;
     Labels labels;                         // without rows
     int32_t n_rows;
-    int32_t bn;                            // classes of a tile: 64, 128 or 256
+    int32_t bn;                            // classes of a tile: a multiple of 32 from 64 to 256
     int32_t a_rows, stages;                // token rows of a CTA's tile that are loaded; pipeline stages
     const Scales *scales;
     const float *bias;
@@ -78,7 +83,8 @@ struct LogitsParams {
     int32_t V, v0, width;
     const int32_t *list_idx;
     const float *list_p;
-    int32_t K;
+    const uint16_t *list_start;            // [T][kBuckets + 1]: where the classes of each bucket begin in the row's list
+    int32_t K, bucket;
     float *part_max, *part_sum, *part_dot;
     void *dz;
     int32_t ldz;
@@ -110,8 +116,11 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// Tells the pair's MMA warp that an accumulator has been read.  Nothing in ordinary memory goes with it (tcgen05.wait::ld and
+// the tcgen05 fence order the reads), so no release at cluster scope: that waits for the thread's stores to global memory,
+// about a microsecond per hand-over.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 // The copy lands in this CTA; its bytes are counted on the barrier of the pair's first CTA.  Run by the whole converged warp,
 // performed by the elected lane, like the MMAs: in a branch taken by one lane every operand is a per-thread value that has to
@@ -181,7 +190,7 @@ struct Schedule {
     // gradients
     int32_t long_job, nt_d, kb_job[2], splits[2], mt_job[2];
 
-    template <int MODE>
+    template <int MODE, int PL>
     __device__ __forceinline__ void init(const KernelParams &p, int32_t n_live, int32_t k_logits) {
         stride = gridDim.x >> 1;
         me = blockIdx.x >> 1;
@@ -194,7 +203,7 @@ struct Schedule {
             bn_logits = p.l.bn;
         } else {
             d_cols = p.g.d;
-            nt_d = (p.g.d + kTile - 1) / kTile;
+            nt_d = (p.g.d + kCols<PL> - 1) / kCols<PL>;
             mt_job[0] = p.g.want_dx ? (n_live + kTile - 1) / kTile : 0;
             mt_job[1] = p.g.want_dw ? (p.g.width + kTile - 1) / kTile : 0;
             kb_job[0] = (p.g.width + 63) / 64;
@@ -214,7 +223,7 @@ struct Schedule {
         mine = me < n_long ? (n_long - me + stride - 1) / stride : 0;
     }
     // The pair's step-th tile; false behind the last one.
-    template <int MODE>
+    template <int MODE, int PL>
     __device__ __forceinline__ bool get(int32_t step, Tile &t) const {
         if (MODE != kGrads) {
             if (step >= mine) return false;
@@ -240,8 +249,8 @@ struct Schedule {
             if (i >= n_short) return false;
         }
         const int32_t row = i / nt_d;
-        t.n0 = (i - row * nt_d) * kTile;
-        t.bn = d_cols - t.n0 > 128 ? 256 : d_cols - t.n0 > 64 ? 128 : 64;
+        t.n0 = (i - row * nt_d) * kCols<PL>;
+        t.bn = d_cols - t.n0 > 128 ? kCols<PL> : d_cols - t.n0 > 64 ? 128 : 64;
         t.split = row / mt_job[t.job];
         t.m0 = (row - t.split * mt_job[t.job]) * kTile;
         t.kb0 = (int32_t)((int64_t)t.split * kb_job[t.job] / splits[t.job]);
@@ -266,12 +275,18 @@ struct Listed {
         idx = l.list_idx + (int64_t)r.row * l.K;
         p = l.list_p + (int64_t)r.row * l.K;
         count = live ? l.K : 0;
-        int32_t lo = 0, hi = count;                    // first entry >= first
-        while (lo < hi) {
-            const int32_t mid = (lo + hi) >> 1;
-            if (__ldg(idx + mid) < first) lo = mid + 1; else hi = mid;
+        if (count) {                                   // first entry >= first: between the starts of its bucket and the next
+            const int32_t bucket = first / l.bucket;
+            const uint16_t *start = l.list_start + (int64_t)r.row * (kBuckets + 1) + min(bucket, kBuckets - 1);
+            int32_t lo = __ldg(start), hi = bucket < kBuckets ? (int32_t)__ldg(start + 1) : count;
+            while (lo < hi) {
+                const int32_t mid = (lo + hi) >> 1;
+                if (__ldg(idx + mid) < first) lo = mid + 1; else hi = mid;
+            }
+            pos = lo;
+        } else {
+            pos = 0;
         }
-        pos = lo;
         next = pos < count ? __ldg(idx + pos) : INT_MAX;
     }
     __device__ __forceinline__ float weight() const { return idx ? __ldg(p + pos) : 1.0f; }
@@ -333,70 +348,75 @@ __device__ __forceinline__ uint32_t lds_b32(uint32_t addr) {
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr));
     return v;
 }
-// The 32 x 32 fp32 values of a warp's exchange lines, stored row by row.
+__device__ __forceinline__ void ld_global_v8(const float *ptr, float (&v)[8]) {
+    asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(ptr) : "memory");
+}
+// Where a warp's rows of dX or dW go.  prev: fp32 values added first, or null; row, prev_row: this lane's row in out and prev.
 struct RowsOut {
     void *out;
-    const float *prev;                     // added first, or null
-    int32_t row, prev_row;                 // this lane's row in out and prev
-    int32_t rows_in, d;
+    const float *prev;
+    int32_t row, prev_row, rows_in, d;
 };
-// FORM 0: fp32 in 16-byte pieces, 8 lanes a row.  1: bf16 in 16-byte pieces, 4 lanes a row.  2: element by element, a row at a time.
-template <int FORM>
-__device__ __forceinline__ void write_rows(const RowsOut &o, uint32_t exchange, int lane, int32_t c0, bool out_bf16)
+// 32 columns of every lane's row, in whole 32-byte sectors (d a multiple of 16, out 32-byte aligned).
+__device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_t c0, bool out_bf16, float (&v)[32])
 {
-    constexpr int kLanes = FORM == 0 ? 8 : FORM == 1 ? 4 : 32, kWide = 32 / kLanes, kSteps = kLanes;
-    const int sub = lane % kLanes;
-    const int32_t c = c0 + sub * kWide;
-    const bool col_in = c < o.d;
+    if (lane >= o.rows_in) return;
+    if (o.prev) {
 #pragma unroll
-    for (int h = 0; h < kSteps; h += 4) {              // four rows per lane in flight
-        float x[4][kWide];
-        int32_t to[4];
-        bool in[4];
+        for (int q = 0; q < 4; ++q) {
+            if (c0 + 8 * q >= o.d) break;
+            float w[8];
+            ld_global_v8(o.prev + (int64_t)o.prev_row * o.d + c0 + 8 * q, w);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = (h + k) * (32 / kLanes) + lane / kLanes;
-            const uint32_t src = exchange + (uint32_t)r * 128;
-            to[k] = __shfl_sync(0xffffffffu, o.row, r);
-            const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
-            in[k] = col_in && r < o.rows_in;
-            if (FORM == 2) {
-                x[k][0] = __uint_as_float(lds_b32(src + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
-                if (o.prev && in[k]) x[k][0] += o.prev[(int64_t)from * o.d + c];
-            } else {
-#pragma unroll
-                for (int q = 0; q < kWide / 4; ++q) {
-                    const uint4 u = lds_v4(src + (uint32_t)(((sub * (kWide / 4) + q) ^ (r & 7)) << 4));
-                    x[k][4 * q] = __uint_as_float(u.x); x[k][4 * q + 1] = __uint_as_float(u.y);
-                    x[k][4 * q + 2] = __uint_as_float(u.z); x[k][4 * q + 3] = __uint_as_float(u.w);
-                    if (o.prev && in[k]) {
-                        const float4 w = *reinterpret_cast<const float4 *>(o.prev + (int64_t)from * o.d + c + 4 * q);
-                        x[k][4 * q] += w.x; x[k][4 * q + 1] += w.y; x[k][4 * q + 2] += w.z; x[k][4 * q + 3] += w.w;
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (!in[k]) continue;
-            const int64_t at = (int64_t)to[k] * o.d + c;
-            if (FORM == 0) {
-                *reinterpret_cast<float4 *>(static_cast<float *>(o.out) + at) = make_float4(x[k][0], x[k][1], x[k][2], x[k][3]);
-            } else if (FORM == 1) {
-                uint32_t pk[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const __nv_bfloat162 b = __floats2bfloat162_rn(x[k][(2 * j) % kWide], x[k][(2 * j + 1) % kWide]);
-                    pk[j] = *reinterpret_cast<const uint32_t *>(&b);
-                }
-                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(o.out) + at) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-            } else if (out_bf16) {
-                static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x[k][0]);
-            } else {
-                static_cast<float *>(o.out)[at] = x[k][0];
-            }
+            for (int j = 0; j < 8; ++j) v[8 * q + j] += w[j];
         }
     }
+    const int64_t at = (int64_t)o.row * o.d + c0;
+    if (out_bf16) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (c0 + 16 * h >= o.d) break;
+            uint32_t pk[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * h + 2 * j], v[16 * h + 2 * j + 1]);
+                pk[j] = *reinterpret_cast<const uint32_t *>(&b);
+            }
+            st_global_v8(static_cast<__nv_bfloat16 *>(o.out) + at + 16 * h, pk);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (c0 + 8 * q >= o.d) break;
+            uint32_t u[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * q + j]);
+            st_global_v8(static_cast<float *>(o.out) + at + 8 * q, u);
+        }
+    }
+}
+// Rows that are not whole sectors: through the warp's exchange lines, then a row at a time, lane = column.
+__device__ __forceinline__ void write_elements(const RowsOut &o, uint32_t exchange, int lane, int32_t c0, bool out_bf16, const float (&v)[32])
+{
+    const uint32_t line = exchange + (uint32_t)lane * 128;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+        sts_v4(line + (uint32_t)((q ^ (lane & 7)) << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
+               __float_as_uint(v[4 * q + 3]));
+    __syncwarp();
+    const int32_t c = c0 + lane;
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r) {
+        const int32_t to = __shfl_sync(0xffffffffu, o.row, r), from = __shfl_sync(0xffffffffu, o.prev_row, r);
+        float x = __uint_as_float(lds_b32(exchange + (uint32_t)r * 128 + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+        if (r >= o.rows_in || c >= o.d) continue;
+        if (o.prev) x += o.prev[(int64_t)from * o.d + c];
+        const int64_t at = (int64_t)to * o.d + c;
+        if (out_bf16) static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x);
+        else static_cast<float *>(o.out)[at] = x;
+    }
+    __syncwarp();
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------
@@ -404,7 +424,8 @@ template <int MODE, int PL, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
 head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelParams p, const int32_t k_logits)
 {
-    constexpr uint32_t kStage = 2 * PL * kSideBytes;
+    constexpr uint32_t kBBytes = kCols<PL> * 64;       // B of a gradient tile: one plane, one CTA
+    constexpr uint32_t kStage = PL * (kSideBytes + kBBytes);
     constexpr int kFewStages = kStageBudget / kStage;
     constexpr uint32_t kFmt = PL == 1 ? 1u : 0u;       // bf16, or fp16 planes
     // instruction descriptor: D fp32, M = 256, N added per tile; bits 15 / 16 select the MN-major form of A / B
@@ -426,7 +447,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
+        for (int s = 0; s < kAccs<PL>; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         fence_proxy_async();
@@ -445,25 +466,25 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 
     const int32_t n_live = MODE == kGrads ? *p.g.n_live : p.l.n_live ? *p.l.n_live : p.l.n_rows;
     Schedule sched = {};
-    sched.init<MODE>(p, n_live, k_logits);
+    sched.init<MODE, PL>(p, n_live, k_logits);
     Tile t;
     bool ok = true;
     // A logits stage holds the rows that exist: with few tokens most of it is classes, and more stages fit.  (The MMAs read
     // 128 token rows all the same; what lies behind the loaded ones belongs to later parts of the pipeline and only
     // reaches the accumulator rows of tokens that do not exist.)
     const uint32_t a_bytes = MODE == kGrads ? kSideBytes : (uint32_t)p.l.a_rows * 128;
-    const uint32_t b_bytes = MODE == kGrads ? kSideBytes : (uint32_t)p.l.bn * 64;
+    const uint32_t b_bytes = MODE == kGrads ? kBBytes : (uint32_t)p.l.bn * 64;
     const uint32_t stage_bytes = PL * (a_bytes + b_bytes);
     const uint32_t n_stages = MODE == kGrads ? kFewStages : (uint32_t)p.l.stages;
 
-    if (warp == 0 || warp == 10) {
-        // ---------------- TMA producers: warp 0 brings A, warp 10 brings B ----------------
+    if (warp == 0 || warp == 2) {
+        // ---------------- TMA producers: warp 0 brings A, warp 2 brings B ----------------
         const bool is_a = warp == 0;
         const uint32_t leader = elect_one();
         const uint32_t full0 = __shfl_sync(0xffffffffu, smem_u32(&ctl->full[0]), 0), bar0 = map_to_rank(full0, 0);
         const uint32_t sm0 = __shfl_sync(0xffffffffu, stage0, 0);
         Pipe px;
-        for (int32_t step = 0; ok && sched.get<MODE>(step, t); ++step) {
+        for (int32_t step = 0; ok && sched.get<MODE, PL>(step, t); ++step) {
             const int32_t r0 = is_a ? t.m0 + (int32_t)rank * 128 : t.n0 + (int32_t)rank * (t.bn / 2);
             const int job = __shfl_sync(0xffffffffu, t.job, 0);
             const CUtensorMap *map = is_a ? &maps.a[job] : &maps.b[job];
@@ -484,7 +505,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, 2 * kStage, leader);
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
-                        const uint32_t dst = (is_a ? sa : sb) + pl * kSideBytes;
+                        const uint32_t dst = is_a ? sa + pl * kSideBytes : sb + pl * kBBytes;
                         const int32_t krow = (job == 0 ? p.g.v0 : 0) + kb * 64;
                         if (is_a) {
                             if (job == 0) tma_load_pair(dst, map, 0, r0, kb, pl, bar, leader);
@@ -510,7 +531,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0);
             const uint32_t leader = elect_one();
             Pipe px, pd;
-            for (int32_t step = 0; ok && sched.get<MODE>(step, t); ++step) {
+            for (int32_t step = 0; ok && sched.get<MODE, PL>(step, t); ++step) {
                 if (PL == 1) {
                     ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
                     if (!ok) break;
@@ -527,7 +548,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                         ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t d_addr = tmem_u + pd.stage * kTile;
+                    const uint32_t d_addr = tmem_u + pd.stage * kCols<PL>;
                     const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
                     const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
 #pragma unroll
@@ -542,13 +563,13 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     px.advance(n_stages);
                     if (PL == 2) {
                         commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
-                        pd.advance(2);
+                        pd.advance(kAccs<PL>);
                     }
                 }
                 if (!ok) break;
                 if (PL == 1) {
                     commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
-                    pd.advance(2);
+                    pd.advance(kAccs<PL>);
                 }
             }
             if (!ok) {                                 // no MMA may still read shared or tensor memory when they go away
@@ -557,12 +578,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             }
         }
         __syncwarp();
-    } else {
+    } else if (warp >= 4) {
         // ---------------- epilogue: thread = row, half of the tile's columns in chunks of 32 ----------------
-        const int ew = warp - 2, qd = warp & 3, half = ew >> 2;
+        const int ew = warp - 4, qd = warp & 3, half = ew >> 2;
         const uint32_t t_lane = tmem_base + ((uint32_t)(qd * 32) << 16);
         const uint32_t exchange = stage0 + kStageBudget + (uint32_t)ew * kExchange;
-        const uint32_t line = exchange + (uint32_t)lane * 128;
         Pipe pd;
         float sc = 1.0f, inv_g = 1.0f;
         if (MODE != kGrads) {
@@ -572,50 +592,65 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             inv_g = p.g.scales->inv_g;
         }
         const bool bias_vec = BIAS && (reinterpret_cast<uintptr_t>(p.l.bias) & 15) == 0;
-        for (int32_t step = 0; sched.get<MODE>(step, t); ++step) {
+        // what a tile needs to know about this lane's row, asked for while the tile before it is worked on
+        auto row_info = [&](const Tile &u) {
+            RowInfo r = {0.0f, 0.0f, -1, 0};
+            const int32_t at = u.m0 + (int32_t)rank * 128 + qd * 32 + lane;
+            if (at >= n_live) return r;
+            if (MODE == kGrads) {
+                if (u.job == 0) r.row = p.g.rows[at].row;
+            } else if (p.l.rows) {
+                r = p.l.rows[at];
+            } else {
+                r.row = at;
+                if (!p.l.labels.flags && p.l.labels.live(at)) r.label = (int32_t)p.l.labels.target[at];
+            }
+            return r;
+        };
+        Tile next;
+        bool more = sched.get<MODE, PL>(0, next);
+        RowInfo next_info = {0.0f, 0.0f, -1, 0};
+        if (more) next_info = row_info(next);
+        for (int32_t step = 0; more; ++step) {
+            t = next;
+            const RowInfo info = next_info;
             const int32_t row0 = t.m0 + (int32_t)rank * 128 + qd * 32, row = row0 + lane;
             const int32_t hc = t.bn >> 1, col0 = t.n0 + half * hc;
             const bool live = row < n_live;
-            RowInfo info = {0.0f, 0.0f, -1, 0};
             Listed list;
-            if (MODE != kGrads) {
-                if (live) {
-                    if (p.l.rows) info = p.l.rows[row];
-                    else { info.row = row; if (!p.l.labels.flags && p.l.labels.live(row)) info.label = (int32_t)p.l.labels.target[row]; }
-                }
-                list.begin(p.l, info, live, p.l.v0 + col0);
-            } else if (t.job == 0 && live) {
-                info.row = p.g.rows[row].row;
-            }
+            if (MODE != kGrads) list.begin(p.l, info, live, p.l.v0 + col0);
+            more = sched.get<MODE, PL>(step + 1, next);
+            if (more) next_info = row_info(next);
             // the tile's sums: left in tensor memory, or (two planes) added up from its 64-element chains in registers
-            float acc[PL == 2 ? 128 : 1];
+            float acc[PL == 2 ? 64 : 1];
             uint32_t t_acc = 0;
             if (PL == 1) {
                 ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                 if (!ok) break;
                 tc_fence_after();
-                t_acc = t_lane + pd.stage * kTile + (uint32_t)(half * hc);
+                t_acc = t_lane + pd.stage * kCols<PL> + (uint32_t)(half * hc);
             } else {
 #pragma unroll
-                for (int j = 0; j < 128; ++j) acc[PL == 2 ? j : 0] = 0.0f;
+                for (int j = 0; j < 64; ++j) acc[PL == 2 ? j : 0] = 0.0f;
                 for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
                     ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint32_t t_sum = t_lane + pd.stage * kCols<PL> + (uint32_t)(half * hc);
+                    uint32_t r[2][32];
+                    tmem_ld_32x32(t_sum, r[0]);
+                    if (hc > 32) tmem_ld_32x32(t_sum + 32, r[1]);
+                    tc_wait_ld();
 #pragma unroll
-                    for (int ch = 0; ch < 8; ++ch) {
-                        if (ch * 16 < hc) {
-                            uint32_t r[16];
-                            tmem_ld_32x16(t_lane + pd.stage * kTile + (uint32_t)(half * hc + ch * 16), r);
-                            tc_wait_ld();
+                    for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] += __uint_as_float(r[0][j]);
+                    if (hc > 32) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) acc[PL == 2 ? ch * 16 + j : 0] += __uint_as_float(r[j]);
-                        }
+                        for (int j = 0; j < 32; ++j) acc[PL == 2 ? 32 + j : 0] += __uint_as_float(r[1][j]);
                     }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
-                    pd.advance(2);
+                    pd.advance(kAccs<PL>);
                 }
                 if (!ok) break;
             }
@@ -626,30 +661,36 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     tc_wait_ld();
 #pragma unroll
                     for (int j = 0; j < 32; ++j) out[j] = __uint_as_float(r[j]);
-                } else {
+                } else {                               // chosen by a uniform branch, so that what follows exists once
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) out[j] = acc[PL == 2 ? ch * 32 + j : 0];
+                    for (int k = 0; k < 2; ++k) {
+                        if (ch == k) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) out[j] = acc[PL == 2 ? k * 32 + j : 0];
+                        }
+                    }
                 }
             };
 
             if (MODE == kStats) {
                 float m = -INFINITY, l = 0.0f, dot = 0.0f;
-#pragma unroll (PL == 2 ? 4 : 1)
+#pragma unroll 1
                 for (int ch = 0; ch < 4; ++ch) {
                     if (ch * 32 >= hc) continue;
-                    const int32_t c0 = col0 + ch * 32;
+                    const int32_t c0 = col0 + ch * 32, end = min(c0 + 32, min(col0 + hc, p.l.width));
                     float b[32], v[32];
                     if (BIAS) load_bias(p.l, c0, bias_vec, b);
                     load_chunk(ch, v);
                     if (BIAS) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]);
-                    } else if (c0 + 32 > p.l.width) {
+                    }
+                    if (c0 + 32 > end) {               // behind the last class, or the other warps' columns
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
+                        for (int j = 0; j < 32; ++j) if (c0 + j >= end) v[j] = -INFINITY;
                     }
                     const float vs = BIAS ? 1.0f : sc;
-                    while (list.next < p.l.v0 + c0 + 32) {
+                    while (list.next < p.l.v0 + end) {
                         const int rel = list.next - (p.l.v0 + c0);
                         float z = 0.0f;
 #pragma unroll
@@ -680,7 +721,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const bool all_live = __all_sync(0xffffffffu, live);
                 const int32_t panels = p.l.ldz / 64;
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
-#pragma unroll (PL == 2 ? 4 : 1)
+#pragma unroll 1
                 for (int ch = 0; ch < 4; ++ch) {
                     if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32;
@@ -735,8 +776,9 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     }
                 }
             } else {
-                // The 32 x 32 values go through the warp's exchange lines so that the stores cover whole rows: a lane's own
-                // row at a time is 32 lines per store instruction, and the load / store unit takes one line per cycle.
+                // A lane stores its own row in whole 32-byte sectors: 32 lines per instruction, so the load / store unit, one
+                // line per cycle, needs 2 K cycles for a bf16 tile.  (16-byte stores took 10 K; passing the values through
+                // shared memory for stores along the rows 5 K, most of it latency.)
                 const GradParams &g = p.g;
                 const bool empty = t.kb0 >= t.kb1;     // nothing was contracted: the accumulator holds no result
                 const bool is_dx = t.job == 0;
@@ -752,25 +794,18 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 o.prev = !(is_dx && g.dx_add) ? nullptr : slot ? slot : static_cast<const float *>(g.dx);
                 o.prev_row = slot ? lane : info.row;
                 o.rows_in = rows_in; o.d = g.d;
-                const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16), vec = g.d % 8 == 0;
-#pragma unroll (PL == 2 ? 4 : 1)
+                const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16);
+                const bool sectors = g.d % 16 == 0 && (reinterpret_cast<uintptr_t>(o.out) & 31) == 0 && (reinterpret_cast<uintptr_t>(o.prev) & 31) == 0;
+#pragma unroll 1
                 for (int ch = 0; ch < 4; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
                     if (ch * 32 >= hc || c0 >= g.d) continue;
                     float v[32];
                     load_chunk(ch, v);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float e[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) e[j] = empty ? 0.0f : v[4 * q + j] * scale;
-                        sts_v4(line + (uint32_t)((q ^ (lane & 7)) << 4), __float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]),
-                               __float_as_uint(e[3]));
-                    }
-                    __syncwarp();
-                    if (!vec) write_rows<2>(o, exchange, lane, c0, out_bf16);
-                    else if (out_bf16) write_rows<1>(o, exchange, lane, c0, true);
-                    else write_rows<0>(o, exchange, lane, c0, false);
+                    for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : v[j] * scale;
+                    if (sectors) write_sectors(o, lane, c0, out_bf16, v);
+                    else write_elements(o, exchange, lane, c0, out_bf16, v);
                     __syncwarp();
                 }
             }
@@ -779,7 +814,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
-                pd.advance(2);
+                pd.advance(kAccs<PL>);
             }
         }
     }
@@ -858,7 +893,7 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
     l.scales = a.scales;
     l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width;
-    l.list_idx = a.list_idx; l.list_p = a.list_p; l.K = a.K;
+    l.list_idx = a.list_idx; l.list_p = a.list_p; l.list_start = a.list_start; l.K = a.K; l.bucket = a.bucket;
     l.part_max = a.part_max; l.part_sum = a.part_sum; l.part_dot = a.part_dot;
     l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
     p.status = a.status;
@@ -895,7 +930,7 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
     const int64_t dz_panels = a.ldz / 64, dz_panel = a.Tpad * 128;
     const bool w_panels = a.w.ld % 64 == 0;
     auto by_panels = [&a](CUtensorMap *m, const Operand &o) {
-        return make_panel_map(m, o.data, o.rows, (int64_t)o.ld * 2, o.ld / 64, 128, a.planes, o.plane_rows * o.ld * 2, 64, 2, CU_TENSOR_MAP_SWIZZLE_128B);
+        return make_panel_map(m, o.data, o.rows, (int64_t)o.ld * 2, o.ld / 64, 128, a.planes, o.plane_rows * o.ld * 2, 64, a.planes == 1 ? 2 : 1, CU_TENSOR_MAP_SWIZZLE_128B);
     };
     if (!make_panel_map(&maps.a[0], a.dz, a.Tpad, 128, dz_panels, dz_panel, a.planes, dz_panels * dz_panel, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
         !make_panel_map(&maps.a[1], a.dz, a.Tpad, 128, dz_panels, dz_panel, a.planes, dz_panels * dz_panel, 64, 2, CU_TENSOR_MAP_SWIZZLE_NONE) ||
@@ -909,7 +944,7 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
     g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
     g.dw = a.dw; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;
     p.status = a.status;
-    const int64_t nt = (a.d + kTile - 1) / kTile;
+    const int64_t cols = a.planes == 1 ? kCols<1> : kCols<2>, nt = (a.d + cols - 1) / cols;
     const int64_t tiles = (a.want_dx ? (a.T + kTile - 1) / kTile * nt * a.dx_splits : 0) +
                           (a.want_dw ? (a.width + kTile - 1) / kTile * nt * a.dw_splits : 0);
     if (tiles > INT_MAX) return TBN_ERR_UNSUPPORTED;
