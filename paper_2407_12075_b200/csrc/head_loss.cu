@@ -46,7 +46,7 @@ __device__ __forceinline__ float warp_max(float v) {
 template <typename TL>
 __global__ void __launch_bounds__(32 * kTeacherWarps)
 teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, int64_t T, int32_t K, int32_t Kp, int32_t V,
-               float inv_tau, int32_t bucket, int32_t *__restrict__ list_idx, float *__restrict__ list_p, uint16_t *__restrict__ list_start,
+               float inv_tau, int32_t bucket, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
                uint8_t *__restrict__ flags, float2 *__restrict__ stats)
 {
     extern __shared__ uint8_t teacher_smem[];
@@ -59,13 +59,11 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     if (t >= T) return;
     float top = -INFINITY;
     bool any = false, nan = false;
+#pragma unroll 4
     for (int32_t j = lane; j < Kp; j += 32) {
-        int64_t c = -1;
-        float l = -INFINITY;
-        if (j < K) {
-            c = index[t * K + j];
-            if (c >= 0 && c < V) l = load_as_float(logit, t * K + j) * inv_tau;
-        }
+        const int64_t c = j < K ? index[t * K + j] : -1;
+        float l = j < K ? load_as_float(logit, t * K + j) * inv_tau : 0.0f;
+        if (c < 0 || c >= V) l = -INFINITY;
         const bool valid = !(l == -INFINITY);
         any |= valid;
         nan |= valid && !(l == l);
@@ -109,8 +107,7 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     }
     for (int32_t j = lane; j < K; j += 32) {
         const uint64_t k = key[j];
-        list_idx[t * K + j] = (int32_t)(k >> 32);
-        list_p[t * K + j] = prob[(uint32_t)k];
+        list[t * K + j] = make_int2((int32_t)(k >> 32), __float_as_int(prob[(uint32_t)k]));
     }
     for (int32_t b = lane; b <= kBuckets; b += 32) {   // where each bucket of classes begins
         const uint64_t first = (uint64_t)b * (uint64_t)bucket << 32;
@@ -274,6 +271,7 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     if (sizeof(TS) == 4 && blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{sx, sw, sg, 1.0f / sx, 1.0f / sw, 1.0f / sg};
     const int64_t r0 = (int64_t)blockIdx.x * a.per_block, r1 = min(a.T, r0 + a.per_block);       // r0 < T for every row block
     int mine = 0;
+#pragma unroll 8
     for (int64_t t = threadIdx.x; t < r0; t += 256) mine += a.labels.live(t) ? 1 : 0;
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0) warp_count[warp] = mine;
@@ -334,60 +332,63 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
 }
 
 // ---- forward: join the pieces of a row ------------------------------------------------------------------------
-// RB rows x (256 / RB) threads: every thread merges every (256 / RB)-th triple, then the threads of a row are merged
-// pairwise, in a fixed order.
-template <int RB>
+// One warp per token, or a whole block where there are few: every lane merges every 32nd (256th) part, then the lanes (and
+// the warps) are merged pairwise, in a fixed order.
+struct Joined { float m, s, dot; };
+__device__ __forceinline__ void merge(Joined &a, float m, float s, float dot) {
+    const float top = fmaxf(a.m, m), ref = top == -INFINITY ? 0.0f : top;
+    a.s = a.s * exp2f(a.m - ref) + s * exp2f(m - ref);
+    a.m = top;
+    a.dot += dot;
+}
+template <int ROWS>
 __global__ void __launch_bounds__(256)
-combine_kernel(const float *__restrict__ part_max, const float *__restrict__ part_sum, const float *__restrict__ part_dot, int32_t parts,
-               int64_t Tpad, const int32_t *__restrict__ n_live, const RowInfo *__restrict__ rows, Labels labels, int32_t n_rows,
-               const float2 *__restrict__ teacher, float tau, float *__restrict__ loss, float *__restrict__ lse)
+combine_kernel(const float4 *__restrict__ part, int32_t parts, const int32_t *__restrict__ n_live, const RowInfo *__restrict__ rows,
+               Labels labels, int32_t n_rows, const float2 *__restrict__ teacher, float tau, float *__restrict__ loss, float *__restrict__ lse)
 {
-    constexpr int kParts = 256 / RB;
-    __shared__ float sm[256], ss[256], sd[256];
-    const int r = threadIdx.x % RB, g = threadIdx.x / RB;
+    static_assert(ROWS == 1 || ROWS == 8, "a block or a warp per token");
+    constexpr int kLanes = 256 / ROWS;
+    __shared__ Joined warps[8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = threadIdx.x % kLanes;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t row = (int64_t)blockIdx.x * RB + r;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS == 8 ? warp : 0);
     bool live = row < (n_live ? *n_live : n_rows);
     if (live && !rows && !labels.live(row)) {          // rows in their own order: the ones left out are still among them
         live = false;
-        if (g == 0) { loss[row] = 0.0f; lse[row] = 0.0f; }
+        if (sub == 0) { loss[row] = 0.0f; lse[row] = 0.0f; }
     }
-    float m = -INFINITY, s = 0.0f, dot = 0.0f;
+    Joined j = {-INFINITY, 0.0f, 0.0f};
     if (live) {
-#pragma unroll 4
-        for (int32_t i = g; i < parts; i += kParts) {
-            const int64_t at = (int64_t)i * Tpad + row;
-            const float pm = part_max[at], ps = part_sum[at];
-            dot += part_dot[at];
-            const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.0f : mn;
-            s = s * exp2f(m - ref) + ps * exp2f(pm - ref);
-            m = mn;
+        const float4 *p = part + row * parts;
+        int32_t i = sub;
+        for (; i + 3 * kLanes < parts; i += 4 * kLanes) {
+            const float4 a = p[i], b = p[i + kLanes], c = p[i + 2 * kLanes], d = p[i + 3 * kLanes];
+            merge(j, a.x, a.y, a.z); merge(j, b.x, b.y, b.z); merge(j, c.x, c.y, c.z); merge(j, d.x, d.y, d.z);
         }
+        for (; i < parts; i += kLanes) { const float4 a = p[i]; merge(j, a.x, a.y, a.z); }
     }
-    sm[threadIdx.x] = m; ss[threadIdx.x] = s; sd[threadIdx.x] = dot;
 #pragma unroll
-    for (int h = kParts / 2; h > 0; h >>= 1) {
+    for (int o = 16; o > 0; o >>= 1) {
+        const float m = __shfl_down_sync(0xffffffffu, j.m, o), s = __shfl_down_sync(0xffffffffu, j.s, o), d = __shfl_down_sync(0xffffffffu, j.dot, o);
+        merge(j, m, s, d);
+    }
+    if (ROWS == 1) {
+        if (lane == 0) warps[warp] = j;
         __syncthreads();
-        if (g < h) {
-            const int other = threadIdx.x + h * RB;
-            const float pm = sm[other], ps = ss[other];
-            dot += sd[other];
-            const float mn = fmaxf(m, pm), ref = mn == -INFINITY ? 0.0f : mn;
-            s = s * exp2f(m - ref) + ps * exp2f(pm - ref);
-            m = mn;
-            sm[threadIdx.x] = m; ss[threadIdx.x] = s; sd[threadIdx.x] = dot;
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < 8; ++w) merge(j, warps[w].m, warps[w].s, warps[w].dot);
         }
     }
-    if (g == 0 && live) {
-        const float lse2 = m + log2f(s);               // all classes at -infinity: -infinity + log2(0)
+    if (sub == 0 && live) {
+        const float lse2 = j.m + log2f(j.s);           // all classes at -infinity: -infinity + log2(0)
         const int64_t t = rows ? (int64_t)rows[row].row : row;
         lse[t] = lse2 * kLn2;
         if (teacher) {
             const float2 e = teacher[t];               // sum p log p, sum p
-            loss[t] = tau * tau * fmaf(kLn2, fmaf(lse2, e.y, -dot), e.x);
+            loss[t] = tau * tau * fmaf(kLn2, fmaf(lse2, e.y, -j.dot), e.x);
         } else {
-            loss[t] = (lse2 - dot) * kLn2;
+            loss[t] = (lse2 - j.dot) * kLn2;
         }
     }
 }
@@ -479,7 +480,7 @@ struct Plan {
     bool direct;
     int64_t Tpad;
     bool dx_slots, dw_slots;
-    size_t o_live, o_scales, o_max, o_rows, o_x, o_w, o_idx, o_p, o_start, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
+    size_t o_live, o_scales, o_max, o_rows, o_x, o_w, o_list, o_start, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
 };
 
 // Classes per tile of a logits launch: the width whose whole rounds over the SM pairs cost least.  A round costs what it
@@ -535,15 +536,14 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     p.o_rows = take(p.direct ? 0 : (size_t)p.Tpad * sizeof(RowInfo));
     p.o_x = take(p.direct ? 0 : (size_t)p.planes * p.Tpad * p.ld * 2);
     p.o_w = take(p.pack_w ? (size_t)p.planes * V * p.ld * 2 : 0);
-    p.o_idx = take((size_t)T * K * 4);
-    p.o_p = take((size_t)T * K * 4);
+    p.o_list = take((size_t)T * K * 8);
     p.o_start = take(K > 0 ? (size_t)T * (kBuckets + 1) * 2 : 0);
     p.o_flags = take(K > 0 ? (size_t)T : 0);
     p.o_teacher = take(K > 0 ? (size_t)T * 8 : 0);
     if (!backward) {
         p.bn = classes_per_tile(T, V, p.cols, 64, 32);
         p.parts = (int32_t)((V + p.bn - 1) / p.bn * 2);
-        p.o_part = take((size_t)3 * p.parts * p.Tpad * 4);
+        p.o_part = take((size_t)p.parts * p.Tpad * sizeof(float4));
     } else {
         int64_t width = (int64_t)(kPieceBytes / ((size_t)2 * p.planes * p.Tpad)) / kTile * kTile;
         if (width < 1024) width = 1024;
@@ -601,22 +601,20 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         while (Kp < c.K) Kp <<= 1;
         const size_t smem = (size_t)kTeacherWarps * Kp * 12;
         const dim3 grid((unsigned)((c.T + kTeacherWarps - 1) / kTeacherWarps));
-        int32_t *idx = reinterpret_cast<int32_t *>(ws + p.o_idx);
-        float *prob = reinterpret_cast<float *>(ws + p.o_p);
+        int2 *list = reinterpret_cast<int2 *>(ws + p.o_list);
         uint8_t *flags = reinterpret_cast<uint8_t *>(ws + p.o_flags);
         float2 *stats = reinterpret_cast<float2 *>(ws + p.o_teacher);
         uint16_t *start = reinterpret_cast<uint16_t *>(ws + p.o_start);
         const int32_t bucket = (int32_t)(((int64_t)c.V + kBuckets - 1) / kBuckets);
         const cudaError_t e = c.top_dtype == TBN_F32
             ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
-                         c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, idx, prob, start, flags, stats)
+                         c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, list, start, flags, stats)
             : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index,
-                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, idx, prob, start, flags, stats);
+                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, list, start, flags, stats);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
-        out->list_idx = idx;
-        out->list_p = prob;
+        out->list = list;
         out->list_start = start;
         out->K = c.K;
         out->bucket = bucket;
@@ -674,18 +672,17 @@ int forward(const HeadCall &c, void *workspace, cudaStream_t s)
     int rc = prepare(c, p, ws, false, &a, s);
     if (rc != TBN_OK) return rc;
     a.v0 = 0; a.width = c.V;
-    a.part_max = reinterpret_cast<float *>(ws + p.o_part);
-    a.part_sum = a.part_max + (size_t)p.parts * p.Tpad;
-    a.part_dot = a.part_sum + (size_t)p.parts * p.Tpad;
+    a.part = reinterpret_cast<float4 *>(ws + p.o_part);
+    a.parts = p.parts;
     rc = launch_head_stats(a, s);
     if (rc != TBN_OK) return rc;
     const float2 *teacher = c.K > 0 ? reinterpret_cast<const float2 *>(ws + p.o_teacher) : nullptr;
     // enough blocks for the GPU: one row per block when there are few tokens
-    const int rb = c.T >= 4096 ? 32 : c.T >= 256 ? 8 : 1;
+    const int rb = c.T >= 256 ? 8 : 1;
     const dim3 grid((unsigned)((c.T + rb - 1) / rb));
-    auto kern = rb == 32 ? combine_kernel<32> : rb == 8 ? combine_kernel<8> : combine_kernel<1>;
-    return launch_pdl(kern, grid, dim3(256), 0, s, a.part_max, a.part_sum, a.part_dot, p.parts, p.Tpad, a.n_live, a.rows, a.labels, (int32_t)c.T, teacher, c.tau,
-                      c.loss_out, c.lse_out) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
+    auto kern = rb == 8 ? combine_kernel<8> : combine_kernel<1>;
+    return launch_pdl(kern, grid, dim3(256), 0, s, static_cast<const float4 *>(a.part), p.parts, a.n_live, a.rows, a.labels, (int32_t)c.T, teacher,
+                      c.tau, c.loss_out, c.lse_out) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 
 int backward(const HeadCall &c, void *workspace, cudaStream_t s)

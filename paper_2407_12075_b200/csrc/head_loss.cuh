@@ -58,12 +58,12 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     float scale2;                          // log2(e) / tau
     int64_t T, Tpad;
     int32_t V, v0, width;
-    const int32_t *list_idx;               // distillation: [T][K] ascending, INT32_MAX behind the last entry; else null
-    const float *list_p;
+    const int2 *list;                      // distillation: [T][K] (class, probability), ascending, INT32_MAX behind the last; else null
     const uint16_t *list_start;            // [T][kBuckets + 1]
     int32_t K, bucket;                     // classes per bucket
-    // forward: a (maximum, sum, dot) triple for every bn / 2 classes and token: [triple][Tpad]
-    float *part_max, *part_sum, *part_dot;
+    // forward: (maximum, sum, dot, unused) of every token and bn / 2 classes: [Tpad][parts]
+    float4 *part;
+    int32_t parts;
     // backward
     void *dz;                              // [planes][ldz / 64][Tpad][64], see tc_head.cu
     int32_t ldz;

@@ -59,6 +59,8 @@ enum { kStats = 0, kDz = 1, kGrads = 2 };
 // columns of a tile at most, and accumulators in the 512 columns of tensor memory
 template <int PL> constexpr int kCols = PL == 1 ? 256 : 128;
 template <int PL> constexpr int kAccs = 512 / kCols<PL>;
+// behind the stages: exchange lines, or the biases of every epilogue warp's columns
+template <int MODE> constexpr uint32_t kScratch = kEpiWarps * (MODE == kGrads ? kExchange : 128 * sizeof(float));
 
 struct Control {
     uint64_t full[kMaxStages], empty[kMaxStages], d_full[4], d_empty[4];
@@ -81,11 +83,11 @@ struct LogitsParams {
     float scale2;
     int64_t Tpad;
     int32_t V, v0, width;
-    const int32_t *list_idx;
-    const float *list_p;
+    const int2 *list;                      // distillation: [T][K] (class, probability) pairs, ascending; else null
     const uint16_t *list_start;            // [T][kBuckets + 1]: where the classes of each bucket begin in the row's list
     int32_t K, bucket;
-    float *part_max, *part_sum, *part_dot;
+    float4 *part;
+    int32_t parts;
     void *dz;
     int32_t ldz;
     float *col_part;
@@ -260,20 +262,26 @@ struct Schedule {
     int32_t bn_logits, d_cols;
 };
 
-// The sparse side of a row: the target class with probability 1, or the teacher's ascending list.
+// The sparse side of a row: the target class with probability 1, or the teacher's ascending list of (class, probability)
+// pairs, of which the next four are kept in registers: a pair is asked for four entries before its turn, so that the entries
+// of one chunk do not each cost a trip to memory.
 struct Listed {
-    const int32_t *idx;
-    const float *p;
-    int32_t pos, count, next;
+    const int2 *entry;                     // the row's list
+    int32_t pos, count, next;              // next: the class of the entry at pos, INT_MAX behind the last one
+    float weight;
+    int2 w1, w2, w3;
 
+    __device__ __forceinline__ int2 at(int32_t i) const { return i < count ? __ldg(entry + i) : make_int2(INT_MAX, 0); }
     __device__ __forceinline__ void begin(const LogitsParams &l, const RowInfo &r, bool live, int32_t first) {
-        if (l.list_idx == nullptr) {
-            idx = nullptr;
+        w1 = w2 = w3 = make_int2(INT_MAX, 0);
+        pos = count = 0;
+        if (l.list == nullptr) {
+            entry = nullptr;
             next = live && r.label >= first ? r.label : INT_MAX;
+            weight = 1.0f;
             return;
         }
-        idx = l.list_idx + (int64_t)r.row * l.K;
-        p = l.list_p + (int64_t)r.row * l.K;
+        entry = l.list + (int64_t)r.row * l.K;
         count = live ? l.K : 0;
         if (count) {                                   // first entry >= first: between the starts of its bucket and the next
             const int32_t bucket = first / l.bucket;
@@ -281,19 +289,21 @@ struct Listed {
             int32_t lo = __ldg(start), hi = bucket < kBuckets ? (int32_t)__ldg(start + 1) : count;
             while (lo < hi) {
                 const int32_t mid = (lo + hi) >> 1;
-                if (__ldg(idx + mid) < first) lo = mid + 1; else hi = mid;
+                if (__ldg(&entry[mid].x) < first) lo = mid + 1; else hi = mid;
             }
             pos = lo;
-        } else {
-            pos = 0;
         }
-        next = pos < count ? __ldg(idx + pos) : INT_MAX;
+        const int2 e = at(pos);
+        w1 = at(pos + 1); w2 = at(pos + 2); w3 = at(pos + 3);
+        next = e.x;
+        weight = __int_as_float(e.y);
     }
-    __device__ __forceinline__ float weight() const { return idx ? __ldg(p + pos) : 1.0f; }
     __device__ __forceinline__ void step() {
-        if (!idx) { next = INT_MAX; return; }
+        next = w1.x;
+        weight = __int_as_float(w1.y);
+        w1 = w2; w2 = w3;
         ++pos;
-        next = pos < count ? __ldg(idx + pos) : INT_MAX;
+        w3 = at(pos + 3);
     }
 };
 
@@ -309,21 +319,6 @@ __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
         }
     }
     return v[0];
-}
-
-// 32 columns of a row's bias times log2(e) / tau, -infinity behind the last class
-__device__ __forceinline__ void load_bias(const LogitsParams &l, int32_t c0, bool vec, float (&b)[32]) {
-    const float *src = l.bias + l.v0 + c0;
-    if (vec && c0 + 32 <= l.width) {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const float4 u = __ldg(reinterpret_cast<const float4 *>(src) + q);
-            b[4 * q] = u.x * l.scale2; b[4 * q + 1] = u.y * l.scale2; b[4 * q + 2] = u.z * l.scale2; b[4 * q + 3] = u.w * l.scale2;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) b[j] = c0 + j < l.width ? __ldg(src + j) * l.scale2 : -INFINITY;
-    }
 }
 
 // A lane's 32 values as the pieces [4 * upper, 4 * upper + 4) of its line of a dz panel: two whole 32-byte sectors, whose
@@ -437,8 +432,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
     const uint32_t stage0 = raw + pad;
-    constexpr uint32_t kExchangeBytes = MODE == kGrads ? kEpiWarps * kExchange : 0u;
-    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget + kExchangeBytes);
+    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget + kScratch<MODE>);
     volatile int *abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -591,7 +585,6 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
         } else if (p.g.scales) {
             inv_g = p.g.scales->inv_g;
         }
-        const bool bias_vec = BIAS && (reinterpret_cast<uintptr_t>(p.l.bias) & 15) == 0;
         // what a tile needs to know about this lane's row, asked for while the tile before it is worked on
         auto row_info = [&](const Tile &u) {
             RowInfo r = {0.0f, 0.0f, -1, 0};
@@ -619,6 +612,15 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             const bool live = row < n_live;
             Listed list;
             if (MODE != kGrads) list.begin(p.l, info, live, p.l.v0 + col0);
+            float *bias_s = reinterpret_cast<float *>(smem_raw + pad + kStageBudget) + ew * 128;
+            if (BIAS) {                                // times log2(e) / tau; -infinity behind the last class
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int32_t c = col0 + j * 32 + lane;
+                    if (j * 32 < hc) bias_s[j * 32 + lane] = c < p.l.width ? __ldg(p.l.bias + p.l.v0 + c) * p.l.scale2 : -INFINITY;
+                }
+                __syncwarp();
+            }
             more = sched.get<MODE, PL>(step + 1, next);
             if (more) next_info = row_info(next);
             // the tile's sums: left in tensor memory, or (two planes) added up from its 64-element chains in registers
@@ -654,13 +656,15 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 }
                 if (!ok) break;
             }
-            auto load_chunk = [&](int ch, float (&out)[32]) {      // 32 columns of the tile
-                if (PL == 1) {
-                    uint32_t r[32];
-                    tmem_ld_32x32(t_acc + ch * 32, r);
+            // 32 columns of the tile.  One plane: the next 32 are asked for before these are worked on.
+            uint32_t ahead[PL == 1 ? 32 : 1];
+            if constexpr (PL == 1) tmem_ld_32x32(t_acc, ahead);
+            auto load_chunk = [&](int ch, float (&out)[32]) {
+                if constexpr (PL == 1) {
                     tc_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) out[j] = __uint_as_float(r[j]);
+                    for (int j = 0; j < 32; ++j) out[j] = __uint_as_float(ahead[j]);
+                    if ((ch + 1) * 32 < hc) tmem_ld_32x32(t_acc + (ch + 1) * 32, ahead);
                 } else {                               // chosen by a uniform branch, so that what follows exists once
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
@@ -678,12 +682,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 for (int ch = 0; ch < 4; ++ch) {
                     if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32, end = min(c0 + 32, min(col0 + hc, p.l.width));
-                    float b[32], v[32];
-                    if (BIAS) load_bias(p.l, c0, bias_vec, b);
+                    float v[32];
                     load_chunk(ch, v);
                     if (BIAS) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]);
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]);
                     }
                     if (c0 + 32 > end) {               // behind the last class, or the other warps' columns
 #pragma unroll
@@ -695,8 +698,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                         float z = 0.0f;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z = rel == j ? v[j] : z;
-                        const float w = list.weight();
-                        if (w != 0.0f) dot = fmaf(w, z * vs, dot);     // 0 times a class at -infinity is 0
+                        if (list.weight != 0.0f) dot = fmaf(list.weight, z * vs, dot);     // 0 times a class at -infinity is 0
                         list.step();
                     }
                     __syncwarp();
@@ -712,10 +714,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     m = m_new;
                 }
                 if (live) {
-                    const int64_t at = (int64_t)((p.l.v0 + col0) / hc) * p.l.Tpad + row;
-                    p.l.part_max[at] = m;
-                    p.l.part_sum[at] = l;
-                    p.l.part_dot[at] = dot;
+                    p.l.part[(int64_t)row * p.l.parts + (p.l.v0 + col0) / hc] = make_float4(m, l, dot, 0.0f);
                 }
             } else if (MODE == kDz) {
                 const bool all_live = __all_sync(0xffffffffu, live);
@@ -725,12 +724,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 for (int ch = 0; ch < 4; ++ch) {
                     if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32;
-                    float b[32], v[32];
-                    if (BIAS) load_bias(p.l, c0, bias_vec, b);
+                    float v[32];
                     load_chunk(ch, v);
                     if (BIAS) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, b[j]) - info.lse2;
+                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]) - info.lse2;
                     } else {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
@@ -743,7 +741,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
                     while (list.next < p.l.v0 + c0 + 32) {
                         const int rel = list.next - (p.l.v0 + c0);
-                        const float sub = info.g * list.weight();
+                        const float sub = info.g * list.weight;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
                         list.step();
@@ -811,6 +809,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             }
             __syncwarp();
             if (PL == 1) {
+                tc_wait_ld();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
@@ -862,7 +861,7 @@ int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_log
     const int pairs = sm_count() / 2;
     if (pairs <= 0) return TBN_ERR_CUDA;
     if (tiles <= 0) return TBN_OK;
-    constexpr size_t smem = kStageBudget + (MODE == kGrads ? kEpiWarps * kExchange : 0) + sizeof(Control) + 1024;
+    constexpr size_t smem = kStageBudget + kScratch<MODE> + sizeof(Control) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory");
     auto kern = head_kernel<MODE, PL, BIAS>;
     int dev = 0;
@@ -893,8 +892,8 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
     l.scales = a.scales;
     l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width;
-    l.list_idx = a.list_idx; l.list_p = a.list_p; l.list_start = a.list_start; l.K = a.K; l.bucket = a.bucket;
-    l.part_max = a.part_max; l.part_sum = a.part_sum; l.part_dot = a.part_dot;
+    l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.bucket = a.bucket;
+    l.part = a.part; l.parts = a.parts;
     l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
     p.status = a.status;
     const int64_t tiles = (a.T + kTile - 1) / kTile * ((a.width + a.bn - 1) / a.bn);
