@@ -155,7 +155,7 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *     p[t][j] = softmax_j(top_logit[t][j] / tau),   q[t][v] = softmax_v(z[t][v] / tau),   lse[t] = log sum_v exp(z[t][v] / tau)
  *     loss[t] = tau^2 * sum_j p[t][j] * (log p[t][j] - log q[t][top_index[t][j]])
  *   Entries whose index is negative or >= vocab, and entries whose logit is -infinity, are left out of p; a token with no
- *   entry left is left out as above.  A class listed twice counts with both its probabilities.  1 <= K <= 1024, 0 < tau.
+ *   entry left is left out as above.  A class listed twice counts with both its probabilities.  1 <= K <= 1024, 1e-30 <= tau <= 1e30.
  * Classes with a bias of -infinity (a masked vocabulary) have probability 0 and gradient 0.  A token whose kept logits
  * hold a NaN or +infinity, or all of whose classes are masked, has a NaN or infinite loss; no other token is affected
  * (in the backward its dloss of 0 does not help: 0 times NaN is NaN, in its row of dx and in dw).

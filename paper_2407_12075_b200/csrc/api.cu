@@ -138,7 +138,7 @@ bool head_sizes_ok(int64_t T, int32_t in_f, int32_t vocab)
 int head_call(head::HeadCall &c, bool backward, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (c.T < 0 || c.d <= 0 || c.V <= 0 || !valid_dtype(c.dtype)) return TBN_ERR_INVALID_ARG;
-    if (c.K > 0 && (!valid_dtype(c.top_dtype) || !(c.tau > 0.0f) || !(c.tau < 3.0e38f) || !(1.0f / c.tau < 3.0e38f))) return TBN_ERR_INVALID_ARG;
+    if (c.K > 0 && (!valid_dtype(c.top_dtype) || !(c.tau >= 1e-30f) || !(c.tau <= 1e30f))) return TBN_ERR_INVALID_ARG;
     if (backward && c.dw && !valid_dtype(c.dw_dtype)) return TBN_ERR_INVALID_ARG;
     if (!head_sizes_ok(c.T, c.d, c.V) || c.K > head::kMaxListed) return TBN_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -62,7 +62,7 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
 #pragma unroll 4
     for (int32_t j = lane; j < Kp; j += 32) {
         const int64_t c = j < K ? index[t * K + j] : -1;
-        float l = j < K ? load_as_float(logit, t * K + j) * inv_tau : 0.0f;
+        float l = j < K ? load_as_float(logit, t * K + j) : 0.0f;
         if (c < 0 || c >= V) l = -INFINITY;
         const bool valid = !(l == -INFINITY);
         any |= valid;
@@ -76,7 +76,7 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     nan = __any_sync(0xffffffffu, nan);
     if (nan) top = 0.0f;                               // the row's result is NaN whatever the reference point
     float sum = 0.0f;
-    for (int32_t j = lane; j < Kp; j += 32) sum += prob[j] == -INFINITY ? 0.0f : expf(prob[j] - top);
+    for (int32_t j = lane; j < Kp; j += 32) sum += prob[j] == -INFINITY ? 0.0f : expf((prob[j] - top) * inv_tau);
     sum = warp_sum(sum);
     const float inv = any ? 1.0f / sum : 0.0f, log_sum = any ? logf(sum) : 0.0f;
     float plogp = 0.0f, total = 0.0f;
@@ -84,8 +84,9 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
         const float l = prob[j];
         float q = 0.0f;
         if (l != -INFINITY) {
-            q = expf(l - top) * inv;
-            if (!(q == 0.0f)) plogp = fmaf(q, l - top - log_sum, plogp);
+            const float e = (l - top) * inv_tau;       // the difference first: the lowest finite logit stays finite
+            q = expf(e) * inv;
+            if (!(q == 0.0f)) plogp = fmaf(q, e - log_sum, plogp);
             total += q;
         }
         prob[j] = q;

@@ -307,6 +307,27 @@ struct Listed {
     }
 };
 
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// v = v * a + b, two at a time; bias: 32 floats in shared memory, 16-byte aligned, added to b where there are any
+template <bool BIAS>
+__device__ __forceinline__ void scale_shift(float (&v)[32], float a, float b, const float4 *bias) {
+    const uint64_t a2 = f32x2_pack(a, a), b2 = f32x2_pack(b, b);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint64_t s0 = b2, s1 = b2;
+        if (BIAS) {
+            const float4 u = bias[q];
+            s0 = f32x2_add(f32x2_pack(u.x, u.y), b2);
+            s1 = f32x2_add(f32x2_pack(u.z, u.w), b2);
+        }
+        f32x2_unpack(f32x2_fma(f32x2_pack(v[4 * q], v[4 * q + 1]), a2, s0), v[4 * q], v[4 * q + 1]);
+        f32x2_unpack(f32x2_fma(f32x2_pack(v[4 * q + 2], v[4 * q + 3]), a2, s1), v[4 * q + 2], v[4 * q + 3]);
+    }
+}
 // 32 x 32 values, lane = row: returns in lane c the sum over the rows of column c (v is overwritten).
 __device__ __forceinline__ float column_sums(float (&v)[32], int lane) {
 #pragma unroll
@@ -401,15 +422,28 @@ __device__ __forceinline__ void write_elements(const RowsOut &o, uint32_t exchan
                __float_as_uint(v[4 * q + 3]));
     __syncwarp();
     const int32_t c = c0 + lane;
-#pragma unroll 8
-    for (int r = 0; r < 32; ++r) {
-        const int32_t to = __shfl_sync(0xffffffffu, o.row, r), from = __shfl_sync(0xffffffffu, o.prev_row, r);
-        float x = __uint_as_float(lds_b32(exchange + (uint32_t)r * 128 + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
-        if (r >= o.rows_in || c >= o.d) continue;
-        if (o.prev) x += o.prev[(int64_t)from * o.d + c];
-        const int64_t at = (int64_t)to * o.d + c;
-        if (out_bf16) static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x);
-        else static_cast<float *>(o.out)[at] = x;
+#pragma unroll 1
+    for (int h = 0; h < 32; h += 8) {                  // eight rows in flight
+        float x[8];
+        int32_t to[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int r = h + k;
+            x[k] = __uint_as_float(lds_b32(exchange + (uint32_t)r * 128 + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+            to[k] = __shfl_sync(0xffffffffu, o.row, r);
+            if (o.prev) {
+                const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
+                if (r < o.rows_in && c < o.d) x[k] += o.prev[(int64_t)from * o.d + c];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (h + k < o.rows_in && c < o.d) {
+                const int64_t at = (int64_t)to[k] * o.d + c;
+                if (out_bf16) static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x[k]);
+                else static_cast<float *>(o.out)[at] = x[k];
+            }
+        }
     }
     __syncwarp();
 }
@@ -613,11 +647,12 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             Listed list;
             if (MODE != kGrads) list.begin(p.l, info, live, p.l.v0 + col0);
             float *bias_s = reinterpret_cast<float *>(smem_raw + pad + kStageBudget) + ew * 128;
-            if (BIAS) {                                // times log2(e) / tau; -infinity behind the last class
+            if (BIAS) {                                // times log2(e) / tau, finite ones kept finite; -infinity behind the last class
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int32_t c = col0 + j * 32 + lane;
-                    if (j * 32 < hc) bias_s[j * 32 + lane] = c < p.l.width ? __ldg(p.l.bias + p.l.v0 + c) * p.l.scale2 : -INFINITY;
+                    const float b = j * 32 < hc && c < p.l.width ? __ldg(p.l.bias + p.l.v0 + c) : -INFINITY;
+                    bias_s[j * 32 + lane] = b == -INFINITY ? b : fmaxf(b * p.l.scale2, -3.402823466e38f) + (b - b);
                 }
                 __syncwarp();
             }
@@ -684,10 +719,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     const int32_t c0 = col0 + ch * 32, end = min(c0 + 32, min(col0 + hc, p.l.width));
                     float v[32];
                     load_chunk(ch, v);
-                    if (BIAS) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]);
-                    }
+                    if (BIAS) scale_shift<true>(v, sc, 0.0f, reinterpret_cast<const float4 *>(bias_s + ch * 32));
                     if (c0 + 32 > end) {               // behind the last class, or the other warps' columns
 #pragma unroll
                         for (int j = 0; j < 32; ++j) if (c0 + j >= end) v[j] = -INFINITY;
@@ -707,10 +739,16 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     for (int j = 4; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], v[j]);
                     const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * vs);
                     const float ref = m_new == -INFINITY ? 0.0f : m_new;
-                    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    scale_shift<false>(v, vs, -ref, nullptr);
+                    uint64_t s0 = 0, s1 = 0;           // four running sums
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s4[j & 3] += exp2_approx(fmaf(v[j], vs, -ref));
-                    l = l * exp2_approx(m - ref) + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+                    for (int j = 0; j < 32; j += 4) {
+                        s0 = f32x2_add(s0, f32x2_pack(exp2_approx(v[j]), exp2_approx(v[j + 1])));
+                        s1 = f32x2_add(s1, f32x2_pack(exp2_approx(v[j + 2]), exp2_approx(v[j + 3])));
+                    }
+                    float e0, e1;
+                    f32x2_unpack(f32x2_add(s0, s1), e0, e1);
+                    l = l * exp2_approx(m - ref) + (e0 + e1);
                     m = m_new;
                 }
                 if (live) {
@@ -726,19 +764,15 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     const int32_t c0 = col0 + ch * 32;
                     float v[32];
                     load_chunk(ch, v);
-                    if (BIAS) {
+                    scale_shift<BIAS>(v, sc, -info.lse2, reinterpret_cast<const float4 *>(bias_s + ch * 32));
+                    if (!BIAS && c0 + 32 > p.l.width) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, bias_s[ch * 32 + j]) - info.lse2;
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = fmaf(v[j], sc, -info.lse2);
-                        if (c0 + 32 > p.l.width) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
-                        }
+                        for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
                     }
+                    const uint64_t g2 = f32x2_pack(info.g, info.g);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = info.g * exp2_approx(v[j]);
+                    for (int j = 0; j < 32; j += 2)
+                        f32x2_unpack(f32x2_mul(f32x2_pack(exp2_approx(v[j]), exp2_approx(v[j + 1])), g2), v[j], v[j + 1]);
                     while (list.next < p.l.v0 + c0 + 32) {
                         const int rel = list.next - (p.l.v0 + c0);
                         const float sub = info.g * list.weight;
