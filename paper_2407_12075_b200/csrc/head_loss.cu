@@ -46,7 +46,7 @@ __device__ __forceinline__ float warp_max(float v) {
 template <typename TL>
 __global__ void __launch_bounds__(32 * kTeacherWarps)
 teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, int64_t T, int32_t K, int32_t Kp, int32_t V,
-               float inv_tau, int32_t bucket, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
+               float inv_tau, int32_t unit, int32_t units, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
                uint8_t *__restrict__ flags, float2 *__restrict__ stats)
 {
     extern __shared__ uint8_t teacher_smem[];
@@ -110,14 +110,12 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
         const uint64_t k = key[j];
         list[t * K + j] = make_int2((int32_t)(k >> 32), __float_as_int(prob[(uint32_t)k]));
     }
-    for (int32_t b = lane; b <= kBuckets; b += 32) {   // where each bucket of classes begins
-        const uint64_t first = (uint64_t)b * (uint64_t)bucket << 32;
-        int32_t lo = 0, hi = K;
-        while (lo < hi) {
-            const int32_t mid = (lo + hi) >> 1;
-            if (key[mid] < first) lo = mid + 1; else hi = mid;
-        }
-        list_start[t * (kBuckets + 1) + b] = (uint16_t)lo;
+    // where each unit of classes begins: entry j is the first one of the units behind entry j - 1's up to its own
+    uint16_t *start = list_start + t * (units + 1);
+    for (int32_t j = lane; j <= K; j += 32) {
+        const int32_t from = j == 0 ? 0 : min((int32_t)(key[j - 1] >> 32) / unit, units) + 1;
+        const int32_t to = j == K ? units : min((int32_t)(key[j] >> 32) / unit, units);
+        for (int32_t u = from; u <= to; ++u) start[u] = (uint16_t)j;
     }
     if (lane == 0) {
         flags[t] = any ? 1 : 0;
@@ -477,6 +475,7 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
     int planes, pack_w;
     int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
+    int32_t unit, units;                   // classes per entry of list_start: half a tile, more where that would be a large table
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
     bool direct;
     int64_t Tpad;
@@ -538,7 +537,6 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     p.o_x = take(p.direct ? 0 : (size_t)p.planes * p.Tpad * p.ld * 2);
     p.o_w = take(p.pack_w ? (size_t)p.planes * V * p.ld * 2 : 0);
     p.o_list = take((size_t)T * K * 8);
-    p.o_start = take(K > 0 ? (size_t)T * (kBuckets + 1) * 2 : 0);
     p.o_flags = take(K > 0 ? (size_t)T : 0);
     p.o_teacher = take(K > 0 ? (size_t)T * 8 : 0);
     if (!backward) {
@@ -577,6 +575,12 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.o_dx = take(p.dx_slots ? (size_t)p.dx_splits * p.Tpad * d * 4 : 0);
         p.o_dw = take(p.dw_slots ? (size_t)p.dw_splits * p.width * d * 4 : 0);
     }
+    if (K > 0) {
+        p.unit = p.bn / 2;
+        while ((int64_t)T * ((V + p.unit - 1) / p.unit) > ((int64_t)1 << 26) && p.unit < V) p.unit *= 2;
+        p.units = (V + p.unit - 1) / p.unit;
+        p.o_start = take((size_t)T * (p.units + 1) * 2);
+    }
     p.total = o;
     return p;
 }
@@ -606,19 +610,19 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         uint8_t *flags = reinterpret_cast<uint8_t *>(ws + p.o_flags);
         float2 *stats = reinterpret_cast<float2 *>(ws + p.o_teacher);
         uint16_t *start = reinterpret_cast<uint16_t *>(ws + p.o_start);
-        const int32_t bucket = (int32_t)(((int64_t)c.V + kBuckets - 1) / kBuckets);
         const cudaError_t e = c.top_dtype == TBN_F32
             ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
-                         c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, list, start, flags, stats)
+                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, list, start, flags, stats)
             : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index,
-                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, bucket, list, start, flags, stats);
+                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, list, start, flags, stats);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
         out->list = list;
         out->list_start = start;
         out->K = c.K;
-        out->bucket = bucket;
+        out->unit = p.unit;
+        out->units = p.units;
     }
     out->labels = labels;
     const int32_t w_ld = p.pack_w ? p.ld : c.d;

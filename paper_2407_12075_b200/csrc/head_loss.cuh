@@ -9,7 +9,6 @@ namespace head {
 
 constexpr int kTile = 256;                 // tokens x classes of one output tile (two CTAs, 128 rows each)
 constexpr int kMaxSplits = 16;
-constexpr int kBuckets = 64;                // of the vocabulary, into which a teacher's sorted list is divided
 
 __host__ __device__ inline int64_t round_up64(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
@@ -59,8 +58,8 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     int64_t T, Tpad;
     int32_t V, v0, width;
     const int2 *list;                      // distillation: [T][K] (class, probability), ascending, INT32_MAX behind the last; else null
-    const uint16_t *list_start;            // [T][kBuckets + 1]
-    int32_t K, bucket;                     // classes per bucket
+    const uint16_t *list_start;            // [T][units + 1]
+    int32_t K, unit, units;                // classes per unit, units of the vocabulary
     // forward: (maximum, sum, dot, unused) of every token and bn / 2 classes: [Tpad][parts]
     float4 *part;
     int32_t parts;

@@ -23,10 +23,10 @@
 // fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products lo*hi, hi*lo and
 // hi*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.  The tensor core cuts its running sum off toward
 // zero at every 16-element step, an error that grows with the length of the chain (measured, dot products of 1024: 2.6e-6
-// of the result's scale as one chain of 192 steps, 7e-7 for the bf16 form's 64), so with fp32 operands the chain ends
-// after every 64 elements: the small products first, then the four hi*hi steps, and the epilogue warps add the 64-element
-// sums in registers, rounding to nearest.  For that the tiles are 256 x 128 (64 running sums per thread) on four accumulators:
-// with 256 x 256 and two, the hand-overs of a chain (commit, wait, read, release) outlast its MMAs.
+// of the result's scale as one chain of 192 steps, 7e-7 for the bf16 form's 64), so with fp32 operands a chain ends after
+// 128 elements, the small products first, and the epilogue warps add the chains in registers, rounding to nearest.  For that
+// the tiles are 256 x 128 (64 running sums per thread) on four accumulators: with 256 x 256 and two, the hand-overs of a
+// chain (commit, wait, read, release) outlast its MMAs.
 //
 // Same conventions as the other tcgen05 kernels: every wait is bounded, a wait that gives up records the status and the
 // kernel winds down and returns.
@@ -84,8 +84,8 @@ struct LogitsParams {
     int64_t Tpad;
     int32_t V, v0, width;
     const int2 *list;                      // distillation: [T][K] (class, probability) pairs, ascending; else null
-    const uint16_t *list_start;            // [T][kBuckets + 1]: where the classes of each bucket begin in the row's list
-    int32_t K, bucket;
+    const uint16_t *list_start;            // [T][units + 1]: where the classes of each unit begin in the row's list
+    int32_t K, unit, units;
     float4 *part;
     int32_t parts;
     void *dz;
@@ -283,15 +283,11 @@ struct Listed {
         }
         entry = l.list + (int64_t)r.row * l.K;
         count = live ? l.K : 0;
-        if (count) {                                   // first entry >= first: between the starts of its bucket and the next
-            const int32_t bucket = first / l.bucket;
-            const uint16_t *start = l.list_start + (int64_t)r.row * (kBuckets + 1) + min(bucket, kBuckets - 1);
-            int32_t lo = __ldg(start), hi = bucket < kBuckets ? (int32_t)__ldg(start + 1) : count;
-            while (lo < hi) {
-                const int32_t mid = (lo + hi) >> 1;
-                if (__ldg(&entry[mid].x) < first) lo = mid + 1; else hi = mid;
-            }
-            pos = lo;
+        if (count) {                                   // first entry >= first: where its unit of classes begins, or behind that
+            const int32_t unit = min(first / l.unit, l.units);
+            pos = (int32_t)__ldg(l.list_start + (int64_t)r.row * (l.units + 1) + unit);
+            if (unit * l.unit != first)
+                while (pos < count && __ldg(&entry[pos].x) < first) ++pos;
         }
         const int2 e = at(pos);
         w1 = at(pos + 1); w2 = at(pos + 2); w3 = at(pos + 3);
@@ -570,26 +566,49 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 // MN-major form: 8192 bytes).  A step of 16 along K: 32 bytes inside the swizzled row, or two 8-row groups.
                 const uint32_t a_hi = (a_mn ? 512u : 1u) << 16, b_hi = (b_mn ? 512u : 1u) << 16;
                 const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
-                for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
-                    ok = wait_bar(smem_u32(&ctl->full[px.stage]), px.phase, abort_flag, p.status, (42 << 24) | (px.stage << 16) | detail);
-                    if (PL == 2 && ok)
-                        ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
-                    if (!ok) break;
-                    tc_fence_after();
+                if constexpr (PL == 1) {
                     const uint32_t d_addr = tmem_u + pd.stage * kCols<PL>;
-                    const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
-                    const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
-#pragma unroll
-                    for (int term = 0; term < (PL == 1 ? 1 : 3); ++term) {       // two planes: lo*hi, hi*lo, hi*hi
-                        const uint32_t at = a_lo + (PL == 2 && term == 0 ? a_bytes >> 4 : 0u), bt = b_lo + (PL == 2 && term == 1 ? b_bytes >> 4 : 0u);
+                    for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
+                        ok = wait_bar(smem_u32(&ctl->full[px.stage]), px.phase, abort_flag, p.status, (42 << 24) | (px.stage << 16) | detail);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + a_bytes;
+                        const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
 #pragma unroll
                         for (int st = 0; st < 4; ++st)
-                            mma_pair(d_addr, at + st * a_step, bt + st * b_step, kDescHi, idesc,
-                                     term > 0 || st > 0 ? 1u : (uint32_t)(PL == 1 && kb > t.kb0), leader);
+                            mma_pair(d_addr, a_lo + st * a_step, b_lo + st * b_step, kDescHi, idesc, st > 0 ? 1u : (uint32_t)(kb > t.kb0), leader);
+                        commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
+                        px.advance(n_stages);
                     }
-                    commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
-                    px.advance(n_stages);
-                    if (PL == 2) {
+                } else {
+                    for (int32_t kb = t.kb0; kb < t.kb1; kb += 2) {              // one chain: 128 elements
+                        const int n = min(2, t.kb1 - kb);
+                        ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
+                        const uint32_t d_addr = tmem_u + pd.stage * kCols<PL>;
+                        Pipe pi = px;
+                        for (int i = 0; i < n && ok; ++i) {                      // lo*hi, hi*lo
+                            ok = wait_bar(smem_u32(&ctl->full[pi.stage]), pi.phase, abort_flag, p.status, (42 << 24) | (pi.stage << 16) | detail);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint32_t sa = stage0 + pi.stage * stage_bytes, sb = sa + PL * a_bytes;
+                            const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
+#pragma unroll
+                            for (int st = 0; st < 4; ++st)
+                                mma_pair(d_addr, a_lo + (a_bytes >> 4) + st * a_step, b_lo + st * b_step, kDescHi, idesc, st > 0 || i > 0 ? 1u : 0u, leader);
+#pragma unroll
+                            for (int st = 0; st < 4; ++st)
+                                mma_pair(d_addr, a_lo + st * a_step, b_lo + (b_bytes >> 4) + st * b_step, kDescHi, idesc, 1u, leader);
+                            pi.advance(n_stages);
+                        }
+                        if (!ok) break;
+                        for (int i = 0; i < n; ++i) {                            // hi*hi
+                            const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
+                            const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
+#pragma unroll
+                            for (int st = 0; st < 4; ++st) mma_pair(d_addr, a_lo + st * a_step, b_lo + st * b_step, kDescHi, idesc, 1u, leader);
+                            commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
+                            px.advance(n_stages);
+                        }
                         commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
                         pd.advance(kAccs<PL>);
                     }
@@ -669,7 +688,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             } else {
 #pragma unroll
                 for (int j = 0; j < 64; ++j) acc[PL == 2 ? j : 0] = 0.0f;
-                for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
+                for (int32_t kb = t.kb0; kb < t.kb1; kb += 2) {
                     ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                     if (!ok) break;
                     tc_fence_after();
@@ -926,7 +945,7 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
     l.scales = a.scales;
     l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width;
-    l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.bucket = a.bucket;
+    l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.unit = a.unit; l.units = a.units;
     l.part = a.part; l.parts = a.parts;
     l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
     p.status = a.status;
