@@ -475,7 +475,7 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
     int planes, pack_w;
     int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
-    int32_t unit, units;                   // classes per entry of list_start: half a tile, more where that would be a large table
+    int32_t unit, units;                   // classes per entry of list_start: an epilogue warp's, more where that would be a large table
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
     bool direct;
     int64_t Tpad;
@@ -521,6 +521,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     Plan p = {};
     p.planes = dtype == TBN_F32 ? 2 : 1;
     p.cols = dtype == TBN_F32 ? 128 : 256;
+    const int32_t groups = dtype == TBN_F32 ? 4 : 2;   // epilogue warps that share a tile's columns
     p.ld = (d + 63) / 64 * 64;                         // packed rows are whole 64-column panels
     p.pack_w = dtype == TBN_F32 || d % 8 != 0;
     p.Tpad = round_up64(T, kTile);
@@ -541,7 +542,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     p.o_teacher = take(K > 0 ? (size_t)T * 8 : 0);
     if (!backward) {
         p.bn = classes_per_tile(T, V, p.cols, 64, 32);
-        p.parts = (int32_t)((V + p.bn - 1) / p.bn * 2);
+        p.parts = (int32_t)((V + p.bn - 1) / p.bn * groups);
         p.o_part = take((size_t)p.parts * p.Tpad * sizeof(float4));
     } else {
         int64_t width = (int64_t)(kPieceBytes / ((size_t)2 * p.planes * p.Tpad)) / kTile * kTile;
@@ -576,7 +577,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.o_dw = take(p.dw_slots ? (size_t)p.dw_splits * p.width * d * 4 : 0);
     }
     if (K > 0) {
-        p.unit = p.bn / 2;
+        p.unit = p.bn / groups;
         while ((int64_t)T * ((V + p.unit - 1) / p.unit) > ((int64_t)1 << 26) && p.unit < V) p.unit *= 2;
         p.units = (V + p.unit - 1) / p.unit;
         p.o_start = take((size_t)T * (p.units + 1) * 2);

@@ -60,7 +60,7 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const int2 *list;                      // distillation: [T][K] (class, probability), ascending, INT32_MAX behind the last; else null
     const uint16_t *list_start;            // [T][units + 1]
     int32_t K, unit, units;                // classes per unit, units of the vocabulary
-    // forward: (maximum, sum, dot, unused) of every token and bn / 2 classes: [Tpad][parts]
+    // forward: (maximum, sum, dot, unused) of every token and epilogue warp's classes (bn / 2, or bn / 4 with two planes): [Tpad][parts]
     float4 *part;
     int32_t parts;
     // backward

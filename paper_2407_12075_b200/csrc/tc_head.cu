@@ -12,7 +12,7 @@
 // step, so a byte staged feeds twice the multiplications of a 128 x 256 tile on one CTA (per 64-element step and SM:
 // 32 KB instead of 48 KB for the same 4.2 MFLOP), which is what keeps shared memory and L2 below the tensor pipe.
 // Warp roles per CTA: 0 = TMA producer of A, 1 = MMA issuer (the first CTA of the pair only), 2 = TMA producer of B, 3 idle,
-// 4-11 = epilogue, two warps per tensor-memory quadrant, 128 columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
+// 4-11 (two planes: 4-19) = epilogue, two (four) warps per tensor-memory quadrant, 128 (32) columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
 // main loop of the next.
 //
 // dz lives in blocks that are images of the shared-memory tiles: panels of 64 classes, in a panel one 128-byte line per
@@ -45,12 +45,10 @@ namespace {
 
 using namespace tc;
 
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = 128 + 32 * kEpiWarps;
 constexpr int kMaxStages = 24;
 constexpr uint32_t kSideBytes = 128 * 128;             // one operand, one plane, one CTA: 128 rows x 64 elements
 constexpr uint32_t kStageBudget = 6 * 2 * kSideBytes;  // 192 KB of stages
-constexpr uint32_t kExchange = 4096;                   // per epilogue warp: 32 lines of 128 bytes
+constexpr uint32_t kExchange = 2048;                   // per epilogue warp: 16 lines of 128 bytes
 constexpr uint32_t kTmemCols = 512;
 constexpr int kGroupM = 32;                            // token tiles that share a sweep over the classes
 
@@ -59,8 +57,13 @@ enum { kStats = 0, kDz = 1, kGrads = 2 };
 // columns of a tile at most, and accumulators in the 512 columns of tensor memory
 template <int PL> constexpr int kCols = PL == 1 ? 256 : 128;
 template <int PL> constexpr int kAccs = 512 / kCols<PL>;
+// epilogue warps: kGroups per tensor-memory quadrant, which share a tile's columns
+template <int PL> constexpr int kGroups = PL == 1 ? 2 : 4;
+template <int PL> constexpr int kEpiWarps = 4 * kGroups<PL>;
+template <int PL> constexpr int kThreads = 128 + 32 * kEpiWarps<PL>;
+template <int PL> constexpr int kWarpCols = kCols<PL> / kGroups<PL>;
 // behind the stages: exchange lines, or the biases of every epilogue warp's columns
-template <int MODE> constexpr uint32_t kScratch = kEpiWarps * (MODE == kGrads ? kExchange : 128 * sizeof(float));
+template <int MODE, int PL> constexpr uint32_t kScratch = kEpiWarps<PL> * (MODE == kGrads ? kExchange : kWarpCols<PL> * sizeof(float));
 
 struct Control {
     uint64_t full[kMaxStages], empty[kMaxStages], d_full[4], d_empty[4];
@@ -368,7 +371,7 @@ __device__ __forceinline__ void ld_global_v8(const float *ptr, float (&v)[8]) {
 struct RowsOut {
     void *out;
     const float *prev;
-    int32_t row, prev_row, rows_in, d;
+    int32_t row, prev_row, rows_in, d, end;          // end: the first column that is not this warp's
 };
 // 32 columns of every lane's row, in whole 32-byte sectors (d a multiple of 16, out 32-byte aligned).
 __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_t c0, bool out_bf16, float (&v)[32])
@@ -377,7 +380,7 @@ __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_
     if (o.prev) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (c0 + 8 * q >= o.d) break;
+            if (c0 + 8 * q >= o.end) break;
             float w[8];
             ld_global_v8(o.prev + (int64_t)o.prev_row * o.d + c0 + 8 * q, w);
 #pragma unroll
@@ -388,7 +391,7 @@ __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_
     if (out_bf16) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (c0 + 16 * h >= o.d) break;
+            if (c0 + 16 * h >= o.end) break;
             uint32_t pk[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -400,7 +403,7 @@ __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_
     } else {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (c0 + 8 * q >= o.d) break;
+            if (c0 + 8 * q >= o.end) break;
             uint32_t u[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[j] = __float_as_uint(v[8 * q + j]);
@@ -411,42 +414,47 @@ __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_
 // Rows that are not whole sectors: through the warp's exchange lines, then a row at a time, lane = column.
 __device__ __forceinline__ void write_elements(const RowsOut &o, uint32_t exchange, int lane, int32_t c0, bool out_bf16, const float (&v)[32])
 {
-    const uint32_t line = exchange + (uint32_t)lane * 128;
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-        sts_v4(line + (uint32_t)((q ^ (lane & 7)) << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]),
-               __float_as_uint(v[4 * q + 3]));
-    __syncwarp();
     const int32_t c = c0 + lane;
 #pragma unroll 1
-    for (int h = 0; h < 32; h += 8) {                  // eight rows in flight
-        float x[8];
-        int32_t to[8];
+    for (int part = 0; part < 2; ++part) {             // 16 rows at a time
+        if ((lane >> 4) == part) {
+            const uint32_t line = exchange + (uint32_t)(lane & 15) * 128;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int r = h + k;
-            x[k] = __uint_as_float(lds_b32(exchange + (uint32_t)r * 128 + (uint32_t)(((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
-            to[k] = __shfl_sync(0xffffffffu, o.row, r);
-            if (o.prev) {
-                const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
-                if (r < o.rows_in && c < o.d) x[k] += o.prev[(int64_t)from * o.d + c];
+            for (int q = 0; q < 8; ++q)
+                sts_v4(line + (uint32_t)((q ^ (lane & 7)) << 4), __float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]),
+                       __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+        }
+        __syncwarp();
+#pragma unroll 1
+        for (int h = 0; h < 16; h += 8) {              // eight rows in flight
+            float x[8];
+            int32_t to[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r = part * 16 + h + k;
+                x[k] = __uint_as_float(lds_b32(exchange + (uint32_t)(h + k) * 128 + (uint32_t)(((lane >> 2) ^ k) << 4) + (lane & 3) * 4));
+                to[k] = __shfl_sync(0xffffffffu, o.row, r);
+                if (o.prev) {
+                    const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
+                    if (r < o.rows_in && c < o.end) x[k] += o.prev[(int64_t)from * o.d + c];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (part * 16 + h + k < o.rows_in && c < o.end) {
+                    const int64_t at = (int64_t)to[k] * o.d + c;
+                    if (out_bf16) static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x[k]);
+                    else static_cast<float *>(o.out)[at] = x[k];
+                }
             }
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (h + k < o.rows_in && c < o.d) {
-                const int64_t at = (int64_t)to[k] * o.d + c;
-                if (out_bf16) static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x[k]);
-                else static_cast<float *>(o.out)[at] = x[k];
-            }
-        }
+        __syncwarp();
     }
-    __syncwarp();
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------
 template <int MODE, int PL, bool BIAS>
-__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kThreads<PL>, 1) __cluster_dims__(2, 1, 1)
 head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelParams p, const int32_t k_logits)
 {
     constexpr uint32_t kBBytes = kCols<PL> * 64;       // B of a gradient tile: one plane, one CTA
@@ -462,7 +470,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
     const uint32_t stage0 = raw + pad;
-    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget + kScratch<MODE>);
+    Control *ctl = reinterpret_cast<Control *>(smem_raw + pad + kStageBudget + kScratch<MODE, PL>);
     volatile int *abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -471,7 +479,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-        for (int s = 0; s < kAccs<PL>; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
+        for (int s = 0; s < kAccs<PL>; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps<PL>); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         fence_proxy_async();
@@ -626,8 +634,8 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
         }
         __syncwarp();
     } else if (warp >= 4) {
-        // ---------------- epilogue: thread = row, half of the tile's columns in chunks of 32 ----------------
-        const int ew = warp - 4, qd = warp & 3, half = ew >> 2;
+        // ---------------- epilogue: thread = row, a group's share of the tile's columns in chunks of 32 --------
+        const int ew = warp - 4, qd = warp & 3, group = ew >> 2;
         const uint32_t t_lane = tmem_base + ((uint32_t)(qd * 32) << 16);
         const uint32_t exchange = stage0 + kStageBudget + (uint32_t)ew * kExchange;
         Pipe pd;
@@ -661,14 +669,14 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             t = next;
             const RowInfo info = next_info;
             const int32_t row0 = t.m0 + (int32_t)rank * 128 + qd * 32, row = row0 + lane;
-            const int32_t hc = t.bn >> 1, col0 = t.n0 + half * hc;
+            const int32_t hc = t.bn / kGroups<PL>, col0 = t.n0 + group * hc;
             const bool live = row < n_live;
             Listed list;
             if (MODE != kGrads) list.begin(p.l, info, live, p.l.v0 + col0);
-            float *bias_s = reinterpret_cast<float *>(smem_raw + pad + kStageBudget) + ew * 128;
+            float *bias_s = reinterpret_cast<float *>(smem_raw + pad + kStageBudget) + ew * kWarpCols<PL>;
             if (BIAS) {                                // times log2(e) / tau, finite ones kept finite; -infinity behind the last class
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < kWarpCols<PL> / 32; ++j) {
                     const int32_t c = col0 + j * 32 + lane;
                     const float b = j * 32 < hc && c < p.l.width ? __ldg(p.l.bias + p.l.v0 + c) : -INFINITY;
                     bias_s[j * 32 + lane] = b == -INFINITY ? b : fmaxf(b * p.l.scale2, -3.402823466e38f) + (b - b);
@@ -678,31 +686,26 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             more = sched.get<MODE, PL>(step + 1, next);
             if (more) next_info = row_info(next);
             // the tile's sums: left in tensor memory, or (two planes) added up from its 64-element chains in registers
-            float acc[PL == 2 ? 64 : 1];
+            float acc[PL == 2 ? kWarpCols<PL> : 1];
             uint32_t t_acc = 0;
             if (PL == 1) {
                 ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                 if (!ok) break;
                 tc_fence_after();
-                t_acc = t_lane + pd.stage * kCols<PL> + (uint32_t)(half * hc);
+                t_acc = t_lane + pd.stage * kCols<PL> + (uint32_t)(group * hc);
             } else {
 #pragma unroll
-                for (int j = 0; j < 64; ++j) acc[PL == 2 ? j : 0] = 0.0f;
+                for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] = 0.0f;
                 for (int32_t kb = t.kb0; kb < t.kb1; kb += 2) {
                     ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t t_sum = t_lane + pd.stage * kCols<PL> + (uint32_t)(half * hc);
-                    uint32_t r[2][32];
-                    tmem_ld_32x32(t_sum, r[0]);
-                    if (hc > 32) tmem_ld_32x32(t_sum + 32, r[1]);
+                    const uint32_t t_sum = t_lane + pd.stage * kCols<PL> + (uint32_t)(group * hc);
+                    uint32_t r[32];
+                    tmem_ld_32x32(t_sum, r);
                     tc_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] += __uint_as_float(r[0][j]);
-                    if (hc > 32) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[PL == 2 ? 32 + j : 0] += __uint_as_float(r[1][j]);
-                    }
+                    for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] += __uint_as_float(r[j]);
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
@@ -719,21 +722,16 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 #pragma unroll
                     for (int j = 0; j < 32; ++j) out[j] = __uint_as_float(ahead[j]);
                     if ((ch + 1) * 32 < hc) tmem_ld_32x32(t_acc + (ch + 1) * 32, ahead);
-                } else {                               // chosen by a uniform branch, so that what follows exists once
+                } else {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        if (ch == k) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) out[j] = acc[PL == 2 ? k * 32 + j : 0];
-                        }
-                    }
+                    for (int j = 0; j < 32; ++j) out[j] = acc[PL == 2 ? j : 0];
                 }
             };
 
             if (MODE == kStats) {
                 float m = -INFINITY, l = 0.0f, dot = 0.0f;
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
+                for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
                     if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32, end = min(c0 + 32, min(col0 + hc, p.l.width));
                     float v[32];
@@ -778,7 +776,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const int32_t panels = p.l.ldz / 64;
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
+                for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
                     if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32;
                     float v[32];
@@ -844,11 +842,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 o.row = to_slot ? lane : is_dx ? info.row : g.v0 + row0 + lane;
                 o.prev = !(is_dx && g.dx_add) ? nullptr : slot ? slot : static_cast<const float *>(g.dx);
                 o.prev_row = slot ? lane : info.row;
-                o.rows_in = rows_in; o.d = g.d;
+                o.rows_in = rows_in; o.d = g.d; o.end = min(g.d, col0 + hc);
                 const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16);
                 const bool sectors = g.d % 16 == 0 && (reinterpret_cast<uintptr_t>(o.out) & 31) == 0 && (reinterpret_cast<uintptr_t>(o.prev) & 31) == 0;
 #pragma unroll 1
-                for (int ch = 0; ch < 4; ++ch) {
+                for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
                     if (ch * 32 >= hc || c0 >= g.d) continue;
                     float v[32];
@@ -914,7 +912,7 @@ int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_log
     const int pairs = sm_count() / 2;
     if (pairs <= 0) return TBN_ERR_CUDA;
     if (tiles <= 0) return TBN_OK;
-    constexpr size_t smem = kStageBudget + kScratch<MODE> + sizeof(Control) + 1024;
+    constexpr size_t smem = kStageBudget + kScratch<MODE, PL> + sizeof(Control) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory");
     auto kern = head_kernel<MODE, PL, BIAS>;
     int dev = 0;
@@ -925,7 +923,7 @@ int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_log
         ready[dev].store(true, std::memory_order_release);
     }
     const unsigned grid = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-    return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, maps, p, k_logits) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
+    return launch_pdl(kern, dim3(grid), dim3(kThreads<PL>), smem, s, maps, p, k_logits) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 
 template <int MODE>
