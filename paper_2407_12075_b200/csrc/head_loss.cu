@@ -30,7 +30,9 @@ constexpr size_t kPieceBytes = (size_t)256 << 20;      // bound on one piece of 
 // One warp per token: p = softmax(logit / tau) over the entries whose index is a class and whose logit is above
 // -infinity, sum p log p, and the entries sorted by class (by position among equals), which is the order in which the
 // epilogues meet the classes.
-constexpr int kTeacherWarps = 4;
+constexpr int kMaxUnits = 2046;                        // of a list_start row: 4 KB per warp
+inline int teacher_warps(int32_t Kp) { return Kp <= 512 ? 4 : 2; }
+inline size_t teacher_smem(int32_t Kp, int32_t pitch) { return (size_t)Kp * 12 + (size_t)pitch * 2; }      // per warp
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -44,18 +46,20 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 
 template <typename TL>
-__global__ void __launch_bounds__(32 * kTeacherWarps)
+__global__ void __launch_bounds__(128)
 teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, int64_t T, int32_t K, int32_t Kp, int32_t V,
-               float inv_tau, int32_t unit, int32_t units, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
+               float inv_tau, int32_t unit, int32_t units, int32_t pitch, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
                uint8_t *__restrict__ flags, float2 *__restrict__ stats)
 {
-    extern __shared__ uint8_t teacher_smem[];
+    extern __shared__ __align__(16) uint8_t teacher_mem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint64_t *key = reinterpret_cast<uint64_t *>(teacher_smem) + (size_t)warp * Kp;
-    float *prob = reinterpret_cast<float *>(reinterpret_cast<uint64_t *>(teacher_smem) + (size_t)kTeacherWarps * Kp) + (size_t)warp * Kp;
+    const int warps = blockDim.x >> 5;
+    uint64_t *key = reinterpret_cast<uint64_t *>(teacher_mem) + (size_t)warp * Kp;
+    float *prob = reinterpret_cast<float *>(reinterpret_cast<uint64_t *>(teacher_mem) + (size_t)warps * Kp) + (size_t)warp * Kp;
+    uint16_t *start = reinterpret_cast<uint16_t *>(teacher_mem + (size_t)warps * Kp * 12) + (size_t)warp * pitch;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t t = (int64_t)blockIdx.x * kTeacherWarps + warp;
+    const int64_t t = (int64_t)blockIdx.x * warps + warp;
     if (t >= T) return;
     float top = -INFINITY;
     bool any = false, nan = false;
@@ -110,13 +114,17 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
         const uint64_t k = key[j];
         list[t * K + j] = make_int2((int32_t)(k >> 32), __float_as_int(prob[(uint32_t)k]));
     }
-    // where each unit of classes begins: entry j is the first one of the units behind entry j - 1's up to its own
-    uint16_t *start = list_start + t * (units + 1);
+    // where each unit of classes begins: entry j is the first one of the units behind entry j - 1's up to its own.  Put
+    // together in shared memory: stores of two bytes all over the row would keep the load / store unit busy for longer than
+    // everything else here.
     for (int32_t j = lane; j <= K; j += 32) {
         const int32_t from = j == 0 ? 0 : min((int32_t)(key[j - 1] >> 32) / unit, units) + 1;
         const int32_t to = j == K ? units : min((int32_t)(key[j] >> 32) / unit, units);
         for (int32_t u = from; u <= to; ++u) start[u] = (uint16_t)j;
     }
+    __syncwarp();
+    uint32_t *out = reinterpret_cast<uint32_t *>(list_start + t * pitch);
+    for (int32_t i = lane; i < pitch / 2; i += 32) out[i] = reinterpret_cast<const uint32_t *>(start)[i];
     if (lane == 0) {
         flags[t] = any ? 1 : 0;
         stats[t] = make_float2(plogp, total);
@@ -475,7 +483,7 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
     int planes, pack_w;
     int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
-    int32_t unit, units;                   // classes per entry of list_start: an epilogue warp's, more where that would be a large table
+    int32_t unit, units, pitch;                 // classes per entry of list_start: an epilogue warp's, more where that would be a large table
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
     bool direct;
     int64_t Tpad;
@@ -578,9 +586,10 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     }
     if (K > 0) {
         p.unit = p.bn / groups;
-        while ((int64_t)T * ((V + p.unit - 1) / p.unit) > ((int64_t)1 << 26) && p.unit < V) p.unit *= 2;
+        while (V / p.unit >= kMaxUnits || (T * (V / p.unit) > ((int64_t)1 << 26) && p.unit < V)) p.unit *= 2;
         p.units = (V + p.unit - 1) / p.unit;
-        p.o_start = take((size_t)T * (p.units + 1) * 2);
+        p.pitch = (p.units + 2) / 2 * 2;               // units + 1 entries in whole 32-bit words
+        p.o_start = take((size_t)T * p.pitch * 2);
     }
     p.total = o;
     return p;
@@ -605,17 +614,18 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     if (c.K > 0) {
         int32_t Kp = 32;
         while (Kp < c.K) Kp <<= 1;
-        const size_t smem = (size_t)kTeacherWarps * Kp * 12;
-        const dim3 grid((unsigned)((c.T + kTeacherWarps - 1) / kTeacherWarps));
+        const int warps = teacher_warps(Kp);
+        const size_t smem = teacher_smem(Kp, p.pitch) * warps;
+        const dim3 grid((unsigned)((c.T + warps - 1) / warps));
         int2 *list = reinterpret_cast<int2 *>(ws + p.o_list);
         uint8_t *flags = reinterpret_cast<uint8_t *>(ws + p.o_flags);
         float2 *stats = reinterpret_cast<float2 *>(ws + p.o_teacher);
         uint16_t *start = reinterpret_cast<uint16_t *>(ws + p.o_start);
         const cudaError_t e = c.top_dtype == TBN_F32
-            ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
-                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, list, start, flags, stats)
-            : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * kTeacherWarps), smem, s, c.top_index,
-                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, list, start, flags, stats);
+            ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * warps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
+                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats)
+            : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * warps), smem, s, c.top_index,
+                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
@@ -624,6 +634,7 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         out->K = c.K;
         out->unit = p.unit;
         out->units = p.units;
+        out->pitch = p.pitch;
     }
     out->labels = labels;
     const int32_t w_ld = p.pack_w ? p.ld : c.d;

@@ -58,8 +58,8 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     int64_t T, Tpad;
     int32_t V, v0, width;
     const int2 *list;                      // distillation: [T][K] (class, probability), ascending, INT32_MAX behind the last; else null
-    const uint16_t *list_start;            // [T][units + 1]
-    int32_t K, unit, units;                // classes per unit, units of the vocabulary
+    const uint16_t *list_start;            // [T][pitch]: where the units + 1 units of classes begin in a row's list
+    int32_t K, unit, units, pitch;
     // forward: (maximum, sum, dot, unused) of every token and epilogue warp's classes (bn / 2, or bn / 4 with two planes): [Tpad][parts]
     float4 *part;
     int32_t parts;

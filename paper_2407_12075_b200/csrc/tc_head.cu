@@ -87,8 +87,8 @@ struct LogitsParams {
     int64_t Tpad;
     int32_t V, v0, width;
     const int2 *list;                      // distillation: [T][K] (class, probability) pairs, ascending; else null
-    const uint16_t *list_start;            // [T][units + 1]: where the classes of each unit begin in the row's list
-    int32_t K, unit, units;
+    const uint16_t *list_start;            // [T][pitch]: where the classes of each unit begin in the row's list
+    int32_t K, unit, units, pitch;
     float4 *part;
     int32_t parts;
     void *dz;
@@ -288,7 +288,7 @@ struct Listed {
         count = live ? l.K : 0;
         if (count) {                                   // first entry >= first: where its unit of classes begins, or behind that
             const int32_t unit = min(first / l.unit, l.units);
-            pos = (int32_t)__ldg(l.list_start + (int64_t)r.row * (l.units + 1) + unit);
+            pos = (int32_t)__ldg(l.list_start + (int64_t)r.row * l.pitch + unit);
             if (unit * l.unit != first)
                 while (pos < count && __ldg(&entry[pos].x) < first) ++pos;
         }
@@ -943,7 +943,7 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
     l.scales = a.scales;
     l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width;
-    l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.unit = a.unit; l.units = a.units;
+    l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.unit = a.unit; l.units = a.units; l.pitch = a.pitch;
     l.part = a.part; l.parts = a.parts;
     l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
     p.status = a.status;
