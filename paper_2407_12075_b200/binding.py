@@ -7,6 +7,7 @@ missing or a call returns a non-zero status, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -533,38 +534,56 @@ def tbn_linear_distill_workspace_bytes(T, in_f, vocab, dtype, K, backward) -> in
 
 def _head_check(x, weight, bias, labels, floats=(), top_logit=None):
     """Shapes, types and devices of a head-loss call; the library sees pointers only.  Returns (T, in_f, vocab, dtype)."""
-    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1]:
-        raise TbnError(-2, f"head loss: x {tuple(x.shape)} and weight {tuple(weight.shape)}")
-    T, V, device = x.shape[0], weight.shape[0], x.device
-    if weight.dtype != x.dtype:
-        raise TypeError(f"x is {x.dtype}, weight is {weight.dtype}")
-    if labels.dtype != torch.int64 or labels.dim() != (1 if top_logit is None else 2) or labels.shape[0] != T:
+    xs, wsh, device, dtype = x.shape, weight.shape, x.device, x.dtype
+    if len(xs) != 2 or len(wsh) != 2 or xs[1] != wsh[1]:
+        raise TbnError(-2, f"head loss: x {tuple(xs)} and weight {tuple(wsh)}")
+    if weight.dtype != dtype:
+        raise TypeError(f"x is {dtype}, weight is {weight.dtype}")
+    T, V = xs[0], wsh[0]
+    ls = labels.shape
+    if labels.dtype != torch.int64 or len(ls) != (1 if top_logit is None else 2) or ls[0] != T:
         raise TbnError(-2, f"head loss: {'targets' if top_logit is None else 'top_index'} must be int64, one row per token")
-    if top_logit is not None and top_logit.shape != labels.shape:
-        raise TbnError(-2, "head loss: top_logit must have the shape of top_index")
-    if bias is not None and (bias.shape != (V,) or bias.dtype != torch.float32):
-        raise TbnError(-2, f"head loss: bias must be float32 of shape ({V},)")
+    if weight.device != device or labels.device != device:
+        raise ValueError(f"head loss: tensors on {device}, {weight.device} and {labels.device}")
+    if top_logit is not None and (top_logit.shape != ls or top_logit.device != device):
+        raise TbnError(-2, "head loss: top_logit must have the shape and device of top_index")
+    if bias is not None and (bias.shape != (V,) or bias.dtype != torch.float32 or bias.device != device):
+        raise TbnError(-2, f"head loss: bias must be float32 of shape ({V},) on {device}")
     for t in floats:
-        if t.shape != (T,) or t.dtype != torch.float32:
-            raise TbnError(-2, f"head loss: lse and dloss must be float32 of shape ({T},)")
-    if not x.is_cuda:
+        if t.shape != (T,) or t.dtype != torch.float32 or t.device != device:
+            raise TbnError(-2, f"head loss: lse and dloss must be float32 of shape ({T},) on {device}")
+    if device.type != "cuda":
         raise ValueError("head loss: the tensors must be on a CUDA device")
-    for t in (weight, labels, bias, top_logit, *floats):
-        if t is not None and t.device != device:
-            raise ValueError(f"head loss: tensors on {device} and {t.device}")
-    return T, x.shape[1], V, _dtype_code(x)
+    return T, xs[1], V, BF16 if dtype == torch.bfloat16 else _dtype_code(x)
 
 
-def _head_call(name, device, need, workspace, *args):
+@functools.lru_cache(maxsize=1024)
+def _head_need(sizes, device_index):
+    """Workspace bytes of a call; they follow from the sizes and the device's number of SMs."""
+    with torch.cuda.device(device_index):
+        if len(sizes) == 5:
+            return tbn_linear_xent_workspace_bytes(*sizes)
+        return tbn_linear_distill_workspace_bytes(*sizes)
+
+
+def _head_call(name, device, sizes, workspace, *args):
     """Runs the entry point on the tensors' device and that device's current stream."""
-    ws = workspace if workspace is not None else _ws(need, device)
-    fn, stream = getattr(lib(), name), torch._C._cuda_getCurrentRawStream(device.index)
-    if torch.cuda.current_device() == device.index:
-        status = fn(*args, _ptr(ws), ws.numel() * ws.element_size(), stream)
+    index = device.index
+    if workspace is None:
+        need = _head_need(sizes, index)
+        workspace = torch.empty(need or 16, dtype=torch.uint8, device=device)
     else:
-        with torch.cuda.device(device):
-            status = fn(*args, _ptr(ws), ws.numel() * ws.element_size(), stream)
-    _check(status, name)
+        if workspace.device != device:
+            raise ValueError(f"head loss: workspace on {workspace.device}, tensors on {device}")
+        need = workspace.numel() * workspace.element_size()
+    fn, stream = getattr(lib(), name), torch._C._cuda_getCurrentRawStream(index)
+    if torch.cuda.current_device() == index:
+        status = fn(*args, _ptr(workspace), need, stream)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _ptr(workspace), need, stream)
+    if status != OK:
+        raise TbnError(status, name)
 
 
 def _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype):
@@ -581,7 +600,7 @@ def tbn_linear_xent_fwd(x: torch.Tensor, weight: torch.Tensor, targets: torch.Te
     T, d, V, dt = _head_check(x, weight, bias, targets)
     loss = torch.empty(T, dtype=torch.float32, device=x.device)
     lse = torch.empty(T, dtype=torch.float32, device=x.device)
-    _head_call("tbn_linear_xent_fwd", x.device, tbn_linear_xent_workspace_bytes(T, d, V, dt, False), workspace, _ptr(x), _ptr(weight), dt,
+    _head_call("tbn_linear_xent_fwd", x.device, (T, d, V, dt, False), workspace, _ptr(x), _ptr(weight), dt,
                T, d, V, _ptr(bias), _ptr(targets), ignore_index, _ptr(loss), _ptr(lse))
     return loss, lse
 
@@ -593,7 +612,7 @@ def tbn_linear_xent_bwd(x: torch.Tensor, weight: torch.Tensor, targets: torch.Te
     dw_dtype: F32 gives the G that tbn_tile_bwd takes; by default dw has the weight's type."""
     T, d, V, dt = _head_check(x, weight, bias, targets, (lse, dloss))
     dx, dw, wd, db = _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype)
-    _head_call("tbn_linear_xent_bwd", x.device, tbn_linear_xent_workspace_bytes(T, d, V, dt, True), workspace, _ptr(x), _ptr(weight), dt,
+    _head_call("tbn_linear_xent_bwd", x.device, (T, d, V, dt, True), workspace, _ptr(x), _ptr(weight), dt,
                T, d, V, _ptr(bias), _ptr(targets), ignore_index, _ptr(lse), _ptr(dloss), _ptr(dx), _ptr(dw), wd, _ptr(db))
     return dx, dw, db
 
@@ -605,7 +624,7 @@ def tbn_linear_distill_fwd(x: torch.Tensor, weight: torch.Tensor, top_index: tor
     K = top_index.shape[1]
     loss = torch.empty(T, dtype=torch.float32, device=x.device)
     lse = torch.empty(T, dtype=torch.float32, device=x.device)
-    _head_call("tbn_linear_distill_fwd", x.device, tbn_linear_distill_workspace_bytes(T, d, V, dt, K, False), workspace, _ptr(x),
+    _head_call("tbn_linear_distill_fwd", x.device, (T, d, V, dt, K, False), workspace, _ptr(x),
                _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit), _dtype_code(top_logit), K, temperature, _ptr(loss),
                _ptr(lse))
     return loss, lse
@@ -619,7 +638,7 @@ def tbn_linear_distill_bwd(x: torch.Tensor, weight: torch.Tensor, top_index: tor
     T, d, V, dt = _head_check(x, weight, bias, top_index, (lse, dloss), top_logit)
     K = top_index.shape[1]
     dx, dw, wd, db = _head_outputs(x, weight, need_dx, need_dw, need_dbias, dw_dtype)
-    _head_call("tbn_linear_distill_bwd", x.device, tbn_linear_distill_workspace_bytes(T, d, V, dt, K, True), workspace, _ptr(x),
+    _head_call("tbn_linear_distill_bwd", x.device, (T, d, V, dt, K, True), workspace, _ptr(x),
                _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit), _dtype_code(top_logit), K, temperature, _ptr(lse),
                _ptr(dloss), _ptr(dx), _ptr(dw), wd, _ptr(db))
     return dx, dw, db

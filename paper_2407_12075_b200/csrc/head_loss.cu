@@ -324,7 +324,18 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
                 continue;
             }
             uint16_t *dst = a.xc + (int64_t)to * a.ld;
-            for (int32_t c = lane * 8; c < a.ld; c += 256) pack8(x + from * a.d, c, a.d, sx, dst + c, dst + plane + c);
+            const TS *src = x + from * a.d;
+            int32_t c = lane * 8;
+            if (sizeof(TS) == 2 && a.d % 8 == 0) {     // four pieces in flight
+                for (; c + 3 * 256 + 8 <= a.d; c += 1024) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = __ldg(reinterpret_cast<const uint4 *>(src + c + k * 256));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4 *>(dst + c + k * 256) = v[k];
+                }
+            }
+            for (; c < a.ld; c += 256) pack8(src, c, a.d, sx, dst + c, dst + plane + c);
         }
     }
     if (blockIdx.x == a.row_blocks - 1) {
@@ -559,7 +570,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.pieces = (int32_t)((Vpad + width - 1) / width);
         p.width = (int32_t)round_up64((Vpad + p.pieces - 1) / p.pieces, kTile);
         p.pieces = (int32_t)((Vpad + p.width - 1) / p.width);
-        p.bn = classes_per_tile(T, V < p.width ? V : p.width, p.cols, 128, 128);
+        p.bn = classes_per_tile(T, V < p.width ? V : p.width, p.cols, 128, 64);       // whole chunks of 32 classes per warp
         // A contraction is split when its few tiles would outlast the rest of the launch.  A split adds its share of the
         // fp32 partial sums, written here and read by the pass that joins them: 8 bytes per element and split at a few
         // TB/s, about 1 step per 2 M elements.  A tile costs about 6 steps beside its products, 2 of the three-product form.

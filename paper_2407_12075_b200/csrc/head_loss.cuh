@@ -51,7 +51,7 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const int32_t *n_live;                 // null: the T rows in their own order (forward)
     const RowInfo *rows;                   // null with n_live
     Labels labels;                         // used without rows
-    int32_t bn;                            // classes of a tile: a multiple of 32 up to 256 (backward: 128 or 256)
+    int32_t bn;                            // classes of a tile: a multiple of 32 up to 256 (backward: of 32 per epilogue warp)
     const Scales *scales;                  // null: all 1
     const float *bias;                     // V or null
     float scale2;                          // log2(e) / tau

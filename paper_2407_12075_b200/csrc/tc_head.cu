@@ -777,8 +777,8 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
 #pragma unroll 1
                 for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
-                    if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32;
+                    if (ch * 32 >= hc || c0 >= p.l.ldz) continue;
                     float v[32];
                     load_chunk(ch, v);
                     scale_shift<BIAS>(v, sc, -info.lse2, reinterpret_cast<const float4 *>(bias_s + ch * 32));
