@@ -168,8 +168,8 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *     dz[t][v] = dloss[t] * tau * (q[t][v] - sum_{j: top_index[t][j] = v} p[t][j])       (cross entropy: one entry, p = 1, tau = 1)
  *     dx[t][i] = sum_v dz[t][v] w[v][i],   dw[v][i] = sum_t dz[t][v] x[t][i],   dbias[v] = sum_t dz[t][v]
  *   dx: T x in_f of `dtype`, or NULL.  dw: vocab x in_f of dw_dtype (TBN_F32: what tbn_tile_bwd takes as G; TBN_BF16), or
- *   NULL.  dbias: vocab floats or NULL.  All are overwritten.  With bf16 operands dz is rounded to bf16 for the two products
- *   (dbias is summed before that rounding); sums are fp32.
+ *   NULL.  dbias: vocab floats or NULL.  All are overwritten; none may overlap an input or the workspace.  With bf16 operands
+ *   dz is rounded to bf16 for the two products (dbias is summed before that rounding); sums are fp32.
  * workspace: tbn_linear_xent_workspace_bytes(..., backward) / tbn_linear_distill_workspace_bytes(..., backward) bytes, with
  *   backward = 0 or 1 for the call it is meant for.  T == 0: the forward is a no-op, the backward writes zeros to dw and dbias.
  * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1024: TBN_ERR_UNSUPPORTED.

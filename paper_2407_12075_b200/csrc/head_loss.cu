@@ -132,7 +132,8 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
 }
 
 // ---- fp32 operands: largest magnitudes ------------------------------------------------------------------
-// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows.
+// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows, of the finite
+// ones: an infinity must not change how the other tokens are rounded.
 constexpr int kMaxBlocks = 592;
 
 __device__ __forceinline__ float block_max(float v) {
@@ -143,8 +144,12 @@ __device__ __forceinline__ float block_max(float v) {
     __syncthreads();
     return warp_max(part[threadIdx.x & 7]);
 }
+__device__ __forceinline__ float max_finite(float m, float v) {
+    v = fabsf(v);
+    return v < INFINITY ? fmaxf(m, v) : m;
+}
 __device__ __forceinline__ float max4(float m, float4 v) {
-    return fmaxf(fmaxf(m, fmaxf(fabsf(v.x), fabsf(v.y))), fmaxf(fabsf(v.z), fabsf(v.w)));
+    return max_finite(max_finite(max_finite(max_finite(m, v.x), v.y), v.z), v.w);
 }
 __global__ void __launch_bounds__(256)
 abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d, const float *__restrict__ w, int64_t w_count,
@@ -162,12 +167,12 @@ abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d,
         mw = max4(max4(max4(max4(mw, v0), v1), v2), v3);
     }
     for (; i < w4; i += threads) mw = max4(mw, __ldg(wv + i));
-    for (i = (w4 << 2) + tid; i < w_count; i += threads) mw = fmaxf(mw, fabsf(w[i]));
+    for (i = (w4 << 2) + tid; i < w_count; i += threads) mw = max_finite(mw, w[i]);
     const int lane = threadIdx.x & 31;
     for (int64_t t = tid >> 5; t < T; t += threads >> 5) {
         if (!labels.live(t)) continue;
-        for (int32_t c = lane; c < d; c += 32) mx = fmaxf(mx, fabsf(x[t * d + c]));
-        if (dloss && lane == 0) mg = fmaxf(mg, fabsf(dloss[t] * tau));
+        for (int32_t c = lane; c < d; c += 32) mx = max_finite(mx, x[t * d + c]);
+        if (dloss && lane == 0) mg = max_finite(mg, dloss[t] * tau);
     }
     __syncwarp();
     mx = block_max(mx);
@@ -180,9 +185,9 @@ abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d,
     }
 }
 // The power of two that takes the largest magnitude to [2^14, 2^15): the high part of every element then keeps 11 bits
-// and the remainder another 11, down to 2^-39 of the largest one, below which fp16 ends.  Infinite or zero: 1.
+// and the remainder another 11, down to 2^-39 of the largest one, below which fp16 ends.  All zero: 1.
 __device__ __forceinline__ float scale_of(float m) {
-    if (!(m > 0.0f) || !(m < INFINITY)) return 1.0f;
+    if (!(m > 0.0f)) return 1.0f;
     int e = (int)(__float_as_uint(m) >> 23) - 127;     // subnormal maxima: -127, clamped below
     e = e > 60 ? 60 : e < -60 ? -60 : e;
     return __uint_as_float((unsigned int)(127 + 14 - e) << 23);
