@@ -26,14 +26,6 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr size_t kPieceBytes = (size_t)256 << 20;      // bound on one piece of dz (a piece has at least 1024 classes)
 
-// ---- the teacher's entries ---------------------------------------------------------------------------
-// One warp per token: p = softmax(logit / tau) over the entries whose index is a class and whose logit is above
-// -infinity, sum p log p, and the entries sorted by class (by position among equals), which is the order in which the
-// epilogues meet the classes.
-constexpr int kMaxUnits = 2046;                        // of a list_start row: 4 KB per warp
-inline int teacher_warps(int32_t Kp) { return Kp <= 512 ? 4 : 2; }
-inline size_t teacher_smem(int32_t Kp, int32_t pitch) { return (size_t)Kp * 12 + (size_t)pitch * 2; }      // per warp
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -45,11 +37,91 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
+// ---- fp32 operands: largest magnitudes ------------------------------------------------------------------
+// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows, of the finite
+// ones: an infinity must not change how the other tokens are rounded.
+constexpr int kMaxBlocks = 592;
+
+struct MaxArgs {
+    const float *x, *w, *dloss;            // dloss: backward
+    int64_t T, w_count;
+    int32_t d;
+    float tau;
+    float *max_part;
+    unsigned int blocks;
+};
+__device__ __forceinline__ float block_max(float v) {
+    __shared__ float part[8];
+    v = warp_max(v);
+    __syncthreads();
+    if (threadIdx.x < 8) part[threadIdx.x] = 0.0f;
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return warp_max(part[threadIdx.x & 7]);
+}
+__device__ __forceinline__ float max_finite(float m, float v) {
+    v = fabsf(v);
+    return v < INFINITY ? fmaxf(m, v) : m;
+}
+__device__ __forceinline__ float max4(float m, float4 v) {
+    return max_finite(max_finite(max_finite(max_finite(m, v.x), v.y), v.z), v.w);
+}
+// Run by block `block` of a.blocks; live(t) is asked by whole warps.
+template <typename Live>
+__device__ __forceinline__ void abs_max(const MaxArgs &a, unsigned int block, Live live)
+{
+    const int64_t tid = (int64_t)block * blockDim.x + threadIdx.x, threads = (int64_t)a.blocks * blockDim.x;
+    float mw = 0.0f, mx = 0.0f, mg = 0.0f;
+    const int64_t w4 = a.w_count >> 2;
+    const float4 *wv = reinterpret_cast<const float4 *>(a.w);
+    int64_t i = tid;
+    for (; i + 3 * threads < w4; i += 4 * threads) {
+        const float4 v0 = __ldg(wv + i), v1 = __ldg(wv + i + threads), v2 = __ldg(wv + i + 2 * threads), v3 = __ldg(wv + i + 3 * threads);
+        mw = max4(max4(max4(max4(mw, v0), v1), v2), v3);
+    }
+    for (; i < w4; i += threads) mw = max4(mw, __ldg(wv + i));
+    for (i = (w4 << 2) + tid; i < a.w_count; i += threads) mw = max_finite(mw, a.w[i]);
+    __syncwarp();
+    const int lane = threadIdx.x & 31;
+    for (int64_t t = tid >> 5; t < a.T; t += threads >> 5) {
+        if (!live(t)) continue;
+#pragma unroll 4
+        for (int32_t c = lane; c < a.d; c += 32) mx = max_finite(mx, a.x[t * a.d + c]);
+        if (a.dloss && lane == 0) mg = max_finite(mg, a.dloss[t] * a.tau);
+        __syncwarp();
+    }
+    mx = block_max(mx);
+    mw = block_max(mw);
+    mg = block_max(mg);
+    if (threadIdx.x == 0) {
+        a.max_part[block] = mx;
+        a.max_part[kMaxBlocks + block] = mw;
+        a.max_part[2 * kMaxBlocks + block] = mg;
+    }
+}
+__global__ void __launch_bounds__(256)
+abs_max_kernel(const MaxArgs a, const Labels labels)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    abs_max(a, blockIdx.x, [&](int64_t t) { return labels.live(t); });
+}
+
+// ---- the teacher's entries ---------------------------------------------------------------------------
+// One warp per token: p = softmax(logit / tau) over the entries whose index is a class and whose logit is above
+// -infinity, sum p log p, and the entries sorted by class (by position among equals), which is the order in which the
+// epilogues meet the classes.
+constexpr int kMaxUnits = 2046;                        // of a list_start row: 4 KB per warp
+inline int teacher_warps(int32_t Kp) { return Kp <= 512 ? 4 : 2; }
+inline size_t teacher_smem(int32_t Kp, int32_t pitch) { return (size_t)Kp * 12 + (size_t)pitch * 2; }      // per warp
+
 template <typename TL>
 __global__ void __launch_bounds__(128)
 teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, int64_t T, int32_t K, int32_t Kp, int32_t V,
                float inv_tau, int32_t unit, int32_t units, int32_t pitch, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
-               uint8_t *__restrict__ flags, float2 *__restrict__ stats)
+               uint8_t *__restrict__ flags, float2 *__restrict__ stats,
+               unsigned int list_blocks, const MaxArgs max_args)
 {
     extern __shared__ __align__(16) uint8_t teacher_mem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -59,6 +131,17 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     uint16_t *start = reinterpret_cast<uint16_t *>(teacher_mem + (size_t)warps * Kp * 12) + (size_t)warp * pitch;
     pdl_launch_dependents();
     pdl_wait();
+    if (blockIdx.x >= list_blocks) {                   // fp32 operands: the blocks behind look for the largest magnitudes
+        abs_max(max_args, blockIdx.x - list_blocks, [&](int64_t row) {
+            bool some = false;
+            for (int32_t j = lane; j < K; j += 32) {
+                const int64_t c = index[row * K + j];
+                some |= c >= 0 && c < V && !(load_as_float(logit, row * K + j) == -INFINITY);
+            }
+            return __any_sync(0xffffffffu, some) != 0;
+        });
+        return;
+    }
     const int64_t t = (int64_t)blockIdx.x * warps + warp;
     if (t >= T) return;
     float top = -INFINITY;
@@ -131,59 +214,6 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     }
 }
 
-// ---- fp32 operands: largest magnitudes ------------------------------------------------------------------
-// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows, of the finite
-// ones: an infinity must not change how the other tokens are rounded.
-constexpr int kMaxBlocks = 592;
-
-__device__ __forceinline__ float block_max(float v) {
-    __shared__ float part[8];
-    v = warp_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return warp_max(part[threadIdx.x & 7]);
-}
-__device__ __forceinline__ float max_finite(float m, float v) {
-    v = fabsf(v);
-    return v < INFINITY ? fmaxf(m, v) : m;
-}
-__device__ __forceinline__ float max4(float m, float4 v) {
-    return max_finite(max_finite(max_finite(max_finite(m, v.x), v.y), v.z), v.w);
-}
-__global__ void __launch_bounds__(256)
-abs_max_kernel(const float *__restrict__ x, Labels labels, int64_t T, int32_t d, const float *__restrict__ w, int64_t w_count,
-               const float *__restrict__ dloss, float tau, float *__restrict__ max_part)
-{
-    pdl_launch_dependents();
-    pdl_wait();
-    const int64_t tid = (int64_t)blockIdx.x * 256 + threadIdx.x, threads = (int64_t)gridDim.x * 256;
-    float mw = 0.0f, mx = 0.0f, mg = 0.0f;
-    const int64_t w4 = w_count >> 2;
-    const float4 *wv = reinterpret_cast<const float4 *>(w);
-    int64_t i = tid;
-    for (; i + 3 * threads < w4; i += 4 * threads) {
-        const float4 v0 = __ldg(wv + i), v1 = __ldg(wv + i + threads), v2 = __ldg(wv + i + 2 * threads), v3 = __ldg(wv + i + 3 * threads);
-        mw = max4(max4(max4(max4(mw, v0), v1), v2), v3);
-    }
-    for (; i < w4; i += threads) mw = max4(mw, __ldg(wv + i));
-    for (i = (w4 << 2) + tid; i < w_count; i += threads) mw = max_finite(mw, w[i]);
-    const int lane = threadIdx.x & 31;
-    for (int64_t t = tid >> 5; t < T; t += threads >> 5) {
-        if (!labels.live(t)) continue;
-        for (int32_t c = lane; c < d; c += 32) mx = max_finite(mx, x[t * d + c]);
-        if (dloss && lane == 0) mg = max_finite(mg, dloss[t] * tau);
-    }
-    __syncwarp();
-    mx = block_max(mx);
-    mw = block_max(mw);
-    mg = block_max(mg);
-    if (threadIdx.x == 0) {
-        max_part[blockIdx.x] = mx;
-        max_part[kMaxBlocks + blockIdx.x] = mw;
-        max_part[2 * kMaxBlocks + blockIdx.x] = mg;
-    }
-}
 // The power of two that takes the largest magnitude to [2^14, 2^15): the high part of every element then keeps 11 bits
 // and the remainder another 11, down to 2^-39 of the largest one, below which fp16 ends.  All zero: 1.
 __device__ __forceinline__ float scale_of(float m) {
@@ -252,6 +282,29 @@ __device__ __forceinline__ void pack8(const TS *__restrict__ src, int32_t c, int
     if (sizeof(TS) == 4) *reinterpret_cast<uint4 *>(lo_dst) = *reinterpret_cast<const uint4 *>(lo);
 }
 
+// A whole row by a warp, lane = column: for rows that are not a multiple of 16 bytes.
+template <typename TS>
+__device__ __forceinline__ void pack_row(const TS *__restrict__ src, int32_t d, int32_t ld, float scale, int lane, uint16_t *hi_dst, uint16_t *lo_dst) {
+    for (int32_t c0 = lane; c0 < ld; c0 += 256) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c0 + 32 * j < d ? load_as_float(src, c0 + 32 * j) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int32_t c = c0 + 32 * j;
+            if (c >= ld) break;
+            if (sizeof(TS) == 4) {
+                __half h, l;
+                split16(v[j] * scale, h, l);
+                hi_dst[c] = __half_as_ushort(h);
+                lo_dst[c] = __half_as_ushort(l);
+            } else {
+                hi_dst[c] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+            }
+        }
+    }
+}
+
 template <typename TS>
 __global__ void __launch_bounds__(256)
 pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a)
@@ -263,12 +316,25 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     pdl_wait();
     float m[3] = {0.0f, 0.0f, 0.0f};
     if (sizeof(TS) == 4) {
-        for (int k = 0; k < 3; ++k) {
-            for (int i = threadIdx.x; i < a.max_blocks; i += 256) m[k] = fmaxf(m[k], a.max_part[k * kMaxBlocks + i]);
-            m[k] = block_max(m[k]);
+#pragma unroll
+        for (int u = 0; u < (kMaxBlocks + 255) / 256; ++u) {
+            const int i = u * 256 + threadIdx.x;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) m[k] = fmaxf(m[k], i < a.max_blocks ? a.max_part[k * kMaxBlocks + i] : 0.0f);
         }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) m[k] = block_max(m[k]);
     }
     const float sx = scale_of(m[0]), sw = scale_of(m[1]), sg = scale_of(m[2]);
+    constexpr int kVec = 16 / sizeof(TS);              // rows in whole 16-byte pieces
+    if (blockIdx.x >= a.row_blocks && a.d % kVec != 0) {
+        const int64_t plane = (int64_t)a.V * a.ld;
+        for (int64_t r = (int64_t)(blockIdx.x - a.row_blocks) * 8 + warp; r < a.V; r += (int64_t)(gridDim.x - a.row_blocks) * 8) {
+            uint16_t *dst = a.wc + r * a.ld;
+            pack_row(w + r * a.d, a.d, a.ld, sw, lane, dst, dst + plane);
+        }
+        return;
+    }
     if (blockIdx.x >= a.row_blocks) {                  // weights
         const int64_t vecs = a.ld >> 3, groups = a.V * vecs, plane = (int64_t)a.V * a.ld;
         const int64_t stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
@@ -330,8 +396,12 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
             }
             uint16_t *dst = a.xc + (int64_t)to * a.ld;
             const TS *src = x + from * a.d;
+            if (a.d % kVec != 0) {
+                pack_row(src, a.d, a.ld, sx, lane, dst, dst + plane);
+                continue;
+            }
             int32_t c = lane * 8;
-            if (sizeof(TS) == 2 && a.d % 8 == 0) {     // four pieces in flight
+            if (sizeof(TS) == 2) {     // four pieces in flight
                 for (; c + 3 * 256 + 8 <= a.d; c += 1024) {
                     uint4 v[4];
 #pragma unroll
@@ -626,22 +696,29 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     RowInfo *rows = reinterpret_cast<RowInfo *>(ws + p.o_rows);
     const bool f32 = c.dtype == TBN_F32;
     Labels labels = {c.targets, c.ignore_index, c.V, nullptr};
+    MaxArgs max_args = {};
+    if (f32) {
+        const int64_t count = (int64_t)c.V * c.d, most = count > c.T * c.d ? count : c.T * c.d;
+        max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T, count, c.d, c.tau,
+                           max_part, blocks_for(most, 4096, kMaxBlocks)};
+    }
 
     if (c.K > 0) {
         int32_t Kp = 32;
         while (Kp < c.K) Kp <<= 1;
         const int warps = teacher_warps(Kp);
         const size_t smem = teacher_smem(Kp, p.pitch) * warps;
-        const dim3 grid((unsigned)((c.T + warps - 1) / warps));
+        const unsigned list_blocks = (unsigned)((c.T + warps - 1) / warps);
+        const dim3 grid(list_blocks + max_args.blocks);
         int2 *list = reinterpret_cast<int2 *>(ws + p.o_list);
         uint8_t *flags = reinterpret_cast<uint8_t *>(ws + p.o_flags);
         float2 *stats = reinterpret_cast<float2 *>(ws + p.o_teacher);
         uint16_t *start = reinterpret_cast<uint16_t *>(ws + p.o_start);
         const cudaError_t e = c.top_dtype == TBN_F32
             ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * warps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
-                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats)
+                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats, list_blocks, max_args)
             : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * warps), smem, s, c.top_index,
-                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats);
+                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats, list_blocks, max_args);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
@@ -663,13 +740,8 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         return TBN_OK;
     }
     PackArgs a = {};
-    if (f32) {
-        const int64_t count = (int64_t)c.V * c.d;
-        a.max_blocks = (int32_t)blocks_for(count > c.T * c.d ? count : c.T * c.d, 4096, kMaxBlocks);
-        if (launch_pdl(abs_max_kernel, dim3((unsigned)a.max_blocks), dim3(256), 0, s, static_cast<const float *>(c.x), labels, c.T, c.d,
-                       static_cast<const float *>(c.w), count, backward ? c.dloss : nullptr, c.tau, max_part) != cudaSuccess)
-            return TBN_ERR_CUDA;
-    }
+    a.max_blocks = (int32_t)max_args.blocks;
+    if (f32 && c.K == 0 && launch_pdl(abs_max_kernel, dim3(max_args.blocks), dim3(256), 0, s, max_args, labels) != cudaSuccess) return TBN_ERR_CUDA;
     a.labels = labels; a.T = c.T; a.Tpad = p.Tpad; a.V = c.V; a.d = c.d; a.ld = p.ld;
     a.per_block = (c.T + 591) / 592 < 8 ? 8 : (c.T + 591) / 592;
     a.row_blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);              // the last one has rows of its own
