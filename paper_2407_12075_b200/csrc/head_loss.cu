@@ -498,21 +498,27 @@ struct FinishArgs {
     unsigned int bias_blocks, dw_blocks, dx_blocks;
     // rows of dw and dx: the sums of their splits
     const float *dw_slots, *dx_slots;
-    int32_t dw_splits, dx_splits, d, dw_bf16, dx_bf16;
+    int32_t dw_splits, dx_splits, d, ld, dw_bf16, dx_bf16;
     int64_t dw_slot_rows, dx_slot_rows;
     void *dw, *dx;                         // dw: the piece's first row
 };
-__device__ __forceinline__ void join_splits(const float *slots, int32_t splits, int64_t slot_rows, int32_t d, int64_t n, const RowInfo *rows,
-                                            void *out, int bf16, int64_t first, int64_t stride) {
-    const int64_t total = n * d, split_stride = slot_rows * d;
-    if (d % 4 == 0) {
-        for (int64_t i = first * 4; i < total; i += stride * 4) {
-            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int k = 0; k < splits; ++k) {
-                const float4 v = *reinterpret_cast<const float4 *>(slots + k * split_stride + i);
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-            }
-            const int64_t r = i / d, at = (rows ? (int64_t)rows[r].row : r) * d + (i - r * d);
+// The sums of the splits' rows, four columns per thread.  Flat over all of them: the rows are few, and a warp per row has too
+// few loads in flight (13 us where this takes 5).
+__device__ __forceinline__ void join_splits(const float *slots, int32_t splits, int64_t slot_rows, int32_t d, int32_t ld, int64_t n,
+                                            const RowInfo *rows, void *out, int bf16, int64_t first, int64_t stride) {
+    const int64_t per_row = (d + 3) / 4, total = n * per_row, split_stride = slot_rows * ld;
+    for (int64_t i = first; i < total; i += stride) {
+        const int64_t r = total <= 0x7fffffff ? (int64_t)((uint32_t)i / (uint32_t)per_row) : i / per_row;
+        const int32_t c = (int32_t)(i - r * per_row) * 4;
+        const float *src = slots + r * ld + c;         // a slot's rows are padded: whole pieces of four
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k) {
+            const float4 v = *reinterpret_cast<const float4 *>(src + k * split_stride);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const int64_t at = (rows ? (int64_t)rows[r].row : r) * d + c;
+        if (d % 4 == 0) {
             if (bf16) {
                 const __nv_bfloat162 lo = __floats2bfloat162_rn(s.x, s.y), hi = __floats2bfloat162_rn(s.z, s.w);
                 *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(out) + at) =
@@ -520,15 +526,15 @@ __device__ __forceinline__ void join_splits(const float *slots, int32_t splits, 
             } else {
                 *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = s;
             }
+        } else {
+            const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (c + j >= d) break;
+                if (bf16) static_cast<__nv_bfloat16 *>(out)[at + j] = __float2bfloat16_rn(v[j]);
+                else static_cast<float *>(out)[at + j] = v[j];
+            }
         }
-        return;
-    }
-    for (int64_t i = first; i < total; i += stride) {
-        float s = 0.0f;
-        for (int k = 0; k < splits; ++k) s += slots[k * split_stride + i];
-        const int64_t r = i / d, at = (rows ? (int64_t)rows[r].row : r) * d + (i - r * d);
-        if (bf16) static_cast<__nv_bfloat16 *>(out)[at] = __float2bfloat16_rn(s);
-        else static_cast<float *>(out)[at] = s;
     }
 }
 __global__ void __launch_bounds__(256)
@@ -554,12 +560,12 @@ finish_kernel(const FinishArgs a)
     }
     b -= a.bias_blocks;
     if (b < a.dw_blocks) {
-        join_splits(a.dw_slots, a.dw_splits, a.dw_slot_rows, a.d, a.width, nullptr, a.dw, a.dw_bf16, (int64_t)b * 256 + threadIdx.x,
+        join_splits(a.dw_slots, a.dw_splits, a.dw_slot_rows, a.d, a.ld, a.width, nullptr, a.dw, a.dw_bf16, (int64_t)b * 256 + threadIdx.x,
                     (int64_t)a.dw_blocks * 256);
         return;
     }
     b -= a.dw_blocks;
-    join_splits(a.dx_slots, a.dx_splits, a.dx_slot_rows, a.d, *a.n_live, a.rows, a.dx, a.dx_bf16, (int64_t)b * 256 + threadIdx.x,
+    join_splits(a.dx_slots, a.dx_splits, a.dx_slot_rows, a.d, a.ld, *a.n_live, a.rows, a.dx, a.dx_bf16, (int64_t)b * 256 + threadIdx.x,
                 (int64_t)a.dx_blocks * 256);
 }
 
@@ -667,8 +673,8 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.dw_slots = p.dw_splits > 1;
         p.o_dz = take((size_t)p.planes * p.Tpad * p.width * 2);
         p.o_col = take((size_t)(p.Tpad / 32) * p.width * 4);
-        p.o_dx = take(p.dx_slots ? (size_t)p.dx_splits * p.Tpad * d * 4 : 0);
-        p.o_dw = take(p.dw_slots ? (size_t)p.dw_splits * p.width * d * 4 : 0);
+        p.o_dx = take(p.dx_slots ? (size_t)p.dx_splits * p.Tpad * p.ld * 4 : 0);
+        p.o_dw = take(p.dw_slots ? (size_t)p.dw_splits * p.width * p.ld * 4 : 0);
     }
     if (K > 0) {
         p.unit = p.bn / groups;
@@ -809,6 +815,7 @@ int backward(const HeadCall &c, void *workspace, cudaStream_t s)
     g.dx = c.dx; g.dx_bf16 = dx_bf16; g.dx_slots = p.dx_slots ? reinterpret_cast<float *>(ws + p.o_dx) : nullptr; g.dx_splits = p.dx_splits;
     g.dw = c.dw; g.dw_bf16 = c.dw_dtype == TBN_BF16; g.dw_slots = p.dw_slots ? reinterpret_cast<float *>(ws + p.o_dw) : nullptr;
     g.dw_splits = p.dw_splits;
+    g.slot_ld = p.ld;
     g.status = c.status;
     for (int32_t piece = 0; piece < p.pieces; ++piece) {
         a.v0 = piece * p.width;
@@ -824,7 +831,7 @@ int backward(const HeadCall &c, void *workspace, cudaStream_t s)
             if (rc != TBN_OK) return rc;
         }
         FinishArgs f = {};
-        f.n_live = a.n_live; f.rows = a.rows; f.scales = a.scales; f.d = c.d; f.width = a.width;
+        f.n_live = a.n_live; f.rows = a.rows; f.scales = a.scales; f.d = c.d; f.ld = p.ld; f.width = a.width;
         if (c.db) {
             f.col_part = a.col_part; f.ldz = a.ldz; f.db = c.db + a.v0;
             f.bias_blocks = (unsigned)((a.width + 31) / 32);

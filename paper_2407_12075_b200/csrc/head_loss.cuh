@@ -82,17 +82,18 @@ struct GradArgs {                          // dX (+)= dz W, dW = dz^T X for one 
     int64_t T, Tpad;
     int32_t d, V, v0, width, ldz;
     bool want_dx, want_dw;
-    // dX: into `dx` by row when no slots are used, else fp32 partial sums [split][Tpad][d], added to when `dx_add`
+    // dX: into `dx` by row when no slots are used, else fp32 partial sums [split][Tpad][slot_ld], added to when `dx_add`
     void *dx;
     int dx_bf16;
     float *dx_slots;
     int32_t dx_splits;
     int dx_add, dx_last;                   // dx_last: this piece is the last one (without splits it finishes dx)
-    // dW: rows v0 .. of `dw`, or fp32 partial sums [split][round_up(width, 256)][d]
+    // dW: rows v0 .. of `dw`, or fp32 partial sums [split][round_up(width, 256)][slot_ld]
     void *dw;
     int dw_bf16;
     float *dw_slots;
     int32_t dw_splits;
+    int32_t slot_ld;                       // d in whole panels of 64
     int *status;
 };
 int launch_head_grads(const GradArgs &a, cudaStream_t s);

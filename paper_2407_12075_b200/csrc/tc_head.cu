@@ -107,7 +107,7 @@ struct GradParams {
     int32_t dx_splits, dx_bf16, dx_add, dx_last;
     void *dw;
     float *dw_slots;
-    int32_t dw_splits, dw_bf16;
+    int32_t dw_splits, dw_bf16, slot_ld;
 };
 struct KernelParams { LogitsParams l; GradParams g; int *status; };
 
@@ -371,9 +371,10 @@ __device__ __forceinline__ void ld_global_v8(const float *ptr, float (&v)[8]) {
 struct RowsOut {
     void *out;
     const float *prev;
-    int32_t row, prev_row, rows_in, d, end;          // end: the first column that is not this warp's
+    int32_t row, prev_row, ld, prev_ld, rows_in, end;      // end: the first column that is not this warp's
 };
-// 32 columns of every lane's row, in whole 32-byte sectors (d a multiple of 16, out 32-byte aligned).
+// 32 columns of every lane's row, in whole 32-byte sectors (rows a multiple of 16 elements, 32-byte aligned).  The columns
+// behind end are not written, but for those of the padding of a slot's row.
 __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_t c0, bool out_bf16, float (&v)[32])
 {
     if (lane >= o.rows_in) return;
@@ -382,12 +383,12 @@ __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_
         for (int q = 0; q < 4; ++q) {
             if (c0 + 8 * q >= o.end) break;
             float w[8];
-            ld_global_v8(o.prev + (int64_t)o.prev_row * o.d + c0 + 8 * q, w);
+            ld_global_v8(o.prev + (int64_t)o.prev_row * o.prev_ld + c0 + 8 * q, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[8 * q + j] += w[j];
         }
     }
-    const int64_t at = (int64_t)o.row * o.d + c0;
+    const int64_t at = (int64_t)o.row * o.ld + c0;
     if (out_bf16) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -436,13 +437,13 @@ __device__ __forceinline__ void write_elements(const RowsOut &o, uint32_t exchan
                 to[k] = __shfl_sync(0xffffffffu, o.row, r);
                 if (o.prev) {
                     const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
-                    if (r < o.rows_in && c < o.end) x[k] += o.prev[(int64_t)from * o.d + c];
+                    if (r < o.rows_in && c < o.end) x[k] += o.prev[(int64_t)from * o.prev_ld + c];
                 }
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 if (part * 16 + h + k < o.rows_in && c < o.end) {
-                    const int64_t at = (int64_t)to[k] * o.d + c;
+                    const int64_t at = (int64_t)to[k] * o.ld + c;
                     if (out_bf16) static_cast<__nv_bfloat16 *>(o.out)[at] = __float2bfloat16_rn(x[k]);
                     else static_cast<float *>(o.out)[at] = x[k];
                 }
@@ -835,16 +836,18 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const int32_t rows_in = (is_dx ? n_live : g.width) - row0;             // rows of this warp that exist
                 const int splits = is_dx ? g.dx_splits : g.dw_splits;
                 float *slot = is_dx ? g.dx_slots : g.dw_slots;
-                if (slot) slot += ((int64_t)t.split * (is_dx ? g.Tpad : round_up64(g.width, kTile)) + row0) * g.d;
+                if (slot) slot += ((int64_t)t.split * (is_dx ? g.Tpad : round_up64(g.width, kTile)) + row0) * g.slot_ld;
                 const bool to_slot = slot != nullptr && (splits > 1 || !(is_dx && g.dx_last));
                 RowsOut o;
                 o.out = to_slot ? static_cast<void *>(slot) : is_dx ? g.dx : g.dw;
                 o.row = to_slot ? lane : is_dx ? info.row : g.v0 + row0 + lane;
                 o.prev = !(is_dx && g.dx_add) ? nullptr : slot ? slot : static_cast<const float *>(g.dx);
                 o.prev_row = slot ? lane : info.row;
-                o.rows_in = rows_in; o.d = g.d; o.end = min(g.d, col0 + hc);
+                o.ld = to_slot ? g.slot_ld : g.d;
+                o.prev_ld = slot ? g.slot_ld : g.d;
+                o.rows_in = rows_in; o.end = min(to_slot ? g.slot_ld : g.d, col0 + hc);
                 const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16);
-                const bool sectors = g.d % 16 == 0 && (reinterpret_cast<uintptr_t>(o.out) & 31) == 0 && (reinterpret_cast<uintptr_t>(o.prev) & 31) == 0;
+                const bool sectors = o.ld % 16 == 0 && (!o.prev || o.prev_ld % 16 == 0) && (reinterpret_cast<uintptr_t>(o.out) & 31) == 0 && (reinterpret_cast<uintptr_t>(o.prev) & 31) == 0;
 #pragma unroll 1
                 for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
@@ -992,7 +995,7 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
     g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.ldz = a.ldz;
     g.want_dx = a.want_dx; g.want_dw = a.want_dw; g.w_panels = w_panels;
     g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
-    g.dw = a.dw; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;
+    g.dw = a.dw; g.slot_ld = a.slot_ld; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;
     p.status = a.status;
     const int64_t cols = a.planes == 1 ? kCols<1> : kCols<2>, nt = (a.d + cols - 1) / cols;
     const int64_t tiles = (a.want_dx ? (a.T + kTile - 1) / kTile * nt * a.dx_splits : 0) +
