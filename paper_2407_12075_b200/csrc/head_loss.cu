@@ -654,9 +654,11 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.bn = classes_per_tile(T, V < p.width ? V : p.width, p.cols, 128, 64);       // whole chunks of 32 classes per warp
         // A contraction is split when its few tiles would outlast the rest of the launch.  A split adds its share of the
         // fp32 partial sums, written here and read by the pass that joins them: 8 bytes per element and split at a few
-        // TB/s, about 1 step per 2 M elements.  A tile costs about 6 steps beside its products, 2 of the three-product form.
+        // TB/s, about 1 step per 2 M elements.  A tile costs about 10 steps beside its products, 6 of the three-product form's (64 x 512 x
+        // 30000, whole gradient: counted as 6 steps, 14 splits and 68 us; as 12, 9 splits and 59 us; 1024 x 512 x 1000 in fp32:
+        // as 6, 2 + 2 splits and 36.9 us; as 12, none and 38.9 us).
         const int64_t nt = (d + p.cols - 1) / p.cols, mt = p.Tpad / kTile, vt = (V < p.width ? round_up64(V, kTile) : p.width) / kTile;
-        const int64_t kx = p.width / 64, kw = (T + 63) / 64, pairs = sm_count() > 1 ? sm_count() / 2 : 74, own = p.planes == 1 ? 6 : 2;
+        const int64_t kx = p.width / 64, kw = (T + 63) / 64, pairs = sm_count() > 1 ? sm_count() / 2 : 74, own = p.planes == 1 ? 10 : 6;
         int64_t best = INT64_MAX;
         p.dx_splits = p.dw_splits = 1;
         for (int32_t i = 1; i <= kMaxSplits && (i == 1 || 2 * i <= kx); ++i) {
