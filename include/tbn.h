@@ -143,7 +143,7 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *
  *     z[t][v] = sum_i x[t][i] * w[v][i] + bias[v]           v < vocab
  *
- * the logits z are never written to memory as a whole: the forward keeps a maximum and a sum per token and 128 classes,
+ * the logits z are never written to memory as a whole: the forward keeps a maximum and a sum per token and tile of classes,
  * the backward recomputes z and holds its gradient for one piece of the vocabulary at a time.
  *
  * tbn_linear_xent_fwd: softmax cross entropy.
@@ -162,7 +162,8 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *
  * x: T x in_f, w: vocab x in_f, both of `dtype` (TBN_BF16 or TBN_F32).  bias: vocab floats or NULL.  targets: T int64.
  * loss, lse: T floats.  Products are accumulated in fp32; fp32 operands are contracted as two fp16 halves of 11 bits each
- * under a common power of two (about 22 bits of every element, ending at 2^-38 of the tensor's largest magnitude).
+ * under a common power of two (about 22 bits of every element, ending at 2^-38 of the tensor's largest magnitude; dz, in
+ * the backward, under that of the largest tau * |dloss|).
  *
  * tbn_linear_xent_bwd, tbn_linear_distill_bwd: lse as the forward wrote it, dloss: T floats (dL/dloss[t]: 1/T for a mean).
  *     dz[t][v] = dloss[t] * tau * (q[t][v] - sum_{j: top_index[t][j] = v} p[t][j])       (cross entropy: one entry, p = 1, tau = 1)

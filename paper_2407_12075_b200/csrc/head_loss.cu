@@ -575,7 +575,7 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 struct Plan {
     int planes, pack_w;
     int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
-    int32_t unit, units, pitch;                 // classes per entry of list_start: an epilogue warp's, more where that would be a large table
+    int32_t unit, units, pitch;            // classes per entry of list_start: an epilogue warp's, more where that is a large table
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
     bool direct;
     int64_t Tpad;
@@ -584,8 +584,8 @@ struct Plan {
 };
 
 // Classes per tile of a logits launch: the width whose whole rounds over the SM pairs cost least.  A round costs what it
-// stages per 64-element step (the token rows that exist and the classes) plus about 64 rows' worth for its hand-over.  256
-// when there are many rounds, where narrow tiles would only read x more often.
+// stages per 64-element step (the token rows that exist and the classes) plus about 64 rows' worth for its hand-over.  The
+// widest when there are many rounds, where narrow tiles would only read x more often.
 int32_t classes_per_tile(int64_t T, int64_t V, int32_t most, int32_t least, int32_t step)
 {
     const int64_t pairs = sm_count() > 1 ? sm_count() / 2 : 74, mt = (T + kTile - 1) / kTile;
@@ -654,11 +654,12 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.bn = classes_per_tile(T, V < p.width ? V : p.width, p.cols, 128, 64);       // whole chunks of 32 classes per warp
         // A contraction is split when its few tiles would outlast the rest of the launch.  A split adds its share of the
         // fp32 partial sums, written here and read by the pass that joins them: 8 bytes per element and split at a few
-        // TB/s, about 1 step per 2 M elements.  A tile costs about 10 steps beside its products, 6 of the three-product form's (64 x 512 x
-        // 30000, whole gradient: counted as 6 steps, 14 splits and 68 us; as 12, 9 splits and 59 us; 1024 x 512 x 1000 in fp32:
-        // as 6, 2 + 2 splits and 36.9 us; as 12, none and 38.9 us).
+        // TB/s, about 1 step per 2 M elements.  A tile costs about 10 steps beside its products, 6 of the three-product
+        // form's (64 x 512 x 30000, whole gradient: counted as 6 steps, 14 splits and 68 us; as 12, 9 splits and 59 us;
+        // 1024 x 512 x 1000 in fp32: as 6, 2 + 2 splits and 36.9 us; as 12, none and 38.9 us).
         const int64_t nt = (d + p.cols - 1) / p.cols, mt = p.Tpad / kTile, vt = (V < p.width ? round_up64(V, kTile) : p.width) / kTile;
-        const int64_t kx = p.width / 64, kw = (T + 63) / 64, pairs = sm_count() > 1 ? sm_count() / 2 : 74, own = p.planes == 1 ? 10 : 6;
+        const int64_t kx = p.width / 64, kw = (T + 63) / 64, pairs = sm_count() > 1 ? sm_count() / 2 : 74;
+        const int64_t own = p.planes == 1 ? 10 : 6;
         int64_t best = INT64_MAX;
         p.dx_splits = p.dw_splits = 1;
         for (int32_t i = 1; i <= kMaxSplits && (i == 1 || 2 * i <= kx); ++i) {
@@ -680,8 +681,8 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     }
     if (K > 0) {
         p.unit = p.bn / groups;
-        while (V / p.unit >= kMaxUnits || (T * (V / p.unit) > ((int64_t)1 << 26) && p.unit < V)) p.unit *= 2;
-        p.units = (V + p.unit - 1) / p.unit;
+        while (V / p.unit >= kMaxUnits || (T * (V / p.unit) > ((int64_t)1 << 26) && V / p.unit > 1)) p.unit *= 2;
+        p.units = (int32_t)(((int64_t)V + p.unit - 1) / p.unit);
         p.pitch = (p.units + 2) / 2 * 2;               // units + 1 entries in whole 32-bit words
         p.o_start = take((size_t)T * p.pitch * 2);
     }
@@ -707,8 +708,8 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     MaxArgs max_args = {};
     if (f32) {
         const int64_t count = (int64_t)c.V * c.d, most = count > c.T * c.d ? count : c.T * c.d;
-        max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T, count, c.d, c.tau,
-                           max_part, blocks_for(most, 4096, kMaxBlocks)};
+        max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T, count,
+                           c.d, c.tau, max_part, blocks_for(most, 4096, kMaxBlocks)};
     }
 
     if (c.K > 0) {
@@ -726,7 +727,8 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
             ? launch_pdl(teacher_kernel<float>, grid, dim3(32 * warps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
                          c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats, list_blocks, max_args)
             : launch_pdl(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * warps), smem, s, c.top_index,
-                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats, list_blocks, max_args);
+                         static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units,
+                         p.pitch, list, start, flags, stats, list_blocks, max_args);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
@@ -749,7 +751,8 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     }
     PackArgs a = {};
     a.max_blocks = (int32_t)max_args.blocks;
-    if (f32 && c.K == 0 && launch_pdl(abs_max_kernel, dim3(max_args.blocks), dim3(256), 0, s, max_args, labels) != cudaSuccess) return TBN_ERR_CUDA;
+    if (f32 && c.K == 0 && launch_pdl(abs_max_kernel, dim3(max_args.blocks), dim3(256), 0, s, max_args, labels) != cudaSuccess)
+        return TBN_ERR_CUDA;
     a.labels = labels; a.T = c.T; a.Tpad = p.Tpad; a.V = c.V; a.d = c.d; a.ld = p.ld;
     a.per_block = (c.T + 591) / 592 < 8 ? 8 : (c.T + 591) / 592;
     a.row_blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);              // the last one has rows of its own
@@ -761,9 +764,10 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         a.loss_out = c.loss_out; a.lse_out = c.lse_out;
     }
     const unsigned blocks = a.row_blocks + (p.pack_w ? blocks_for((int64_t)c.V * (p.ld / 8), 256, 2368) : 0u);
-    const cudaError_t e = f32 ? launch_pdl(pack_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x), static_cast<const float *>(c.w), a)
-                              : launch_pdl(pack_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s, static_cast<const __nv_bfloat16 *>(c.x),
-                                           static_cast<const __nv_bfloat16 *>(c.w), a);
+    const cudaError_t e = f32 ? launch_pdl(pack_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x),
+                                           static_cast<const float *>(c.w), a)
+                              : launch_pdl(pack_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s,
+                                           static_cast<const __nv_bfloat16 *>(c.x), static_cast<const __nv_bfloat16 *>(c.w), a);
     if (e != cudaSuccess) return TBN_ERR_CUDA;
     out->x = Operand{ws + p.o_x, p.Tpad, p.Tpad, p.ld, p.ld};
     out->n_live = n_live; out->rows = rows; out->scales = f32 ? scales : nullptr;
@@ -794,8 +798,8 @@ int forward(const HeadCall &c, void *workspace, cudaStream_t s)
     const int rb = c.T >= 256 ? 8 : 1;
     const dim3 grid((unsigned)((c.T + rb - 1) / rb));
     auto kern = rb == 8 ? combine_kernel<8> : combine_kernel<1>;
-    return launch_pdl(kern, grid, dim3(256), 0, s, static_cast<const float4 *>(a.part), p.parts, a.n_live, a.rows, a.labels, (int32_t)c.T, teacher,
-                      c.tau, c.loss_out, c.lse_out) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
+    return launch_pdl(kern, grid, dim3(256), 0, s, static_cast<const float4 *>(a.part), p.parts, a.n_live, a.rows, a.labels,
+                      (int32_t)c.T, teacher, c.tau, c.loss_out, c.lse_out) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 
 int backward(const HeadCall &c, void *workspace, cudaStream_t s)

@@ -12,8 +12,8 @@
 // step, so a byte staged feeds twice the multiplications of a 128 x 256 tile on one CTA (per 64-element step and SM:
 // 32 KB instead of 48 KB for the same 4.2 MFLOP), which is what keeps shared memory and L2 below the tensor pipe.
 // Warp roles per CTA: 0 = TMA producer of A, 1 = MMA issuer (the first CTA of the pair only), 2 = TMA producer of B, 3 idle,
-// 4-11 (two planes: 4-19) = epilogue, two (four) warps per tensor-memory quadrant, 128 (32) columns each.  Two accumulators of 256 columns: the epilogue of a tile runs beside the
-// main loop of the next.
+// 4-11 (two planes: 4-19) = epilogue, two (four) warps per tensor-memory quadrant, 128 (32) columns each.  Two accumulators of
+// 256 columns: the epilogue of a tile runs beside the main loop of the next.
 //
 // dz lives in blocks that are images of the shared-memory tiles: panels of 64 classes, in a panel one 128-byte line per
 // token, the 16-byte pieces of a line permuted by the low three bits of the token as the 128-byte swizzle of tcgen05 wants
@@ -25,7 +25,7 @@
 // zero at every 16-element step, an error that grows with the length of the chain (measured, dot products of 1024: 2.6e-6
 // of the result's scale as one chain of 192 steps, 7e-7 for the bf16 form's 64), so with fp32 operands a chain ends after
 // 128 elements, the small products first, and the epilogue warps add the chains in registers, rounding to nearest.  For that
-// the tiles are 256 x 128 (64 running sums per thread) on four accumulators: with 256 x 256 and two, the hand-overs of a
+// the tiles are 256 x 128 (32 running sums per thread) on four accumulators: with 256 x 256 and two, the hand-overs of a
 // chain (commit, wait, read, release) outlast its MMAs.
 //
 // Same conventions as the other tcgen05 kernels: every wait is bounded, a wait that gives up records the status and the
@@ -686,7 +686,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             }
             more = sched.get<MODE, PL>(step + 1, next);
             if (more) next_info = row_info(next);
-            // the tile's sums: left in tensor memory, or (two planes) added up from its 64-element chains in registers
+            // the tile's sums: left in tensor memory, or (two planes) added up from its 128-element chains in registers
             float acc[PL == 2 ? kWarpCols<PL> : 1];
             uint32_t t_acc = 0;
             if (PL == 1) {
@@ -847,7 +847,8 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 o.prev_ld = slot ? g.slot_ld : g.d;
                 o.rows_in = rows_in; o.end = min(to_slot ? g.slot_ld : g.d, col0 + hc);
                 const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16);
-                const bool sectors = o.ld % 16 == 0 && (!o.prev || o.prev_ld % 16 == 0) && (reinterpret_cast<uintptr_t>(o.out) & 31) == 0 && (reinterpret_cast<uintptr_t>(o.prev) & 31) == 0;
+                const bool sectors = o.ld % 16 == 0 && (!o.prev || o.prev_ld % 16 == 0) &&
+                                     ((reinterpret_cast<uintptr_t>(o.out) | reinterpret_cast<uintptr_t>(o.prev)) & 31) == 0;
 #pragma unroll 1
                 for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
@@ -983,7 +984,8 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
     const int64_t dz_panels = a.ldz / 64, dz_panel = a.Tpad * 128;
     const bool w_panels = a.w.ld % 64 == 0;
     auto by_panels = [&a](CUtensorMap *m, const Operand &o) {
-        return make_panel_map(m, o.data, o.rows, (int64_t)o.ld * 2, o.ld / 64, 128, a.planes, o.plane_rows * o.ld * 2, 64, a.planes == 1 ? 2 : 1, CU_TENSOR_MAP_SWIZZLE_128B);
+        return make_panel_map(m, o.data, o.rows, (int64_t)o.ld * 2, o.ld / 64, 128, a.planes, o.plane_rows * o.ld * 2, 64,
+                              a.planes == 1 ? 2 : 1, CU_TENSOR_MAP_SWIZZLE_128B);
     };
     if (!make_panel_map(&maps.a[0], a.dz, a.Tpad, 128, dz_panels, dz_panel, a.planes, dz_panels * dz_panel, 128, 1, CU_TENSOR_MAP_SWIZZLE_NONE) ||
         !make_panel_map(&maps.a[1], a.dz, a.Tpad, 128, dz_panels, dz_panel, a.planes, dz_panels * dz_panel, 64, 2, CU_TENSOR_MAP_SWIZZLE_NONE) ||

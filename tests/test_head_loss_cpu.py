@@ -101,6 +101,15 @@ def test_workspace_queries(lib):
     assert lib.tbn_linear_distill_workspace_bytes(4, 64, 100, B.BF16, 2000, 0) == 0
 
 
+@pytest.mark.parametrize("T,V,K", [(1 << 27, 2**31 - 1025, 1), (2**31 - 1025, 2**31 - 1025, 1024), (1, 2**31 - 1025, 3), (2**31 - 1025, 1, 2)])
+def test_distill_workspace_at_the_largest_sizes(lib, T, V, K):
+    """The lists (8 bytes per entry) and the table of their starts (two entries of 2 bytes per token at least) are in it."""
+    for dtype in (B.BF16, B.F32):
+        for backward in (0, 1):
+            rest = lib.tbn_linear_xent_workspace_bytes(T, 1, V, dtype, backward)
+            assert lib.tbn_linear_distill_workspace_bytes(T, 1, V, dtype, K, backward) >= rest + T * (8 * K + 4)
+
+
 def test_binding_checks_shapes_types_and_devices():
     x, w = torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(10, 8, dtype=torch.bfloat16)
     t, f = torch.zeros(4, dtype=torch.int64), torch.zeros(4)
