@@ -554,7 +554,7 @@ finish_kernel(const FinishArgs a)
         __syncthreads();
         if (g == 0 && c < a.width) {
             for (int i = 1; i < 8; ++i) s += sum[i][lane];
-            a.db[c] = a.scales ? s * a.scales->inv_g : s;
+            a.db[c] = s * (a.scales ? a.scales->inv_g : common_mantissa(a.rows, *a.n_live));
         }
         return;
     }

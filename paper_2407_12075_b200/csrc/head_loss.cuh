@@ -20,6 +20,17 @@ struct __align__(16) RowInfo {
     int32_t row;                           // the row's index in the caller's tensors
 };
 
+#ifdef __CUDACC__
+// The factor in [1, 2) that the bf16 form takes out of the gradient's tokens before dz is rounded and puts back into the sums:
+// the mantissa of the first kept token's g.  Under a mean every token has the same g; with it in dz the largest entry of
+// every row, -g (1 - q), would be rounded the same way, and all of dx and dw off by up to 2^-8 with it.
+__device__ __forceinline__ float common_mantissa(const RowInfo *rows, int32_t n_live)
+{
+    const uint32_t b = n_live > 0 ? __float_as_uint(rows[0].g) : 0u, e = b & 0x7f800000u;
+    return e == 0u || e == 0x7f800000u ? 1.0f : __uint_as_float((b & 0x007fffffu) | 0x3f800000u);
+}
+#endif
+
 // Powers of two that bring the fp32 operands into the range of fp16 (all 1 for bf16 operands), and their inverses.
 struct Scales { float x, w, g, inv_x, inv_w, inv_g; };
 

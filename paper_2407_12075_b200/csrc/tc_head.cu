@@ -647,6 +647,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
         } else if (p.g.scales) {
             inv_g = p.g.scales->inv_g;
         }
+        const float mantissa = PL == 1 && MODE != kStats ? common_mantissa(MODE == kDz ? p.l.rows : p.g.rows, n_live) : 1.0f;
         // what a tile needs to know about this lane's row, asked for while the tile before it is worked on
         auto row_info = [&](const Tile &u) {
             RowInfo r = {0.0f, 0.0f, -1, 0};
@@ -774,6 +775,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 }
             } else if (MODE == kDz) {
                 const bool all_live = __all_sync(0xffffffffu, live);
+                const float row_g = PL == 1 ? info.g / mantissa : info.g;
                 const int32_t panels = p.l.ldz / 64;
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
 #pragma unroll 1
@@ -787,13 +789,13 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 #pragma unroll
                         for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;
                     }
-                    const uint64_t g2 = f32x2_pack(info.g, info.g);
+                    const uint64_t g2 = f32x2_pack(row_g, row_g);
 #pragma unroll
                     for (int j = 0; j < 32; j += 2)
                         f32x2_unpack(f32x2_mul(f32x2_pack(exp2_approx(v[j]), exp2_approx(v[j + 1])), g2), v[j], v[j + 1]);
                     while (list.next < p.l.v0 + c0 + 32) {
                         const int rel = list.next - (p.l.v0 + c0);
-                        const float sub = info.g * list.weight;
+                        const float sub = row_g * list.weight;
 #pragma unroll
                         for (int j = 0; j < 32; ++j) if (rel == j) v[j] -= sub;
                         list.step();
@@ -832,7 +834,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const GradParams &g = p.g;
                 const bool empty = t.kb0 >= t.kb1;     // nothing was contracted: the accumulator holds no result
                 const bool is_dx = t.job == 0;
-                const float scale = g.scales ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : 1.0f;
+                const float scale = PL == 2 ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : mantissa;
                 const int32_t rows_in = (is_dx ? n_live : g.width) - row0;             // rows of this warp that exist
                 const int splits = is_dx ? g.dx_splits : g.dw_splits;
                 float *slot = is_dx ? g.dx_slots : g.dw_slots;

@@ -87,9 +87,10 @@ def test_distillation_matches_64_bit_form(T, d, V, dtype, K, tau):
 
 
 # ---- what a row or an entry may hold -------------------------------------------------------------------
-def test_left_out_tokens_reach_nothing():
+@pytest.mark.parametrize("T", [300, 100])                        # kept rows packed to the front; rows read in place
+def test_left_out_tokens_reach_nothing(T):
     """Infinities and NaN in the rows of ignored tokens, of every kind of target that is left out."""
-    T, d, V = 300, 64, 500
+    d, V = 64, 500
     g, x, w, bias, dloss = make(1, T, d, V, torch.bfloat16, True)
     targets = torch.randint(0, V, (T,), generator=g)
     targets[::3], targets[1::7], targets[2::11] = -100, V, -5
@@ -241,6 +242,24 @@ def test_signed_and_zero_loss_gradients():
     dloss[1::5] = 0.0
     check_xent(x, w, bias, torch.randint(0, 320, (150,), generator=g), dloss)
     check_xent(x, w, bias, torch.randint(0, 320, (150,), generator=g), torch.zeros(150))
+
+
+@pytest.mark.parametrize("T", [171, 300])
+def test_a_mean_of_any_number_of_tokens_is_not_off_as_a_whole(T):
+    """256 classes of one logit each: every q is 2^-8, so every dz / dloss is 2^-8 or 2^-8 - 1, which bf16 holds exactly.  With
+    one dloss for all tokens that leaves the sums' own error: (T / 16 + 8) cut-offs of 2^-23 (the 8 cover the factor taken out
+    and put back and the output's rounding to fp32).  1 / T itself is 0.2 % off in bf16 for both T."""
+    d, V = 64, 256
+    g, x, w, _, _ = make(T, T, d, V, torch.bfloat16, False)
+    x[:, -1] = 0
+    w[:, :-1] = 0
+    dloss = torch.full((T,), 1.0 / T)
+    targets = torch.randint(0, V, (T,), generator=g)
+    targets[::5] = -100
+    _, _, dx, dw, db = check_xent(x, w, None, targets, dloss, dw_dtype=B.F32)
+    ref = reference(x, w, None, dloss, 1.0, *one_hot(targets, V))
+    assert_within(dw, ref["dw"], ref["dw_abs"] * (T / 16 + 8) * 2.0 ** -23, "dw")
+    assert_within(dx, ref["dx"], ref["dx_abs"] * (V / 16 + 8) * 2.0 ** -23 + ref["dx"].abs() * 2.0 ** -8, "dx")
 
 
 @pytest.mark.parametrize("scale_x,scale_w", [(1e-12, 1e10), (1e8, 1e-9), (1e-3, 1e-3)])
