@@ -6,6 +6,7 @@ of launches):
 Cases: linear_k2, linear_k16 (8192 x 8192, T = 8192), bin_k2, bin_k16 (binary activations, 8192 x 8192, T = 4096),
 binbytes_k2, binbytes_k16 (the same with the activation signs as bytes),
 conv_s2 (64 -> 128, 32 x 32, batch 64), attention (64 images x 12 heads x 197 tokens), binarize, tile_bwd,
+head_xent, head_xent_f32, head_distill (forward and backward of a head over 8192 classes, 4096 tokens of 1024),
 first_conv (dense 3 -> 64, 32 x 32, batch 256), compact_gelu (second MLP layer of a ViT-B block fed the first layer's 384 distinct pre-activations, T = 25,216).
 Inputs are seeded device-side random values of the benchmark's shapes; every run checks the device status word.
 """
@@ -72,6 +73,25 @@ def main():
         xc = torch.rand(256, 3, 32, 32, device=dev, generator=gen).to(torch.bfloat16)
         W0 = torch.randn(64, 3, 3, 3, device=dev, generator=gen) * 0.27
         run = lambda: B.tbn_conv2d_dense_fwd(xc, W0, 1, 1, act=B.ACT_RELU)
+    elif args.case in ("head_xent", "head_xent_f32", "head_distill"):
+        T, d, V = 4096, 1024, 8192
+        dt = torch.float32 if args.case.endswith("f32") else torch.bfloat16
+        x = torch.randn(T, d, device=dev, generator=gen).to(dt)
+        w = (torch.randn(V, d, device=dev, generator=gen) * 2 / d ** 0.5).to(dt)
+        dloss = torch.full((T,), 1.0 / T, device=dev)
+        if args.case == "head_distill":
+            index = torch.randint(0, V, (T, 64), device=dev, generator=gen)
+            logit = torch.randn(T, 64, device=dev, generator=gen) * 3
+
+            def run():
+                _, lse = B.tbn_linear_distill_fwd(x, w, index, logit, 2.0)
+                B.tbn_linear_distill_bwd(x, w, index, logit, lse, dloss, 2.0)
+        else:
+            targets = torch.randint(0, V, (T,), device=dev, generator=gen)
+
+            def run():
+                _, lse = B.tbn_linear_xent_fwd(x, w, targets)
+                B.tbn_linear_xent_bwd(x, w, targets, lse, dloss)
     elif args.case == "tile_bwd":
         N, k = 4096 * 4096, 4
         W = torch.randn(N, device=dev, generator=gen) * 0.02
