@@ -521,26 +521,28 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             const int32_t r0 = is_a ? t.m0 + (int32_t)rank * 128 : t.n0 + (int32_t)rank * (t.bn / 2);
             const int job = __shfl_sync(0xffffffffu, t.job, 0);
             const CUtensorMap *map = is_a ? &maps.a[job] : &maps.b[job];
+            // A half tile of rows that do not exist is not loaded: what the second CTA holds instead reaches no result
+            const bool second = t.m0 + 128 < (job == 0 ? n_live : p.g.width), load_a = rank == 0 || second;
             for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
                 ok = wait_bar(smem_u32(&ctl->empty[px.stage]), px.phase ^ 1u, abort_flag, p.status, (40 << 24) | (px.stage << 16) | detail);
                 if (!ok) break;
                 const uint32_t bar = bar0 + px.stage * 8, sa = sm0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
                 if (MODE != kGrads) {
-                    // with at most 128 tokens the second CTA's half of the tile stays as it is: its rows reach no result
-                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((p.l.a_rows == 128 ? 2 : 1) * a_bytes + 2 * b_bytes), leader);
+                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((second ? 2 : 1) * a_bytes + 2 * b_bytes), leader);
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
                         if (!is_a) tma_load_pair(sb + pl * b_bytes, map, kb * 64, p.l.v0 + r0, pl, bar, leader);
-                        else if (rank == 0 || p.l.a_rows == 128) tma_load_pair(sa + pl * a_bytes, map, kb * 64, r0, pl, bar, leader);
+                        else if (load_a) tma_load_pair(sa + pl * a_bytes, map, kb * 64, r0, pl, bar, leader);
                     }
                 } else {
                     // dX: dz as 128 tokens x 64 classes, dW: as two panels of 64 tokens x 64 classes
-                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, 2 * kStage, leader);
+                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((second ? 2 : 1) * kSideBytes + 2 * kBBytes), leader);
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
                         const uint32_t dst = is_a ? sa + pl * kSideBytes : sb + pl * kBBytes;
                         const int32_t krow = (job == 0 ? p.g.v0 : 0) + kb * 64;
                         if (is_a) {
+                            if (!load_a) continue;
                             if (job == 0) tma_load_pair(dst, map, 0, r0, kb, pl, bar, leader);
                             else tma_load_pair(dst, map, 0, kb * 64, r0 / 64, pl, bar, leader);
                         } else if (job == 1 || p.g.w_panels) {
@@ -673,6 +675,9 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             const int32_t row0 = t.m0 + (int32_t)rank * 128 + qd * 32, row = row0 + lane;
             const int32_t hc = t.bn / kGroups<PL>, col0 = t.n0 + group * hc;
             const bool live = row < n_live;
+            // rows that nothing is written for: dz has zeros up to the next 64 tokens, which dW contracts over
+            const int32_t row_end = MODE == kDz ? (n_live + 63) & ~63 : MODE == kGrads && t.job == 1 ? p.g.width : n_live;
+            const int chunks = row0 < row_end ? kWarpCols<PL> / 32 : 0;
             Listed list;
             if (MODE != kGrads) list.begin(p.l, info, live, p.l.v0 + col0);
             float *bias_s = reinterpret_cast<float *>(smem_raw + pad + kStageBudget) + ew * kWarpCols<PL>;
@@ -703,11 +708,13 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t t_sum = t_lane + pd.stage * kCols<PL> + (uint32_t)(group * hc);
-                    uint32_t r[32];
-                    tmem_ld_32x32(t_sum, r);
-                    tc_wait_ld();
+                    if (chunks) {
+                        uint32_t r[32];
+                        tmem_ld_32x32(t_sum, r);
+                        tc_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] += __uint_as_float(r[j]);
+                        for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] += __uint_as_float(r[j]);
+                    }
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&ctl->d_empty[pd.stage]), 0));
@@ -717,7 +724,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             }
             // 32 columns of the tile.  One plane: the next 32 are asked for before these are worked on.
             uint32_t ahead[PL == 1 ? 32 : 1];
-            if constexpr (PL == 1) tmem_ld_32x32(t_acc, ahead);
+            if constexpr (PL == 1) { if (chunks) tmem_ld_32x32(t_acc, ahead); }
             auto load_chunk = [&](int ch, float (&out)[32]) {
                 if constexpr (PL == 1) {
                     tc_wait_ld();
@@ -733,7 +740,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             if (MODE == kStats) {
                 float m = -INFINITY, l = 0.0f, dot = 0.0f;
 #pragma unroll 1
-                for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
+                for (int ch = 0; ch < chunks; ++ch) {
                     if (ch * 32 >= hc) continue;
                     const int32_t c0 = col0 + ch * 32, end = min(c0 + 32, min(col0 + hc, p.l.width));
                     float v[32];
@@ -779,7 +786,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const int32_t panels = p.l.ldz / 64;
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
 #pragma unroll 1
-                for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
+                for (int ch = 0; ch < chunks; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
                     if (ch * 32 >= hc || c0 >= p.l.ldz) continue;
                     float v[32];
@@ -852,7 +859,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const bool sectors = o.ld % 16 == 0 && (!o.prev || o.prev_ld % 16 == 0) &&
                                      ((reinterpret_cast<uintptr_t>(o.out) | reinterpret_cast<uintptr_t>(o.prev)) & 31) == 0;
 #pragma unroll 1
-                for (int ch = 0; ch < kWarpCols<PL> / 32; ++ch) {
+                for (int ch = 0; ch < chunks; ++ch) {
                     const int32_t c0 = col0 + ch * 32;
                     if (ch * 32 >= hc || c0 >= g.d) continue;
                     float v[32];
@@ -943,7 +950,6 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     KernelParams p = {};
     LogitsParams &l = p.l;
     l.n_live = a.n_live; l.rows = a.rows; l.labels = a.labels; l.n_rows = (int32_t)a.T; l.bn = a.bn;
-    // the second CTA's rows: none for T <= 128
     l.a_rows = (int32_t)rows;
     const int64_t stage = (int64_t)a.planes * (rows * 128 + a.bn * 64), fit = (kStageBudget - kSideBytes + rows * 128) / stage;
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
