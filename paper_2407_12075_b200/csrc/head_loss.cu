@@ -50,15 +50,16 @@ struct MaxArgs {
     float *max_part;
     unsigned int blocks;
 };
-__device__ __forceinline__ float block_max(float v) {
-    __shared__ float part[8];
-    v = warp_max(v);
+// The block's maxima of three values that are not negative (up to eight warps).
+__device__ __forceinline__ void block_max(float (&v)[3]) {
+    __shared__ float part[3][8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[k] = warp_max(v[k]);
+    if (lane < 3) part[lane][warp] = lane == 0 ? v[0] : lane == 1 ? v[1] : v[2];
     __syncthreads();
-    if (threadIdx.x < 8) part[threadIdx.x] = 0.0f;
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    return warp_max(part[threadIdx.x & 7]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[k] = warp_max((lane & 7) < warps ? part[k][lane & 7] : 0.0f);
 }
 __device__ __forceinline__ float max_finite(float m, float v) {
     v = fabsf(v);
@@ -91,13 +92,11 @@ __device__ __forceinline__ void abs_max(const MaxArgs &a, unsigned int block, Li
         if (a.dloss && lane == 0) mg = max_finite(mg, a.dloss[t] * a.tau);
         __syncwarp();
     }
-    mx = block_max(mx);
-    mw = block_max(mw);
-    mg = block_max(mg);
+    float m[3] = {mx, mw, mg};
+    block_max(m);
     if (threadIdx.x == 0) {
-        a.max_part[block] = mx;
-        a.max_part[kMaxBlocks + block] = mw;
-        a.max_part[2 * kMaxBlocks + block] = mg;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) a.max_part[k * kMaxBlocks + block] = m[k];
     }
 }
 __global__ void __launch_bounds__(256)
@@ -254,18 +253,28 @@ struct PackArgs {
 
 // eight elements of a row from column c, zeros from column d on
 template <typename TS>
-__device__ __forceinline__ void pack8(const TS *__restrict__ src, int32_t c, int32_t d, float scale, uint16_t *hi_dst, uint16_t *lo_dst) {
+__device__ __forceinline__ void load8(const TS *__restrict__ src, int32_t c, int32_t d, float (&v)[8]) {
+    if (sizeof(TS) == 4 && d % 4 == 0 && c + 8 <= d) {
+        const float4 a = __ldg(reinterpret_cast<const float4 *>(src + c)), b = __ldg(reinterpret_cast<const float4 *>(src + c) + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = c + j < d ? load_as_float(src, c + j) : 0.0f;
+    }
+}
+template <typename TS>
+__device__ __forceinline__ void pack8(const TS *__restrict__ src, int32_t c, int32_t d, float scale, uint16_t *hi_dst, uint16_t *lo_dst,
+                                      const float (*given)[8] = nullptr) {
     alignas(16) uint16_t hi[8], lo[8];
     if (sizeof(TS) == 2 && d % 8 == 0 && c + 8 <= d) {
         *reinterpret_cast<uint4 *>(hi) = __ldg(reinterpret_cast<const uint4 *>(src + c));
     } else {
         float v[8];
-        if (sizeof(TS) == 4 && d % 4 == 0 && c + 8 <= d) {
-            const float4 a = __ldg(reinterpret_cast<const float4 *>(src + c)), b = __ldg(reinterpret_cast<const float4 *>(src + c) + 1);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-        } else {
+        if (given) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = c + j < d ? load_as_float(src, c + j) : 0.0f;
+            for (int j = 0; j < 8; ++j) v[j] = (*given)[j];
+        } else {
+            load8(src, c, d, v);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -314,6 +323,23 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     pdl_wait();
+    constexpr int kVec = 16 / sizeof(TS);              // rows in whole 16-byte pieces
+    const int64_t r0 = (int64_t)blockIdx.x * a.per_block, r1 = min(a.T, r0 + a.per_block);       // r0 < T for every row block
+    // everything that does not wait for the scales is asked for before they are put together: a weight block's first eight
+    // elements, a row block's count of the kept rows before its own
+    const int64_t vecs = a.ld >> 3, groups = a.V * vecs;
+    const int64_t first = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
+    const bool weights = blockIdx.x >= a.row_blocks, early = sizeof(TS) == 4 && weights && a.d % kVec == 0 && first < groups;
+    float ahead[8];
+    if (early) {
+        const int64_t r = first / vecs;
+        load8(w + r * a.d, (int32_t)(first - r * vecs) * 8, a.d, ahead);
+    }
+    int mine = 0;
+    if (!weights) {
+#pragma unroll 8
+        for (int64_t t = threadIdx.x; t < r0; t += 256) mine += a.labels.live(t) ? 1 : 0;
+    }
     float m[3] = {0.0f, 0.0f, 0.0f};
     if (sizeof(TS) == 4) {
 #pragma unroll
@@ -322,11 +348,9 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
 #pragma unroll
             for (int k = 0; k < 3; ++k) m[k] = fmaxf(m[k], i < a.max_blocks ? a.max_part[k * kMaxBlocks + i] : 0.0f);
         }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) m[k] = block_max(m[k]);
+        block_max(m);
     }
     const float sx = scale_of(m[0]), sw = scale_of(m[1]), sg = scale_of(m[2]);
-    constexpr int kVec = 16 / sizeof(TS);              // rows in whole 16-byte pieces
     if (blockIdx.x >= a.row_blocks && a.d % kVec != 0) {
         const int64_t plane = (int64_t)a.V * a.ld;
         for (int64_t r = (int64_t)(blockIdx.x - a.row_blocks) * 8 + warp; r < a.V; r += (int64_t)(gridDim.x - a.row_blocks) * 8) {
@@ -336,21 +360,16 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
         return;
     }
     if (blockIdx.x >= a.row_blocks) {                  // weights
-        const int64_t vecs = a.ld >> 3, groups = a.V * vecs, plane = (int64_t)a.V * a.ld;
-        const int64_t stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
-        for (int64_t i = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x; i < groups; i += stride) {
+        const int64_t plane = (int64_t)a.V * a.ld, stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
+        for (int64_t i = first; i < groups; i += stride) {
             const int64_t r = i / vecs;
             const int32_t c = (int32_t)(i - r * vecs) * 8;
             uint16_t *dst = a.wc + r * a.ld + c;
-            pack8(w + r * a.d, c, a.d, sw, dst, dst + plane);
+            pack8(w + r * a.d, c, a.d, sw, dst, dst + plane, early && i == first ? &ahead : nullptr);
         }
         return;
     }
     if (sizeof(TS) == 4 && blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{sx, sw, sg, 1.0f / sx, 1.0f / sw, 1.0f / sg};
-    const int64_t r0 = (int64_t)blockIdx.x * a.per_block, r1 = min(a.T, r0 + a.per_block);       // r0 < T for every row block
-    int mine = 0;
-#pragma unroll 8
-    for (int64_t t = threadIdx.x; t < r0; t += 256) mine += a.labels.live(t) ? 1 : 0;
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0) warp_count[warp] = mine;
     __syncthreads();
@@ -415,8 +434,8 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     }
     if (blockIdx.x == a.row_blocks - 1) {
         if (threadIdx.x == 0) *a.n_live = (int32_t)base;
-        const int64_t end = (base + 63) / 64 * 64, vecs = (end - base) * (a.ld >> 3);
-        for (int64_t i = threadIdx.x; i < vecs; i += 256) {
+        const int64_t end = (base + 63) / 64 * 64;
+        for (int64_t i = threadIdx.x; i < (end - base) * vecs; i += 256) {
             uint4 *p = reinterpret_cast<uint4 *>(a.xc + base * a.ld) + i;
             *p = make_uint4(0u, 0u, 0u, 0u);
             if (sizeof(TS) == 4) *(p + (plane >> 3)) = make_uint4(0u, 0u, 0u, 0u);
