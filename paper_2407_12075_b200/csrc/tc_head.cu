@@ -738,7 +738,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             };
 
             if (MODE == kStats) {
-                float m = -INFINITY, l = 0.0f, dot = 0.0f;
+                float m = -INFINITY, l = 0.0f, dot = 0.0f;     // m: without a bias before scaling
 #pragma unroll 1
                 for (int ch = 0; ch < chunks; ++ch) {
                     if (ch * 32 >= hc) continue;
@@ -763,9 +763,18 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
                     for (int j = 4; j < 32; ++j) mx[j & 3] = fmaxf(mx[j & 3], v[j]);
-                    const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * vs);
+                    // The difference to the maximum before it is scaled: exact near the maximum, so that the largest term is 1
+                    // however large the logits are (scaled first, a product and its rounded self differ by more than exp2's range
+                    // from 2^31 on: infinite sums)
+                    const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
                     const float ref = m_new == -INFINITY ? 0.0f : m_new;
-                    scale_shift<false>(v, vs, -ref, nullptr);
+                    const uint64_t ref2 = f32x2_pack(-ref, -ref), vs2 = f32x2_pack(vs, vs);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        uint64_t u = f32x2_add(f32x2_pack(v[j], v[j + 1]), ref2);
+                        if (!BIAS) u = f32x2_mul(u, vs2);
+                        f32x2_unpack(u, v[j], v[j + 1]);
+                    }
                     uint64_t s0 = 0, s1 = 0;           // four running sums
 #pragma unroll
                     for (int j = 0; j < 32; j += 4) {
@@ -774,11 +783,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     }
                     float e0, e1;
                     f32x2_unpack(f32x2_add(s0, s1), e0, e1);
-                    l = l * exp2_approx(m - ref) + (e0 + e1);
+                    l = l * exp2_approx((m - ref) * vs) + (e0 + e1);
                     m = m_new;
                 }
                 if (live) {
-                    p.l.part[(int64_t)row * p.l.parts + (p.l.v0 + col0) / hc] = make_float4(m, l, dot, 0.0f);
+                    p.l.part[(int64_t)row * p.l.parts + (p.l.v0 + col0) / hc] = make_float4(BIAS ? m : m * sc, l, dot, 0.0f);
                 }
             } else if (MODE == kDz) {
                 const bool all_live = __all_sync(0xffffffffu, live);
