@@ -51,6 +51,7 @@ constexpr uint32_t kStageBudget = 6 * 2 * kSideBytes;  // 192 KB of stages
 constexpr uint32_t kExchange = 2048;                   // per epilogue warp: 16 lines of 128 bytes
 constexpr uint32_t kTmemCols = 512;
 constexpr int kGroupM = 32;                            // token tiles that share a sweep over the classes
+constexpr float kCoarseLse = 4096.0f;                  // |log2 of a row's sum| from which on its rounding shows in the probabilities
 
 enum { kStats = 0, kDz = 1, kGrads = 2 };
 
@@ -792,6 +793,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             } else if (MODE == kDz) {
                 const bool all_live = __all_sync(0xffffffffu, live);
                 const float row_g = PL == 1 ? info.g / mantissa : info.g;
+                // lse is a float: a logit and the lse that it makes up differ by up to 2^-22 of it (four roundings).  Where that is
+                // more than a thousandth, what comes within it, and what comes out above lse, is a probability of 1.
+                const bool coarse = fabsf(info.lse2) > kCoarseLse;
+                const bool any_coarse = __any_sync(0xffffffffu, coarse);
+                const float lse2 = coarse ? info.lse2 - 1.5f * 0x1p-22f * fabsf(info.lse2) : info.lse2;
                 const int32_t panels = p.l.ldz / 64;
                 uint16_t *dz = static_cast<uint16_t *>(p.l.dz);
 #pragma unroll 1
@@ -800,7 +806,11 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if (ch * 32 >= hc || c0 >= p.l.ldz) continue;
                     float v[32];
                     load_chunk(ch, v);
-                    scale_shift<BIAS>(v, sc, -info.lse2, reinterpret_cast<const float4 *>(bias_s + ch * 32));
+                    scale_shift<BIAS>(v, sc, -lse2, reinterpret_cast<const float4 *>(bias_s + ch * 32));
+                    if (any_coarse) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = coarse && v[j] > 0.0f ? 0.0f : v[j];       // NaN stays
+                    }
                     if (!BIAS && c0 + 32 > p.l.width) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) if (c0 + j >= p.l.width) v[j] = -INFINITY;

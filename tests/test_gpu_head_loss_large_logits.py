@@ -36,3 +36,30 @@ def test_loss_of_a_cold_softmax(dtype, tau):
     """Logits of order 1 at a temperature near 0."""
     _, x, w, dloss, targets = make(9, 130, 64, 300, dtype)
     check(x, w, None, dloss, tau=tau, index=targets[:, None].clamp(min=0), logit=torch.zeros(130, 1, device=DEV), names=("lse", "loss"))
+
+
+@pytest.mark.parametrize("every", [9, 1])
+@pytest.mark.parametrize("factor", [1e3, 1e6, 1e9, 1e12])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_gradient_of_large_logits(every, factor, with_bias):
+    """Tokens with large logits, alone or among ordinary ones."""
+    g, x, w, dloss, targets = make(10, 140, 64, 300, torch.bfloat16)
+    x[::every] *= factor
+    got, _, _ = check(x, w, torch.randn(300, generator=g).to(DEV) if with_bias else None, dloss, targets=targets)
+    assert all(bool(torch.isfinite(t).all()) for t in got.values())
+
+
+@BOTH
+@pytest.mark.parametrize("factor", [1e4, 1e7, 1e12])
+def test_gradient_of_sure_tokens(dtype, factor):
+    """Targets that are the largest logit by far: q is 1 there, the gradient 0 but for what is left of the rounding of lse."""
+    _, x, w, dloss, _ = make(11, 140, 64, 300, dtype)
+    x *= factor
+    z = x.double() @ w.double().t()
+    top = z.topk(2, 1).values
+    targets = torch.where(top[:, 0] - top[:, 1] > 1e-3 * top[:, 0].abs(), z.argmax(1), torch.full((140,), -100, device=DEV))
+    assert int((targets >= 0).sum()) > 70
+    got, _, _ = check(x, w, None, dloss, targets=targets)
+    size = float(dloss.max() * w.abs().max().float() * 2)
+    # q >= exp(-2^-22 lse) below |log2 sum| = 4096, 1 above it
+    assert float(got["dx"].float().abs().max()) <= size * 4096 * 2.0 ** -22
