@@ -5,6 +5,7 @@
 //   cross entropy (tau = 1)   loss_t = lse_t - z_t,label
 //   distillation              loss_t = tau^2 sum_j p_tj (log p_tj - z_t,idx(t,j) / tau + lse_t)
 //   gradient                  dz_tv = dloss_t tau (exp(z_tv / tau - lse_t) - sum_{j: idx(t,j) = v} p_tj)
+//                             (held without tau, which the sums over it are multiplied by: it may be anything from 1e-30 to 1e30)
 //
 // Cross entropy is distillation from one entry of probability 1, so both share every kernel; only where the entries come
 // from differs.  The logits are never stored: the forward keeps one (maximum, sum, weighted dot) triple per token and 128
@@ -38,7 +39,7 @@ __device__ __forceinline__ float warp_max(float v) {
 }
 
 // ---- fp32 operands: largest magnitudes ------------------------------------------------------------------
-// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss * tau| over the kept rows, of the finite
+// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss| over the kept rows, of the finite
 // ones: an infinity must not change how the other tokens are rounded.
 constexpr int kMaxBlocks = 592;
 
@@ -46,7 +47,6 @@ struct MaxArgs {
     const float *x, *w, *dloss;            // dloss: backward
     int64_t T, w_count;
     int32_t d;
-    float tau;
     float *max_part;
     unsigned int blocks;
 };
@@ -89,7 +89,7 @@ __device__ __forceinline__ void abs_max(const MaxArgs &a, unsigned int block, Li
         if (!live(t)) continue;
 #pragma unroll 4
         for (int32_t c = lane; c < a.d; c += 32) mx = max_finite(mx, a.x[t * a.d + c]);
-        if (a.dloss && lane == 0) mg = max_finite(mg, a.dloss[t] * a.tau);
+        if (a.dloss && lane == 0) mg = max_finite(mg, a.dloss[t]);
         __syncwarp();
     }
     float m[3] = {mx, mw, mg};
@@ -244,7 +244,6 @@ struct PackArgs {
     RowInfo *rows;
     int32_t *n_live;
     Scales *scales;                        // fp32 only: written here for the kernels that follow
-    float tau;
     const float *lse, *dloss;              // backward
     float *loss_out, *lse_out;             // forward: zeroed for the tokens left out
     void *dx;                              // backward: rows zeroed for the tokens left out (or null)
@@ -390,7 +389,7 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
         if (live) {
             RowInfo info;
             info.lse2 = a.lse ? a.lse[t] * kLog2e : 0.0f;
-            info.g = a.dloss ? a.dloss[t] * a.tau * sg : 0.0f;
+            info.g = a.dloss ? a.dloss[t] * sg : 0.0f;
             info.label = a.labels.flags ? -1 : (int32_t)a.labels.target[t];
             info.row = (int32_t)t;
             a.rows[at] = info;
@@ -498,7 +497,7 @@ combine_kernel(const float4 *__restrict__ part, int32_t parts, const int32_t *__
         lse[t] = lse2 * kLn2;
         if (teacher) {
             const float2 e = teacher[t];               // sum p log p, sum p
-            loss[t] = tau * tau * fmaf(kLn2, fmaf(lse2, e.y, -j.dot), e.x);
+            loss[t] = tau * (tau * fmaf(kLn2, fmaf(lse2, e.y, -j.dot), e.x));      // tau * tau may be below fp32 where this is not
         } else {
             loss[t] = (lse2 - j.dot) * kLn2;
         }
@@ -510,6 +509,7 @@ struct FinishArgs {
     const int32_t *n_live;
     const RowInfo *rows;
     const Scales *scales;
+    float tau;
     // db[v0 + c] = sum over the 32-row groups of the kept tokens (bias_blocks blocks of 32 classes)
     const float *col_part;
     int32_t ldz, width;
@@ -573,7 +573,7 @@ finish_kernel(const FinishArgs a)
         __syncthreads();
         if (g == 0 && c < a.width) {
             for (int i = 1; i < 8; ++i) s += sum[i][lane];
-            a.db[c] = s * (a.scales ? a.scales->inv_g : common_mantissa(a.rows, *a.n_live));
+            a.db[c] = s * a.tau * (a.scales ? a.scales->inv_g : common_mantissa(a.rows, *a.n_live));
         }
         return;
     }
@@ -741,7 +741,7 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     if (f32) {
         const int64_t count = (int64_t)c.V * c.d, most = count > c.T * c.d ? count : c.T * c.d;
         max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T, count,
-                           c.d, c.tau, max_part, blocks_for(most, 4096, kMaxBlocks)};
+                           c.d, max_part, blocks_for(most, 4096, kMaxBlocks)};
     }
 
     if (c.K > 0) {
@@ -789,7 +789,7 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     a.per_block = (c.T + 591) / 592 < 8 ? 8 : (c.T + 591) / 592;
     a.row_blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);              // the last one has rows of its own
     a.max_part = max_part; a.xc = reinterpret_cast<uint16_t *>(ws + p.o_x); a.wc = reinterpret_cast<uint16_t *>(ws + p.o_w);
-    a.rows = rows; a.n_live = n_live; a.scales = scales; a.tau = c.tau;
+    a.rows = rows; a.n_live = n_live; a.scales = scales;
     if (backward) {
         a.lse = c.lse; a.dloss = c.dloss; a.dx = c.dx; a.dx_bytes = c.dx_dtype == TBN_F32 ? 4 : 2;
     } else {
@@ -847,7 +847,7 @@ int backward(const HeadCall &c, void *workspace, cudaStream_t s)
     a.col_part = c.db ? reinterpret_cast<float *>(ws + p.o_col) : nullptr;
 
     GradArgs g = {};
-    g.x = a.x; g.w = a.w; g.planes = a.planes; g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.dz = a.dz;
+    g.x = a.x; g.w = a.w; g.planes = a.planes; g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.tau = c.tau; g.dz = a.dz;
     g.T = c.T; g.Tpad = p.Tpad; g.d = c.d; g.V = c.V; g.ldz = p.width;
     g.want_dx = c.dx != nullptr; g.want_dw = c.dw != nullptr;
     g.dx = c.dx; g.dx_bf16 = dx_bf16; g.dx_slots = p.dx_slots ? reinterpret_cast<float *>(ws + p.o_dx) : nullptr; g.dx_splits = p.dx_splits;
@@ -869,7 +869,7 @@ int backward(const HeadCall &c, void *workspace, cudaStream_t s)
             if (rc != TBN_OK) return rc;
         }
         FinishArgs f = {};
-        f.n_live = a.n_live; f.rows = a.rows; f.scales = a.scales; f.d = c.d; f.ld = p.ld; f.width = a.width;
+        f.n_live = a.n_live; f.rows = a.rows; f.scales = a.scales; f.tau = c.tau; f.d = c.d; f.ld = p.ld; f.width = a.width;
         if (c.db) {
             f.col_part = a.col_part; f.ldz = a.ldz; f.db = c.db + a.v0;
             f.bias_blocks = (unsigned)((a.width + 31) / 32);

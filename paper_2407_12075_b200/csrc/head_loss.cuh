@@ -15,7 +15,7 @@ __host__ __device__ inline int64_t round_up64(int64_t v, int64_t a) { return (v 
 // What the epilogues need to know about one kept token row.
 struct __align__(16) RowInfo {
     float lse2;                            // log2 of the row's sum of exponentials (backward)
-    float g;                               // dloss * tau (* the fp16 scale of the gradient): backward
+    float g;                               // dloss (* the fp16 scale of the gradient): backward
     int32_t label;                         // cross entropy: the target class
     int32_t row;                           // the row's index in the caller's tensors
 };
@@ -89,6 +89,7 @@ struct GradArgs {                          // dX (+)= dz W, dW = dz^T X for one 
     const int32_t *n_live;
     const RowInfo *rows;
     const Scales *scales;
+    float tau;                             // what the sums over dz are multiplied by
     const void *dz;
     int64_t T, Tpad;
     int32_t d, V, v0, width, ldz;

@@ -100,6 +100,7 @@ struct GradParams {
     const int32_t *n_live;
     const RowInfo *rows;
     const Scales *scales;
+    float tau;
     int64_t Tpad;
     int32_t d, v0, width, ldz;
     int32_t want_dx, want_dw, w_panels;    // w_panels: w can be read as panels of 64 columns
@@ -860,7 +861,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const GradParams &g = p.g;
                 const bool empty = t.kb0 >= t.kb1;     // nothing was contracted: the accumulator holds no result
                 const bool is_dx = t.job == 0;
-                const float scale = PL == 2 ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : mantissa;
+                const float scale = g.tau * (PL == 2 ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : mantissa);
                 const int32_t rows_in = (is_dx ? n_live : g.width) - row0;             // rows of this warp that exist
                 const int splits = is_dx ? g.dx_splits : g.dw_splits;
                 float *slot = is_dx ? g.dx_slots : g.dw_slots;
@@ -1024,7 +1025,7 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
         return TBN_ERR_CUDA;
     KernelParams p = {};
     GradParams &g = p.g;
-    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.ldz = a.ldz;
+    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.tau = a.tau; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.ldz = a.ldz;
     g.want_dx = a.want_dx; g.want_dw = a.want_dw; g.w_panels = w_panels;
     g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
     g.dw = a.dw; g.slot_ld = a.slot_ld; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;

@@ -86,8 +86,8 @@ def assert_close(got, val, bound, what, rows=None):
     if rows is not None:
         got, val, bound = got[rows], val[rows], bound[rows]
     ok = (got - val).abs() <= bound
-    top = float(torch.finfo(torch.float32).max)          # what fp32 and bf16 cannot hold is an infinity of its sign
-    ok |= (val.abs() > top) & (got == val.sign() * math.inf)
+    top = float(torch.finfo(torch.float32).max)          # a value within the bound that fp32 and bf16 cannot hold is an infinity
+    ok |= ((val + bound > top) & (got == math.inf)) | ((val - bound < -top) & (got == -math.inf))
     over = ~ok
     assert not bool(over.any()), (f"{what}: {int(over.sum())} of {over.numel()} outside, worst {float((got - val).abs()[over].nan_to_num(math.inf).max()):.3g}, "
                                   f"first at {over.nonzero()[0].tolist()}: {float(got[over][0]):.6g} for {float(val[over][0]):.6g} +- {float(bound[over][0]):.3g}")
