@@ -18,8 +18,6 @@ __global__ void record_status_kernel(int *status, int code, int detail)
     if (atomicCAS(status, 0, code) == 0) status[1] = detail;
 }
 
-namespace {
-
 int *device_status_ptr()
 {
     // one address per device, looked up lazily (the symbol has a distinct instance on each device)
@@ -33,6 +31,8 @@ int *device_status_ptr()
     }
     return cache[dev];
 }
+
+namespace {
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool valid_dtype(int d) { return d == TBN_F32 || d == TBN_BF16; }
@@ -135,7 +135,7 @@ bool head_sizes_ok(int64_t T, int32_t in_f, int32_t vocab)
     return T >= 0 && in_f > 0 && vocab > 0 && T <= kHeadMost && in_f <= kHeadMost && vocab <= kHeadMost;
 }
 
-int head_call(head::HeadCall &c, bool backward, void *workspace, size_t workspace_bytes, void *stream)
+int head_call(const head::HeadCall &c, bool backward, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (c.T < 0 || c.d <= 0 || c.V <= 0 || !valid_dtype(c.dtype)) return TBN_ERR_INVALID_ARG;
     if (c.K > 0 && (!valid_dtype(c.top_dtype) || !(c.tau >= 1e-30f) || !(c.tau <= 1e30f))) return TBN_ERR_INVALID_ARG;
@@ -159,10 +159,7 @@ int head_call(head::HeadCall &c, bool backward, void *workspace, size_t workspac
     if (c.K > 0 ? (!c.top_index || !c.top_logit) : !c.targets) return TBN_ERR_INVALID_ARG;
     if (backward ? (!c.lse || !c.dloss) : (!c.loss_out || !c.lse_out)) return TBN_ERR_INVALID_ARG;
     if (backward && !c.dx && !c.dw && !c.db) return TBN_OK;
-    if (!workspace || workspace_bytes < head::workspace_bytes(c.T, c.d, c.V, c.dtype, c.K, backward)) return TBN_ERR_WORKSPACE;
-    c.status = device_status_ptr();
-    if (!c.status) return TBN_ERR_CUDA;
-    return backward ? head::backward(c, workspace, s) : head::forward(c, workspace, s);
+    return backward ? head::backward(c, workspace, workspace_bytes, s) : head::forward(c, workspace, workspace_bytes, s);
 }
 
 // Validation shared by the fully-connected and convolution entry points.

@@ -624,18 +624,18 @@ int64_t grads_makespan(int64_t n0, int64_t k0, int64_t n1, int64_t k1, int64_t o
 {
     if (n0 > 0 && (n1 == 0 || k0 >= k1)) { const int64_t n = n0, k = k0; n0 = n1; k0 = k1; n1 = n; k1 = k; }      // 1: the longer
     const int64_t l = k1 + own, sh = k0 + own, a = n1 / pairs, r = n1 % pairs;
-    int64_t t = (a + (r ? 1 : 0)) * l;
-    for (;; ++t) {
-        const int64_t late = r ? (t - (a + 1) * l) / sh : 0, early = (t - a * l) / sh;
-        const int64_t room = r * late + (pairs - r) * early;
-        if (room >= n0) return t;
-        const int64_t missing = (n0 - room) / pairs * sh;             // at least this much longer
-        if (missing > sh) t += missing - sh;
-    }
+    if (r == 0) return a * l + (n0 + pairs - 1) / pairs * sh;
+    // r pairs finish their longer tiles at (a + 1) l, the others at a l.  The answer is one of the times at which a pair of one
+    // kind or the other finishes a shorter tile, whichever comes first with room for all of them.
+    const int64_t first = l / sh, started = (l + sh - 1) / sh;        // shorter tiles of a pair that is early, done and begun by (a + 1) l
+    const int64_t rest = n0 - (pairs - r) * first, late = rest > 0 ? (rest + pairs - 1) / pairs : 0;
+    const int64_t need = (n0 + r * started + pairs - 1) / pairs, early = need > started ? need : started;
+    const int64_t t_late = (a + 1) * l + late * sh, t_early = a * l + early * sh;
+    return t_late < t_early ? t_late : t_early;
 }
 
 // Tile counts follow from the sizes alone; how many tokens are kept is known on the device only.
-Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward, bool dx_bf16)
+Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward)
 {
     Plan p = {};
     p.planes = dtype == TBN_F32 ? 2 : 1;
@@ -691,7 +691,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
             }
             if (mt * nt * i > 4 * pairs) break;
         }
-        p.dx_slots = p.dx_splits > 1 || (p.pieces > 1 && dx_bf16);
+        p.dx_slots = p.dx_splits > 1 || (p.pieces > 1 && dtype == TBN_BF16);
         p.dw_slots = p.dw_splits > 1;
         p.o_dz = take((size_t)p.planes * p.Tpad * p.width * 2);
         p.o_col = take((size_t)(p.Tpad / 32) * p.width * 4);
@@ -731,6 +731,8 @@ unsigned blocks_for(int64_t items, int64_t per_block, int64_t most)
 // Labels, operands and per-row values: everything before the first contraction.
 int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArgs *out, cudaStream_t s)
 {
+    out->status = device_status_ptr();
+    if (!out->status) return TBN_ERR_CUDA;
     int32_t *n_live = reinterpret_cast<int32_t *>(ws + p.o_live);
     Scales *scales = reinterpret_cast<Scales *>(ws + p.o_scales);
     float *max_part = reinterpret_cast<float *>(ws + p.o_max);
@@ -776,7 +778,6 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     out->w = Operand{p.pack_w ? static_cast<const void *>(ws + p.o_w) : c.w, c.V, c.V, w_ld, w_ld};
     out->planes = p.planes; out->bn = p.bn;
     out->bias = c.bias; out->scale2 = kLog2e / c.tau; out->T = c.T; out->Tpad = p.Tpad; out->V = c.V;
-    out->status = c.status;
     if (p.direct) {
         out->x = Operand{c.x, c.T, c.T, c.d, c.d};
         return TBN_OK;
@@ -810,12 +811,13 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
 
 size_t workspace_bytes(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward)
 {
-    return make_plan(T, d, V, dtype, K, backward, true).total;
+    return make_plan(T, d, V, dtype, K, backward).total;
 }
 
-int forward(const HeadCall &c, void *workspace, cudaStream_t s)
+int forward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStream_t s)
 {
-    const Plan p = make_plan(c.T, c.d, c.V, c.dtype, c.K, false, true);
+    const Plan p = make_plan(c.T, c.d, c.V, c.dtype, c.K, false);
+    if (!workspace || workspace_bytes < p.total) return TBN_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     LogitsArgs a = {};
     int rc = prepare(c, p, ws, false, &a, s);
@@ -834,10 +836,11 @@ int forward(const HeadCall &c, void *workspace, cudaStream_t s)
                       (int32_t)c.T, teacher, c.tau, c.loss_out, c.lse_out) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 
-int backward(const HeadCall &c, void *workspace, cudaStream_t s)
+int backward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStream_t s)
 {
-    const bool dx_bf16 = c.dx_dtype == TBN_BF16;
-    const Plan p = make_plan(c.T, c.d, c.V, c.dtype, c.K, true, dx_bf16);
+    const bool dx_bf16 = c.dx_dtype == TBN_BF16;       // dx has the operands' type
+    const Plan p = make_plan(c.T, c.d, c.V, c.dtype, c.K, true);
+    if (!workspace || workspace_bytes < p.total) return TBN_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     LogitsArgs a = {};
     int rc = prepare(c, p, ws, true, &a, s);
@@ -854,7 +857,7 @@ int backward(const HeadCall &c, void *workspace, cudaStream_t s)
     g.dw = c.dw; g.dw_bf16 = c.dw_dtype == TBN_BF16; g.dw_slots = p.dw_slots ? reinterpret_cast<float *>(ws + p.o_dw) : nullptr;
     g.dw_splits = p.dw_splits;
     g.slot_ld = p.ld;
-    g.status = c.status;
+    g.status = a.status;
     for (int32_t piece = 0; piece < p.pieces; ++piece) {
         a.v0 = piece * p.width;
         a.width = c.V - a.v0 < p.width ? c.V - a.v0 : p.width;

@@ -5,6 +5,9 @@
 #include "common.cuh"
 
 namespace tbn {
+
+int *device_status_ptr();                  // the current device's status record (api.cu); null on error
+
 namespace head {
 
 constexpr int kTile = 256;                 // tokens x classes of one output tile (two CTAs, 128 rows each)
@@ -130,12 +133,11 @@ struct HeadCall {
     void *dx, *dw;
     int dx_dtype, dw_dtype;
     float *db;
-    int *status;
 };
 constexpr int32_t kMaxListed = 1024;
 size_t workspace_bytes(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward);
-int forward(const HeadCall &c, void *workspace, cudaStream_t s);
-int backward(const HeadCall &c, void *workspace, cudaStream_t s);
+int forward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStream_t s);
+int backward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStream_t s);
 
 }  // namespace head
 }  // namespace tbn

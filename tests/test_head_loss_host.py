@@ -1,0 +1,25 @@
+"""What a head-loss call costs before anything runs on the GPU: workspace and host time."""
+import time
+
+import pytest
+
+from paper_2407_12075_b200 import binding as B
+from paper_2407_12075_b200 import build as tbn_build
+
+
+@pytest.fixture(scope="module")
+def lib():
+    tbn_build.build()
+    return B.lib()
+
+
+@pytest.mark.parametrize("T,d,V,dtype", [(2100, 64, 9001, B.BF16), (8192, 64, 131072, B.BF16), (4096, 128, 100000, B.BF16), (333, 768, 10007, B.BF16),
+                                         (777, 501, 4999, B.F32), (1, 64, 500000, B.F32), (100000, 2048, 1000, B.BF16)])
+def test_planning_a_backward_takes_little_host_time(lib, T, d, V, dtype):
+    """The splits of the two gradient products are chosen anew in every call: microseconds, beside a launch's two or three."""
+    best = 1.0
+    for _ in range(300):
+        t0 = time.perf_counter()
+        lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 1)
+        best = min(best, time.perf_counter() - t0)
+    assert best < 20e-6, best
