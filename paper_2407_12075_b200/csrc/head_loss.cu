@@ -231,12 +231,14 @@ __device__ __forceinline__ void split16(float v, __half &hi, __half &lo) {
 // Block b < row_blocks owns rows [b * per_block, ...).  It counts the kept rows before its own (re-reading the labels: at
 // most a few hundred blocks, so a few megabytes of L2 reads for tens of thousands of tokens, and no second launch or
 // hand-over between blocks), then packs its rows in order.  The last row block zeroes the rows up to the next multiple of
-// 64, which the weight gradient contracts over.  The blocks behind pack the weights, where they cannot be read in place
-// (fp32, or rows that are not a multiple of 16 bytes).
+// 64, which the weight gradient contracts over.  The blocks behind pack weights, where they cannot be read in place (fp32,
+// or rows that are not a multiple of 16 bytes): all of them, or in the backward one piece of the vocabulary (the later pieces
+// without row blocks), so that the workspace does not grow with the vocabulary.
 struct PackArgs {
     Labels labels;
     int64_t T, Tpad, per_block;
-    int32_t V, d, ld;
+    int32_t w_rows, d, ld;
+    int64_t w_plane_rows;
     unsigned int row_blocks;
     const float *max_part;                 // fp32 only
     int32_t max_blocks;
@@ -326,7 +328,7 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     const int64_t r0 = (int64_t)blockIdx.x * a.per_block, r1 = min(a.T, r0 + a.per_block);       // r0 < T for every row block
     // everything that does not wait for the scales is asked for before they are put together: a weight block's first eight
     // elements, a row block's count of the kept rows before its own
-    const int64_t vecs = a.ld >> 3, groups = a.V * vecs;
+    const int64_t vecs = a.ld >> 3, groups = a.w_rows * vecs;
     const int64_t first = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
     const bool weights = blockIdx.x >= a.row_blocks, early = sizeof(TS) == 4 && weights && a.d % kVec == 0 && first < groups;
     float ahead[8];
@@ -351,15 +353,15 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     }
     const float sx = scale_of(m[0]), sw = scale_of(m[1]), sg = scale_of(m[2]);
     if (blockIdx.x >= a.row_blocks && a.d % kVec != 0) {
-        const int64_t plane = (int64_t)a.V * a.ld;
-        for (int64_t r = (int64_t)(blockIdx.x - a.row_blocks) * 8 + warp; r < a.V; r += (int64_t)(gridDim.x - a.row_blocks) * 8) {
+        const int64_t plane = a.w_plane_rows * a.ld;
+        for (int64_t r = (int64_t)(blockIdx.x - a.row_blocks) * 8 + warp; r < a.w_rows; r += (int64_t)(gridDim.x - a.row_blocks) * 8) {
             uint16_t *dst = a.wc + r * a.ld;
             pack_row(w + r * a.d, a.d, a.ld, sw, lane, dst, dst + plane);
         }
         return;
     }
     if (blockIdx.x >= a.row_blocks) {                  // weights
-        const int64_t plane = (int64_t)a.V * a.ld, stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
+        const int64_t plane = a.w_plane_rows * a.ld, stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
         for (int64_t i = first; i < groups; i += stride) {
             const int64_t r = i / vecs;
             const int32_t c = (int32_t)(i - r * vecs) * 8;
@@ -596,6 +598,7 @@ struct Plan {
     int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
     int32_t unit, units, pitch;            // classes per entry of list_start: an epilogue warp's, more where that is a large table
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
+    int32_t w_rows;                        // weights packed at a time
     bool direct;
     int64_t Tpad;
     bool dx_slots, dw_slots;
@@ -655,7 +658,6 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     p.o_max = take(3 * kMaxBlocks * 4);
     p.o_rows = take(p.direct ? 0 : (size_t)p.Tpad * sizeof(RowInfo));
     p.o_x = take(p.direct ? 0 : (size_t)p.planes * p.Tpad * p.ld * 2);
-    p.o_w = take(p.pack_w ? (size_t)p.planes * V * p.ld * 2 : 0);
     p.o_list = take((size_t)T * K * 8);
     p.o_flags = take(K > 0 ? (size_t)T : 0);
     p.o_teacher = take(K > 0 ? (size_t)T * 8 : 0);
@@ -698,6 +700,8 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.o_dx = take(p.dx_slots ? (size_t)p.dx_splits * p.Tpad * p.ld * 4 : 0);
         p.o_dw = take(p.dw_slots ? (size_t)p.dw_splits * p.width * p.ld * 4 : 0);
     }
+    p.w_rows = backward && p.width < V ? p.width : V;
+    p.o_w = take(p.pack_w ? (size_t)p.planes * p.w_rows * p.ld * 2 : 0);
     if (K > 0) {
         p.unit = p.bn / groups;
         while (V / p.unit >= kMaxUnits || (T * (V / p.unit) > ((int64_t)1 << 26) && V / p.unit > 1)) p.unit *= 2;
@@ -728,6 +732,29 @@ unsigned blocks_for(int64_t items, int64_t per_block, int64_t most)
     return (unsigned)(b < 1 ? 1 : b > most ? most : b);
 }
 
+// Blocks that look for the largest magnitudes.
+unsigned max_blocks(const HeadCall &c)
+{
+    const int64_t most = (int64_t)(c.V > c.T ? c.V : c.T) * c.d;
+    return c.dtype == TBN_F32 ? blocks_for(most, 4096, kMaxBlocks) : 0u;
+}
+
+// The packing launch: the rows that `a` asks for, and the weights of the piece that begins at class v0.
+cudaError_t pack(const HeadCall &c, const Plan &p, char *ws, PackArgs a, int32_t v0, cudaStream_t s)
+{
+    a.w_rows = c.V - v0 < p.w_rows ? c.V - v0 : p.w_rows;
+    a.w_plane_rows = p.w_rows; a.d = c.d; a.ld = p.ld;
+    a.wc = reinterpret_cast<uint16_t *>(ws + p.o_w);
+    a.max_part = reinterpret_cast<float *>(ws + p.o_max);
+    a.max_blocks = (int32_t)max_blocks(c);
+    const unsigned blocks = a.row_blocks + (p.pack_w ? blocks_for((int64_t)a.w_rows * (p.ld / 8), 256, 2368) : 0u);
+    const int64_t w0 = (int64_t)v0 * c.d;
+    return c.dtype == TBN_F32 ? launch_pdl(pack_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x),
+                                           static_cast<const float *>(c.w) + w0, a)
+                              : launch_pdl(pack_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s,
+                                           static_cast<const __nv_bfloat16 *>(c.x), static_cast<const __nv_bfloat16 *>(c.w) + w0, a);
+}
+
 // Labels, operands and per-row values: everything before the first contraction.
 int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArgs *out, cudaStream_t s)
 {
@@ -741,9 +768,8 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     Labels labels = {c.targets, c.ignore_index, c.V, nullptr};
     MaxArgs max_args = {};
     if (f32) {
-        const int64_t count = (int64_t)c.V * c.d, most = count > c.T * c.d ? count : c.T * c.d;
-        max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T, count,
-                           c.d, max_part, blocks_for(most, 4096, kMaxBlocks)};
+        max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T,
+                           (int64_t)c.V * c.d, c.d, max_part, max_blocks(c)};
     }
 
     if (c.K > 0) {
@@ -775,7 +801,7 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     }
     out->labels = labels;
     const int32_t w_ld = p.pack_w ? p.ld : c.d;
-    out->w = Operand{p.pack_w ? static_cast<const void *>(ws + p.o_w) : c.w, c.V, c.V, w_ld, w_ld};
+    out->w = Operand{p.pack_w ? static_cast<const void *>(ws + p.o_w) : c.w, p.pack_w ? p.w_rows : c.V, p.pack_w ? p.w_rows : c.V, w_ld, w_ld};
     out->planes = p.planes; out->bn = p.bn;
     out->bias = c.bias; out->scale2 = kLog2e / c.tau; out->T = c.T; out->Tpad = p.Tpad; out->V = c.V;
     if (p.direct) {
@@ -783,25 +809,19 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         return TBN_OK;
     }
     PackArgs a = {};
-    a.max_blocks = (int32_t)max_args.blocks;
     if (f32 && c.K == 0 && launch_spread(abs_max_kernel, dim3(max_args.blocks), dim3(256), 0, s, max_args, labels) != cudaSuccess)
         return TBN_ERR_CUDA;
-    a.labels = labels; a.T = c.T; a.Tpad = p.Tpad; a.V = c.V; a.d = c.d; a.ld = p.ld;
+    a.labels = labels; a.T = c.T; a.Tpad = p.Tpad;
     a.per_block = (c.T + 591) / 592 < 8 ? 8 : (c.T + 591) / 592;
     a.row_blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);              // the last one has rows of its own
-    a.max_part = max_part; a.xc = reinterpret_cast<uint16_t *>(ws + p.o_x); a.wc = reinterpret_cast<uint16_t *>(ws + p.o_w);
+    a.xc = reinterpret_cast<uint16_t *>(ws + p.o_x);
     a.rows = rows; a.n_live = n_live; a.scales = scales;
     if (backward) {
         a.lse = c.lse; a.dloss = c.dloss; a.dx = c.dx; a.dx_bytes = c.dx_dtype == TBN_F32 ? 4 : 2;
     } else {
         a.loss_out = c.loss_out; a.lse_out = c.lse_out;
     }
-    const unsigned blocks = a.row_blocks + (p.pack_w ? blocks_for((int64_t)c.V * (p.ld / 8), 256, 2368) : 0u);
-    const cudaError_t e = f32 ? launch_pdl(pack_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x),
-                                           static_cast<const float *>(c.w), a)
-                              : launch_pdl(pack_kernel<__nv_bfloat16>, dim3(blocks), dim3(256), 0, s,
-                                           static_cast<const __nv_bfloat16 *>(c.x), static_cast<const __nv_bfloat16 *>(c.w), a);
-    if (e != cudaSuccess) return TBN_ERR_CUDA;
+    if (pack(c, p, ws, a, 0, s) != cudaSuccess) return TBN_ERR_CUDA;
     out->x = Operand{ws + p.o_x, p.Tpad, p.Tpad, p.ld, p.ld};
     out->n_live = n_live; out->rows = rows; out->scales = f32 ? scales : nullptr;
     return TBN_OK;
@@ -861,6 +881,9 @@ int backward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStr
     for (int32_t piece = 0; piece < p.pieces; ++piece) {
         a.v0 = piece * p.width;
         a.width = c.V - a.v0 < p.width ? c.V - a.v0 : p.width;
+        a.w_row0 = g.w_row0 = p.pack_w ? 0 : a.v0;
+        if (p.pack_w) a.w.rows = g.w.rows = a.width;
+        if (p.pack_w && piece > 0 && pack(c, p, ws, PackArgs{}, a.v0, s) != cudaSuccess) return TBN_ERR_CUDA;
         rc = launch_head_dz(a, s);
         if (rc != TBN_OK) return rc;
         const bool grads = g.want_dx || g.want_dw, last = piece == p.pieces - 1;

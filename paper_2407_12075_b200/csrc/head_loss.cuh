@@ -61,6 +61,7 @@ int sm_count();
 
 struct LogitsArgs {                        // logits of all kept tokens against classes [v0, v0 + width)
     Operand x, w;
+    int32_t w_row0;                        // w's row of class v0 (0 where w is packed for one piece at a time)
     int planes;
     const int32_t *n_live;                 // null: the T rows in their own order (forward)
     const RowInfo *rows;                   // null with n_live
@@ -88,6 +89,7 @@ int launch_head_dz(const LogitsArgs &a, cudaStream_t s);
 
 struct GradArgs {                          // dX (+)= dz W, dW = dz^T X for one piece of the vocabulary
     Operand x, w;
+    int32_t w_row0;                        // as in LogitsArgs
     int planes;
     const int32_t *n_live;
     const RowInfo *rows;

@@ -86,7 +86,7 @@ struct LogitsParams {
     const float *bias;
     float scale2;
     int64_t Tpad;
-    int32_t V, v0, width;
+    int32_t V, v0, width, w_row0;          // w_row0: w's row of class v0
     const int2 *list;                      // distillation: [T][K] (class, probability) pairs, ascending; else null
     const uint16_t *list_start;            // [T][pitch]: where the classes of each unit begin in the row's list
     int32_t K, unit, units, pitch;
@@ -102,7 +102,7 @@ struct GradParams {
     const Scales *scales;
     float tau;
     int64_t Tpad;
-    int32_t d, v0, width, ldz;
+    int32_t d, v0, width, w_row0, ldz;
     int32_t want_dx, want_dw, w_panels;    // w_panels: w can be read as panels of 64 columns
     void *dx;
     float *dx_slots;
@@ -533,7 +533,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((second ? 2 : 1) * a_bytes + 2 * b_bytes), leader);
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
-                        if (!is_a) tma_load_pair(sb + pl * b_bytes, map, kb * 64, p.l.v0 + r0, pl, bar, leader);
+                        if (!is_a) tma_load_pair(sb + pl * b_bytes, map, kb * 64, p.l.w_row0 + r0, pl, bar, leader);
                         else if (load_a) tma_load_pair(sa + pl * a_bytes, map, kb * 64, r0, pl, bar, leader);
                     }
                 } else {
@@ -542,7 +542,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 #pragma unroll
                     for (int pl = 0; pl < PL; ++pl) {
                         const uint32_t dst = is_a ? sa + pl * kSideBytes : sb + pl * kBBytes;
-                        const int32_t krow = (job == 0 ? p.g.v0 : 0) + kb * 64;
+                        const int32_t krow = (job == 0 ? p.g.w_row0 : 0) + kb * 64;
                         if (is_a) {
                             if (!load_a) continue;
                             if (job == 0) tma_load_pair(dst, map, 0, r0, kb, pl, bar, leader);
@@ -977,7 +977,7 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     const int64_t stage = (int64_t)a.planes * (rows * 128 + a.bn * 64), fit = (kStageBudget - kSideBytes + rows * 128) / stage;
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
     l.scales = a.scales;
-    l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width;
+    l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width; l.w_row0 = a.w_row0;
     l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.unit = a.unit; l.units = a.units; l.pitch = a.pitch;
     l.part = a.part; l.parts = a.parts;
     l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
@@ -1025,7 +1025,7 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
         return TBN_ERR_CUDA;
     KernelParams p = {};
     GradParams &g = p.g;
-    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.tau = a.tau; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.ldz = a.ldz;
+    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.tau = a.tau; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.w_row0 = a.w_row0; g.ldz = a.ldz;
     g.want_dx = a.want_dx; g.want_dw = a.want_dw; g.w_panels = w_panels;
     g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
     g.dw = a.dw; g.slot_ld = a.slot_ld; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;

@@ -23,3 +23,11 @@ def test_planning_a_backward_takes_little_host_time(lib, T, d, V, dtype):
         lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 1)
         best = min(best, time.perf_counter() - t0)
     assert best < 20e-6, best
+
+
+def test_packed_weights_of_the_backward_are_bounded(lib):
+    """Weights that cannot be read in place are packed for one piece of the vocabulary at a time."""
+    T = 4096
+    for dtype, d in ((B.F32, 1024), (B.BF16, 1001)):
+        small, large = (lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 1) for V in (1 << 18, 1 << 21))
+        assert large < small + (128 << 20)
