@@ -161,9 +161,8 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  * (in the backward its dloss of 0 does not help: 0 times NaN is NaN, in its row of dx and in dw).
  *
  * x: T x in_f, w: vocab x in_f, both of `dtype` (TBN_BF16 or TBN_F32).  bias: vocab floats or NULL.  targets: T int64.
- * loss, lse: T floats.  Products are accumulated in fp32; fp32 operands are contracted as two fp16 halves of 11 bits each
- * under a common power of two (about 22 bits of every element, ending at 2^-38 of the tensor's largest magnitude; dz, in
- * the backward, under that of the largest tau * |dloss|).
+ * loss, lse: T floats.  Products are accumulated in fp32; fp32 operands (and in the backward dz) are contracted as three bf16
+ * parts, which hold all 24 bits of every element down to 2^-133.  Logits whose size over tau exceeds 2^127 count as infinite.
  *
  * tbn_linear_xent_bwd, tbn_linear_distill_bwd: lse as the forward wrote it, dloss: T floats (dL/dloss[t]: 1/T for a mean).
  *     dz[t][v] = dloss[t] * tau * (q[t][v] - sum_{j: top_index[t][j] = v} p[t][j])       (cross entropy: one entry, p = 1, tau = 1)

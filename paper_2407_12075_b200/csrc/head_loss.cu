@@ -8,13 +8,12 @@
 //                             (held without tau, which the sums over it are multiplied by: it may be anything from 1e-30 to 1e30)
 //
 // Cross entropy is distillation from one entry of probability 1, so both share every kernel; only where the entries come
-// from differs.  The logits are never stored: the forward keeps one (maximum, sum, weighted dot) triple per token and 128
-// classes, the backward recomputes the logits piece by piece of the vocabulary and stores dz for one piece at a time.
+// from differs.  The logits are never stored: the forward keeps one (maximum, sum, weighted dot) record of 16 bytes per token
+// and 128 classes (64 with fp32 operands, fewer in narrow tiles), the backward recomputes the logits piece by piece of the
+// vocabulary and stores dz for one piece at a time.
 //
 // Tokens that are left out (ignored targets, empty teacher rows) are dropped first: the kept rows are packed to the front,
 // so no kernel computes anything for the others and nothing in their rows -- infinities, NaN -- can reach a result.
-#include <cuda_fp16.h>
-
 #include <climits>
 
 #include "head_loss.cuh"
@@ -38,75 +37,6 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// ---- fp32 operands: largest magnitudes ------------------------------------------------------------------
-// max_part[0..2][block]: the blocks' max |x| over the kept rows, max |w|, max |dloss| over the kept rows, of the finite
-// ones: an infinity must not change how the other tokens are rounded.
-constexpr int kMaxBlocks = 592;
-
-struct MaxArgs {
-    const float *x, *w, *dloss;            // dloss: backward
-    int64_t T, w_count;
-    int32_t d;
-    float *max_part;
-    unsigned int blocks;
-};
-// The block's maxima of three values that are not negative (up to eight warps).
-__device__ __forceinline__ void block_max(float (&v)[3]) {
-    __shared__ float part[3][8];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) v[k] = warp_max(v[k]);
-    if (lane < 3) part[lane][warp] = lane == 0 ? v[0] : lane == 1 ? v[1] : v[2];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 3; ++k) v[k] = warp_max((lane & 7) < warps ? part[k][lane & 7] : 0.0f);
-}
-__device__ __forceinline__ float max_finite(float m, float v) {
-    v = fabsf(v);
-    return v < INFINITY ? fmaxf(m, v) : m;
-}
-__device__ __forceinline__ float max4(float m, float4 v) {
-    return max_finite(max_finite(max_finite(max_finite(m, v.x), v.y), v.z), v.w);
-}
-// Run by block `block` of a.blocks; live(t) is asked by whole warps.
-template <typename Live>
-__device__ __forceinline__ void abs_max(const MaxArgs &a, unsigned int block, Live live)
-{
-    const int64_t tid = (int64_t)block * blockDim.x + threadIdx.x, threads = (int64_t)a.blocks * blockDim.x;
-    float mw = 0.0f, mx = 0.0f, mg = 0.0f;
-    const int64_t w4 = a.w_count >> 2;
-    const float4 *wv = reinterpret_cast<const float4 *>(a.w);
-    int64_t i = tid;
-    for (; i + 3 * threads < w4; i += 4 * threads) {
-        const float4 v0 = __ldg(wv + i), v1 = __ldg(wv + i + threads), v2 = __ldg(wv + i + 2 * threads), v3 = __ldg(wv + i + 3 * threads);
-        mw = max4(max4(max4(max4(mw, v0), v1), v2), v3);
-    }
-    for (; i < w4; i += threads) mw = max4(mw, __ldg(wv + i));
-    for (i = (w4 << 2) + tid; i < a.w_count; i += threads) mw = max_finite(mw, a.w[i]);
-    __syncwarp();
-    const int lane = threadIdx.x & 31;
-    for (int64_t t = tid >> 5; t < a.T; t += threads >> 5) {
-        if (!live(t)) continue;
-#pragma unroll 4
-        for (int32_t c = lane; c < a.d; c += 32) mx = max_finite(mx, a.x[t * a.d + c]);
-        if (a.dloss && lane == 0) mg = max_finite(mg, a.dloss[t]);
-        __syncwarp();
-    }
-    float m[3] = {mx, mw, mg};
-    block_max(m);
-    if (threadIdx.x == 0) {
-#pragma unroll
-        for (int k = 0; k < 3; ++k) a.max_part[k * kMaxBlocks + block] = m[k];
-    }
-}
-__global__ void __launch_bounds__(256)
-abs_max_kernel(const MaxArgs a, const Labels labels)
-{
-    pdl_launch_dependents();
-    pdl_wait();
-    abs_max(a, blockIdx.x, [&](int64_t t) { return labels.live(t); });
-}
-
 // ---- the teacher's entries ---------------------------------------------------------------------------
 // One warp per token: p = softmax(logit / tau) over the entries whose index is a class and whose logit is above
 // -infinity, sum p log p, and the entries sorted by class (by position among equals), which is the order in which the
@@ -119,8 +49,7 @@ template <typename TL>
 __global__ void __launch_bounds__(128)
 teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, int64_t T, int32_t K, int32_t Kp, int32_t V,
                float inv_tau, int32_t unit, int32_t units, int32_t pitch, int2 *__restrict__ list, uint16_t *__restrict__ list_start,
-               uint8_t *__restrict__ flags, float2 *__restrict__ stats,
-               unsigned int list_blocks, const MaxArgs max_args)
+               uint8_t *__restrict__ flags, float2 *__restrict__ stats)
 {
     extern __shared__ __align__(16) uint8_t teacher_mem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -130,17 +59,6 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     uint16_t *start = reinterpret_cast<uint16_t *>(teacher_mem + (size_t)warps * Kp * 12) + (size_t)warp * pitch;
     pdl_launch_dependents();
     pdl_wait();
-    if (blockIdx.x >= list_blocks) {                   // fp32 operands: the blocks behind look for the largest magnitudes
-        abs_max(max_args, blockIdx.x - list_blocks, [&](int64_t row) {
-            bool some = false;
-            for (int32_t j = lane; j < K; j += 32) {
-                const int64_t c = index[row * K + j];
-                some |= c >= 0 && c < V && !(load_as_float(logit, row * K + j) == -INFINITY);
-            }
-            return __any_sync(0xffffffffu, some) != 0;
-        });
-        return;
-    }
     const int64_t t = (int64_t)blockIdx.x * warps + warp;
     if (t >= T) return;
     float top = -INFINITY;
@@ -213,21 +131,22 @@ teacher_kernel(const int64_t *__restrict__ index, const TL *__restrict__ logit, 
     }
 }
 
-// The power of two that takes the largest magnitude to [2^14, 2^15): the high part of every element then keeps 11 bits
-// and the remainder another 11, down to 2^-39 of the largest one, below which fp16 ends.  All zero: 1.
-__device__ __forceinline__ float scale_of(float m) {
-    if (!(m > 0.0f)) return 1.0f;
-    int e = (int)(__float_as_uint(m) >> 23) - 127;     // subnormal maxima: -127, clamped below
-    e = e > 60 ? 60 : e < -60 ? -60 : e;
-    return __uint_as_float((unsigned int)(127 + 14 - e) << 23);
-}
-__device__ __forceinline__ void split16(float v, __half &hi, __half &lo) {
-    hi = __float2half_rn(v);
-    lo = __float2half_rn(v - __half2float(hi));
+// The three bf16 parts of a value, each rounded to nearest from what the ones before leave over: 24 bits, down to 2^-133, where
+// bf16 ends.  A first part that rounding up would take out of the range is the largest bf16.
+__device__ __forceinline__ void split3(float v, uint16_t &hi, uint16_t &mid, uint16_t &lo) {
+    constexpr float kLargest = 3.38953139e38f;         // 2^128 - 2^120
+    __nv_bfloat16 h = __float2bfloat16_rn(v);
+    if (fabsf(v) > kLargest && fabsf(v) < INFINITY) h = __float2bfloat16_rn(copysignf(kLargest, v));
+    float r = v - __bfloat162float(h);
+    const __nv_bfloat16 m = __float2bfloat16_rn(r);
+    r -= __bfloat162float(m);
+    hi = __bfloat16_as_ushort(h);
+    mid = __bfloat16_as_ushort(m);
+    lo = __bfloat16_as_ushort(__float2bfloat16_rn(r));
 }
 
 // ---- operands in the form the contractions read ---------------------------------------------------------------
-// Rows padded to 16 bytes, fp32 as two fp16 planes.  Activations are always packed: the kept tokens come to the front.
+// Rows padded to 16 bytes, fp32 as three bf16 planes.  Activations are always packed: the kept tokens come to the front.
 // Block b < row_blocks owns rows [b * per_block, ...).  It counts the kept rows before its own (re-reading the labels: at
 // most a few hundred blocks, so a few megabytes of L2 reads for tens of thousands of tokens, and no second launch or
 // hand-over between blocks), then packs its rows in order.  The last row block zeroes the rows up to the next multiple of
@@ -240,61 +159,46 @@ struct PackArgs {
     int32_t w_rows, d, ld;
     int64_t w_plane_rows;
     unsigned int row_blocks;
-    const float *max_part;                 // fp32 only
-    int32_t max_blocks;
     uint16_t *xc, *wc;
     RowInfo *rows;
     int32_t *n_live;
-    Scales *scales;                        // fp32 only: written here for the kernels that follow
     const float *lse, *dloss;              // backward
     float *loss_out, *lse_out;             // forward: zeroed for the tokens left out
     void *dx;                              // backward: rows zeroed for the tokens left out (or null)
     int dx_bytes;
 };
 
-// eight elements of a row from column c, zeros from column d on
+// eight elements of a row from column c, zeros from column d on; dst: their place in the first plane
 template <typename TS>
-__device__ __forceinline__ void load8(const TS *__restrict__ src, int32_t c, int32_t d, float (&v)[8]) {
-    if (sizeof(TS) == 4 && d % 4 == 0 && c + 8 <= d) {
-        const float4 a = __ldg(reinterpret_cast<const float4 *>(src + c)), b = __ldg(reinterpret_cast<const float4 *>(src + c) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < d ? load_as_float(src, c + j) : 0.0f;
-    }
-}
-template <typename TS>
-__device__ __forceinline__ void pack8(const TS *__restrict__ src, int32_t c, int32_t d, float scale, uint16_t *hi_dst, uint16_t *lo_dst,
-                                      const float (*given)[8] = nullptr) {
-    alignas(16) uint16_t hi[8], lo[8];
+__device__ __forceinline__ void pack8(const TS *__restrict__ src, int32_t c, int32_t d, uint16_t *dst, int64_t plane) {
+    alignas(16) uint16_t hi[8], mid[8], lo[8];
     if (sizeof(TS) == 2 && d % 8 == 0 && c + 8 <= d) {
         *reinterpret_cast<uint4 *>(hi) = __ldg(reinterpret_cast<const uint4 *>(src + c));
     } else {
         float v[8];
-        if (given) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = (*given)[j];
+        if (sizeof(TS) == 4 && d % 4 == 0 && c + 8 <= d) {
+            const float4 a = __ldg(reinterpret_cast<const float4 *>(src + c)), b = __ldg(reinterpret_cast<const float4 *>(src + c) + 1);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
-            load8(src, c, d, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = c + j < d ? load_as_float(src, c + j) : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (sizeof(TS) == 4) {
-                __half h, l;
-                split16(v[j] * scale, h, l);
-                hi[j] = __half_as_ushort(h); lo[j] = __half_as_ushort(l);
-            } else {
-                hi[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
-            }
+            if (sizeof(TS) == 4) split3(v[j], hi[j], mid[j], lo[j]);
+            else hi[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
         }
     }
-    *reinterpret_cast<uint4 *>(hi_dst) = *reinterpret_cast<const uint4 *>(hi);
-    if (sizeof(TS) == 4) *reinterpret_cast<uint4 *>(lo_dst) = *reinterpret_cast<const uint4 *>(lo);
+    *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(hi);
+    if (sizeof(TS) == 4) {
+        *reinterpret_cast<uint4 *>(dst + plane) = *reinterpret_cast<const uint4 *>(mid);
+        *reinterpret_cast<uint4 *>(dst + 2 * plane) = *reinterpret_cast<const uint4 *>(lo);
+    }
 }
 
 // A whole row by a warp, lane = column: for rows that are not a multiple of 16 bytes.
 template <typename TS>
-__device__ __forceinline__ void pack_row(const TS *__restrict__ src, int32_t d, int32_t ld, float scale, int lane, uint16_t *hi_dst, uint16_t *lo_dst) {
+__device__ __forceinline__ void pack_row(const TS *__restrict__ src, int32_t d, int32_t ld, int lane, uint16_t *dst, int64_t plane) {
     for (int32_t c0 = lane; c0 < ld; c0 += 256) {
         float v[8];
 #pragma unroll
@@ -303,14 +207,8 @@ __device__ __forceinline__ void pack_row(const TS *__restrict__ src, int32_t d, 
         for (int j = 0; j < 8; ++j) {
             const int32_t c = c0 + 32 * j;
             if (c >= ld) break;
-            if (sizeof(TS) == 4) {
-                __half h, l;
-                split16(v[j] * scale, h, l);
-                hi_dst[c] = __half_as_ushort(h);
-                lo_dst[c] = __half_as_ushort(l);
-            } else {
-                hi_dst[c] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
-            }
+            if (sizeof(TS) == 4) split3(v[j], dst[c], dst[plane + c], dst[2 * plane + c]);
+            else dst[c] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
         }
     }
 }
@@ -326,51 +224,23 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
     pdl_wait();
     constexpr int kVec = 16 / sizeof(TS);              // rows in whole 16-byte pieces
     const int64_t r0 = (int64_t)blockIdx.x * a.per_block, r1 = min(a.T, r0 + a.per_block);       // r0 < T for every row block
-    // everything that does not wait for the scales is asked for before they are put together: a weight block's first eight
-    // elements, a row block's count of the kept rows before its own
-    const int64_t vecs = a.ld >> 3, groups = a.w_rows * vecs;
-    const int64_t first = (int64_t)(blockIdx.x - a.row_blocks) * 256 + threadIdx.x;
-    const bool weights = blockIdx.x >= a.row_blocks, early = sizeof(TS) == 4 && weights && a.d % kVec == 0 && first < groups;
-    float ahead[8];
-    if (early) {
-        const int64_t r = first / vecs;
-        load8(w + r * a.d, (int32_t)(first - r * vecs) * 8, a.d, ahead);
-    }
-    int mine = 0;
-    if (!weights) {
-#pragma unroll 8
-        for (int64_t t = threadIdx.x; t < r0; t += 256) mine += a.labels.live(t) ? 1 : 0;
-    }
-    float m[3] = {0.0f, 0.0f, 0.0f};
-    if (sizeof(TS) == 4) {
-#pragma unroll
-        for (int u = 0; u < (kMaxBlocks + 255) / 256; ++u) {
-            const int i = u * 256 + threadIdx.x;
-#pragma unroll
-            for (int k = 0; k < 3; ++k) m[k] = fmaxf(m[k], i < a.max_blocks ? a.max_part[k * kMaxBlocks + i] : 0.0f);
-        }
-        block_max(m);
-    }
-    const float sx = scale_of(m[0]), sw = scale_of(m[1]), sg = scale_of(m[2]);
-    if (blockIdx.x >= a.row_blocks && a.d % kVec != 0) {
-        const int64_t plane = a.w_plane_rows * a.ld;
-        for (int64_t r = (int64_t)(blockIdx.x - a.row_blocks) * 8 + warp; r < a.w_rows; r += (int64_t)(gridDim.x - a.row_blocks) * 8) {
-            uint16_t *dst = a.wc + r * a.ld;
-            pack_row(w + r * a.d, a.d, a.ld, sw, lane, dst, dst + plane);
-        }
-        return;
-    }
+    const int64_t vecs = a.ld >> 3;
     if (blockIdx.x >= a.row_blocks) {                  // weights
-        const int64_t plane = a.w_plane_rows * a.ld, stride = (int64_t)(gridDim.x - a.row_blocks) * 256;
-        for (int64_t i = first; i < groups; i += stride) {
+        const int64_t plane = a.w_plane_rows * a.ld, block = blockIdx.x - a.row_blocks, blocks = gridDim.x - a.row_blocks;
+        if (a.d % kVec != 0) {
+            for (int64_t r = block * 8 + warp; r < a.w_rows; r += blocks * 8) pack_row(w + r * a.d, a.d, a.ld, lane, a.wc + r * a.ld, plane);
+            return;
+        }
+        for (int64_t i = block * 256 + threadIdx.x; i < a.w_rows * vecs; i += blocks * 256) {
             const int64_t r = i / vecs;
             const int32_t c = (int32_t)(i - r * vecs) * 8;
-            uint16_t *dst = a.wc + r * a.ld + c;
-            pack8(w + r * a.d, c, a.d, sw, dst, dst + plane, early && i == first ? &ahead : nullptr);
+            pack8(w + r * a.d, c, a.d, a.wc + r * a.ld + c, plane);
         }
         return;
     }
-    if (sizeof(TS) == 4 && blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{sx, sw, sg, 1.0f / sx, 1.0f / sw, 1.0f / sg};
+    int mine = 0;
+#pragma unroll 8
+    for (int64_t t = threadIdx.x; t < r0; t += 256) mine += a.labels.live(t) ? 1 : 0;
     mine = __reduce_add_sync(0xffffffffu, mine);
     if (lane == 0) warp_count[warp] = mine;
     __syncthreads();
@@ -391,7 +261,7 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
         if (live) {
             RowInfo info;
             info.lse2 = a.lse ? a.lse[t] * kLog2e : 0.0f;
-            info.g = a.dloss ? a.dloss[t] * sg : 0.0f;
+            info.g = a.dloss ? a.dloss[t] : 0.0f;
             info.label = a.labels.flags ? -1 : (int32_t)a.labels.target[t];
             info.row = (int32_t)t;
             a.rows[at] = info;
@@ -417,7 +287,7 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
             uint16_t *dst = a.xc + (int64_t)to * a.ld;
             const TS *src = x + from * a.d;
             if (a.d % kVec != 0) {
-                pack_row(src, a.d, a.ld, sx, lane, dst, dst + plane);
+                pack_row(src, a.d, a.ld, lane, dst, plane);
                 continue;
             }
             int32_t c = lane * 8;
@@ -430,7 +300,7 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
                     for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4 *>(dst + c + k * 256) = v[k];
                 }
             }
-            for (; c < a.ld; c += 256) pack8(src, c, a.d, sx, dst + c, dst + plane + c);
+            for (; c < a.ld; c += 256) pack8(src, c, a.d, dst + c, plane);
         }
     }
     if (blockIdx.x == a.row_blocks - 1) {
@@ -438,8 +308,8 @@ pack_kernel(const TS *__restrict__ x, const TS *__restrict__ w, const PackArgs a
         const int64_t end = (base + 63) / 64 * 64;
         for (int64_t i = threadIdx.x; i < (end - base) * vecs; i += 256) {
             uint4 *p = reinterpret_cast<uint4 *>(a.xc + base * a.ld) + i;
-            *p = make_uint4(0u, 0u, 0u, 0u);
-            if (sizeof(TS) == 4) *(p + (plane >> 3)) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int pl = 0; pl < (sizeof(TS) == 4 ? 3 : 1); ++pl) p[pl * (plane >> 3)] = make_uint4(0u, 0u, 0u, 0u);
         }
     }
 }
@@ -510,8 +380,8 @@ combine_kernel(const float4 *__restrict__ part, int32_t parts, const int32_t *__
 struct FinishArgs {
     const int32_t *n_live;
     const RowInfo *rows;
-    const Scales *scales;
     float tau;
+    int32_t planes;
     // db[v0 + c] = sum over the 32-row groups of the kept tokens (bias_blocks blocks of 32 classes)
     const float *col_part;
     int32_t ldz, width;
@@ -523,10 +393,10 @@ struct FinishArgs {
     int64_t dw_slot_rows, dx_slot_rows;
     void *dw, *dx;                         // dw: the piece's first row
 };
-// The sums of the splits' rows, four columns per thread.  Flat over all of them: the rows are few, and a warp per row has too
+// The sums of the splits' rows, times scale, four columns per thread.  Flat over all of them: the rows are few, and a warp per row has too
 // few loads in flight (13 us where this takes 5).
 __device__ __forceinline__ void join_splits(const float *slots, int32_t splits, int64_t slot_rows, int32_t d, int32_t ld, int64_t n,
-                                            const RowInfo *rows, void *out, int bf16, int64_t first, int64_t stride) {
+                                            const RowInfo *rows, float scale, void *out, int bf16, int64_t first, int64_t stride) {
     const int64_t per_row = (d + 3) / 4, total = n * per_row, split_stride = slot_rows * ld;
     for (int64_t i = first; i < total; i += stride) {
         const int64_t r = total <= 0x7fffffff ? (int64_t)((uint32_t)i / (uint32_t)per_row) : i / per_row;
@@ -538,6 +408,7 @@ __device__ __forceinline__ void join_splits(const float *slots, int32_t splits, 
             const float4 v = *reinterpret_cast<const float4 *>(src + k * split_stride);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
+        s.x *= scale; s.y *= scale; s.z *= scale; s.w *= scale;
         const int64_t at = (rows ? (int64_t)rows[r].row : r) * d + c;
         if (d % 4 == 0) {
             if (bf16) {
@@ -565,6 +436,7 @@ finish_kernel(const FinishArgs a)
     pdl_launch_dependents();
     pdl_wait();
     unsigned int b = blockIdx.x;
+    const float scale = a.tau * (a.planes == 1 ? common_mantissa(a.rows, *a.n_live) : 1.0f);
     if (b < a.bias_blocks) {
         const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
         const int32_t groups = (*a.n_live + 31) / 32, c = b * 32 + lane;
@@ -575,18 +447,18 @@ finish_kernel(const FinishArgs a)
         __syncthreads();
         if (g == 0 && c < a.width) {
             for (int i = 1; i < 8; ++i) s += sum[i][lane];
-            a.db[c] = s * a.tau * (a.scales ? a.scales->inv_g : common_mantissa(a.rows, *a.n_live));
+            a.db[c] = s * scale;
         }
         return;
     }
     b -= a.bias_blocks;
     if (b < a.dw_blocks) {
-        join_splits(a.dw_slots, a.dw_splits, a.dw_slot_rows, a.d, a.ld, a.width, nullptr, a.dw, a.dw_bf16, (int64_t)b * 256 + threadIdx.x,
+        join_splits(a.dw_slots, a.dw_splits, a.dw_slot_rows, a.d, a.ld, a.width, nullptr, scale, a.dw, a.dw_bf16, (int64_t)b * 256 + threadIdx.x,
                     (int64_t)a.dw_blocks * 256);
         return;
     }
     b -= a.dw_blocks;
-    join_splits(a.dx_slots, a.dx_splits, a.dx_slot_rows, a.d, a.ld, *a.n_live, a.rows, a.dx, a.dx_bf16, (int64_t)b * 256 + threadIdx.x,
+    join_splits(a.dx_slots, a.dx_splits, a.dx_slot_rows, a.d, a.ld, *a.n_live, a.rows, scale, a.dx, a.dx_bf16, (int64_t)b * 256 + threadIdx.x,
                 (int64_t)a.dx_blocks * 256);
 }
 
@@ -595,14 +467,14 @@ inline size_t pad256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Plan {
     int planes, pack_w;
-    int32_t cols;                          // widest tile: 256 classes or columns, 128 with two planes
+    int32_t cols;                          // widest tile: 256 classes or columns, 128 with three planes
     int32_t unit, units, pitch;            // classes per entry of list_start: an epilogue warp's, more where that is a large table
     int32_t ld, bn, parts, width, pieces, dx_splits, dw_splits;
     int32_t w_rows;                        // weights packed at a time
     bool direct;
     int64_t Tpad;
     bool dx_slots, dw_slots;
-    size_t o_live, o_scales, o_max, o_rows, o_x, o_w, o_list, o_start, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
+    size_t o_live, o_rows, o_x, o_w, o_list, o_start, o_flags, o_teacher, o_part, o_dz, o_col, o_dx, o_dw, total;
 };
 
 // Classes per tile of a logits launch: the width whose whole rounds over the SM pairs cost least.  A round costs what it
@@ -641,9 +513,9 @@ int64_t grads_makespan(int64_t n0, int64_t k0, int64_t n1, int64_t k1, int64_t o
 Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backward)
 {
     Plan p = {};
-    p.planes = dtype == TBN_F32 ? 2 : 1;
+    p.planes = dtype == TBN_F32 ? 3 : 1;
     p.cols = dtype == TBN_F32 ? 128 : 256;
-    const int32_t groups = dtype == TBN_F32 ? 4 : 2;   // epilogue warps that share a tile's columns
+    constexpr int32_t groups = 2;                      // epilogue warps that share a tile's columns
     p.ld = (d + 63) / 64 * 64;                         // packed rows are whole 64-column panels
     p.pack_w = dtype == TBN_F32 || d % 8 != 0;
     p.Tpad = round_up64(T, kTile);
@@ -654,8 +526,6 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
     size_t o = 0;
     auto take = [&o](size_t bytes) { const size_t at = o; o += pad256(bytes); return at; };
     p.o_live = take(4);
-    p.o_scales = take(sizeof(Scales));
-    p.o_max = take(3 * kMaxBlocks * 4);
     p.o_rows = take(p.direct ? 0 : (size_t)p.Tpad * sizeof(RowInfo));
     p.o_x = take(p.direct ? 0 : (size_t)p.planes * p.Tpad * p.ld * 2);
     p.o_list = take((size_t)T * K * 8);
@@ -675,19 +545,19 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
         p.bn = classes_per_tile(T, V < p.width ? V : p.width, p.cols, 128, 64);       // whole chunks of 32 classes per warp
         // A contraction is split when its few tiles would outlast the rest of the launch.  A split adds its share of the
         // fp32 partial sums, written here and read by the pass that joins them: 8 bytes per element and split at a few
-        // TB/s, about 1 step per 2 M elements.  A tile costs about 10 steps beside its products, 6 of the three-product
-        // form's (64 x 512 x 30000, whole gradient: counted as 6 steps, 14 splits and 68 us; as 12, 9 splits and 59 us;
-        // 1024 x 512 x 1000 in fp32: as 6, 2 + 2 splits and 36.9 us; as 12, none and 38.9 us).
+        // TB/s, about 1 step per 2 M elements.  A tile costs about 10 steps beside its products (64 x 512 x 30000, whole
+        // gradient: counted as 6 steps, 14 splits and 68 us; as 12, 9 splits and 59 us).  A step of the six-product form takes
+        // three times as long.
         const int64_t nt = (d + p.cols - 1) / p.cols, mt = p.Tpad / kTile, vt = (V < p.width ? round_up64(V, kTile) : p.width) / kTile;
         const int64_t kx = p.width / 64, kw = (T + 63) / 64, pairs = sm_count() > 1 ? sm_count() / 2 : 74;
-        const int64_t own = p.planes == 1 ? 10 : 6;
+        const int64_t own = p.planes == 1 ? 10 : 3, per_step = (p.planes == 1 ? 2 : 6) << 20;
         int64_t best = INT64_MAX;
         p.dx_splits = p.dw_splits = 1;
         for (int32_t i = 1; i <= kMaxSplits && (i == 1 || 2 * i <= kx); ++i) {
             for (int32_t j = 1; j <= kMaxSplits && (j == 1 || 2 * j <= kw); ++j) {
                 if (j > 1 && vt * nt * j > 4 * pairs) break;
                 const int64_t join = (i > 1 ? i * p.Tpad * d : 0) + (j > 1 ? j * vt * kTile * d : 0);
-                const int64_t c = grads_makespan(mt * nt * i, (kx + i - 1) / i, vt * nt * j, (kw + j - 1) / j, own, pairs) + (join >> 21) +
+                const int64_t c = grads_makespan(mt * nt * i, (kx + i - 1) / i, vt * nt * j, (kw + j - 1) / j, own, pairs) + join / per_step +
                                   (join > 0 ? own : 0);
                 if (c < best) { best = c; p.dx_splits = i; p.dw_splits = j; }
             }
@@ -715,9 +585,8 @@ Plan make_plan(int64_t T, int32_t d, int32_t V, int dtype, int32_t K, bool backw
 
 // The first kernel of a call that has the GPU's every SM to fill, launched the ordinary way.  Launched early (launch_pdl), its
 // blocks are placed while the kernel before it still holds most SMs with its shared memory, all on the few that are free, and
-// stay there: the teacher's lists of 512 tokens took 26 us that way and take 9.6, those of 2048 tokens 25 and 10.8; the largest
-// magnitudes of 1024 x 512 x 1000 lose nothing by it (step 55.2 and 53.7 us).  The packing kernel after it is better off early
-// (6.7 and 4.9 us).
+// stay there: the teacher's lists of 512 tokens took 26 us that way and take 9.6, those of 2048 tokens 25 and 10.8.  The packing
+// kernel after it is better off early (6.7 and 4.9 us).
 template <typename... KArgs, typename... Args>
 cudaError_t launch_spread(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args)
 {
@@ -732,21 +601,12 @@ unsigned blocks_for(int64_t items, int64_t per_block, int64_t most)
     return (unsigned)(b < 1 ? 1 : b > most ? most : b);
 }
 
-// Blocks that look for the largest magnitudes.
-unsigned max_blocks(const HeadCall &c)
-{
-    const int64_t most = (int64_t)(c.V > c.T ? c.V : c.T) * c.d;
-    return c.dtype == TBN_F32 ? blocks_for(most, 4096, kMaxBlocks) : 0u;
-}
-
 // The packing launch: the rows that `a` asks for, and the weights of the piece that begins at class v0.
 cudaError_t pack(const HeadCall &c, const Plan &p, char *ws, PackArgs a, int32_t v0, cudaStream_t s)
 {
     a.w_rows = c.V - v0 < p.w_rows ? c.V - v0 : p.w_rows;
     a.w_plane_rows = p.w_rows; a.d = c.d; a.ld = p.ld;
     a.wc = reinterpret_cast<uint16_t *>(ws + p.o_w);
-    a.max_part = reinterpret_cast<float *>(ws + p.o_max);
-    a.max_blocks = (int32_t)max_blocks(c);
     const unsigned blocks = a.row_blocks + (p.pack_w ? blocks_for((int64_t)a.w_rows * (p.ld / 8), 256, 2368) : 0u);
     const int64_t w0 = (int64_t)v0 * c.d;
     return c.dtype == TBN_F32 ? launch_pdl(pack_kernel<float>, dim3(blocks), dim3(256), 0, s, static_cast<const float *>(c.x),
@@ -761,34 +621,25 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     out->status = device_status_ptr();
     if (!out->status) return TBN_ERR_CUDA;
     int32_t *n_live = reinterpret_cast<int32_t *>(ws + p.o_live);
-    Scales *scales = reinterpret_cast<Scales *>(ws + p.o_scales);
-    float *max_part = reinterpret_cast<float *>(ws + p.o_max);
     RowInfo *rows = reinterpret_cast<RowInfo *>(ws + p.o_rows);
-    const bool f32 = c.dtype == TBN_F32;
     Labels labels = {c.targets, c.ignore_index, c.V, nullptr};
-    MaxArgs max_args = {};
-    if (f32) {
-        max_args = MaxArgs{static_cast<const float *>(c.x), static_cast<const float *>(c.w), backward ? c.dloss : nullptr, c.T,
-                           (int64_t)c.V * c.d, c.d, max_part, max_blocks(c)};
-    }
 
     if (c.K > 0) {
         int32_t Kp = 32;
         while (Kp < c.K) Kp <<= 1;
         const int warps = teacher_warps(Kp);
         const size_t smem = teacher_smem(Kp, p.pitch) * warps;
-        const unsigned list_blocks = (unsigned)((c.T + warps - 1) / warps);
-        const dim3 grid(list_blocks + max_args.blocks);
+        const dim3 grid((unsigned)((c.T + warps - 1) / warps));
         int2 *list = reinterpret_cast<int2 *>(ws + p.o_list);
         uint8_t *flags = reinterpret_cast<uint8_t *>(ws + p.o_flags);
         float2 *stats = reinterpret_cast<float2 *>(ws + p.o_teacher);
         uint16_t *start = reinterpret_cast<uint16_t *>(ws + p.o_start);
         const cudaError_t e = c.top_dtype == TBN_F32
             ? launch_spread(teacher_kernel<float>, grid, dim3(32 * warps), smem, s, c.top_index, static_cast<const float *>(c.top_logit),
-                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats, list_blocks, max_args)
+                         c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units, p.pitch, list, start, flags, stats)
             : launch_spread(teacher_kernel<__nv_bfloat16>, grid, dim3(32 * warps), smem, s, c.top_index,
                          static_cast<const __nv_bfloat16 *>(c.top_logit), c.T, c.K, Kp, c.V, 1.0f / c.tau, p.unit, p.units,
-                         p.pitch, list, start, flags, stats, list_blocks, max_args);
+                         p.pitch, list, start, flags, stats);
         if (e != cudaSuccess) return TBN_ERR_CUDA;
         labels.flags = flags;
         labels.target = nullptr;
@@ -809,13 +660,11 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
         return TBN_OK;
     }
     PackArgs a = {};
-    if (f32 && c.K == 0 && launch_spread(abs_max_kernel, dim3(max_args.blocks), dim3(256), 0, s, max_args, labels) != cudaSuccess)
-        return TBN_ERR_CUDA;
     a.labels = labels; a.T = c.T; a.Tpad = p.Tpad;
     a.per_block = (c.T + 591) / 592 < 8 ? 8 : (c.T + 591) / 592;
     a.row_blocks = (unsigned)((c.T + a.per_block - 1) / a.per_block);              // the last one has rows of its own
     a.xc = reinterpret_cast<uint16_t *>(ws + p.o_x);
-    a.rows = rows; a.n_live = n_live; a.scales = scales;
+    a.rows = rows; a.n_live = n_live;
     if (backward) {
         a.lse = c.lse; a.dloss = c.dloss; a.dx = c.dx; a.dx_bytes = c.dx_dtype == TBN_F32 ? 4 : 2;
     } else {
@@ -823,7 +672,7 @@ int prepare(const HeadCall &c, const Plan &p, char *ws, bool backward, LogitsArg
     }
     if (pack(c, p, ws, a, 0, s) != cudaSuccess) return TBN_ERR_CUDA;
     out->x = Operand{ws + p.o_x, p.Tpad, p.Tpad, p.ld, p.ld};
-    out->n_live = n_live; out->rows = rows; out->scales = f32 ? scales : nullptr;
+    out->n_live = n_live; out->rows = rows;
     return TBN_OK;
 }
 
@@ -870,7 +719,7 @@ int backward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStr
     a.col_part = c.db ? reinterpret_cast<float *>(ws + p.o_col) : nullptr;
 
     GradArgs g = {};
-    g.x = a.x; g.w = a.w; g.planes = a.planes; g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.tau = c.tau; g.dz = a.dz;
+    g.x = a.x; g.w = a.w; g.planes = a.planes; g.n_live = a.n_live; g.rows = a.rows; g.tau = c.tau; g.dz = a.dz;
     g.T = c.T; g.Tpad = p.Tpad; g.d = c.d; g.V = c.V; g.ldz = p.width;
     g.want_dx = c.dx != nullptr; g.want_dw = c.dw != nullptr;
     g.dx = c.dx; g.dx_bf16 = dx_bf16; g.dx_slots = p.dx_slots ? reinterpret_cast<float *>(ws + p.o_dx) : nullptr; g.dx_splits = p.dx_splits;
@@ -895,7 +744,7 @@ int backward(const HeadCall &c, void *workspace, size_t workspace_bytes, cudaStr
             if (rc != TBN_OK) return rc;
         }
         FinishArgs f = {};
-        f.n_live = a.n_live; f.rows = a.rows; f.scales = a.scales; f.tau = c.tau; f.d = c.d; f.ld = p.ld; f.width = a.width;
+        f.n_live = a.n_live; f.rows = a.rows; f.tau = c.tau; f.planes = p.planes; f.d = c.d; f.ld = p.ld; f.width = a.width;
         if (c.db) {
             f.col_part = a.col_part; f.ldz = a.ldz; f.db = c.db + a.v0;
             f.bias_blocks = (unsigned)((a.width + 31) / 32);

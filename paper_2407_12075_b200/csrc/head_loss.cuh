@@ -18,7 +18,7 @@ __host__ __device__ inline int64_t round_up64(int64_t v, int64_t a) { return (v 
 // What the epilogues need to know about one kept token row.
 struct __align__(16) RowInfo {
     float lse2;                            // log2 of the row's sum of exponentials (backward)
-    float g;                               // dloss (* the fp16 scale of the gradient): backward
+    float g;                               // dloss (backward)
     int32_t label;                         // cross entropy: the target class
     int32_t row;                           // the row's index in the caller's tensors
 };
@@ -34,10 +34,7 @@ __device__ __forceinline__ float common_mantissa(const RowInfo *rows, int32_t n_
 }
 #endif
 
-// Powers of two that bring the fp32 operands into the range of fp16 (all 1 for bf16 operands), and their inverses.
-struct Scales { float x, w, g, inv_x, inv_w, inv_g; };
-
-// A bf16 (one plane) or fp32 (two fp16 planes: high part, remainder) operand as the contractions read it.
+// A bf16 (one plane) or fp32 (three bf16 planes: the value's first, second and third eight bits) operand as the contractions read it.
 struct Operand {
     const void *data;
     int64_t rows, plane_rows;              // rows that exist, rows between two planes
@@ -67,7 +64,6 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const RowInfo *rows;                   // null with n_live
     Labels labels;                         // used without rows
     int32_t bn;                            // classes of a tile: a multiple of 32 up to 256 (backward: of 32 per epilogue warp)
-    const Scales *scales;                  // null: all 1
     const float *bias;                     // V or null
     float scale2;                          // log2(e) / tau
     int64_t T, Tpad;
@@ -75,7 +71,7 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const int2 *list;                      // distillation: [T][K] (class, probability), ascending, INT32_MAX behind the last; else null
     const uint16_t *list_start;            // [T][pitch]: where the units + 1 units of classes begin in a row's list
     int32_t K, unit, units, pitch;
-    // forward: (maximum, sum, dot, unused) of every token and epilogue warp's classes (bn / 2, or bn / 4 with two planes): [Tpad][parts]
+    // forward: (maximum, sum, dot, unused) of every token and epilogue warp's classes (bn / 2): [Tpad][parts]
     float4 *part;
     int32_t parts;
     // backward
@@ -93,7 +89,6 @@ struct GradArgs {                          // dX (+)= dz W, dW = dz^T X for one 
     int planes;
     const int32_t *n_live;
     const RowInfo *rows;
-    const Scales *scales;
     float tau;                             // what the sums over dz are multiplied by
     const void *dz;
     int64_t T, Tpad;

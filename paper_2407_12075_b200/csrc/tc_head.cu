@@ -12,26 +12,25 @@
 // step, so a byte staged feeds twice the multiplications of a 128 x 256 tile on one CTA (per 64-element step and SM:
 // 32 KB instead of 48 KB for the same 4.2 MFLOP), which is what keeps shared memory and L2 below the tensor pipe.
 // Warp roles per CTA: 0 = TMA producer of A, 1 = MMA issuer (the first CTA of the pair only), 2 = TMA producer of B, 3 idle,
-// 4-11 (two planes: 4-19) = epilogue, two (four) warps per tensor-memory quadrant, 128 (32) columns each.  Two accumulators of
-// 256 columns: the epilogue of a tile runs beside the main loop of the next.
+// 4-11 = epilogue, two warps per tensor-memory quadrant, half of the tile's columns each.  Two accumulators of 256 columns (fp32:
+// four of 128): the epilogue of a tile runs beside the main loop of the next.
 //
 // dz lives in blocks that are images of the shared-memory tiles: panels of 64 classes, in a panel one 128-byte line per
 // token, the 16-byte pieces of a line permuted by the low three bits of the token as the 128-byte swizzle of tcgen05 wants
 // them.  The same 8 KB of 64 tokens x 64 classes is a K-major tile for dX and an MN-major tile for dW, and every tile is one
 // or two contiguous reads.
 //
-// fp32 operands come as two fp16 planes (x = hi + lo to 22 bits after a power-of-two scale); the products lo*hi, hi*lo and
-// hi*hi are accumulated, the dropped lo*lo is below 2^-22 of the result.  The tensor core cuts its running sum off toward
-// zero at every 16-element step, an error that grows with the length of the chain (measured, dot products of 1024: 2.6e-6
-// of the result's scale as one chain of 192 steps, 7e-7 for the bf16 form's 64), so with fp32 operands a chain ends after
-// 128 elements, the small products first, and the epilogue warps add the chains in registers, rounding to nearest.  For that
-// the tiles are 256 x 128 (32 running sums per thread) on four accumulators: with 256 x 256 and two, the hand-overs of a
-// chain (commit, wait, read, release) outlast its MMAs.
+// fp32 operands come as three bf16 planes, x = hi + mid + lo to its 24 bits, with the exponents of fp32 and no scale: nothing in a
+// tensor changes how another of its elements is held.  Six products are accumulated, the smallest first: lo*hi and hi*lo, then
+// mid*mid, mid*hi and hi*mid, then hi*hi; what is dropped is below 2^-22 of |x||w|.  (Two fp16 planes under one power of two per
+// tensor need three products, but one large element then costs all others their bits, and entries of dz below 2^-39 of
+// the largest vanish, which is all that the classes nobody is trained on have.)  The tensor core cuts its running sum off
+// toward zero at every 16-element step, an error that grows with the length of the chain, so a chain ends after 64 elements and
+// the epilogue warps add the chains in registers, rounding to nearest.  The tiles are 256 x 128 (64 running sums per thread) on four
+// accumulators.  A stage is one plane of both operands: eight fit, and each is free again when its products are done.
 //
 // Same conventions as the other tcgen05 kernels: every wait is bounded, a wait that gives up records the status and the
 // kernel winds down and returns.
-#include <cuda_fp16.h>
-
 #include <atomic>
 #include <climits>
 
@@ -59,12 +58,10 @@ enum { kStats = 0, kDz = 1, kGrads = 2 };
 template <int PL> constexpr int kCols = PL == 1 ? 256 : 128;
 template <int PL> constexpr int kAccs = 512 / kCols<PL>;
 // epilogue warps: kGroups per tensor-memory quadrant, which share a tile's columns
-template <int PL> constexpr int kGroups = PL == 1 ? 2 : 4;
-template <int PL> constexpr int kEpiWarps = 4 * kGroups<PL>;
-template <int PL> constexpr int kThreads = 128 + 32 * kEpiWarps<PL>;
-template <int PL> constexpr int kWarpCols = kCols<PL> / kGroups<PL>;
+constexpr int kGroups = 2, kEpiWarps = 4 * kGroups, kThreads = 128 + 32 * kEpiWarps;
+template <int PL> constexpr int kWarpCols = kCols<PL> / kGroups;
 // behind the stages: exchange lines, or the biases of every epilogue warp's columns
-template <int MODE, int PL> constexpr uint32_t kScratch = kEpiWarps<PL> * (MODE == kGrads ? kExchange : kWarpCols<PL> * sizeof(float));
+template <int MODE, int PL> constexpr uint32_t kScratch = kEpiWarps * (MODE == kGrads ? kExchange : kWarpCols<PL> * sizeof(float));
 
 struct Control {
     uint64_t full[kMaxStages], empty[kMaxStages], d_full[4], d_empty[4];
@@ -82,7 +79,6 @@ struct LogitsParams {
     int32_t n_rows;
     int32_t bn;                            // classes of a tile: a multiple of 32 from 64 to 256
     int32_t a_rows, stages;                // token rows of a CTA's tile that are loaded; pipeline stages
-    const Scales *scales;
     const float *bias;
     float scale2;
     int64_t Tpad;
@@ -99,7 +95,6 @@ struct LogitsParams {
 struct GradParams {
     const int32_t *n_live;
     const RowInfo *rows;
-    const Scales *scales;
     float tau;
     int64_t Tpad;
     int32_t d, v0, width, w_row0, ldz;
@@ -370,9 +365,12 @@ __device__ __forceinline__ void ld_global_v8(const float *ptr, float (&v)[8]) {
                  : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "l"(ptr) : "memory");
 }
 // Where a warp's rows of dX or dW go.  prev: fp32 values added first, or null; row, prev_row: this lane's row in out and prev.
+// scale: what the whole sum is multiplied by, 1 for a part of it (parts of sums that are too large for fp32 would meet as
+// infinities of both signs).
 struct RowsOut {
     void *out;
     const float *prev;
+    float scale;
     int32_t row, prev_row, ld, prev_ld, rows_in, end;      // end: the first column that is not this warp's
 };
 // 32 columns of every lane's row, in whole 32-byte sectors (rows a multiple of 16 elements, 32-byte aligned).  The columns
@@ -390,6 +388,8 @@ __device__ __forceinline__ void write_sectors(const RowsOut &o, int lane, int32_
             for (int j = 0; j < 8; ++j) v[8 * q + j] += w[j];
         }
     }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] *= o.scale;
     const int64_t at = (int64_t)o.row * o.ld + c0;
     if (out_bf16) {
 #pragma unroll
@@ -441,6 +441,7 @@ __device__ __forceinline__ void write_elements(const RowsOut &o, uint32_t exchan
                     const int32_t from = __shfl_sync(0xffffffffu, o.prev_row, r);
                     if (r < o.rows_in && c < o.end) x[k] += o.prev[(int64_t)from * o.prev_ld + c];
                 }
+                x[k] *= o.scale;
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -457,15 +458,14 @@ __device__ __forceinline__ void write_elements(const RowsOut &o, uint32_t exchan
 
 // ---- the kernel ------------------------------------------------------------------------------------------
 template <int MODE, int PL, bool BIAS>
-__global__ void __launch_bounds__(kThreads<PL>, 1) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kThreads, 1) __cluster_dims__(2, 1, 1)
 head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelParams p, const int32_t k_logits)
 {
+    static_assert(PL == 1 || PL == 3, "bf16, or the three parts of fp32");
     constexpr uint32_t kBBytes = kCols<PL> * 64;       // B of a gradient tile: one plane, one CTA
-    constexpr uint32_t kStage = PL * (kSideBytes + kBBytes);
-    constexpr int kFewStages = kStageBudget / kStage;
-    constexpr uint32_t kFmt = PL == 1 ? 1u : 0u;       // bf16, or fp16 planes
-    // instruction descriptor: D fp32, M = 256, N added per tile; bits 15 / 16 select the MN-major form of A / B
-    constexpr uint32_t kIdesc = (1u << 4) | (kFmt << 7) | (kFmt << 10) | ((uint32_t)(kTile >> 4) << 24);
+    constexpr int kFewStages = kStageBudget / (kSideBytes + kBBytes);
+    // instruction descriptor: D fp32, A and B bf16, M = 256, N added per tile; bits 15 / 16 select the MN-major form of A / B
+    constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 4) << 24);
     // 128-byte swizzle, 8-row groups 1024 bytes apart, descriptor version 1
     constexpr uint32_t kDescHi = 64u | (1u << 14) | (2u << 29);
 
@@ -482,7 +482,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     if (MODE == kDz) pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-        for (int s = 0; s < kAccs<PL>; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps<PL>); }
+        for (int s = 0; s < kAccs<PL>; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
         ctl->abort_flag = 0;
         fence_barrier_init();
         fence_proxy_async();
@@ -509,7 +509,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
     // reaches the accumulator rows of tokens that do not exist.)
     const uint32_t a_bytes = MODE == kGrads ? kSideBytes : (uint32_t)p.l.a_rows * 128;
     const uint32_t b_bytes = MODE == kGrads ? kBBytes : (uint32_t)p.l.bn * 64;
-    const uint32_t stage_bytes = PL * (a_bytes + b_bytes);
+    const uint32_t stage_bytes = a_bytes + b_bytes;    // one plane
     const uint32_t n_stages = MODE == kGrads ? kFewStages : (uint32_t)p.l.stages;
 
     if (warp == 0 || warp == 2) {
@@ -525,37 +525,33 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             const CUtensorMap *map = is_a ? &maps.a[job] : &maps.b[job];
             // A half tile of rows that do not exist is not loaded: what the second CTA holds instead reaches no result
             const bool second = t.m0 + 128 < (job == 0 ? n_live : p.g.width), load_a = rank == 0 || second;
-            for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
-                ok = wait_bar(smem_u32(&ctl->empty[px.stage]), px.phase ^ 1u, abort_flag, p.status, (40 << 24) | (px.stage << 16) | detail);
-                if (!ok) break;
-                const uint32_t bar = bar0 + px.stage * 8, sa = sm0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
-                if (MODE != kGrads) {
-                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((second ? 2 : 1) * a_bytes + 2 * b_bytes), leader);
+            for (int32_t kb = t.kb0; ok && kb < t.kb1; ++kb) {
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) {
-                        if (!is_a) tma_load_pair(sb + pl * b_bytes, map, kb * 64, p.l.w_row0 + r0, pl, bar, leader);
-                        else if (load_a) tma_load_pair(sa + pl * a_bytes, map, kb * 64, r0, pl, bar, leader);
-                    }
-                } else {
-                    // dX: dz as 128 tokens x 64 classes, dW: as two panels of 64 tokens x 64 classes
-                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, PL * ((second ? 2 : 1) * kSideBytes + 2 * kBBytes), leader);
-#pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) {
-                        const uint32_t dst = is_a ? sa + pl * kSideBytes : sb + pl * kBBytes;
+                for (int u = 0; u < PL; ++u) {
+                    const int pl = PL == 1 ? 0 : u == 0 ? 2 : u - 1;             // lo, hi, mid: in the order of their first use
+                    ok = wait_bar(smem_u32(&ctl->empty[px.stage]), px.phase ^ 1u, abort_flag, p.status, (40 << 24) | (px.stage << 16) | detail);
+                    if (!ok) break;
+                    const uint32_t bar = bar0 + px.stage * 8, sa = sm0 + px.stage * stage_bytes, sb = sa + a_bytes;
+                    if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, (second ? 2 : 1) * a_bytes + 2 * b_bytes, leader);
+                    if (MODE != kGrads) {
+                        if (!is_a) tma_load_pair(sb, map, kb * 64, p.l.w_row0 + r0, pl, bar, leader);
+                        else if (load_a) tma_load_pair(sa, map, kb * 64, r0, pl, bar, leader);
+                    } else {
+                        // dX: dz as 128 tokens x 64 classes, dW: as two panels of 64 tokens x 64 classes
                         const int32_t krow = (job == 0 ? p.g.w_row0 : 0) + kb * 64;
                         if (is_a) {
-                            if (!load_a) continue;
-                            if (job == 0) tma_load_pair(dst, map, 0, r0, kb, pl, bar, leader);
-                            else tma_load_pair(dst, map, 0, kb * 64, r0 / 64, pl, bar, leader);
+                            if (!load_a) {}
+                            else if (job == 0) tma_load_pair(sa, map, 0, r0, kb, pl, bar, leader);
+                            else tma_load_pair(sa, map, 0, kb * 64, r0 / 64, pl, bar, leader);
                         } else if (job == 1 || p.g.w_panels) {
-                            tma_load_pair(dst, map, r0 & 63, krow, r0 >> 6, pl, bar, leader);
+                            tma_load_pair(sb, map, r0 & 63, krow, r0 >> 6, pl, bar, leader);
                         } else {                       // rows that are not whole panels
-                            tma_load_pair(dst, map, r0, krow, pl, bar, leader);
-                            tma_load_pair(dst + kSideBytes / 2, map, r0 + 64, krow, pl, bar, leader);
+                            tma_load_pair(sb, map, r0, krow, pl, bar, leader);
+                            tma_load_pair(sb + kSideBytes / 2, map, r0 + 64, krow, pl, bar, leader);
                         }
                     }
+                    px.advance(n_stages);
                 }
-                px.advance(n_stages);
             }
         }
         if (!ok) {                                     // let copies in flight land before the shared memory goes away
@@ -594,34 +590,42 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                         px.advance(n_stages);
                     }
                 } else {
-                    for (int32_t kb = t.kb0; kb < t.kb1; kb += 2) {              // one chain: 128 elements
-                        const int n = min(2, t.kb1 - kb);
+                    // the products of part i of A and part j of B: four MMAs
+                    auto product = [&](uint32_t d_addr, const Pipe &a, const Pipe &b, uint32_t accumulate) {
+                        const uint32_t sa = stage0 + a.stage * stage_bytes, sb = stage0 + b.stage * stage_bytes + a_bytes;
+                        const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
+#pragma unroll
+                        for (int st = 0; st < 4; ++st)
+                            mma_pair(d_addr, a_lo + st * a_step, b_lo + st * b_step, kDescHi, idesc, st > 0 ? 1u : accumulate, leader);
+                    };
+                    auto loaded = [&](const Pipe &s) {
+                        return wait_bar(smem_u32(&ctl->full[s.stage]), s.phase, abort_flag, p.status, (42 << 24) | (s.stage << 16) | detail);
+                    };
+                    for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {                 // one chain: 64 elements
                         ok = wait_bar(smem_u32(&ctl->d_empty[pd.stage]), pd.phase ^ 1u, abort_flag, p.status, (41 << 24) | detail);
-                        const uint32_t d_addr = tmem_u + pd.stage * kCols<PL>;
-                        Pipe pi = px;
-                        for (int i = 0; i < n && ok; ++i) {                      // lo*hi, hi*lo
-                            ok = wait_bar(smem_u32(&ctl->full[pi.stage]), pi.phase, abort_flag, p.status, (42 << 24) | (pi.stage << 16) | detail);
-                            if (!ok) break;
-                            tc_fence_after();
-                            const uint32_t sa = stage0 + pi.stage * stage_bytes, sb = sa + PL * a_bytes;
-                            const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
-#pragma unroll
-                            for (int st = 0; st < 4; ++st)
-                                mma_pair(d_addr, a_lo + (a_bytes >> 4) + st * a_step, b_lo + st * b_step, kDescHi, idesc, st > 0 || i > 0 ? 1u : 0u, leader);
-#pragma unroll
-                            for (int st = 0; st < 4; ++st)
-                                mma_pair(d_addr, a_lo + st * a_step, b_lo + (b_bytes >> 4) + st * b_step, kDescHi, idesc, 1u, leader);
-                            pi.advance(n_stages);
-                        }
                         if (!ok) break;
-                        for (int i = 0; i < n; ++i) {                            // hi*hi
-                            const uint32_t sa = stage0 + px.stage * stage_bytes, sb = sa + PL * a_bytes;
-                            const uint32_t a_lo = ((sa & 0x3FFFFu) >> 4) | a_hi, b_lo = ((sb & 0x3FFFFu) >> 4) | b_hi;
-#pragma unroll
-                            for (int st = 0; st < 4; ++st) mma_pair(d_addr, a_lo + st * a_step, b_lo + st * b_step, kDescHi, idesc, 1u, leader);
-                            commit_pair(smem_u32(&ctl->empty[px.stage]), leader);
-                            px.advance(n_stages);
-                        }
+                        const uint32_t d_addr = tmem_u + pd.stage * kCols<PL>;
+                        Pipe lo = px;
+                        px.advance(n_stages);
+                        Pipe hi = px;
+                        px.advance(n_stages);
+                        Pipe mid = px;
+                        px.advance(n_stages);
+                        ok = loaded(lo) && loaded(hi);
+                        if (!ok) break;
+                        tc_fence_after();
+                        product(d_addr, lo, hi, 0u);
+                        product(d_addr, hi, lo, 1u);
+                        commit_pair(smem_u32(&ctl->empty[lo.stage]), leader);
+                        ok = loaded(mid);
+                        if (!ok) break;
+                        tc_fence_after();
+                        product(d_addr, mid, mid, 1u);
+                        product(d_addr, mid, hi, 1u);
+                        product(d_addr, hi, mid, 1u);
+                        commit_pair(smem_u32(&ctl->empty[mid.stage]), leader);
+                        product(d_addr, hi, hi, 1u);
+                        commit_pair(smem_u32(&ctl->empty[hi.stage]), leader);
                         commit_pair(smem_u32(&ctl->d_full[pd.stage]), leader);
                         pd.advance(kAccs<PL>);
                     }
@@ -644,13 +648,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
         const uint32_t t_lane = tmem_base + ((uint32_t)(qd * 32) << 16);
         const uint32_t exchange = stage0 + kStageBudget + (uint32_t)ew * kExchange;
         Pipe pd;
-        float sc = 1.0f, inv_g = 1.0f;
-        if (MODE != kGrads) {
-            sc = p.l.scale2;
-            if (p.l.scales) sc *= p.l.scales->inv_x * p.l.scales->inv_w;
-        } else if (p.g.scales) {
-            inv_g = p.g.scales->inv_g;
-        }
+        const float sc = MODE != kGrads ? p.l.scale2 : 1.0f;
         const float mantissa = PL == 1 && MODE != kStats ? common_mantissa(MODE == kDz ? p.l.rows : p.g.rows, n_live) : 1.0f;
         // what a tile needs to know about this lane's row, asked for while the tile before it is worked on
         auto row_info = [&](const Tile &u) {
@@ -675,7 +673,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             t = next;
             const RowInfo info = next_info;
             const int32_t row0 = t.m0 + (int32_t)rank * 128 + qd * 32, row = row0 + lane;
-            const int32_t hc = t.bn / kGroups<PL>, col0 = t.n0 + group * hc;
+            const int32_t hc = t.bn / kGroups, col0 = t.n0 + group * hc;
             const bool live = row < n_live;
             // rows that nothing is written for: dz has zeros up to the next 64 tokens, which dW contracts over
             const int32_t row_end = MODE == kDz ? (n_live + 63) & ~63 : MODE == kGrads && t.job == 1 ? p.g.width : n_live;
@@ -694,28 +692,29 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
             }
             more = sched.get<MODE, PL>(step + 1, next);
             if (more) next_info = row_info(next);
-            // the tile's sums: left in tensor memory, or (two planes) added up from its 128-element chains in registers
-            float acc[PL == 2 ? kWarpCols<PL> : 1];
+            // the tile's sums: left in tensor memory, or (three planes) added up from its 64-element chains in registers
+            float acc[PL == 3 ? 64 : 1];
             uint32_t t_acc = 0;
-            if (PL == 1) {
+            if constexpr (PL == 1) {
                 ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                 if (!ok) break;
                 tc_fence_after();
                 t_acc = t_lane + pd.stage * kCols<PL> + (uint32_t)(group * hc);
             } else {
 #pragma unroll
-                for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] = 0.0f;
-                for (int32_t kb = t.kb0; kb < t.kb1; kb += 2) {
+                for (int j = 0; j < 64; ++j) acc[j] = 0.0f;
+                for (int32_t kb = t.kb0; kb < t.kb1; ++kb) {
                     ok = wait_bar(smem_u32(&ctl->d_full[pd.stage]), pd.phase, abort_flag, p.status, (43 << 24) | detail);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t t_sum = t_lane + pd.stage * kCols<PL> + (uint32_t)(group * hc);
                     if (chunks) {
-                        uint32_t r[32];
+                        uint32_t r[32], r2[32];        // of a narrow tile, up to 32 columns behind its own are read and not used
                         tmem_ld_32x32(t_sum, r);
+                        tmem_ld_32x32(t_sum + 32, r2);
                         tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) acc[PL == 2 ? j : 0] += __uint_as_float(r[j]);
+                        for (int j = 0; j < 32; ++j) { acc[j] += __uint_as_float(r[j]); acc[32 + j] += __uint_as_float(r2[j]); }
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -735,7 +734,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if ((ch + 1) * 32 < hc) tmem_ld_32x32(t_acc + (ch + 1) * 32, ahead);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) out[j] = acc[PL == 2 ? j : 0];
+                    for (int j = 0; j < 32; ++j) out[j] = ch == 0 ? acc[j] : acc[32 + j];
                 }
             };
 
@@ -833,25 +832,27 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                         for (int j = 0; j < 32; ++j) v[j] = live ? v[j] : 0.0f;
                     }
                     uint16_t *dst = dz + ((int64_t)(c0 >> 6) * p.l.Tpad + row) * 64;
-                    uint32_t pk[16], lo[PL == 2 ? 16 : 1];
+                    if (p.l.col_part) {
+                        float sum[32];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        if (PL == 1) {
+                        for (int j = 0; j < 32; ++j) sum[j] = v[j];
+                        const float s = column_sums(sum, lane);
+                        p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
+                    }
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl) {  // the parts of fp32: each of what the ones before leave over
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
                             const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
                             pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-                        } else {
-                            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-                            const float2 back = __half22float2(h);
-                            const __half2 r = __floats2half2_rn(v[2 * i] - back.x, v[2 * i + 1] - back.y);
-                            pk[i] = *reinterpret_cast<const uint32_t *>(&h);
-                            lo[PL == 2 ? i : 0] = *reinterpret_cast<const uint32_t *>(&r);
+                            if (pl + 1 < PL) {
+                                const float2 back = __bfloat1622float2(h);
+                                v[2 * i] -= back.x;
+                                v[2 * i + 1] -= back.y;
+                            }
                         }
-                    }
-                    store_line(dst, lane, (c0 >> 5) & 1, pk);
-                    if constexpr (PL == 2) store_line(dst + (int64_t)panels * p.l.Tpad * 64, lane, (c0 >> 5) & 1, lo);
-                    if (p.l.col_part) {
-                        const float s = column_sums(v, lane);
-                        p.l.col_part[(int64_t)(row >> 5) * p.l.ldz + c0 + lane] = s;
+                        store_line(dst + (int64_t)pl * panels * p.l.Tpad * 64, lane, (c0 >> 5) & 1, pk);
                     }
                 }
             } else {
@@ -861,7 +862,6 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 const GradParams &g = p.g;
                 const bool empty = t.kb0 >= t.kb1;     // nothing was contracted: the accumulator holds no result
                 const bool is_dx = t.job == 0;
-                const float scale = g.tau * (PL == 2 ? inv_g * (is_dx ? g.scales->inv_w : g.scales->inv_x) : mantissa);
                 const int32_t rows_in = (is_dx ? n_live : g.width) - row0;             // rows of this warp that exist
                 const int splits = is_dx ? g.dx_splits : g.dw_splits;
                 float *slot = is_dx ? g.dx_slots : g.dw_slots;
@@ -874,6 +874,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                 o.prev_row = slot ? lane : info.row;
                 o.ld = to_slot ? g.slot_ld : g.d;
                 o.prev_ld = slot ? g.slot_ld : g.d;
+                o.scale = to_slot || (is_dx && !g.dx_last) ? 1.0f : g.tau * mantissa;
                 o.rows_in = rows_in; o.end = min(to_slot ? g.slot_ld : g.d, col0 + hc);
                 const bool out_bf16 = !to_slot && (is_dx ? g.dx_bf16 : g.dw_bf16);
                 const bool sectors = o.ld % 16 == 0 && (!o.prev || o.prev_ld % 16 == 0) &&
@@ -885,7 +886,7 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     float v[32];
                     load_chunk(ch, v);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : v[j] * scale;
+                    for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : v[j];
                     if (sectors) write_sectors(o, lane, c0, out_bf16, v);
                     else write_elements(o, exchange, lane, c0, out_bf16, v);
                     __syncwarp();
@@ -959,7 +960,7 @@ int launch(const Maps &maps, const KernelParams &p, int64_t tiles, int32_t k_log
         ready[dev].store(true, std::memory_order_release);
     }
     const unsigned grid = 2u * (unsigned)(tiles < pairs ? tiles : pairs);
-    return launch_pdl(kern, dim3(grid), dim3(kThreads<PL>), smem, s, maps, p, k_logits) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
+    return launch_pdl(kern, dim3(grid), dim3(kThreads), smem, s, maps, p, k_logits) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 
 template <int MODE>
@@ -974,9 +975,8 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     LogitsParams &l = p.l;
     l.n_live = a.n_live; l.rows = a.rows; l.labels = a.labels; l.n_rows = (int32_t)a.T; l.bn = a.bn;
     l.a_rows = (int32_t)rows;
-    const int64_t stage = (int64_t)a.planes * (rows * 128 + a.bn * 64), fit = (kStageBudget - kSideBytes + rows * 128) / stage;
+    const int64_t stage = rows * 128 + a.bn * 64, fit = (kStageBudget - kSideBytes + rows * 128) / stage;
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
-    l.scales = a.scales;
     l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width; l.w_row0 = a.w_row0;
     l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.unit = a.unit; l.units = a.units; l.pitch = a.pitch;
     l.part = a.part; l.parts = a.parts;
@@ -986,7 +986,7 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     if (tiles > INT_MAX) return TBN_ERR_UNSUPPORTED;
     const int32_t kb = (a.x.cols + 63) / 64;
     if (a.planes == 1) return a.bias ? launch<MODE, 1, true>(maps, p, tiles, kb, s) : launch<MODE, 1, false>(maps, p, tiles, kb, s);
-    return a.bias ? launch<MODE, 2, true>(maps, p, tiles, kb, s) : launch<MODE, 2, false>(maps, p, tiles, kb, s);
+    return a.bias ? launch<MODE, 3, true>(maps, p, tiles, kb, s) : launch<MODE, 3, false>(maps, p, tiles, kb, s);
 }
 
 }  // namespace
@@ -1025,16 +1025,16 @@ int launch_head_grads(const GradArgs &a, cudaStream_t s)
         return TBN_ERR_CUDA;
     KernelParams p = {};
     GradParams &g = p.g;
-    g.n_live = a.n_live; g.rows = a.rows; g.scales = a.scales; g.tau = a.tau; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.w_row0 = a.w_row0; g.ldz = a.ldz;
+    g.n_live = a.n_live; g.rows = a.rows; g.tau = a.tau; g.Tpad = a.Tpad; g.d = a.d; g.v0 = a.v0; g.width = a.width; g.w_row0 = a.w_row0; g.ldz = a.ldz;
     g.want_dx = a.want_dx; g.want_dw = a.want_dw; g.w_panels = w_panels;
     g.dx = a.dx; g.dx_slots = a.dx_slots; g.dx_splits = a.dx_splits; g.dx_bf16 = a.dx_bf16; g.dx_add = a.dx_add; g.dx_last = a.dx_last;
     g.dw = a.dw; g.slot_ld = a.slot_ld; g.dw_slots = a.dw_slots; g.dw_splits = a.dw_splits; g.dw_bf16 = a.dw_bf16;
     p.status = a.status;
-    const int64_t cols = a.planes == 1 ? kCols<1> : kCols<2>, nt = (a.d + cols - 1) / cols;
+    const int64_t cols = a.planes == 1 ? kCols<1> : kCols<3>, nt = (a.d + cols - 1) / cols;
     const int64_t tiles = (a.want_dx ? (a.T + kTile - 1) / kTile * nt * a.dx_splits : 0) +
                           (a.want_dw ? (a.width + kTile - 1) / kTile * nt * a.dw_splits : 0);
     if (tiles > INT_MAX) return TBN_ERR_UNSUPPORTED;
-    return a.planes == 1 ? launch<kGrads, 1, false>(maps, p, tiles, 0, s) : launch<kGrads, 2, false>(maps, p, tiles, 0, s);
+    return a.planes == 1 ? launch<kGrads, 1, false>(maps, p, tiles, 0, s) : launch<kGrads, 3, false>(maps, p, tiles, 0, s);
 }
 
 }  // namespace head

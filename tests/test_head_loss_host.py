@@ -31,3 +31,10 @@ def test_packed_weights_of_the_backward_are_bounded(lib):
     for dtype, d in ((B.F32, 1024), (B.BF16, 1001)):
         small, large = (lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 1) for V in (1 << 18, 1 << 21))
         assert large < small + (128 << 20)
+
+
+def test_partial_statistics_are_small_beside_the_logits(lib):
+    """One record of 16 bytes per token and 64 classes or more: a sixteenth of the fp32 logits (and the small packed operands)."""
+    for dtype in (B.BF16, B.F32):
+        T, d, V = 8192, 64, 131072
+        assert lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 0) < T * V * 4 / 15 + 6 * (T + V) * d
