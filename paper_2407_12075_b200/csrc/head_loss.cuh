@@ -25,12 +25,16 @@ struct __align__(16) RowInfo {
 
 #ifdef __CUDACC__
 // The factor in [1, 2) that the bf16 form takes out of the gradient's tokens before dz is rounded and puts back into the sums:
-// the mantissa of the first kept token's g.  Under a mean every token has the same g; with it in dz the largest entry of
-// every row, -g (1 - q), would be rounded the same way, and all of dx and dw off by up to 2^-8 with it.
+// the mantissa of the first kept token's g that has one (of the first 32, so that the look is short: tokens of weight 0 at
+// the front are common, a whole warp of them is not).  Under a mean every token has the same g; with it in dz the largest
+// entry of every row, -g (1 - q), would be rounded the same way, and all of dx and dw off by up to 2^-8 with it.
 __device__ __forceinline__ float common_mantissa(const RowInfo *rows, int32_t n_live)
 {
-    const uint32_t b = n_live > 0 ? __float_as_uint(rows[0].g) : 0u, e = b & 0x7f800000u;
-    return e == 0u || e == 0x7f800000u ? 1.0f : __uint_as_float((b & 0x007fffffu) | 0x3f800000u);
+    for (int32_t i = 0; i < n_live && i < 32; ++i) {
+        const uint32_t b = __float_as_uint(rows[i].g), e = b & 0x7f800000u;
+        if (e != 0u && e != 0x7f800000u) return __uint_as_float((b & 0x007fffffu) | 0x3f800000u);
+    }
+    return 1.0f;
 }
 #endif
 
