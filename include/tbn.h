@@ -170,6 +170,8 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *   dx: T x in_f of `dtype`, or NULL.  dw: vocab x in_f of dw_dtype (TBN_F32: what tbn_tile_bwd takes as G; TBN_BF16), or
  *   NULL.  dbias: vocab floats or NULL.  All are overwritten; none may overlap an input or the workspace.  With bf16 operands
  *   dz is rounded to bf16 for the two products (dbias is summed before that rounding); sums are fp32.
+ *   q is exp(z / tau - lse) with lse as a float, so it is off by up to |lse| 2^-22 of itself; from |lse| = 2839 on (2^12 in log2),
+ *   classes within |lse| 2^-21 of lse have q = 1.
  * workspace: tbn_linear_xent_workspace_bytes(..., backward) / tbn_linear_distill_workspace_bytes(..., backward) bytes, with
  *   backward = 0 or 1 for the call it is meant for.  T == 0: the forward is a no-op, the backward writes zeros to dw and dbias.
  * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1024: TBN_ERR_UNSUPPORTED.

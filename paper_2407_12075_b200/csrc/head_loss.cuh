@@ -71,7 +71,7 @@ struct LogitsArgs {                        // logits of all kept tokens against 
     const float *bias;                     // V or null
     float scale2;                          // log2(e) / tau
     int64_t T, Tpad;
-    int32_t V, v0, width;
+    int32_t v0, width;
     const int2 *list;                      // distillation: [T][K] (class, probability), ascending, INT32_MAX behind the last; else null
     const uint16_t *list_start;            // [T][pitch]: where the units + 1 units of classes begin in a row's list
     int32_t K, unit, units, pitch;
@@ -96,7 +96,7 @@ struct GradArgs {                          // dX (+)= dz W, dW = dz^T X for one 
     float tau;                             // what the sums over dz are multiplied by
     const void *dz;
     int64_t T, Tpad;
-    int32_t d, V, v0, width, ldz;
+    int32_t d, v0, width, ldz;
     bool want_dx, want_dw;
     // dX: into `dx` by row when no slots are used, else fp32 partial sums [split][Tpad][slot_ld], added to when `dx_add`
     void *dx;

@@ -82,7 +82,7 @@ struct LogitsParams {
     const float *bias;
     float scale2;
     int64_t Tpad;
-    int32_t V, v0, width, w_row0;          // w_row0: w's row of class v0
+    int32_t v0, width, w_row0;             // w_row0: w's row of class v0
     const int2 *list;                      // distillation: [T][K] (class, probability) pairs, ascending; else null
     const uint16_t *list_start;            // [T][pitch]: where the classes of each unit begin in the row's list
     int32_t K, unit, units, pitch;
@@ -977,7 +977,7 @@ int launch_logits(const LogitsArgs &a, cudaStream_t s)
     l.a_rows = (int32_t)rows;
     const int64_t stage = rows * 128 + a.bn * 64, fit = (kStageBudget - kSideBytes + rows * 128) / stage;
     l.stages = (int32_t)(fit > kMaxStages ? kMaxStages : fit);
-    l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.V = a.V; l.v0 = a.v0; l.width = a.width; l.w_row0 = a.w_row0;
+    l.bias = a.bias; l.scale2 = a.scale2; l.Tpad = a.Tpad; l.v0 = a.v0; l.width = a.width; l.w_row0 = a.w_row0;
     l.list = a.list; l.list_start = a.list_start; l.K = a.K; l.unit = a.unit; l.units = a.units; l.pitch = a.pitch;
     l.part = a.part; l.parts = a.parts;
     l.dz = a.dz; l.ldz = a.ldz; l.col_part = a.col_part;
@@ -1011,7 +1011,8 @@ int launch_head_dz(const LogitsArgs &a, cudaStream_t s) { return launch_logits<k
 int launch_head_grads(const GradArgs &a, cudaStream_t s)
 {
     Maps maps = {};
-    // dz lines are written for whole 256-token tiles; the tokens behind the last kept one are zeros
+    // dz is written up to the next multiple of 64 tokens, with zeros behind the last kept one: that is what dW contracts over.  The
+    // lines behind that hold anything; dX loads them with its 128 tokens, into accumulator rows that are not stored.
     const int64_t dz_panels = a.ldz / 64, dz_panel = a.Tpad * 128;
     const bool w_panels = a.w.ld % 64 == 0;
     auto by_panels = [&a](CUtensorMap *m, const Operand &o) {
