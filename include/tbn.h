@@ -174,7 +174,8 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *   classes within |lse| 2^-21 of lse have q = 1.
  * workspace: tbn_linear_xent_workspace_bytes(..., backward) / tbn_linear_distill_workspace_bytes(..., backward) bytes, with
  *   backward = 0 or 1 for the call it is meant for.  T == 0: the forward is a no-op, the backward writes zeros to dw and dbias.
- * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1024: TBN_ERR_UNSUPPORTED.
+ * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1024, or x or w of more than 2^38 elements (rows counted in whole
+ *   64s): TBN_ERR_UNSUPPORTED.
  */
 size_t tbn_linear_xent_workspace_bytes(int64_t T, int32_t in_f, int32_t vocab, int dtype, int backward);
 int tbn_linear_xent_fwd(const void *x, const void *w, int dtype, int64_t T, int32_t in_f, int32_t vocab, const float *bias,

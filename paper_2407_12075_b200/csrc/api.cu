@@ -132,7 +132,9 @@ constexpr int64_t kHeadMost = 0x7fffffffLL - 1024;     // tile and row indices a
 
 bool head_sizes_ok(int64_t T, int32_t in_f, int32_t vocab)
 {
-    return T >= 0 && in_f > 0 && vocab > 0 && T <= kHeadMost && in_f <= kHeadMost && vocab <= kHeadMost;
+    // rows x in_f: as a tensor map's 40-bit strides hold it, and far from where byte counts of the workspace would wrap
+    const int64_t rows = T > vocab ? T : vocab, ld = ((int64_t)in_f + 63) / 64 * 64;
+    return T >= 0 && in_f > 0 && vocab > 0 && T <= kHeadMost && in_f <= kHeadMost && vocab <= kHeadMost && rows <= ((int64_t)1 << 38) / ld;
 }
 
 int head_call(const head::HeadCall &c, bool backward, void *workspace, size_t workspace_bytes, void *stream)

@@ -38,3 +38,13 @@ def test_partial_statistics_are_small_beside_the_logits(lib):
     for dtype in (B.BF16, B.F32):
         T, d, V = 8192, 64, 131072
         assert lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 0) < T * V * 4 / 15 + 6 * (T + V) * d
+
+
+def test_operands_whose_byte_counts_would_wrap_are_refused(lib):
+    top, P = 2**31 - 1025, 0x10000                       # P: never dereferenced
+    for T, d, V in ((top, top, top), (4, top, top), (top, 2049, 4)):
+        for dtype in (B.BF16, B.F32):
+            assert lib.tbn_linear_xent_workspace_bytes(T, d, V, dtype, 1) == 0
+            assert lib.tbn_linear_xent_fwd(P, P, dtype, T, d, V, None, P, -100, P, P, P, 1 << 62, None) == -3
+            assert lib.tbn_linear_distill_bwd(P, P, dtype, T, d, V, None, P, P, B.F32, 3, 1.0, P, P, P, P, dtype, None, P, 1 << 62, None) == -3
+    assert lib.tbn_linear_xent_workspace_bytes(top, 1, top, B.F32, 1) > 0
