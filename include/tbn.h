@@ -193,6 +193,94 @@ int tbn_linear_distill_bwd(const void *x, const void *w, int dtype, int64_t T, i
                            const float *dloss, void *dx, void *dw, int dw_dtype, float *dbias,
                            void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * The rest of a training step around a tiled head: token ids in, LayerNorm with its gradient, and what follows the gradients.
+ * The paper trains with ordinary layers and an ordinary optimizer and defines none of these.  Together with the calls above a
+ * step with a tied tiled head is  tile_fwd -> embedding_fwd -> ... -> layernorm_train_fwd -> linear_xent_fwd / _bwd ->
+ * layernorm_bwd -> ... -> embedding_bwd (added to the head's dw) -> tile_bwd -> grad_norm -> adamw_step.
+ *
+ * Embedding.  ids: T int64.  An id that is negative, >= vocab or equal to padding_idx (-1: none) gives a row of zeros and gets no
+ * gradient.
+ *     y[t][:] = scale * table[ids[t]][:]                          table: vocab x d of table_dtype, y: T x d of y_dtype
+ *     dw[v][:] = (accumulate ? dw[v][:] : 0) + scale * sum_{t: ids[t] = v} dy[t][:]
+ * tbn_embedding_tiled_fwd reads the table as a tiled layer of vocab rows of d inputs (N = vocab * d): tile_bits, k, alpha,
+ * alpha_mode as tbn_aggregate_tile writes them; no row of B_hat is stored.
+ * tbn_embedding_bwd: dy: T x d of dy_dtype, dw: vocab x d of dw_dtype (TBN_F32: what tbn_tile_bwd takes as G).  Rows are added in
+ *   fp32 in the order of the tokens in pieces that T decides, and rounded once.  With accumulate rows that no token names are
+ *   neither read nor written: a tied head's dw takes the embedding's part this way.  workspace:
+ *   tbn_embedding_bwd_workspace_bytes(T, d, vocab) bytes.  T == 0: zeros, or with accumulate a no-op.
+ * Errors: vocab * d not a multiple of k: TBN_ERR_SHAPE.  T, vocab beyond 2^31 - 1024 or d beyond 2^23: TBN_ERR_UNSUPPORTED.
+ */
+int tbn_embedding_fwd(const int64_t *ids, int64_t T, const void *table, int table_dtype, int32_t vocab, int32_t d, int64_t padding_idx,
+                      float scale, void *y, int y_dtype, void *stream);
+int tbn_embedding_tiled_fwd(const int64_t *ids, int64_t T, int32_t vocab, int32_t d, const uint32_t *tile_bits, int32_t k, const float *alpha,
+                            int alpha_mode, int64_t padding_idx, float scale, void *y, int y_dtype, void *stream);
+size_t tbn_embedding_bwd_workspace_bytes(int64_t T, int32_t d, int32_t vocab);
+int tbn_embedding_bwd(const int64_t *ids, int64_t T, const void *dy, int dy_dtype, int32_t vocab, int32_t d, int64_t padding_idx, float scale,
+                      void *dw, int dw_dtype, int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* LayerNorm for training (tbn_layernorm_fwd below is the form that keeps nothing).
+ *     s[t][:] = x[t][:] + residual[t][:]   rounded to x_dtype; s = x without a residual
+ *     mean[t], rstd[t] = 1 / sqrt(var + eps)  of s[t][:] (biased variance, fp32),    y = (s - mean) * rstd * gamma + beta
+ * tbn_layernorm_train_fwd: x, residual (or NULL), sum: T x d of x_dtype; sum receives s and is needed with a residual, ignored
+ *   without one; y: T x d of y_dtype; gamma, beta: d floats or NULL; mean, rstd: T floats, or NULL.
+ * tbn_layernorm_bwd: dy: T x d of dy_dtype; x: the s of the forward, T x d of x_dtype; mean, rstd as the forward wrote them.
+ *     h = (x - mean) * rstd,  a = dy * gamma,  dx = rstd * (a - mean_i(a) - h * mean_i(a h)) + dsum
+ *     dgamma[i] = sum_t dy[t][i] h[t][i],  dbeta[i] = sum_t dy[t][i]
+ *   dsum (T x d of x_dtype, or NULL): a gradient that reaches s by other ways.  dx (T x d of x_dtype) is the gradient of x and of
+ *   the residual.  dgamma, dbeta: d floats or NULL.  All are overwritten; sums are fp32 in an order that T and d decide.
+ *   workspace: tbn_layernorm_bwd_workspace_bytes(T, d) bytes; not needed when dgamma and dbeta are NULL.  T == 0: zeros.
+ * No output may overlap an input.  A row that holds an infinity or a NaN has NaN in its y and dx and in dgamma; no other row is
+ * affected. */
+int tbn_layernorm_train_fwd(const void *x, const void *residual, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *beta, float eps,
+                            void *sum, void *y, int y_dtype, float *mean, float *rstd, void *stream);
+size_t tbn_layernorm_bwd_workspace_bytes(int64_t T, int32_t d);
+int tbn_layernorm_bwd(const void *dy, int dy_dtype, const void *x, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *mean,
+                      const float *rstd, const void *dsum, void *dx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/* AdamW over many tensors.  `tensors` is a HOST array of `count` descriptors that hold device pointers; it is read during the call
+ * only.  For every element, in fp32:
+ *     g = grad_scale * grad,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g g
+ *     param = param * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * param: n values of param_dtype (bf16 parameters are rounded to nearest, and an update below 2^-9 of a value does not move it;
+ * a fp32 param with a bf16 copy does not have that limit).  copy: n bf16 values that receive param, or NULL.
+ * States of 32 bits: m and v are n floats each, the scales are NULL.  States of 8 bits: m is n int8 and v n uint8 codes, m_scale and
+ * v_scale hold one float for each 256 elements (ceil(n / 256)):
+ *     m = c |c| m_scale,  c = -127 .. 127 (-128: NaN);      v = c^4 v_scale,  c = 0 .. 254 (255: infinity)
+ * all zero at the start.  A new code is the one below or the one above the value in units of the scale, drawn so that its mean is
+ * the value; the draw is a function of seed, t, the tensor's place in the array and the element, so equal calls give equal
+ * bits.  A v above zero keeps a code above zero.  The parameters are updated from m and v before they are rounded.
+ * Pointers need the alignment of their type only; tensors whose pointers begin at multiples of eight elements are faster.
+ * n == 0 is allowed.  No tensor may overlap another one.
+ *
+ * tbn_adamw_step: step is t, from 1 on.  step_dev, lr_dev (device, or NULL) replace step and lr when given, so that a captured step
+ *   can be replayed with other values; a step below 1 counts as 1.  grad_scale: one float on the device, or NULL for 1; where it is
+ *   infinite or NaN nothing is changed by the call.  0 <= beta1, beta2 < 1, eps >= 1e-30, lr finite.
+ * tbn_grad_norm: norm = sqrt(sum over all tensors' grad^2) (64-bit sums in a fixed order); scale = max_norm / norm where norm >
+ *   max_norm, else 1; NaN where the norm is infinite or NaN, which makes tbn_adamw_step leave everything as it is.  norm, scale: one
+ *   float each or NULL.  Only grad, n and grad_dtype are read.  workspace: tbn_grad_norm_workspace_bytes(count) bytes.
+ * tbn_adamw_unpack: the values of 8-bit states: m_out[i], v_out[i] (HOST arrays of device pointers to n floats; an array or an
+ *   entry may be NULL).
+ */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    int64_t n;
+    float weight_decay;
+    int32_t param_dtype, grad_dtype; /* TBN_F32 or TBN_BF16 */
+    int32_t state_bits;              /* 32 or 8 */
+} tbn_adamw_tensor;
+int tbn_adamw_step(const tbn_adamw_tensor *tensors, int32_t count, int64_t step, const int64_t *step_dev, double lr, const float *lr_dev,
+                   double beta1, double beta2, double eps, const float *grad_scale, uint64_t seed, void *stream);
+size_t tbn_grad_norm_workspace_bytes(int32_t count);
+int tbn_grad_norm(const tbn_adamw_tensor *tensors, int32_t count, double max_norm, float *norm, float *scale, void *workspace,
+                  size_t workspace_bytes, void *stream);
+int tbn_adamw_unpack(const tbn_adamw_tensor *tensors, int32_t count, float *const *m_out, float *const *v_out, void *stream);
+
 /* Pack an existing real-valued tile (Sec. 5.1: tiles are stored one bit per element):
  * src[i] > 0 -> bit 1, else 0.  src: q fp32 values.  tile_bits: tbn_tile_words(q) words. */
 int tbn_pack_tile(const float *src, int64_t q, uint32_t *tile_bits, void *stream);

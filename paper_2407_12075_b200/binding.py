@@ -22,6 +22,7 @@ ACT_NONE, ACT_RELU, ACT_GELU = 0, 1, 2
 PATH_AUTO, PATH_GENERIC, PATH_SMALL, PATH_TENSOR = 0, 1, 2, 3
 
 c_i32, c_i64, c_int, c_vp, c_sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+c_f32, c_f64 = ctypes.c_float, ctypes.c_double
 
 _LINEAR_ARGS = [c_vp, c_int, c_i64, c_i32, c_i32, c_vp, c_i32, c_vp, c_int, c_vp, c_int, c_vp, c_int,
                 c_vp, c_sz, c_vp]
@@ -89,6 +90,17 @@ SIGNATURES = {
     "tbn_binarize_bytes_fwd": (c_int, [c_vp, c_int, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp]),
     "tbn_linear_bin_bytes_fwd": (c_int, [c_vp, c_vp, c_i64, c_i32, c_i32, c_vp, c_i32, c_vp, c_int, c_vp, c_vp, c_int, c_vp,
                                          c_int, c_vp]),
+    "tbn_embedding_fwd": (c_int, [c_vp, c_i64, c_vp, c_int, c_i32, c_i32, c_i64, c_f32, c_vp, c_int, c_vp]),
+    "tbn_embedding_tiled_fwd": (c_int, [c_vp, c_i64, c_i32, c_i32, c_vp, c_i32, c_vp, c_int, c_i64, c_f32, c_vp, c_int, c_vp]),
+    "tbn_embedding_bwd_workspace_bytes": (c_sz, [c_i64, c_i32, c_i32]),
+    "tbn_embedding_bwd": (c_int, [c_vp, c_i64, c_vp, c_int, c_i32, c_i32, c_i64, c_f32, c_vp, c_int, c_int, c_vp, c_sz, c_vp]),
+    "tbn_layernorm_train_fwd": (c_int, [c_vp, c_vp, c_int, c_i64, c_i32, c_vp, c_vp, c_f32, c_vp, c_vp, c_int, c_vp, c_vp, c_vp]),
+    "tbn_layernorm_bwd_workspace_bytes": (c_sz, [c_i64, c_i32]),
+    "tbn_layernorm_bwd": (c_int, [c_vp, c_int, c_vp, c_int, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]),
+    "tbn_adamw_step": (c_int, [c_vp, c_i32, c_i64, c_vp, c_f64, c_vp, c_f64, c_f64, c_f64, c_vp, ctypes.c_uint64, c_vp]),
+    "tbn_grad_norm_workspace_bytes": (c_sz, [c_i32]),
+    "tbn_grad_norm": (c_int, [c_vp, c_i32, c_f64, c_vp, c_vp, c_vp, c_sz, c_vp]),
+    "tbn_adamw_unpack": (c_int, [c_vp, c_i32, c_vp, c_vp, c_vp]),
 }
 
 _lib = None
@@ -642,3 +654,254 @@ def tbn_linear_distill_bwd(x: torch.Tensor, weight: torch.Tensor, top_index: tor
                _ptr(weight), dt, T, d, V, _ptr(bias), _ptr(top_index), _ptr(top_logit), _dtype_code(top_logit), K, temperature, _ptr(lse),
                _ptr(dloss), _ptr(dx), _ptr(dw), wd, _ptr(db))
     return dx, dw, db
+
+
+# ---- embedding, LayerNorm for training, AdamW --------------------------------------------------------------------
+def _on_device(name, device, *args):
+    """Runs the entry point on the tensors' device and that device's current stream."""
+    index = device.index
+    fn, stream = getattr(lib(), name), torch._C._cuda_getCurrentRawStream(index)
+    if torch.cuda.current_device() == index:
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, stream)
+    if status != OK:
+        raise TbnError(status, name)
+
+
+def _same_device(where, device, *tensors):
+    if device.type != "cuda":
+        raise ValueError(f"{where}: the tensors must be on a CUDA device")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"{where}: tensors on {device} and {t.device}")
+
+
+def _workspace(where, workspace, need, device):
+    if workspace is None:
+        return torch.empty(need or 16, dtype=torch.uint8, device=device)
+    if workspace.device != device:
+        raise ValueError(f"{where}: workspace on {workspace.device}, tensors on {device}")
+    return workspace
+
+
+def _embedding_ids(ids, where):
+    if ids.dtype != torch.int64:
+        raise TypeError(f"{where}: ids must be int64, not {ids.dtype}")
+    return ids.numel()
+
+
+def tbn_embedding_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, padding_idx: int = -1, y_dtype: int | None = None) -> torch.Tensor:
+    """scale * table[ids]; ids of any shape, y of shape ids.shape + (d,).  Ids outside the table and padding_idx give zeros."""
+    T, device = _embedding_ids(ids, "embedding"), ids.device
+    if table.dim() != 2:
+        raise TbnError(-2, f"embedding: table {tuple(table.shape)}")
+    _same_device("embedding", device, table)
+    V, d = table.shape
+    td = _dtype_code(table)
+    yd = td if y_dtype is None else y_dtype
+    y = torch.empty((*ids.shape, d), dtype=_torch_dtype(yd), device=device)
+    _on_device("tbn_embedding_fwd", device, _ptr(ids), T, _ptr(table), td, V, d, padding_idx, scale, _ptr(y), yd)
+    return y
+
+
+def tbn_embedding_tiled_fwd(ids: torch.Tensor, vocab: int, d: int, tile: torch.Tensor, k: int, alpha: torch.Tensor, alpha_mode: int,
+                            scale: float = 1.0, padding_idx: int = -1, y_dtype: int = BF16) -> torch.Tensor:
+    """tbn_embedding_fwd from a tiled table of vocab x d weights: its bits and scaling factors as tbn_aggregate_tile gives them."""
+    T, device = _embedding_ids(ids, "embedding"), ids.device
+    _same_device("embedding", device, tile, alpha)
+    if k <= 0 or (vocab * d) % k:
+        raise TbnError(-2, "tbn_embedding_tiled_fwd")
+    if tile.dtype != torch.int32 or tile.numel() < tbn_tile_words(vocab * d // k):
+        raise TbnError(-2, f"embedding: the tile must be int32 of {tbn_tile_words(vocab * d // k)} words")
+    if alpha.dtype != torch.float32 or alpha.numel() < (k if alpha_mode == ALPHA_PER_TILE else 1):
+        raise TbnError(-2, "embedding: alpha must be float32, one value or one for each tile")
+    y = torch.empty((*ids.shape, d), dtype=_torch_dtype(y_dtype), device=device)
+    _on_device("tbn_embedding_tiled_fwd", device, _ptr(ids), T, vocab, d, _ptr(tile), k, _ptr(alpha), alpha_mode, padding_idx, scale, _ptr(y), y_dtype)
+    return y
+
+
+def tbn_embedding_bwd_workspace_bytes(T, d, vocab) -> int:
+    return int(lib().tbn_embedding_bwd_workspace_bytes(T, d, vocab))
+
+
+def tbn_embedding_bwd(ids: torch.Tensor, dy: torch.Tensor, vocab: int, scale: float = 1.0, padding_idx: int = -1, dw_dtype: int | None = None,
+                      add_to: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of an embedding's table (vocab x d): the rows of dy that share an id, added up.  add_to: a gradient that is there
+    already (a tied head's), which the sums are added to in place; otherwise a new tensor of dw_dtype (dy's type by default)."""
+    T, device = _embedding_ids(ids, "embedding"), ids.device
+    if dy.shape[:-1] != ids.shape or dy.dim() < 1:
+        raise TbnError(-2, f"embedding: ids {tuple(ids.shape)} and dy {tuple(dy.shape)}")
+    d, gd = dy.shape[-1], _dtype_code(dy)
+    _same_device("embedding", device, dy, add_to)
+    if add_to is not None:
+        if add_to.shape != (vocab, d):
+            raise TbnError(-2, f"embedding: add_to {tuple(add_to.shape)}, not ({vocab}, {d})")
+        wd, dw = _dtype_code(add_to), add_to
+    else:
+        wd = gd if dw_dtype is None else dw_dtype
+        dw = torch.empty((vocab, d), dtype=_torch_dtype(wd), device=device)
+    ws = _workspace("embedding", workspace, tbn_embedding_bwd_workspace_bytes(T, d, vocab), device)
+    _on_device("tbn_embedding_bwd", device, _ptr(ids), T, _ptr(dy), gd, vocab, d, padding_idx, scale, _ptr(dw), wd, int(add_to is not None),
+               _ptr(ws), ws.numel() * ws.element_size())
+    return dw
+
+
+def _norm_vectors(where, d, device, *vectors):
+    for v in vectors:
+        if v is not None and (v.shape != (d,) or v.dtype != torch.float32 or v.device != device):
+            raise TbnError(-2, f"{where}: must be float32 of shape ({d},) on {device}")
+
+
+def tbn_layernorm_train_fwd(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, eps: float = 1e-5,
+                            residual: torch.Tensor | None = None, y_dtype: int | None = None):
+    """LayerNorm of s = x + residual (rounded to x's type; s is x without a residual) over the last dimension, for training.
+    Returns (y, s, mean, rstd): what tbn_layernorm_bwd takes besides dy."""
+    shape, device = x.shape, x.device
+    d = shape[-1]
+    T = x.numel() // d if d else 0
+    _same_device("layer norm", device, residual)
+    _norm_vectors("layer norm: gamma and beta", d, device, gamma, beta)
+    if residual is not None and (residual.shape != shape or residual.dtype != x.dtype):
+        raise TbnError(-2, f"layer norm: x {tuple(shape)} {x.dtype} and residual {tuple(residual.shape)} {residual.dtype}")
+    xd = _dtype_code(x)
+    yd = xd if y_dtype is None else y_dtype
+    y = torch.empty(shape, dtype=_torch_dtype(yd), device=device)
+    s = torch.empty_like(x) if residual is not None else x
+    stats = torch.empty((2, T), dtype=torch.float32, device=device)
+    at = stats.data_ptr()
+    _on_device("tbn_layernorm_train_fwd", device, _ptr(x), _ptr(residual), xd, T, d, _ptr(gamma), _ptr(beta), eps,
+               _ptr(s) if residual is not None else None, _ptr(y), yd, at, at + 4 * T)
+    return y, s, stats[0], stats[1]
+
+
+def tbn_layernorm_bwd_workspace_bytes(T, d) -> int:
+    return int(lib().tbn_layernorm_bwd_workspace_bytes(T, d))
+
+
+def tbn_layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: torch.Tensor | None = None,
+                      dsum: torch.Tensor | None = None, need_dgamma: bool = True, need_dbeta: bool = True, workspace: torch.Tensor | None = None):
+    """Gradient of tbn_layernorm_train_fwd: (dx, dgamma, dbeta), None for what is not asked for.  dx is also the residual's; dsum
+    is a gradient that reaches s by other ways and is added to dx."""
+    shape, device = s.shape, s.device
+    d = shape[-1]
+    T = s.numel() // d if d else 0
+    _same_device("layer norm", device, dy, dsum)
+    if dy.shape != shape or (dsum is not None and (dsum.shape != shape or dsum.dtype != s.dtype)):
+        raise TbnError(-2, f"layer norm: dy {tuple(dy.shape)}, s {tuple(shape)}" + ("" if dsum is None else f", dsum {tuple(dsum.shape)} {dsum.dtype}"))
+    _norm_vectors("layer norm: gamma", d, device, gamma)
+    _norm_vectors("layer norm: mean and rstd", T, device, mean, rstd)
+    dx = torch.empty_like(s)
+    sums = torch.empty((int(need_dgamma) + int(need_dbeta), d), dtype=torch.float32, device=device) if need_dgamma or need_dbeta else None
+    dgamma = sums[0] if need_dgamma else None
+    dbeta = sums[-1] if need_dbeta else None
+    ws = None
+    if sums is not None:
+        ws = _workspace("layer norm", workspace, tbn_layernorm_bwd_workspace_bytes(T, d), device)
+    _on_device("tbn_layernorm_bwd", device, _ptr(dy), _dtype_code(dy), _ptr(s), _dtype_code(s), T, d, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dsum),
+               _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    return dx, dgamma, dbeta
+
+
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", c_vp), ("grad", c_vp), ("m", c_vp), ("v", c_vp), ("m_scale", c_vp), ("v_scale", c_vp), ("copy", c_vp), ("n", c_i64),
+                ("weight_decay", c_f32), ("param_dtype", c_i32), ("grad_dtype", c_i32), ("state_bits", c_i32)]
+
+
+class AdamWTensors:
+    """The tensors of an optimizer, as tbn_adamw_tensors describes them to the library: made once, used in every step.  It keeps the
+    tensors alive; they are updated in place and must stay the tensors they are (new gradients are written into the same ones)."""
+    __slots__ = ("table", "at", "count", "device", "kept", "state_bits")
+
+    def __init__(self, table, device, kept, state_bits):
+        self.table, self.at, self.count = table, ctypes.addressof(table), len(kept)
+        self.device, self.kept, self.state_bits = device, kept, state_bits
+
+
+def tbn_adamw_state(params, bits: int = 8):
+    """States before the first step: lists (m, v, m_scale, v_scale) of zeros for tbn_adamw_tensors (32 bits: the scales are None)."""
+    if bits not in (8, 32):
+        raise ValueError(f"AdamW states have 8 or 32 bits, not {bits}")
+    zeros = lambda n, dtype: [torch.zeros(n(p), dtype=dtype, device=p.device) for p in params]  # noqa: E731
+    if bits == 32:
+        return zeros(torch.Tensor.numel, torch.float32), zeros(torch.Tensor.numel, torch.float32), None, None
+    scales = lambda p: -(-p.numel() // 256)  # noqa: E731
+    return zeros(torch.Tensor.numel, torch.int8), zeros(torch.Tensor.numel, torch.uint8), zeros(scales, torch.float32), zeros(scales, torch.float32)
+
+
+def tbn_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=None, weight_decay=0.0) -> AdamWTensors:
+    """Describes an optimizer's tensors: lists of the same length (copies: bf16 tensors that receive the parameters, entries may be
+    None; weight_decay: a number, or one for each tensor).  States as tbn_adamw_state gives them."""
+    params, grads, m, v = list(params), list(grads), list(m), list(v)
+    n = len(params)
+    none = [None] * n
+    m_scale, v_scale, copies = (none if c is None else list(c) for c in (m_scale, v_scale, copies))
+    decay = [float(w) for w in weight_decay] if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
+    if any(len(c) != n for c in (grads, m, v, m_scale, v_scale, copies, decay)):
+        raise TbnError(-2, "adamw: lists of different lengths")
+    table, kept, bits_seen = (_AdamWTensor * max(n, 1))(), [], set()
+    device = params[0].device if n else torch.device("cuda", torch.cuda.current_device() if torch.cuda.is_available() else 0)
+    for i, (p, g, a, b, sa, sb, c) in enumerate(zip(params, grads, m, v, m_scale, v_scale, copies)):
+        size = p.numel()
+        _same_device("adamw", device, p, g, a, b, sa, sb, c)
+        if g.shape != p.shape or a.numel() != size or b.numel() != size or (c is not None and c.numel() != size):
+            raise TbnError(-2, f"adamw: tensor {i}: sizes differ")
+        if a.dtype == torch.int8 and b.dtype == torch.uint8:
+            bits, blocks = 8, -(-size // 256)
+            if any(s is None or s.numel() != blocks or s.dtype != torch.float32 for s in (sa, sb)):
+                raise TbnError(-2, f"adamw: tensor {i}: m_scale and v_scale must be float32 of {blocks} values")
+        elif a.dtype == torch.float32 and b.dtype == torch.float32:
+            bits = 32
+        else:
+            raise TypeError(f"adamw: tensor {i}: states of {a.dtype} and {b.dtype}")
+        if c is not None and c.dtype != torch.bfloat16:
+            raise TypeError(f"adamw: tensor {i}: a copy of {c.dtype}")
+        ptr = lambda t: _ptr(t) if t is not None and t.numel() else None  # noqa: E731
+        table[i] = _AdamWTensor(ptr(p), ptr(g), ptr(a), ptr(b), ptr(sa), ptr(sb), ptr(c), size, decay[i], _dtype_code(p), _dtype_code(g), bits)
+        kept.append((p, g, a, b, sa, sb, c))
+        bits_seen.add(bits)
+    return AdamWTensors(table, device, kept, bits_seen)
+
+
+def tbn_grad_norm(tensors: AdamWTensors, max_norm: float, workspace: torch.Tensor | None = None):
+    """Global norm of the gradients and the factor that brings it down to max_norm: (norm [1], scale [1]), on the device.  scale goes
+    to tbn_adamw_step as it is; it is NaN, and the step leaves everything as it is, where the norm is not finite."""
+    out = torch.empty((2, 1), dtype=torch.float32, device=tensors.device)
+    ws = workspace
+    if ws is None:
+        with torch.cuda.device(tensors.device):
+            need = int(lib().tbn_grad_norm_workspace_bytes(tensors.count))
+    ws = _workspace("grad norm", workspace, need if workspace is None else 0, tensors.device)
+    at = out.data_ptr()
+    _on_device("tbn_grad_norm", tensors.device, tensors.at, tensors.count, max_norm, at, at + 4, _ptr(ws), ws.numel() * ws.element_size())
+    return out[0], out[1]
+
+
+def tbn_adamw_step(tensors: AdamWTensors, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                   grad_scale: torch.Tensor | None = None, seed: int = 0):
+    """One AdamW step in place.  step: from 1 on, or an int64 device tensor of one value; lr: a number or a float32 device tensor of
+    one value (as a captured graph needs them).  grad_scale: a factor of the gradients on the device, as tbn_grad_norm gives it.
+    seed: of the roundings of 8-bit states."""
+    step_t, lr_t = isinstance(step, torch.Tensor), isinstance(lr, torch.Tensor)
+    if step_t or lr_t or grad_scale is not None:
+        _same_device("adamw", tensors.device, step if step_t else None, lr if lr_t else None, grad_scale)
+        for t, dtype, what in ((step, torch.int64, "step"), (lr, torch.float32, "lr"), (grad_scale, torch.float32, "grad_scale")):
+            if isinstance(t, torch.Tensor) and (t.dtype != dtype or t.numel() != 1):
+                raise TypeError(f"adamw: {what} must be one value of {dtype}")
+    _on_device("tbn_adamw_step", tensors.device, tensors.at, tensors.count, 1 if step_t else step, _ptr(step) if step_t else None, 0.0 if lr_t else lr,
+               _ptr(lr) if lr_t else None, beta1, beta2, eps, _ptr(grad_scale), seed & 0xFFFFFFFFFFFFFFFF)
+
+
+def tbn_adamw_unpack(tensors: AdamWTensors, m_out=None, v_out=None):
+    """The values of 8-bit states, as lists of float32 tensors (m, v); m_out, v_out: tensors to write them to."""
+    lists = []
+    for given in (m_out, v_out):
+        out = [torch.empty(k[0].numel(), dtype=torch.float32, device=tensors.device) for k in tensors.kept] if given is None else list(given)
+        if len(out) != tensors.count or any(o.numel() != k[0].numel() or o.dtype != torch.float32 for o, k in zip(out, tensors.kept)):
+            raise TbnError(-2, "adamw: one float32 tensor of the parameter's size for each tensor")
+        _same_device("adamw", tensors.device, *out)
+        lists.append(out)
+    arrays = [(c_vp * max(len(o), 1))(*[_ptr(t) if t.numel() else None for t in o]) for o in lists]
+    _on_device("tbn_adamw_unpack", tensors.device, tensors.at, tensors.count, ctypes.addressof(arrays[0]), ctypes.addressof(arrays[1]))
+    return lists[0], lists[1]

@@ -5,8 +5,11 @@
 #include <cstring>
 #include <mutex>
 
+#include "adamw.cuh"
 #include "common.cuh"
+#include "embedding.cuh"
 #include "head_loss.cuh"
+#include "norm_train.cuh"
 
 namespace tbn {
 
@@ -163,6 +166,35 @@ int head_call(const head::HeadCall &c, bool backward, void *workspace, size_t wo
     if (backward && !c.dx && !c.dw && !c.db) return TBN_OK;
     return backward ? head::backward(c, workspace, workspace_bytes, s) : head::forward(c, workspace, workspace_bytes, s);
 }
+
+// ---- embedding, LayerNorm for training, AdamW -----------------------------------------------------------------------------
+constexpr int32_t kMostColumns = 1 << 23;              // of a row: 256 columns each are a grid's second index
+
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+inline bool misaligned(const void *p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype_bytes(dtype) - 1)) != 0; }
+
+bool embedding_sizes_ok(int64_t T, int32_t vocab, int32_t d)
+{
+    return T >= 0 && vocab > 0 && d > 0 && T <= kHeadMost && vocab <= kHeadMost && d <= kMostColumns;
+}
+
+// `rows`: T x d of `dtype`, written by the forward and read by the backward
+int embedding_check(const int64_t *ids, int64_t T, int32_t vocab, int32_t d, const void *rows, int dtype)
+{
+    if (T < 0 || vocab <= 0 || d <= 0 || !valid_dtype(dtype)) return TBN_ERR_INVALID_ARG;
+    if (!embedding_sizes_ok(T, vocab, d)) return TBN_ERR_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(ids) & 7u) || !aligned16(rows)) return TBN_ERR_INVALID_ARG;
+    return T > 0 && (!ids || !rows) ? TBN_ERR_INVALID_ARG : TBN_OK;
+}
+
+int adamw_grad_check(const tbn_adamw_tensor &t)
+{
+    if (t.n < 0 || !valid_dtype(t.grad_dtype)) return TBN_ERR_INVALID_ARG;
+    if (t.n > adamw::kMost) return TBN_ERR_UNSUPPORTED;
+    return t.n > 0 && (!t.grad || misaligned(t.grad, t.grad_dtype)) ? TBN_ERR_INVALID_ARG : TBN_OK;
+}
+
+bool adamw_scales_ok(const tbn_adamw_tensor &t) { return t.m_scale && t.v_scale && aligned4(t.m_scale) && aligned4(t.v_scale); }
 
 // Validation shared by the fully-connected and convolution entry points.
 int check_layer_common(const void *x, int x_dtype, const uint32_t *tile, int32_t k, const float *alpha,
@@ -900,6 +932,147 @@ int tbn_linear_distill_bwd(const void *x, const void *w, int dtype, int64_t T, i
     c.top_index = top_index; c.top_logit = top_logit; c.top_dtype = top_dtype; c.K = K; c.tau = tau; c.lse = lse; c.dloss = dloss;
     c.dx = dx; c.dx_dtype = dtype; c.dw = dw; c.dw_dtype = dw_dtype; c.db = dbias;
     return head_call(c, true, workspace, workspace_bytes, stream);
+}
+
+// ---- embedding, LayerNorm for training, AdamW ------------------------------------------------------------------------
+int tbn_embedding_fwd(const int64_t *ids, int64_t T, const void *table, int table_dtype, int32_t vocab, int32_t d, int64_t padding_idx,
+                      float scale, void *y, int y_dtype, void *stream)
+{
+    int rc = embedding_check(ids, T, vocab, d, y, y_dtype);
+    if (rc != TBN_OK) return rc;
+    if (!valid_dtype(table_dtype) || !aligned16(table)) return TBN_ERR_INVALID_ARG;
+    if (T == 0) return TBN_OK;
+    if (!table) return TBN_ERR_INVALID_ARG;
+    embed::LookupArgs a = {};
+    a.ids = ids; a.T = T; a.d = d; a.V = vocab; a.padding = padding_idx; a.scale = scale; a.table = table; a.table_dtype = table_dtype;
+    a.y = y; a.y_dtype = y_dtype;
+    return embed::lookup(a, static_cast<cudaStream_t>(stream));
+}
+
+int tbn_embedding_tiled_fwd(const int64_t *ids, int64_t T, int32_t vocab, int32_t d, const uint32_t *tile_bits, int32_t k, const float *alpha,
+                            int alpha_mode, int64_t padding_idx, float scale, void *y, int y_dtype, void *stream)
+{
+    int rc = embedding_check(ids, T, vocab, d, y, y_dtype);
+    if (rc != TBN_OK) return rc;
+    if (!tile_bits || !alpha || !aligned16(tile_bits) || (reinterpret_cast<uintptr_t>(alpha) & 3u) || k <= 0 || !valid_alpha_mode(alpha_mode))
+        return TBN_ERR_INVALID_ARG;
+    if ((int64_t)vocab * d % k != 0) return TBN_ERR_SHAPE;
+    if (T == 0) return TBN_OK;
+    embed::LookupArgs a = {};
+    a.ids = ids; a.T = T; a.d = d; a.V = vocab; a.padding = padding_idx; a.scale = scale;
+    a.tile = tile_bits; a.k = k; a.q = (int64_t)vocab * d / k; a.alpha = alpha; a.per_tile = alpha_mode == TBN_ALPHA_PER_TILE;
+    a.y = y; a.y_dtype = y_dtype;
+    return embed::lookup(a, static_cast<cudaStream_t>(stream));
+}
+
+size_t tbn_embedding_bwd_workspace_bytes(int64_t T, int32_t d, int32_t vocab)
+{
+    if (!embedding_sizes_ok(T, vocab, d) || T == 0) return 0;
+    return embed::gradient_workspace_bytes(T, d, vocab);
+}
+
+int tbn_embedding_bwd(const int64_t *ids, int64_t T, const void *dy, int dy_dtype, int32_t vocab, int32_t d, int64_t padding_idx, float scale,
+                      void *dw, int dw_dtype, int accumulate, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = embedding_check(ids, T, vocab, d, dy, dy_dtype);
+    if (rc != TBN_OK) return rc;
+    if (!dw || !aligned16(dw) || !valid_dtype(dw_dtype)) return TBN_ERR_INVALID_ARG;
+    if (T > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < embed::gradient_workspace_bytes(T, d, vocab))) return TBN_ERR_WORKSPACE;
+    embed::GradArgs a = {};
+    a.ids = ids; a.T = T; a.d = d; a.V = vocab; a.padding = padding_idx; a.scale = scale; a.dy = dy; a.dy_dtype = dy_dtype;
+    a.dw = dw; a.dw_dtype = dw_dtype; a.add = accumulate != 0;
+    return embed::gradient(a, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int tbn_layernorm_train_fwd(const void *x, const void *residual, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *beta, float eps,
+                            void *sum, void *y, int y_dtype, float *mean, float *rstd, void *stream)
+{
+    if (T < 0 || d <= 0 || !valid_dtype(x_dtype) || !valid_dtype(y_dtype) || !(eps >= 0.0f)) return TBN_ERR_INVALID_ARG;
+    if (T > kHeadMost || d > kMostColumns) return TBN_ERR_UNSUPPORTED;
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(sum) || !aligned16(y) || !aligned4(gamma) || !aligned4(beta) || !aligned4(mean) ||
+        !aligned4(rstd))
+        return TBN_ERR_INVALID_ARG;
+    if (T == 0) return TBN_OK;
+    if (!x || !y || (residual && !sum)) return TBN_ERR_INVALID_ARG;
+    norm::ForwardArgs a = {x, residual, x_dtype, y_dtype, T, d, gamma, beta, eps, residual ? sum : nullptr, y, mean, rstd};
+    return norm::forward(a, static_cast<cudaStream_t>(stream));
+}
+
+size_t tbn_layernorm_bwd_workspace_bytes(int64_t T, int32_t d)
+{
+    if (T <= 0 || d <= 0 || T > kHeadMost || d > kMostColumns) return 0;
+    return norm::backward_workspace_bytes(T, d);
+}
+
+int tbn_layernorm_bwd(const void *dy, int dy_dtype, const void *x, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *mean,
+                      const float *rstd, const void *dsum, void *dx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes,
+                      void *stream)
+{
+    if (T < 0 || d <= 0 || !valid_dtype(x_dtype) || !valid_dtype(dy_dtype)) return TBN_ERR_INVALID_ARG;
+    if (T > kHeadMost || d > kMostColumns) return TBN_ERR_UNSUPPORTED;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(dsum) || !aligned16(dx) || !aligned16(workspace) || !aligned4(gamma) || !aligned4(mean) ||
+        !aligned4(rstd) || !aligned4(dgamma) || !aligned4(dbeta))
+        return TBN_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (dgamma && cudaMemsetAsync(dgamma, 0, (size_t)d * 4, s) != cudaSuccess) return TBN_ERR_CUDA;
+        if (dbeta && cudaMemsetAsync(dbeta, 0, (size_t)d * 4, s) != cudaSuccess) return TBN_ERR_CUDA;
+        return TBN_OK;
+    }
+    if (!dy || !x || !mean || !rstd || !dx) return TBN_ERR_INVALID_ARG;
+    if ((dgamma || dbeta) && (!workspace || workspace_bytes < norm::backward_workspace_bytes(T, d))) return TBN_ERR_WORKSPACE;
+    norm::BackwardArgs a = {dy, x, dy_dtype, x_dtype, T, d, gamma, mean, rstd, dsum, dx, dgamma, dbeta};
+    return norm::backward(a, workspace, s);
+}
+
+int tbn_adamw_step(const tbn_adamw_tensor *tensors, int32_t count, int64_t step, const int64_t *step_dev, double lr, const float *lr_dev,
+                   double beta1, double beta2, double eps, const float *grad_scale, uint64_t seed, void *stream)
+{
+    if (count < 0 || (count > 0 && !tensors) || (!step_dev && step < 1) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
+        !(eps >= 1e-30 && eps <= 1e30) || (!lr_dev && !(lr >= -1e30 && lr <= 1e30)))
+        return TBN_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(step_dev) & 7u) || !aligned4(lr_dev) || !aligned4(grad_scale)) return TBN_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i) {
+        const tbn_adamw_tensor &t = tensors[i];
+        int rc = adamw_grad_check(t);
+        if (rc != TBN_OK) return rc;
+        if (!valid_dtype(t.param_dtype) || (t.state_bits != 32 && t.state_bits != 8) || !(t.weight_decay >= -1e30f && t.weight_decay <= 1e30f))
+            return TBN_ERR_INVALID_ARG;
+        if (t.n == 0) continue;
+        if (!t.param || !t.m || !t.v || misaligned(t.param, t.param_dtype) || (reinterpret_cast<uintptr_t>(t.copy) & 1u)) return TBN_ERR_INVALID_ARG;
+        if (t.state_bits == 32 ? (!aligned4(t.m) || !aligned4(t.v)) : !adamw_scales_ok(t)) return TBN_ERR_INVALID_ARG;
+    }
+    adamw::Hyper h = {};
+    h.lr = lr; h.beta1 = beta1; h.beta2 = beta2; h.eps = eps; h.step = step; h.step_dev = step_dev; h.lr_dev = lr_dev; h.grad_scale = grad_scale;
+    h.seed = seed;
+    return adamw::launch_step(tensors, count, h, static_cast<cudaStream_t>(stream));
+}
+
+size_t tbn_grad_norm_workspace_bytes(int32_t count) { return count < 0 ? 0 : adamw::norm_workspace_bytes(count); }
+
+int tbn_grad_norm(const tbn_adamw_tensor *tensors, int32_t count, double max_norm, float *norm, float *scale, void *workspace,
+                  size_t workspace_bytes, void *stream)
+{
+    if (count < 0 || (count > 0 && !tensors) || !(max_norm > 0.0) || !aligned4(norm) || !aligned4(scale)) return TBN_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i) {
+        const int rc = adamw_grad_check(tensors[i]);
+        if (rc != TBN_OK) return rc;
+    }
+    if (!workspace || !aligned16(workspace) || workspace_bytes < adamw::norm_workspace_bytes(count)) return TBN_ERR_WORKSPACE;
+    return adamw::launch_norm(tensors, count, max_norm, norm, scale, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int tbn_adamw_unpack(const tbn_adamw_tensor *tensors, int32_t count, float *const *m_out, float *const *v_out, void *stream)
+{
+    if (count < 0 || (count > 0 && !tensors)) return TBN_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i) {
+        const tbn_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || t.state_bits != 8) return TBN_ERR_INVALID_ARG;
+        if (t.n > adamw::kMost) return TBN_ERR_UNSUPPORTED;
+        if (t.n == 0) continue;
+        if (!t.m || !t.v || !adamw_scales_ok(t) || (m_out && !aligned4(m_out[i])) || (v_out && !aligned4(v_out[i]))) return TBN_ERR_INVALID_ARG;
+    }
+    return adamw::launch_unpack(tensors, count, m_out, v_out, static_cast<cudaStream_t>(stream));
 }
 
 int tbn_linear_compact_fwd(const void *z, int64_t T, int32_t rz, int32_t kz, const float *alpha_z, int alpha_mode_z, int act_z,

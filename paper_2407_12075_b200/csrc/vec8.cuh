@@ -1,0 +1,65 @@
+// Eight consecutive fp32 or bf16 values of a lane: one 32-byte or 16-byte access (a warp's request covers whole lines).
+#pragma once
+
+#include "common.cuh"
+
+namespace tbn {
+
+template <typename T> struct Raw8;                                   // as loaded: fp32 and bf16 keep their bits until they are used
+template <> struct Raw8<float> { uint32_t w[8]; };
+template <> struct Raw8<__nv_bfloat16> { uint32_t w[4]; };
+
+__device__ __forceinline__ Raw8<float> load8(const float *p)
+{
+    Raw8<float> r;
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+                 : "l"(p) : "memory");
+    return r;
+}
+__device__ __forceinline__ Raw8<__nv_bfloat16> load8(const __nv_bfloat16 *p)
+{
+    Raw8<__nv_bfloat16> r;
+    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p) : "memory");
+    return r;
+}
+__device__ __forceinline__ void unpack8(const Raw8<float> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r.w[e]);
+}
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[2 * e] = __uint_as_float(r.w[e] << 16);
+        v[2 * e + 1] = __uint_as_float(r.w[e] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8])
+{
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+                    "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])) : "memory");
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8])
+{
+    asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};"
+                 :: "l"(p), "r"(pack_bf16(v[0], v[1])), "r"(pack_bf16(v[2], v[3])), "r"(pack_bf16(v[4], v[5])), "r"(pack_bf16(v[6], v[7]))
+                 : "memory");
+}
+// Whether rows of `pitch` values from p on all begin where an access of eight values may.
+template <typename T> inline bool aligned8(const void *p, int64_t pitch = 0)
+{
+    return (reinterpret_cast<uintptr_t>(p) % (8 * sizeof(T))) == 0 && pitch % 8 == 0;
+}
+
+__device__ __forceinline__ float value_of(float v) { return v; }
+__device__ __forceinline__ float value_of(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+}  // namespace tbn
