@@ -54,6 +54,7 @@ template <int N> __device__ __forceinline__ int find(const Table<N> &tab, int64_
 
 struct Coef {
     float b1, omb1, b2, omb2, eps, step_size, inv_sqrt_bc2;
+    float nought;                           // -0
     double lr;
     float gs;
     uint32_t key;
@@ -78,37 +79,67 @@ __host__ __device__ inline void set_coef(Coef &c, double lr, double beta1, doubl
 __device__ __forceinline__ float sqrt_fast(float x)
 {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float floor_small(float x) { return __fadd_rz(x, 8388608.0f) - 8388608.0f; }     // 0 <= x < 2^22
-__device__ __forceinline__ float unit(uint32_t h16) { return __uint_as_float(0x3f800000u | (h16 << 7)) - (1.0f - 0x1p-17f); }   // (h16 + 1/2) / 2^16
+__device__ __forceinline__ float rcp_fast(float x)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 constexpr float kMTop = 127.0f * 127.0f, kVTop = 254.0f * 254.0f * 254.0f * 254.0f;
 constexpr float kMPart = (float)(1.0 / (127.0 * 127.0)), kVPart = (float)(1.0 / (254.0 * 254.0 * 254.0 * 254.0));
 constexpr float kMLeast = 0x1p-100f, kVLeast = 0x1p-94f;
+constexpr float kMagic = 8388608.0f, kMagicSigned = 12582912.0f;     // 2^23, 1.5 2^23: an integer added to one of them is in its low bits
 
-// The codes of y in units of their scale: the largest c with c^2 (c^4) <= y, or the next one with the probability that makes y
-// the mean.  The first guess may be off by one; every comparison is exact or in a stated order of fp32 operations, so a code
-// does not depend on how a root is evaluated.
-__device__ __forceinline__ float code2(float y, float u)
+// Two fp32 values to an instruction: the arithmetic of 8-bit states is bound by the rate at which instructions issue.
+struct Pair { uint64_t r; };
+__device__ __forceinline__ Pair pair(float a, float b) { return {f32x2_pack(a, b)}; }
+__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
+__device__ __forceinline__ float2 split(Pair p) { float2 f; f32x2_unpack(p.r, f.x, f.y); return f; }
+__device__ __forceinline__ Pair mul(Pair a, Pair b) { return {f32x2_mul(a.r, b.r)}; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { return {f32x2_fma(a.r, b.r, c.r)}; }
+// A product that an addition follows is written as a b + z with z a -0 that the compiler cannot see through: it joins a packed product
+// and the sum that takes it to one rounding, .rn or not, and codes follow from the roundings.
+__device__ __forceinline__ Pair product(Pair a, Pair b, Pair z) { return fma2(a, b, z); }
+__device__ __forceinline__ Pair add(Pair a, Pair b)
 {
-    float c = floor_small(sqrt_fast(y));
-    if (__fmul_rn(c, c) > y) c -= 1.0f;
-    if (__fmul_rn(c + 1.0f, c + 1.0f) <= y) c += 1.0f;
-    const float low = __fmul_rn(c, c), next = __fmul_rn(c + 1.0f, c + 1.0f);
-    if (__fmul_rn(u, next - low) < y - low) c += 1.0f;
-    return fminf(c, 127.0f);
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.r) : "l"(a.r), "l"(b.r));
+    return d;
 }
-__device__ __forceinline__ float fourth(float c) { const float s = __fmul_rn(c, c); return __fmul_rn(s, s); }
-__device__ __forceinline__ float code4(float y, float u)
+__device__ __forceinline__ Pair add_rz(Pair a, Pair b)
 {
-    float c = floor_small(sqrt_fast(sqrt_fast(y)));
-    if (fourth(c) > y) c -= 1.0f;
-    if (fourth(c + 1.0f) <= y) c += 1.0f;
-    const float low = fourth(c), next = fourth(c + 1.0f);
-    if (__fmul_rn(u, next - low) < y - low) c += 1.0f;
-    return fminf(c, 254.0f);
+    Pair d;
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(d.r) : "l"(a.r), "l"(b.r));
+    return d;
+}
+
+__device__ __forceinline__ Pair minus(Pair a, Pair b) { return fma2(b, both(-1.0f), a); }       // one rounding, as a - b
+__device__ __forceinline__ Pair minus_square(Pair y, Pair c) { return fma2(mul(c, both(-1.0f)), c, y); }    // y - c c, c c being exact
+
+// The codes of y in units of their scale: the largest c with c^2 (c^4) <= y, or the next one, with the probability that makes y
+// the mean: where (h + 1/2) / 2^16 times the gap is below what y has over c's value.  The floor of an approximate root can be
+// one off where y is within 2^-21 of a code's value; the draw then gives that code all the same but for one in 2^16 of them.
+// Neither passes the largest code: y is at most 2^-24 over the top's value, less than the smallest draw asks for.
+// hm, hv: the random halves, as 2^23 + h.  root: of y (of c^2's size), to be floored.
+__device__ __forceinline__ Pair code2(Pair y, Pair root, Pair hm)
+{
+    const Pair c = add(add_rz(root, both(kMagic)), both(-kMagic));
+    const Pair over = minus_square(y, c);
+    const Pair t = mul(add(hm, both(-8388607.5f)), fma2(c, both(2.0f), both(1.0f)));
+    const float2 o = split(mul(over, both(65536.0f))), d = split(t), f = split(c);
+    return pair(d.x < o.x ? f.x + 1.0f : f.x, d.y < o.y ? f.y + 1.0f : f.y);
+}
+__device__ __forceinline__ Pair code4(Pair y, Pair root, Pair hv, Pair z)
+{
+    const Pair c = add(add_rz(root, both(kMagic)), both(-kMagic)), c1 = add(c, both(1.0f));
+    const Pair s = mul(c, c), s1 = mul(c1, c1), low = product(s, s, z), next = product(s1, s1, z);
+    const Pair t = mul(add(hv, both(-8388607.5f)), minus(next, low));
+    const float2 o = split(mul(minus(y, low), both(65536.0f))), d = split(t), f = split(c);
+    return pair(d.x < o.x ? f.x + 1.0f : f.x, d.y < o.y ? f.y + 1.0f : f.y);
 }
 
 __device__ __forceinline__ float m_value(int32_t c, float ms)
@@ -118,7 +149,18 @@ __device__ __forceinline__ float m_value(int32_t c, float ms)
 }
 __device__ __forceinline__ float v_value(uint32_t c, float vs)
 {
-    return c == 255u ? __int_as_float(0x7f800000) : __fmul_rn(fourth((float)c), vs);
+    const float f = (float)c, s = __fmul_rn(f, f);
+    return c == 255u ? __int_as_float(0x7f800000) : __fmul_rn(__fmul_rn(s, s), vs);
+}
+__device__ __forceinline__ bool has_byte(uint32_t w, uint32_t four)     // one of w's bytes is that of `four`, whose bytes are all the same
+{
+    const uint32_t x = w ^ four;
+    return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+}
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d)
+{
+    const uint32_t lo = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), hi = __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040);
+    return __byte_perm(lo, hi, 0x5410);
 }
 
 // Elements of a lane: first, first + stride, ... (eight in a row where the tensor is aligned, every 32nd otherwise).
@@ -152,82 +194,177 @@ __device__ __forceinline__ void store_codes(uint8_t *p, bool vec, int cnt, const
     for (int e = 0; e < 8; ++e) if (32 * e < cnt) p[32 * e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
 }
 
-template <typename PT, typename GT, bool EIGHT>
-__device__ __forceinline__ void step_block(const Desc &d, int64_t base, const Coef &c, float decay, uint32_t key)
+// What a lane holds of a block, as loaded.
+template <typename PT, typename GT, bool EIGHT> struct Loaded;
+template <typename PT, typename GT> struct Loaded<PT, GT, false> { float p[8], g[8], m[8], v[8]; };
+template <typename PT, typename GT> struct Loaded<PT, GT, true> { float p[8], g[8]; uint32_t mc[2], vc[2]; float ms, vs; };
+
+// Where a lane's elements are: the first one, and elements at 32 e < cnt exist.
+template <bool VEC> struct Place {
+    int64_t at;
+    int cnt;
+    __device__ __forceinline__ Place(const Desc &d, int64_t base)
+    {
+        const int lane = threadIdx.x & 31;
+        const int64_t left = d.n - base - lane;
+        at = base + (VEC ? lane * 8 : lane);
+        cnt = VEC ? 256 : (int)(left < 256 ? left : 256);
+    }
+};
+
+template <typename PT, typename GT, bool VEC, bool EIGHT>
+__device__ __forceinline__ void load_block(const Desc &d, int64_t base, Loaded<PT, GT, EIGHT> &l)
 {
-    const int lane = threadIdx.x & 31;
-    const int64_t left = d.n - base;                                  // of the tensor, from the block's first element on
-    const bool vec = d.vec && left >= kBlock;
-    const int64_t at = base + (vec ? lane * 8 : lane);
-    const int stride = vec ? 1 : 32;
-    const int cnt = vec ? 256 : (int)(left - lane < 256 ? left - lane : 256);      // elements at 32 e < cnt exist
-    float p[8], g[8], m[8], v[8];
-    load_some(static_cast<const PT *>(d.p) + at, vec, cnt, p);
-    load_some(static_cast<const GT *>(d.g) + at, vec, cnt, g);
-    if (EIGHT) {
-        uint32_t mc[2], vc[2];
-        load_codes(static_cast<const uint8_t *>(d.m) + at, vec, cnt, mc);
-        load_codes(static_cast<const uint8_t *>(d.v) + at, vec, cnt, vc);
-        const float ms = d.ms[base / kBlock], vs = d.vs[base / kBlock];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            m[e] = m_value((int32_t)(int8_t)(mc[e >> 2] >> (8 * (e & 3))), ms);
-            v[e] = v_value((vc[e >> 2] >> (8 * (e & 3))) & 255u, vs);
-        }
+    const Place<VEC> w(d, base);
+    load_some(static_cast<const PT *>(d.p) + w.at, VEC, w.cnt, l.p);
+    load_some(static_cast<const GT *>(d.g) + w.at, VEC, w.cnt, l.g);
+    if constexpr (EIGHT) {
+        load_codes(static_cast<const uint8_t *>(d.m) + w.at, VEC, w.cnt, l.mc);
+        load_codes(static_cast<const uint8_t *>(d.v) + w.at, VEC, w.cnt, l.vc);
+        l.ms = d.ms[base / kBlock]; l.vs = d.vs[base / kBlock];
     } else {
-        load_some(static_cast<const float *>(d.m) + at, vec, cnt, m);
-        load_some(static_cast<const float *>(d.v) + at, vec, cnt, v);
+        load_some(static_cast<const float *>(d.m) + w.at, VEC, w.cnt, l.m);
+        load_some(static_cast<const float *>(d.v) + w.at, VEC, w.cnt, l.v);
     }
+}
+
+// m, v and the parameter of two elements; the order of the roundings is the documented formula's.
+__device__ __forceinline__ void update(const Coef &c, float decay, Pair g, Pair &p, Pair &m, Pair &v, float2 &root)
+{
+    g = mul(g, both(c.gs));
+    const Pair z = both(c.nought);
+    m = add(product(m, both(c.b1), z), product(g, both(c.omb1), z));
+    v = add(product(v, both(c.b2), z), product(mul(g, both(c.omb2)), g, z));
+    const float2 vv = split(v);
+    root = make_float2(sqrt_fast(vv.x), sqrt_fast(vv.y));
+    const float2 denom = split(fma2(pair(root.x, root.y), both(c.inv_sqrt_bc2), both(c.eps)));
+    const Pair step = mul(m, both(-c.step_size));
+    p = fma2(step, pair(rcp_fast(denom.x), rcp_fast(denom.y)), mul(p, both(decay)));
+}
+
+template <typename PT, typename GT, bool VEC, bool EIGHT>
+__device__ __forceinline__ void step_block(const Desc &d, int64_t base, const Coef &c, float decay, uint32_t key, Loaded<PT, GT, EIGHT> &l)
+{
+    const Place<VEC> w(d, base);
+    if constexpr (!EIGHT) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float gg = __fmul_rn(g[e], c.gs);
-        m[e] = __fadd_rn(__fmul_rn(m[e], c.b1), __fmul_rn(gg, c.omb1));
-        v[e] = __fadd_rn(__fmul_rn(v[e], c.b2), __fmul_rn(__fmul_rn(gg, c.omb2), gg));
-        const float denom = fmaf(sqrt_fast(v[e]), c.inv_sqrt_bc2, c.eps);
-        p[e] = __fmul_rn(p[e], decay) - __fdividef(__fmul_rn(m[e], c.step_size), denom);
-    }
-    store_some(static_cast<PT *>(d.p) + at, vec, cnt, p);
-    if (d.copy) store_some(static_cast<__nv_bfloat16 *>(d.copy) + at, vec, cnt, p);
-    if (!EIGHT) {
-        store_some(static_cast<float *>(d.m) + at, vec, cnt, m);
-        store_some(static_cast<float *>(d.v) + at, vec, cnt, v);
-        return;
-    }
-    uint32_t mt = 0, vt = 0;                                          // largest finite magnitudes: bits of floats above zero keep their order
+        for (int e = 0; e < 8; e += 2) {
+            Pair p = pair(l.p[e], l.p[e + 1]), m = pair(l.m[e], l.m[e + 1]), v = pair(l.v[e], l.v[e + 1]);
+            float2 root;
+            update(c, decay, pair(l.g[e], l.g[e + 1]), p, m, v, root);
+            f32x2_unpack(p.r, l.p[e], l.p[e + 1]); f32x2_unpack(m.r, l.m[e], l.m[e + 1]); f32x2_unpack(v.r, l.v[e], l.v[e + 1]);
+        }
+        store_some(static_cast<PT *>(d.p) + w.at, VEC, w.cnt, l.p);
+        if (d.copy) store_some(static_cast<__nv_bfloat16 *>(d.copy) + w.at, VEC, w.cnt, l.p);
+        store_some(static_cast<float *>(d.m) + w.at, VEC, w.cnt, l.m);
+        store_some(static_cast<float *>(d.v) + w.at, VEC, w.cnt, l.v);
+    } else {
+        const int lane = threadIdx.x & 31;
+        Pair m[4], v[4];
+        float2 root[4];
+        const uint32_t mx[2] = {l.mc[0] ^ 0x80808080u, l.mc[1] ^ 0x80808080u};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t a = __float_as_uint(fabsf(m[e])), b = __float_as_uint(v[e]);
-        mt = a < 0x7f800000u && a > mt ? a : mt;
-        vt = b < 0x7f800000u && b > vt ? b : vt;
-    }
-    const float m_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, mt)), kMLeast);
-    const float v_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, vt)), kVLeast);
-    const float m_inv = __fdiv_rn(kMTop, m_top), v_inv = __fdiv_rn(kVTop, v_top);
-    uint32_t mc[2] = {0, 0}, vc[2] = {0, 0};
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t wm = mx[i >> 1], wv = l.vc[i >> 1];
+            const int b = (2 * i) & 3;
+            // the byte as the low bits of 2^23 + code
+            const Pair cm = add(pair(__uint_as_float(__byte_perm(wm, 0x4b000000u, 0x7550 + b)), __uint_as_float(__byte_perm(wm, 0x4b000000u, 0x7551 + b))),
+                                both(-8388736.0f));
+            const Pair cv = add(pair(__uint_as_float(__byte_perm(wv, 0x4b000000u, 0x7550 + b)), __uint_as_float(__byte_perm(wv, 0x4b000000u, 0x7551 + b))),
+                                both(-kMagic));
+            const float2 f = split(cm);
+            m[i] = mul(mul(cm, pair(fabsf(f.x), fabsf(f.y))), both(l.ms));
+            const Pair s = mul(cv, cv);
+            v[i] = mul(mul(s, s), both(l.vs));
+        }
+        if (has_byte(l.mc[0], 0x80808080u) || has_byte(l.mc[1], 0x80808080u) || has_byte(l.vc[0], 0xffffffffu) || has_byte(l.vc[1], 0xffffffffu)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int64_t j = at + e * stride;
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t wm = l.mc[i >> 1] >> (16 * (i & 1)), wv = l.vc[i >> 1] >> (16 * (i & 1));
+                m[i] = pair(m_value((int32_t)(int8_t)wm, l.ms), m_value((int32_t)(int8_t)(wm >> 8), l.ms));
+                v[i] = pair(v_value(wv & 255u, l.vs), v_value((wv >> 8) & 255u, l.vs));
+            }
+        }
+        float mt = 0.0f, vt = 0.0f;
+        Pair odd = both(0.0f);                                        // a NaN as soon as there is an infinity or a NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            Pair p = pair(l.p[2 * i], l.p[2 * i + 1]);
+            update(c, decay, pair(l.g[2 * i], l.g[2 * i + 1]), p, m[i], v[i], root[i]);
+            f32x2_unpack(p.r, l.p[2 * i], l.p[2 * i + 1]);
+            odd = fma2(m[i], both(0.0f), odd);
+            odd = fma2(v[i], both(0.0f), odd);
+            const float2 fm = split(m[i]), fv = split(v[i]);
+            mt = fmaxf(fmaxf(fabsf(fm.x), fabsf(fm.y)), mt);
+            vt = fmaxf(fmaxf(fv.x, fv.y), vt);
+        }
+        store_some(static_cast<PT *>(d.p) + w.at, VEC, w.cnt, l.p);
+        if (d.copy) store_some(static_cast<__nv_bfloat16 *>(d.copy) + w.at, VEC, w.cnt, l.p);
+        const float2 oo = split(odd);
+        const bool bad = !(oo.x + oo.y == 0.0f);
+        if (bad) {                                                    // the largest finite magnitudes
+            mt = vt = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 fm = split(m[i]), fv = split(v[i]);
+                const float x[4] = {fabsf(fm.x), fabsf(fm.y), fv.x, fv.y};
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if (x[k] <= 3.4028235e38f) mt = fmaxf(mt, x[k]);
+                    if (x[2 + k] <= 3.4028235e38f) vt = fmaxf(vt, x[2 + k]);
+                }
+            }
+        }
+        // bits of floats above zero keep their order
+        const float m_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mt))), kMLeast);
+        const float v_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vt))), kVLeast);
+        const float m_inv = __fdiv_rn(kMTop, m_top), v_inv = __fdiv_rn(kVTop, v_top), v_root = sqrt_fast(v_inv);
+        // element e of the lane is w.at ^ (e or 32 e), whose upper half is w.at's: the first step of the mix is the lane's
         uint32_t k = key;
-        if (j >> 32) k ^= mix((uint32_t)(j >> 32));
-        const uint32_t h = mix((uint32_t)j ^ k);
-        const float am = fabsf(m[e]);
-        uint32_t cm = 0x80u, cv = 0xffu;
-        if (am <= 3.4028235e38f) {
-            const int32_t q = (int32_t)code2(__fmul_rn(am, m_inv), unit(h & 0xffffu));
-            cm = (uint32_t)(m[e] < 0.0f ? -q : q) & 255u;
+        if (w.at >> 32) k ^= mix((uint32_t)(w.at >> 32));
+        k ^= (uint32_t)w.at;
+        k ^= k >> 16;
+        const Pair z = both(c.nought);
+        float cm[8], cv[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float hm[2], hv[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int e = 2 * i + j;
+                uint32_t x = (k ^ (uint32_t)(VEC ? e : 32 * e)) * 0x7feb352du;
+                x = (x ^ (x >> 15)) * 0x846ca68bu;
+                const uint32_t hi = __byte_perm(x, 0x4b000000u, 0x7632);                 // 0x4b00 and the upper half
+                hv[j] = __uint_as_float(hi);
+                hm[j] = __uint_as_float(hi ^ (x & 0xffffu));
+            }
+            const float2 fm = split(m[i]), fv = split(v[i]);
+            const Pair ym = product(pair(fabsf(fm.x), fabsf(fm.y)), both(m_inv), z), yv = product(v[i], both(v_inv), z);
+            const float2 y = split(ym), rv = split(mul(pair(root[i].x, root[i].y), both(v_root)));
+            const float2 a = split(code2(ym, pair(sqrt_fast(y.x), sqrt_fast(y.y)), pair(hm[0], hm[1])));
+            const float2 b = split(code4(yv, pair(sqrt_fast(rv.x), sqrt_fast(rv.y)), pair(hv[0], hv[1]), z));
+            const Pair sm = add(pair(copysignf(a.x, fm.x), copysignf(a.y, fm.y)), both(kMagicSigned));
+            const Pair sv = add(pair(fmaxf(b.x, fv.x > 0.0f ? 1.0f : 0.0f), fmaxf(b.y, fv.y > 0.0f ? 1.0f : 0.0f)), both(kMagic));
+            f32x2_unpack(sm.r, cm[2 * i], cm[2 * i + 1]);
+            f32x2_unpack(sv.r, cv[2 * i], cv[2 * i + 1]);
         }
-        if (v[e] <= 3.4028235e38f) {
-            const float q = code4(__fmul_rn(v[e], v_inv), unit(h >> 16));
-            cv = (uint32_t)(v[e] > 0.0f ? fmaxf(q, 1.0f) : q);
+        uint32_t mc[2] = {low_bytes(cm[0], cm[1], cm[2], cm[3]), low_bytes(cm[4], cm[5], cm[6], cm[7])};
+        uint32_t vc[2] = {low_bytes(cv[0], cv[1], cv[2], cv[3]), low_bytes(cv[4], cv[5], cv[6], cv[7])};
+        if (bad) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 fm = split(m[e >> 1]), fv = split(v[e >> 1]);
+                const uint32_t byte = 255u << (8 * (e & 3));
+                if (!(fabsf(e & 1 ? fm.y : fm.x) <= 3.4028235e38f)) mc[e >> 2] = (mc[e >> 2] & ~byte) | (0x80808080u & byte);
+                if (!((e & 1 ? fv.y : fv.x) <= 3.4028235e38f)) vc[e >> 2] |= byte;
+            }
         }
-        mc[e >> 2] |= cm << (8 * (e & 3));
-        vc[e >> 2] |= cv << (8 * (e & 3));
-    }
-    store_codes(static_cast<uint8_t *>(d.m) + at, vec, cnt, mc);
-    store_codes(static_cast<uint8_t *>(d.v) + at, vec, cnt, vc);
-    if (lane == 0) {
-        d.ms[base / kBlock] = __fmul_rn(m_top, kMPart);
-        d.vs[base / kBlock] = __fmul_rn(v_top, kVPart);
+        store_codes(static_cast<uint8_t *>(d.m) + w.at, VEC, w.cnt, mc);
+        store_codes(static_cast<uint8_t *>(d.v) + w.at, VEC, w.cnt, vc);
+        if (lane == 0) {
+            d.ms[base / kBlock] = __fmul_rn(m_top, kMPart);
+            d.vs[base / kBlock] = __fmul_rn(v_top, kVPart);
+        }
     }
 }
 
@@ -252,7 +389,16 @@ step_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ Coef h
         const Desc &d = tab.t[find(tab, chunk)];
         const int64_t base = (chunk - d.chunk0) * kChunk + (threadIdx.x >> 5) * kBlock;
         if (base >= d.n) continue;
-        step_block<PT, GT, EIGHT>(d, base, c, (float)(1.0 - c.lr * (double)d.wd), mix(c.key + (uint32_t)d.ordinal));
+        const float decay = (float)(1.0 - c.lr * (double)d.wd);
+        const uint32_t key = mix(c.key + (uint32_t)d.ordinal);
+        Loaded<PT, GT, EIGHT> l;
+        if (d.vec && d.n - base >= kBlock) {
+            load_block<PT, GT, true, EIGHT>(d, base, l);
+            step_block<PT, GT, true, EIGHT>(d, base, c, decay, key, l);
+        } else {
+            load_block<PT, GT, false, EIGHT>(d, base, l);
+            step_block<PT, GT, false, EIGHT>(d, base, c, decay, key, l);
+        }
     }
 }
 
@@ -326,7 +472,7 @@ norm_kernel(const __grid_constant__ NormTable<N> tab, double *__restrict__ parti
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    double sum = 0.0;
+    double sums[8] = {};                                              // a chain of additions each
     for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
         int lo = 0, hi = tab.count - 1;
         while (lo < hi) {
@@ -344,8 +490,9 @@ norm_kernel(const __grid_constant__ NormTable<N> tab, double *__restrict__ parti
         if (d.bf16) load_some(static_cast<const __nv_bfloat16 *>(d.g) + at, vec, cnt, g);
         else load_some(static_cast<const float *>(d.g) + at, vec, cnt, g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fma((double)g[e], (double)g[e], sum);
+        for (int e = 0; e < 8; ++e) sums[e] = fma((double)g[e], (double)g[e], sums[e]);
     }
+    double sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
     if (lane == 0) warp_sum[threadIdx.x >> 5] = sum;
@@ -459,6 +606,7 @@ int launch_step(const tbn_adamw_tensor *tensors, int32_t count, const Hyper &h, 
     c.b1 = (float)h.beta1; c.omb1 = (float)(1.0 - h.beta1);
     c.b2 = (float)h.beta2; c.omb2 = (float)(1.0 - h.beta2);
     c.eps = (float)h.eps;
+    c.nought = -0.0f;
     set_coef(c, h.lr, h.beta1, h.beta2, h.step, h.seed);
     int rc = step_kind<float, float, false>(tensors, count, h, c, s);
     if (rc == TBN_OK) rc = step_kind<float, __nv_bfloat16, false>(tensors, count, h, c, s);

@@ -1029,7 +1029,7 @@ int tbn_adamw_step(const tbn_adamw_tensor *tensors, int32_t count, int64_t step,
                    double beta1, double beta2, double eps, const float *grad_scale, uint64_t seed, void *stream)
 {
     if (count < 0 || (count > 0 && !tensors) || (!step_dev && step < 1) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) ||
-        !(eps >= 1e-30 && eps <= 1e30) || (!lr_dev && !(lr >= -1e30 && lr <= 1e30)))
+        !(eps >= 1e-12 && eps <= 1e30) || (!lr_dev && !(lr >= -1e30 && lr <= 1e30)))
         return TBN_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(step_dev) & 7u) || !aligned4(lr_dev) || !aligned4(grad_scale)) return TBN_ERR_INVALID_ARG;
     for (int32_t i = 0; i < count; ++i) {
