@@ -9,6 +9,7 @@
 // Rounding is at random, with the value as its mean: with beta2 = 0.999 a step moves v by a thousandth where the codes are a
 // sixtieth apart at best, and rounded to nearest it would stay where it is for good.
 #include <atomic>
+#include <type_traits>
 
 #include "adamw.cuh"
 #include "vec8.cuh"
@@ -19,7 +20,11 @@ namespace adamw {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = kThreads * 8;        // elements that a thread block takes at a time
+constexpr int kWarps = kThreads / 32;
+// Thread blocks to an SM.  With 8-bit states a warp loads its next block while it computes, for which the registers are needed; with 32-bit
+// ones there is little to compute and a fourth thread block hides more.
+constexpr int step_per_sm(bool eight) { return eight ? 3 : 4; }
+constexpr int kNormPerSm = 6, kUnpackPerSm = 8;
 
 struct Desc {
     void *p;
@@ -35,21 +40,24 @@ struct Desc {
 };
 
 // Tensors go to the kernel in its parameters: nothing to copy, nothing that a captured graph could find changed.
-template <int N> struct Table {
-    Desc t[N];
-    int32_t count;
+// A chunk is what a thread block takes at a time: `per` blocks of 256 elements to each warp, so that what a tensor takes to be found and
+// set up is paid once for them; one block where there is too little work for every SM otherwise.
+template <typename D, int N> struct TableOf {
+    D t[N];
+    int32_t count, per;
     int64_t chunks;
 };
+template <int N> using Table = TableOf<Desc, N>;
 constexpr int kFew = 24, kMany = 256;       // 2 KB and 22 KB of parameters
 
-template <int N> __device__ __forceinline__ int find(const Table<N> &tab, int64_t chunk)
+template <typename D, int N> __device__ __forceinline__ const D &find(const TableOf<D, N> &tab, int64_t chunk)
 {
     int lo = 0, hi = tab.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (tab.t[mid].chunk0 <= chunk) lo = mid; else hi = mid - 1;
     }
-    return lo;
+    return tab.t[lo];
 }
 
 struct Coef {
@@ -120,26 +128,37 @@ __device__ __forceinline__ Pair add_rz(Pair a, Pair b)
 __device__ __forceinline__ Pair minus(Pair a, Pair b) { return fma2(b, both(-1.0f), a); }       // one rounding, as a - b
 __device__ __forceinline__ Pair minus_square(Pair y, Pair c) { return fma2(mul(c, both(-1.0f)), c, y); }    // y - c c, c c being exact
 
+__device__ __forceinline__ float one_if_less(float a, float b)
+{
+    float r;
+    asm("set.lt.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)  // NaN if one of them is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
 // The codes of y in units of their scale: the largest c with c^2 (c^4) <= y, or the next one, with the probability that makes y
-// the mean: where (h + 1/2) / 2^16 times the gap is below what y has over c's value.  The floor of an approximate root can be
-// one off where y is within 2^-21 of a code's value; the draw then gives that code all the same but for one in 2^16 of them.
-// Neither passes the largest code: y is at most 2^-24 over the top's value, less than the smallest draw asks for.
-// hm, hv: the random halves, as 2^23 + h.  root: of y (of c^2's size), to be floored.
-__device__ __forceinline__ Pair code2(Pair y, Pair root, Pair hm)
+// the mean: where u times the gap is below what y has over c's value.  The floor of an approximate root can be one off where y is within
+// 2^-21 of a code's value; the draw then gives that code all the same but for one in 2^16 of them.  Neither passes the largest code: y
+// is at most 2^-24 over the top's value, less than the smallest draw asks for.  root: of y (of c^2's size), to be floored.
+__device__ __forceinline__ Pair code2(Pair y, Pair root, Pair u)
 {
     const Pair c = add(add_rz(root, both(kMagic)), both(-kMagic));
-    const Pair over = minus_square(y, c);
-    const Pair t = mul(add(hm, both(-8388607.5f)), fma2(c, both(2.0f), both(1.0f)));
-    const float2 o = split(mul(over, both(65536.0f))), d = split(t), f = split(c);
-    return pair(d.x < o.x ? f.x + 1.0f : f.x, d.y < o.y ? f.y + 1.0f : f.y);
+    const Pair over = minus_square(y, c), t = mul(u, fma2(c, both(2.0f), both(1.0f)));
+    const float2 o = split(over), d = split(t);
+    return add(c, pair(one_if_less(d.x, o.x), one_if_less(d.y, o.y)));
 }
-__device__ __forceinline__ Pair code4(Pair y, Pair root, Pair hv, Pair z)
+__device__ __forceinline__ Pair code4(Pair y, Pair root, Pair u, Pair z)
 {
     const Pair c = add(add_rz(root, both(kMagic)), both(-kMagic)), c1 = add(c, both(1.0f));
     const Pair s = mul(c, c), s1 = mul(c1, c1), low = product(s, s, z), next = product(s1, s1, z);
-    const Pair t = mul(add(hv, both(-8388607.5f)), minus(next, low));
-    const float2 o = split(mul(minus(y, low), both(65536.0f))), d = split(t), f = split(c);
-    return pair(d.x < o.x ? f.x + 1.0f : f.x, d.y < o.y ? f.y + 1.0f : f.y);
+    const Pair over = minus(y, low), t = mul(u, minus(next, low));
+    const float2 o = split(over), d = split(t);
+    return add(c, pair(one_if_less(d.x, o.x), one_if_less(d.y, o.y)));
 }
 
 __device__ __forceinline__ float m_value(int32_t c, float ms)
@@ -170,6 +189,19 @@ template <typename T> __device__ __forceinline__ void load_some(const T *p, bool
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 32 * e < cnt ? value_of(p[32 * e]) : 0.0f;
 }
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
+template <bool VEC, typename T> __device__ __forceinline__ void load_raw(const T *p, int cnt, Raw8<T> &r)
+{
+    if (VEC) { r = load8(p); return; }
+    constexpr int kPer = 4 / (int)sizeof(T);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t b = 32 * e < cnt ? bits_of(p[32 * e]) : 0u;
+        if (e % kPer == 0) r.w[e / kPer] = b;
+        else r.w[e / kPer] |= b << 16;
+    }
+}
 template <typename T> __device__ __forceinline__ void store_some(T *p, bool vec, int cnt, const float (&v)[8])
 {
     if (vec) { store8(p, v); return; }
@@ -196,37 +228,88 @@ __device__ __forceinline__ void store_codes(uint8_t *p, bool vec, int cnt, const
 
 // What a lane holds of a block, as loaded.
 template <typename PT, typename GT, bool EIGHT> struct Loaded;
-template <typename PT, typename GT> struct Loaded<PT, GT, false> { float p[8], g[8], m[8], v[8]; };
-template <typename PT, typename GT> struct Loaded<PT, GT, true> { float p[8], g[8]; uint32_t mc[2], vc[2]; float ms, vs; };
+template <typename PT, typename GT> struct Loaded<PT, GT, false> { Raw8<PT> p; Raw8<GT> g; Raw8<float> m, v; };
+template <typename PT, typename GT> struct Loaded<PT, GT, true> { Raw8<PT> p; Raw8<GT> g; uint32_t mc[2], vc[2]; float ms, vs; };
 
-// Where a lane's elements are: the first one, and elements at 32 e < cnt exist.
-template <bool VEC> struct Place {
-    int64_t at;
-    int cnt;
-    __device__ __forceinline__ Place(const Desc &d, int64_t base)
+// Where a lane's elements of a block are (VEC: eight in a row, otherwise every 32nd).
+template <typename PT, typename GT, bool VEC, bool EIGHT> struct Cursor {
+    typedef typename std::conditional<EIGHT, uint8_t, float>::type ST;
+    PT *p;
+    const GT *g;
+    ST *m, *v;
+    __nv_bfloat16 *copy;
+    float *ms, *vs;
+    __device__ __forceinline__ Cursor(const Desc &d, int64_t base)
     {
-        const int lane = threadIdx.x & 31;
-        const int64_t left = d.n - base - lane;
-        at = base + (VEC ? lane * 8 : lane);
-        cnt = VEC ? 256 : (int)(left < 256 ? left : 256);
+        const int64_t at = base + (threadIdx.x & 31) * (VEC ? 8 : 1);
+        p = static_cast<PT *>(d.p) + at; g = static_cast<const GT *>(d.g) + at;
+        m = static_cast<ST *>(d.m) + at; v = static_cast<ST *>(d.v) + at;
+        copy = d.copy ? static_cast<__nv_bfloat16 *>(d.copy) + at : nullptr;
+        if (EIGHT) { ms = d.ms + base / kBlock; vs = d.vs + base / kBlock; }
+    }
+    __device__ __forceinline__ void on()
+    {
+        p += kBlock; g += kBlock; m += kBlock; v += kBlock;
+        if (copy) copy += kBlock;
+    }
+    __device__ __forceinline__ void load(Loaded<PT, GT, EIGHT> &l, int cnt) const
+    {
+        load_raw<VEC>(p, cnt, l.p);
+        load_raw<VEC>(g, cnt, l.g);
+        if constexpr (EIGHT) {
+            load_codes(m, VEC, cnt, l.mc);
+            load_codes(v, VEC, cnt, l.vc);
+            l.ms = *ms; l.vs = *vs;
+        } else {
+            load_raw<VEC>(m, cnt, l.m);
+            load_raw<VEC>(v, cnt, l.v);
+        }
+    }
+    __device__ __forceinline__ void store_param(const float (&x)[8], int cnt) const
+    {
+        store_some(p, VEC, cnt, x);
+        if (copy) store_some(copy, VEC, cnt, x);
     }
 };
 
-template <typename PT, typename GT, bool VEC, bool EIGHT>
-__device__ __forceinline__ void load_block(const Desc &d, int64_t base, Loaded<PT, GT, EIGHT> &l)
-{
-    const Place<VEC> w(d, base);
-    load_some(static_cast<const PT *>(d.p) + w.at, VEC, w.cnt, l.p);
-    load_some(static_cast<const GT *>(d.g) + w.at, VEC, w.cnt, l.g);
-    if constexpr (EIGHT) {
-        load_codes(static_cast<const uint8_t *>(d.m) + w.at, VEC, w.cnt, l.mc);
-        load_codes(static_cast<const uint8_t *>(d.v) + w.at, VEC, w.cnt, l.vc);
-        l.ms = d.ms[base / kBlock]; l.vs = d.vs[base / kBlock];
-    } else {
-        load_some(static_cast<const float *>(d.m) + w.at, VEC, w.cnt, l.m);
-        load_some(static_cast<const float *>(d.v) + w.at, VEC, w.cnt, l.v);
+// Blocks on their way from memory: a ring of a warp's own in shared memory, filled by asynchronous copies, so that two blocks are being
+// fetched while a third is computed without a register held for them.
+constexpr int kStages = 3;
+template <typename PT, typename GT> struct Ring {
+    static constexpr int kP = 0, kG = kBlock * (int)sizeof(PT), kM = kG + kBlock * (int)sizeof(GT), kV = kM + kBlock, kBytes = kV + kBlock;
+    static __device__ __forceinline__ void copy16(uint32_t to, const void *from)
+    {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
     }
-}
+    static __device__ __forceinline__ void fetch(uint32_t to, const Cursor<PT, GT, true, true> &at, int ahead)
+    {
+        const int lane = threadIdx.x & 31;
+        const int k = ahead * kBlock;
+        // 512 bytes to a copy of the warp: of fp32 values the lane's own eight are copied by two lanes
+        const char *p = reinterpret_cast<const char *>(at.p + k) - lane * (8 * (int)sizeof(PT) - 16);
+        const char *g = reinterpret_cast<const char *>(at.g + k) - lane * (8 * (int)sizeof(GT) - 16);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(PT) / 2; ++i) copy16(to + kP + i * 512 + lane * 16, p + i * 512);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(GT) / 2; ++i) copy16(to + kG + i * 512 + lane * 16, g + i * 512);
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to + kM + lane * 8), "l"(at.m + k) : "memory");
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to + kV + lane * 8), "l"(at.v + k) : "memory");
+    }
+    template <typename T> static __device__ __forceinline__ void take8(const char *from, Raw8<T> &r)
+    {
+        const uint4 *q = reinterpret_cast<const uint4 *>(from + (threadIdx.x & 31) * (8 * sizeof(T)));
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) { const uint4 x = q[i]; r.w[4 * i] = x.x; r.w[4 * i + 1] = x.y; r.w[4 * i + 2] = x.z; r.w[4 * i + 3] = x.w; }
+    }
+    static __device__ __forceinline__ void take(const char *from, Loaded<PT, GT, true> &l)
+    {
+        const int lane = threadIdx.x & 31;
+        take8(from + kP, l.p);
+        take8(from + kG, l.g);
+        const uint2 m = *reinterpret_cast<const uint2 *>(from + kM + lane * 8), v = *reinterpret_cast<const uint2 *>(from + kV + lane * 8);
+        l.mc[0] = m.x; l.mc[1] = m.y; l.vc[0] = v.x; l.vc[1] = v.y;
+    }
+};
 
 // m, v and the parameter of two elements; the order of the roundings is the documented formula's.
 __device__ __forceinline__ void update(const Coef &c, float decay, Pair g, Pair &p, Pair &m, Pair &v, float2 &root)
@@ -242,137 +325,142 @@ __device__ __forceinline__ void update(const Coef &c, float decay, Pair g, Pair 
     p = fma2(step, pair(rcp_fast(denom.x), rcp_fast(denom.y)), mul(p, both(decay)));
 }
 
-template <typename PT, typename GT, bool VEC, bool EIGHT>
-__device__ __forceinline__ void step_block(const Desc &d, int64_t base, const Coef &c, float decay, uint32_t key, Loaded<PT, GT, EIGHT> &l)
+// With 32-bit states.
+template <typename PT, typename GT, bool VEC>
+__device__ __forceinline__ void step_block(const Cursor<PT, GT, VEC, false> &at, int cnt, const Coef &c, float decay, const Loaded<PT, GT, false> &l)
 {
-    const Place<VEC> w(d, base);
-    if constexpr (!EIGHT) {
+    float p[8], g[8], m[8], v[8];
+    unpack8(l.p, p);
+    unpack8(l.g, g);
+    unpack8(l.m, m);
+    unpack8(l.v, v);
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            Pair p = pair(l.p[e], l.p[e + 1]), m = pair(l.m[e], l.m[e + 1]), v = pair(l.v[e], l.v[e + 1]);
-            float2 root;
-            update(c, decay, pair(l.g[e], l.g[e + 1]), p, m, v, root);
-            f32x2_unpack(p.r, l.p[e], l.p[e + 1]); f32x2_unpack(m.r, l.m[e], l.m[e + 1]); f32x2_unpack(v.r, l.v[e], l.v[e + 1]);
-        }
-        store_some(static_cast<PT *>(d.p) + w.at, VEC, w.cnt, l.p);
-        if (d.copy) store_some(static_cast<__nv_bfloat16 *>(d.copy) + w.at, VEC, w.cnt, l.p);
-        store_some(static_cast<float *>(d.m) + w.at, VEC, w.cnt, l.m);
-        store_some(static_cast<float *>(d.v) + w.at, VEC, w.cnt, l.v);
-    } else {
-        const int lane = threadIdx.x & 31;
-        Pair m[4], v[4];
-        float2 root[4];
-        const uint32_t mx[2] = {l.mc[0] ^ 0x80808080u, l.mc[1] ^ 0x80808080u};
+    for (int e = 0; e < 8; e += 2) {
+        Pair pp = pair(p[e], p[e + 1]), mm = pair(m[e], m[e + 1]), vv = pair(v[e], v[e + 1]);
+        float2 root;
+        update(c, decay, pair(g[e], g[e + 1]), pp, mm, vv, root);
+        f32x2_unpack(pp.r, p[e], p[e + 1]); f32x2_unpack(mm.r, m[e], m[e + 1]); f32x2_unpack(vv.r, v[e], v[e + 1]);
+    }
+    at.store_param(p, cnt);
+    store_some(at.m, VEC, cnt, m);
+    store_some(at.v, VEC, cnt, v);
+}
+
+// With 8-bit states; the block's new scales go to ms and vs.  k: what the random numbers of the block follow from (the tensor's key and the lane's first element).
+template <typename PT, typename GT, bool VEC>
+__device__ __forceinline__ void step_block(const Cursor<PT, GT, VEC, true> &at, int cnt, const Coef &c, float decay, uint32_t k,
+                                           const Loaded<PT, GT, true> &l, float &ms, float &vs)
+{
+    float p[8], g[8];
+    unpack8(l.p, p);
+    unpack8(l.g, g);
+    Pair m[4], v[4];
+    float2 root[4];
+    const uint32_t mx[2] = {l.mc[0] ^ 0x80808080u, l.mc[1] ^ 0x80808080u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t wm = mx[i >> 1], wv = l.vc[i >> 1];
-            const int b = (2 * i) & 3;
-            // the byte as the low bits of 2^23 + code
-            const Pair cm = add(pair(__uint_as_float(__byte_perm(wm, 0x4b000000u, 0x7550 + b)), __uint_as_float(__byte_perm(wm, 0x4b000000u, 0x7551 + b))),
-                                both(-8388736.0f));
-            const Pair cv = add(pair(__uint_as_float(__byte_perm(wv, 0x4b000000u, 0x7550 + b)), __uint_as_float(__byte_perm(wv, 0x4b000000u, 0x7551 + b))),
-                                both(-kMagic));
-            const float2 f = split(cm);
-            m[i] = mul(mul(cm, pair(fabsf(f.x), fabsf(f.y))), both(l.ms));
-            const Pair s = mul(cv, cv);
-            v[i] = mul(mul(s, s), both(l.vs));
-        }
-        if (has_byte(l.mc[0], 0x80808080u) || has_byte(l.mc[1], 0x80808080u) || has_byte(l.vc[0], 0xffffffffu) || has_byte(l.vc[1], 0xffffffffu)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t wm = l.mc[i >> 1] >> (16 * (i & 1)), wv = l.vc[i >> 1] >> (16 * (i & 1));
-                m[i] = pair(m_value((int32_t)(int8_t)wm, l.ms), m_value((int32_t)(int8_t)(wm >> 8), l.ms));
-                v[i] = pair(v_value(wv & 255u, l.vs), v_value((wv >> 8) & 255u, l.vs));
-            }
-        }
-        float mt = 0.0f, vt = 0.0f;
-        Pair odd = both(0.0f);                                        // a NaN as soon as there is an infinity or a NaN
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            Pair p = pair(l.p[2 * i], l.p[2 * i + 1]);
-            update(c, decay, pair(l.g[2 * i], l.g[2 * i + 1]), p, m[i], v[i], root[i]);
-            f32x2_unpack(p.r, l.p[2 * i], l.p[2 * i + 1]);
-            odd = fma2(m[i], both(0.0f), odd);
-            odd = fma2(v[i], both(0.0f), odd);
-            const float2 fm = split(m[i]), fv = split(v[i]);
-            mt = fmaxf(fmaxf(fabsf(fm.x), fabsf(fm.y)), mt);
-            vt = fmaxf(fmaxf(fv.x, fv.y), vt);
-        }
-        store_some(static_cast<PT *>(d.p) + w.at, VEC, w.cnt, l.p);
-        if (d.copy) store_some(static_cast<__nv_bfloat16 *>(d.copy) + w.at, VEC, w.cnt, l.p);
-        const float2 oo = split(odd);
-        const bool bad = !(oo.x + oo.y == 0.0f);
-        if (bad) {                                                    // the largest finite magnitudes
-            mt = vt = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 fm = split(m[i]), fv = split(v[i]);
-                const float x[4] = {fabsf(fm.x), fabsf(fm.y), fv.x, fv.y};
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    if (x[k] <= 3.4028235e38f) mt = fmaxf(mt, x[k]);
-                    if (x[2 + k] <= 3.4028235e38f) vt = fmaxf(vt, x[2 + k]);
-                }
-            }
-        }
-        // bits of floats above zero keep their order
-        const float m_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mt))), kMLeast);
-        const float v_top = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vt))), kVLeast);
-        const float m_inv = __fdiv_rn(kMTop, m_top), v_inv = __fdiv_rn(kVTop, v_top), v_root = sqrt_fast(v_inv);
-        // element e of the lane is w.at ^ (e or 32 e), whose upper half is w.at's: the first step of the mix is the lane's
-        uint32_t k = key;
-        if (w.at >> 32) k ^= mix((uint32_t)(w.at >> 32));
-        k ^= (uint32_t)w.at;
-        k ^= k >> 16;
-        const Pair z = both(c.nought);
-        float cm[8], cv[8];
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t wm = mx[i >> 1], wv = l.vc[i >> 1];
+        const int b = (2 * i) & 3;
+        // the byte as the low bits of 2^23 + code
+        const Pair cm = add(pair(__uint_as_float(__byte_perm(wm, 0x4b000000u, 0x7550 + b)), __uint_as_float(__byte_perm(wm, 0x4b000000u, 0x7551 + b))),
+                            both(-8388736.0f));
+        const Pair cv = add(pair(__uint_as_float(__byte_perm(wv, 0x4b000000u, 0x7550 + b)), __uint_as_float(__byte_perm(wv, 0x4b000000u, 0x7551 + b))),
+                            both(-kMagic));
+        const float2 f = split(cm);
+        m[i] = mul(pair(__fmul_rn(f.x, fabsf(f.x)), __fmul_rn(f.y, fabsf(f.y))), both(l.ms));
+        const Pair s = mul(cv, cv);
+        v[i] = mul(mul(s, s), both(l.vs));
+    }
+    if (has_byte(l.mc[0], 0x80808080u) || has_byte(l.mc[1], 0x80808080u) || has_byte(l.vc[0], 0xffffffffu) || has_byte(l.vc[1], 0xffffffffu)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float hm[2], hv[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int e = 2 * i + j;
-                uint32_t x = (k ^ (uint32_t)(VEC ? e : 32 * e)) * 0x7feb352du;
-                x = (x ^ (x >> 15)) * 0x846ca68bu;
-                const uint32_t hi = __byte_perm(x, 0x4b000000u, 0x7632);                 // 0x4b00 and the upper half
-                hv[j] = __uint_as_float(hi);
-                hm[j] = __uint_as_float(hi ^ (x & 0xffffu));
-            }
-            const float2 fm = split(m[i]), fv = split(v[i]);
-            const Pair ym = product(pair(fabsf(fm.x), fabsf(fm.y)), both(m_inv), z), yv = product(v[i], both(v_inv), z);
-            const float2 y = split(ym), rv = split(mul(pair(root[i].x, root[i].y), both(v_root)));
-            const float2 a = split(code2(ym, pair(sqrt_fast(y.x), sqrt_fast(y.y)), pair(hm[0], hm[1])));
-            const float2 b = split(code4(yv, pair(sqrt_fast(rv.x), sqrt_fast(rv.y)), pair(hv[0], hv[1]), z));
-            const Pair sm = add(pair(copysignf(a.x, fm.x), copysignf(a.y, fm.y)), both(kMagicSigned));
-            const Pair sv = add(pair(fmaxf(b.x, fv.x > 0.0f ? 1.0f : 0.0f), fmaxf(b.y, fv.y > 0.0f ? 1.0f : 0.0f)), both(kMagic));
-            f32x2_unpack(sm.r, cm[2 * i], cm[2 * i + 1]);
-            f32x2_unpack(sv.r, cv[2 * i], cv[2 * i + 1]);
-        }
-        uint32_t mc[2] = {low_bytes(cm[0], cm[1], cm[2], cm[3]), low_bytes(cm[4], cm[5], cm[6], cm[7])};
-        uint32_t vc[2] = {low_bytes(cv[0], cv[1], cv[2], cv[3]), low_bytes(cv[4], cv[5], cv[6], cv[7])};
-        if (bad) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float2 fm = split(m[e >> 1]), fv = split(v[e >> 1]);
-                const uint32_t byte = 255u << (8 * (e & 3));
-                if (!(fabsf(e & 1 ? fm.y : fm.x) <= 3.4028235e38f)) mc[e >> 2] = (mc[e >> 2] & ~byte) | (0x80808080u & byte);
-                if (!((e & 1 ? fv.y : fv.x) <= 3.4028235e38f)) vc[e >> 2] |= byte;
-            }
-        }
-        store_codes(static_cast<uint8_t *>(d.m) + w.at, VEC, w.cnt, mc);
-        store_codes(static_cast<uint8_t *>(d.v) + w.at, VEC, w.cnt, vc);
-        if (lane == 0) {
-            d.ms[base / kBlock] = __fmul_rn(m_top, kMPart);
-            d.vs[base / kBlock] = __fmul_rn(v_top, kVPart);
+            const uint32_t wm = l.mc[i >> 1] >> (16 * (i & 1)), wv = l.vc[i >> 1] >> (16 * (i & 1));
+            m[i] = pair(m_value((int32_t)(int8_t)wm, l.ms), m_value((int32_t)(int8_t)(wm >> 8), l.ms));
+            v[i] = pair(v_value(wv & 255u, l.vs), v_value((wv >> 8) & 255u, l.vs));
         }
     }
+    float mt = 0.0f, vt = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        Pair pp = pair(p[2 * i], p[2 * i + 1]);
+        update(c, decay, pair(g[2 * i], g[2 * i + 1]), pp, m[i], v[i], root[i]);
+        f32x2_unpack(pp.r, p[2 * i], p[2 * i + 1]);
+        const float2 fm = split(m[i]), fv = split(v[i]);
+        mt = max3_nan(mt, fabsf(fm.x), fabsf(fm.y));
+        vt = max3_nan(vt, fv.x, fv.y);
+    }
+    at.store_param(p, cnt);
+    // bits of floats above zero keep their order; those of infinity and NaN come last
+    uint32_t mb = __reduce_max_sync(0xffffffffu, __float_as_uint(mt)), vb = __reduce_max_sync(0xffffffffu, __float_as_uint(vt));
+    const bool bad = mb >= 0x7f800000u || vb >= 0x7f800000u;
+    if (bad) {                                                        // the largest finite magnitudes
+        mb = vb = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 fm = split(m[i]), fv = split(v[i]);
+            const uint32_t x[4] = {__float_as_uint(fabsf(fm.x)), __float_as_uint(fabsf(fm.y)), __float_as_uint(fv.x), __float_as_uint(fv.y)};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (x[j] < 0x7f800000u && x[j] > mb) mb = x[j];
+                if (x[2 + j] < 0x7f800000u && x[2 + j] > vb) vb = x[2 + j];
+            }
+        }
+        mb = __reduce_max_sync(0xffffffffu, mb);
+        vb = __reduce_max_sync(0xffffffffu, vb);
+    }
+    const float m_top = fmaxf(__uint_as_float(mb), kMLeast), v_top = fmaxf(__uint_as_float(vb), kVLeast);
+    const float m_inv = __fdiv_rn(kMTop, m_top), v_inv = __fdiv_rn(kVTop, v_top), v_root = sqrt_fast(v_inv);
+    const Pair z = both(c.nought);
+    float cm[8], cv[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float hm[2], hv[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            // mix(key ^ element): the element is the lane's first one ^ e or 32 e, so the first step of the mix is the lane's; the halves as
+            // the low bits of 128 + h / 2^16
+            const int e = 2 * i + j;
+            uint32_t x = (k ^ (uint32_t)(VEC ? e : 32 * e)) * 0x7feb352du;
+            x = (x ^ (x >> 15)) * 0x846ca68bu;
+            const uint32_t hi = __byte_perm(x, 0x43000000u, 0x7632);
+            hv[j] = __uint_as_float(hi);
+            hm[j] = __uint_as_float(hi ^ (x & 0xffffu));
+        }
+        const Pair shift = both(-(128.0f - 0x1p-17f));                // (h + 1/2) / 2^16, in no order of roundings: it is exact
+        const float2 fm = split(m[i]);
+        const Pair ym = pair(__fmul_rn(fabsf(fm.x), m_inv), __fmul_rn(fabsf(fm.y), m_inv)), yv = product(v[i], both(v_inv), z);
+        const float2 y = split(ym), rv = split(mul(pair(root[i].x, root[i].y), both(v_root)));
+        const float2 a = split(code2(ym, pair(sqrt_fast(y.x), sqrt_fast(y.y)), add(pair(hm[0], hm[1]), shift)));
+        const Pair b = code4(yv, pair(sqrt_fast(rv.x), sqrt_fast(rv.y)), add(pair(hv[0], hv[1]), shift), z);
+        const Pair sm = add(pair(copysignf(a.x, fm.x), copysignf(a.y, fm.y)), both(kMagicSigned)), sv = add(b, both(kMagic));
+        f32x2_unpack(sm.r, cm[2 * i], cm[2 * i + 1]);
+        f32x2_unpack(sv.r, cv[2 * i], cv[2 * i + 1]);
+    }
+    uint32_t mc[2] = {low_bytes(cm[0], cm[1], cm[2], cm[3]), low_bytes(cm[4], cm[5], cm[6], cm[7])};
+    uint32_t vc[2] = {low_bytes(cv[0], cv[1], cv[2], cv[3]), low_bytes(cv[4], cv[5], cv[6], cv[7])};
+    if (bad || has_byte(vc[0], 0) || has_byte(vc[1], 0)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float2 fm = split(m[e >> 1]), fv = split(v[e >> 1]);
+            const float x = e & 1 ? fv.y : fv.x;
+            const uint32_t byte = 255u << (8 * (e & 3));
+            if (x > 0.0f && (vc[e >> 2] & byte) == 0) vc[e >> 2] |= 0x01010101u & byte;
+            if (!(fabsf(e & 1 ? fm.y : fm.x) <= 3.4028235e38f)) mc[e >> 2] = (mc[e >> 2] & ~byte) | (0x80808080u & byte);
+            if (!(x <= 3.4028235e38f)) vc[e >> 2] |= byte;
+        }
+    }
+    store_codes(at.m, VEC, cnt, mc);
+    store_codes(at.v, VEC, cnt, vc);
+    ms = __fmul_rn(m_top, kMPart);
+    vs = __fmul_rn(v_top, kVPart);
 }
 
 template <int N, typename PT, typename GT, bool EIGHT>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, step_per_sm(EIGHT))
 step_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ Coef host, const __grid_constant__ Hyper h)
 {
     __shared__ Coef shared;
+    extern __shared__ __align__(16) char rings[];
     pdl_launch_dependents();
     pdl_wait();
     if (threadIdx.x == 0) {
@@ -386,18 +474,76 @@ step_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ Coef h
     const Coef c = shared;
     if (!(fabsf(c.gs) <= 3.4028235e38f)) return;                      // gradients without a finite norm: no step
     for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
-        const Desc &d = tab.t[find(tab, chunk)];
-        const int64_t base = (chunk - d.chunk0) * kChunk + (threadIdx.x >> 5) * kBlock;
+        const Desc &d = find(tab, chunk);
+        int64_t base = ((chunk - d.chunk0) * kWarps + (threadIdx.x >> 5)) * tab.per * kBlock;
         if (base >= d.n) continue;
         const float decay = (float)(1.0 - c.lr * (double)d.wd);
-        const uint32_t key = mix(c.key + (uint32_t)d.ordinal);
-        Loaded<PT, GT, EIGHT> l;
-        if (d.vec && d.n - base >= kBlock) {
-            load_block<PT, GT, true, EIGHT>(d, base, l);
-            step_block<PT, GT, true, EIGHT>(d, base, c, decay, key, l);
-        } else {
-            load_block<PT, GT, false, EIGHT>(d, base, l);
-            step_block<PT, GT, false, EIGHT>(d, base, c, decay, key, l);
+        // whole blocks of an aligned tensor that the warp has here, then the others
+        const int64_t there = d.vec ? (d.n - base) / kBlock : 0;
+        int left = tab.per, fast = (int)(there < left ? there : left);
+        uint32_t key = 0;
+        if (EIGHT) key = mix(c.key + (uint32_t)d.ordinal) ^ mix((uint32_t)(base >> 32));           // a chunk never crosses a multiple of 2^32
+        if (fast > 0) {
+            Cursor<PT, GT, true, EIGHT> at(d, base);
+            if constexpr (EIGHT) {
+                typedef Ring<PT, GT> R;
+                char *ring = rings + (threadIdx.x >> 5) * (kStages * R::kBytes);
+                const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+                auto fetch = [&](int i, int ahead, int slot) {        // one group of copies for each block, empty behind the last one
+                    if (i < fast) R::fetch(ring_at + slot * R::kBytes, at, ahead);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                };
+                __syncwarp();                                         // the ring's last blocks have been taken
+#pragma unroll
+                for (int i = 0; i < kStages - 1; ++i) fetch(i, i, i);
+                // block i's scales are lane i's
+                const int lane = threadIdx.x & 31;
+                float ms = 0.0f, vs = 0.0f;
+                if (lane < fast) { ms = at.ms[lane]; vs = at.vs[lane]; }
+                int slot = 0;
+#pragma unroll 1
+                for (int i = 0; i < fast; ++i) {
+                    asm volatile("cp.async.wait_group %0;" :: "n"(kStages - 2) : "memory");
+                    __syncwarp();
+                    Loaded<PT, GT, EIGHT> l;
+                    R::take(ring + slot * R::kBytes, l);
+                    l.ms = __shfl_sync(0xffffffffu, ms, i); l.vs = __shfl_sync(0xffffffffu, vs, i);
+                    // into the slot that every lane took before the barrier above
+                    fetch(i + kStages - 1, kStages - 1, slot == 0 ? kStages - 1 : slot - 1);
+                    slot = slot + 1 == kStages ? 0 : slot + 1;
+                    uint32_t k = key ^ ((uint32_t)base + lane * 8);
+                    float m_new, v_new;
+                    step_block(at, 256, c, decay, k ^ (k >> 16), l, m_new, v_new);
+                    if (lane == i) { ms = m_new; vs = v_new; }
+                    base += kBlock;
+                    at.on();
+                }
+                if (lane < fast) { at.ms[lane] = ms; at.vs[lane] = vs; }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < fast; ++i, at.on(), base += kBlock) {
+                    Loaded<PT, GT, EIGHT> l;
+                    at.load(l, 256);
+                    step_block(at, 256, c, decay, l);
+                }
+            }
+            left -= fast;
+        }
+#pragma unroll 1
+        for (; left > 0 && base < d.n; --left, base += kBlock) {
+            const Cursor<PT, GT, false, EIGHT> at(d, base);
+            const int64_t rest = d.n - base - (threadIdx.x & 31);
+            const int cnt = (int)(rest < 256 ? rest : 256);           // elements at 32 e < cnt exist
+            Loaded<PT, GT, EIGHT> l;
+            at.load(l, cnt);
+            if constexpr (EIGHT) {
+                uint32_t k = key ^ ((uint32_t)base + (threadIdx.x & 31));
+                float ms, vs;
+                step_block(at, cnt, c, decay, k ^ (k >> 16), l, ms, vs);
+                if ((threadIdx.x & 31) == 0) { *at.ms = ms; *at.vs = vs; }
+            } else {
+                step_block(at, cnt, c, decay, l);
+            }
         }
     }
 }
@@ -410,11 +556,7 @@ struct UnpackDesc {
     int64_t n, chunk0;
     int32_t vec;
 };
-template <int N> struct UnpackTable {
-    UnpackDesc t[N];
-    int32_t count;
-    int64_t chunks;
-};
+template <int N> using UnpackTable = TableOf<UnpackDesc, N>;
 
 template <int N>
 __global__ void __launch_bounds__(kThreads)
@@ -424,30 +566,26 @@ unpack_kernel(const __grid_constant__ UnpackTable<N> tab)
     pdl_wait();
     const int lane = threadIdx.x & 31;
     for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
-        int lo = 0, hi = tab.count - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (tab.t[mid].chunk0 <= chunk) lo = mid; else hi = mid - 1;
-        }
-        const UnpackDesc &d = tab.t[lo];
-        const int64_t base = (chunk - d.chunk0) * kChunk + (threadIdx.x >> 5) * kBlock;
-        if (base >= d.n) continue;
-        const int64_t left = d.n - base;
-        const bool vec = d.vec && left >= kBlock;
-        const int64_t at = base + (vec ? lane * 8 : lane);
-        const int cnt = vec ? 256 : (int)(left - lane < 256 ? left - lane : 256);
-        uint32_t mc[2], vc[2];
-        load_codes(d.m + at, vec, cnt, mc);
-        load_codes(d.v + at, vec, cnt, vc);
-        const float ms = d.ms[base / kBlock], vs = d.vs[base / kBlock];
-        float m[8], v[8];
+        const UnpackDesc &d = find(tab, chunk);
+        int64_t base = ((chunk - d.chunk0) * tab.per * kWarps + (threadIdx.x >> 5)) * kBlock;
+        for (int i = 0; i < tab.per && base < d.n; ++i, base += kWarps * kBlock) {
+            const int64_t left = d.n - base;
+            const bool vec = d.vec && left >= kBlock;
+            const int64_t at = base + (vec ? lane * 8 : lane);
+            const int cnt = vec ? 256 : (int)(left - lane < 256 ? left - lane : 256);
+            uint32_t mc[2], vc[2];
+            load_codes(d.m + at, vec, cnt, mc);
+            load_codes(d.v + at, vec, cnt, vc);
+            const float ms = d.ms[base / kBlock], vs = d.vs[base / kBlock];
+            float m[8], v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            m[e] = m_value((int32_t)(int8_t)(mc[e >> 2] >> (8 * (e & 3))), ms);
-            v[e] = v_value((vc[e >> 2] >> (8 * (e & 3))) & 255u, vs);
+            for (int e = 0; e < 8; ++e) {
+                m[e] = m_value((int32_t)(int8_t)(mc[e >> 2] >> (8 * (e & 3))), ms);
+                v[e] = v_value((vc[e >> 2] >> (8 * (e & 3))) & 255u, vs);
+            }
+            if (d.m_out) store_some(d.m_out + at, vec, cnt, m);
+            if (d.v_out) store_some(d.v_out + at, vec, cnt, v);
         }
-        if (d.m_out) store_some(d.m_out + at, vec, cnt, m);
-        if (d.v_out) store_some(d.v_out + at, vec, cnt, v);
     }
 }
 
@@ -457,42 +595,100 @@ struct NormDesc {
     int64_t n, chunk0;
     int32_t bf16, vec;
 };
-template <int N> struct NormTable {
-    NormDesc t[N];
-    int32_t count;
-    int64_t chunks;
-};
+template <int N> using NormTable = TableOf<NormDesc, N>;
 
-// Squares are added in 64 bits from the first one on: nothing overflows, and the order of the sums is fixed by the sizes.
+// Squares are added in 64 bits from the first one on: the factor that the norm gives enters every element of a step, and sums of 32 bits
+// would be off in its last bits.  |g| is made a 64-bit number by shifts of its bits (201 M bf16 gradients: 62 us; with the conversion
+// instruction 144, with pairs of fp32 sums 100).  Zero and subnormal numbers become 2^-127 to 2^-126 that way: the last kernel takes a
+// sum below 2^-200 for 0.  Infinities and NaN become 2^128 and more: a thread whose sum is 2^256 goes over its elements again with the
+// conversion.
+__device__ __forceinline__ void add_squares(const Raw8<float> &r, double (&sums)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t a = r.w[e] & 0x7fffffffu;
+        const double x = __hiloint2double((int)((a >> 3) + (896u << 20)), (int)(a << 29));
+        sums[e] = fma(x, x, sums[e]);
+    }
+}
+__device__ __forceinline__ void add_squares(const Raw8<__nv_bfloat16> &r, double (&sums)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const double lo = __hiloint2double((int)((r.w[e] & 0x7fffu) * 8192u + (896u << 20)), 0);
+        const double hi = __hiloint2double((int)(((r.w[e] & 0x7fff0000u) >> 3) + (896u << 20)), 0);
+        sums[2 * e] = fma(lo, lo, sums[2 * e]);
+        sums[2 * e + 1] = fma(hi, hi, sums[2 * e + 1]);
+    }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads)
 norm_kernel(const __grid_constant__ NormTable<N> tab, double *__restrict__ partial)
 {
-    __shared__ double warp_sum[kThreads / 32];
+    __shared__ double warp_sum[kWarps];
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    double sums[8] = {};                                              // a chain of additions each
-    for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
-        int lo = 0, hi = tab.count - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (tab.t[mid].chunk0 <= chunk) lo = mid; else hi = mid - 1;
-        }
-        const NormDesc &d = tab.t[lo];
-        const int64_t base = (chunk - d.chunk0) * kChunk + (threadIdx.x >> 5) * kBlock;
-        if (base >= d.n) continue;
-        const int64_t left = d.n - base;
-        const bool vec = d.vec && left >= kBlock;
-        const int64_t at = base + (vec ? lane * 8 : lane);
-        const int cnt = vec ? 256 : (int)(left - lane < 256 ? left - lane : 256);
-        float g[8];
-        if (d.bf16) load_some(static_cast<const __nv_bfloat16 *>(d.g) + at, vec, cnt, g);
-        else load_some(static_cast<const float *>(d.g) + at, vec, cnt, g);
+    constexpr int kStride = kWarps * kBlock;
+    // f(what a lane has of a block, as loaded)
+    auto go_over = [&](auto f) {
+        auto tensor = [&](const auto *g, const NormDesc &d, int64_t base) {
+            typedef typename std::remove_cv<typename std::remove_reference<decltype(*g)>::type>::type GT;
+            constexpr int kGroup = 8 / (int)sizeof(GT);
+            int left = tab.per;
+            // whole blocks of an aligned tensor in groups, one group loaded while the one before it is added up
+            const int64_t there = d.vec && d.n - base >= kBlock ? (d.n - base - kBlock) / kStride + 1 : 0;
+            const int count = (int)(there < left ? there : left) / kGroup;
+            if (count > 0) {
+                Raw8<GT> r[kGroup], ahead[kGroup];
+                const GT *at = g + base + lane * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[e] = fma((double)g[e], (double)g[e], sums[e]);
-    }
+                for (int i = 0; i < kGroup; ++i) r[i] = load8(at + i * kStride);
+#pragma unroll 1
+                for (int k = 1;; ++k) {
+                    at += kGroup * kStride;
+                    if (k < count) {
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) ahead[i] = load8(at + i * kStride);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i) f(r[i]);
+                    if (k >= count) break;
+#pragma unroll
+                    for (int i = 0; i < kGroup; ++i) r[i] = ahead[i];
+                }
+                left -= count * kGroup;
+                base += (int64_t)count * kGroup * kStride;
+            }
+#pragma unroll 1
+            for (; left > 0 && base < d.n; --left, base += kStride) {
+                const int64_t rest = d.n - base;
+                Raw8<GT> r;
+                if (d.vec && rest >= kBlock) load_raw<true>(g + base + lane * 8, 256, r);
+                else load_raw<false>(g + base + lane, (int)(rest - lane < 256 ? rest - lane : 256), r);
+                f(r);
+            }
+        };
+        for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
+            const NormDesc &d = find(tab, chunk);
+            const int64_t base = ((chunk - d.chunk0) * tab.per * kWarps + (threadIdx.x >> 5)) * kBlock;
+            if (d.bf16) tensor(static_cast<const __nv_bfloat16 *>(d.g), d, base);
+            else tensor(static_cast<const float *>(d.g), d, base);
+        }
+    };
+    double sums[8] = {};
+    go_over([&](const auto &r) { add_squares(r, sums); });
     double sum = ((sums[0] + sums[1]) + (sums[2] + sums[3])) + ((sums[4] + sums[5]) + (sums[6] + sums[7]));
+    if (sum >= 0x1p256) {
+        sum = 0.0;
+        go_over([&](const auto &r) {
+            float g[8];
+            unpack8(r, g);
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) sum = fma((double)g[e], (double)g[e], sum);
+        });
+    }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
     if (lane == 0) warp_sum[threadIdx.x >> 5] = sum;
@@ -500,7 +696,7 @@ norm_kernel(const __grid_constant__ NormTable<N> tab, double *__restrict__ parti
     if (threadIdx.x == 0) {
         double t = 0.0;
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) t += warp_sum[w];
+        for (int w = 0; w < kWarps; ++w) t += warp_sum[w];
         partial[blockIdx.x] = t;
     }
 }
@@ -520,7 +716,7 @@ norm_final_kernel(const double *__restrict__ partial, int32_t count, double max_
         __syncthreads();
     }
     if (threadIdx.x == 0) {
-        const double len = sqrt(red[0]);
+        const double len = red[0] < 0x1p-200 ? 0.0 : sqrt(red[0]);
         if (norm) *norm = (float)len;
         const bool finite = len <= 1.7976931348623157e308;
         if (scale) *scale = !finite ? __int_as_float(0x7fffffff) : len > max_norm ? (float)(max_norm / len) : 1.0f;
@@ -542,7 +738,6 @@ int sm_count()
 }
 
 bool at8(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % (size_t)(8 * bytes)) == 0; }
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
 unsigned grid_of(int64_t chunks, int per_sm)
 {
     const int64_t most = (int64_t)sm_count() * per_sm;
@@ -550,28 +745,37 @@ unsigned grid_of(int64_t chunks, int per_sm)
 }
 
 // Runs `put` and `go` over the tensors that `want` picks, as many to a launch as a table holds.
-template <template <int> class Tab, typename Put, typename Go, typename Want>
-int in_tables(const tbn_adamw_tensor *tensors, int32_t count, Want want, Put put, Go go)
+template <typename D, typename Put, typename Go, typename Want>
+int in_tables(const tbn_adamw_tensor *tensors, int32_t count, int per_sm, int least_per, int most_per, Want want, Put put, Go go)
 {
     int32_t picked = 0;
     for (int32_t i = 0; i < count; ++i) picked += tensors[i].n > 0 && want(tensors[i]);
     int32_t i = 0;
     while (picked > 0) {
         auto fill = [&](auto &tab, int most) {
-            tab.count = 0; tab.chunks = 0;
-            for (; i < count && tab.count < most; ++i) {
+            int64_t blocks = 0;
+            for (tab.count = 0; i < count && tab.count < most; ++i) {
                 if (tensors[i].n <= 0 || !want(tensors[i])) continue;
                 auto &d = tab.t[tab.count++];
                 put(d, tensors[i], i);
                 d.n = tensors[i].n;
-                d.chunk0 = tab.chunks;
-                tab.chunks += chunks_of(tensors[i].n);
+                blocks += (d.n + kBlock - 1) / kBlock;
             }
             picked -= tab.count;
+            // as many blocks to a warp as leave the thread blocks eight chunks each
+            const int64_t round = (int64_t)sm_count() * per_sm * kWarps;
+            tab.per = least_per;
+            while (tab.per < most_per && blocks >= 16 * round * tab.per) tab.per *= 2;
+            const int64_t chunk = (int64_t)tab.per * kWarps * kBlock;
+            tab.chunks = 0;
+            for (int32_t k = 0; k < tab.count; ++k) {
+                tab.t[k].chunk0 = tab.chunks;
+                tab.chunks += (tab.t[k].n + chunk - 1) / chunk;
+            }
         };
         int rc;
-        if (picked <= kFew) { Tab<kFew> tab; fill(tab, kFew); rc = go(tab); }
-        else { Tab<kMany> tab; fill(tab, kMany); rc = go(tab); }
+        if (picked <= kFew) { TableOf<D, kFew> tab; fill(tab, kFew); rc = go(tab, std::integral_constant<int, kFew>{}); }
+        else { TableOf<D, kMany> tab; fill(tab, kMany); rc = go(tab, std::integral_constant<int, kMany>{}); }
         if (rc != TBN_OK) return rc;
     }
     return TBN_OK;
@@ -581,8 +785,8 @@ template <typename PT, typename GT, bool EIGHT>
 int step_kind(const tbn_adamw_tensor *tensors, int32_t count, const Hyper &h, const Coef &host, cudaStream_t s)
 {
     const int pd = sizeof(PT) == 2 ? TBN_BF16 : TBN_F32, gd = sizeof(GT) == 2 ? TBN_BF16 : TBN_F32;
-    return in_tables<Table>(
-        tensors, count,
+    return in_tables<Desc>(
+        tensors, count, step_per_sm(EIGHT), 1, EIGHT ? 8 : 4,
         [&](const tbn_adamw_tensor &t) { return t.param_dtype == pd && t.grad_dtype == gd && (t.state_bits == 8) == EIGHT; },
         [&](Desc &d, const tbn_adamw_tensor &t, int32_t i) {
             d.p = t.param; d.g = t.grad; d.m = t.m; d.v = t.v; d.ms = t.m_scale; d.vs = t.v_scale; d.copy = t.copy;
@@ -590,11 +794,12 @@ int step_kind(const tbn_adamw_tensor *tensors, int32_t count, const Hyper &h, co
             const int sb = EIGHT ? 1 : 4;
             d.vec = at8(t.param, sizeof(PT)) && at8(t.grad, sizeof(GT)) && at8(t.m, sb) && at8(t.v, sb) && (!t.copy || at8(t.copy, 2));
         },
-        [&](const auto &tab) {
-            auto go = [&](auto kernel) {
-                return launch_pdl(kernel, dim3(grid_of(tab.chunks, 4)), dim3(kThreads), 0, s, tab, host, h) == cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
-            };
-            return go(step_kernel<sizeof(tab.t) / sizeof(Desc), PT, GT, EIGHT>);
+        [&](const auto &tab, auto size) {
+            auto kernel = step_kernel<decltype(size)::value, PT, GT, EIGHT>;
+            const int smem = EIGHT ? kWarps * kStages * Ring<PT, GT>::kBytes : 0;
+            if (smem > 32 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return (int)TBN_ERR_CUDA;
+            return launch_pdl(kernel, dim3(grid_of(tab.chunks, step_per_sm(EIGHT))), dim3(kThreads), smem, s, tab, host, h) == cudaSuccess
+                       ? (int)TBN_OK : (int)TBN_ERR_CUDA;
         });
 }
 
@@ -621,21 +826,19 @@ int launch_step(const tbn_adamw_tensor *tensors, int32_t count, const Hyper &h, 
 
 int launch_unpack(const tbn_adamw_tensor *tensors, int32_t count, float *const *m, float *const *v, cudaStream_t s)
 {
-    return in_tables<UnpackTable>(
-        tensors, count, [](const tbn_adamw_tensor &) { return true; },
+    return in_tables<UnpackDesc>(
+        tensors, count, kUnpackPerSm, 1, 4, [](const tbn_adamw_tensor &) { return true; },
         [&](UnpackDesc &d, const tbn_adamw_tensor &t, int32_t i) {
             d.m = static_cast<const uint8_t *>(t.m); d.v = static_cast<const uint8_t *>(t.v);
             d.ms = t.m_scale; d.vs = t.v_scale;
             d.m_out = m ? m[i] : nullptr; d.v_out = v ? v[i] : nullptr;
             d.vec = at8(t.m, 1) && at8(t.v, 1) && at8(d.m_out, 4) && at8(d.v_out, 4);
         },
-        [&](const auto &tab) {
-            return launch_pdl(unpack_kernel<sizeof(tab.t) / sizeof(UnpackDesc)>, dim3(grid_of(tab.chunks, 8)), dim3(kThreads), 0, s, tab) ==
+        [&](const auto &tab, auto size) {
+            return launch_pdl(unpack_kernel<decltype(size)::value>, dim3(grid_of(tab.chunks, kUnpackPerSm)), dim3(kThreads), 0, s, tab) ==
                            cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
         });
 }
-
-constexpr int kNormPerSm = 8;
 
 size_t norm_workspace_bytes(int32_t count)
 {
@@ -646,16 +849,16 @@ int launch_norm(const tbn_adamw_tensor *tensors, int32_t count, double max_norm,
 {
     double *partial = static_cast<double *>(workspace);
     int32_t used = 0;
-    int rc = in_tables<NormTable>(
-        tensors, count, [](const tbn_adamw_tensor &) { return true; },
+    int rc = in_tables<NormDesc>(
+        tensors, count, kNormPerSm, 4, 16, [](const tbn_adamw_tensor &) { return true; },
         [&](NormDesc &d, const tbn_adamw_tensor &t, int32_t) {
             d.g = t.grad; d.bf16 = t.grad_dtype == TBN_BF16; d.vec = at8(t.grad, d.bf16 ? 2 : 4);
         },
-        [&](const auto &tab) {
+        [&](const auto &tab, auto size) {
             const unsigned grid = grid_of(tab.chunks, kNormPerSm);
             double *out = partial + used;
             used += (int32_t)grid;
-            return launch_pdl(norm_kernel<sizeof(tab.t) / sizeof(NormDesc)>, dim3(grid), dim3(kThreads), 0, s, tab, out) == cudaSuccess
+            return launch_pdl(norm_kernel<decltype(size)::value>, dim3(grid), dim3(kThreads), 0, s, tab, out) == cudaSuccess
                        ? TBN_OK : TBN_ERR_CUDA;
         });
     if (rc != TBN_OK) return rc;
