@@ -4,9 +4,15 @@
 //   s = x + residual,  h = (s - mean) rstd,  y = h gamma + beta
 //   a = dy gamma,  ds = rstd (a - mean(a) - h mean(a h)) (+ dsum),  dgamma = sum_t dy h,  dbeta = sum_t dy
 //
-// Both are bound by HBM: each row is read once and held in registers, and the columns' sums stay in registers over all rows of
-// a thread block.
+// Both are bound by HBM: each row is read once, through a ring in shared memory that asynchronous copies fill (so that the next
+// rows are on their way while one is worked on), and held in registers; the columns' sums stay in registers over all rows of a thread
+// block.  A row is shared by 1 to 8 warps, a lane has 1 to 4 pieces of eight columns.
+//
+// Rows that do not begin on 16 bytes are read and written as the aligned pieces that cover them, what is not the row's being masked.
+// Where a piece begins in a row then depends on the row, (t d) mod 8, so a thread block keeps to rows of one remainder, and a lane
+// to its columns.
 #include <atomic>
+#include <type_traits>
 
 #include "norm_train.cuh"
 #include "vec8.cuh"
@@ -32,124 +38,227 @@ __device__ __forceinline__ void group_sync(int group, int threads)
     else asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(threads) : "memory");
 }
 
-// Columns of a thread in a row group of `threads`: pieces of eight in a row (VEC) or single columns, NP * 8 in all.
-template <bool VEC> __device__ __forceinline__ int32_t column(int i, int e, int tid, int threads)
-{
-    return VEC ? (i * threads + tid) * 8 + e : (i * 8 + e) * threads + tid;
-}
-template <bool VEC, typename T> __device__ __forceinline__ void load_piece(const T *row, int i, int tid, int threads, int32_t d, float (&v)[8])
-{
-    if (VEC) {
-        const int32_t c = column<true>(i, 0, tid, threads);
-        if (c < d) unpack8(load8(row + c), v);
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int32_t c = column<false>(i, e, tid, threads);
-            v[e] = c < d ? value_of(row[c]) : 0.0f;
-        }
-    }
-}
-template <bool VEC, typename T> __device__ __forceinline__ void store_piece(T *row, int i, int tid, int threads, int32_t d, const float (&v)[8])
-{
-    if (VEC) {
-        const int32_t c = column<true>(i, 0, tid, threads);
-        if (c < d) store8(row + c, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int32_t c = column<false>(i, e, tid, threads);
-            if (c < d) store_from_float(row, c, v[e]);
-        }
-    }
-}
-
 template <typename XT> __device__ __forceinline__ float rounded(float v);
 template <> __device__ __forceinline__ float rounded<float>(float v) { return v; }
 template <> __device__ __forceinline__ float rounded<__nv_bfloat16>(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 
-// One row to a group of `warps` warps.  The mean and the centred second moment are taken per warp and joined over the warps
-// (two sets of n1 and n2 values: M2 = M2a + M2b + (mean_b - mean_a)^2 n1 n2 / (n1 + n2)), so that a group meets once a row.
-template <typename XT, typename YT, int NP, bool VEC>
-__global__ void __launch_bounds__(kThreads)
-forward_kernel(const XT *__restrict__ x, const XT *__restrict__ residual, int64_t T, int32_t d, int warps, const float *__restrict__ gamma,
-               const float *__restrict__ beta, float eps, XT *__restrict__ sum, YT *__restrict__ y, float *__restrict__ mean_out,
-               float *__restrict__ rstd_out)
-{
-    __shared__ float3 part[kMaxWarps];
-    pdl_launch_dependents();
-    pdl_wait();
-    const int threads = warps * 32, group = threadIdx.x / threads, tid = threadIdx.x - group * threads;
-    const int64_t t = (int64_t)blockIdx.x * (blockDim.x / threads) + group;
-    if (t >= T) return;                                               // a whole group
-    float v[NP][8];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) load_piece<VEC>(x + t * d, i, tid, threads, d, v[i]);
-    if (residual) {
+// How a call's rows and columns are spread over thread blocks, warps and lanes.
+struct Shape {
+    int np, warps, groups;                  // pieces of eight columns to a lane, warps to a row, rows to a thread block
+    int classes;                            // remainders (t d) mod unit that occur: thread block b takes rows t = b mod classes
+    bool lng;
+};
+
+// What a lane has to do with the rows of its group.
+template <int NP> struct Lane {
+    int32_t d, shift;                       // shift: columns between the aligned piece that the row begins in and the row
+    int threads, group, tid;
+    int64_t row, row_step, rows;            // first row, from one to the next, how many
+    int64_t total;                          // elements of the whole tensor
+    uint32_t mask[NP];                      // which of a piece's eight columns are the row's
+    __device__ __forceinline__ Lane(int64_t T, int32_t d_, int warps, int groups, int classes) : d(d_)
+    {
+        threads = warps * 32;
+        group = threadIdx.x / threads;
+        tid = threadIdx.x - group * threads;
+        const int cls = blockIdx.x % classes;
+        const int64_t first = (int64_t)(blockIdx.x / classes) * groups + group, step = (int64_t)(gridDim.x / classes) * groups;
+        const int64_t here = (T - cls + classes - 1) / classes;      // rows of the class
+        rows = first < here ? (here - first - 1) / step + 1 : 0;
+        row = cls + first * classes;
+        row_step = step * classes;
+        total = T * d;
+        shift = (int32_t)(((int64_t)cls * d) & 7);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float r[8];
-            load_piece<VEC>(residual + t * d, i, tid, threads, d, r);
+            mask[i] = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = rounded<XT>(v[i][e] + r[e]);
-            if (sum) store_piece<VEC>(sum + t * d, i, tid, threads, d, v[i]);
-        }
-    }
-    float s = 0.0f;
-    int32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { s += v[i][e]; mine += column<VEC>(i, e, tid, threads) < d; }
-    float n = warps == 1 ? (float)d : (float)__reduce_add_sync(0xffffffffu, mine);
-    float mean = n > 0.0f ? warp_sum(s) / n : 0.0f;
-    float q = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (column<VEC>(i, e, tid, threads) < d) { const float c = v[i][e] - mean; q = fmaf(c, c, q); }
-    q = warp_sum(q);
-    if (warps > 1) {
-        const int first = group * warps;
-        if ((tid & 31) == 0) part[first + (tid >> 5)] = make_float3(n, mean, q);
-        group_sync(group, threads);
-        n = part[first].x; mean = part[first].y; q = part[first].z;
-        for (int w = 1; w < warps; ++w) {
-            const float3 b = part[first + w];
-            if (b.x > 0.0f) {
-                const float both = n + b.x, delta = b.y - mean, share = b.x / both;
-                mean = fmaf(delta, share, mean);
-                q += fmaf(delta * delta, n * share, b.z);
-                n = both;
+            for (int e = 0; e < 8; ++e) {
+                const int32_t c = at(i) + e - shift;
+                if (c >= 0 && c < d) mask[i] |= 1u << e;
             }
         }
     }
-    const float rstd = rsqrtf(q / (float)d + eps);
-    if (tid == 0) {
-        if (mean_out) mean_out[t] = mean;
-        if (rstd_out) rstd_out[t] = rstd;
-    }
+    __device__ __forceinline__ int32_t at(int i) const { return (i * threads + tid) * 8; }         // a piece's first column, from the aligned start on
+    __device__ __forceinline__ int64_t start(int64_t t) const { return t * d - shift; }            // the aligned start of row t
+};
+
+// Ring of a warp in shared memory.  A lane copies and takes its own pieces, so that nothing but its own copies is waited for.
+template <typename T, int NP>
+__device__ __forceinline__ void fetch(uint32_t to, const T *x, int64_t start, const Lane<NP> &l)
+{
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        float o[8], w[8];
+        if (l.mask[i] == 0) continue;
+        const int64_t at = start + l.at(i);
+        const int64_t left = (l.total - at) * (int64_t)sizeof(T);     // bytes of the tensor from here on: the last piece may be a part
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = (v[i][e] - mean) * rstd;
-        if (gamma) {
-            load_piece<VEC>(gamma, i, tid, threads, d, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] *= w[e];
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            const int size = left - h * 16 >= 16 ? 16 : left - h * 16 > 0 ? (int)(left - h * 16) : 0;
+            const T *from = size > 0 ? x + at + h * (16 / (int)sizeof(T)) : x;
+            const uint32_t slot = to + (i * ((int)sizeof(T) / 2) + h) * 512 + lane * 16;
+            if (sizeof(T) == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(slot), "l"(from), "r"(size) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" :: "r"(slot), "l"(from), "r"(size) : "memory");
         }
-        if (beta) {
-            load_piece<VEC>(beta, i, tid, threads, d, w);
+    }
+}
+template <typename T, int NP> __device__ __forceinline__ void take(const char *from, int i, const Lane<NP> &l, float (&v)[8])
+{
+    Raw8<T> r;
+    const uint4 *q = reinterpret_cast<const uint4 *>(from + i * (int)sizeof(T) / 2 * 512) + (threadIdx.x & 31);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] += w[e];
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const uint4 x = q[h * 32];
+        r.w[4 * h] = x.x; r.w[4 * h + 1] = x.y; r.w[4 * h + 2] = x.z; r.w[4 * h + 3] = x.w;
+    }
+    unpack8(r, v);
+    if (l.mask[i] != 0xffu) {                                         // a row's ends, and lanes behind it
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (!(l.mask[i] >> e & 1u)) v[e] = 0.0f;
+    }
+}
+__device__ __forceinline__ void store16(float *p, const float (&v)[8])
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store16(__nv_bfloat16 *p, const float (&v)[8]) { store8(p, v); }
+template <typename T, int NP> __device__ __forceinline__ void put(T *x, int64_t start, int i, const Lane<NP> &l, const float (&v)[8])
+{
+    T *p = x + start + l.at(i);
+    if (l.mask[i] == 0xffu) { store16(p, v); return; }
+    if (l.mask[i] == 0) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (l.mask[i] >> e & 1u) store_from_float(p, e, v[e]);
+}
+// A vector of d floats (or ones) in shared memory, from the aligned start on, as the thread block's rows lie.
+__device__ __forceinline__ void stage_vector(float *to, const float *from, float otherwise, int32_t d, int32_t shift, int32_t room)
+{
+    for (int32_t c = threadIdx.x; c < room; c += blockDim.x) to[c] = from && c >= shift && c - shift < d ? from[c - shift] : otherwise;
+}
+__device__ __forceinline__ void read8(const float *from, float (&v)[8])
+{
+    const float4 a = reinterpret_cast<const float4 *>(from)[0], b = reinterpret_cast<const float4 *>(from)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
+// Rows in the ring: two thread blocks of eight warps to an SM, half its shared memory each, less what gains and offsets take there.
+constexpr int stages_for(int row_bytes)     // of one warp
+{
+    const int s = 92 * 1024 / (kMaxWarps * row_bytes);
+    return s < 2 ? 2 : s > 4 ? 4 : s;
+}
+template <typename XT, typename YT, int NP> struct ForwardRing {
+    static constexpr int kX = NP * 256 * (int)sizeof(XT), kBytes = 2 * kX, kStages = stages_for(kBytes);
+};
+template <typename XT, typename YT, int NP> struct BackwardRing {
+    static constexpr int kX = NP * 256 * (int)sizeof(XT), kY = NP * 256 * (int)sizeof(YT), kBytes = 2 * kX + kY, kStages = stages_for(kBytes);
+};
+
+// The mean and the centred second moment are taken per warp and joined over the warps of a row (of two sets of n1 and n2 values:
+// M2 = M2a + M2b + (mean_b - mean_a)^2 n1 n2 / (n1 + n2)), so that a group meets once a row.
+template <typename XT, typename YT, int NP>
+__global__ void __launch_bounds__(kThreads, 2)
+forward_kernel(const ForwardArgs a, const Shape sh)
+{
+    typedef ForwardRing<XT, YT, NP> R;
+    __shared__ float3 part[2][kMaxWarps];
+    extern __shared__ __align__(16) char smem[];
+    pdl_launch_dependents();
+    pdl_wait();
+    const Lane<NP> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
+    const int32_t room = sh.warps * NP * 256;
+    float *gamma = reinterpret_cast<float *>(smem), *beta = gamma + room;
+    char *ring = smem + 2 * room * 4 + (threadIdx.x >> 5) * (R::kStages * R::kBytes);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const XT *x = static_cast<const XT *>(a.x), *residual = static_cast<const XT *>(a.residual);
+    XT *sum = static_cast<XT *>(a.sum);
+    YT *y = static_cast<YT *>(a.y);
+    auto get = [&](int64_t k) {
+        if (k < l.rows) {
+            const int64_t start = l.start(l.row + k * l.row_step);
+            const uint32_t to = ring_at + (uint32_t)(k % R::kStages) * R::kBytes;
+            fetch(to, x, start, l);
+            if (residual) fetch(to + R::kX, residual, start, l);
         }
-        store_piece<VEC>(y + t * d, i, tid, threads, d, o);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int k = 0; k < R::kStages - 1; ++k) get(k);
+    stage_vector(gamma, a.gamma, 1.0f, a.d, l.shift, room);
+    stage_vector(beta, a.beta, 0.0f, a.d, l.shift, room);
+    __syncthreads();
+    int32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) mine += __popc(l.mask[i]);
+    const float n_warp = (float)__reduce_add_sync(0xffffffffu, mine), share = n_warp > 0.0f ? 1.0f / n_warp : 0.0f, inv_d = 1.0f / (float)a.d;
+    int turn = 0;
+    for (int64_t k = 0; k < l.rows; ++k, turn ^= 1) {
+        const int64_t t = l.row + k * l.row_step, start = l.start(t);
+        asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
+        const char *from = ring + (int)(k % R::kStages) * R::kBytes;
+        float v[NP][8];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) take<XT>(from, i, l, v[i]);
+        if (residual) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                float r[8];
+                take<XT>(from + R::kX, i, l, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = rounded<XT>(v[i][e] + r[e]);
+                put(sum, start, i, l, v[i]);
+            }
+        }
+        get(k + R::kStages - 1);                                      // into the slot that was taken a row ago
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s += v[i][e];
+        float n = n_warp, mean = warp_sum(s) * share, q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            float c[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) c[e] = v[i][e] - mean;
+            if (l.mask[i] != 0xffu) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) if (!(l.mask[i] >> e & 1u)) c[e] = 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q = fmaf(c[e], c[e], q);
+        }
+        q = warp_sum(q);
+        if (sh.warps > 1) {
+            const float3 *all = part[turn] + l.group * sh.warps;
+            if ((l.tid & 31) == 0) part[turn][threadIdx.x >> 5] = make_float3(n, mean, q);
+            group_sync(l.group, l.threads);
+            n = all[0].x; mean = all[0].y; q = all[0].z;
+            for (int w = 1; w < sh.warps; ++w) {
+                const float3 b = all[w];
+                if (b.x > 0.0f) {
+                    const float both = n + b.x, delta = b.y - mean, part_b = b.x / both;
+                    mean = fmaf(delta, part_b, mean);
+                    q += fmaf(delta * delta, n * part_b, b.z);
+                    n = both;
+                }
+            }
+        }
+        const float rstd = rsqrtf(q * inv_d + a.eps);
+        if (l.tid == 0) {
+            if (a.mean) a.mean[t] = mean;
+            if (a.rstd) a.rstd[t] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            float o[8], w[8], b[8];
+            read8(gamma + l.at(i), w);
+            read8(beta + l.at(i), b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf((v[i][e] - mean) * rstd, w[e], b[e]);
+            put(y, start, i, l, o);
+        }
     }
 }
 
@@ -194,92 +303,110 @@ forward_long_kernel(const XT *__restrict__ x, const XT *__restrict__ residual, i
     }
 }
 
-// A thread block walks over rows with a stride; a thread keeps its columns' share of dgamma and dbeta in registers to the end.
-template <typename XT, typename YT, int NP, bool VEC>
-__global__ void __launch_bounds__(kThreads)
-backward_kernel(const YT *__restrict__ dy, const XT *__restrict__ x, int64_t T, int32_t d, int warps, const float *__restrict__ gamma,
-                const float *__restrict__ mean, const float *__restrict__ rstd, const XT *__restrict__ dsum, XT *__restrict__ dx,
-                float *__restrict__ partial)
+// A thread block walks over rows with a stride; a lane keeps its columns' share of dgamma and dbeta in registers to the end.
+template <typename XT, typename YT, int NP>
+__global__ void __launch_bounds__(kThreads, NP == 4 ? 1 : 2)
+backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partial)
 {
+    typedef BackwardRing<XT, YT, NP> R;
     __shared__ float2 part[2][kMaxWarps];
-    extern __shared__ float columns[];                                // with several groups: [groups][2][d]
+    extern __shared__ __align__(16) char smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const int threads = warps * 32, group = threadIdx.x / threads, tid = threadIdx.x - group * threads;
-    const int groups = blockDim.x / threads;
-    float dg[NP][8], db[NP][8], w[NP][8];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { dg[i][e] = db[i][e] = 0.0f; w[i][e] = 1.0f; }
-        if (gamma) load_piece<VEC>(gamma, i, tid, threads, d, w[i]);
-    }
-    const float inv_d = 1.0f / (float)d;
-    int turn = 0;
-    for (int64_t t = (int64_t)blockIdx.x * groups + group; t < T; t += (int64_t)gridDim.x * groups, turn ^= 1) {
-        float g[NP][8], h[NP][8];
-        const float mu = mean[t], rs = rstd[t];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            load_piece<VEC>(dy + t * d, i, tid, threads, d, g[i]);
-            load_piece<VEC>(x + t * d, i, tid, threads, d, h[i]);
+    const Lane<NP> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
+    const int32_t room = sh.warps * NP * 256;
+    float *gamma = reinterpret_cast<float *>(smem);
+    char *rings = smem + room * 4, *ring = rings + (threadIdx.x >> 5) * (R::kStages * R::kBytes);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const XT *x = static_cast<const XT *>(a.x), *dsum = static_cast<const XT *>(a.dsum);
+    const YT *dy = static_cast<const YT *>(a.dy);
+    XT *dx = static_cast<XT *>(a.dx);
+    auto get = [&](int64_t k) {
+        if (k < l.rows) {
+            const int64_t start = l.start(l.row + k * l.row_step);
+            const uint32_t to = ring_at + (uint32_t)(k % R::kStages) * R::kBytes;
+            fetch(to, x, start, l);
+            fetch(to + R::kX, dy, start, l);
+            if (dsum) fetch(to + R::kX + R::kY, dsum, start, l);
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int k = 0; k < R::kStages - 1; ++k) get(k);
+    stage_vector(gamma, a.gamma, 1.0f, a.d, l.shift, room);
+    __syncthreads();
+    float dg[NP][8], db[NP][8];
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dg[i][e] = db[i][e] = 0.0f;
+    const float inv_d = 1.0f / (float)a.d;
+    float mu_next = 0.0f, rs_next = 0.0f;
+    if (l.rows > 0) { mu_next = a.mean[l.row]; rs_next = a.rstd[l.row]; }
+    int turn = 0;
+    for (int64_t k = 0; k < l.rows; ++k, turn ^= 1) {
+        const int64_t t = l.row + k * l.row_step, start = l.start(t);
+        const float mu = mu_next, rs = rs_next;
+        if (k + 1 < l.rows) { mu_next = a.mean[t + l.row_step]; rs_next = a.rstd[t + l.row_step]; }
+        asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
+        const char *from = ring + (int)(k % R::kStages) * R::kBytes;
+        float g[NP][8], h[NP][8];
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
+        for (int i = 0; i < NP; ++i) {
+            float w[8];
+            take<XT>(from, i, l, h[i]);
+            take<YT>(from + R::kX, i, l, g[i]);
+            read8(gamma + l.at(i), w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                h[i][e] = (h[i][e] - mu) * rs;                        // beyond the row: times a g of zero
+                h[i][e] = (h[i][e] - mu) * rs;                        // of a masked column: times a g of zero
                 db[i][e] += g[i][e];
                 dg[i][e] = fmaf(g[i][e], h[i][e], dg[i][e]);
-                g[i][e] *= w[i][e];
+                g[i][e] *= w[e];
                 s1 += g[i][e];
                 s2 = fmaf(g[i][e], h[i][e], s2);
             }
+        }
         s1 = warp_sum(s1); s2 = warp_sum(s2);
-        if (warps > 1) {
-            const int first = group * warps;
-            if ((tid & 31) == 0) part[turn][first + (tid >> 5)] = make_float2(s1, s2);
-            group_sync(group, threads);
+        if (sh.warps > 1) {
+            const float2 *all = part[turn] + l.group * sh.warps;
+            if ((l.tid & 31) == 0) part[turn][threadIdx.x >> 5] = make_float2(s1, s2);
+            group_sync(l.group, l.threads);
             s1 = s2 = 0.0f;
-            for (int k = 0; k < warps; ++k) { s1 += part[turn][first + k].x; s2 += part[turn][first + k].y; }
+            for (int w = 0; w < sh.warps; ++w) { s1 += all[w].x; s2 += all[w].y; }
         }
         s1 *= inv_d; s2 *= inv_d;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float r[8];
-            if (dsum) load_piece<VEC>(dsum + t * d, i, tid, threads, d, r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float o = (g[i][e] - s1 - h[i][e] * s2) * rs;
-                g[i][e] = dsum ? o + r[e] : o;
+            for (int e = 0; e < 8; ++e) g[i][e] = (g[i][e] - s1 - h[i][e] * s2) * rs;
+            if (dsum) {
+                float r[8];
+                take<XT>(from + R::kX + R::kY, i, l, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[i][e] += r[e];
             }
-            store_piece<VEC>(dx + t * d, i, tid, threads, d, g[i]);
+            put(dx, start, i, l, g[i]);
         }
+        get(k + R::kStages - 1);                                      // into the slot that was taken a row ago
     }
     if (!partial) return;
-    float *out = partial + (int64_t)blockIdx.x * 2 * d;
-    if (groups == 1) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int32_t c = column<VEC>(i, e, tid, threads);
-                if (c < d) { out[c] = dg[i][e]; out[d + c] = db[i][e]; }
-            }
-        return;
-    }
+    // the groups' sums, in their order; the rings are done with
+    float *columns = reinterpret_cast<float *>(rings), *out = partial + (int64_t)blockIdx.x * 2 * a.d;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < NP; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int32_t c = column<VEC>(i, e, tid, threads);
-            if (c < d) { columns[group * 2 * d + c] = dg[i][e]; columns[group * 2 * d + d + c] = db[i][e]; }
+            columns[(l.group * 2) * room + l.at(i) + e] = dg[i][e];
+            columns[(l.group * 2 + 1) * room + l.at(i) + e] = db[i][e];
         }
     __syncthreads();
-    for (int32_t c = threadIdx.x; c < 2 * d; c += blockDim.x) {
-        float t = columns[c];
-        for (int k = 1; k < groups; ++k) t += columns[k * 2 * d + c];
+    for (int32_t c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
+        const int32_t which = c >= a.d, at = which * room + l.shift + c - which * a.d;
+        float t = columns[at];
+        for (int k = 1; k < sh.groups; ++k) t += columns[k * 2 * room + at];
         out[c] = t;
     }
 }
@@ -336,25 +463,27 @@ column_sums_kernel(const YT *__restrict__ dy, const XT *__restrict__ x, int64_t 
     }
 }
 
-// Adds the thread blocks' sums in a fixed order: 32 columns to a block, 8 rows of them at a time.
-__global__ void __launch_bounds__(kThreads)
+// Adds the thread blocks' sums in a fixed order: 32 columns to a block, 32 rows of them at a time.
+__global__ void __launch_bounds__(1024)
 finish_kernel(const float *__restrict__ partial, int32_t parts, int32_t d, float *__restrict__ dgamma, float *__restrict__ dbeta)
 {
-    __shared__ float red[kThreads / 32][32];
+    __shared__ float red[32][33];
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;                // of dgamma's d and dbeta's d
     float t = 0.0f;
-    if (c < 2 * (int64_t)d)
-        for (int32_t k = row; k < parts; k += kThreads / 32) t += partial[(int64_t)k * 2 * d + c];
-    red[row][lane] = t;
+    if (c < 2 * (int64_t)d) {
+#pragma unroll 4
+        for (int32_t k = row; k < parts; k += 32) t += partial[(int64_t)k * 2 * d + c];
+    }
+    red[lane][row] = t;
     __syncthreads();
-    if (row == 0 && c < 2 * (int64_t)d) {
-#pragma unroll
-        for (int k = 1; k < kThreads / 32; ++k) t += red[k][lane];
-        if (c < d) { if (dgamma) dgamma[c] = t; }
-        else if (dbeta) dbeta[c - d] = t;
+    t = warp_sum(red[row][lane]);                                     // warp `row` has column `row` now
+    const int64_t o = (int64_t)blockIdx.x * 32 + row;
+    if (lane == 0 && o < 2 * (int64_t)d) {
+        if (o < d) { if (dgamma) dgamma[o] = t; }
+        else if (dbeta) dbeta[o - d] = t;
     }
 }
 
@@ -371,85 +500,96 @@ int sm_count()
     return n;
 }
 
-struct Shape {
-    int np, warps, groups;                  // pieces of eight columns to a thread, warps to a row, rows to a thread block
-    bool vec, lng;
-};
-Shape shape_of(int32_t d, bool vec)
+// `most`: pieces to a lane at most, from which on more warps share a row.  The fewest warps of those that leave the fewest lanes without
+// columns; four pieces in any case where eight warps need them.
+Shape shape_of(int32_t d, int most)
 {
     Shape s;
-    s.vec = vec;
-    s.lng = d > kThreads * 8 * 4;
-    s.np = d <= kThreads * 8 ? 1 : d <= kThreads * 16 ? 2 : 4;
-    s.warps = (d + 256 * s.np - 1) / (256 * s.np);
+    s.classes = d % 8 == 0 ? 1 : d % 4 == 0 ? 2 : d % 2 == 0 ? 4 : 8;
+    const int32_t pieces = (d + (s.classes > 1 ? 7 : 0) + 7) / 8;     // that a row can touch
+    s.lng = pieces > kMaxWarps * 32 * 4;
+    s.np = 4; s.warps = kMaxWarps;
+    int32_t least = 0x7fffffff;
+    for (int np = 1; np <= 4; ++np) {
+        const int32_t warps = (pieces + 32 * np - 1) / (32 * np);
+        if (warps > kMaxWarps || (np > most && least != 0x7fffffff)) continue;
+        if (warps * np < least || (warps * np == least && warps < s.warps)) { least = warps * np; s.np = np; s.warps = (int)warps; }
+    }
     s.groups = kMaxWarps / s.warps;
     return s;
 }
-// Thread blocks of the backward pass: what fits on the GPU at a time, and no more than there are rows.
-int64_t backward_blocks(int64_t T, const Shape &s)
+constexpr int kMostForward = 4, kMostBackward = 3;
+// Thread blocks: two to an SM, and no more than there are rows; as many of each class.
+int64_t blocks_of(int64_t T, const Shape &s, int per_sm)
 {
-    const int64_t most = (int64_t)sm_count() * 2, need = (T + s.groups - 1) / s.groups;
-    return need < most ? need : most;
+    const int64_t most = (int64_t)sm_count() * per_sm / s.classes, need = ((T + s.classes - 1) / s.classes + s.groups - 1) / s.groups;
+    return (need < most ? need : most) * s.classes;
 }
+// Dynamic shared memory with which two thread blocks fit on an SM (228 KB, 1 KB of each block's is the system's).
+constexpr size_t kHalf = 113 * 1024;
 constexpr int kLongParts = 64;
 
-template <typename F> cudaError_t with_shape(const Shape &s, F f)
+template <typename F> cudaError_t with_pieces(int np, F f)
 {
-    if (s.vec) return s.np == 1 ? f(std::integral_constant<int, 1>{}, std::true_type{}) : s.np == 2 ? f(std::integral_constant<int, 2>{}, std::true_type{})
-                                                                                       : f(std::integral_constant<int, 4>{}, std::true_type{});
-    return s.np == 1 ? f(std::integral_constant<int, 1>{}, std::false_type{}) : s.np == 2 ? f(std::integral_constant<int, 2>{}, std::false_type{})
-                                                                                  : f(std::integral_constant<int, 4>{}, std::false_type{});
+    return np == 1 ? f(std::integral_constant<int, 1>{}) : np == 2 ? f(std::integral_constant<int, 2>{})
+         : np == 3 ? f(std::integral_constant<int, 3>{}) : f(std::integral_constant<int, 4>{});
+}
+template <typename K> cudaError_t allow(K kernel, size_t smem)
+{
+    return smem > 32 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
 }
 
 template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs &a, cudaStream_t s)
 {
-    const bool vec = aligned8<XT>(a.x, a.d) && aligned8<XT>(a.residual) && aligned8<XT>(a.sum) && aligned8<YT>(a.y) && aligned8<float>(a.gamma) &&
-                     aligned8<float>(a.beta);
-    const Shape sh = shape_of(a.d, vec);
-    const XT *x = static_cast<const XT *>(a.x), *r = static_cast<const XT *>(a.residual);
-    XT *sum = static_cast<XT *>(a.sum);
-    YT *y = static_cast<YT *>(a.y);
+    const Shape sh = shape_of(a.d, kMostForward);
     if (sh.lng) {
         const int64_t most = (int64_t)sm_count() * 8;
-        return launch_pdl(forward_long_kernel<XT, YT>, dim3((unsigned)(a.T < most ? a.T : most)), dim3(kThreads), 0, s, x, r, a.T, a.d, a.gamma,
-                          a.beta, a.eps, sum, y, a.mean, a.rstd);
+        return launch_pdl(forward_long_kernel<XT, YT>, dim3((unsigned)(a.T < most ? a.T : most)), dim3(kThreads), 0, s, static_cast<const XT *>(a.x),
+                          static_cast<const XT *>(a.residual), a.T, a.d, a.gamma, a.beta, a.eps, static_cast<XT *>(a.sum), static_cast<YT *>(a.y), a.mean,
+                          a.rstd);
     }
-    return with_shape(sh, [&](auto np, auto v) {
-        return launch_pdl(forward_kernel<XT, YT, decltype(np)::value, decltype(v)::value>, dim3((unsigned)((a.T + sh.groups - 1) / sh.groups)),
-                          dim3(sh.groups * sh.warps * 32), 0, s, x, r, a.T, a.d, sh.warps, a.gamma, a.beta, a.eps, sum, y, a.mean, a.rstd);
+    return with_pieces(sh.np, [&](auto np) {
+        constexpr int NP = decltype(np)::value;
+        typedef ForwardRing<XT, YT, NP> R;
+        const size_t smem = (size_t)2 * sh.warps * NP * 256 * 4 + (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
+        const cudaError_t e = allow(forward_kernel<XT, YT, NP>, smem);
+        if (e != cudaSuccess) return e;
+        return launch_pdl(forward_kernel<XT, YT, NP>, dim3((unsigned)blocks_of(a.T, sh, smem <= kHalf ? 2 : 1)), dim3(sh.groups * sh.warps * 32), smem, s, a, sh);
     });
 }
 
 template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArgs &a, float *partial, cudaStream_t s)
 {
-    const bool vec = aligned8<XT>(a.x, a.d) && aligned8<YT>(a.dy) && aligned8<XT>(a.dsum) && aligned8<XT>(a.dx) && aligned8<float>(a.gamma);
-    const Shape sh = shape_of(a.d, vec);
-    const YT *dy = static_cast<const YT *>(a.dy);
-    const XT *x = static_cast<const XT *>(a.x), *dsum = static_cast<const XT *>(a.dsum);
-    XT *dx = static_cast<XT *>(a.dx);
+    const Shape sh = shape_of(a.d, kMostBackward);
     const bool sums = a.dgamma || a.dbeta;
-    int32_t parts;
+    int32_t parts = 0;
     cudaError_t e;
     if (sh.lng) {
+        const YT *dy = static_cast<const YT *>(a.dy);
+        const XT *x = static_cast<const XT *>(a.x);
         const int64_t most = (int64_t)sm_count() * 8;
         e = launch_pdl(backward_long_kernel<XT, YT>, dim3((unsigned)(a.T < most ? a.T : most)), dim3(kThreads), 0, s, dy, x, a.T, a.d, a.gamma,
-                       a.mean, a.rstd, dsum, dx);
+                       a.mean, a.rstd, static_cast<const XT *>(a.dsum), static_cast<XT *>(a.dx));
         parts = (int32_t)(a.T < kLongParts ? a.T : kLongParts);
         const int32_t slabs = (a.d + kThreads - 1) / kThreads;
         if (e == cudaSuccess && sums)
             e = launch_pdl(column_sums_kernel<XT, YT>, dim3(slabs < 4096 ? slabs : 4096, parts), dim3(kThreads), 0, s, dy, x, a.T, a.d, a.mean,
                            a.rstd, partial);
     } else {
-        parts = (int32_t)backward_blocks(a.T, sh);
-        const size_t smem = sh.groups > 1 ? (size_t)sh.groups * 2 * a.d * 4 : 0;       // at most 8 x 2 x 256 floats' worth
-        e = with_shape(sh, [&](auto np, auto v) {
-            return launch_pdl(backward_kernel<XT, YT, decltype(np)::value, decltype(v)::value>, dim3((unsigned)parts),
-                              dim3(sh.groups * sh.warps * 32), smem, s, dy, x, a.T, a.d, sh.warps, a.gamma, a.mean, a.rstd, dsum, dx,
-                              sums ? partial : nullptr);
+        e = with_pieces(sh.np, [&](auto np) {
+            constexpr int NP = decltype(np)::value;
+            typedef BackwardRing<XT, YT, NP> R;
+            const size_t room = (size_t)sh.warps * NP * 256 * 4, rings = (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
+            const size_t sums_room = (size_t)sh.groups * 2 * room;    // the same space as the rings, which are larger
+            const size_t smem = room + (rings > sums_room ? rings : sums_room);
+            const cudaError_t e1 = allow(backward_kernel<XT, YT, NP>, smem);
+            if (e1 != cudaSuccess) return e1;
+            parts = (int32_t)blocks_of(a.T, sh, NP < 4 && smem <= kHalf ? 2 : 1);
+            return launch_pdl(backward_kernel<XT, YT, NP>, dim3((unsigned)parts), dim3(sh.groups * sh.warps * 32), smem, s, a, sh, sums ? partial : nullptr);
         });
     }
     if (e != cudaSuccess || !sums) return e;
-    return launch_pdl(finish_kernel, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), dim3(kThreads), 0, s, static_cast<const float *>(partial), parts,
+    return launch_pdl(finish_kernel, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), dim3(1024), 0, s, static_cast<const float *>(partial), parts,
                       a.d, a.dgamma, a.dbeta);
 }
 
@@ -457,8 +597,8 @@ template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArg
 
 size_t backward_workspace_bytes(int64_t T, int32_t d)
 {
-    const Shape sh = shape_of(d, true);
-    const int64_t parts = sh.lng ? (T < kLongParts ? T : kLongParts) : backward_blocks(T, sh);
+    const Shape sh = shape_of(d, kMostBackward);
+    const int64_t parts = sh.lng ? (T < kLongParts ? T : kLongParts) : blocks_of(T, sh, 2);        // at most
     return (size_t)parts * 2 * (size_t)d * 4;
 }
 
