@@ -102,22 +102,9 @@ constexpr float kMPart = (float)(1.0 / (127.0 * 127.0)), kVPart = (float)(1.0 / 
 constexpr float kMLeast = 0x1p-100f, kVLeast = 0x1p-94f;
 constexpr float kMagic = 8388608.0f, kMagicSigned = 12582912.0f;     // 2^23, 1.5 2^23: an integer added to one of them is in its low bits
 
-// Two fp32 values to an instruction: the arithmetic of 8-bit states is bound by the rate at which instructions issue.
-struct Pair { uint64_t r; };
-__device__ __forceinline__ Pair pair(float a, float b) { return {f32x2_pack(a, b)}; }
-__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
-__device__ __forceinline__ float2 split(Pair p) { float2 f; f32x2_unpack(p.r, f.x, f.y); return f; }
-__device__ __forceinline__ Pair mul(Pair a, Pair b) { return {f32x2_mul(a.r, b.r)}; }
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { return {f32x2_fma(a.r, b.r, c.r)}; }
 // A product that an addition follows is written as a b + z with z a -0 that the compiler cannot see through: it joins a packed product
 // and the sum that takes it to one rounding, .rn or not, and codes follow from the roundings.
 __device__ __forceinline__ Pair product(Pair a, Pair b, Pair z) { return fma2(a, b, z); }
-__device__ __forceinline__ Pair add(Pair a, Pair b)
-{
-    Pair d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.r) : "l"(a.r), "l"(b.r));
-    return d;
-}
 __device__ __forceinline__ Pair add_rz(Pair a, Pair b)
 {
     Pair d;

@@ -49,98 +49,135 @@ struct Shape {
     bool lng;
 };
 
-// What a lane has to do with the rows of its group.
-template <int NP> struct Lane {
-    int32_t d, shift;                       // shift: columns between the aligned piece that the row begins in and the row
-    int threads, group, tid;
+// What a lane has to do with the rows of its group.  EVEN: d is a multiple of eight, so that rows begin and end with whole pieces.
+template <int NP, bool EVEN> struct Lane {
+    int32_t shift;                          // columns between the aligned piece that a row begins in and the row
+    int threads, group, warp, lane;         // of the group
+    int32_t at;                             // the lane's first column from the aligned start on; its next pieces are 256 columns apart
     int64_t row, row_step, rows;            // first row, from one to the next, how many
     int64_t total;                          // elements of the whole tensor
     uint32_t mask[NP];                      // which of a piece's eight columns are the row's
-    __device__ __forceinline__ Lane(int64_t T, int32_t d_, int warps, int groups, int classes) : d(d_)
+    __device__ __forceinline__ Lane(int64_t T, int32_t d, int warps, int groups, int classes)
     {
         threads = warps * 32;
         group = threadIdx.x / threads;
-        tid = threadIdx.x - group * threads;
-        const int cls = blockIdx.x % classes;
-        const int64_t first = (int64_t)(blockIdx.x / classes) * groups + group, step = (int64_t)(gridDim.x / classes) * groups;
+        warp = (threadIdx.x >> 5) - group * warps;
+        lane = threadIdx.x & 31;
+        at = (warp * NP * 32 + lane) * 8;
+        const int cls = EVEN ? 0 : blockIdx.x % classes;
+        const int64_t first = (int64_t)(EVEN ? blockIdx.x : blockIdx.x / classes) * groups + group, step = (int64_t)(gridDim.x / classes) * groups;
         const int64_t here = (T - cls + classes - 1) / classes;      // rows of the class
         rows = first < here ? (here - first - 1) / step + 1 : 0;
         row = cls + first * classes;
         row_step = step * classes;
         total = T * d;
-        shift = (int32_t)(((int64_t)cls * d) & 7);
+        shift = EVEN ? 0 : (int32_t)(((int64_t)cls * d) & 7);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             mask[i] = 0;
+            if (EVEN) mask[i] = at + i * 256 < d ? 0xffu : 0u;
+            else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int32_t c = at(i) + e - shift;
-                if (c >= 0 && c < d) mask[i] |= 1u << e;
-            }
+                for (int e = 0; e < 8; ++e) {
+                    const int32_t c = at + i * 256 + e - shift;
+                    if (c >= 0 && c < d) mask[i] |= 1u << e;
+                }
         }
     }
-    __device__ __forceinline__ int32_t at(int i) const { return (i * threads + tid) * 8; }         // a piece's first column, from the aligned start on
-    __device__ __forceinline__ int64_t start(int64_t t) const { return t * d - shift; }            // the aligned start of row t
 };
 
 // Ring of a warp in shared memory.  A lane copies and takes its own pieces, so that nothing but its own copies is waited for.
-template <typename T, int NP>
-__device__ __forceinline__ void fetch(uint32_t to, const T *x, int64_t start, const Lane<NP> &l)
+// start: of the row in x, plus the lane's first column.
+template <typename T, int NP, bool EVEN>
+__device__ __forceinline__ void fetch(uint32_t to, const T *x, int64_t start, const Lane<NP, EVEN> &l)
 {
-    const int lane = threadIdx.x & 31;
+    const T *from = x + start;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         if (l.mask[i] == 0) continue;
-        const int64_t at = start + l.at(i);
-        const int64_t left = (l.total - at) * (int64_t)sizeof(T);     // bytes of the tensor from here on: the last piece may be a part
 #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-            const int size = left - h * 16 >= 16 ? 16 : left - h * 16 > 0 ? (int)(left - h * 16) : 0;
-            const T *from = size > 0 ? x + at + h * (16 / (int)sizeof(T)) : x;
-            const uint32_t slot = to + (i * ((int)sizeof(T) / 2) + h) * 512 + lane * 16;
-            if (sizeof(T) == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(slot), "l"(from), "r"(size) : "memory");
-            else asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" :: "r"(slot), "l"(from), "r"(size) : "memory");
+            constexpr int kPer = 16 / (int)sizeof(T);
+            const uint32_t slot = to + (i * ((int)sizeof(T) / 2) + h) * 512;
+            const T *f = from + i * 256 + h * kPer;
+            if (EVEN) {
+                if (sizeof(T) == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(f) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(f) : "memory");
+            } else {                                                  // the tensor's last piece may be a part: what is behind it is not read
+                const int64_t left = l.total - start - i * 256 - h * kPer;
+                const int size = left >= kPer ? 16 : left > 0 ? (int)left * (int)sizeof(T) : 0;
+                if (size == 0) f = x;
+                if (sizeof(T) == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(slot), "l"(f), "r"(size) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" :: "r"(slot), "l"(f), "r"(size) : "memory");
+            }
         }
     }
 }
-template <typename T, int NP> __device__ __forceinline__ void take(const char *from, int i, const Lane<NP> &l, float (&v)[8])
+__device__ __forceinline__ void keep(Pair (&v)[4], uint32_t mask)     // zero where there is no column
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 f = split(v[e]);
+        v[e] = pair(mask >> (2 * e) & 1u ? f.x : 0.0f, mask >> (2 * e + 1) & 1u ? f.y : 0.0f);
+    }
+}
+// Slots of pieces without columns hold zeros from the start on.
+template <typename T, int NP, bool EVEN> __device__ __forceinline__ void take(const char *from, int i, const Lane<NP, EVEN> &l, Pair (&v)[4])
 {
     Raw8<T> r;
-    const uint4 *q = reinterpret_cast<const uint4 *>(from + i * (int)sizeof(T) / 2 * 512) + (threadIdx.x & 31);
+    const uint4 *q = reinterpret_cast<const uint4 *>(from + i * (int)sizeof(T) / 2 * 512);
 #pragma unroll
     for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
         const uint4 x = q[h * 32];
         r.w[4 * h] = x.x; r.w[4 * h + 1] = x.y; r.w[4 * h + 2] = x.z; r.w[4 * h + 3] = x.w;
     }
     unpack8(r, v);
-    if (l.mask[i] != 0xffu) {                                         // a row's ends, and lanes behind it
+    if (!EVEN && l.mask[i] != 0xffu) keep(v, l.mask[i]);
+}
+__device__ __forceinline__ void store16(float *p, const Pair (&v)[4])
+{
+    float f[8];
+    spread8(v, f);
+    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ void store16(__nv_bfloat16 *p, const Pair (&v)[4])
+{
+    float f[8];
+    spread8(v, f);
+    store8(p, f);
+}
+template <typename T, int NP, bool EVEN> __device__ __forceinline__ void put(T *x, int64_t start, int i, const Lane<NP, EVEN> &l, const Pair (&v)[4])
+{
+    T *p = x + start + i * 256;
+    if (l.mask[i] == 0xffu) store16(p, v);
+    else if (!EVEN && l.mask[i] != 0) {
+        float f[8];
+        spread8(v, f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (!(l.mask[i] >> e & 1u)) v[e] = 0.0f;
+        for (int e = 0; e < 8; ++e) if (l.mask[i] >> e & 1u) store_from_float(p, e, f[e]);
     }
-}
-__device__ __forceinline__ void store16(float *p, const float (&v)[8])
-{
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ void store16(__nv_bfloat16 *p, const float (&v)[8]) { store8(p, v); }
-template <typename T, int NP> __device__ __forceinline__ void put(T *x, int64_t start, int i, const Lane<NP> &l, const float (&v)[8])
-{
-    T *p = x + start + l.at(i);
-    if (l.mask[i] == 0xffu) { store16(p, v); return; }
-    if (l.mask[i] == 0) return;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) if (l.mask[i] >> e & 1u) store_from_float(p, e, v[e]);
 }
 // A vector of d floats (or ones) in shared memory, from the aligned start on, as the thread block's rows lie.
 __device__ __forceinline__ void stage_vector(float *to, const float *from, float otherwise, int32_t d, int32_t shift, int32_t room)
 {
     for (int32_t c = threadIdx.x; c < room; c += blockDim.x) to[c] = from && c >= shift && c - shift < d ? from[c - shift] : otherwise;
 }
-__device__ __forceinline__ void read8(const float *from, float (&v)[8])
+__device__ __forceinline__ void read8(const float *from, Pair (&v)[4])
 {
     const float4 a = reinterpret_cast<const float4 *>(from)[0], b = reinterpret_cast<const float4 *>(from)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    v[0] = pair(a.x, a.y); v[1] = pair(a.z, a.w); v[2] = pair(b.x, b.y); v[3] = pair(b.z, b.w);
+}
+template <typename XT> __device__ __forceinline__ void round8(Pair (&v)[4]);
+template <> __device__ __forceinline__ void round8<float>(Pair (&)[4]) {}
+template <> __device__ __forceinline__ void round8<__nv_bfloat16>(Pair (&v)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float2 f = split(v[e]);
+        const uint32_t w = pack_bf16(f.x, f.y);
+        v[e] = pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
 }
 
 // Rows in the ring: two thread blocks of eight warps to an SM, half its shared memory each, less what gains and offsets take there.
@@ -158,7 +195,7 @@ template <typename XT, typename YT, int NP> struct BackwardRing {
 
 // The mean and the centred second moment are taken per warp and joined over the warps of a row (of two sets of n1 and n2 values:
 // M2 = M2a + M2b + (mean_b - mean_a)^2 n1 n2 / (n1 + n2)), so that a group meets once a row.
-template <typename XT, typename YT, int NP>
+template <typename XT, typename YT, int NP, bool EVEN>
 __global__ void __launch_bounds__(kThreads, 2)
 forward_kernel(const ForwardArgs a, const Shape sh)
 {
@@ -167,97 +204,110 @@ forward_kernel(const ForwardArgs a, const Shape sh)
     extern __shared__ __align__(16) char smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const Lane<NP> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
+    const Lane<NP, EVEN> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
     const int32_t room = sh.warps * NP * 256;
-    float *gamma = reinterpret_cast<float *>(smem), *beta = gamma + room;
-    char *ring = smem + 2 * room * 4 + (threadIdx.x >> 5) * (R::kStages * R::kBytes);
+    float *gamma = reinterpret_cast<float *>(smem) + l.at, *beta = gamma + room;
+    char *ring = smem + 2 * room * 4 + (threadIdx.x >> 5) * (R::kStages * R::kBytes) + l.lane * 16;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const XT *x = static_cast<const XT *>(a.x), *residual = static_cast<const XT *>(a.residual);
     XT *sum = static_cast<XT *>(a.sum);
     YT *y = static_cast<YT *>(a.y);
-    auto get = [&](int64_t k) {
-        if (k < l.rows) {
-            const int64_t start = l.start(l.row + k * l.row_step);
-            const uint32_t to = ring_at + (uint32_t)(k % R::kStages) * R::kBytes;
-            fetch(to, x, start, l);
-            if (residual) fetch(to + R::kX, residual, start, l);
+    const int64_t step = l.row_step * a.d;                            // elements from one row to the next
+    int64_t t = l.row, start = t * a.d - l.shift + l.at, ahead = start;
+    int32_t left = (int32_t)l.rows, coming = left;                    // rows to work on, to fetch
+    auto get = [&](int slot) {
+        if (coming > 0) {
+            const uint32_t to = ring_at + slot * R::kBytes;
+            fetch(to, x, ahead, l);
+            if (residual) fetch(to + R::kX, residual, ahead, l);
+            --coming;
+            ahead += step;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+        if (l.mask[i] == 0)
+            for (int k = 0; k < R::kStages * 2; ++k)                  // the piece in each stage's two tensors
+                for (int h = 0; h < (int)sizeof(XT) / 2; ++h)
+                    *reinterpret_cast<uint4 *>(ring + k * R::kX + (i * ((int)sizeof(XT) / 2) + h) * 512) = make_uint4(0, 0, 0, 0);
     for (int k = 0; k < R::kStages - 1; ++k) get(k);
-    stage_vector(gamma, a.gamma, 1.0f, a.d, l.shift, room);
-    stage_vector(beta, a.beta, 0.0f, a.d, l.shift, room);
+    stage_vector(reinterpret_cast<float *>(smem), a.gamma, 1.0f, a.d, l.shift, room);
+    stage_vector(reinterpret_cast<float *>(smem) + room, a.beta, 0.0f, a.d, l.shift, room);
     __syncthreads();
     int32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) mine += __popc(l.mask[i]);
     const float n_warp = (float)__reduce_add_sync(0xffffffffu, mine), share = n_warp > 0.0f ? 1.0f / n_warp : 0.0f, inv_d = 1.0f / (float)a.d;
-    int turn = 0;
-    for (int64_t k = 0; k < l.rows; ++k, turn ^= 1) {
-        const int64_t t = l.row + k * l.row_step, start = l.start(t);
+    int turn = 0, slot = 0;
+    for (; left > 0; --left, turn ^= 1, t += l.row_step, start += step) {
         asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
-        const char *from = ring + (int)(k % R::kStages) * R::kBytes;
-        float v[NP][8];
+        const char *from = ring + slot * R::kBytes;
+        Pair v[NP][4], s = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NP; ++i) take<XT>(from, i, l, v[i]);
         if (residual) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                float r[8];
+                Pair r[4];
                 take<XT>(from + R::kX, i, l, r);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = rounded<XT>(v[i][e] + r[e]);
+                for (int e = 0; e < 4; ++e) v[i][e] = add(v[i][e], r[e]);
+                round8<XT>(v[i]);
                 put(sum, start, i, l, v[i]);
             }
         }
-        get(k + R::kStages - 1);                                      // into the slot that was taken a row ago
-        float s = 0.0f;
+        get(slot == 0 ? R::kStages - 1 : slot - 1);                   // into the slot that was taken a row ago
+        slot = slot + 1 == R::kStages ? 0 : slot + 1;
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s += v[i][e];
-        float n = n_warp, mean = warp_sum(s) * share, q = 0.0f;
+            for (int e = 0; e < 4; ++e) s = add(s, v[i][e]);
+        const float2 s2 = split(s);
+        float n = n_warp, mean = warp_sum(s2.x + s2.y) * share;
+        const float local = mean;
+        Pair q2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float c[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) c[e] = v[i][e] - mean;
-            if (l.mask[i] != 0xffu) {
+            for (int e = 0; e < 4; ++e) v[i][e] = add(v[i][e], both(-local));
+            if (!EVEN && l.mask[i] != 0xffu) keep(v[i], l.mask[i]);
+            if (!EVEN || l.mask[i] != 0) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) if (!(l.mask[i] >> e & 1u)) c[e] = 0.0f;
+                for (int e = 0; e < 4; ++e) q2 = fma2(v[i][e], v[i][e], q2);
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q = fmaf(c[e], c[e], q);
         }
-        q = warp_sum(q);
+        const float2 qq = split(q2);
+        float q = warp_sum(qq.x + qq.y);
         if (sh.warps > 1) {
             const float3 *all = part[turn] + l.group * sh.warps;
-            if ((l.tid & 31) == 0) part[turn][threadIdx.x >> 5] = make_float3(n, mean, q);
+            if (l.lane == 0) part[turn][threadIdx.x >> 5] = make_float3(n, mean, q);
             group_sync(l.group, l.threads);
             n = all[0].x; mean = all[0].y; q = all[0].z;
             for (int w = 1; w < sh.warps; ++w) {
                 const float3 b = all[w];
                 if (b.x > 0.0f) {
-                    const float both = n + b.x, delta = b.y - mean, part_b = b.x / both;
+                    const float sum_n = n + b.x, delta = b.y - mean, part_b = __fdividef(b.x, sum_n);
                     mean = fmaf(delta, part_b, mean);
                     q += fmaf(delta * delta, n * part_b, b.z);
-                    n = both;
+                    n = sum_n;
                 }
             }
         }
         const float rstd = rsqrtf(q * inv_d + a.eps);
-        if (l.tid == 0) {
+        if (l.lane == 0 && l.warp == 0) {
             if (a.mean) a.mean[t] = mean;
             if (a.rstd) a.rstd[t] = rstd;
         }
+        const Pair back = both(local - mean), r2 = both(rstd);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float o[8], w[8], b[8];
-            read8(gamma + l.at(i), w);
-            read8(beta + l.at(i), b);
+            Pair w[4], b[4];
+            read8(gamma + i * 256, w);
+            read8(beta + i * 256, b);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf((v[i][e] - mean) * rstd, w[e], b[e]);
-            put(y, start, i, l, o);
+            for (int e = 0; e < 4; ++e) v[i][e] = fma2(mul(add(v[i][e], back), r2), w[e], b[e]);
+            put(y, start, i, l, v[i]);
         }
     }
 }
@@ -304,7 +354,7 @@ forward_long_kernel(const XT *__restrict__ x, const XT *__restrict__ residual, i
 }
 
 // A thread block walks over rows with a stride; a lane keeps its columns' share of dgamma and dbeta in registers to the end.
-template <typename XT, typename YT, int NP>
+template <typename XT, typename YT, int NP, bool EVEN>
 __global__ void __launch_bounds__(kThreads, NP == 4 ? 1 : 2)
 backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partial)
 {
@@ -313,82 +363,100 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
     extern __shared__ __align__(16) char smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const Lane<NP> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
+    const Lane<NP, EVEN> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
     const int32_t room = sh.warps * NP * 256;
-    float *gamma = reinterpret_cast<float *>(smem);
-    char *rings = smem + room * 4, *ring = rings + (threadIdx.x >> 5) * (R::kStages * R::kBytes);
+    const float *gamma = reinterpret_cast<const float *>(smem) + l.at;
+    char *rings = smem + room * 4, *ring = rings + (threadIdx.x >> 5) * (R::kStages * R::kBytes) + l.lane * 16;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const XT *x = static_cast<const XT *>(a.x), *dsum = static_cast<const XT *>(a.dsum);
     const YT *dy = static_cast<const YT *>(a.dy);
     XT *dx = static_cast<XT *>(a.dx);
-    auto get = [&](int64_t k) {
-        if (k < l.rows) {
-            const int64_t start = l.start(l.row + k * l.row_step);
-            const uint32_t to = ring_at + (uint32_t)(k % R::kStages) * R::kBytes;
-            fetch(to, x, start, l);
-            fetch(to + R::kX, dy, start, l);
-            if (dsum) fetch(to + R::kX + R::kY, dsum, start, l);
+    const int64_t step = l.row_step * a.d;
+    int64_t start = l.row * a.d - l.shift + l.at, ahead = start;
+    int32_t left = (int32_t)l.rows, coming = left;
+    auto get = [&](int slot) {
+        if (coming > 0) {
+            const uint32_t to = ring_at + slot * R::kBytes;
+            fetch(to, x, ahead, l);
+            fetch(to + R::kX, dy, ahead, l);
+            if (dsum) fetch(to + R::kX + R::kY, dsum, ahead, l);
+            --coming;
+            ahead += step;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+        if (l.mask[i] == 0)
+            for (int k = 0; k < R::kStages; ++k)
+                for (int h = 0; h < 2; ++h) {                         // the piece's halves in x, dsum and dy
+                    const uint4 zero = make_uint4(0, 0, 0, 0);
+                    if (h < (int)sizeof(XT) / 2) {
+                        const int at = k * R::kBytes + (i * ((int)sizeof(XT) / 2) + h) * 512;
+                        *reinterpret_cast<uint4 *>(ring + at) = *reinterpret_cast<uint4 *>(ring + at + R::kX + R::kY) = zero;
+                    }
+                    if (h < (int)sizeof(YT) / 2) *reinterpret_cast<uint4 *>(ring + k * R::kBytes + R::kX + (i * ((int)sizeof(YT) / 2) + h) * 512) = zero;
+                }
     for (int k = 0; k < R::kStages - 1; ++k) get(k);
-    stage_vector(gamma, a.gamma, 1.0f, a.d, l.shift, room);
+    stage_vector(reinterpret_cast<float *>(smem), a.gamma, 1.0f, a.d, l.shift, room);
     __syncthreads();
-    float dg[NP][8], db[NP][8];
+    Pair dg[NP][4], db[NP][4];
 #pragma unroll
     for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dg[i][e] = db[i][e] = 0.0f;
+        for (int e = 0; e < 4; ++e) dg[i][e] = db[i][e] = both(0.0f);
     const float inv_d = 1.0f / (float)a.d;
+    const float *mean = a.mean + l.row, *rstd = a.rstd + l.row;
     float mu_next = 0.0f, rs_next = 0.0f;
-    if (l.rows > 0) { mu_next = a.mean[l.row]; rs_next = a.rstd[l.row]; }
-    int turn = 0;
-    for (int64_t k = 0; k < l.rows; ++k, turn ^= 1) {
-        const int64_t t = l.row + k * l.row_step, start = l.start(t);
-        const float mu = mu_next, rs = rs_next;
-        if (k + 1 < l.rows) { mu_next = a.mean[t + l.row_step]; rs_next = a.rstd[t + l.row_step]; }
+    if (left > 0) { mu_next = *mean; rs_next = *rstd; }
+    int turn = 0, slot = 0;
+    for (; left > 0; --left, turn ^= 1, start += step) {
+        const Pair mu = both(-mu_next), rs = both(rs_next);
+        if (left > 1) { mean += l.row_step; rstd += l.row_step; mu_next = *mean; rs_next = *rstd; }
         asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
-        const char *from = ring + (int)(k % R::kStages) * R::kBytes;
-        float g[NP][8], h[NP][8];
-        float s1 = 0.0f, s2 = 0.0f;
+        const char *from = ring + slot * R::kBytes;
+        Pair g[NP][4], h[NP][4], s1 = both(0.0f), s2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            float w[8];
+            Pair w[4];
             take<XT>(from, i, l, h[i]);
             take<YT>(from + R::kX, i, l, g[i]);
-            read8(gamma + l.at(i), w);
+            read8(gamma + i * 256, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[i][e] = (h[i][e] - mu) * rs;                        // of a masked column: times a g of zero
-                db[i][e] += g[i][e];
-                dg[i][e] = fmaf(g[i][e], h[i][e], dg[i][e]);
-                g[i][e] *= w[e];
-                s1 += g[i][e];
-                s2 = fmaf(g[i][e], h[i][e], s2);
+            for (int e = 0; e < 4; ++e) {
+                h[i][e] = mul(add(h[i][e], mu), rs);                  // of a masked column: times a g of zero
+                db[i][e] = add(db[i][e], g[i][e]);
+                dg[i][e] = fma2(g[i][e], h[i][e], dg[i][e]);
+                g[i][e] = mul(g[i][e], w[e]);
+                s1 = add(s1, g[i][e]);
+                s2 = fma2(g[i][e], h[i][e], s2);
             }
         }
-        s1 = warp_sum(s1); s2 = warp_sum(s2);
+        const float2 p1 = split(s1), p2 = split(s2);
+        float t1 = warp_sum(p1.x + p1.y), t2 = warp_sum(p2.x + p2.y);
         if (sh.warps > 1) {
             const float2 *all = part[turn] + l.group * sh.warps;
-            if ((l.tid & 31) == 0) part[turn][threadIdx.x >> 5] = make_float2(s1, s2);
+            if (l.lane == 0) part[turn][threadIdx.x >> 5] = make_float2(t1, t2);
             group_sync(l.group, l.threads);
-            s1 = s2 = 0.0f;
-            for (int w = 0; w < sh.warps; ++w) { s1 += all[w].x; s2 += all[w].y; }
+            t1 = t2 = 0.0f;
+            for (int w = 0; w < sh.warps; ++w) { t1 += all[w].x; t2 += all[w].y; }
         }
-        s1 *= inv_d; s2 *= inv_d;
+        const Pair m1 = both(-t1 * inv_d), m2 = both(-t2 * inv_d);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) g[i][e] = (g[i][e] - s1 - h[i][e] * s2) * rs;
             if (dsum) {
-                float r[8];
+                Pair r[4];
                 take<XT>(from + R::kX + R::kY, i, l, r);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[i][e] += r[e];
+                for (int e = 0; e < 4; ++e) g[i][e] = fma2(fma2(h[i][e], m2, add(g[i][e], m1)), rs, r[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g[i][e] = mul(fma2(h[i][e], m2, add(g[i][e], m1)), rs);
             }
             put(dx, start, i, l, g[i]);
         }
-        get(k + R::kStages - 1);                                      // into the slot that was taken a row ago
+        get(slot == 0 ? R::kStages - 1 : slot - 1);                   // into the slot that was taken a row ago
+        slot = slot + 1 == R::kStages ? 0 : slot + 1;
     }
     if (!partial) return;
     // the groups' sums, in their order; the rings are done with
@@ -398,9 +466,10 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
 #pragma unroll
     for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            columns[(l.group * 2) * room + l.at(i) + e] = dg[i][e];
-            columns[(l.group * 2 + 1) * room + l.at(i) + e] = db[i][e];
+        for (int e = 0; e < 4; ++e) {
+            float2 *to = reinterpret_cast<float2 *>(columns + l.group * 2 * room + l.at + i * 256 + 2 * e);
+            to[0] = split(dg[i][e]);
+            to[room / 2] = split(db[i][e]);
         }
     __syncthreads();
     for (int32_t c = threadIdx.x; c < 2 * a.d; c += blockDim.x) {
@@ -529,10 +598,14 @@ int64_t blocks_of(int64_t T, const Shape &s, int per_sm)
 constexpr size_t kHalf = 113 * 1024;
 constexpr int kLongParts = 64;
 
-template <typename F> cudaError_t with_pieces(int np, F f)
+template <typename E, typename F> cudaError_t with_pieces(int np, E even, F f)
 {
-    return np == 1 ? f(std::integral_constant<int, 1>{}) : np == 2 ? f(std::integral_constant<int, 2>{})
-         : np == 3 ? f(std::integral_constant<int, 3>{}) : f(std::integral_constant<int, 4>{});
+    return np == 1 ? f(std::integral_constant<int, 1>{}, even) : np == 2 ? f(std::integral_constant<int, 2>{}, even)
+         : np == 3 ? f(std::integral_constant<int, 3>{}, even) : f(std::integral_constant<int, 4>{}, even);
+}
+template <typename F> cudaError_t with_shape(const Shape &s, F f)
+{
+    return s.classes == 1 ? with_pieces(s.np, std::true_type{}, f) : with_pieces(s.np, std::false_type{}, f);
 }
 template <typename K> cudaError_t allow(K kernel, size_t smem)
 {
@@ -548,13 +621,14 @@ template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs 
                           static_cast<const XT *>(a.residual), a.T, a.d, a.gamma, a.beta, a.eps, static_cast<XT *>(a.sum), static_cast<YT *>(a.y), a.mean,
                           a.rstd);
     }
-    return with_pieces(sh.np, [&](auto np) {
+    return with_shape(sh, [&](auto np, auto even) {
         constexpr int NP = decltype(np)::value;
+        constexpr bool EVEN = decltype(even)::value;
         typedef ForwardRing<XT, YT, NP> R;
         const size_t smem = (size_t)2 * sh.warps * NP * 256 * 4 + (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
-        const cudaError_t e = allow(forward_kernel<XT, YT, NP>, smem);
+        const cudaError_t e = allow(forward_kernel<XT, YT, NP, EVEN>, smem);
         if (e != cudaSuccess) return e;
-        return launch_pdl(forward_kernel<XT, YT, NP>, dim3((unsigned)blocks_of(a.T, sh, smem <= kHalf ? 2 : 1)), dim3(sh.groups * sh.warps * 32), smem, s, a, sh);
+        return launch_pdl(forward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)blocks_of(a.T, sh, smem <= kHalf ? 2 : 1)), dim3(sh.groups * sh.warps * 32), smem, s, a, sh);
     });
 }
 
@@ -576,16 +650,17 @@ template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArg
             e = launch_pdl(column_sums_kernel<XT, YT>, dim3(slabs < 4096 ? slabs : 4096, parts), dim3(kThreads), 0, s, dy, x, a.T, a.d, a.mean,
                            a.rstd, partial);
     } else {
-        e = with_pieces(sh.np, [&](auto np) {
+        e = with_shape(sh, [&](auto np, auto even) {
             constexpr int NP = decltype(np)::value;
+        constexpr bool EVEN = decltype(even)::value;
             typedef BackwardRing<XT, YT, NP> R;
             const size_t room = (size_t)sh.warps * NP * 256 * 4, rings = (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
             const size_t sums_room = (size_t)sh.groups * 2 * room;    // the same space as the rings, which are larger
             const size_t smem = room + (rings > sums_room ? rings : sums_room);
-            const cudaError_t e1 = allow(backward_kernel<XT, YT, NP>, smem);
+            const cudaError_t e1 = allow(backward_kernel<XT, YT, NP, EVEN>, smem);
             if (e1 != cudaSuccess) return e1;
             parts = (int32_t)blocks_of(a.T, sh, NP < 4 && smem <= kHalf ? 2 : 1);
-            return launch_pdl(backward_kernel<XT, YT, NP>, dim3((unsigned)parts), dim3(sh.groups * sh.warps * 32), smem, s, a, sh, sums ? partial : nullptr);
+            return launch_pdl(backward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)parts), dim3(sh.groups * sh.warps * 32), smem, s, a, sh, sums ? partial : nullptr);
         });
     }
     if (e != cudaSuccess || !sums) return e;

@@ -59,6 +59,37 @@ template <typename T> inline bool aligned8(const void *p, int64_t pitch = 0)
     return (reinterpret_cast<uintptr_t>(p) % (8 * sizeof(T))) == 0 && pitch % 8 == 0;
 }
 
+// Two fp32 values to an instruction, where the rate at which instructions issue is what bounds a kernel.  (The compiler may join a
+// product and the sum that takes it to one rounding.)
+struct Pair { uint64_t r; };
+__device__ __forceinline__ Pair pair(float a, float b) { return {f32x2_pack(a, b)}; }
+__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
+__device__ __forceinline__ float2 split(Pair p) { float2 f; f32x2_unpack(p.r, f.x, f.y); return f; }
+__device__ __forceinline__ Pair mul(Pair a, Pair b) { return {f32x2_mul(a.r, b.r)}; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { return {f32x2_fma(a.r, b.r, c.r)}; }
+__device__ __forceinline__ Pair add(Pair a, Pair b)
+{
+    Pair d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d.r) : "l"(a.r), "l"(b.r));
+    return d;
+}
+// Raw8 as four pairs, and back.
+__device__ __forceinline__ void unpack8(const Raw8<float> &r, Pair (&v)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pair(__uint_as_float(r.w[2 * e]), __uint_as_float(r.w[2 * e + 1]));
+}
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, Pair (&v)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = pair(__uint_as_float(r.w[e] << 16), __uint_as_float(r.w[e] & 0xffff0000u));
+}
+__device__ __forceinline__ void spread8(const Pair (&v)[4], float (&f)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f32x2_unpack(v[e].r, f[2 * e], f[2 * e + 1]);
+}
+
 __device__ __forceinline__ float value_of(float v) { return v; }
 __device__ __forceinline__ float value_of(__nv_bfloat16 v) { return __bfloat162float(v); }
 
