@@ -229,7 +229,8 @@ int tbn_embedding_bwd(const int64_t *ids, int64_t T, const void *dy, int dy_dtyp
  *     dgamma[i] = sum_t dy[t][i] h[t][i],  dbeta[i] = sum_t dy[t][i]
  *   dsum (T x d of x_dtype, or NULL): a gradient that reaches s by other ways.  dx (T x d of x_dtype) is the gradient of x and of
  *   the residual.  dgamma, dbeta: d floats or NULL.  All are overwritten; sums are fp32 in an order that T and d decide.
- *   workspace: tbn_layernorm_bwd_workspace_bytes(T, d) bytes; not needed when dgamma and dbeta are NULL.  T == 0: zeros.
+ *   workspace: tbn_layernorm_bwd_workspace_bytes(T, d) bytes (0 for a few rows); not needed when dgamma and dbeta are NULL.
+ *   T == 0: zeros.
  * No output may overlap an input.  A row that holds an infinity or a NaN has NaN in its y and dx and in dgamma; no other row is
  * affected. */
 int tbn_layernorm_train_fwd(const void *x, const void *residual, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *beta, float eps,

@@ -660,12 +660,12 @@ def tbn_linear_distill_bwd(x: torch.Tensor, weight: torch.Tensor, top_index: tor
 def _on_device(name, device, *args):
     """Runs the entry point on the tensors' device and that device's current stream."""
     index = device.index
-    fn, stream = getattr(lib(), name), torch._C._cuda_getCurrentRawStream(index)
-    if torch.cuda.current_device() == index:
-        status = fn(*args, stream)
+    fn = getattr(_lib or lib(), name)
+    if torch._C._cuda_getDevice() == index:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(index):
-            status = fn(*args, stream)
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     if status != OK:
         raise TbnError(status, name)
 
@@ -678,12 +678,21 @@ def _same_device(where, device, *tensors):
             raise ValueError(f"{where}: tensors on {device} and {t.device}")
 
 
-def _workspace(where, workspace, need, device):
+@functools.lru_cache(maxsize=1024)
+def _workspace_need(name, device_index, *sizes):
+    """Workspace bytes of a call; they follow from the sizes and the device's number of SMs."""
+    with torch.cuda.device(device_index):
+        return int(getattr(lib(), name)(*sizes))
+
+
+def _workspace(where, workspace, device, name, *sizes):
+    """(tensor, its bytes)"""
     if workspace is None:
-        return torch.empty(need or 16, dtype=torch.uint8, device=device)
+        need = _workspace_need(name, device.index, *sizes)
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None, need
     if workspace.device != device:
         raise ValueError(f"{where}: workspace on {workspace.device}, tensors on {device}")
-    return workspace
+    return workspace, workspace.numel() * workspace.element_size()
 
 
 def _embedding_ids(ids, where):
@@ -695,14 +704,16 @@ def _embedding_ids(ids, where):
 def tbn_embedding_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, padding_idx: int = -1, y_dtype: int | None = None) -> torch.Tensor:
     """scale * table[ids]; ids of any shape, y of shape ids.shape + (d,).  Ids outside the table and padding_idx give zeros."""
     T, device = _embedding_ids(ids, "embedding"), ids.device
-    if table.dim() != 2:
-        raise TbnError(-2, f"embedding: table {tuple(table.shape)}")
+    shape = table.shape
+    if len(shape) != 2:
+        raise TbnError(-2, f"embedding: table {tuple(shape)}")
     _same_device("embedding", device, table)
-    V, d = table.shape
+    V, d = shape
     td = _dtype_code(table)
-    yd = td if y_dtype is None else y_dtype
-    y = torch.empty((*ids.shape, d), dtype=_torch_dtype(yd), device=device)
-    _on_device("tbn_embedding_fwd", device, _ptr(ids), T, _ptr(table), td, V, d, padding_idx, scale, _ptr(y), yd)
+    if y_dtype is None:
+        y_dtype = td
+    y = torch.empty(*ids.shape, d, dtype=_torch_dtype(y_dtype), device=device)
+    _on_device("tbn_embedding_fwd", device, _ptr(ids), T, _ptr(table), td, V, d, padding_idx, scale, y.data_ptr(), y_dtype)
     return y
 
 
@@ -713,12 +724,13 @@ def tbn_embedding_tiled_fwd(ids: torch.Tensor, vocab: int, d: int, tile: torch.T
     _same_device("embedding", device, tile, alpha)
     if k <= 0 or (vocab * d) % k:
         raise TbnError(-2, "tbn_embedding_tiled_fwd")
-    if tile.dtype != torch.int32 or tile.numel() < tbn_tile_words(vocab * d // k):
+    if tile.dtype != torch.int32 or tile.numel() < -(-(vocab * d // k) // 128) * 4:
         raise TbnError(-2, f"embedding: the tile must be int32 of {tbn_tile_words(vocab * d // k)} words")
     if alpha.dtype != torch.float32 or alpha.numel() < (k if alpha_mode == ALPHA_PER_TILE else 1):
         raise TbnError(-2, "embedding: alpha must be float32, one value or one for each tile")
-    y = torch.empty((*ids.shape, d), dtype=_torch_dtype(y_dtype), device=device)
-    _on_device("tbn_embedding_tiled_fwd", device, _ptr(ids), T, vocab, d, _ptr(tile), k, _ptr(alpha), alpha_mode, padding_idx, scale, _ptr(y), y_dtype)
+    y = torch.empty(*ids.shape, d, dtype=_torch_dtype(y_dtype), device=device)
+    _on_device("tbn_embedding_tiled_fwd", device, _ptr(ids), T, vocab, d, _ptr(tile), k, _ptr(alpha), alpha_mode, padding_idx, scale, y.data_ptr(),
+               y_dtype)
     return y
 
 
@@ -731,9 +743,10 @@ def tbn_embedding_bwd(ids: torch.Tensor, dy: torch.Tensor, vocab: int, scale: fl
     """Gradient of an embedding's table (vocab x d): the rows of dy that share an id, added up.  add_to: a gradient that is there
     already (a tied head's), which the sums are added to in place; otherwise a new tensor of dw_dtype (dy's type by default)."""
     T, device = _embedding_ids(ids, "embedding"), ids.device
-    if dy.shape[:-1] != ids.shape or dy.dim() < 1:
-        raise TbnError(-2, f"embedding: ids {tuple(ids.shape)} and dy {tuple(dy.shape)}")
-    d, gd = dy.shape[-1], _dtype_code(dy)
+    shape = dy.shape
+    if len(shape) < 1 or shape[:-1] != ids.shape:
+        raise TbnError(-2, f"embedding: ids {tuple(ids.shape)} and dy {tuple(shape)}")
+    d, gd = shape[-1], _dtype_code(dy)
     _same_device("embedding", device, dy, add_to)
     if add_to is not None:
         if add_to.shape != (vocab, d):
@@ -741,39 +754,47 @@ def tbn_embedding_bwd(ids: torch.Tensor, dy: torch.Tensor, vocab: int, scale: fl
         wd, dw = _dtype_code(add_to), add_to
     else:
         wd = gd if dw_dtype is None else dw_dtype
-        dw = torch.empty((vocab, d), dtype=_torch_dtype(wd), device=device)
-    ws = _workspace("embedding", workspace, tbn_embedding_bwd_workspace_bytes(T, d, vocab), device)
-    _on_device("tbn_embedding_bwd", device, _ptr(ids), T, _ptr(dy), gd, vocab, d, padding_idx, scale, _ptr(dw), wd, int(add_to is not None),
-               _ptr(ws), ws.numel() * ws.element_size())
+        dw = torch.empty(vocab, d, dtype=_torch_dtype(wd), device=device)
+    ws, size = _workspace("embedding", workspace, device, "tbn_embedding_bwd_workspace_bytes", T, d, vocab)
+    _on_device("tbn_embedding_bwd", device, _ptr(ids), T, _ptr(dy), gd, vocab, d, padding_idx, scale, _ptr(dw), wd, int(add_to is not None), _ptr(ws), size)
     return dw
 
 
-def _norm_vectors(where, d, device, *vectors):
-    for v in vectors:
-        if v is not None and (v.shape != (d,) or v.dtype != torch.float32 or v.device != device):
-            raise TbnError(-2, f"{where}: must be float32 of shape ({d},) on {device}")
+def _norm_vector(v, n, device, what):
+    """Address of a float32 vector of n values."""
+    if v is None:
+        return None
+    if v.dtype is not torch.float32 or v.shape != (n,) or v.device != device:
+        raise TbnError(-2, f"layer norm: {what} must be float32 of shape ({n},) on {device}")
+    return _ptr(v)
 
 
 def tbn_layernorm_train_fwd(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, eps: float = 1e-5,
                             residual: torch.Tensor | None = None, y_dtype: int | None = None):
     """LayerNorm of s = x + residual (rounded to x's type; s is x without a residual) over the last dimension, for training.
     Returns (y, s, mean, rstd): what tbn_layernorm_bwd takes besides dy."""
-    shape, device = x.shape, x.device
-    d = shape[-1]
+    device, xd, d = x.device, _dtype_code(x), x.shape[-1]
     T = x.numel() // d if d else 0
-    _same_device("layer norm", device, residual)
-    _norm_vectors("layer norm: gamma and beta", d, device, gamma, beta)
-    if residual is not None and (residual.shape != shape or residual.dtype != x.dtype):
-        raise TbnError(-2, f"layer norm: x {tuple(shape)} {x.dtype} and residual {tuple(residual.shape)} {residual.dtype}")
-    xd = _dtype_code(x)
-    yd = xd if y_dtype is None else y_dtype
-    y = torch.empty(shape, dtype=_torch_dtype(yd), device=device)
-    s = torch.empty_like(x) if residual is not None else x
-    stats = torch.empty((2, T), dtype=torch.float32, device=device)
-    at = stats.data_ptr()
-    _on_device("tbn_layernorm_train_fwd", device, _ptr(x), _ptr(residual), xd, T, d, _ptr(gamma), _ptr(beta), eps,
-               _ptr(s) if residual is not None else None, _ptr(y), yd, at, at + 4 * T)
-    return y, s, stats[0], stats[1]
+    if device.type != "cuda":
+        raise ValueError("layer norm: the tensors must be on a CUDA device")
+    x_at, g_at, b_at = _ptr(x), _norm_vector(gamma, d, device, "gamma"), _norm_vector(beta, d, device, "beta")
+    if residual is None:
+        s, r_at, s_at = x, None, None
+    else:
+        if residual.device != device:
+            raise ValueError(f"layer norm: tensors on {device} and {residual.device}")
+        if residual.shape != x.shape or residual.dtype is not x.dtype:
+            raise TbnError(-2, f"layer norm: x {tuple(x.shape)} {x.dtype} and residual {tuple(residual.shape)} {residual.dtype}")
+        s, r_at = torch.empty_like(x), _ptr(residual)
+        s_at = s.data_ptr()
+    if y_dtype is None or y_dtype == xd:
+        y_dtype, y = xd, torch.empty_like(x)
+    else:
+        y = torch.empty_like(x, dtype=_torch_dtype(y_dtype))
+    mean = torch.empty(T, dtype=torch.float32, device=device)
+    rstd = torch.empty_like(mean)
+    _on_device("tbn_layernorm_train_fwd", device, x_at, r_at, xd, T, d, g_at, b_at, eps, s_at, y.data_ptr(), y_dtype, mean.data_ptr(), rstd.data_ptr())
+    return y, s, mean, rstd
 
 
 def tbn_layernorm_bwd_workspace_bytes(T, d) -> int:
@@ -787,20 +808,23 @@ def tbn_layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, mean: torch.Tensor, rst
     shape, device = s.shape, s.device
     d = shape[-1]
     T = s.numel() // d if d else 0
-    _same_device("layer norm", device, dy, dsum)
-    if dy.shape != shape or (dsum is not None and (dsum.shape != shape or dsum.dtype != s.dtype)):
+    if device.type != "cuda" or dy.device != device or (dsum is not None and dsum.device != device):
+        raise ValueError(f"layer norm: the tensors must be on one CUDA device: {device}, {dy.device}" + ("" if dsum is None else f", {dsum.device}"))
+    if dy.shape != shape or (dsum is not None and (dsum.shape != shape or dsum.dtype is not s.dtype)):
         raise TbnError(-2, f"layer norm: dy {tuple(dy.shape)}, s {tuple(shape)}" + ("" if dsum is None else f", dsum {tuple(dsum.shape)} {dsum.dtype}"))
-    _norm_vectors("layer norm: gamma", d, device, gamma)
-    _norm_vectors("layer norm: mean and rstd", T, device, mean, rstd)
-    dx = torch.empty_like(s)
-    sums = torch.empty((int(need_dgamma) + int(need_dbeta), d), dtype=torch.float32, device=device) if need_dgamma or need_dbeta else None
-    dgamma = sums[0] if need_dgamma else None
-    dbeta = sums[-1] if need_dbeta else None
-    ws = None
-    if sums is not None:
-        ws = _workspace("layer norm", workspace, tbn_layernorm_bwd_workspace_bytes(T, d), device)
-    _on_device("tbn_layernorm_bwd", device, _ptr(dy), _dtype_code(dy), _ptr(s), _dtype_code(s), T, d, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dsum),
-               _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size())
+    g_at, m_at, r_at = _norm_vector(gamma, d, device, "gamma"), _norm_vector(mean, T, device, "mean"), _norm_vector(rstd, T, device, "rstd")
+    dx, dgamma, dbeta, dg_at, db_at, ws_at, size = torch.empty_like(s), None, None, None, None, None, 0
+    if need_dgamma:
+        dgamma = torch.empty(d, dtype=torch.float32, device=device)
+        dg_at = dgamma.data_ptr()
+    if need_dbeta:
+        dbeta = torch.empty(d, dtype=torch.float32, device=device)
+        db_at = dbeta.data_ptr()
+    if need_dgamma or need_dbeta:
+        ws, size = _workspace("layer norm", workspace, device, "tbn_layernorm_bwd_workspace_bytes", T, d)
+        ws_at = _ptr(ws)
+    _on_device("tbn_layernorm_bwd", device, _ptr(dy), _dtype_code(dy), _ptr(s), _dtype_code(s), T, d, g_at, m_at, r_at, _ptr(dsum), dx.data_ptr(), dg_at,
+               db_at, ws_at, size)
     return dx, dgamma, dbeta
 
 
@@ -867,15 +891,12 @@ def tbn_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=No
 def tbn_grad_norm(tensors: AdamWTensors, max_norm: float, workspace: torch.Tensor | None = None):
     """Global norm of the gradients and the factor that brings it down to max_norm: (norm [1], scale [1]), on the device.  scale goes
     to tbn_adamw_step as it is; it is NaN, and the step leaves everything as it is, where the norm is not finite."""
-    out = torch.empty((2, 1), dtype=torch.float32, device=tensors.device)
-    ws = workspace
-    if ws is None:
-        with torch.cuda.device(tensors.device):
-            need = int(lib().tbn_grad_norm_workspace_bytes(tensors.count))
-    ws = _workspace("grad norm", workspace, need if workspace is None else 0, tensors.device)
-    at = out.data_ptr()
-    _on_device("tbn_grad_norm", tensors.device, tensors.at, tensors.count, max_norm, at, at + 4, _ptr(ws), ws.numel() * ws.element_size())
-    return out[0], out[1]
+    device = tensors.device
+    norm = torch.empty(1, dtype=torch.float32, device=device)
+    scale = torch.empty(1, dtype=torch.float32, device=device)
+    ws, size = _workspace("grad norm", workspace, device, "tbn_grad_norm_workspace_bytes", tensors.count)
+    _on_device("tbn_grad_norm", device, tensors.at, tensors.count, max_norm, norm.data_ptr(), scale.data_ptr(), _ptr(ws), size)
+    return norm, scale
 
 
 def tbn_adamw_step(tensors: AdamWTensors, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,

@@ -711,19 +711,6 @@ norm_final_kernel(const double *__restrict__ partial, int32_t count, double max_
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
-int sm_count()
-{
-    static std::atomic<int> cache[64];
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-    n = cache[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        cache[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 bool at8(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % (size_t)(8 * bytes)) == 0; }
 unsigned grid_of(int64_t chunks, int per_sm)
 {
@@ -784,7 +771,8 @@ int step_kind(const tbn_adamw_tensor *tensors, int32_t count, const Hyper &h, co
         [&](const auto &tab, auto size) {
             auto kernel = step_kernel<decltype(size)::value, PT, GT, EIGHT>;
             const int smem = EIGHT ? kWarps * kStages * Ring<PT, GT>::kBytes : 0;
-            if (smem > 32 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return (int)TBN_ERR_CUDA;
+            static std::atomic<uint64_t> done;
+            if (smem > 0 && allow_smem(kernel, done) != cudaSuccess) return (int)TBN_ERR_CUDA;
             return launch_pdl(kernel, dim3(grid_of(tab.chunks, step_per_sm(EIGHT))), dim3(kThreads), smem, s, tab, host, h) == cudaSuccess
                        ? (int)TBN_OK : (int)TBN_ERR_CUDA;
         });

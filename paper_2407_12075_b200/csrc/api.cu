@@ -1020,7 +1020,8 @@ int tbn_layernorm_bwd(const void *dy, int dy_dtype, const void *x, int x_dtype, 
         return TBN_OK;
     }
     if (!dy || !x || !mean || !rstd || !dx) return TBN_ERR_INVALID_ARG;
-    if ((dgamma || dbeta) && (!workspace || workspace_bytes < norm::backward_workspace_bytes(T, d))) return TBN_ERR_WORKSPACE;
+    const size_t need = dgamma || dbeta ? norm::backward_workspace_bytes(T, d) : 0;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return TBN_ERR_WORKSPACE;
     norm::BackwardArgs a = {dy, x, dy_dtype, x_dtype, T, d, gamma, mean, rstd, dsum, dx, dgamma, dbeta};
     return norm::backward(a, workspace, s);
 }

@@ -6,8 +6,6 @@
 // id (stable, by digits of the id), equal pieces of the sorted list are summed by a warp each, 256 columns at a time, and where an
 // id's tokens go on over several pieces the pieces' sums are added in order by a kernel of their own.  No row of dy is read
 // twice, no atomic decides an order.
-#include <atomic>
-
 #include "embedding.cuh"
 #include "vec8.cuh"
 
@@ -17,19 +15,6 @@ namespace embed {
 namespace {
 
 constexpr int kThreads = 256;
-
-int sm_count()
-{
-    static std::atomic<int> cache[64];
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-    n = cache[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        cache[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
 
 __device__ __forceinline__ bool inside(int64_t id, int32_t V, int64_t padding) { return id >= 0 && id < V && id != padding; }
 

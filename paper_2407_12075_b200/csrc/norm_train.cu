@@ -458,9 +458,10 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
         get(slot == 0 ? R::kStages - 1 : slot - 1);                   // into the slot that was taken a row ago
         slot = slot + 1 == R::kStages ? 0 : slot + 1;
     }
-    if (!partial) return;
+    if (!a.dgamma && !a.dbeta) return;
     // the groups' sums, in their order; the rings are done with
-    float *columns = reinterpret_cast<float *>(rings), *out = partial + (int64_t)blockIdx.x * 2 * a.d;
+    float *columns = reinterpret_cast<float *>(rings);
+    float *out_g = gridDim.x == 1 ? a.dgamma : partial + (int64_t)blockIdx.x * 2 * a.d, *out_b = gridDim.x == 1 ? a.dbeta : out_g + a.d;
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
 #pragma unroll
@@ -476,7 +477,8 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
         const int32_t which = c >= a.d, at = which * room + l.shift + c - which * a.d;
         float t = columns[at];
         for (int k = 1; k < sh.groups; ++k) t += columns[k * 2 * room + at];
-        out[c] = t;
+        float *out = which ? out_b : out_g;
+        if (out) out[c - which * a.d] = t;
     }
 }
 
@@ -556,19 +558,6 @@ finish_kernel(const float *__restrict__ partial, int32_t parts, int32_t d, float
     }
 }
 
-int sm_count()
-{
-    static std::atomic<int> cache[64];
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-    n = cache[dev].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
-        cache[dev].store(n, std::memory_order_relaxed);
-    }
-    return n;
-}
-
 // `most`: pieces to a lane at most, from which on more warps share a row.  The fewest warps of those that leave the fewest lanes without
 // columns; four pieces in any case where eight warps need them.
 Shape shape_of(int32_t d, int most)
@@ -594,6 +583,9 @@ int64_t blocks_of(int64_t T, const Shape &s, int per_sm)
     const int64_t most = (int64_t)sm_count() * per_sm / s.classes, need = ((T + s.classes - 1) / s.classes + s.groups - 1) / s.groups;
     return (need < most ? need : most) * s.classes;
 }
+// The backward pass of a few rows is one thread block's, which writes the columns' sums itself: up to four rows of a group after one another
+// take less than a second kernel (16 x 512: 3.8 us against 5.7).
+bool one_block(int64_t T, const Shape &s) { return !s.lng && s.classes == 1 && T <= 4 * s.groups; }
 // Dynamic shared memory with which two thread blocks fit on an SM (228 KB, 1 KB of each block's is the system's).
 constexpr size_t kHalf = 113 * 1024;
 constexpr int kLongParts = 64;
@@ -607,11 +599,6 @@ template <typename F> cudaError_t with_shape(const Shape &s, F f)
 {
     return s.classes == 1 ? with_pieces(s.np, std::true_type{}, f) : with_pieces(s.np, std::false_type{}, f);
 }
-template <typename K> cudaError_t allow(K kernel, size_t smem)
-{
-    return smem > 32 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-}
-
 template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs &a, cudaStream_t s)
 {
     const Shape sh = shape_of(a.d, kMostForward);
@@ -626,7 +613,8 @@ template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs 
         constexpr bool EVEN = decltype(even)::value;
         typedef ForwardRing<XT, YT, NP> R;
         const size_t smem = (size_t)2 * sh.warps * NP * 256 * 4 + (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
-        const cudaError_t e = allow(forward_kernel<XT, YT, NP, EVEN>, smem);
+        static std::atomic<uint64_t> done;
+        const cudaError_t e = allow_smem(forward_kernel<XT, YT, NP, EVEN>, done);
         if (e != cudaSuccess) return e;
         return launch_pdl(forward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)blocks_of(a.T, sh, smem <= kHalf ? 2 : 1)), dim3(sh.groups * sh.warps * 32), smem, s, a, sh);
     });
@@ -657,13 +645,14 @@ template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArg
             const size_t room = (size_t)sh.warps * NP * 256 * 4, rings = (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
             const size_t sums_room = (size_t)sh.groups * 2 * room;    // the same space as the rings, which are larger
             const size_t smem = room + (rings > sums_room ? rings : sums_room);
-            const cudaError_t e1 = allow(backward_kernel<XT, YT, NP, EVEN>, smem);
+            static std::atomic<uint64_t> done;
+            const cudaError_t e1 = allow_smem(backward_kernel<XT, YT, NP, EVEN>, done);
             if (e1 != cudaSuccess) return e1;
-            parts = (int32_t)blocks_of(a.T, sh, NP < 4 && smem <= kHalf ? 2 : 1);
-            return launch_pdl(backward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)parts), dim3(sh.groups * sh.warps * 32), smem, s, a, sh, sums ? partial : nullptr);
+            parts = one_block(a.T, sh) ? 1 : (int32_t)blocks_of(a.T, sh, NP < 4 && smem <= kHalf ? 2 : 1);
+            return launch_pdl(backward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)parts), dim3(sh.groups * sh.warps * 32), smem, s, a, sh, partial);
         });
     }
-    if (e != cudaSuccess || !sums) return e;
+    if (e != cudaSuccess || !sums || (!sh.lng && parts == 1)) return e;            // one thread block has written them
     return launch_pdl(finish_kernel, dim3((unsigned)((2 * (int64_t)a.d + 31) / 32)), dim3(1024), 0, s, static_cast<const float *>(partial), parts,
                       a.d, a.dgamma, a.dbeta);
 }
@@ -673,6 +662,7 @@ template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArg
 size_t backward_workspace_bytes(int64_t T, int32_t d)
 {
     const Shape sh = shape_of(d, kMostBackward);
+    if (one_block(T, sh)) return 0;
     const int64_t parts = sh.lng ? (T < kLongParts ? T : kLongParts) : blocks_of(T, sh, 2);        // at most
     return (size_t)parts * 2 * (size_t)d * 4;
 }

@@ -1,6 +1,8 @@
 // Eight consecutive fp32 or bf16 values of a lane: one 32-byte or 16-byte access (a warp's request covers whole lines).
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace tbn {
@@ -88,6 +90,34 @@ __device__ __forceinline__ void spread8(const Pair (&v)[4], float (&f)[8])
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) f32x2_unpack(v[e].r, f[2 * e], f[2 * e + 1]);
+}
+
+// Lets a kernel have the largest dynamic shared memory, once for each device.  `done`: the kernel's own, one bit for a device.
+template <typename K> cudaError_t allow_smem(K kernel, std::atomic<uint64_t> &done)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = (uint64_t)1 << (dev & 63);
+    if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    cudaFuncAttributes at;
+    e = cudaFuncGetAttributes(&at, kernel);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - (int)at.sharedSizeBytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+// Multiprocessors of the current device.
+inline int sm_count()
+{
+    static std::atomic<int> cache[64];
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    n = cache[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 148;
+        cache[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
 }
 
 __device__ __forceinline__ float value_of(float v) { return v; }

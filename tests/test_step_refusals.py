@@ -43,11 +43,11 @@ def test_layernorm(lib):
     refused(lib.tbn_layernorm_train_fwd, args, [(0, None, -1), (0, P + 2, -1), (1, P + 2, -1), (2, 2, -1), (3, -1, -1), (3, 1 << 31, -3), (4, 0, -1),
                                                 (4, 1 << 24, -3), (5, P + 1, -1), (6, P + 2, -1), (7, -1.0, -1), (7, NAN, -1), (8, None, -1),
                                                 (8, P + 8, -1), (9, None, -1), (10, 2, -1), (11, P + 2, -1), (12, P + 1, -1)])
-    args = [P, B.BF16, P, B.BF16, 4, 64, P, P, P, P, P, P, P, P, 1 << 30, None]
+    args = [P, B.BF16, P, B.BF16, 400, 64, P, P, P, P, P, P, P, P, 1 << 30, None]
     refused(lib.tbn_layernorm_bwd, args, [(0, None, -1), (0, P + 2, -1), (1, 2, -1), (2, None, -1), (3, 9, -1), (4, -1, -1), (4, 1 << 31, -3), (5, 0, -1),
                                           (6, P + 2, -1), (7, None, -1), (8, None, -1), (9, P + 4, -1), (10, None, -1), (11, P + 1, -1), (12, P + 2, -1),
                                           (13, None, -4), (13, P + 4, -1), (14, 64, -4)])
-    assert lib.tbn_layernorm_bwd_workspace_bytes(4, 64) > 0 and lib.tbn_layernorm_bwd_workspace_bytes(0, 64) == 0
+    assert lib.tbn_layernorm_bwd_workspace_bytes(400, 64) > 0 and lib.tbn_layernorm_bwd_workspace_bytes(0, 64) == 0
 
 
 def tensor(**changes):
