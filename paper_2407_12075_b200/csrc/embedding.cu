@@ -18,78 +18,178 @@ constexpr int kThreads = 256;
 
 __device__ __forceinline__ bool inside(int64_t id, int32_t V, int64_t padding) { return id >= 0 && id < V && id != padding; }
 
-// Columns of a lane within 256 of a row: eight in a row (VEC) or every 32nd.
-template <bool VEC, typename T> __device__ __forceinline__ void load_cols(const T *row, int32_t c0, int32_t d, float (&v)[8])
+// Eight values in a row from any element on.  At odd places they are cut out of the two or three aligned pieces that hold them, unless
+// one of those reaches behind `end`, the tensor's.
+__device__ __forceinline__ void load_any(const __nv_bfloat16 *p, const __nv_bfloat16 *end, bool aligned, Raw8<__nv_bfloat16> &r)
 {
-    const int lane = threadIdx.x & 31;
-    if (VEC) {
-        if (c0 + lane * 8 < d) { unpack8(load8(row + c0 + lane * 8), v); return; }
+    if (aligned) { r = load8(p); return; }
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / 2;        // 0 .. 7
+    const __nv_bfloat16 *q = p - off;
+    if (q + 16 > end) {
+        uint32_t h[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-    } else {
+        for (int e = 0; e < 8; ++e) h[e] = __bfloat16_as_ushort(p[e]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c0 + lane + 32 * e < d ? value_of(row[c0 + lane + 32 * e]) : 0.0f;
+        for (int e = 0; e < 4; ++e) r.w[e] = h[2 * e] | h[2 * e + 1] << 16;
+        return;
     }
+    const Raw8<__nv_bfloat16> a = load8(q), b = load8(q + 8);
+    uint32_t w[6] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1]}, x[5];
+    const bool two = off & 4, one = off & 2;                          // words to leave out, in two steps: 2, then 1
+    const uint32_t v[7] = {two ? w[2] : w[0], two ? w[3] : w[1], two ? w[4] : w[2], two ? w[5] : w[3], two ? b.w[2] : w[4], two ? b.w[3] : w[5], 0};
+#pragma unroll
+    for (int e = 0; e < 5; ++e) x[e] = one ? v[e + 1] : v[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r.w[e] = off & 1 ? __funnelshift_r(x[e], x[e + 1], 16) : x[e];
 }
-template <bool VEC, typename T> __device__ __forceinline__ void store_cols(T *row, int32_t c0, int32_t d, const float (&v)[8])
+__device__ __forceinline__ void load_any(const float *p, const float *end, bool aligned, Raw8<float> &r)
 {
-    const int lane = threadIdx.x & 31;
-    if (VEC) {
-        if (c0 + lane * 8 < d) store8(row + c0 + lane * 8, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) if (c0 + lane + 32 * e < d) store_from_float(row, c0 + lane + 32 * e, v[e]);
+    if (aligned) {
+        const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
+        return;
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.w[e] = __float_as_uint(p[e]);
+}
+__device__ __forceinline__ void store_row(float *p, const float (&v)[8])          // 16-byte aligned
+{
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[8]) { store8(p, v); }
+template <typename T> __device__ __forceinline__ Raw8<T> zero8()
+{
+    Raw8<T> r;
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(r.w) / 4); ++e) r.w[e] = 0;
+    return r;
 }
 
-// A warp takes 256 columns of one token.
-template <typename WT, typename YT, bool VEC>
+// The eight columns from c on of row `row` of a table, scaled; what is behind column d is left as it is in v.
+template <typename WT> struct DenseRows {
+    const WT *table, *end;
+    int32_t d;
+    bool even;
+    float scale;
+    struct Row { const WT *at; };
+    __device__ __forceinline__ Row row(int64_t id) const { return {table + id * d}; }
+    typedef Raw8<WT> Piece;
+    __device__ __forceinline__ void load(const Row &r, int32_t c, Piece &p) const { load_any(r.at + c, end, even, p); }
+    __device__ __forceinline__ void values(const Row &, int32_t, const Piece &p, float (&v)[8]) const
+    {
+        unpack8(p, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= scale;
+    }
+    __device__ __forceinline__ float one(const Row &r, int32_t c) const { return value_of(r.at[c]) * scale; }
+};
+// The same from a tiled table: bit (f mod q) and scaling factor (f / q) of element f = id d + c.
+struct TiledRows {
+    const uint32_t *tile;
+    const float *alpha;
+    int64_t q, words;                       // words that the tile occupies
+    int32_t d, rows;                        // rows of the table that a tile spans, 0 if it ends inside of one
+    int per_tile;
+    float scale;
+    struct Row { int64_t i; int32_t j; };   // the row's first bit and factor
+    __device__ __forceinline__ Row row(int64_t id) const
+    {
+        if (rows > 0) { const int32_t j = (int32_t)id / rows; return {(int64_t)((int32_t)id - j * rows) * d, j}; }
+        const int64_t f = id * d, j = f / q;
+        return {f - j * q, (int32_t)j};
+    }
+    struct Piece { uint32_t bits; float a; };
+    __device__ __forceinline__ void place(const Row &r, int32_t c, int64_t &i, int64_t &j) const
+    {
+        i = r.i + c; j = r.j;
+        if (i >= q) { const int64_t more = i / q; j += more; i -= more * q; }
+    }
+    __device__ __forceinline__ void load(const Row &r, int32_t c, Piece &p) const
+    {
+        int64_t i, j;
+        place(r, c, i, j);
+        p.a = i + 8 <= q ? __ldg(alpha + (per_tile ? j : 0)) * scale : -1.0f;         // -1: the piece goes over a tile's end
+        const int64_t w = i >> 5;
+        const uint32_t lo = __ldg(tile + w), hi = (i & 31) > 24 && w + 1 < words ? __ldg(tile + w + 1) : 0;
+        p.bits = __funnelshift_r(lo, hi, (uint32_t)(i & 31));
+    }
+    __device__ __forceinline__ void values(const Row &r, int32_t c, const Piece &p, float (&v)[8]) const
+    {
+        if (p.a == -1.0f) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (c + e < d) v[e] = one(r, c + e);
+            return;
+        }
+        const uint32_t a = __float_as_uint(p.a);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(a ^ (~(p.bits << (31 - e)) & 0x80000000u));
+    }
+    __device__ __forceinline__ float one(const Row &r, int32_t c) const
+    {
+        int64_t i, j;
+        place(r, c, i, j);
+        const float a = __ldg(alpha + (per_tile ? j : 0)) * scale;
+        return tile_bit(tile, i) ? a : -a;
+    }
+};
+
+// A warp takes up to 1024 columns of one token, which it loads before it stores any: d is a multiple of eight.
+template <typename ROWS, typename YT>
 __global__ void __launch_bounds__(kThreads)
-lookup_kernel(const LookupArgs a, int32_t segs)
+lookup_kernel(const LookupArgs a, const ROWS rows, int32_t segs)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t warps = (int64_t)gridDim.x * (kThreads / 32), total = a.T * segs;
-    for (int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); w < total; w += warps) {
-        const int64_t t = w / segs;
-        const int32_t c0 = (int32_t)(w - t * segs) * 256;
-        const int64_t id = a.ids[t];
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (inside(id, a.V, a.padding)) {
-            load_cols<VEC>(static_cast<const WT *>(a.table) + id * a.d, c0, a.d, v);
+    const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const int64_t t = segs == 1 ? w : w / segs;
+    if (t >= a.T) return;
+    const int32_t c0 = (int32_t)(w - t * segs) * 1024 + (threadIdx.x & 31) * 8;
+    const int64_t id = a.ids[t];
+    const bool in = inside(id, a.V, a.padding);
+    YT *y = static_cast<YT *>(a.y) + t * a.d;
+    const typename ROWS::Row row = rows.row(in ? id : 0);
+    typename ROWS::Piece p[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-        }
-        store_cols<VEC>(static_cast<YT *>(a.y) + t * a.d, c0, a.d, v);
+    for (int i = 0; i < 4; ++i)
+        if (in && c0 + i * 256 < a.d) rows.load(row, c0 + i * 256, p[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (c0 + i * 256 >= a.d) break;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (in) rows.values(row, c0 + i * 256, p[i], v);
+        store_row(y + c0 + i * 256, v);
     }
 }
 
-template <typename YT, bool VEC>
+// Other rows: y as one array, an aligned piece of eight to a thread; pieces that lie in two rows or more go value by value.
+template <typename ROWS, typename YT>
 __global__ void __launch_bounds__(kThreads)
-lookup_tiled_kernel(const LookupArgs a, int32_t segs)
+lookup_odd_kernel(const LookupArgs a, const ROWS rows)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (kThreads / 32), total = a.T * segs;
-    for (int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); w < total; w += warps) {
-        const int64_t t = w / segs;
-        const int32_t c0 = (int32_t)(w - t * segs) * 256;
+    const int64_t o = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8, total = a.T * a.d;
+    if (o >= total) return;
+    YT *y = static_cast<YT *>(a.y);
+    int64_t t = total <= 0x7fffffff ? (int64_t)((uint32_t)o / (uint32_t)a.d) : o / a.d;
+    int32_t c = (int32_t)(o - t * a.d);
+    if (c + 8 <= a.d) {
         const int64_t id = a.ids[t];
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (inside(id, a.V, a.padding)) {
-            const int64_t f0 = id * a.d + c0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int32_t c = VEC ? lane * 8 + e : lane + 32 * e;
-                if (c0 + c < a.d) {
-                    const int64_t f = f0 + c, j = f / a.q, i = f - j * a.q;
-                    const float al = __ldg(a.alpha + (a.per_tile ? j : 0)) * a.scale;
-                    v[e] = tile_bit(a.tile, i) ? al : -al;
-                }
-            }
+            const typename ROWS::Row row = rows.row(id);
+            typename ROWS::Piece p;
+            rows.load(row, c, p);
+            rows.values(row, c, p, v);
         }
-        store_cols<VEC>(static_cast<YT *>(a.y) + t * a.d, c0, a.d, v);
+        store_row(y + o, v);
+        return;
+    }
+    for (int e = 0; e < 8 && o + e < total; ++e) {
+        const int64_t id = a.ids[t];
+        store_from_float(y, o + e, inside(id, a.V, a.padding) ? rows.one(rows.row(id), c) : 0.0f);
+        if (++c == a.d) { c = 0; ++t; }
     }
 }
 
@@ -123,13 +223,13 @@ __device__ __forceinline__ uint32_t key_of(const Sort &s, int64_t t)
     const int64_t id = s.ids[t];
     return inside(id, s.V, s.padding) ? (uint32_t)id : (uint32_t)s.V;           // what is outside goes to the end
 }
-__device__ __forceinline__ void fill(const Fill &f, unsigned block, unsigned blocks)
+template <int THREADS> __device__ __forceinline__ void fill(const Fill &f, unsigned block, unsigned blocks)
 {
     const int64_t whole = f.bytes / 16;
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    for (int64_t i = (int64_t)block * kThreads + threadIdx.x; i < whole; i += (int64_t)blocks * kThreads) reinterpret_cast<uint4 *>(f.to)[i] = zero;
+    for (int64_t i = (int64_t)block * THREADS + threadIdx.x; i < whole; i += (int64_t)blocks * THREADS) reinterpret_cast<uint4 *>(f.to)[i] = zero;
     if (block == 0)
-        for (int64_t i = whole * 8 + threadIdx.x; i < f.bytes / 2; i += kThreads) reinterpret_cast<uint16_t *>(f.to)[i] = 0;
+        for (int64_t i = whole * 8 + threadIdx.x; i < f.bytes / 2; i += THREADS) reinterpret_cast<uint16_t *>(f.to)[i] = 0;
 }
 
 __global__ void __launch_bounds__(kThreads)
@@ -138,7 +238,7 @@ count_kernel(const Sort s, const Fill f)
     __shared__ uint32_t bin[kMaxBins];
     pdl_launch_dependents();
     pdl_wait();
-    if (blockIdx.x >= (unsigned)s.parts) { fill(f, blockIdx.x - s.parts, gridDim.x - s.parts); return; }
+    if (blockIdx.x >= (unsigned)s.parts) { fill<kThreads>(f, blockIdx.x - s.parts, gridDim.x - s.parts); return; }
     const int bins = 1 << s.bits;
     for (int b = threadIdx.x; b < bins; b += kThreads) bin[b] = 0;
     __syncthreads();
@@ -160,7 +260,7 @@ place_kernel(const Sort s, int32_t pass, const Fill f)
     __shared__ uint32_t warp_total[kSortWarps];
     pdl_launch_dependents();
     pdl_wait();
-    if (blockIdx.x >= (unsigned)s.parts) { fill(f, blockIdx.x - s.parts, gridDim.x - s.parts); return; }
+    if (blockIdx.x >= (unsigned)s.parts) { fill<kThreads>(f, blockIdx.x - s.parts, gridDim.x - s.parts); return; }
     const int bins = 1 << s.bits, shift = pass * s.bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t *count = s.count[pass & 1];
     uint32_t *next = s.count[(pass + 1) & 1];
@@ -244,22 +344,142 @@ clear_kernel(uint32_t *__restrict__ count, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) count[i] = 0;
 }
 
+// Up to 8192 tokens are sorted by one thread block, in registers and shared memory: a warp takes a stretch of the list, eight tokens to a lane
+// at most, finds each token's place among the warp's of its digit as it goes, and after the sums over warps and digits every
+// token goes to its place in a list that the next pass reads.  One launch instead of three, of which each waits for the one before.
+constexpr int kOneThreads = 1024, kOneWarps = kOneThreads / 32, kOneTokens = 8192, kOneBins = 256;
+struct OneSmem {
+    uint2 list[kOneTokens];
+    uint32_t seen[kOneWarps][kOneBins];     // tokens of a digit in the warps before, then where the warp's first one goes
+    uint32_t base[kOneBins];
+};
+__global__ void __launch_bounds__(kOneThreads)
+sort_kernel(const Sort s, const Fill f)
+{
+    extern __shared__ __align__(16) char raw[];
+    OneSmem &m = *reinterpret_cast<OneSmem *>(raw);
+    pdl_launch_dependents();
+    pdl_wait();
+    if (blockIdx.x > 0) { fill<kOneThreads>(f, blockIdx.x - 1, gridDim.x - 1); return; }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = 1 << s.bits;
+    const int T = (int)s.T, rounds = (T + kOneThreads - 1) / kOneThreads, first = warp * rounds * 32 + lane;
+    uint2 item[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (r < rounds && first + r * 32 < T) item[r] = make_uint2(key_of(s, first + r * 32), (uint32_t)(first + r * 32));
+    for (int pass = 0; pass < s.passes; ++pass) {
+        const int shift = pass * s.bits;
+        for (int b = threadIdx.x; b < kOneWarps * bins; b += kOneThreads) m.seen[b >> s.bits][b & (bins - 1)] = 0;
+        __syncthreads();
+        uint32_t before[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            if (r >= rounds) break;
+            const bool here = first + r * 32 < T;
+            const uint32_t digit = here ? (item[r].x >> shift) & (uint32_t)(bins - 1) : 0xffffffffu;
+            const uint32_t same = __match_any_sync(0xffffffffu, digit), rank = __popc(same & ((1u << lane) - 1u));
+            uint32_t c = 0;
+            if (here) c = m.seen[warp][digit];
+            before[r] = c + rank;
+            __syncwarp();
+            if (here && rank == 0) m.seen[warp][digit] = c + __popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        {                                                             // four threads to a digit, eight warps to each
+            const int b = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+            uint32_t c[8], sum = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { c[k] = b < bins ? m.seen[quarter * 8 + k][b] : 0; sum += c[k]; }
+            uint32_t run = sum;
+            uint32_t o = __shfl_up_sync(0xffffffffu, run, 1, 4);
+            if (quarter >= 1) run += o;
+            o = __shfl_up_sync(0xffffffffu, run, 2, 4);
+            if (quarter >= 2) run += o;
+            if (quarter == 3) m.base[b] = run;
+            __syncthreads();
+            if (warp == 0) {
+                uint32_t t[kOneBins / 32], all = 0;
+#pragma unroll
+                for (int k = 0; k < kOneBins / 32; ++k) { t[k] = all; all += m.base[lane * (kOneBins / 32) + k]; }
+                uint32_t up = all;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const uint32_t x = __shfl_up_sync(0xffffffffu, up, off);
+                    if (lane >= off) up += x;
+                }
+#pragma unroll
+                for (int k = 0; k < kOneBins / 32; ++k) m.base[lane * (kOneBins / 32) + k] = t[k] + up - all;
+            }
+            __syncthreads();
+            uint32_t at = m.base[b] + run - sum;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (b < bins) { m.seen[quarter * 8 + k][b] = at; at += c[k]; }
+        }
+        __syncthreads();
+        const bool last = pass + 1 == s.passes;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < rounds && first + r * 32 < T) {
+                uint2 *to = last ? s.list[0] : m.list;
+                to[m.seen[warp][(item[r].x >> shift) & (uint32_t)(bins - 1)] + before[r]] = item[r];
+            }
+        if (last) return;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < rounds && first + r * 32 < T) item[r] = m.list[first + r * 32];
+    }
+}
+
 // ---- sums -------------------------------------------------------------------------------------------------------------------
+// A lane's eight columns of a row of dw (from column c on), added to and written; rows are aligned where EVEN.
+template <bool EVEN, typename WT> __device__ __forceinline__ void write_sum(WT *row, int32_t c, int32_t d, const float (&acc)[8], float scale, int add)
+{
+    if (c >= d) return;
+    float o[8];
+    if (EVEN) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
+        if (add) {
+            Raw8<WT> r;
+            load_any(row + c, row + d, true, r);
+            unpack8(r, o);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(scale, acc[e], o[e]);
+        store_row(row + c, o);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (c + e >= d) break;
+            store_from_float(row, c + e, fmaf(scale, acc[e], add ? value_of(row[c + e]) : 0.0f));
+        }
+    }
+}
+// Sums of pieces lie in rows of `pitch` floats (a multiple of eight).
+__device__ __forceinline__ void put_partial(float *row, int32_t c, const float (&acc)[8]) { store_row(row + c, acc); }
+
 // A warp takes one piece of the sorted list and 256 columns.  An id's tokens that begin and end in the piece are done with; what
-// comes from the piece before, or goes on in the next one, is written to `partial` ([piece][2][d]: first, last).
-template <typename GT, typename WT, bool VEC>
+// comes from the piece before, or goes on in the next one, is written to `partial` ([piece][2][pitch]: first, last).
+constexpr int kAhead = 8;                   // rows loaded before the first is added
+template <typename GT, typename WT, bool EVEN>
 __global__ void __launch_bounds__(kThreads)
 sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, int32_t segs, float scale,
-           const GT *__restrict__ dy, WT *__restrict__ dw, int add, float *__restrict__ partial)
+           const GT *__restrict__ dy, WT *__restrict__ dw, int add, float *__restrict__ partial, int32_t pitch)
 {
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
     const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    const int64_t c = w / segs;
-    if (c >= pieces) return;
-    const int32_t c0 = (int32_t)(w - c * segs) * 256;
-    const int64_t a = c * piece, b = a + piece < T ? a + piece : T;
+    const int64_t k = segs == 1 ? w : w / segs;
+    if (k >= pieces) return;
+    const int32_t c = (int32_t)(w - k * segs) * 256 + lane * 8;
+    const int64_t a = k * piece, b = a + piece < T ? a + piece : T;
+    const GT *end = dy + T * d;
+    uint2 item = make_uint2(0xffffffffu, 0);
+    if (a + lane < b) item = list[a + lane];
     const uint32_t left = a > 0 ? list[a - 1].x : 0xffffffffu, right = b < T ? list[b].x : 0xffffffffu;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     uint32_t cur = 0xffffffffu;
@@ -267,29 +487,43 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
     auto put = [&](bool to_right) {
         if (cur >= (uint32_t)V) return;
         if (from_left || to_right) {
-            store_cols<VEC>(partial + (c * 2 + (from_left ? 0 : 1)) * d, c0, d, acc);
-            return;
+            if (c < d) put_partial(partial + (k * 2 + (from_left ? 0 : 1)) * pitch, c, acc);
+        } else {
+            write_sum<EVEN>(dw + (int64_t)cur * d, c, d, acc, scale, add);
         }
-        WT *row = dw + (int64_t)cur * d;
-        float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (add) load_cols<VEC>(row, c0, d, o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(scale, acc[e], o[e]);
-        store_cols<VEC>(row, c0, d, o);
     };
     for (int64_t p0 = a; p0 < b; p0 += 32) {
-        uint2 item = make_uint2(0xffffffffu, 0);
-        if (p0 + lane < b) item = list[p0 + lane];
+        if (p0 > a) {
+            item = make_uint2(0xffffffffu, 0);
+            if (p0 + lane < b) item = list[p0 + lane];
+        }
         const int n = (int)(b - p0 < 32 ? b - p0 : 32);
-        for (int i0 = 0; i0 < n; i0 += 8) {
-            float v[8][8];
+        for (int i0 = 0; i0 < n; i0 += kAhead) {
+            Raw8<GT> r[kAhead];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kAhead; ++i) {
                 const uint32_t key = __shfl_sync(0xffffffffu, item.x, i0 + i), tok = __shfl_sync(0xffffffffu, item.y, i0 + i);
-                if (i0 + i < n && key < (uint32_t)V) load_cols<VEC>(dy + (int64_t)tok * d, c0, d, v[i]);
+                r[i] = zero8<GT>();
+                if (key < (uint32_t)V && c < d) {                     // beyond the piece: a key of 2^32 - 1
+                    const GT *row = dy + (int64_t)tok * d;
+                    if (EVEN || c + 8 <= d) {
+                        load_any(row + c, end, EVEN, r[i]);
+                    } else {
+                        uint32_t h[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) h[e] = c + e < d ? __float_as_uint(value_of(row[c + e])) : 0u;
+                        if (sizeof(GT) == 4) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) r[i].w[e % (int)(sizeof(r[i].w) / 4)] = h[e];
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) r[i].w[e] = h[2 * e] >> 16 | (h[2 * e + 1] & 0xffff0000u);
+                        }
+                    }
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kAhead; ++i) {
                 if (i0 + i >= n) break;
                 const uint32_t key = __shfl_sync(0xffffffffu, item.x, i0 + i);
                 if (key != cur) {
@@ -299,10 +533,10 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
 #pragma unroll
                     for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
                 }
-                if (key < (uint32_t)V) {
+                float v[8];
+                unpack8(r[i], v);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[e] += v[i][e];
-                }
+                for (int e = 0; e < 8; ++e) acc[e] += v[e];
             }
         }
     }
@@ -312,10 +546,10 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
 // The ids whose tokens lie in several pieces.  A warp looks at one piece: does its last id begin in it and go on?  Short runs it
 // adds up by itself, long ones are shared by the block's warps.
 constexpr int kAlone = 16;
-template <typename WT, bool VEC>
+template <typename WT, bool EVEN>
 __global__ void __launch_bounds__(kThreads)
 join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, float scale, WT *__restrict__ dw, int add,
-            const float *__restrict__ partial)
+            const float *__restrict__ partial, int32_t pitch)
 {
     constexpr int kWarps = kThreads / 32;
     __shared__ int64_t more[kWarps];                                  // pieces after the warp's own that the run covers
@@ -324,69 +558,66 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * kWarps + warp;
-    const int32_t c0 = blockIdx.y * 256;
+    const int64_t k = (int64_t)blockIdx.x * kWarps + warp;
+    const int32_t c = blockIdx.y * 256 + lane * 8;
     int64_t n = 0;
     uint32_t key = 0xffffffffu;
-    if (c + 1 < pieces) {
-        const int64_t a = c * piece, b = a + piece;                   // b < T: another piece follows
+    if (k + 1 < pieces) {
+        const int64_t a = k * piece, b = a + piece;                   // b < T: another piece follows
+        const uint32_t first = list[a].x, next = list[b].x, before = a > 0 ? list[a - 1].x : 0xffffffffu;
+        const int64_t o1 = k + 2 + lane;                              // the pieces after the next one, of which it is the first id
+        const uint32_t ahead = o1 < pieces ? list[o1 * piece].x : 0xffffffffu;
         key = list[b - 1].x;
-        const bool begins = a == 0 || list[a].x != key || list[a - 1].x != key;
-        if (key < (uint32_t)V && begins && list[b].x == key) {
-            for (n = 1;; n += 32) {                                   // the pieces after the next one whose first id it is
-                const int64_t o = c + 1 + n + lane;
-                const bool on = o < pieces && list[o * piece].x == key;
-                const uint32_t off = __ballot_sync(0xffffffffu, !on);
-                if (off) { n += __ffs(off) - 1; break; }
+        if (key < (uint32_t)V && next == key && (first != key || before != key)) {
+            uint32_t off = __ballot_sync(0xffffffffu, ahead != key);
+            n = 1;
+            while (off == 0) {
+                n += 32;
+                const int64_t o = k + 1 + n + lane;
+                off = __ballot_sync(0xffffffffu, !(o < pieces && list[o * piece].x == key));
             }
+            n += __ffs(off) - 1;
         }
     }
     auto add_up = [&](int64_t from, int64_t lo, int64_t hi, float (&acc)[8]) {          // partials lo .. hi of the run of piece `from`
+        if (c >= d) return;
         int64_t i = lo;
         for (; i + 4 <= hi; i += 4) {
-            float v[4][8];
+            Raw8<float> r[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) load_cols<VEC>(partial + ((from + i + j) * 2 + (i + j == 0 ? 1 : 0)) * d, c0, d, v[j]);
+            for (int j = 0; j < 4; ++j) load_any(partial + ((from + i + j) * 2 + (i + j == 0 ? 1 : 0)) * pitch + c, partial, true, r[j]);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += v[j][e];
+                for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(r[j].w[e]);
         }
         for (; i < hi; ++i) {
-            float v[8];
-            load_cols<VEC>(partial + ((from + i) * 2 + (i == 0 ? 1 : 0)) * d, c0, d, v);
+            Raw8<float> r;
+            load_any(partial + ((from + i) * 2 + (i == 0 ? 1 : 0)) * pitch + c, partial, true, r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] += v[e];
+            for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(r.w[e]);
         }
-    };
-    auto finish = [&](uint32_t id, const float (&acc)[8]) {
-        WT *row = dw + (int64_t)id * d;
-        float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (add) load_cols<VEC>(row, c0, d, o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(scale, acc[e], o[e]);
-        store_cols<VEC>(row, c0, d, o);
     };
     if (n > 0 && n <= kAlone) {
         float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        add_up(c, 0, n + 1, acc);
-        finish(key, acc);
+        add_up(k, 0, n + 1, acc);
+        write_sum<EVEN>(dw + (int64_t)key * d, c, d, acc, scale, add);
     }
     if (lane == 0) { more[warp] = n > kAlone ? n : 0; key_at[warp] = key; }
     __syncthreads();
-    for (int k = 0; k < kWarps; ++k) {
-        const int64_t len = more[k] + 1;                              // the same for the whole block
+    for (int j = 0; j < kWarps; ++j) {
+        const int64_t len = more[j] + 1;                              // the same for the whole block
         if (len == 1) continue;
         float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        add_up((int64_t)blockIdx.x * kWarps + k, len * warp / kWarps, len * (warp + 1) / kWarps, acc);
+        add_up((int64_t)blockIdx.x * kWarps + j, len * warp / kWarps, len * (warp + 1) / kWarps, acc);
 #pragma unroll
         for (int e = 0; e < 8; ++e) red[warp][e * 32 + lane] = acc[e];
         __syncthreads();
         if (warp == 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                for (int j = 1; j < kWarps; ++j) acc[e] += red[j][e * 32 + lane];
-            finish(key_at[k], acc);
+                for (int i = 1; i < kWarps; ++i) acc[e] += red[i][e * 32 + lane];
+            write_sum<EVEN>(dw + (int64_t)key_at[j] * d, c, d, acc, scale, add);
         }
         __syncthreads();
     }
@@ -397,14 +628,15 @@ zero_kernel(const Fill f)
 {
     pdl_launch_dependents();
     pdl_wait();
-    fill(f, blockIdx.x, gridDim.x);
+    fill<kThreads>(f, blockIdx.x, gridDim.x);
 }
 
 // ---- host side ----------------------------------------------------------------------------------------------------------------
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct Plan {
-    int32_t part, parts, bits, passes, piece;
+    int32_t part, parts, bits, passes, piece, pitch;
+    bool one;                               // sorted by one thread block
     int64_t pieces;
     size_t o_list[2], o_count[2], o_partial, total;
 };
@@ -413,7 +645,9 @@ Plan make_plan(int64_t T, int32_t d, int32_t V)
     Plan p = {};
     int32_t need = 1;
     while (((int64_t)V >> need) != 0) ++need;                         // bits of V, the key of what is outside
-    p.passes = (need + 9) / 10;
+    p.one = T <= kOneTokens;
+    const int32_t most_bits = p.one ? 8 : 10;
+    p.passes = (need + most_bits - 1) / most_bits;
     p.bits = (need + p.passes - 1) / p.passes;
     // parts of 1024 tokens: four rounds of a block's warps; more when the blocks' sums over all parts' counts would grow
     int64_t part = 1024;
@@ -423,40 +657,54 @@ Plan make_plan(int64_t T, int32_t d, int32_t V)
     p.parts = (int32_t)((T + part - 1) / part);
     p.piece = T <= 4096 ? 8 : T <= 32768 ? 16 : T <= 131072 ? 32 : 64;
     p.pieces = (T + p.piece - 1) / p.piece;
+    p.pitch = (d + 7) / 8 * 8;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += round_up(bytes, 256); return at; };
-    for (int i = 0; i < 2; ++i) p.o_list[i] = take((size_t)T * sizeof(uint2));
-    for (int i = 0; i < 2; ++i) p.o_count[i] = take((size_t)p.parts << (p.bits + 2));
-    p.o_partial = take((size_t)p.pieces * 2 * d * 4);
+    p.o_list[0] = take((size_t)T * sizeof(uint2));
+    if (!p.one) {
+        p.o_list[1] = take((size_t)T * sizeof(uint2));
+        for (int i = 0; i < 2; ++i) p.o_count[i] = take((size_t)p.parts << (p.bits + 2));
+    }
+    p.o_partial = take(p.pieces > 1 ? (size_t)p.pieces * 2 * p.pitch * 4 : 0);
     p.total = o;
     return p;
 }
 
+template <typename ROWS, typename YT> cudaError_t lookup_rows(const LookupArgs &a, const ROWS &rows, cudaStream_t s)
+{
+    if (a.d % 8 == 0) {
+        const int32_t segs = (a.d + 1023) / 1024;
+        const int64_t blocks = (a.T * segs + kThreads / 32 - 1) / (kThreads / 32);
+        if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+        return launch_pdl(lookup_kernel<ROWS, YT>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, rows, segs);
+    }
+    const int64_t blocks = (a.T * a.d + kThreads * 8 - 1) / (kThreads * 8);
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_pdl(lookup_odd_kernel<ROWS, YT>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, rows);
+}
 template <typename WT, typename YT> cudaError_t lookup_typed(const LookupArgs &a, cudaStream_t s)
 {
-    const int32_t segs = (a.d + 255) / 256;
-    const int64_t blocks = (a.T * segs + kThreads / 32 - 1) / (kThreads / 32), most = (int64_t)1 << 30;
-    const dim3 grid((unsigned)(blocks < most ? blocks : most));
     if (a.table) {
-        const bool vec = aligned8<WT>(a.table, a.d) && aligned8<YT>(a.y);
-        return launch_pdl(vec ? lookup_kernel<WT, YT, true> : lookup_kernel<WT, YT, false>, grid, dim3(kThreads), 0, s, a, segs);
+        const WT *table = static_cast<const WT *>(a.table);
+        return lookup_rows<DenseRows<WT>, YT>(a, DenseRows<WT>{table, table + (int64_t)a.V * a.d, a.d, a.d % 8 == 0, a.scale}, s);
     }
-    const bool vec = aligned8<YT>(a.y, a.d);
-    return launch_pdl(vec ? lookup_tiled_kernel<YT, true> : lookup_tiled_kernel<YT, false>, grid, dim3(kThreads), 0, s, a, segs);
+    const int32_t rows = a.q % a.d == 0 ? (int32_t)(a.q / a.d) : 0;
+    return lookup_rows<TiledRows, YT>(a, TiledRows{a.tile, a.alpha, a.q, (a.q + 31) / 32, a.d, rows, a.per_tile, a.scale}, s);
 }
 
 template <typename GT, typename WT> cudaError_t sums_typed(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
 {
     const int32_t segs = (a.d + 255) / 256;
-    const bool vec = aligned8<GT>(a.dy, a.d) && aligned8<WT>(a.dw) && aligned8<float>(partial);
+    const bool even = a.d % 8 == 0;
     const GT *dy = static_cast<const GT *>(a.dy);
     WT *dw = static_cast<WT *>(a.dw);
     const int64_t blocks = (p.pieces * segs + kThreads / 32 - 1) / (kThreads / 32);
-    cudaError_t e = launch_pdl(vec ? sum_kernel<GT, WT, true> : sum_kernel<GT, WT, false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V,
-                               a.d, p.piece, p.pieces, segs, a.scale, dy, dw, a.add, partial);
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    cudaError_t e = launch_pdl(even ? sum_kernel<GT, WT, true> : sum_kernel<GT, WT, false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V,
+                               a.d, p.piece, p.pieces, segs, a.scale, dy, dw, a.add, partial, p.pitch);
     if (e != cudaSuccess || p.pieces == 1) return e;
-    return launch_pdl(vec ? join_kernel<WT, true> : join_kernel<WT, false>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs),
-                      dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, a.scale, dw, a.add, static_cast<const float *>(partial));
+    return launch_pdl(even ? join_kernel<WT, true> : join_kernel<WT, false>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs),
+                      dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, a.scale, dw, a.add, static_cast<const float *>(partial), p.pitch);
 }
 
 }  // namespace
@@ -487,22 +735,32 @@ int gradient(const GradArgs &a, void *workspace, cudaStream_t s)
         so.list[i] = reinterpret_cast<uint2 *>(ws + p.o_list[i]);
         so.count[i] = reinterpret_cast<uint32_t *>(ws + p.o_count[i]);
     }
-    // the zeros, in as many equal stretches as the sort has launches
-    const int launches = p.passes + 1;
-    const int64_t share = a.add ? 0 : (dw_bytes / launches + 15) / 16 * 16;
-    auto stretch = [&](int i) {
-        const int64_t lo = share * i < dw_bytes ? share * i : dw_bytes, hi = i == launches - 1 ? dw_bytes : lo + share < dw_bytes ? lo + share : dw_bytes;
-        return a.add ? Fill{static_cast<char *>(a.dw), 0} : Fill{static_cast<char *>(a.dw) + lo, hi - lo};
-    };
-    const dim3 grid((unsigned)p.parts + (a.add ? 0u : fillers));
-    if (launch_pdl(count_kernel, grid, dim3(kThreads), 0, s, so, stretch(0)) != cudaSuccess) return TBN_ERR_CUDA;
-    for (int i = 0; i < p.passes; ++i) {
-        if (launch_pdl(place_kernel, grid, dim3(kThreads), 0, s, so, i, stretch(i + 1)) != cudaSuccess) return TBN_ERR_CUDA;
-        if (i + 2 < p.passes &&
-            launch_pdl(clear_kernel, dim3(64), dim3(kThreads), 0, s, so.count[i & 1], (int64_t)p.parts << p.bits) != cudaSuccess)
-            return TBN_ERR_CUDA;
+    const uint2 *list = so.list[0];
+    if (p.one) {
+        static std::atomic<uint64_t> done;
+        if (allow_smem(sort_kernel, done) != cudaSuccess) return TBN_ERR_CUDA;
+        const Fill f = {static_cast<char *>(a.dw), a.add ? 0 : dw_bytes};
+        const int64_t blocks = (dw_bytes + 65535) / 65536, most = (int64_t)sm_count() * 2;
+        const unsigned grid = 1u + (a.add ? 0u : (unsigned)(blocks < most ? blocks : most));
+        if (launch_pdl(sort_kernel, dim3(grid), dim3(kOneThreads), sizeof(OneSmem), s, so, f) != cudaSuccess) return TBN_ERR_CUDA;
+    } else {
+        // the zeros, in as many equal stretches as the sort has launches
+        const int launches = p.passes + 1;
+        const int64_t share = (dw_bytes / launches + 15) / 16 * 16;
+        auto stretch = [&](int i) {
+            const int64_t lo = share * i < dw_bytes ? share * i : dw_bytes, hi = i == launches - 1 ? dw_bytes : lo + share < dw_bytes ? lo + share : dw_bytes;
+            return a.add ? Fill{static_cast<char *>(a.dw), 0} : Fill{static_cast<char *>(a.dw) + lo, hi - lo};
+        };
+        const dim3 grid((unsigned)p.parts + (a.add ? 0u : fillers));
+        if (launch_pdl(count_kernel, grid, dim3(kThreads), 0, s, so, stretch(0)) != cudaSuccess) return TBN_ERR_CUDA;
+        for (int i = 0; i < p.passes; ++i) {
+            if (launch_pdl(place_kernel, grid, dim3(kThreads), 0, s, so, i, stretch(i + 1)) != cudaSuccess) return TBN_ERR_CUDA;
+            if (i + 2 < p.passes &&
+                launch_pdl(clear_kernel, dim3(64), dim3(kThreads), 0, s, so.count[i & 1], (int64_t)p.parts << p.bits) != cudaSuccess)
+                return TBN_ERR_CUDA;
+        }
+        list = so.list[p.passes & 1];
     }
-    const uint2 *list = so.list[p.passes & 1];
     float *partial = reinterpret_cast<float *>(ws + p.o_partial);
     cudaError_t e;
     if (a.dy_dtype == TBN_F32) e = a.dw_dtype == TBN_F32 ? sums_typed<float, float>(a, p, list, partial, s) : sums_typed<float, __nv_bfloat16>(a, p, list, partial, s);
