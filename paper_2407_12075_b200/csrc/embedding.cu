@@ -58,14 +58,6 @@ __device__ __forceinline__ void store_row(float *p, const float (&v)[8])        
     reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 __device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[8]) { store8(p, v); }
-template <typename T> __device__ __forceinline__ Raw8<T> zero8()
-{
-    Raw8<T> r;
-#pragma unroll
-    for (int e = 0; e < (int)(sizeof(r.w) / 4); ++e) r.w[e] = 0;
-    return r;
-}
-
 // The eight columns from c on of row `row` of a table, scaled; what is behind column d is left as it is in v.
 template <typename WT> struct DenseRows {
     const WT *table, *end;
@@ -232,6 +224,19 @@ template <int THREADS> __device__ __forceinline__ void fill(const Fill &f, unsig
         for (int64_t i = whole * 8 + threadIdx.x; i < f.bytes / 2; i += THREADS) reinterpret_cast<uint16_t *>(f.to)[i] = 0;
 }
 
+// The lanes that are `here` with the same digit of `bits` bits, one vote for each bit (4096 tokens: 2.1 us less a pass than
+// __match_any_sync).
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, bool here)
+{
+    uint32_t same = __ballot_sync(0xffffffffu, here);
+    for (int b = 0; b < bits; ++b) {
+        const bool one = digit >> b & 1u;
+        const uint32_t v = __ballot_sync(0xffffffffu, one);
+        same &= one ? v : ~v;
+    }
+    return same;
+}
+
 __global__ void __launch_bounds__(kThreads)
 count_kernel(const Sort s, const Fill f)
 {
@@ -275,6 +280,7 @@ place_kernel(const Sort s, int32_t pass, const Fill f)
         total[j] = before[j] = 0;
         const int b = threadIdx.x * per + j;
         if (j < per && b < bins)
+#pragma unroll 8
             for (int32_t p = 0; p < s.parts; ++p) {
                 const uint32_t c = count[(int64_t)p * bins + b];
                 total[j] += c;
@@ -320,8 +326,7 @@ place_kernel(const Sort s, int32_t pass, const Fill f)
         const bool here = t < w1;
         uint2 item = make_uint2(0, 0);
         if (here) item = pass == 0 ? make_uint2(key_of(s, t), (uint32_t)t) : from[t];
-        const uint32_t digit = here ? (item.x >> shift) & (uint32_t)(bins - 1) : 0xffffffffu;
-        const uint32_t same = __match_any_sync(0xffffffffu, digit);
+        const uint32_t digit = (item.x >> shift) & (uint32_t)(bins - 1), same = same_digit(digit, s.bits, here);
         const uint32_t rank = __popc(same & ((1u << lane) - 1u));
         uint32_t at = 0;
         if (here) at = seen[warp][digit] + rank;
@@ -344,199 +349,178 @@ clear_kernel(uint32_t *__restrict__ count, int64_t n)
     for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) count[i] = 0;
 }
 
-// Up to 8192 tokens are sorted by one thread block, in registers and shared memory: a warp takes a stretch of the list, eight tokens to a lane
-// at most, finds each token's place among the warp's of its digit as it goes, and after the sums over warps and digits every
-// token goes to its place in a list that the next pass reads.  One launch instead of three, of which each waits for the one before.
-constexpr int kOneThreads = 1024, kOneWarps = kOneThreads / 32, kOneTokens = 8192, kOneBins = 256;
-struct OneSmem {
-    uint2 list[kOneTokens];
-    uint32_t seen[kOneWarps][kOneBins];     // tokens of a digit in the warps before, then where the warp's first one goes
-    uint32_t base[kOneBins];
-};
-__global__ void __launch_bounds__(kOneThreads)
-sort_kernel(const Sort s, const Fill f)
+// Few tokens are sorted in one launch, by counting: a token goes behind all with a smaller id and those before it with its own.  A thread
+// block takes 32 tokens, one to a lane, and its warps a share of the list each; T^2 comparisons, at two instructions for 32 of them, spread over
+// the SMs (4096 tokens: RANK_US us; one thread block sorting by digits took 13.8, the launches above 19).
+constexpr int kRankTokens = 8192;
+__global__ void __launch_bounds__(kThreads)
+rank_kernel(const Sort s, const Fill f, unsigned rankers)
 {
-    extern __shared__ __align__(16) char raw[];
-    OneSmem &m = *reinterpret_cast<OneSmem *>(raw);
+    extern __shared__ __align__(16) char smem[];
+    uint32_t *key = reinterpret_cast<uint32_t *>(smem);               // T of them, then ones beyond every key up to a multiple of 4
+    __shared__ uint32_t part[kSortWarps][32];
     pdl_launch_dependents();
     pdl_wait();
-    if (blockIdx.x > 0) { fill<kOneThreads>(f, blockIdx.x - 1, gridDim.x - 1); return; }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, bins = 1 << s.bits;
-    const int T = (int)s.T, rounds = (T + kOneThreads - 1) / kOneThreads, first = warp * rounds * 32 + lane;
-    uint2 item[8];
+    if (blockIdx.x >= rankers) { fill<kThreads>(f, blockIdx.x - rankers, gridDim.x - rankers); return; }
+    const int T = (int)s.T, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int padded = (T + 31) & ~31;
+#pragma unroll 16
+    for (int t = threadIdx.x; t < padded; t += kThreads) key[t] = t < T ? key_of(s, t) : 0xffffffffu;
+    __syncthreads();
+    const int t0 = blockIdx.x * 32;
+    const uint32_t mine = key[t0 + lane];
+    uint32_t count = 0;
+    // the list in groups of 32: those before the block's own count where not larger, those behind it where smaller
+    const int groups = padded / 32, own = blockIdx.x;
+    for (int g = warp; g < groups; g += kSortWarps) {
+        const uint4 *k4 = reinterpret_cast<const uint4 *>(key + g * 32);
+        const uint32_t limit = mine + (g < own ? 1u : 0u);            // not larger: smaller than the next number
+        if (g != own) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
-        if (r < rounds && first + r * 32 < T) item[r] = make_uint2(key_of(s, first + r * 32), (uint32_t)(first + r * 32));
-    for (int pass = 0; pass < s.passes; ++pass) {
-        const int shift = pass * s.bits;
-        for (int b = threadIdx.x; b < kOneWarps * bins; b += kOneThreads) m.seen[b >> s.bits][b & (bins - 1)] = 0;
-        __syncthreads();
-        uint32_t before[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            if (r >= rounds) break;
-            const bool here = first + r * 32 < T;
-            const uint32_t digit = here ? (item[r].x >> shift) & (uint32_t)(bins - 1) : 0xffffffffu;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit), rank = __popc(same & ((1u << lane) - 1u));
-            uint32_t c = 0;
-            if (here) c = m.seen[warp][digit];
-            before[r] = c + rank;
-            __syncwarp();
-            if (here && rank == 0) m.seen[warp][digit] = c + __popc(same);
-            __syncwarp();
-        }
-        __syncthreads();
-        {                                                             // four threads to a digit, eight warps to each
-            const int b = threadIdx.x >> 2, quarter = threadIdx.x & 3;
-            uint32_t c[8], sum = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) { c[k] = b < bins ? m.seen[quarter * 8 + k][b] : 0; sum += c[k]; }
-            uint32_t run = sum;
-            uint32_t o = __shfl_up_sync(0xffffffffu, run, 1, 4);
-            if (quarter >= 1) run += o;
-            o = __shfl_up_sync(0xffffffffu, run, 2, 4);
-            if (quarter >= 2) run += o;
-            if (quarter == 3) m.base[b] = run;
-            __syncthreads();
-            if (warp == 0) {
-                uint32_t t[kOneBins / 32], all = 0;
-#pragma unroll
-                for (int k = 0; k < kOneBins / 32; ++k) { t[k] = all; all += m.base[lane * (kOneBins / 32) + k]; }
-                uint32_t up = all;
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const uint32_t x = __shfl_up_sync(0xffffffffu, up, off);
-                    if (lane >= off) up += x;
-                }
-#pragma unroll
-                for (int k = 0; k < kOneBins / 32; ++k) m.base[lane * (kOneBins / 32) + k] = t[k] + up - all;
+            for (int i = 0; i < 8; ++i) {
+                const uint4 k = k4[i];
+                count += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
             }
-            __syncthreads();
-            uint32_t at = m.base[b] + run - sum;
+        } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (b < bins) { m.seen[quarter * 8 + k][b] = at; at += c[k]; }
-        }
-        __syncthreads();
-        const bool last = pass + 1 == s.passes;
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-            if (r < rounds && first + r * 32 < T) {
-                uint2 *to = last ? s.list[0] : m.list;
-                to[m.seen[warp][(item[r].x >> shift) & (uint32_t)(bins - 1)] + before[r]] = item[r];
+            for (int i = 0; i < 32; ++i) {
+                const uint32_t k = key[t0 + i];
+                count += k < mine || (k == mine && i < lane);
             }
-        if (last) return;
-        __syncthreads();
+        }
+    }
+    part[warp][lane] = count;
+    __syncthreads();
+    if (warp == 0 && t0 + lane < T) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-            if (r < rounds && first + r * 32 < T) item[r] = m.list[first + r * 32];
+        for (int w = 1; w < kSortWarps; ++w) count += part[w][lane];
+        s.list[0][count] = make_uint2(mine, (uint32_t)(t0 + lane));
     }
 }
 
 // ---- sums -------------------------------------------------------------------------------------------------------------------
-// A lane's eight columns of a row of dw (from column c on), added to and written; rows are aligned where EVEN.
-template <bool EVEN, typename WT> __device__ __forceinline__ void write_sum(WT *row, int32_t c, int32_t d, const float (&acc)[8], float scale, int add)
+// A lane's eight columns of a row of dw (from column c on): what was there (of aligned rows: `old`, loaded ahead) and the sum, written.
+template <bool EVEN, bool ADD, typename WT>
+__device__ __forceinline__ void write_sum(WT *row, int32_t c, int32_t d, const float (&acc)[8], float scale, const Raw8<WT> &old)
 {
     if (c >= d) return;
-    float o[8];
     if (EVEN) {
+        float o[8];
+        if (ADD) unpack8(old, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = 0.0f;
-        if (add) {
-            Raw8<WT> r;
-            load_any(row + c, row + d, true, r);
-            unpack8(r, o);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(scale, acc[e], o[e]);
+        for (int e = 0; e < 8; ++e) o[e] = ADD ? fmaf(scale, acc[e], o[e]) : scale * acc[e];
         store_row(row + c, o);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (c + e >= d) break;
-            store_from_float(row, c + e, fmaf(scale, acc[e], add ? value_of(row[c + e]) : 0.0f));
+            store_from_float(row, c + e, ADD ? fmaf(scale, acc[e], value_of(row[c + e])) : scale * acc[e]);
         }
     }
 }
 // Sums of pieces lie in rows of `pitch` floats (a multiple of eight).
 __device__ __forceinline__ void put_partial(float *row, int32_t c, const float (&acc)[8]) { store_row(row + c, acc); }
 
-// A warp takes one piece of the sorted list and 256 columns.  An id's tokens that begin and end in the piece are done with; what
+// A warp takes one piece of the sorted list and NP * 256 columns.  An id's tokens that begin and end in the piece are done with; what
 // comes from the piece before, or goes on in the next one, is written to `partial` ([piece][2][pitch]: first, last).
-constexpr int kAhead = 8;                   // rows loaded before the first is added
-template <typename GT, typename WT, bool EVEN>
+template <typename GT, typename WT, int NP, bool EVEN, bool ADD>
 __global__ void __launch_bounds__(kThreads)
 sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, int32_t segs, float scale,
-           const GT *__restrict__ dy, WT *__restrict__ dw, int add, float *__restrict__ partial, int32_t pitch)
+           const GT *__restrict__ dy, WT *dw, float *__restrict__ partial, int32_t pitch)
 {
+    // rows of dy loaded before the first is added, with the rows of dw that sums beginning there will be added to
+    constexpr int kAhead = ADD ? 8 / NP / (NP > 1 ? 1 : 2) : NP == 1 ? 8 : sizeof(GT) == 2 ? 8 / NP * 2 : 8 / NP;
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
     const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t k = segs == 1 ? w : w / segs;
     if (k >= pieces) return;
-    const int32_t c = (int32_t)(w - k * segs) * 256 + lane * 8;
-    const int64_t a = k * piece, b = a + piece < T ? a + piece : T;
+    const int32_t c0 = (int32_t)(w - k * segs) * (256 * NP) + lane * 8;
+    const int64_t a = k * piece;
+    const int n = (int)(T - a < piece ? T - a : piece);
     const GT *end = dy + T * d;
     uint2 item = make_uint2(0xffffffffu, 0);
-    if (a + lane < b) item = list[a + lane];
-    const uint32_t left = a > 0 ? list[a - 1].x : 0xffffffffu, right = b < T ? list[b].x : 0xffffffffu;
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (lane < n) item = list[a + lane];
+    const uint32_t left = a > 0 ? list[a - 1].x : 0xffffffffu, right = a + n < T ? list[a + n].x : 0xffffffffu;
+    float acc[NP][8];
+    Raw8<WT> old[NP];
     uint32_t cur = 0xffffffffu;
     bool from_left = false;
     auto put = [&](bool to_right) {
         if (cur >= (uint32_t)V) return;
         if (from_left || to_right) {
-            if (c < d) put_partial(partial + (k * 2 + (from_left ? 0 : 1)) * pitch, c, acc);
+            float *row = partial + (k * 2 + (from_left ? 0 : 1)) * pitch;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) if (c0 + j * 256 < d) put_partial(row, c0 + j * 256, acc[j]);
         } else {
-            write_sum<EVEN>(dw + (int64_t)cur * d, c, d, acc, scale, add);
+            WT *row = dw + (int64_t)cur * d;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) write_sum<EVEN, ADD>(row, c0 + j * 256, d, acc[j], scale, old[j]);
         }
     };
-    for (int64_t p0 = a; p0 < b; p0 += 32) {
-        if (p0 > a) {
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+        if (i0 > 0 && (i0 & 31) == 0) {
             item = make_uint2(0xffffffffu, 0);
-            if (p0 + lane < b) item = list[p0 + lane];
+            if (i0 + lane < n) item = list[a + i0 + lane];
         }
-        const int n = (int)(b - p0 < 32 ? b - p0 : 32);
-        for (int i0 = 0; i0 < n; i0 += kAhead) {
-            Raw8<GT> r[kAhead];
+        Raw8<GT> r[kAhead][NP];
+        Raw8<WT> there[ADD && EVEN ? kAhead : 1][NP];
+        uint32_t before = cur;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const uint32_t key = __shfl_sync(0xffffffffu, item.x, i0 + i), tok = __shfl_sync(0xffffffffu, item.y, i0 + i);
-                r[i] = zero8<GT>();
-                if (key < (uint32_t)V && c < d) {                     // beyond the piece: a key of 2^32 - 1
-                    const GT *row = dy + (int64_t)tok * d;
-                    if (EVEN || c + 8 <= d) {
-                        load_any(row + c, end, EVEN, r[i]);
+        for (int i = 0; i < kAhead; ++i) {
+            const uint32_t key = __shfl_sync(0xffffffffu, item.x, (i0 + i) & 31), tok = __shfl_sync(0xffffffffu, item.y, (i0 + i) & 31);
+            const bool starts = key != before;
+            before = key;
+            if (key >= (uint32_t)V) continue;                         // beyond the piece: a key of 2^32 - 1
+            if (ADD && EVEN && starts) {
+#pragma unroll
+                for (int j = 0; j < NP; ++j)
+                    if (c0 + j * 256 < d) load_any(dw + (int64_t)key * d + c0 + j * 256, dw, true, there[ADD && EVEN ? i : 0][j]);
+            }
+            const GT *row = dy + (int64_t)tok * d;
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                const int32_t c = c0 + j * 256;
+                if (EVEN ? c < d : c + 8 <= d) {
+                    load_any(row + c, end, EVEN, r[i][j]);
+                } else if (!EVEN && c < d) {
+                    uint32_t h[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[e] = c + e < d ? __float_as_uint(value_of(row[c + e])) : 0u;
+                    if (sizeof(GT) == 4) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) r[i][j].w[e % (int)(sizeof(r[i][j].w) / 4)] = h[e];
                     } else {
-                        uint32_t h[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) h[e] = c + e < d ? __float_as_uint(value_of(row[c + e])) : 0u;
-                        if (sizeof(GT) == 4) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) r[i].w[e % (int)(sizeof(r[i].w) / 4)] = h[e];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) r[i].w[e] = h[2 * e] >> 16 | (h[2 * e + 1] & 0xffff0000u);
-                        }
+                        for (int e = 0; e < 4; ++e) r[i][j].w[e] = h[2 * e] >> 16 | (h[2 * e + 1] & 0xffff0000u);
                     }
                 }
             }
+        }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (i0 + i >= n) break;
-                const uint32_t key = __shfl_sync(0xffffffffu, item.x, i0 + i);
-                if (key != cur) {
-                    put(false);
-                    from_left = p0 + i0 + i == a && key == left;
-                    cur = key;
+        for (int i = 0; i < kAhead; ++i) {
+            const uint32_t key = __shfl_sync(0xffffffffu, item.x, (i0 + i) & 31);
+            if (i0 + i >= n) break;
+            const bool starts = key != cur;
+            if (starts) {
+                put(false);
+                from_left = i0 + i == 0 && key == left;
+                cur = key;
+                if (ADD && EVEN) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+                    for (int j = 0; j < NP; ++j) old[j] = there[ADD && EVEN ? i : 0][j];
                 }
-                float v[8];
-                unpack8(r[i], v);
+            }
+            if (key >= (uint32_t)V) continue;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] += v[e];
+            for (int j = 0; j < NP; ++j) {
+                if (c0 + j * 256 >= d) continue;
+                float v[8];
+                unpack8(r[i][j], v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[j][e] = starts ? v[e] : acc[j][e] + v[e];
             }
         }
     }
@@ -546,9 +530,9 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
 // The ids whose tokens lie in several pieces.  A warp looks at one piece: does its last id begin in it and go on?  Short runs it
 // adds up by itself, long ones are shared by the block's warps.
 constexpr int kAlone = 16;
-template <typename WT, bool EVEN>
+template <typename WT, bool EVEN, bool ADD>
 __global__ void __launch_bounds__(kThreads)
-join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, float scale, WT *__restrict__ dw, int add,
+join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, float scale, WT *dw,
             const float *__restrict__ partial, int32_t pitch)
 {
     constexpr int kWarps = kThreads / 32;
@@ -582,12 +566,12 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
     auto add_up = [&](int64_t from, int64_t lo, int64_t hi, float (&acc)[8]) {          // partials lo .. hi of the run of piece `from`
         if (c >= d) return;
         int64_t i = lo;
-        for (; i + 4 <= hi; i += 4) {
-            Raw8<float> r[4];
+        for (; i + 8 <= hi; i += 8) {
+            Raw8<float> r[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) load_any(partial + ((from + i + j) * 2 + (i + j == 0 ? 1 : 0)) * pitch + c, partial, true, r[j]);
+            for (int j = 0; j < 8; ++j) load_any(partial + ((from + i + j) * 2 + (i + j == 0 ? 1 : 0)) * pitch + c, partial, true, r[j]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 8; ++j)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(r[j].w[e]);
         }
@@ -598,10 +582,15 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
             for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(r.w[e]);
         }
     };
+    auto row_there = [&](uint32_t id, Raw8<WT> &old) {
+        if (ADD && EVEN && c < d) load_any(dw + (int64_t)id * d + c, dw, true, old);
+    };
     if (n > 0 && n <= kAlone) {
         float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        Raw8<WT> old;
+        row_there(key, old);
         add_up(k, 0, n + 1, acc);
-        write_sum<EVEN>(dw + (int64_t)key * d, c, d, acc, scale, add);
+        write_sum<EVEN, ADD>(dw + (int64_t)key * d, c, d, acc, scale, old);
     }
     if (lane == 0) { more[warp] = n > kAlone ? n : 0; key_at[warp] = key; }
     __syncthreads();
@@ -609,6 +598,8 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
         const int64_t len = more[j] + 1;                              // the same for the whole block
         if (len == 1) continue;
         float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        Raw8<WT> old;
+        if (warp == 0) row_there(key_at[j], old);
         add_up((int64_t)blockIdx.x * kWarps + j, len * warp / kWarps, len * (warp + 1) / kWarps, acc);
 #pragma unroll
         for (int e = 0; e < 8; ++e) red[warp][e * 32 + lane] = acc[e];
@@ -617,7 +608,7 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 for (int i = 1; i < kWarps; ++i) acc[e] += red[i][e * 32 + lane];
-            write_sum<EVEN>(dw + (int64_t)key_at[j] * d, c, d, acc, scale, add);
+            write_sum<EVEN, ADD>(dw + (int64_t)key_at[j] * d, c, d, acc, scale, old);
         }
         __syncthreads();
     }
@@ -636,7 +627,7 @@ size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct Plan {
     int32_t part, parts, bits, passes, piece, pitch;
-    bool one;                               // sorted by one thread block
+    bool one;                               // sorted in one launch
     int64_t pieces;
     size_t o_list[2], o_count[2], o_partial, total;
 };
@@ -645,9 +636,8 @@ Plan make_plan(int64_t T, int32_t d, int32_t V)
     Plan p = {};
     int32_t need = 1;
     while (((int64_t)V >> need) != 0) ++need;                         // bits of V, the key of what is outside
-    p.one = T <= kOneTokens;
-    const int32_t most_bits = p.one ? 8 : 10;
-    p.passes = (need + most_bits - 1) / most_bits;
+    p.one = T <= kRankTokens;
+    p.passes = (need + 9) / 10;
     p.bits = (need + p.passes - 1) / p.passes;
     // parts of 1024 tokens: four rounds of a block's warps; more when the blocks' sums over all parts' counts would grow
     int64_t part = 1024;
@@ -692,19 +682,33 @@ template <typename WT, typename YT> cudaError_t lookup_typed(const LookupArgs &a
     return lookup_rows<TiledRows, YT>(a, TiledRows{a.tile, a.alpha, a.q, (a.q + 31) / 32, a.d, rows, a.per_tile, a.scale}, s);
 }
 
-template <typename GT, typename WT> cudaError_t sums_typed(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
+template <typename GT, typename WT, int NP, bool EVEN, bool ADD>
+cudaError_t sum_pieces(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
 {
-    const int32_t segs = (a.d + 255) / 256;
-    const bool even = a.d % 8 == 0;
-    const GT *dy = static_cast<const GT *>(a.dy);
-    WT *dw = static_cast<WT *>(a.dw);
+    const int32_t segs = (a.d + 256 * NP - 1) / (256 * NP);
     const int64_t blocks = (p.pieces * segs + kThreads / 32 - 1) / (kThreads / 32);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    cudaError_t e = launch_pdl(even ? sum_kernel<GT, WT, true> : sum_kernel<GT, WT, false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V,
-                               a.d, p.piece, p.pieces, segs, a.scale, dy, dw, a.add, partial, p.pitch);
+    return launch_pdl(sum_kernel<GT, WT, NP, EVEN, ADD>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, segs, a.scale,
+                      static_cast<const GT *>(a.dy), static_cast<WT *>(a.dw), partial, p.pitch);
+}
+template <typename GT, typename WT, bool EVEN, bool ADD>
+cudaError_t sums(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
+{
+    // the more columns to a warp the less a row costs, while there are warps for every SM
+    const int64_t warps = (int64_t)sm_count() * 12;
+    cudaError_t e;
+    if (a.d > 512 && p.pieces * ((a.d + 1023) / 1024) >= warps) e = sum_pieces<GT, WT, ADD ? 2 : 4, EVEN, ADD>(a, p, list, partial, s);
+    else if (a.d > 256 && p.pieces * ((a.d + 511) / 512) >= warps) e = sum_pieces<GT, WT, 2, EVEN, ADD>(a, p, list, partial, s);
+    else e = sum_pieces<GT, WT, 1, EVEN, ADD>(a, p, list, partial, s);
     if (e != cudaSuccess || p.pieces == 1) return e;
-    return launch_pdl(even ? join_kernel<WT, true> : join_kernel<WT, false>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs),
-                      dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, a.scale, dw, a.add, static_cast<const float *>(partial), p.pitch);
+    const int32_t segs = (a.d + 255) / 256;
+    return launch_pdl(join_kernel<WT, EVEN, ADD>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs), dim3(kThreads), 0, s,
+                      list, a.T, a.V, a.d, p.piece, p.pieces, a.scale, static_cast<WT *>(a.dw), static_cast<const float *>(partial), p.pitch);
+}
+template <typename GT, typename WT> cudaError_t sums_typed(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
+{
+    if (a.d % 8 == 0) return a.add ? sums<GT, WT, true, true>(a, p, list, partial, s) : sums<GT, WT, true, false>(a, p, list, partial, s);
+    return a.add ? sums<GT, WT, false, true>(a, p, list, partial, s) : sums<GT, WT, false, false>(a, p, list, partial, s);
 }
 
 }  // namespace
@@ -737,12 +741,11 @@ int gradient(const GradArgs &a, void *workspace, cudaStream_t s)
     }
     const uint2 *list = so.list[0];
     if (p.one) {
-        static std::atomic<uint64_t> done;
-        if (allow_smem(sort_kernel, done) != cudaSuccess) return TBN_ERR_CUDA;
         const Fill f = {static_cast<char *>(a.dw), a.add ? 0 : dw_bytes};
-        const int64_t blocks = (dw_bytes + 65535) / 65536, most = (int64_t)sm_count() * 2;
-        const unsigned grid = 1u + (a.add ? 0u : (unsigned)(blocks < most ? blocks : most));
-        if (launch_pdl(sort_kernel, dim3(grid), dim3(kOneThreads), sizeof(OneSmem), s, so, f) != cudaSuccess) return TBN_ERR_CUDA;
+        const unsigned rankers = (unsigned)((a.T + 31) / 32);
+        const int64_t blocks = (dw_bytes + 16383) / 16384;
+        const unsigned grid = rankers + (a.add ? 0u : (unsigned)(blocks < fillers ? blocks : fillers));
+        if (launch_spread(rank_kernel, dim3(grid), dim3(kThreads), (size_t)rankers * 128, s, so, f, rankers) != cudaSuccess) return TBN_ERR_CUDA;
     } else {
         // the zeros, in as many equal stretches as the sort has launches
         const int launches = p.passes + 1;
@@ -752,7 +755,7 @@ int gradient(const GradArgs &a, void *workspace, cudaStream_t s)
             return a.add ? Fill{static_cast<char *>(a.dw), 0} : Fill{static_cast<char *>(a.dw) + lo, hi - lo};
         };
         const dim3 grid((unsigned)p.parts + (a.add ? 0u : fillers));
-        if (launch_pdl(count_kernel, grid, dim3(kThreads), 0, s, so, stretch(0)) != cudaSuccess) return TBN_ERR_CUDA;
+        if (launch_spread(count_kernel, grid, dim3(kThreads), 0, s, so, stretch(0)) != cudaSuccess) return TBN_ERR_CUDA;
         for (int i = 0; i < p.passes; ++i) {
             if (launch_pdl(place_kernel, grid, dim3(kThreads), 0, s, so, i, stretch(i + 1)) != cudaSuccess) return TBN_ERR_CUDA;
             if (i + 2 < p.passes &&

@@ -106,6 +106,15 @@ template <typename K> cudaError_t allow_smem(K kernel, std::atomic<uint64_t> &do
     if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
     return e;
 }
+// An ordinary launch, for the first kernel of a call where it has few small blocks that are to lie on SMs of their own: launched early
+// (launch_pdl) they are placed while the kernel before holds most SMs, several on each of the few that are free.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_spread(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
 // Multiprocessors of the current device.
 inline int sm_count()
 {
