@@ -688,7 +688,7 @@ cudaError_t sum_pieces(const GradArgs &a, const Plan &p, const uint2 *list, floa
     const int32_t segs = (a.d + 256 * NP - 1) / (256 * NP);
     const int64_t blocks = (p.pieces * segs + kThreads / 32 - 1) / (kThreads / 32);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    return launch_pdl(sum_kernel<GT, WT, NP, EVEN, ADD>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, segs, a.scale,
+    return launch_spread(sum_kernel<GT, WT, NP, EVEN, ADD>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, segs, a.scale,
                       static_cast<const GT *>(a.dy), static_cast<WT *>(a.dw), partial, p.pitch);
 }
 template <typename GT, typename WT, bool EVEN, bool ADD>
@@ -702,7 +702,7 @@ cudaError_t sums(const GradArgs &a, const Plan &p, const uint2 *list, float *par
     else e = sum_pieces<GT, WT, 1, EVEN, ADD>(a, p, list, partial, s);
     if (e != cudaSuccess || p.pieces == 1) return e;
     const int32_t segs = (a.d + 255) / 256;
-    return launch_pdl(join_kernel<WT, EVEN, ADD>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs), dim3(kThreads), 0, s,
+    return launch_spread(join_kernel<WT, EVEN, ADD>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs), dim3(kThreads), 0, s,
                       list, a.T, a.V, a.d, p.piece, p.pieces, a.scale, static_cast<WT *>(a.dw), static_cast<const float *>(partial), p.pitch);
 }
 template <typename GT, typename WT> cudaError_t sums_typed(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
@@ -757,9 +757,9 @@ int gradient(const GradArgs &a, void *workspace, cudaStream_t s)
         const dim3 grid((unsigned)p.parts + (a.add ? 0u : fillers));
         if (launch_spread(count_kernel, grid, dim3(kThreads), 0, s, so, stretch(0)) != cudaSuccess) return TBN_ERR_CUDA;
         for (int i = 0; i < p.passes; ++i) {
-            if (launch_pdl(place_kernel, grid, dim3(kThreads), 0, s, so, i, stretch(i + 1)) != cudaSuccess) return TBN_ERR_CUDA;
+            if (launch_spread(place_kernel, grid, dim3(kThreads), 0, s, so, i, stretch(i + 1)) != cudaSuccess) return TBN_ERR_CUDA;
             if (i + 2 < p.passes &&
-                launch_pdl(clear_kernel, dim3(64), dim3(kThreads), 0, s, so.count[i & 1], (int64_t)p.parts << p.bits) != cudaSuccess)
+                launch_spread(clear_kernel, dim3(64), dim3(kThreads), 0, s, so.count[i & 1], (int64_t)p.parts << p.bits) != cudaSuccess)
                 return TBN_ERR_CUDA;
         }
         list = so.list[p.passes & 1];

@@ -590,6 +590,16 @@ bool one_block(int64_t T, const Shape &s) { return !s.lng && s.classes == 1 && T
 constexpr size_t kHalf = 113 * 1024;
 constexpr int kLongParts = 64;
 
+// Early, where the thread blocks fill the GPU or are a handful; those in between would be placed two to an SM while others are empty
+// (777 x 501 step: 14.8 us against 12.3).
+template <typename... KArgs, typename... Args>
+cudaError_t launch(int64_t blocks, int per_sm, void (*kernel)(KArgs...), int threads, size_t smem, cudaStream_t s, Args... args)
+{
+    const dim3 grid((unsigned)blocks), block(threads);
+    if (blocks <= 8 || blocks + 8 >= (int64_t)sm_count() * per_sm) return launch_pdl(kernel, grid, block, smem, s, args...);
+    return launch_spread(kernel, grid, block, smem, s, args...);
+}
+
 template <typename E, typename F> cudaError_t with_pieces(int np, E even, F f)
 {
     return np == 1 ? f(std::integral_constant<int, 1>{}, even) : np == 2 ? f(std::integral_constant<int, 2>{}, even)
@@ -616,7 +626,8 @@ template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs 
         static std::atomic<uint64_t> done;
         const cudaError_t e = allow_smem(forward_kernel<XT, YT, NP, EVEN>, done);
         if (e != cudaSuccess) return e;
-        return launch_pdl(forward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)blocks_of(a.T, sh, smem <= kHalf ? 2 : 1)), dim3(sh.groups * sh.warps * 32), smem, s, a, sh);
+        const int per_sm = smem <= kHalf ? 2 : 1;
+        return launch(blocks_of(a.T, sh, per_sm), per_sm, forward_kernel<XT, YT, NP, EVEN>, sh.groups * sh.warps * 32, smem, s, a, sh);
     });
 }
 
@@ -648,8 +659,9 @@ template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArg
             static std::atomic<uint64_t> done;
             const cudaError_t e1 = allow_smem(backward_kernel<XT, YT, NP, EVEN>, done);
             if (e1 != cudaSuccess) return e1;
-            parts = one_block(a.T, sh) ? 1 : (int32_t)blocks_of(a.T, sh, NP < 4 && smem <= kHalf ? 2 : 1);
-            return launch_pdl(backward_kernel<XT, YT, NP, EVEN>, dim3((unsigned)parts), dim3(sh.groups * sh.warps * 32), smem, s, a, sh, partial);
+            const int per_sm = NP < 4 && smem <= kHalf ? 2 : 1;
+            parts = one_block(a.T, sh) ? 1 : (int32_t)blocks_of(a.T, sh, per_sm);
+            return launch(parts, per_sm, backward_kernel<XT, YT, NP, EVEN>, sh.groups * sh.warps * 32, smem, s, a, sh, partial);
         });
     }
     if (e != cudaSuccess || !sums || (!sh.lng && parts == 1)) return e;            // one thread block has written them
