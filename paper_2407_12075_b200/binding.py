@@ -657,15 +657,27 @@ def tbn_linear_distill_bwd(x: torch.Tensor, weight: torch.Tensor, top_index: tor
 
 
 # ---- embedding, LayerNorm for training, AdamW --------------------------------------------------------------------
+# A short call's time is the host's: types and devices are looked at once, and tensors are made like ones that are there.
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+_current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _code(t):
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
+
+
 def _on_device(name, device, *args):
     """Runs the entry point on the tensors' device and that device's current stream."""
     index = device.index
     fn = getattr(_lib or lib(), name)
-    if torch._C._cuda_getDevice() == index:
-        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if _current_device() == index:
+        status = fn(*args, _current_stream(index))
     else:
         with torch.cuda.device(index):
-            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+            status = fn(*args, _current_stream(index))
     if status != OK:
         raise TbnError(status, name)
 
@@ -695,42 +707,40 @@ def _workspace(where, workspace, device, name, *sizes):
     return workspace, workspace.numel() * workspace.element_size()
 
 
-def _embedding_ids(ids, where):
-    if ids.dtype != torch.int64:
-        raise TypeError(f"{where}: ids must be int64, not {ids.dtype}")
-    return ids.numel()
-
-
 def tbn_embedding_fwd(ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0, padding_idx: int = -1, y_dtype: int | None = None) -> torch.Tensor:
     """scale * table[ids]; ids of any shape, y of shape ids.shape + (d,).  Ids outside the table and padding_idx give zeros."""
-    T, device = _embedding_ids(ids, "embedding"), ids.device
-    shape = table.shape
+    shape, device, td = table.shape, table.device, _code(table)
+    if ids.dtype is not torch.int64:
+        raise TypeError(f"embedding: ids must be int64, not {ids.dtype}")
     if len(shape) != 2:
         raise TbnError(-2, f"embedding: table {tuple(shape)}")
-    _same_device("embedding", device, table)
-    V, d = shape
-    td = _dtype_code(table)
+    if not table.is_cuda or ids.device != device:
+        raise ValueError(f"embedding: the tensors must be on one CUDA device: {ids.device}, {device}")
+    d = shape[1]
     if y_dtype is None:
         y_dtype = td
     y = torch.empty(*ids.shape, d, dtype=_torch_dtype(y_dtype), device=device)
-    _on_device("tbn_embedding_fwd", device, _ptr(ids), T, _ptr(table), td, V, d, padding_idx, scale, y.data_ptr(), y_dtype)
+    _on_device("tbn_embedding_fwd", device, _ptr(ids), ids.numel(), _ptr(table), td, shape[0], d, padding_idx, scale, y.data_ptr(), y_dtype)
     return y
 
 
 def tbn_embedding_tiled_fwd(ids: torch.Tensor, vocab: int, d: int, tile: torch.Tensor, k: int, alpha: torch.Tensor, alpha_mode: int,
                             scale: float = 1.0, padding_idx: int = -1, y_dtype: int = BF16) -> torch.Tensor:
     """tbn_embedding_fwd from a tiled table of vocab x d weights: its bits and scaling factors as tbn_aggregate_tile gives them."""
-    T, device = _embedding_ids(ids, "embedding"), ids.device
-    _same_device("embedding", device, tile, alpha)
+    device = ids.device
+    if ids.dtype is not torch.int64:
+        raise TypeError(f"embedding: ids must be int64, not {ids.dtype}")
+    if not ids.is_cuda or tile.device != device or alpha.device != device:
+        raise ValueError(f"embedding: the tensors must be on one CUDA device: {device}, {tile.device}, {alpha.device}")
     if k <= 0 or (vocab * d) % k:
         raise TbnError(-2, "tbn_embedding_tiled_fwd")
-    if tile.dtype != torch.int32 or tile.numel() < -(-(vocab * d // k) // 128) * 4:
+    if tile.dtype is not torch.int32 or tile.numel() < -(-(vocab * d // k) // 128) * 4:
         raise TbnError(-2, f"embedding: the tile must be int32 of {tbn_tile_words(vocab * d // k)} words")
-    if alpha.dtype != torch.float32 or alpha.numel() < (k if alpha_mode == ALPHA_PER_TILE else 1):
+    if alpha.dtype is not torch.float32 or alpha.numel() < (k if alpha_mode == ALPHA_PER_TILE else 1):
         raise TbnError(-2, "embedding: alpha must be float32, one value or one for each tile")
     y = torch.empty(*ids.shape, d, dtype=_torch_dtype(y_dtype), device=device)
-    _on_device("tbn_embedding_tiled_fwd", device, _ptr(ids), T, vocab, d, _ptr(tile), k, _ptr(alpha), alpha_mode, padding_idx, scale, y.data_ptr(),
-               y_dtype)
+    _on_device("tbn_embedding_tiled_fwd", device, _ptr(ids), ids.numel(), vocab, d, _ptr(tile), k, _ptr(alpha), alpha_mode, padding_idx, scale,
+               y.data_ptr(), y_dtype)
     return y
 
 
@@ -742,21 +752,24 @@ def tbn_embedding_bwd(ids: torch.Tensor, dy: torch.Tensor, vocab: int, scale: fl
                       add_to: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient of an embedding's table (vocab x d): the rows of dy that share an id, added up.  add_to: a gradient that is there
     already (a tied head's), which the sums are added to in place; otherwise a new tensor of dw_dtype (dy's type by default)."""
-    T, device = _embedding_ids(ids, "embedding"), ids.device
-    shape = dy.shape
+    shape, device, gd = dy.shape, dy.device, _code(dy)
+    if ids.dtype is not torch.int64:
+        raise TypeError(f"embedding: ids must be int64, not {ids.dtype}")
     if len(shape) < 1 or shape[:-1] != ids.shape:
         raise TbnError(-2, f"embedding: ids {tuple(ids.shape)} and dy {tuple(shape)}")
-    d, gd = shape[-1], _dtype_code(dy)
-    _same_device("embedding", device, dy, add_to)
+    if not dy.is_cuda or ids.device != device or (add_to is not None and add_to.device != device):
+        raise ValueError(f"embedding: the tensors must be on one CUDA device: {ids.device}, {device}" + ("" if add_to is None else f", {add_to.device}"))
+    T, d = ids.numel(), shape[-1]
     if add_to is not None:
         if add_to.shape != (vocab, d):
             raise TbnError(-2, f"embedding: add_to {tuple(add_to.shape)}, not ({vocab}, {d})")
-        wd, dw = _dtype_code(add_to), add_to
+        wd, dw = _code(add_to), add_to
     else:
         wd = gd if dw_dtype is None else dw_dtype
         dw = torch.empty(vocab, d, dtype=_torch_dtype(wd), device=device)
     ws, size = _workspace("embedding", workspace, device, "tbn_embedding_bwd_workspace_bytes", T, d, vocab)
-    _on_device("tbn_embedding_bwd", device, _ptr(ids), T, _ptr(dy), gd, vocab, d, padding_idx, scale, _ptr(dw), wd, int(add_to is not None), _ptr(ws), size)
+    _on_device("tbn_embedding_bwd", device, _ptr(ids), T, _ptr(dy), gd, vocab, d, padding_idx, scale, _ptr(dw), wd, 0 if add_to is None else 1,
+               _ptr(ws), size)
     return dw
 
 
@@ -764,7 +777,7 @@ def _norm_vector(v, n, device, what):
     """Address of a float32 vector of n values."""
     if v is None:
         return None
-    if v.dtype is not torch.float32 or v.shape != (n,) or v.device != device:
+    if v.dtype is not torch.float32 or v.numel() != n or v.dim() != 1 or v.device != device:
         raise TbnError(-2, f"layer norm: {what} must be float32 of shape ({n},) on {device}")
     return _ptr(v)
 
@@ -773,14 +786,13 @@ def tbn_layernorm_train_fwd(x: torch.Tensor, gamma: torch.Tensor | None = None, 
                             residual: torch.Tensor | None = None, y_dtype: int | None = None):
     """LayerNorm of s = x + residual (rounded to x's type; s is x without a residual) over the last dimension, for training.
     Returns (y, s, mean, rstd): what tbn_layernorm_bwd takes besides dy."""
-    device, xd, d = x.device, _dtype_code(x), x.shape[-1]
+    device, xd, d = x.device, _code(x), x.shape[-1]
     T = x.numel() // d if d else 0
-    if device.type != "cuda":
+    if not x.is_cuda:
         raise ValueError("layer norm: the tensors must be on a CUDA device")
     x_at, g_at, b_at = _ptr(x), _norm_vector(gamma, d, device, "gamma"), _norm_vector(beta, d, device, "beta")
-    if residual is None:
-        s, r_at, s_at = x, None, None
-    else:
+    s, r_at, s_at = x, None, None
+    if residual is not None:
         if residual.device != device:
             raise ValueError(f"layer norm: tensors on {device} and {residual.device}")
         if residual.shape != x.shape or residual.dtype is not x.dtype:
@@ -808,12 +820,12 @@ def tbn_layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, mean: torch.Tensor, rst
     shape, device = s.shape, s.device
     d = shape[-1]
     T = s.numel() // d if d else 0
-    if device.type != "cuda" or dy.device != device or (dsum is not None and dsum.device != device):
+    if not s.is_cuda or dy.device != device or (dsum is not None and dsum.device != device):
         raise ValueError(f"layer norm: the tensors must be on one CUDA device: {device}, {dy.device}" + ("" if dsum is None else f", {dsum.device}"))
     if dy.shape != shape or (dsum is not None and (dsum.shape != shape or dsum.dtype is not s.dtype)):
         raise TbnError(-2, f"layer norm: dy {tuple(dy.shape)}, s {tuple(shape)}" + ("" if dsum is None else f", dsum {tuple(dsum.shape)} {dsum.dtype}"))
     g_at, m_at, r_at = _norm_vector(gamma, d, device, "gamma"), _norm_vector(mean, T, device, "mean"), _norm_vector(rstd, T, device, "rstd")
-    dx, dgamma, dbeta, dg_at, db_at, ws_at, size = torch.empty_like(s), None, None, None, None, None, 0
+    dx, dgamma, dbeta, dg_at, db_at, ws, size = torch.empty_like(s), None, None, None, None, None, 0
     if need_dgamma:
         dgamma = torch.empty(d, dtype=torch.float32, device=device)
         dg_at = dgamma.data_ptr()
@@ -822,9 +834,8 @@ def tbn_layernorm_bwd(dy: torch.Tensor, s: torch.Tensor, mean: torch.Tensor, rst
         db_at = dbeta.data_ptr()
     if need_dgamma or need_dbeta:
         ws, size = _workspace("layer norm", workspace, device, "tbn_layernorm_bwd_workspace_bytes", T, d)
-        ws_at = _ptr(ws)
-    _on_device("tbn_layernorm_bwd", device, _ptr(dy), _dtype_code(dy), _ptr(s), _dtype_code(s), T, d, g_at, m_at, r_at, _ptr(dsum), dx.data_ptr(), dg_at,
-               db_at, ws_at, size)
+    _on_device("tbn_layernorm_bwd", device, _ptr(dy), _code(dy), _ptr(s), _code(s), T, d, g_at, m_at, r_at, _ptr(dsum), dx.data_ptr(), dg_at, db_at,
+               _ptr(ws), size)
     return dx, dgamma, dbeta
 
 
@@ -882,7 +893,7 @@ def tbn_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=No
         if c is not None and c.dtype != torch.bfloat16:
             raise TypeError(f"adamw: tensor {i}: a copy of {c.dtype}")
         ptr = lambda t: _ptr(t) if t is not None and t.numel() else None  # noqa: E731
-        table[i] = _AdamWTensor(ptr(p), ptr(g), ptr(a), ptr(b), ptr(sa), ptr(sb), ptr(c), size, decay[i], _dtype_code(p), _dtype_code(g), bits)
+        table[i] = _AdamWTensor(ptr(p), ptr(g), ptr(a), ptr(b), ptr(sa), ptr(sb), ptr(c), size, decay[i], _code(p), _code(g), bits)
         kept.append((p, g, a, b, sa, sb, c))
         bits_seen.add(bits)
     return AdamWTensors(table, device, kept, bits_seen)

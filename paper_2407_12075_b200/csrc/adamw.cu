@@ -736,10 +736,10 @@ int in_tables(const tbn_adamw_tensor *tensors, int32_t count, int per_sm, int le
                 blocks += (d.n + kBlock - 1) / kBlock;
             }
             picked -= tab.count;
-            // as many blocks to a warp as leave the thread blocks eight chunks each
+            // as many blocks to a warp as leave the thread blocks two chunks each
             const int64_t round = (int64_t)sm_count() * per_sm * kWarps;
             tab.per = least_per;
-            while (tab.per < most_per && blocks >= 16 * round * tab.per) tab.per *= 2;
+            while (tab.per < most_per && blocks >= 4 * round * tab.per) tab.per *= 2;
             const int64_t chunk = (int64_t)tab.per * kWarps * kBlock;
             tab.chunks = 0;
             for (int32_t k = 0; k < tab.count; ++k) {

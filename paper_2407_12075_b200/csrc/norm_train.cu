@@ -545,7 +545,7 @@ finish_kernel(const float *__restrict__ partial, int32_t parts, int32_t d, float
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;                // of dgamma's d and dbeta's d
     float t = 0.0f;
     if (c < 2 * (int64_t)d) {
-#pragma unroll 4
+#pragma unroll 10
         for (int32_t k = row; k < parts; k += 32) t += partial[(int64_t)k * 2 * d + c];
     }
     red[lane][row] = t;
