@@ -149,6 +149,12 @@ __device__ __forceinline__ void expect_tx_elect(uint32_t bar, uint32_t bytes, ui
         "setp.ne.b32 q, %2, 0;\n\t"
         "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(leader) : "memory");
 }
+__device__ __forceinline__ void arrive_pair_elect(uint32_t cluster_addr, uint32_t leader) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}" ::"r"(cluster_addr), "r"(leader) : "memory");
+}
 __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate,
                                          uint32_t leader) {
     asm volatile(
@@ -481,7 +487,8 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
 
     if (MODE == kDz) pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        // full: the first CTA's A producer, which also says how many bytes come, and the second CTA's
+        for (int s = 0; s < kMaxStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 2); mbar_init(smem_u32(&ctl->empty[s]), 1); }
         for (int s = 0; s < kAccs<PL>; ++s) { mbar_init(smem_u32(&ctl->d_full[s]), 1); mbar_init(smem_u32(&ctl->d_empty[s]), 2 * kEpiWarps); }
         ctl->abort_flag = 0;
         fence_barrier_init();
@@ -533,6 +540,9 @@ head_kernel(const __grid_constant__ Maps maps, const __grid_constant__ KernelPar
                     if (!ok) break;
                     const uint32_t bar = bar0 + px.stage * 8, sa = sm0 + px.stage * stage_bytes, sb = sa + a_bytes;
                     if (is_a && rank == 0) expect_tx_elect(full0 + px.stage * 8, (second ? 2 : 1) * a_bytes + 2 * b_bytes, leader);
+                    // A producer that loads nothing (a half tile without rows) takes part all the same: otherwise the pipeline could go
+                    // round between two of its looks at a barrier, of whose phase it sees the parity only, and it would wait for good
+                    if (is_a && rank == 1) arrive_pair_elect(bar, leader);
                     if (MODE != kGrads) {
                         if (!is_a) tma_load_pair(sb, map, kb * 64, p.l.w_row0 + r0, pl, bar, leader);
                         else if (load_a) tma_load_pair(sa, map, kb * 64, r0, pl, bar, leader);
