@@ -311,9 +311,21 @@ place_kernel(const Sort s, int32_t pass, const Fill f)
     const int64_t w0 = t0 + (int64_t)warp * (s.part / kSortWarps);
     int64_t w1 = w0 + s.part / kSortWarps;
     if (w1 > t1) w1 = t1;
-    for (int64_t t = w0 + lane; t < w1; t += 32) {
-        const uint32_t key = pass == 0 ? key_of(s, t) : from[t].x;
-        atomicAdd(&seen[warp][(key >> shift) & (uint32_t)(bins - 1)], 1u);
+    // four rounds at a time, whose tokens are asked for together
+    auto items = [&](int64_t tb, uint2 (&item)[4]) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t t = tb + r * 32 + lane;
+            item[r] = make_uint2(0, 0);
+            if (t < w1) item[r] = pass == 0 ? make_uint2(key_of(s, t), (uint32_t)t) : from[t];
+        }
+    };
+    for (int64_t tb = w0; tb < w1; tb += 128) {
+        uint2 item[4];
+        items(tb, item);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (tb + r * 32 + lane < w1) atomicAdd(&seen[warp][(item[r].x >> shift) & (uint32_t)(bins - 1)], 1u);
     }
     __syncthreads();
     for (int b = threadIdx.x; b < bins; b += kThreads) {
@@ -321,21 +333,26 @@ place_kernel(const Sort s, int32_t pass, const Fill f)
         for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = seen[w][b]; seen[w][b] = at; at += c; }
     }
     __syncthreads();
-    for (int64_t tb = w0; tb < w1; tb += 32) {
-        const int64_t t = tb + lane;
-        const bool here = t < w1;
-        uint2 item = make_uint2(0, 0);
-        if (here) item = pass == 0 ? make_uint2(key_of(s, t), (uint32_t)t) : from[t];
-        const uint32_t digit = (item.x >> shift) & (uint32_t)(bins - 1), same = same_digit(digit, s.bits, here);
-        const uint32_t rank = __popc(same & ((1u << lane) - 1u));
-        uint32_t at = 0;
-        if (here) at = seen[warp][digit] + rank;
-        __syncwarp();
-        if (here && rank == 0) seen[warp][digit] += __popc(same);
-        __syncwarp();
-        if (here) {
-            to[at] = item;
-            if (pass + 1 < s.passes) atomicAdd(&next[(int64_t)(at / (uint32_t)s.part) * bins + ((item.x >> (shift + s.bits)) & (uint32_t)(bins - 1))], 1u);
+    for (int64_t tb = w0; tb < w1; tb += 128) {
+        uint2 four[4];
+        items(tb, four);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if (tb + r * 32 >= w1) break;
+            const bool here = tb + r * 32 + lane < w1;
+            const uint2 item = four[r];
+            const uint32_t digit = (item.x >> shift) & (uint32_t)(bins - 1), same = same_digit(digit, s.bits, here);
+            const uint32_t rank = __popc(same & ((1u << lane) - 1u));
+            uint32_t at = 0;
+            if (here) at = seen[warp][digit] + rank;
+            __syncwarp();
+            if (here && rank == 0) seen[warp][digit] += __popc(same);
+            __syncwarp();
+            if (here) {
+                to[at] = item;
+                if (pass + 1 < s.passes)
+                    atomicAdd(&next[(int64_t)(at / (uint32_t)s.part) * bins + ((item.x >> (shift + s.bits)) & (uint32_t)(bins - 1))], 1u);
+            }
         }
     }
 }

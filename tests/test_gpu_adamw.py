@@ -358,3 +358,40 @@ def test_wrapper_refuses_what_does_not_fit():
     h32 = B.tbn_adamw_tensors([p], [g], *B.tbn_adamw_state([p], 32))
     with pytest.raises(B.TbnError):
         B.tbn_adamw_unpack(h32)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("n", [256 * 9 + 5, 3_000_003])
+def test_alignment_does_not_change_the_result(bits, n):
+    """The same tensor where accesses of eight elements may begin, and one element further on: the same bits."""
+    a = make([n], F, H, bits, seed=60, copy=True)
+    shift = lambda x: None if x is None else cut(torch.cat([x[:1], x]), n, 1)  # noqa: E731
+    b = {k: [x.clone() if k.endswith("scale") and x is not None else shift(x) for x in v] for k, v in a.items()}
+    for t in (a, b):
+        h = B.tbn_adamw_tensors(**t, weight_decay=0.1)
+        for step in (4, 5):
+            B.tbn_adamw_step(h, step, 1e-3, seed=77)
+    for k in a:
+        assert all(x is None or torch.equal(x, y) for x, y in zip(a[k], b[k])), k
+
+
+def test_two_streams_at_once():
+    """Two optimizers stepped on two streams give what each gives alone."""
+    tensors = [make([200_000, 33, 4096], F, H, bits, seed=70 + bits) for bits in (8, 32)]
+    alone = [clone(t) for t in tensors]
+    for t in alone:
+        h = B.tbn_adamw_tensors(**t)
+        for step in range(1, 6):
+            _, scale = B.tbn_grad_norm(h, 0.1)
+            B.tbn_adamw_step(h, step, 1e-3, grad_scale=scale, seed=2)
+    torch.cuda.synchronize()
+    streams, handles = [torch.cuda.Stream() for _ in tensors], [B.tbn_adamw_tensors(**t) for t in tensors]
+    for step in range(1, 6):
+        for h, s in zip(handles, streams):
+            with torch.cuda.stream(s):
+                _, scale = B.tbn_grad_norm(h, 0.1)
+                B.tbn_adamw_step(h, step, 1e-3, grad_scale=scale, seed=2)
+    torch.cuda.synchronize()
+    for t, w in zip(tensors, alone):
+        for k in t:
+            assert all(x is None or torch.equal(x, y) for x, y in zip(t[k], w[k])), k

@@ -188,3 +188,38 @@ def test_nothing_is_written_outside_the_outputs_and_bits_repeat(d):
         assert (torch.isnan(edge) if math.isnan(fill) else edge == fill).all()
         runs.append(outs)
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("d", [96, 501, 1500, 2050])
+def test_a_row_does_not_depend_on_the_batch(d):
+    """y, dx and the statistics of a row are the same bits alone, among a few rows and among many.  Rows that are not whole pieces of eight
+    columns are added up from the aligned piece on that they begin in, in another order where they begin elsewhere: there the row's place
+    in its piece has to be the same."""
+    T, same = 1200, 8 // math.gcd(d, 8)
+    x, r, gamma, beta, dy, dsum = case(T, d, "bf16", "bf16", True, True, seed=80)
+    many = B.tbn_layernorm_train_fwd(x, gamma, beta, residual=r)
+    dx = B.tbn_layernorm_bwd(dy, *many[1:], gamma, dsum=dsum)[0]
+    for a, b in ((0, 1), (5, 8), (1100, 1160)):
+        a = a // same * same
+        few = B.tbn_layernorm_train_fwd(x[a:b].clone(), gamma, beta, residual=r[a:b].clone())
+        assert all(torch.equal(p, q[a:b]) for p, q in zip(few, many))
+        assert torch.equal(B.tbn_layernorm_bwd(dy[a:b].clone(), *few[1:], gamma, dsum=dsum[a:b].clone())[0], dx[a:b])
+
+
+def test_two_streams_at_once():
+    jobs = [case(3000, d, "bf16", "bf16", True, True, seed=90 + d) for d in (768, 501)]
+
+    def run(job):
+        x, r, gamma, beta, dy, dsum = job
+        y, *kept = B.tbn_layernorm_train_fwd(x, gamma, beta, residual=r)
+        return (y, *kept, *B.tbn_layernorm_bwd(dy, *kept, gamma, dsum=dsum))
+    want = [run(j) for j in jobs]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in jobs], []
+    for _ in range(4):
+        for j, s in zip(jobs, streams):
+            with torch.cuda.stream(s):
+                got.append(run(j))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i % 2]))
