@@ -585,7 +585,7 @@ struct NormDesc {
 template <int N> using NormTable = TableOf<NormDesc, N>;
 
 // Squares are added in 64 bits from the first one on: the factor that the norm gives enters every element of a step, and sums of 32 bits
-// would be off in its last bits.  |g| is made a 64-bit number by shifts of its bits (201 M bf16 gradients: 62 us; with the conversion
+// would be off in its last bits.  |g| is made a 64-bit number by shifts of its bits (201 M bf16 gradients: 70 us; with the conversion
 // instruction 144, with pairs of fp32 sums 100).  Zero and subnormal numbers become 2^-127 to 2^-126 that way: the last kernel takes a
 // sum below 2^-200 for 0.  Infinities and NaN become 2^128 and more: a thread whose sum is 2^256 goes over its elements again with the
 // conversion.
@@ -688,22 +688,26 @@ norm_kernel(const __grid_constant__ NormTable<N> tab, double *__restrict__ parti
     }
 }
 
-__global__ void __launch_bounds__(kThreads)
+// One block adds the thread blocks' sums, in an order that their number decides.
+__global__ void __launch_bounds__(1024)
 norm_final_kernel(const double *__restrict__ partial, int32_t count, double max_norm, float *__restrict__ norm, float *__restrict__ scale)
 {
-    __shared__ double red[kThreads];
+    __shared__ double red[32];
     pdl_launch_dependents();
     pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     double t = 0.0;
-    for (int32_t i = threadIdx.x; i < count; i += kThreads) t += partial[i];
-    red[threadIdx.x] = t;
+    for (int32_t i = threadIdx.x; i < count; i += 1024) t += partial[i];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+    if (lane == 0) red[warp] = t;
     __syncthreads();
-    for (int off = kThreads / 2; off > 0; off >>= 1) {
-        if ((int)threadIdx.x < off) red[threadIdx.x] += red[threadIdx.x + off];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) {
-        const double len = red[0] < 0x1p-200 ? 0.0 : sqrt(red[0]);
+    if (warp != 0) return;
+    t = red[lane];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) t += __shfl_xor_sync(0xffffffffu, t, off);
+    if (lane == 0) {
+        const double len = t < 0x1p-200 ? 0.0 : sqrt(t);
         if (norm) *norm = (float)len;
         const bool finite = len <= 1.7976931348623157e308;
         if (scale) *scale = !finite ? __int_as_float(0x7fffffff) : len > max_norm ? (float)(max_norm / len) : 1.0f;
@@ -837,7 +841,7 @@ int launch_norm(const tbn_adamw_tensor *tensors, int32_t count, double max_norm,
                        ? TBN_OK : TBN_ERR_CUDA;
         });
     if (rc != TBN_OK) return rc;
-    return launch_pdl(norm_final_kernel, dim3(1), dim3(kThreads), 0, s, static_cast<const double *>(partial), used, max_norm, norm, scale) ==
+    return launch_pdl(norm_final_kernel, dim3(1), dim3(1024), 0, s, static_cast<const double *>(partial), used, max_norm, norm, scale) ==
                    cudaSuccess ? TBN_OK : TBN_ERR_CUDA;
 }
 

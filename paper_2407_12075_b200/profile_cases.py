@@ -6,6 +6,8 @@ of launches):
 Cases: linear_k2, linear_k16 (8192 x 8192, T = 8192), bin_k2, bin_k16 (binary activations, 8192 x 8192, T = 4096),
 binbytes_k2, binbytes_k16 (the same with the activation signs as bytes),
 conv_s2 (64 -> 128, 32 x 32, batch 64), attention (64 images x 12 heads x 197 tokens), binarize, tile_bwd,
+norm_train (LayerNorm with residual and its gradient, 8192 x 2048), embedding (lookup and gradient, 16,384 tokens of 1024 over 20,011 ids),
+adamw, adamw8 (one step of 25 million elements, states in 32 or 8 bits, gradients clipped),
 head_xent, head_xent_f32, head_distill (forward and backward of a head over 8192 classes, 4096 tokens of 1024),
 first_conv (dense 3 -> 64, 32 x 32, batch 256), compact_gelu (second MLP layer of a ViT-B block fed the first layer's 384 distinct pre-activations, T = 25,216).
 Inputs are seeded device-side random values of the benchmark's shapes; every run checks the device status word.
@@ -98,6 +100,28 @@ def main():
         G = torch.randn(N, device=dev, generator=gen)
         _, tile, alpha = B.tbn_tile_fwd(W, k)
         run = lambda: B.tbn_tile_bwd(G, tile, alpha, W, k)
+    elif args.case == "norm_train":
+        T, d = 8192, 2048
+        x, r, dy = (torch.randn(T, d, device=dev, generator=gen).to(torch.bfloat16) for _ in range(3))
+        gamma, beta = torch.ones(d, device=dev), torch.zeros(d, device=dev)
+
+        def run():
+            _, s, mean, rstd = B.tbn_layernorm_train_fwd(x, gamma, beta, residual=r)
+            B.tbn_layernorm_bwd(dy, s, mean, rstd, gamma, dsum=r)
+    elif args.case == "embedding":
+        T, d, V = 16384, 1024, 20011
+        ids = (torch.rand(T, device=dev, generator=gen) ** 4 * V).to(torch.int64)
+        table = torch.randn(V, d, device=dev, generator=gen).to(torch.bfloat16)
+
+        def run():
+            B.tbn_embedding_bwd(ids, B.tbn_embedding_fwd(ids, table, 32.0), V, 32.0)
+    elif args.case in ("adamw", "adamw8"):
+        params = [torch.randn(5000, 5000, device=dev, generator=gen) * 0.02, torch.ones(5000, device=dev)]
+        grads = [(torch.randn(p.shape, device=dev, generator=gen) * 1e-3).to(torch.bfloat16) for p in params]
+        opt = B.tbn_adamw_tensors(params, grads, *B.tbn_adamw_state(params, 8 if args.case == "adamw8" else 32), weight_decay=[0.1, 0.0])
+
+        def run():
+            B.tbn_adamw_step(opt, 1, 1e-3, grad_scale=B.tbn_grad_norm(opt, 1.0)[1])
     else:
         raise SystemExit(f"unknown case {args.case}")
     for _ in range(args.reps):
