@@ -25,10 +25,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxWarps = 8;                // warps that share a row at most
 
-__device__ __forceinline__ float warp_sum(float v)
+// Sum over groups of SUB lanes.
+template <int SUB = 32> __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    for (int off = SUB / 2; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
 }
 // Threads of one row group meet; a group of one warp needs no barrier of its own.
@@ -45,25 +46,28 @@ template <> __device__ __forceinline__ float rounded<__nv_bfloat16>(float v) { r
 // How a call's rows and columns are spread over thread blocks, warps and lanes.
 struct Shape {
     int np, warps, groups;                  // pieces of eight columns to a lane, warps to a row, rows to a thread block
+    int sub;                                // lanes to a row: 32, or 4, 8 or 16 of narrow rows, several of which a warp works on
     int classes;                            // remainders (t d) mod unit that occur: thread block b takes rows t = b mod classes
     bool lng;
 };
 
 // What a lane has to do with the rows of its group.  EVEN: d is a multiple of eight, so that rows begin and end with whole pieces.
-template <int NP, bool EVEN> struct Lane {
+template <int NP, bool EVEN, int SUB> struct Lane {
     int32_t shift;                          // columns between the aligned piece that a row begins in and the row
-    int threads, group, warp, lane;         // of the group
+    int threads, group, lane;               // threads of a row's group; lane of the warp
+    bool first;                             // of the group's lanes
     int32_t at;                             // the lane's first column from the aligned start on; its next pieces are 256 columns apart
     int64_t row, row_step, rows;            // first row, from one to the next, how many
     int64_t total;                          // elements of the whole tensor
     uint32_t mask[NP];                      // which of a piece's eight columns are the row's
     __device__ __forceinline__ Lane(int64_t T, int32_t d, int warps, int groups, int classes)
     {
-        threads = warps * 32;
+        threads = SUB < 32 ? SUB : warps * 32;
         group = threadIdx.x / threads;
-        warp = (threadIdx.x >> 5) - group * warps;
         lane = threadIdx.x & 31;
-        at = (warp * NP * 32 + lane) * 8;
+        const int in_group = threadIdx.x - group * threads;
+        first = in_group == 0;
+        at = SUB < 32 ? in_group * 8 : ((in_group >> 5) * NP * 32 + lane) * 8;
         const int cls = EVEN ? 0 : blockIdx.x % classes;
         const int64_t first = (int64_t)(EVEN ? blockIdx.x : blockIdx.x / classes) * groups + group, step = (int64_t)(gridDim.x / classes) * groups;
         const int64_t here = (T - cls + classes - 1) / classes;      // rows of the class
@@ -88,22 +92,23 @@ template <int NP, bool EVEN> struct Lane {
 
 // Ring of a warp in shared memory.  A lane copies and takes its own pieces, so that nothing but its own copies is waited for.
 // start: of the row in x, plus the lane's first column.
-template <typename T, int NP, bool EVEN>
-__device__ __forceinline__ void fetch(uint32_t to, const T *x, int64_t start, const Lane<NP, EVEN> &l)
+template <typename T, int NP, bool EVEN, int SUB>
+__device__ __forceinline__ void fetch(uint32_t to, const T *x, int64_t start, const Lane<NP, EVEN, SUB> &l)
 {
     const T *from = x + start;
+    constexpr int kPer = 16 / (int)sizeof(T);
+    const bool whole = EVEN || start + (NP - 1) * 256 + 8 <= l.total;             // at the tensor's end a piece may be a part
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         if (l.mask[i] == 0) continue;
 #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-            constexpr int kPer = 16 / (int)sizeof(T);
             const uint32_t slot = to + (i * ((int)sizeof(T) / 2) + h) * 512;
             const T *f = from + i * 256 + h * kPer;
-            if (EVEN) {
+            if (whole) {
                 if (sizeof(T) == 2) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(f) : "memory");
                 else asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" :: "r"(slot), "l"(f) : "memory");
-            } else {                                                  // the tensor's last piece may be a part: what is behind it is not read
+            } else {                                                  // what is behind the end is not read
                 const int64_t left = l.total - start - i * 256 - h * kPer;
                 const int size = left >= kPer ? 16 : left > 0 ? (int)left * (int)sizeof(T) : 0;
                 if (size == 0) f = x;
@@ -122,7 +127,7 @@ __device__ __forceinline__ void keep(Pair (&v)[4], uint32_t mask)     // zero wh
     }
 }
 // Slots of pieces without columns hold zeros from the start on.
-template <typename T, int NP, bool EVEN> __device__ __forceinline__ void take(const char *from, int i, const Lane<NP, EVEN> &l, Pair (&v)[4])
+template <typename T, int NP, bool EVEN, int SUB> __device__ __forceinline__ void take(const char *from, int i, const Lane<NP, EVEN, SUB> &l, Pair (&v)[4])
 {
     Raw8<T> r;
     const uint4 *q = reinterpret_cast<const uint4 *>(from + i * (int)sizeof(T) / 2 * 512);
@@ -147,7 +152,7 @@ __device__ __forceinline__ void store16(__nv_bfloat16 *p, const Pair (&v)[4])
     spread8(v, f);
     store8(p, f);
 }
-template <typename T, int NP, bool EVEN> __device__ __forceinline__ void put(T *x, int64_t start, int i, const Lane<NP, EVEN> &l, const Pair (&v)[4])
+template <typename T, int NP, bool EVEN, int SUB> __device__ __forceinline__ void put(T *x, int64_t start, int i, const Lane<NP, EVEN, SUB> &l, const Pair (&v)[4])
 {
     T *p = x + start + i * 256;
     if (l.mask[i] == 0xffu) store16(p, v);
@@ -195,7 +200,7 @@ template <typename XT, typename YT, int NP> struct BackwardRing {
 
 // The mean and the centred second moment are taken per warp and joined over the warps of a row (of two sets of n1 and n2 values:
 // M2 = M2a + M2b + (mean_b - mean_a)^2 n1 n2 / (n1 + n2)), so that a group meets once a row.
-template <typename XT, typename YT, int NP, bool EVEN>
+template <typename XT, typename YT, int NP, bool EVEN, int SUB>
 __global__ void __launch_bounds__(kThreads, 2)
 forward_kernel(const ForwardArgs a, const Shape sh)
 {
@@ -204,8 +209,8 @@ forward_kernel(const ForwardArgs a, const Shape sh)
     extern __shared__ __align__(16) char smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const Lane<NP, EVEN> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
-    const int32_t room = sh.warps * NP * 256;
+    const Lane<NP, EVEN, SUB> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
+    const int32_t room = SUB < 32 ? SUB * 8 : sh.warps * NP * 256;
     float *gamma = reinterpret_cast<float *>(smem) + l.at, *beta = gamma + room;
     char *ring = smem + 2 * room * 4 + (threadIdx.x >> 5) * (R::kStages * R::kBytes) + l.lane * 16;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
@@ -214,7 +219,8 @@ forward_kernel(const ForwardArgs a, const Shape sh)
     YT *y = static_cast<YT *>(a.y);
     const int64_t step = l.row_step * a.d;                            // elements from one row to the next
     int64_t t = l.row, start = t * a.d - l.shift + l.at, ahead = start;
-    int32_t left = (int32_t)l.rows, coming = left;                    // rows to work on, to fetch
+    int32_t own = (int32_t)l.rows, coming = own;                      // rows to work on, to fetch
+    const int32_t turns = SUB < 32 ? (int32_t)__reduce_max_sync(0xffffffffu, (uint32_t)own) : own;       // of the warp's rows together
     auto get = [&](int slot) {
         if (coming > 0) {
             const uint32_t to = ring_at + slot * R::kBytes;
@@ -238,9 +244,10 @@ forward_kernel(const ForwardArgs a, const Shape sh)
     int32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < NP; ++i) mine += __popc(l.mask[i]);
-    const float n_warp = (float)__reduce_add_sync(0xffffffffu, mine), share = n_warp > 0.0f ? 1.0f / n_warp : 0.0f, inv_d = 1.0f / (float)a.d;
+    const float n_warp = SUB < 32 ? (float)a.d : (float)__reduce_add_sync(0xffffffffu, mine), share = n_warp > 0.0f ? 1.0f / n_warp : 0.0f, inv_d = 1.0f / (float)a.d;
     int turn = 0, slot = 0;
-    for (; left > 0; --left, turn ^= 1, t += l.row_step, start += step) {
+    for (int32_t k = 0; k < turns; ++k, turn ^= 1, t += l.row_step, start += step) {
+        const bool here = SUB == 32 || k < own;
         asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
         const char *from = ring + slot * R::kBytes;
         Pair v[NP][4], s = both(0.0f);
@@ -254,7 +261,7 @@ forward_kernel(const ForwardArgs a, const Shape sh)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[i][e] = add(v[i][e], r[e]);
                 round8<XT>(v[i]);
-                put(sum, start, i, l, v[i]);
+                if (here) put(sum, start, i, l, v[i]);
             }
         }
         get(slot == 0 ? R::kStages - 1 : slot - 1);                   // into the slot that was taken a row ago
@@ -264,7 +271,7 @@ forward_kernel(const ForwardArgs a, const Shape sh)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s = add(s, v[i][e]);
         const float2 s2 = split(s);
-        float n = n_warp, mean = warp_sum(s2.x + s2.y) * share;
+        float n = n_warp, mean = warp_sum<SUB>(s2.x + s2.y) * share;
         const float local = mean;
         Pair q2 = both(0.0f);
 #pragma unroll
@@ -278,8 +285,8 @@ forward_kernel(const ForwardArgs a, const Shape sh)
             }
         }
         const float2 qq = split(q2);
-        float q = warp_sum(qq.x + qq.y);
-        if (sh.warps > 1) {
+        float q = warp_sum<SUB>(qq.x + qq.y);
+        if (SUB == 32 && sh.warps > 1) {
             const float3 *all = part[turn] + l.group * sh.warps;
             if (l.lane == 0) part[turn][threadIdx.x >> 5] = make_float3(n, mean, q);
             group_sync(l.group, l.threads);
@@ -295,7 +302,7 @@ forward_kernel(const ForwardArgs a, const Shape sh)
             }
         }
         const float rstd = rsqrtf(q * inv_d + a.eps);
-        if (l.lane == 0 && l.warp == 0) {
+        if (l.first && here) {
             if (a.mean) a.mean[t] = mean;
             if (a.rstd) a.rstd[t] = rstd;
         }
@@ -307,7 +314,7 @@ forward_kernel(const ForwardArgs a, const Shape sh)
             read8(beta + i * 256, b);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[i][e] = fma2(mul(add(v[i][e], back), r2), w[e], b[e]);
-            put(y, start, i, l, v[i]);
+            if (here) put(y, start, i, l, v[i]);
         }
     }
 }
@@ -354,7 +361,7 @@ forward_long_kernel(const XT *__restrict__ x, const XT *__restrict__ residual, i
 }
 
 // A thread block walks over rows with a stride; a lane keeps its columns' share of dgamma and dbeta in registers to the end.
-template <typename XT, typename YT, int NP, bool EVEN>
+template <typename XT, typename YT, int NP, bool EVEN, int SUB>
 __global__ void __launch_bounds__(kThreads, NP == 4 ? 1 : 2)
 backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partial)
 {
@@ -363,8 +370,8 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
     extern __shared__ __align__(16) char smem[];
     pdl_launch_dependents();
     pdl_wait();
-    const Lane<NP, EVEN> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
-    const int32_t room = sh.warps * NP * 256;
+    const Lane<NP, EVEN, SUB> l(a.T, a.d, sh.warps, sh.groups, sh.classes);
+    const int32_t room = SUB < 32 ? SUB * 8 : sh.warps * NP * 256;
     const float *gamma = reinterpret_cast<const float *>(smem) + l.at;
     char *rings = smem + room * 4, *ring = rings + (threadIdx.x >> 5) * (R::kStages * R::kBytes) + l.lane * 16;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
@@ -373,7 +380,8 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
     XT *dx = static_cast<XT *>(a.dx);
     const int64_t step = l.row_step * a.d;
     int64_t start = l.row * a.d - l.shift + l.at, ahead = start;
-    int32_t left = (int32_t)l.rows, coming = left;
+    const int32_t own = (int32_t)l.rows, turns = SUB < 32 ? (int32_t)__reduce_max_sync(0xffffffffu, (uint32_t)own) : own;
+    int32_t coming = own;
     auto get = [&](int slot) {
         if (coming > 0) {
             const uint32_t to = ring_at + slot * R::kBytes;
@@ -408,11 +416,12 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
     const float inv_d = 1.0f / (float)a.d;
     const float *mean = a.mean + l.row, *rstd = a.rstd + l.row;
     float mu_next = 0.0f, rs_next = 0.0f;
-    if (left > 0) { mu_next = *mean; rs_next = *rstd; }
+    if (own > 0) { mu_next = *mean; rs_next = *rstd; }
     int turn = 0, slot = 0;
-    for (; left > 0; --left, turn ^= 1, start += step) {
+    for (int32_t k = 0; k < turns; ++k, turn ^= 1, start += step) {
+        const bool here = SUB == 32 || k < own;
         const Pair mu = both(-mu_next), rs = both(rs_next);
-        if (left > 1) { mean += l.row_step; rstd += l.row_step; mu_next = *mean; rs_next = *rstd; }
+        if (k + 1 < own) { mean += l.row_step; rstd += l.row_step; mu_next = *mean; rs_next = *rstd; }
         asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
         const char *from = ring + slot * R::kBytes;
         Pair g[NP][4], h[NP][4], s1 = both(0.0f), s2 = both(0.0f);
@@ -421,6 +430,10 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
             Pair w[4];
             take<XT>(from, i, l, h[i]);
             take<YT>(from + R::kX, i, l, g[i]);
+            if (!here) {                                              // the warp's other rows have one more
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[i][e] = g[i][e] = both(0.0f);
+            }
             read8(gamma + i * 256, w);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -433,8 +446,8 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
             }
         }
         const float2 p1 = split(s1), p2 = split(s2);
-        float t1 = warp_sum(p1.x + p1.y), t2 = warp_sum(p2.x + p2.y);
-        if (sh.warps > 1) {
+        float t1 = warp_sum<SUB>(p1.x + p1.y), t2 = warp_sum<SUB>(p2.x + p2.y);
+        if (SUB == 32 && sh.warps > 1) {
             const float2 *all = part[turn] + l.group * sh.warps;
             if (l.lane == 0) part[turn][threadIdx.x >> 5] = make_float2(t1, t2);
             group_sync(l.group, l.threads);
@@ -453,7 +466,7 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[i][e] = mul(fma2(h[i][e], m2, add(g[i][e], m1)), rs);
             }
-            put(dx, start, i, l, g[i]);
+            if (here) put(dx, start, i, l, g[i]);
         }
         get(slot == 0 ? R::kStages - 1 : slot - 1);                   // into the slot that was taken a row ago
         slot = slot + 1 == R::kStages ? 0 : slot + 1;
@@ -573,9 +586,12 @@ Shape shape_of(int32_t d, int most)
         if (warps > kMaxWarps || (np > most && least != 0x7fffffff)) continue;
         if (warps * np < least || (warps * np == least && warps < s.warps)) { least = warps * np; s.np = np; s.warps = (int)warps; }
     }
-    s.groups = kMaxWarps / s.warps;
+    s.sub = pieces <= 4 ? 4 : pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
+    s.groups = s.sub < 32 ? kThreads / s.sub : kMaxWarps / s.warps;
     return s;
 }
+int threads_of(const Shape &s) { return s.sub < 32 ? kThreads : s.groups * s.warps * 32; }
+size_t room_of(const Shape &s) { return (size_t)(s.sub < 32 ? s.sub * 8 : s.warps * s.np * 256) * 4; }        // of a row's columns as floats
 constexpr int kMostForward = 4, kMostBackward = 3;
 // Thread blocks: two to an SM, and no more than there are rows; as many of each class.
 int64_t blocks_of(int64_t T, const Shape &s, int per_sm)
@@ -600,15 +616,18 @@ cudaError_t launch(int64_t blocks, int per_sm, void (*kernel)(KArgs...), int thr
     return launch_spread(kernel, grid, block, smem, s, args...);
 }
 
-template <typename E, typename F> cudaError_t with_pieces(int np, E even, F f)
+template <int I> using Int = std::integral_constant<int, I>;
+template <typename E, typename F> cudaError_t with_pieces(const Shape &s, E even, F f)
 {
-    return np == 1 ? f(std::integral_constant<int, 1>{}, even) : np == 2 ? f(std::integral_constant<int, 2>{}, even)
-         : np == 3 ? f(std::integral_constant<int, 3>{}, even) : f(std::integral_constant<int, 4>{}, even);
+    if (s.sub < 32) return s.sub == 4 ? f(Int<1>{}, even, Int<4>{}) : s.sub == 8 ? f(Int<1>{}, even, Int<8>{}) : f(Int<1>{}, even, Int<16>{});
+    return s.np == 1 ? f(Int<1>{}, even, Int<32>{}) : s.np == 2 ? f(Int<2>{}, even, Int<32>{}) : s.np == 3 ? f(Int<3>{}, even, Int<32>{})
+                                                                                                       : f(Int<4>{}, even, Int<32>{});
 }
 template <typename F> cudaError_t with_shape(const Shape &s, F f)
 {
-    return s.classes == 1 ? with_pieces(s.np, std::true_type{}, f) : with_pieces(s.np, std::false_type{}, f);
+    return s.classes == 1 ? with_pieces(s, std::true_type{}, f) : with_pieces(s, std::false_type{}, f);
 }
+
 template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs &a, cudaStream_t s)
 {
     const Shape sh = shape_of(a.d, kMostForward);
@@ -618,16 +637,17 @@ template <typename XT, typename YT> cudaError_t forward_typed(const ForwardArgs 
                           static_cast<const XT *>(a.residual), a.T, a.d, a.gamma, a.beta, a.eps, static_cast<XT *>(a.sum), static_cast<YT *>(a.y), a.mean,
                           a.rstd);
     }
-    return with_shape(sh, [&](auto np, auto even) {
+    return with_shape(sh, [&](auto np, auto even, auto sub) {
         constexpr int NP = decltype(np)::value;
         constexpr bool EVEN = decltype(even)::value;
+        constexpr int SUB = decltype(sub)::value;
         typedef ForwardRing<XT, YT, NP> R;
-        const size_t smem = (size_t)2 * sh.warps * NP * 256 * 4 + (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
+        const size_t smem = 2 * room_of(sh) + (size_t)threads_of(sh) / 32 * R::kStages * R::kBytes;
         static std::atomic<uint64_t> done;
-        const cudaError_t e = allow_smem(forward_kernel<XT, YT, NP, EVEN>, done);
+        const cudaError_t e = allow_smem(forward_kernel<XT, YT, NP, EVEN, SUB>, done);
         if (e != cudaSuccess) return e;
         const int per_sm = smem <= kHalf ? 2 : 1;
-        return launch(blocks_of(a.T, sh, per_sm), per_sm, forward_kernel<XT, YT, NP, EVEN>, sh.groups * sh.warps * 32, smem, s, a, sh);
+        return launch(blocks_of(a.T, sh, per_sm), per_sm, forward_kernel<XT, YT, NP, EVEN, SUB>, threads_of(sh), smem, s, a, sh);
     });
 }
 
@@ -649,19 +669,20 @@ template <typename XT, typename YT> cudaError_t backward_typed(const BackwardArg
             e = launch_pdl(column_sums_kernel<XT, YT>, dim3(slabs < 4096 ? slabs : 4096, parts), dim3(kThreads), 0, s, dy, x, a.T, a.d, a.mean,
                            a.rstd, partial);
     } else {
-        e = with_shape(sh, [&](auto np, auto even) {
+        e = with_shape(sh, [&](auto np, auto even, auto sub) {
             constexpr int NP = decltype(np)::value;
         constexpr bool EVEN = decltype(even)::value;
+        constexpr int SUB = decltype(sub)::value;
             typedef BackwardRing<XT, YT, NP> R;
-            const size_t room = (size_t)sh.warps * NP * 256 * 4, rings = (size_t)sh.groups * sh.warps * R::kStages * R::kBytes;
+            const size_t room = room_of(sh), rings = (size_t)threads_of(sh) / 32 * R::kStages * R::kBytes;
             const size_t sums_room = (size_t)sh.groups * 2 * room;    // the same space as the rings, which are larger
             const size_t smem = room + (rings > sums_room ? rings : sums_room);
             static std::atomic<uint64_t> done;
-            const cudaError_t e1 = allow_smem(backward_kernel<XT, YT, NP, EVEN>, done);
+            const cudaError_t e1 = allow_smem(backward_kernel<XT, YT, NP, EVEN, SUB>, done);
             if (e1 != cudaSuccess) return e1;
             const int per_sm = NP < 4 && smem <= kHalf ? 2 : 1;
             parts = one_block(a.T, sh) ? 1 : (int32_t)blocks_of(a.T, sh, per_sm);
-            return launch(parts, per_sm, backward_kernel<XT, YT, NP, EVEN>, sh.groups * sh.warps * 32, smem, s, a, sh, partial);
+            return launch(parts, per_sm, backward_kernel<XT, YT, NP, EVEN, SUB>, threads_of(sh), smem, s, a, sh, partial);
         });
     }
     if (e != cudaSuccess || !sums || (!sh.lng && parts == 1)) return e;            // one thread block has written them

@@ -45,7 +45,7 @@ def case(T, d, x_dtype, y_dtype, residual, affine, seed=0):
 
 
 SHAPES = [(1, 1), (3, 2), (2, 31), (5, 64), (1, 255), (7, 256), (9, 257), (33, 501), (4, 768), (1000, 96), (130, 1024), (17, 2047), (6, 2048), (5, 2056),
-          (3, 4096), (2, 4097), (3, 8192), (2, 8200), (2, 20001), (3000, 40), (1, 8200), (1, 8192), (1, 20001), (32, 512), (33, 512), (16, 255), (70, 20001)]
+          (3, 4096), (2, 4097), (3, 8192), (2, 8200), (2, 20001), (3000, 40), (1, 8200), (1, 8192), (1, 20001), (32, 512), (33, 512), (16, 255), (70, 20001), (500, 32), (77, 16), (5000, 24), (301, 63), (900, 100), (129, 128), (1300, 121)]
 
 
 @pytest.mark.parametrize("T,d", SHAPES)
