@@ -847,11 +847,11 @@ class _AdamWTensor(ctypes.Structure):
 class AdamWTensors:
     """The tensors of an optimizer, as tbn_adamw_tensors describes them to the library: made once, used in every step.  It keeps the
     tensors alive; they are updated in place and must stay the tensors they are (new gradients are written into the same ones)."""
-    __slots__ = ("table", "at", "count", "device", "kept", "state_bits")
+    __slots__ = ("table", "at", "count", "device", "kept")
 
-    def __init__(self, table, device, kept, state_bits):
+    def __init__(self, table, device, kept):
         self.table, self.at, self.count = table, ctypes.addressof(table), len(kept)
-        self.device, self.kept, self.state_bits = device, kept, state_bits
+        self.device, self.kept = device, kept
 
 
 def tbn_adamw_state(params, bits: int = 8):
@@ -875,7 +875,7 @@ def tbn_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=No
     decay = [float(w) for w in weight_decay] if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
     if any(len(c) != n for c in (grads, m, v, m_scale, v_scale, copies, decay)):
         raise TbnError(-2, "adamw: lists of different lengths")
-    table, kept, bits_seen = (_AdamWTensor * max(n, 1))(), [], set()
+    table, kept = (_AdamWTensor * max(n, 1))(), []
     device = params[0].device if n else torch.device("cuda", torch.cuda.current_device() if torch.cuda.is_available() else 0)
     for i, (p, g, a, b, sa, sb, c) in enumerate(zip(params, grads, m, v, m_scale, v_scale, copies)):
         size = p.numel()
@@ -895,8 +895,7 @@ def tbn_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=No
         ptr = lambda t: _ptr(t) if t is not None and t.numel() else None  # noqa: E731
         table[i] = _AdamWTensor(ptr(p), ptr(g), ptr(a), ptr(b), ptr(sa), ptr(sb), ptr(c), size, decay[i], _code(p), _code(g), bits)
         kept.append((p, g, a, b, sa, sb, c))
-        bits_seen.add(bits)
-    return AdamWTensors(table, device, kept, bits_seen)
+    return AdamWTensors(table, device, kept)
 
 
 def tbn_grad_norm(tensors: AdamWTensors, max_norm: float, workspace: torch.Tensor | None = None):

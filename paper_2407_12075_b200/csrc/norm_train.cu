@@ -60,6 +60,7 @@ template <int NP, bool EVEN, int SUB> struct Lane {
     int64_t row, row_step, rows;            // first row, from one to the next, how many
     int64_t total;                          // elements of the whole tensor
     uint32_t mask[NP];                      // which of a piece's eight columns are the row's
+    uint32_t edges;                         // pieces of which a lane of the warp has a part
     __device__ __forceinline__ Lane(int64_t T, int32_t d, int warps, int groups, int classes)
     {
         threads = SUB < 32 ? SUB : warps * 32;
@@ -86,6 +87,12 @@ template <int NP, bool EVEN, int SUB> struct Lane {
                     const int32_t c = at + i * 256 + e - shift;
                     if (c >= 0 && c < d) mask[i] |= 1u << e;
                 }
+        }
+        edges = 0;
+        if (!EVEN) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+                if (__any_sync(0xffffffffu, mask[i] != 0 && mask[i] != 0xffu)) edges |= 1u << i;
         }
     }
 };
@@ -118,14 +125,39 @@ __device__ __forceinline__ void fetch(uint32_t to, const T *x, int64_t start, co
         }
     }
 }
-__device__ __forceinline__ void keep(Pair (&v)[4], uint32_t mask)     // zero where there is no column
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float2 f = split(v[e]);
-        v[e] = pair(mask >> (2 * e) & 1u ? f.x : 0.0f, mask >> (2 * e + 1) & 1u ? f.y : 0.0f);
+// A piece's eight mask bits as the signs of eight bytes, which a byte permutation spreads over a value's bits.
+struct Signs {
+    uint32_t lo, hi;
+    __device__ __forceinline__ explicit Signs(uint32_t mask)
+        : lo((((mask & 15u) * 0x00204081u) & 0x01010101u) * 0x80u), hi((((mask >> 4) * 0x00204081u) & 0x01010101u) * 0x80u) {}
+    template <uint32_t SELECT> static __device__ __forceinline__ uint32_t spread(uint32_t s)
+    {
+        uint32_t r;
+        asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(s), "n"(SELECT));
+        return r;
     }
-}
+    __device__ __forceinline__ void keep(Raw8<__nv_bfloat16> &r) const
+    {
+        r.w[0] &= spread<0x9988>(lo); r.w[1] &= spread<0xbbaa>(lo);
+        r.w[2] &= spread<0x9988>(hi); r.w[3] &= spread<0xbbaa>(hi);
+    }
+    __device__ __forceinline__ void keep(Raw8<float> &r) const
+    {
+        r.w[0] &= spread<0x8888>(lo); r.w[1] &= spread<0x9999>(lo); r.w[2] &= spread<0xaaaa>(lo); r.w[3] &= spread<0xbbbb>(lo);
+        r.w[4] &= spread<0x8888>(hi); r.w[5] &= spread<0x9999>(hi); r.w[6] &= spread<0xaaaa>(hi); r.w[7] &= spread<0xbbbb>(hi);
+    }
+    __device__ __forceinline__ void keep(Pair (&v)[4]) const          // zero where there is no column
+    {
+        Raw8<float> r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 f = split(v[e]);
+            r.w[2 * e] = __float_as_uint(f.x); r.w[2 * e + 1] = __float_as_uint(f.y);
+        }
+        keep(r);
+        unpack8(r, v);
+    }
+};
 // Slots of pieces without columns hold zeros from the start on.
 template <typename T, int NP, bool EVEN, int SUB> __device__ __forceinline__ void take(const char *from, int i, const Lane<NP, EVEN, SUB> &l, Pair (&v)[4])
 {
@@ -136,8 +168,8 @@ template <typename T, int NP, bool EVEN, int SUB> __device__ __forceinline__ voi
         const uint4 x = q[h * 32];
         r.w[4 * h] = x.x; r.w[4 * h + 1] = x.y; r.w[4 * h + 2] = x.z; r.w[4 * h + 3] = x.w;
     }
+    if (!EVEN && (l.edges >> i & 1u)) Signs(l.mask[i]).keep(r);
     unpack8(r, v);
-    if (!EVEN && l.mask[i] != 0xffu) keep(v, l.mask[i]);
 }
 __device__ __forceinline__ void store16(float *p, const Pair (&v)[4])
 {
@@ -278,8 +310,8 @@ forward_kernel(const ForwardArgs a, const Shape sh)
         for (int i = 0; i < NP; ++i) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[i][e] = add(v[i][e], both(-local));
-            if (!EVEN && l.mask[i] != 0xffu) keep(v[i], l.mask[i]);
-            if (!EVEN || l.mask[i] != 0) {
+            if (!EVEN && (l.edges >> i & 1u)) Signs(l.mask[i]).keep(v[i]);
+            if (l.mask[i] != 0) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) q2 = fma2(v[i][e], v[i][e], q2);
             }
