@@ -442,6 +442,10 @@ __device__ __forceinline__ void step_block(const Cursor<PT, GT, VEC, true> &at, 
     vs = __fmul_rn(v_top, kVPart);
 }
 
+// One step of the tensors of one kind.  32-bit states: HBM; 134 M elements with a bf16 copy take 657 us (6.1 TB/s).  8-bit states: HBM and the
+// rate at which instructions issue (66 for an element); 201 M elements with fp32 parameters and bf16 gradients take 546 us (5.2 TB/s; reads
+// and writes alone 514 in this order), 20.6 M with bf16 parameters 67.  A warp has its blocks in a row: their scales are whole sectors, where
+// scales written one by one cost 60 us more at 201 M, and memory is gone through in long stretches (blocks dealt out in turn: 602 us).
 template <int N, typename PT, typename GT, bool EIGHT>
 __global__ void __launch_bounds__(kThreads, step_per_sm(EIGHT))
 step_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ Coef host, const __grid_constant__ Hyper h)
@@ -536,6 +540,7 @@ step_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ Coef h
 }
 
 // ---- values of 8-bit states ---------------------------------------------------------------------------------------------
+// Two bytes read and eight written an element: 355 us for 201 M (5.7 TB/s), what a stream of mostly writes reaches.
 struct UnpackDesc {
     const uint8_t *m, *v;
     const float *ms, *vs;
