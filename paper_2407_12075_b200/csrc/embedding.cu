@@ -22,40 +22,57 @@ constexpr int kThreads = 256;
 
 __device__ __forceinline__ bool inside(int64_t id, int32_t V, int64_t padding) { return id >= 0 && id < V && id != padding; }
 
-// Eight values in a row from any element on.  At odd places they are cut out of the two or three aligned pieces that hold them, unless
-// one of those reaches behind `end`, the tensor's.
-__device__ __forceinline__ void load_any(const __nv_bfloat16 *p, const __nv_bfloat16 *end, bool aligned, Raw8<__nv_bfloat16> &r)
+// Eight values in a row, 16-byte aligned.
+__device__ __forceinline__ void load_row(const __nv_bfloat16 *p, Raw8<__nv_bfloat16> &r) { r = load8(p); }
+__device__ __forceinline__ void load_row(const float *p, Raw8<float> &r)
 {
-    if (aligned) { r = load8(p); return; }
-    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / 2;        // 0 .. 7
-    const __nv_bfloat16 *q = p - off;
-    if (q + 16 > end) {
-        uint32_t h[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = __bfloat16_as_ushort(p[e]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r.w[e] = h[2 * e] | h[2 * e + 1] << 16;
-        return;
-    }
-    const Raw8<__nv_bfloat16> a = load8(q), b = load8(q + 8);
-    uint32_t w[6] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1]}, x[5];
-    const bool two = off & 4, one = off & 2;                          // words to leave out, in two steps: 2, then 1
-    const uint32_t v[7] = {two ? w[2] : w[0], two ? w[3] : w[1], two ? w[4] : w[2], two ? w[5] : w[3], two ? b.w[2] : w[4], two ? b.w[3] : w[5], 0};
-#pragma unroll
-    for (int e = 0; e < 5; ++e) x[e] = one ? v[e + 1] : v[e];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r.w[e] = off & 1 ? __funnelshift_r(x[e], x[e + 1], 16) : x[e];
+    const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
+    r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
 }
-__device__ __forceinline__ void load_any(const float *p, const float *end, bool aligned, Raw8<float> &r)
-{
-    if (aligned) {
-        const uint4 a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1];
-        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w; r.w[4] = b.x; r.w[5] = b.y; r.w[6] = b.z; r.w[7] = b.w;
-        return;
-    }
+// Eight values in a row from any element on, asked for (ask) and put together (take) apart, so that several are on their way at a time.
+// bf16: cut out of the two aligned pieces that hold them, or value by value where the second reaches behind `end`, the tensor's.
+template <typename T, bool ALIGNED> struct OddPiece {
+    Raw8<T> r;
+    __device__ __forceinline__ void ask(const T *p, const T *)
+    {
+        if (ALIGNED) load_row(p, r);
+        else
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r.w[e] = __float_as_uint(p[e]);
-}
+            for (int e = 0; e < 8; ++e) r.w[e % (int)(sizeof(r.w) / 4)] = __float_as_uint(value_of(p[e]));     // fp32
+    }
+    __device__ __forceinline__ Raw8<T> take(const T *, const T *) const { return r; }
+};
+template <> struct OddPiece<__nv_bfloat16, false> {
+    Raw8<__nv_bfloat16> r;
+    uint4 second;
+    static __device__ __forceinline__ uint32_t off(const __nv_bfloat16 *p) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / 2; }
+    __device__ __forceinline__ void ask(const __nv_bfloat16 *p, const __nv_bfloat16 *end)
+    {
+        const __nv_bfloat16 *q = p - off(p), *q2 = q + 16 <= end ? q + 8 : q;
+        const uint4 a = *reinterpret_cast<const uint4 *>(q);
+        second = *reinterpret_cast<const uint4 *>(q2);
+        r.w[0] = a.x; r.w[1] = a.y; r.w[2] = a.z; r.w[3] = a.w;
+    }
+    __device__ __forceinline__ Raw8<__nv_bfloat16> take(const __nv_bfloat16 *p, const __nv_bfloat16 *end) const
+    {
+        Raw8<__nv_bfloat16> o;
+        const uint32_t k = off(p);
+        if (p - k + 16 > end && k != 0) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o.w[e] = __bfloat16_as_ushort(p[2 * e]) | (uint32_t)__bfloat16_as_ushort(p[2 * e + 1]) << 16;
+            return o;
+        }
+        const bool two = k & 4, one = k & 2;                          // words to leave out, in two steps: 2, then 1
+        const uint32_t v[6] = {two ? r.w[2] : r.w[0], two ? r.w[3] : r.w[1], two ? second.x : r.w[2], two ? second.y : r.w[3],
+                               two ? second.z : second.x, two ? second.w : second.y};
+        uint32_t x[5];
+#pragma unroll
+        for (int e = 0; e < 5; ++e) x[e] = one ? v[e + 1] : v[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o.w[e] = __funnelshift_r(x[e], x[e + 1], k & 1 ? 16 : 0);
+        return o;
+    }
+};
 __device__ __forceinline__ void store_row(float *p, const float (&v)[8])          // 16-byte aligned
 {
     reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
@@ -63,18 +80,17 @@ __device__ __forceinline__ void store_row(float *p, const float (&v)[8])        
 }
 __device__ __forceinline__ void store_row(__nv_bfloat16 *p, const float (&v)[8]) { store8(p, v); }
 // The eight columns from c on of row `row` of a table, scaled; what is behind column d is left as it is in v.
-template <typename WT> struct DenseRows {
+template <typename WT, bool EVEN> struct DenseRows {
     const WT *table, *end;
     int32_t d;
-    bool even;
     float scale;
     struct Row { const WT *at; };
     __device__ __forceinline__ Row row(int64_t id) const { return {table + id * d}; }
-    typedef Raw8<WT> Piece;
-    __device__ __forceinline__ void load(const Row &r, int32_t c, Piece &p) const { load_any(r.at + c, end, even, p); }
-    __device__ __forceinline__ void values(const Row &, int32_t, const Piece &p, float (&v)[8]) const
+    typedef OddPiece<WT, EVEN> Piece;
+    __device__ __forceinline__ void load(const Row &r, int32_t c, Piece &p) const { p.ask(r.at + c, end); }
+    __device__ __forceinline__ void values(const Row &r, int32_t c, const Piece &p, float (&v)[8]) const
     {
-        unpack8(p, v);
+        unpack8(p.take(r.at + c, end), v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= scale;
     }
@@ -158,7 +174,8 @@ lookup_kernel(const LookupArgs a, const ROWS rows, int32_t segs)
     }
 }
 
-// Other rows: y as one array, an aligned piece of eight to a thread; pieces that lie in two rows or more go value by value.
+// Other rows: y as one array, an aligned piece of eight to a thread.  (Several to a thread: 8192 x 2047 bf16 5 to 15 us slower.)  The values of
+// a piece that lies in two rows are asked for together, one by one where rows are shorter than a piece.
 template <typename ROWS, typename YT>
 __global__ void __launch_bounds__(kThreads)
 lookup_odd_kernel(const LookupArgs a, const ROWS rows)
@@ -169,9 +186,9 @@ lookup_odd_kernel(const LookupArgs a, const ROWS rows)
     YT *y = static_cast<YT *>(a.y);
     int64_t t = total <= 0x7fffffff ? (int64_t)((uint32_t)o / (uint32_t)a.d) : o / a.d;
     int32_t c = (int32_t)(o - t * a.d);
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    int64_t id = a.ids[t];
     if (c + 8 <= a.d) {
-        const int64_t id = a.ids[t];
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (inside(id, a.V, a.padding)) {
             const typename ROWS::Row row = rows.row(id);
             typename ROWS::Piece p;
@@ -179,12 +196,29 @@ lookup_odd_kernel(const LookupArgs a, const ROWS rows)
             rows.values(row, c, p, v);
         }
         store_row(y + o, v);
-        return;
-    }
-    for (int e = 0; e < 8 && o + e < total; ++e) {
-        const int64_t id = a.ids[t];
-        store_from_float(y, o + e, inside(id, a.V, a.padding) ? rows.one(rows.row(id), c) : 0.0f);
-        if (++c == a.d) { c = 0; ++t; }
+    } else if (a.d >= 8) {
+        const int32_t here = a.d - c;                                 // of the first row; the rest is the next one's, if there is one
+        const int64_t id2 = t + 1 < a.T ? a.ids[t + 1] : -1;
+        const bool in = inside(id, a.V, a.padding), in2 = inside(id2, a.V, a.padding);
+        const typename ROWS::Row row = rows.row(in ? id : 0), row2 = rows.row(in2 ? id2 : 0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (e < here) { if (in) v[e] = rows.one(row, c + e); }
+            else if (in2) v[e] = rows.one(row2, e - here);
+        }
+        if (o + 8 <= total) store_row(y + o, v);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (o + e < total) store_from_float(y, o + e, v[e]);
+    } else {
+        for (int e = 0; e < 8 && o + e < total; ++e) {
+            store_from_float(y, o + e, inside(id, a.V, a.padding) ? rows.one(rows.row(id), c) : 0.0f);
+            if (++c == a.d) {
+                c = 0;
+                ++t;
+                id = t < a.T ? a.ids[t] : -1;
+            }
+        }
     }
 }
 
@@ -415,24 +449,39 @@ rank_kernel(const Sort s, const Fill f, unsigned rankers)
 }
 
 // ---- sums -------------------------------------------------------------------------------------------------------------------
-// A lane's eight columns of a row of dw (from column c on): what was there (of aligned rows: `old`, loaded ahead) and the sum, written.
+// Columns of a row of dw are taken in the aligned pieces that cover it: piece c / 8 begins at column c - shift, shift = (id d) mod 8 (0 where
+// d is a multiple of eight: EVEN).  The same columns of dy's rows begin anywhere.
+template <bool EVEN> __device__ __forceinline__ int32_t shift_of(uint32_t id, int32_t d) { return EVEN ? 0 : (int32_t)((id * (uint32_t)d) & 7u); }
+template <bool EVEN> __device__ __forceinline__ bool all_in(int32_t c, int32_t d) { return EVEN ? c < d : c >= 0 && c + 8 <= d; }
+template <bool EVEN> __device__ __forceinline__ bool some_in(int32_t c, int32_t d) { return EVEN ? c < d : c > -8 && c < d; }
+
+// A row's columns of a piece at its ends, zeros beside them; all asked for together.
+template <typename T> __device__ __forceinline__ void load_part(const T *row, int32_t c, int32_t d, Raw8<T> &r)
+{
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = c + e >= 0 && c + e < d ? __float_as_uint(value_of(row[c + e])) : 0u;
+    if (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.w[e % (int)(sizeof(r.w) / 4)] = h[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.w[e] = h[2 * e] >> 16 | (h[2 * e + 1] & 0xffff0000u);
+    }
+}
+// A lane's eight columns of a row of dw, from column c on: what was there (`old`, loaded ahead) and the sum, written.
 template <bool EVEN, bool ADD, typename WT>
 __device__ __forceinline__ void write_sum(WT *row, int32_t c, int32_t d, const float (&acc)[8], float scale, const Raw8<WT> &old)
 {
-    if (c >= d) return;
-    if (EVEN) {
-        float o[8];
-        if (ADD) unpack8(old, o);
+    if (!some_in<EVEN>(c, d)) return;
+    float o[8];
+    if (ADD) unpack8(old, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = ADD ? fmaf(scale, acc[e], o[e]) : scale * acc[e];
-        store_row(row + c, o);
-    } else {
+    for (int e = 0; e < 8; ++e) o[e] = ADD ? fmaf(scale, acc[e], o[e]) : scale * acc[e];
+    if (all_in<EVEN>(c, d)) store_row(row + c, o);
+    else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (c + e >= d) break;
-            store_from_float(row, c + e, ADD ? fmaf(scale, acc[e], value_of(row[c + e])) : scale * acc[e]);
-        }
-    }
+        for (int e = 0; e < 8; ++e) if (c + e >= 0 && c + e < d) store_from_float(row, c + e, o[e]);
 }
 // Sums of pieces lie in rows of `pitch` floats (a multiple of eight).
 __device__ __forceinline__ void put_partial(float *row, int32_t c, const float (&acc)[8]) { store_row(row + c, acc); }
@@ -446,7 +495,7 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
            const GT *__restrict__ dy, WT *dw, float *__restrict__ partial, int32_t pitch)
 {
     // rows of dy loaded before the first is added, with the rows of dw that sums beginning there will be added to
-    constexpr int kAhead = ADD ? 8 / NP / (NP > 1 ? 1 : 2) : NP == 1 ? 8 : sizeof(GT) == 2 ? 8 / NP * 2 : 8 / NP;
+    constexpr int kAhead = ADD ? 8 / NP / (NP > 1 ? 1 : 2) : NP == 1 ? 8 : sizeof(GT) == 2 && EVEN ? 8 / NP * 2 : 8 / NP;
     pdl_wait();
     const int lane = threadIdx.x & 31;
     const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
@@ -468,11 +517,12 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
         if (from_left || to_right) {
             float *row = partial + (k * 2 + (from_left ? 0 : 1)) * pitch;
 #pragma unroll
-            for (int j = 0; j < NP; ++j) if (c0 + j * 256 < d) put_partial(row, c0 + j * 256, acc[j]);
+            for (int j = 0; j < NP; ++j) if (c0 + j * 256 < pitch) put_partial(row, c0 + j * 256, acc[j]);
         } else {
             WT *row = dw + (int64_t)cur * d;
+            const int32_t shift = shift_of<EVEN>(cur, d);
 #pragma unroll
-            for (int j = 0; j < NP; ++j) write_sum<EVEN, ADD>(row, c0 + j * 256, d, acc[j], scale, old[j]);
+            for (int j = 0; j < NP; ++j) write_sum<EVEN, ADD>(row, c0 + j * 256 - shift, d, acc[j], scale, old[j]);
         }
     };
 #pragma unroll 1
@@ -481,8 +531,8 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
             item = make_uint2(0xffffffffu, 0);
             if (i0 + lane < n) item = list[a + i0 + lane];
         }
-        Raw8<GT> r[kAhead][NP];
-        Raw8<WT> there[ADD && EVEN ? kAhead : 1][NP];
+        OddPiece<GT, EVEN> r[kAhead][NP];
+        Raw8<WT> there[ADD ? kAhead : 1][NP];
         uint32_t before = cur;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -490,51 +540,47 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
             const bool starts = key != before;
             before = key;
             if (key >= (uint32_t)V) continue;                         // beyond the piece: a key of 2^32 - 1
-            if (ADD && EVEN && starts) {
+            const int32_t shift = shift_of<EVEN>(key, d);
+            if (ADD && starts) {
 #pragma unroll
-                for (int j = 0; j < NP; ++j)
-                    if (c0 + j * 256 < d) load_any(dw + (int64_t)key * d + c0 + j * 256, dw, true, there[ADD && EVEN ? i : 0][j]);
+                for (int j = 0; j < NP; ++j) {
+                    const int32_t c = c0 + j * 256 - shift;
+                    if (all_in<EVEN>(c, d)) load_row(dw + (int64_t)key * d + c, there[ADD ? i : 0][j]);
+                    else if (some_in<EVEN>(c, d)) load_part(dw + (int64_t)key * d, c, d, there[ADD ? i : 0][j]);
+                }
             }
             const GT *row = dy + (int64_t)tok * d;
 #pragma unroll
             for (int j = 0; j < NP; ++j) {
-                const int32_t c = c0 + j * 256;
-                if (EVEN ? c < d : c + 8 <= d) {
-                    load_any(row + c, end, EVEN, r[i][j]);
-                } else if (!EVEN && c < d) {
-                    uint32_t h[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) h[e] = c + e < d ? __float_as_uint(value_of(row[c + e])) : 0u;
-                    if (sizeof(GT) == 4) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) r[i][j].w[e % (int)(sizeof(r[i][j].w) / 4)] = h[e];
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) r[i][j].w[e] = h[2 * e] >> 16 | (h[2 * e + 1] & 0xffff0000u);
-                    }
+                const int32_t c = c0 + j * 256 - shift;
+                if (all_in<EVEN>(c, d)) {
+                    r[i][j].ask(row + c, end);
+                } else if (!EVEN && some_in<EVEN>(c, d)) {
+                    load_part(row, c, d, r[i][j].r);
                 }
             }
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const uint32_t key = __shfl_sync(0xffffffffu, item.x, (i0 + i) & 31);
+            const uint32_t key = __shfl_sync(0xffffffffu, item.x, (i0 + i) & 31), tok = EVEN ? 0 : __shfl_sync(0xffffffffu, item.y, (i0 + i) & 31);
             if (i0 + i >= n) break;
             const bool starts = key != cur;
             if (starts) {
                 put(false);
                 from_left = i0 + i == 0 && key == left;
                 cur = key;
-                if (ADD && EVEN) {
+                if (ADD) {
 #pragma unroll
-                    for (int j = 0; j < NP; ++j) old[j] = there[ADD && EVEN ? i : 0][j];
+                    for (int j = 0; j < NP; ++j) old[j] = there[ADD ? i : 0][j];
                 }
             }
             if (key >= (uint32_t)V) continue;
 #pragma unroll
             for (int j = 0; j < NP; ++j) {
-                if (c0 + j * 256 >= d) continue;
+                const int32_t c = c0 + j * 256 - shift_of<EVEN>(key, d);
+                if (!some_in<EVEN>(c, d)) continue;
                 float v[8];
-                unpack8(r[i][j], v);
+                unpack8(!EVEN && all_in<EVEN>(c, d) ? r[i][j].take(dy + (int64_t)tok * d + c, end) : r[i][j].r, v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[j][e] = starts ? v[e] : acc[j][e] + v[e];
             }
@@ -579,12 +625,12 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
         }
     }
     auto add_up = [&](int64_t from, int64_t lo, int64_t hi, float (&acc)[8]) {          // partials lo .. hi of the run of piece `from`
-        if (c >= d) return;
+        if (c >= pitch) return;
         int64_t i = lo;
         for (; i + 8 <= hi; i += 8) {
             Raw8<float> r[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) load_any(partial + ((from + i + j) * 2 + (i + j == 0 ? 1 : 0)) * pitch + c, partial, true, r[j]);
+            for (int j = 0; j < 8; ++j) load_row(partial + ((from + i + j) * 2 + (i + j == 0 ? 1 : 0)) * pitch + c, r[j]);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -592,20 +638,22 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
         }
         for (; i < hi; ++i) {
             Raw8<float> r;
-            load_any(partial + ((from + i) * 2 + (i == 0 ? 1 : 0)) * pitch + c, partial, true, r);
+            load_row(partial + ((from + i) * 2 + (i == 0 ? 1 : 0)) * pitch + c, r);
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] += __uint_as_float(r.w[e]);
         }
     };
     auto row_there = [&](uint32_t id, Raw8<WT> &old) {
-        if (ADD && EVEN && c < d) load_any(dw + (int64_t)id * d + c, dw, true, old);
+        const int32_t at = c - shift_of<EVEN>(id, d);
+        if (ADD && all_in<EVEN>(at, d)) load_row(dw + (int64_t)id * d + at, old);
+        else if (ADD && some_in<EVEN>(at, d)) load_part(dw + (int64_t)id * d, at, d, old);
     };
     if (n > 0 && n <= kAlone) {
         float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         Raw8<WT> old;
         row_there(key, old);
         add_up(k, 0, n + 1, acc);
-        write_sum<EVEN, ADD>(dw + (int64_t)key * d, c, d, acc, scale, old);
+        write_sum<EVEN, ADD>(dw + (int64_t)key * d, c - shift_of<EVEN>(key, d), d, acc, scale, old);
     }
     if (lane == 0) { more[warp] = n > kAlone ? n : 0; key_at[warp] = key; }
     __syncthreads();
@@ -623,7 +671,7 @@ join_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 for (int i = 1; i < kWarps; ++i) acc[e] += red[i][e * 32 + lane];
-            write_sum<EVEN, ADD>(dw + (int64_t)key_at[j] * d, c, d, acc, scale, old);
+            write_sum<EVEN, ADD>(dw + (int64_t)key_at[j] * d, c - shift_of<EVEN>(key_at[j], d), d, acc, scale, old);
         }
         __syncthreads();
     }
@@ -661,7 +709,7 @@ Plan make_plan(int64_t T, int32_t d, int32_t V)
     p.parts = (int32_t)((T + part - 1) / part);
     p.piece = T <= 4096 ? 8 : T <= 32768 ? 16 : T <= 131072 ? 32 : 64;
     p.pieces = (T + p.piece - 1) / p.piece;
-    p.pitch = (d + 7) / 8 * 8;
+    p.pitch = (d % 8 ? d + 7 : d) / 8 * 8 + (d % 8 ? 8 : 0);         // whole pieces that a row can touch
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += round_up(bytes, 256); return at; };
     p.o_list[0] = take((size_t)T * sizeof(uint2));
@@ -674,14 +722,15 @@ Plan make_plan(int64_t T, int32_t d, int32_t V)
     return p;
 }
 
-template <typename ROWS, typename YT> cudaError_t lookup_rows(const LookupArgs &a, const ROWS &rows, cudaStream_t s)
+template <typename YT, typename ROWS> cudaError_t lookup_even(const LookupArgs &a, const ROWS &rows, cudaStream_t s)
 {
-    if (a.d % 8 == 0) {
-        const int32_t segs = (a.d + 1023) / 1024;
-        const int64_t blocks = (a.T * segs + kThreads / 32 - 1) / (kThreads / 32);
-        if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-        return launch_pdl(lookup_kernel<ROWS, YT>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, rows, segs);
-    }
+    const int32_t segs = (a.d + 1023) / 1024;
+    const int64_t blocks = (a.T * segs + kThreads / 32 - 1) / (kThreads / 32);
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_pdl(lookup_kernel<ROWS, YT>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, rows, segs);
+}
+template <typename YT, typename ROWS> cudaError_t lookup_odd(const LookupArgs &a, const ROWS &rows, cudaStream_t s)
+{
     const int64_t blocks = (a.T * a.d + kThreads * 8 - 1) / (kThreads * 8);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     return launch_pdl(lookup_odd_kernel<ROWS, YT>, dim3((unsigned)blocks), dim3(kThreads), 0, s, a, rows);
@@ -690,16 +739,19 @@ template <typename WT, typename YT> cudaError_t lookup_typed(const LookupArgs &a
 {
     if (a.table) {
         const WT *table = static_cast<const WT *>(a.table);
-        return lookup_rows<DenseRows<WT>, YT>(a, DenseRows<WT>{table, table + (int64_t)a.V * a.d, a.d, a.d % 8 == 0, a.scale}, s);
+        const WT *end = table + (int64_t)a.V * a.d;
+        return a.d % 8 == 0 ? lookup_even<YT>(a, DenseRows<WT, true>{table, end, a.d, a.scale}, s)
+                            : lookup_odd<YT>(a, DenseRows<WT, false>{table, end, a.d, a.scale}, s);
     }
     const int32_t rows = a.q % a.d == 0 ? (int32_t)(a.q / a.d) : 0;
-    return lookup_rows<TiledRows, YT>(a, TiledRows{a.tile, a.alpha, a.q, (a.q + 31) / 32, a.d, rows, a.per_tile, a.scale}, s);
+    const TiledRows tiled = {a.tile, a.alpha, a.q, (a.q + 31) / 32, a.d, rows, a.per_tile, a.scale};
+    return a.d % 8 == 0 ? lookup_even<YT>(a, tiled, s) : lookup_odd<YT>(a, tiled, s);
 }
 
 template <typename GT, typename WT, int NP, bool EVEN, bool ADD>
 cudaError_t sum_pieces(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
 {
-    const int32_t segs = (a.d + 256 * NP - 1) / (256 * NP);
+    const int32_t segs = (p.pitch + 256 * NP - 1) / (256 * NP);
     const int64_t blocks = (p.pieces * segs + kThreads / 32 - 1) / (kThreads / 32);
     if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
     return launch_pdl(sum_kernel<GT, WT, NP, EVEN, ADD>, dim3((unsigned)blocks), dim3(kThreads), 0, s, list, a.T, a.V, a.d, p.piece, p.pieces, segs, a.scale,
@@ -711,11 +763,11 @@ cudaError_t sums(const GradArgs &a, const Plan &p, const uint2 *list, float *par
     // the more columns to a warp the less a row costs, while there are warps for every SM
     const int64_t warps = (int64_t)sm_count() * 12;
     cudaError_t e;
-    if (a.d > 512 && p.pieces * ((a.d + 1023) / 1024) >= warps) e = sum_pieces<GT, WT, ADD ? 2 : 4, EVEN, ADD>(a, p, list, partial, s);
+    if (a.d > 512 && p.pieces * ((a.d + 1023) / 1024) >= warps) e = sum_pieces<GT, WT, ADD || !EVEN ? 2 : 4, EVEN, ADD>(a, p, list, partial, s);
     else if (a.d > 256 && p.pieces * ((a.d + 511) / 512) >= warps) e = sum_pieces<GT, WT, 2, EVEN, ADD>(a, p, list, partial, s);
     else e = sum_pieces<GT, WT, 1, EVEN, ADD>(a, p, list, partial, s);
     if (e != cudaSuccess || p.pieces == 1) return e;
-    const int32_t segs = (a.d + 255) / 256;
+    const int32_t segs = (p.pitch + 255) / 256;
     return launch_pdl(join_kernel<WT, EVEN, ADD>, dim3((unsigned)((p.pieces + kThreads / 32 - 1) / (kThreads / 32)), (unsigned)segs), dim3(kThreads), 0, s,
                       list, a.T, a.V, a.d, p.piece, p.pieces, a.scale, static_cast<WT *>(a.dw), static_cast<const float *>(partial), p.pitch);
 }

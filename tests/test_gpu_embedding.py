@@ -82,7 +82,7 @@ def check_gradient(ids, dy, V, scale, padding, dw_dtype, before, got):
     assert torch.equal(got[alone], before[alone] if before is not None else torch.zeros_like(got[alone]))
 
 
-GRADS = [(1, 1, 1), (7000, 900, 501), (8192, 300, 30), (8193, 70000, 24), (33, 5, 1003), (1, 70000, 64), (5, 3, 9), (40, 1000, 256), (300, 50, 257), (1024, 5000, 64), (1025, 1023, 40), (2049, 1024, 8), (4097, 65535, 72),
+GRADS = [(1, 1, 1), (6000, 40, 1021), (20000, 700, 333), (9, 3, 7), (40, 2, 2050), (7000, 900, 501), (8192, 300, 30), (8193, 70000, 24), (33, 5, 1003), (1, 70000, 64), (5, 3, 9), (40, 1000, 256), (300, 50, 257), (1024, 5000, 64), (1025, 1023, 40), (2049, 1024, 8), (4097, 65535, 72),
          (5000, 65536, 264), (9000, 200000, 33), (40000, 1500, 16), (140000, 3000, 8), (200000, 300000, 8)]
 
 
