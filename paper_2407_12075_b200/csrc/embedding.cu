@@ -494,8 +494,9 @@ __global__ void __launch_bounds__(kThreads)
 sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, int32_t segs, float scale,
            const GT *__restrict__ dy, WT *dw, float *__restrict__ partial, int32_t pitch)
 {
-    // rows of dy loaded before the first is added, with the rows of dw that sums beginning there will be added to
-    constexpr int kAhead = ADD ? 4 : NP == 1 ? 8 : sizeof(GT) == 2 && EVEN ? 8 / NP * 2 : 8 / NP;
+    // Rows of dy loaded before the first is added, with the rows of dw that sums beginning there will be added to: more of them hide more of
+    // each load and leave fewer warps to an SM (us, with 2 / 4 / 8: 16384 x 2048 bf16 added 65 / 64 / 73, 16384 x 2047 98 / 114 / 223).
+    constexpr int kAhead = NP == 1 ? (EVEN || sizeof(GT) == 4 ? 4 : 2) : sizeof(GT) == 2 ? 8 / NP * 2 : 8 / NP;
     pdl_wait();
     const int lane = threadIdx.x & 31;
     const int64_t w = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
@@ -760,12 +761,13 @@ cudaError_t sum_pieces(const GradArgs &a, const Plan &p, const uint2 *list, floa
 template <typename GT, typename WT, bool EVEN, bool ADD>
 cudaError_t sums(const GradArgs &a, const Plan &p, const uint2 *list, float *partial, cudaStream_t s)
 {
-    // The more columns to a warp the less a row costs, while there are warps for every SM and registers for the rows on their way.  With dw's
-    // rows beside them one piece to a lane is fastest (us, one / two pieces: 16384 x 2048 bf16 64 / 67, 16384 x 2047 114 / 181).
+    // The more columns to a warp the less a row costs, while there are warps for every SM and registers for the rows on their way.  Odd rows,
+    // and sums with dw's rows beside them, are fastest with one piece to a lane (us, one / two pieces: dense 16384 x 2047 bf16 104 / 128,
+    // added 98 / 181, 16384 x 2048 added 64 / 67).
     const int64_t warps = (int64_t)sm_count() * 12;
     cudaError_t e = cudaErrorNotReady;
-    if constexpr (!ADD) {
-        if (a.d > 512 && p.pieces * ((a.d + 1023) / 1024) >= warps) e = sum_pieces<GT, WT, EVEN ? 4 : 2, EVEN, ADD>(a, p, list, partial, s);
+    if constexpr (EVEN && !ADD) {
+        if (a.d > 512 && p.pieces * ((a.d + 1023) / 1024) >= warps) e = sum_pieces<GT, WT, 4, EVEN, ADD>(a, p, list, partial, s);
         else if (a.d > 256 && p.pieces * ((a.d + 511) / 512) >= warps) e = sum_pieces<GT, WT, 2, EVEN, ADD>(a, p, list, partial, s);
     }
     if (e == cudaErrorNotReady) e = sum_pieces<GT, WT, 1, EVEN, ADD>(a, p, list, partial, s);
