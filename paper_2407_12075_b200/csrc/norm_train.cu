@@ -475,7 +475,7 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
             read8(gamma + i * 256, w);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                h[i][e] = mul(add(h[i][e], mu), rs);                  // of a masked column: times a g of zero
+                h[i][e] = mul(add(h[i][e], mu), rs);                  // of a column that the row does not have: meets a g of zero
                 db[i][e] = add(db[i][e], g[i][e]);
                 dg[i][e] = fma2(g[i][e], h[i][e], dg[i][e]);
                 g[i][e] = mul(g[i][e], w[e]);
@@ -484,7 +484,23 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
             }
         }
         const float2 p1 = split(s1), p2 = split(s2);
-        float t1 = warp_sum<SUB>(p1.x + p1.y), t2 = warp_sum<SUB>(p2.x + p2.y);
+        float t1 = p1.x + p1.y, t2 = p2.x + p2.y;
+        if (!(fabsf(t2) <= 3.4028235e38f)) {                          // where -mean rstd is beyond all floats, columns that the row lacks gave NaN
+            Pair only = both(0.0f);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                Pair c[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) c[e] = mul(g[i][e], h[i][e]);
+                Signs(l.mask[i]).keep(c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) only = add(only, c[e]);
+            }
+            const float2 p = split(only);
+            t2 = p.x + p.y;
+        }
+        t1 = warp_sum<SUB>(t1);
+        t2 = warp_sum<SUB>(t2);
         if (SUB == 32 && sh.warps > 1) {
             const float2 *all = part[turn] + l.group * sh.warps;
             if (l.lane == 0) part[turn][threadIdx.x >> 5] = make_float2(t1, t2);
