@@ -460,6 +460,7 @@ backward_kernel(const BackwardArgs a, const Shape sh, float *__restrict__ partia
         const bool here = SUB == 32 || k < own;
         const Pair mu = both(-mu_next), rs = both(rs_next);
         if (k + 1 < own) { mean += l.row_step; rstd += l.row_step; mu_next = *mean; rs_next = *rstd; }
+        else if (SUB < 32) mu_next = rs_next = 0.0f;                  // behind the last row h is to be 0: the one before may have an infinite one
         asm volatile("cp.async.wait_group %0;" :: "n"(R::kStages - 2) : "memory");
         const char *from = ring + slot * R::kBytes;
         Pair g[NP][4], h[NP][4], s1 = both(0.0f), s2 = both(0.0f);
