@@ -259,8 +259,10 @@ int tbn_layernorm_bwd(const void *dy, int dy_dtype, const void *x, int x_dtype, 
  *   can be replayed with other values; a step below 1 counts as 1.  grad_scale: one float on the device, or NULL for 1; where it is
  *   infinite or NaN nothing is changed by the call.  0 <= beta1, beta2 < 1, eps >= 1e-12, lr finite.
  * tbn_grad_norm: norm = sqrt(sum over all tensors' grad^2) (64-bit sums in a fixed order; a norm below 2^-100 is 0); scale = max_norm / norm where norm >
- *   max_norm, else 1; NaN where the norm is infinite or NaN, which makes tbn_adamw_step leave everything as it is.  norm, scale: one
- *   float each or NULL.  Only grad, n and grad_dtype are read.  workspace: tbn_grad_norm_workspace_bytes(count) bytes.
+ *   max_norm, else 1.  Where a gradient is infinite or NaN, norm is too and scale is NaN, which makes tbn_adamw_step leave everything as it
+ *   is.  Both follow from the 64-bit norm: finite gradients whose norm is no float give norm = infinity and the finite scale, and the step
+ *   is taken, so that scale, not norm, says whether one is left out.  norm, scale: one float each or NULL.  Only grad, n and grad_dtype
+ *   are read.  workspace: tbn_grad_norm_workspace_bytes(count) bytes.
  * tbn_adamw_unpack: the values of 8-bit states: m_out[i], v_out[i] (HOST arrays of device pointers to n floats; an array or an
  *   entry may be NULL).
  */

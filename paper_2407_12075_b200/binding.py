@@ -900,7 +900,8 @@ def tbn_adamw_tensors(params, grads, m, v, m_scale=None, v_scale=None, copies=No
 
 def tbn_grad_norm(tensors: AdamWTensors, max_norm: float, workspace: torch.Tensor | None = None):
     """Global norm of the gradients and the factor that brings it down to max_norm: (norm [1], scale [1]), on the device.  scale goes
-    to tbn_adamw_step as it is; it is NaN, and the step leaves everything as it is, where the norm is not finite."""
+    to tbn_adamw_step as it is; it is NaN, and the step leaves everything as it is, where a gradient is not finite.  (A norm of finite
+    gradients that is beyond all floats reads infinity; its scale is finite, and the step is taken.)"""
     device = tensors.device
     norm = torch.empty(1, dtype=torch.float32, device=device)
     scale = torch.empty(1, dtype=torch.float32, device=device)

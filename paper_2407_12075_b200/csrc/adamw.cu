@@ -463,7 +463,7 @@ step_kernel(const __grid_constant__ Table<N> tab, const __grid_constant__ Coef h
     }
     __syncthreads();
     const Coef c = shared;
-    if (!(fabsf(c.gs) <= 3.4028235e38f)) return;                      // gradients without a finite norm: no step
+    if (!(fabsf(c.gs) <= 3.4028235e38f)) return;                      // a gradient that is not finite: no step
     for (int64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
         const Desc &d = find(tab, chunk);
         int64_t base = ((chunk - d.chunk0) * kWarps + (threadIdx.x >> 5)) * tab.per * kBlock;
