@@ -632,7 +632,7 @@ Shape shape_of(int32_t d, int most)
 {
     Shape s;
     s.classes = d % 8 == 0 ? 1 : d % 4 == 0 ? 2 : d % 2 == 0 ? 4 : 8;
-    const int32_t pieces = (d + (s.classes > 1 ? 7 : 0) + 7) / 8;     // that a row can touch
+    const int32_t pieces = (d + 8 - 8 / s.classes + 7) / 8;           // that a row can touch: it begins up to 0, 4, 6 or 7 columns inside of one
     s.lng = pieces > kMaxWarps * 32 * 4;
     s.np = 4; s.warps = kMaxWarps;
     int32_t least = 0x7fffffff;
