@@ -170,12 +170,6 @@ __device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d
 }
 
 // Elements of a lane: first, first + stride, ... (eight in a row where the tensor is aligned, every 32nd otherwise).
-template <typename T> __device__ __forceinline__ void load_some(const T *p, bool vec, int cnt, float (&v)[8])
-{
-    if (vec) { unpack8(load8(p), v); return; }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 32 * e < cnt ? value_of(p[32 * e]) : 0.0f;
-}
 __device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat16 v) { return __bfloat16_as_ushort(v); }
 template <bool VEC, typename T> __device__ __forceinline__ void load_raw(const T *p, int cnt, Raw8<T> &r)

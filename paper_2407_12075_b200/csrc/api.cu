@@ -960,7 +960,7 @@ int tbn_embedding_tiled_fwd(const int64_t *ids, int64_t T, int32_t vocab, int32_
     if (T == 0) return TBN_OK;
     embed::LookupArgs a = {};
     a.ids = ids; a.T = T; a.d = d; a.V = vocab; a.padding = padding_idx; a.scale = scale;
-    a.tile = tile_bits; a.k = k; a.q = (int64_t)vocab * d / k; a.alpha = alpha; a.per_tile = alpha_mode == TBN_ALPHA_PER_TILE;
+    a.tile = tile_bits; a.q = (int64_t)vocab * d / k; a.alpha = alpha; a.per_tile = alpha_mode == TBN_ALPHA_PER_TILE;
     a.y = y; a.y_dtype = y_dtype;
     return embed::lookup(a, static_cast<cudaStream_t>(stream));
 }

@@ -15,7 +15,6 @@ struct LookupArgs {
     const void *table;                      // V x d, or null with a tiled table
     int table_dtype;
     const uint32_t *tile;
-    int32_t k;
     int64_t q;
     const float *alpha;
     int per_tile;

@@ -55,11 +55,6 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8])
                  :: "l"(p), "r"(pack_bf16(v[0], v[1])), "r"(pack_bf16(v[2], v[3])), "r"(pack_bf16(v[4], v[5])), "r"(pack_bf16(v[6], v[7]))
                  : "memory");
 }
-// Whether rows of `pitch` values from p on all begin where an access of eight values may.
-template <typename T> inline bool aligned8(const void *p, int64_t pitch = 0)
-{
-    return (reinterpret_cast<uintptr_t>(p) % (8 * sizeof(T))) == 0 && pitch % 8 == 0;
-}
 
 // Two fp32 values to an instruction, where the rate at which instructions issue is what bounds a kernel.  (The compiler may join a
 // product and the sum that takes it to one rounding.)
