@@ -77,7 +77,8 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
 
 __host__ __device__ inline void set_coef(Coef &c, double lr, double beta1, double beta2, int64_t step, uint64_t seed)
 {
-    const double t = (double)(step < 1 ? 1 : step);
+    if (step < 1) step = 1;                                           // for the random numbers too
+    const double t = (double)step;
     c.lr = lr;
     c.step_size = (float)(lr / (1.0 - pow(beta1, t)));
     c.inv_sqrt_bc2 = (float)(1.0 / sqrt(1.0 - pow(beta2, t)));
