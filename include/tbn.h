@@ -174,7 +174,7 @@ int tbn_tile_bwd(const float *G, const uint32_t *tile_bits, const float *alpha, 
  *   classes within |lse| 2^-21 of lse have q = 1.
  * workspace: tbn_linear_xent_workspace_bytes(..., backward) / tbn_linear_distill_workspace_bytes(..., backward) bytes, with
  *   backward = 0 or 1 for the call it is meant for.  T == 0: the forward is a no-op, the backward writes zeros to dw and dbias.
- * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1024, or x or w of more than 2^38 elements (rows counted in whole
+ * Errors: as tbn_linear_fwd; T, vocab or in_f beyond 2^31 - 1025, or x or w of more than 2^38 elements (rows counted in whole
  *   64s): TBN_ERR_UNSUPPORTED.
  */
 size_t tbn_linear_xent_workspace_bytes(int64_t T, int32_t in_f, int32_t vocab, int dtype, int backward);
@@ -209,7 +209,7 @@ int tbn_linear_distill_bwd(const void *x, const void *w, int dtype, int64_t T, i
  *   fp32 in the order of the tokens in pieces that T decides, and rounded once.  With accumulate rows that no token names are
  *   neither read nor written: a tied head's dw takes the embedding's part this way.  workspace:
  *   tbn_embedding_bwd_workspace_bytes(T, d, vocab) bytes.  T == 0: zeros, or with accumulate a no-op.
- * Errors: vocab * d not a multiple of k: TBN_ERR_SHAPE.  T, vocab beyond 2^31 - 1024 or d beyond 2^23: TBN_ERR_UNSUPPORTED.
+ * Errors: vocab * d not a multiple of k: TBN_ERR_SHAPE.  T, vocab beyond 2^31 - 1025 or d beyond 2^23: TBN_ERR_UNSUPPORTED.
  */
 int tbn_embedding_fwd(const int64_t *ids, int64_t T, const void *table, int table_dtype, int32_t vocab, int32_t d, int64_t padding_idx,
                       float scale, void *y, int y_dtype, void *stream);
@@ -231,6 +231,7 @@ int tbn_embedding_bwd(const int64_t *ids, int64_t T, const void *dy, int dy_dtyp
  *   the residual.  dgamma, dbeta: d floats or NULL.  All are overwritten; sums are fp32 in an order that T and d decide.
  *   workspace: tbn_layernorm_bwd_workspace_bytes(T, d) bytes (0 for a few rows); not needed when dgamma and dbeta are NULL.
  *   T == 0: zeros.
+ * T beyond 2^31 - 1025 or d beyond 2^23: TBN_ERR_UNSUPPORTED.
  * No output may overlap an input.  A row that holds an infinity or a NaN has NaN in its y and dx and in dgamma; no other row is
  * affected. */
 int tbn_layernorm_train_fwd(const void *x, const void *residual, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *beta, float eps,
