@@ -68,6 +68,7 @@ struct Coef {
     uint32_t key;
 };
 
+// A published 32-bit integer hash of two multiplications: C. Wellons, "Prospecting for Hash Functions" (2018), its variant of least bias.
 __host__ __device__ __forceinline__ uint32_t mix(uint32_t x)
 {
     x ^= x >> 16; x *= 0x7feb352du;

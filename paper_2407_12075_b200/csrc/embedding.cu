@@ -402,7 +402,7 @@ clear_kernel(uint32_t *__restrict__ count, int64_t n)
 
 // Few tokens are sorted in one launch, by counting: a token goes behind all with a smaller id and those before it with its own.  A thread
 // block takes 32 tokens, one to a lane, and its warps a share of the list each; T^2 comparisons, at two instructions for 32 of them, spread over
-// the SMs (4096 tokens: 7.8 us; one thread block sorting by digits took 13.8, the launches above 19).
+// the SMs (4096 tokens: 5.9 us within a step; by itself 7.8, where one thread block sorting by digits took 13.8 and the launches above 19).
 constexpr int kRankTokens = 8192;
 __global__ void __launch_bounds__(kThreads)
 rank_kernel(const Sort s, const Fill f, unsigned rankers)
@@ -488,14 +488,17 @@ __device__ __forceinline__ void put_partial(float *row, int32_t c, const float (
 
 // A warp takes one piece of the sorted list and NP * 256 columns.  An id's tokens that begin and end in the piece are done with; what
 // comes from the piece before, or goes on in the next one, is written to `partial` ([piece][2][pitch]: first, last).  16384 x 2048 bf16 over
-// 50021 ids: 17 us (1024 columns to a warp; 256: 34); 4096 x 1024 added to fp32: 8 us (rows of dw read where a sum ends: 11).
+// 50021 ids: 23 us within a step, 17 by itself (1024 columns to a warp; with 256 34); 4096 x 1024 added to fp32: 6.4 and 8 (11 with rows of
+// dw read where a sum ends).
 template <typename GT, typename WT, int NP, bool EVEN, bool ADD>
 __global__ void __launch_bounds__(kThreads)
 sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int32_t piece, int64_t pieces, int32_t segs, float scale,
            const GT *__restrict__ dy, WT *dw, float *__restrict__ partial, int32_t pitch)
 {
     // Rows of dy loaded before the first is added, with the rows of dw that sums beginning there will be added to: more of them hide more of
-    // each load and leave fewer warps to an SM (us, with 2 / 4 / 8: 16384 x 2048 bf16 added 65 / 64 / 73, 16384 x 2047 98 / 114 / 223).
+    // each load and leave fewer warps to an SM (us, with 2 / 4 / 8: 16384 x 2048 bf16 added 65 / 64 / 73).  Odd bf16 rows have two pieces on
+    // their way for each (us, with 2 / 4: added 16384 x 2047 98 / 114, 32768 x 1023 108 / 133, 9000 x 1500 46 / 54, 32768 x 63 53 / 54; as a
+    // whole table 104 / 112, 98 / 96, 84 / 84, 50 / 49).
     constexpr int kAhead = NP == 1 ? (EVEN || sizeof(GT) == 4 ? 4 : 2) : sizeof(GT) == 2 ? 8 / NP * 2 : 8 / NP;
     pdl_wait();
     const int lane = threadIdx.x & 31;
@@ -591,7 +594,8 @@ sum_kernel(const uint2 *__restrict__ list, int64_t T, int32_t V, int32_t d, int3
 }
 
 // The ids whose tokens lie in several pieces.  A warp looks at one piece: does its last id begin in it and go on?  Short runs it
-// adds up by itself, long ones are shared by the block's warps.  A chain of dependent reads (list, pieces, sums): 7 to 11 us.
+// adds up by itself, long ones are shared by the block's warps.  A chain of dependent reads (list, pieces, sums): 4 us at 4096 x 1024, 6 to 11
+// above 8192 tokens.
 constexpr int kAlone = 16;
 template <typename WT, bool EVEN, bool ADD>
 __global__ void __launch_bounds__(kThreads)
