@@ -233,7 +233,7 @@ int tbn_embedding_bwd(const int64_t *ids, int64_t T, const void *dy, int dy_dtyp
  *   T == 0: zeros.
  * T beyond 2^31 - 1025 or d beyond 2^23: TBN_ERR_UNSUPPORTED.
  * No output may overlap an input.  A row that holds an infinity or a NaN has NaN in its y and dx and in dgamma; no other row is
- * affected. */
+ * affected.  A finite row whose sum is beyond the largest float may have NaN too; one whose sum of squared deviations is has rstd = 0 and y = beta. */
 int tbn_layernorm_train_fwd(const void *x, const void *residual, int x_dtype, int64_t T, int32_t d, const float *gamma, const float *beta, float eps,
                             void *sum, void *y, int y_dtype, float *mean, float *rstd, void *stream);
 size_t tbn_layernorm_bwd_workspace_bytes(int64_t T, int32_t d);
